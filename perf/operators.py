@@ -87,12 +87,12 @@ def _scores(c, g):
 def _rows_of(c, g, choices):
     """One of `choices` for each row."""
     at = torch.randint(len(choices), (c["rows"],), generator=g, device="cuda")
-    return torch.tensor(choices, device="cuda")[at]
+    return torch.tensor(choices, dtype=torch.int32 if type(choices[0]) is int else torch.float32, device="cuda")[at]
 
 
 def _filters(c, g):
     rows, kind = c["rows"], c["filters"]
-    full = lambda v: torch.full((rows,), v, device="cuda")  # noqa: E731
+    full = lambda v: torch.full((rows,), v, dtype=torch.int32 if type(v) is int else torch.float32, device="cuda")  # noqa: E731
     if kind == "usual":
         return dict(temperature=full(0.8), top_k=full(50), top_p=full(0.95))
     if kind == "top_p":
