@@ -200,6 +200,55 @@ qsv_status qsv_reset_fidelity(qsv_ctx* ctx, const qsv_circuit* c, const float* p
  * (1 - 2 bit_q); entries < 0 (no valid outcome) are skipped, a row without valid shots gives 0. */
 qsv_status qsv_shot_expz(qsv_ctx* ctx, const long long* samples_dev, int64_t shots, float* out_dev);
 
+/* What a row of outcomes is given as: scores (natural logarithms of weights, up to a constant), probabilities (as
+ * QSV_M_PROBS and QSV_M_MARGINAL write them, up to a factor), or the context's state, whose probabilities are taken as
+ * QSV_M_PROBS would write them. */
+typedef enum {
+    QSV_S_F32 = 1,    /* scores, IEEE 32 bits */
+    QSV_S_F16 = 2,    /* scores, IEEE 16 bits */
+    QSV_S_BF16 = 3,   /* scores, the upper half of a float32 */
+    QSV_S_PROBS = 4,  /* probabilities, float32 */
+    QSV_S_STATE = 5   /* the context's state: scores_dev NULL, rows = batch, cols = 2^n, row_stride ignored */
+} qsv_scores_kind;
+
+/* Outcomes drawn from rows of scores, probabilities or amplitudes after temperature, min-p, top-k and top-p, from the
+ * caller's uniforms.  v_k is the value of outcome k, m the highest one.  Masked outcomes (scores: -inf or NaN;
+ * probabilities: NaN and all that are not positive) are never drawn; the type's lowest finite value is an ordinary score.
+ * The order is v descending, the lowest index first among equals (-0 equals 0), and e_k = exp((v_k - m) / T) for scores,
+ * (v_k / m)^(1 / T) for probabilities, 1 where v_k = m (which may be +inf).  Then, one after the other:
+ *   temperature  T, finite, >= 0; T = 0 keeps the first outcome alone and ends the list;
+ *   min_p        keeps e_k >= min_p, in 0..1 (0: all);
+ *   top_k        keeps the first top_k of these (0: all);
+ *   top_p        >= 0, with w_k = rint(e_k 2^S), S = min(51, 62 - ceil(log2 cols)), W the sum of w over these and
+ *                H = ceil(rint(top_p 2^31) W / 2^31): keeps an outcome while the weights before it in the order sum to
+ *                less than H, and the first one always (top_p >= 1: all).
+ * The draw is QSV_M_SAMPLE's: W' the sum of w over what is left, r = floor(u 2^53), t = floor(r W' / 2^53), the smallest k
+ * whose running sum in the order of the INDEX exceeds t.  e_k is taken in float64, so a result can differ from the
+ * definition only where a value lies within about 2^-48 of a border; sums are of whole numbers, so a call's results do not
+ * depend on how its work is split.  A row without an outcome, or with a parameter out of its range (NaN too), gives -1 for
+ * every shot, logp -inf and kept 0; a uniform outside [0, 1) gives -1 and -inf for its shot. */
+typedef struct {
+    int32_t kind;                 /* qsv_scores_kind */
+    int32_t reserved;             /* must be 0 */
+    const void* scores_dev;       /* row r starts at element r * row_stride; aligned to its element */
+    int64_t rows;                 /* 0..2^24; 0 is a no-op */
+    int64_t cols;                 /* 1..2^30 */
+    int64_t row_stride;           /* >= cols (any value for one row), in elements */
+    const float* temperature_dev; /* [rows] or NULL (1) */
+    const int32_t* top_k_dev;     /* [rows] or NULL (0) */
+    const float* top_p_dev;       /* [rows] or NULL (1) */
+    const float* min_p_dev;       /* [rows] or NULL (0) */
+    const double* uniforms_dev;   /* float64 [rows][shots], values in [0, 1) */
+    int64_t shots;                /* >= 0, rows * shots <= 2^32 */
+    int64_t* out_dev;             /* int64 [rows][shots] */
+    float* logp_dev;              /* float32 [rows][shots] or NULL: ln(w_k / W') of the outcome drawn */
+    int32_t* kept_dev;            /* int32 [rows] or NULL: the number of outcomes left */
+} qsv_sample_req;
+
+/* Workspace size in bytes that qsv_sample needs for such rows, that of the plans included; 0 on bad arguments. */
+size_t qsv_sample_workspace_bytes(int64_t rows, int64_t cols);
+qsv_status qsv_sample(qsv_ctx* ctx, const qsv_sample_req* req);
+
 /* Expectation value of a Pauli string on the current state (task statement: "measurement
  * (... <Z> ...)", widened to X and Y): P = product over qubits of X (bit set in xmask), Y (ymask)
  * or Z (zmask), identity elsewhere; the masks must not overlap and name qubits < n_qubits.

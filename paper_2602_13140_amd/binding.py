@@ -37,6 +37,16 @@ class qsv_loss(ctypes.Structure):
 
 
 QSV_LOSS_TRASH, QSV_LOSS_MSE_Z = 1, 2
+QSV_S_F32, QSV_S_F16, QSV_S_BF16, QSV_S_PROBS, QSV_S_STATE = range(1, 6)
+
+
+class qsv_sample_req(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("reserved", ctypes.c_int32), ("scores_dev", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("temperature_dev", ctypes.c_void_p), ("top_k_dev", ctypes.c_void_p),
+                ("top_p_dev", ctypes.c_void_p), ("min_p_dev", ctypes.c_void_p),
+                ("uniforms_dev", ctypes.c_void_p), ("shots", ctypes.c_int64), ("out_dev", ctypes.c_void_p),
+                ("logp_dev", ctypes.c_void_p), ("kept_dev", ctypes.c_void_p)]
 
 
 class QsvError(RuntimeError):
@@ -99,6 +109,10 @@ def load():
     L.qsv_reset_fidelity.argtypes = [vp, ctypes.POINTER(qsv_circuit), vp, vp, ctypes.c_uint64, vp, i64, vp]
     L.qsv_shot_expz.restype = i32
     L.qsv_shot_expz.argtypes = [vp, vp, i64, vp]
+    L.qsv_sample_workspace_bytes.restype = ctypes.c_size_t
+    L.qsv_sample_workspace_bytes.argtypes = [i64, i64]
+    L.qsv_sample.restype = i32
+    L.qsv_sample.argtypes = [vp, ctypes.POINTER(qsv_sample_req)]
     L.qsv_pauli_expect.restype = i32
     L.qsv_pauli_expect.argtypes = [vp, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint64, vp]
     L.qsv_plan_describe.restype = i64
@@ -139,6 +153,10 @@ def qsv_grad_workspace_bytes(n, batch, circ):
     return int(load().qsv_grad_workspace_bytes(n, batch, ctypes.byref(circ)))
 
 
+def qsv_sample_workspace_bytes(rows, cols):
+    return int(load().qsv_sample_workspace_bytes(rows, cols))
+
+
 def qsv_plan_describe(circ, n, batch=1, inverse=0, tile_log2=0):
     L = load()
     need = L.qsv_plan_describe(ctypes.byref(circ), n, batch, inverse, tile_log2, None, 0)
@@ -151,6 +169,23 @@ def qsv_plan_describe(circ, n, batch=1, inverse=0, tile_log2=0):
 
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+_TYPE_OF = {QSV_S_F32: "torch.float32", QSV_S_F16: "torch.float16", QSV_S_BF16: "torch.bfloat16", QSV_S_PROBS: "torch.float32"}
+
+
+def _rows(t, kind):
+    """Rows of scores: [rows][cols] of the kind's type, values of a row next to each other, any row stride."""
+    assert t.is_cuda and t.dim() == 2 and str(t.dtype) == _TYPE_OF[kind] and (t.shape[1] == 1 or t.stride(1) == 1)
+    return t
+
+
+def _flat(t, dtype, *shape):
+    """The address of a contiguous tensor of this type and shape; None stays None."""
+    if t is None:
+        return None
+    assert t.is_cuda and str(t.dtype) == "torch." + dtype and tuple(t.shape) == shape and t.is_contiguous(), (dtype, shape)
+    return t.data_ptr()
 
 
 class Context:
@@ -238,6 +273,27 @@ class Context:
 
     def qsv_shot_expz(self, samples, out):
         self._check(self.L.qsv_shot_expz(self.h, _ptr(samples), samples.shape[1], _ptr(out)))
+
+    def qsv_sample(self, kind, out, uniforms, scores=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                   logp=None, kept=None):
+        r = qsv_sample_req()
+        r.kind = kind
+        if kind == QSV_S_STATE:
+            assert scores is None
+            r.rows, r.cols = self.batch, 1 << self.n
+        else:
+            s = _rows(scores, kind)
+            r.scores_dev, r.rows, r.cols, r.row_stride = s.data_ptr(), s.shape[0], s.shape[1], s.stride(0)
+        r.shots = uniforms.shape[1]
+        r.temperature_dev = _flat(temperature, "float32", r.rows)
+        r.top_k_dev = _flat(top_k, "int32", r.rows)
+        r.top_p_dev = _flat(top_p, "float32", r.rows)
+        r.min_p_dev = _flat(min_p, "float32", r.rows)
+        r.uniforms_dev = _flat(uniforms, "float64", r.rows, r.shots)
+        r.out_dev = _flat(out, "int64", r.rows, r.shots)
+        r.logp_dev = _flat(logp, "float32", r.rows, r.shots)
+        r.kept_dev = _flat(kept, "int32", r.rows)
+        self._check(self.L.qsv_sample(self.h, ctypes.byref(r)))
 
     def qsv_pauli_expect(self, out, xmask=0, ymask=0, zmask=0):
         self._check(self.L.qsv_pauli_expect(self.h, xmask, ymask, zmask, _ptr(out)))

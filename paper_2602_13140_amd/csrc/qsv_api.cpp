@@ -15,6 +15,8 @@
 
 #include "qsv.h"
 #include "qsv_kernels.h"
+#include "qsv_requests.h"
+#include "qsv_scores.h"
 #include "qsv_lower.h"
 #include "qsv_plan.h"
 
@@ -1047,6 +1049,41 @@ qsv_status qsv_measure_static(qsv_ctx* ctx, const qsv_measure_req* req) {
     QSV_HIP(ctx, static_scratch(ctx->device, &fixed), "address of the fixed scratch array");
     Arena ar(fixed, kStaticScratchBytes);
     return measure_impl(ctx, req, ar);
+}
+
+// The workspace of qsv_sample behind the plans' region.
+size_t qsv_sample_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || rows > kMostRows || cols < 1 || cols > kMostCols) return 0;
+    return kOpsRegion + align_up(sample_scratch_bytes(rows, cols));
+}
+
+qsv_status qsv_sample(qsv_ctx* ctx, const qsv_sample_req* req) {
+    if (!ctx) return QSV_ERR_INVALID_ARG;
+    if (const char* why = check_sample(req, ctx->n, ctx->batch)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    if (req->rows == 0 || (req->shots == 0 && !req->kept_dev)) return QSV_OK;
+    qsv_status st = bind_device(ctx);
+    if (st != QSV_OK) return st;
+    const bool state = req->kind == QSV_S_STATE;
+    SampleArgs a{};
+    a.scores = state ? ctx->state : req->scores_dev;
+    a.rows = req->rows;
+    a.stride = state ? req->cols : req->rows > 1 ? req->row_stride : req->cols;
+    a.cols = (uint32_t)req->cols;
+    a.bits = std::min(51, 62 - ceil_log2_i64(req->cols));
+    a.temperature = req->temperature_dev;
+    a.top_k = req->top_k_dev;
+    a.top_p = req->top_p_dev;
+    a.min_p = req->min_p_dev;
+    a.uniforms = req->uniforms_dev;
+    a.shots = req->shots;
+    a.out = (long long*)req->out_dev;
+    a.logp = req->logp_dev;
+    a.kept = req->kept_dev;
+    Arena ar(ctx);
+    void* scratch = ar.take(sample_scratch_bytes(req->rows, req->cols));
+    if (!scratch) return ws_fail(ctx, ar, "qsv_sample");
+    QSV_HIP(ctx, launch_sample_scores(req->kind, a, scratch, ctx->stream), "sample scores");
+    return QSV_OK;
 }
 
 qsv_status qsv_pauli_expect(qsv_ctx* ctx, uint64_t xmask, uint64_t ymask, uint64_t zmask, float* out_dev) {

@@ -1,0 +1,42 @@
+// Checks of the requests on rows of scores: host only, no device is asked.
+#pragma once
+#include <cstdint>
+
+#include "qsv.h"
+
+namespace qsv {
+
+constexpr int64_t kMostRows = (int64_t)1 << 24, kMostCols = (int64_t)1 << 30, kMostShots = (int64_t)1 << 32,
+                  kMostStride = (int64_t)1 << 36;
+
+inline int score_bytes(int kind) { return kind == QSV_S_STATE ? 8 : kind == QSV_S_F16 || kind == QSV_S_BF16 ? 2 : 4; }
+
+// Rows of scores in memory: what is wrong with them, or NULL.
+inline const char* check_rows(int kind, const void* scores, int64_t rows, int64_t cols, int64_t stride) {
+    if (rows < 0 || rows > kMostRows) return "rows must be in 0..2^24";
+    if (cols < 1 || cols > kMostCols) return "cols must be in 1..2^30";
+    if (rows == 0) return nullptr;
+    if (!scores) return "scores_dev is NULL";
+    if ((uintptr_t)scores % score_bytes(kind)) return "scores_dev must be aligned to its element";
+    if (rows > 1 && (stride < cols || stride > kMostStride)) return "row_stride must be in cols..2^36";
+    return nullptr;
+}
+
+// What is wrong with a request of qsv_sample on a context of batch samples of n qubits, or NULL.
+inline const char* check_sample(const qsv_sample_req* q, int n, int64_t batch) {
+    if (!q) return "req is NULL";
+    if (q->reserved != 0) return "reserved must be 0";
+    if (q->kind < QSV_S_F32 || q->kind > QSV_S_STATE) return "unknown kind of scores";
+    if (q->kind == QSV_S_STATE) {
+        if (q->scores_dev) return "scores_dev must be NULL for the context's state";
+        if (q->rows != batch || q->cols != ((int64_t)1 << n)) return "the context's state has batch rows of 2^n outcomes";
+    } else if (const char* why = check_rows(q->kind, q->scores_dev, q->rows, q->cols, q->row_stride)) {
+        return why;
+    }
+    if (q->shots < 0 || q->shots > kMostShots || q->rows * q->shots > kMostShots)
+        return "shots must be >= 0 with rows * shots <= 2^32";
+    if (q->rows > 0 && q->shots > 0 && (!q->uniforms_dev || !q->out_dev)) return "uniforms_dev or out_dev is NULL";
+    return nullptr;
+}
+
+}  // namespace qsv

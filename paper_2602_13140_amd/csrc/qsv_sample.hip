@@ -1,0 +1,1076 @@
+// Outcomes drawn from rows of scores, probabilities or amplitudes after temperature, min-p, top-k and top-p.
+//
+// All filters cut one order: value descending, ties by the lowest index first.  So what is left of a row is known by a
+// cut (key, ne): everything above the key and the first ne, by index, of what equals it.  Keys are the values' bits made
+// to order as whole numbers, 16 of them for 16-bit scores.  A cut is found without sorting: a histogram over the distance
+// from the row's highest value (counts, and for top-p weights), then histograms over the keys of the one bin the cut falls
+// into, 11 bits at a time, until the bin is one key.
+//
+// Weights are whole numbers, rint(e 2^S) with e in 64 bits: their sums are the same in any order, so a call's results do
+// not depend on how its work was split or in which order atomics arrived.
+#include "qsv_scores.h"
+
+#include <hip/hip_fp16.h>
+
+#include <algorithm>
+
+namespace qsv {
+namespace {
+
+typedef unsigned long long u64;
+typedef unsigned u32;
+
+constexpr float kInf = __builtin_inff();
+constexpr u32 kAll = 0xffffffffu;      // a cut that keeps every outcome that equals its key
+
+template <int KIND> constexpr bool kLogs = KIND <= kScoreBF16;          // scores; else probabilities
+template <int KIND> constexpr bool kKeys16 = KIND == kScoreF16 || KIND == kScoreBF16;
+// the lowest key an outcome can have; masked ones have lower ones
+template <int KIND> constexpr u32 kLowest = KIND == kScoreF32 ? 0x00800000u : KIND == kScoreBF16 ? 0x0080u : KIND == kScoreF16 ? 0x0400u : 1u;
+
+// Masked values (NaN, -inf; of probabilities all that are not positive) as one value, -0 as 0.
+template <int KIND> __device__ __forceinline__ float clean(float v) {
+    if (kLogs<KIND>) return v > -kInf ? v + 0.f : -kInf;
+    return v > 0.f ? v : 0.f;
+}
+
+template <int KIND> __device__ __forceinline__ u32 key_of(float v) {
+    if (!kLogs<KIND>) return __float_as_uint(v);
+    if (KIND == kScoreF16) {
+        const u32 b = __half_as_ushort(__float2half_rn(v));
+        return (b & 0x8000u) ? b ^ 0xffffu : b | 0x8000u;
+    }
+    const u32 b = __float_as_uint(v);
+    const u32 k = b ^ ((u32)((int)b >> 31) | 0x80000000u);
+    return KIND == kScoreBF16 ? k >> 16 : k;
+}
+
+template <int KIND> __device__ __forceinline__ float value_of(u32 k) {
+    if (!kLogs<KIND>) return __uint_as_float(k);
+    if (KIND == kScoreF16) {
+        const u32 b = (k & 0x8000u) ? k ^ 0x8000u : k ^ 0xffffu;
+        return __half2float(__ushort_as_half((unsigned short)b));
+    }
+    const u32 f = KIND == kScoreBF16 ? k << 16 : k;
+    if (f & 0x80000000u) return __uint_as_float(f ^ 0x80000000u);
+    return __uint_as_float(KIND == kScoreBF16 ? (f ^ 0xffff0000u) : ~f);
+}
+
+// ---- rows ------------------------------------------------------------------------------------------------------------
+// A row is read four values a lane in aligned vectors: vector j holds the values 4 j - skew .. 4 j - skew + 3, where skew
+// values lie between the last aligned address and the row's start.  Vectors that reach over an end are read value by value.
+struct Row {
+    const char* p;
+    u32 cols, skew, vecs;
+};
+
+template <int KIND> __device__ __forceinline__ Row row_of(const SampleArgs& a, u64 r) {
+    constexpr int size = KIND == kScoreState ? 8 : kKeys16<KIND> ? 2 : 4;
+    Row w;
+    w.p = (const char*)a.scores + r * (u64)a.stride * size;
+    w.cols = a.cols;
+    w.skew = KIND == kScoreState ? 0u : (u32)(((uintptr_t)w.p / size) & 3u);
+    w.vecs = (w.cols + w.skew + 3u) >> 2;
+    return w;
+}
+
+template <int KIND> __device__ __forceinline__ float one_value(const Row& w, u32 k) {
+    if (KIND == kScoreState) {
+        const float2 z = ((const float2*)w.p)[k];
+        return __builtin_fmaf(z.y, z.y, z.x * z.x);     // the probability as every measurement has it
+    }
+    if (KIND == kScoreF16) return __half2float(((const __half*)w.p)[k]);
+    if (KIND == kScoreBF16) return __uint_as_float((u32)((const unsigned short*)w.p)[k] << 16);
+    return ((const float*)w.p)[k];
+}
+
+template <int KIND> __device__ __forceinline__ void load4(const Row& w, u32 j, float (&v)[4]) {
+    const long long first = 4ll * j - w.skew;
+    if (first >= 0 && first + 4 <= (long long)w.cols) {
+        if (KIND == kScoreState) {
+            const float4* q = (const float4*)(w.p + first * 8);
+            const float4 x = q[0], y = q[1];
+            v[0] = __builtin_fmaf(x.y, x.y, x.x * x.x);
+            v[1] = __builtin_fmaf(x.w, x.w, x.z * x.z);
+            v[2] = __builtin_fmaf(y.y, y.y, y.x * y.x);
+            v[3] = __builtin_fmaf(y.w, y.w, y.z * y.z);
+        } else if (kKeys16<KIND>) {
+            const uint2 x = *(const uint2*)(w.p + first * 2);
+            if (KIND == kScoreBF16) {
+                v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u);
+                v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
+            } else {
+                v[0] = __half2float(__ushort_as_half((unsigned short)x.x));
+                v[1] = __half2float(__ushort_as_half((unsigned short)(x.x >> 16)));
+                v[2] = __half2float(__ushort_as_half((unsigned short)x.y));
+                v[3] = __half2float(__ushort_as_half((unsigned short)(x.y >> 16)));
+            }
+        } else {
+            const float4 x = *(const float4*)(w.p + first * 4);
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = clean<KIND>(v[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const long long k = first + i;
+        v[i] = k >= 0 && k < (long long)w.cols ? clean<KIND>(one_value<KIND>(w, (u32)k)) : (kLogs<KIND> ? -kInf : 0.f);
+    }
+}
+
+// ---- weights ---------------------------------------------------------------------------------------------------------
+// 2^x for x <= 0, relative error below 2^-51; below 2^-200 that (nothing differs there: weights end at 2^-52).
+__device__ __forceinline__ double exp2_neg(double x) {
+    x = fmax(x, -200.0);
+    const double n = __builtin_rint(x);
+    const double f = (x - n) * 0.69314718055994530942;     // |f| <= 0.347: the series to f^13 / 13!
+    double s = 1.0 / 6227020800.0;
+    s = fma(s, f, 1.0 / 479001600.0);
+    s = fma(s, f, 1.0 / 39916800.0);
+    s = fma(s, f, 1.0 / 3628800.0);
+    s = fma(s, f, 1.0 / 362880.0);
+    s = fma(s, f, 1.0 / 40320.0);
+    s = fma(s, f, 1.0 / 5040.0);
+    s = fma(s, f, 1.0 / 720.0);
+    s = fma(s, f, 1.0 / 120.0);
+    s = fma(s, f, 1.0 / 24.0);
+    s = fma(s, f, 1.0 / 6.0);
+    s = fma(s, f, 0.5);
+    s = fma(s, f, 1.0);
+    s = fma(s, f, 1.0);
+    return __builtin_ldexp(s, (int)n);
+}
+
+// How a row's values become weights.
+struct Scale {
+    float m;           // the highest value
+    double md, c;      // scores: log2(e) / T; probabilities: 1 / T
+    double one;        // 2^S
+    float per_bin;     // scores: bins for a distance of 1 below m
+    bool t_one;
+    u32 kmax;
+};
+
+template <int KIND, int NB> __device__ __forceinline__ Scale scale_of(u32 kmax, float t, int bits) {
+    Scale s;
+    s.kmax = kmax;
+    s.m = value_of<KIND>(kmax);
+    s.md = (double)s.m;
+    s.c = (kLogs<KIND> ? 1.4426950408889634074 : 1.0) / (double)t;
+    s.one = __builtin_ldexp(1.0, bits);
+    s.t_one = t == 1.f;
+    s.per_bin = (float)(s.c * (double)NB / (double)(bits + 2));
+    return s;
+}
+
+template <int KIND> __device__ __forceinline__ double weight64(const Scale& s, float v) {
+    if (v == s.m) return 1.0;
+    if (kLogs<KIND>) return exp2_neg(((double)v - s.md) * s.c);
+    const double q = (double)v / s.md;
+    return s.t_one ? q : exp2_neg(log2(q) * s.c);
+}
+
+template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, float v) {
+    // adding 2^52 rounds to a whole number, which the low bits then hold
+    const double x = fma(weight64<KIND>(s, v), s.one, 4503599627370496.0);
+    return (u64)__double_as_longlong(x) & 0xfffffffffffffull;
+}
+
+// Bin of the first histogram: not decreasing in the distance from the highest value.  Scores: linear in it over the S + 2
+// factors of two in which weights are not 0; probabilities: 32 bins a factor of two.
+template <int KIND, int NB> __device__ __forceinline__ u32 bin_of(const Scale& s, float v, u32 key) {
+    if (kLogs<KIND>) return v == s.m ? 0u : (u32)fminf((s.m - v) * s.per_bin, (float)(NB - 1));
+    constexpr int shift = NB >= 2048 ? 18 : NB >= 1024 ? 19 : 21;
+    return min((s.kmax - key) >> shift, (u32)(NB - 1));
+}
+
+// Workgroups are numbered over two grid dimensions (one holds less than 2^32 threads); the last ones may have no work.
+constexpr u64 kGridX = 1 << 20;
+__device__ __forceinline__ u64 grid_block() { return (u64)blockIdx.y * kGridX + blockIdx.x; }
+__host__ inline dim3 grid_of(u64 blocks) { return dim3((unsigned)std::min(blocks, kGridX), (unsigned)((blocks + kGridX - 1) / kGridX)); }
+
+// ---- wavefronts and workgroups ---------------------------------------------------------------------------------------
+template <class T> __device__ __forceinline__ T wave_sum(T v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+template <class T> __device__ __forceinline__ T wave_scan(T v, int lane) {      // inclusive
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const T up = __shfl_up(v, o, 64);
+        if (lane >= o) v += up;
+    }
+    return v;
+}
+
+// Sums over the workgroup before each thread's own, and the whole sum.  sm: NT / 64 entries that nothing else uses.
+template <int NT> __device__ __forceinline__ u64 block_scan(u64 v, u64* sm, u64* total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u64 incl = wave_scan(v, lane);
+    __syncthreads();
+    if (lane == 63) sm[wave] = incl;
+    __syncthreads();
+    u64 before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) {
+        const u64 x = sm[i];
+        if (i < wave) before += x;
+        all += x;
+    }
+    *total = all;
+    return before + incl - v;
+}
+
+template <int NT> __device__ __forceinline__ u32 block_max(u32 v, u64* sm) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = max(v, (u32)__shfl_xor((int)v, o, 64));
+    __syncthreads();
+    if (lane == 0) sm[wave] = v;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) v = max(v, (u32)sm[i]);
+    return v;
+}
+
+// The lowest key of lo .. hi for which `is` holds; it holds for hi and, with a key, for all above.  64 probes at a time.
+template <class F> __device__ __forceinline__ u32 first_key(u32 lo, u32 hi, F is) {
+    const u32 lane = threadIdx.x & 63;
+    while (lo < hi) {
+        const u32 step = (hi - lo + 63u) >> 6;
+        const u32 probe = min(lo + lane * step, hi);
+        const u64 hit = __ballot(is(probe));
+        if (hit == 0) { lo += 63u * step + 1u; continue; }     // (lane 63's probe lies below hi then)
+        const u32 f = (u32)__ffsll((long long)hit) - 1u;
+        const u32 top = min(lo + f * step, hi);
+        if (f > 0) lo = lo + (f - 1u) * step + 1u;
+        hi = top;
+    }
+    return hi;
+}
+
+// ---- the search for a cut --------------------------------------------------------------------------------------------
+struct Cut { u32 key, ne; };
+
+struct Find {
+    u32 klo, khi;        // the keys the cut is among
+    u32 done;            // the cut is known: (klo, ne)
+    u32 ne;
+    u64 target;          // outcomes, or (top-p) weights
+    u64 count, weight;   // of what lies above khi
+};
+
+// The bin in which the running sum (of counts, or of weights) over cnt / wt reaches target, and what lies before it.  false: it
+// never does.  Ends with a barrier.
+struct Hit { u32 bin; u64 count, weight; };
+struct ByCount { static constexpr bool value = false; };
+struct ByWeight { static constexpr bool value = true; };
+template <int NT, int NB, bool BYW> __device__ __forceinline__ bool select_bin(const u32* cnt, const u64* wt, u64 target, u64* sm, Hit* hit, Hit* at) {
+    constexpr int per = NB / NT > 0 ? NB / NT : 1;
+    const int b0 = threadIdx.x * per;
+    u64 c = 0, w = 0;
+    if (b0 < NB) {
+#pragma unroll
+        for (int i = 0; i < per; ++i) { c += cnt[b0 + i]; if (wt) w += wt[b0 + i]; }
+    }
+    u64 ct, wtot = 0, cb = block_scan<NT>(c, sm, &ct), wb = 0;
+    if (wt) wb = block_scan<NT>(w, sm, &wtot);
+    const u64 before = BYW ? wb : cb, mine = BYW ? w : c;
+    if (before < target && before + mine >= target) {
+        u32 b = b0;
+        u64 run = before;
+        for (int i = 0; i < per; ++i) {
+            const u64 x = BYW ? wt[b0 + i] : (u64)cnt[b0 + i];
+            if (run + x >= target) { b = b0 + i; break; }
+            run += x;
+            cb += cnt[b0 + i];
+            if (wt) wb += wt[b0 + i];
+        }
+        hit->bin = b;
+        hit->count = cb;
+        hit->weight = wb;
+    }
+    __syncthreads();
+    *at = *hit;
+    __syncthreads();
+    return (BYW ? wtot : ct) >= target;
+}
+
+// ceil(P W / 2^31), the weights that top-p keeps of W; at least 1, which the first outcome alone exceeds.
+__device__ __forceinline__ u64 mass_of(float top_p, u64 w) {
+    const u64 part = (u64)__builtin_rint((double)top_p * 2147483648.0);
+    const u64 low = part * (w & 0x7fffffffull);
+    const u64 h = part * (w >> 31) + (low >> 31) + ((low & 0x7fffffffull) != 0);
+    return h > 0 ? h : 1;
+}
+
+// The keys of bin b of the first histogram, from `lowest` on.
+template <int KIND, int NB> __device__ __forceinline__ void keys_of_bin(const Scale& s, u32 b, u32 lowest, u32* klo, u32* khi) {
+    auto bin = [&](u32 k) { return bin_of<KIND, NB>(s, value_of<KIND>(k), k); };
+    *klo = first_key(lowest, s.kmax, [&](u32 k) { return bin(k) <= b; });
+    // the first key of a lower bin, if there is one, ends the bin
+    *khi = b == 0 ? s.kmax : first_key(*klo, s.kmax, [&](u32 k) { return bin(k) < b; }) - 1u;
+}
+
+template <int NB> __device__ __forceinline__ int key_shift(u32 range) {
+    constexpr int bits = NB >= 2048 ? 11 : NB >= 1024 ? 10 : 8;
+    const int have = range ? 32 - __clz((int)range) : 0;
+    return have > bits ? have - bits : 0;
+}
+
+// What is known of the cut once its bin is: the next keys to look at, or the cut itself.
+template <int KIND, bool BYW> __device__ __forceinline__ void settle(const Scale& s, Find& f) {
+    if (f.klo < f.khi) return;
+    f.done = 1;
+    if (BYW) {
+        const u64 w = weight<KIND>(s, value_of<KIND>(f.klo));
+        f.ne = (u32)((f.target - f.weight + w - 1) / (w ? w : 1));
+    } else {
+        f.ne = (u32)(f.target - f.count);
+    }
+}
+
+// A row's parameters; ok = false: one of them is out of its range, and no outcome is drawn.
+struct Params {
+    float t, top_p, min_p;
+    int top_k;
+    bool ok;
+};
+
+__device__ __forceinline__ Params params_of(const SampleArgs& a, u64 r) {
+    Params p;
+    p.t = a.temperature ? a.temperature[r] : 1.f;
+    p.top_k = a.top_k ? a.top_k[r] : 0;
+    p.top_p = a.top_p ? a.top_p[r] : 1.f;
+    p.min_p = a.min_p ? a.min_p[r] : 0.f;
+    p.ok = p.t >= 0.f && p.t < kInf && p.top_k >= 0 && p.top_p >= 0.f && p.top_p < kInf && p.min_p >= 0.f && p.min_p <= 1.f;
+    return p;
+}
+
+__device__ __forceinline__ u64 draw_at(double u, u64 w) {           // floor(floor(u 2^53) w / 2^53)
+    const u64 r = (u64)(u * 9007199254740992.0);
+    return (__umul64hi(r, w) << 11) | ((r * w) >> 53);
+}
+
+__device__ __forceinline__ void write_shot(const SampleArgs& a, u64 at, long long k, u64 w, u64 total) {
+    a.out[at] = k;
+    if (a.logp) a.logp[at] = k < 0 ? -kInf : (float)log((double)w / (double)total);
+}
+
+template <int NT> __device__ __forceinline__ void write_none(const SampleArgs& a, u64 row, u64 first, u64 last) {
+    for (u64 i = first + threadIdx.x; i < last; i += NT) write_shot(a, row * a.shots + i, -1, 0, 1);
+}
+
+// ---- a row's chunks --------------------------------------------------------------------------------------------------
+// What a wavefront's vectors of one step hold of the outcomes that are kept: four flags a lane; running: equals so far.
+template <int KIND> __device__ __forceinline__ u32 kept_flags(const float (&v)[4], const Cut& cut, u64 eq_before, int lane, u32* running) {
+    u32 gt = 0, eq = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u32 k = key_of<KIND>(v[i]);
+        gt |= (u32)(k > cut.key) << i;
+        eq |= (u32)(k == cut.key) << i;
+    }
+    if (cut.ne == kAll) return gt | eq;
+    if (__ballot(eq != 0) == 0) return gt;
+    const u32 n = __popc(eq), incl = wave_scan(n, lane);
+    u64 rank = eq_before + *running + incl - n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((eq >> i) & 1u) { if (rank < cut.ne) gt |= 1u << i; ++rank; }
+    *running += __shfl(incl, 63, 64);
+    return gt;
+}
+
+// One chunk's sums: weights above the cut (WEIGHTS), and numbers above and at it (packed, 16 bits each).
+template <int KIND, bool WEIGHTS> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const Cut& cut, u32 j0, int steps, int lane, u64* w, u32* n) {
+    u64 sum = 0;
+    u32 num = 0;
+    for (int it = 0; it < steps; ++it) {
+        const u32 j = j0 + (u32)it * 64u + lane;
+        if (j >= row.vecs) break;
+        float v[4];
+        load4<KIND>(row, j, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32 k = key_of<KIND>(v[i]);
+            num += (k > cut.key) + ((u32)(k == cut.key) << 16);
+            if (WEIGHTS && k > cut.key) sum += weight<KIND>(s, v[i]);
+        }
+    }
+    *n = wave_sum(num);
+    if (WEIGHTS) *w = wave_sum(sum);
+}
+
+// The outcome of a chunk at which the running sum of kept weights, `base` before the chunk, exceeds t.  Whole wavefront.
+template <int KIND> __device__ __forceinline__ long long find_in_chunk(const Row& row, const Scale& s, const Cut& cut, u32 j0, int steps, u64 eq_before, u64 base, u64 t, int lane, u64* w_at) {
+    u32 running = 0;
+    for (int it = 0; it < steps; ++it) {
+        const u32 j = j0 + (u32)it * 64u + lane;
+        float v[4] = {kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f};
+        if (j < row.vecs) load4<KIND>(row, j, v);
+        const u32 keep = kept_flags<KIND>(v, cut, eq_before, lane, &running);
+        u64 w[4], four = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { w[i] = (keep >> i) & 1u ? weight<KIND>(s, v[i]) : 0; four += w[i]; }
+        const u64 incl = wave_scan(four, lane);
+        const u64 hit = __ballot(base + incl > t);
+        if (hit) {
+            const int who = __ffsll((long long)hit) - 1;
+            u64 run = base + incl - four, wk = 0;
+            long long k = 4ll * j - row.skew;
+            int at = -1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { run += w[i]; if (at < 0 && run > t) { at = i; wk = w[i]; } }
+            k += at;
+            *w_at = __shfl(wk, who, 64);
+            return __shfl(k, who, 64);
+        }
+        base += __shfl(incl, 63, 64);
+    }
+    *w_at = 0;
+    return -1;
+}
+
+// ---- one workgroup a row ---------------------------------------------------------------------------------------------
+template <int NT> struct Shape;
+// bins of a histogram, chunks, vectors of a lane in a chunk, outcomes of the list
+template <> struct Shape<64> { static constexpr int bins = 256, chunks = 4, steps = 1, list = 512; static constexpr u32 most = 512; };
+template <> struct Shape<256> { static constexpr int bins = 1024, chunks = 36, steps = 1, list = 2048; static constexpr u32 most = 8192; };
+template <> struct Shape<1024> { static constexpr int bins = 2048, chunks = 264, steps = 4, list = 2048; static constexpr u32 most = 262144; };
+
+template <int KIND, int NT>
+__global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
+    constexpr int NB = Shape<NT>::bins, NC = Shape<NT>::chunks, STEPS = Shape<NT>::steps, LIST = Shape<NT>::list;
+    __shared__ u64 wt[2][NB];
+    __shared__ u32 cnt[2][NB];
+    __shared__ u64 sm[16];
+    __shared__ Hit hit;
+    __shared__ u64 chunk_w[NC];             // kept weights up to the chunk's end
+    __shared__ u32 chunk_n[NC], chunk_eq[NC];
+    static_assert(sizeof(u64) * LIST <= sizeof wt && sizeof(u32) * LIST <= sizeof cnt, "the list takes the histograms' place");
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u64 r = grid_block();
+    if (r >= (u64)a.rows) return;
+    const Row row = row_of<KIND>(a, r);
+    const Params p = params_of(a, r);
+    const u32 nchunks = (row.vecs + 64 * STEPS - 1) / (64 * STEPS);
+
+    u32 kmax = 0;
+    for (u32 j = threadIdx.x; j < row.vecs; j += NT) {
+        float v[4];
+        load4<KIND>(row, j, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kmax = max(kmax, key_of<KIND>(v[i]));
+    }
+    kmax = block_max<NT>(kmax, sm);
+    if (!p.ok || kmax < kLowest<KIND>) {
+        write_none<NT>(a, r, 0, a.shots);
+        if (threadIdx.x == 0 && a.kept) a.kept[r] = 0;
+        return;
+    }
+    const bool greedy = p.t == 0.f;
+    const Scale s = scale_of<KIND, NB>(kmax, greedy ? 1.f : p.t, a.bits);
+    u32 lowest = kLowest<KIND>;
+    if (p.min_p > 0.f && !greedy)
+        lowest = first_key(lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
+
+    // a histogram of the values with keys in klo .. khi: the first one over distances, later ones over keys
+    auto histogram = [&](int h, bool first, bool weights, u32 klo, u32 khi) {
+        for (int i = threadIdx.x; i < NB; i += NT) { cnt[h][i] = 0; wt[h][i] = 0; }
+        __syncthreads();
+        const int shift = key_shift<NB>(khi - klo);
+        for (u32 j = threadIdx.x; j < row.vecs; j += NT) {
+            float v[4];
+            load4<KIND>(row, j, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32 k = key_of<KIND>(v[i]);
+                if (k < klo || k > khi) continue;
+                const u32 b = first ? bin_of<KIND, NB>(s, v[i], k) : (khi - k) >> shift;
+                atomicAdd(&cnt[h][b], 1u);
+                if (weights) atomicAdd(&wt[h][b], weight<KIND>(s, v[i]));
+            }
+        }
+        __syncthreads();
+    };
+
+    Cut cut{lowest, kAll};
+    u64 kept = ~0ull;                      // not known yet
+    if (greedy) {
+        cut = Cut{kmax, 1};
+        kept = 1;
+    } else if ((p.top_k > 0 && (u32)p.top_k < row.cols) || p.top_p < 1.f) {
+        const bool by_mass = p.top_p < 1.f;
+        histogram(0, true, by_mass, lowest, kmax);
+        u64 mass = 0;
+        bool have_mass = false;
+        auto narrow = [&](auto byw, Find f) -> Find {
+            constexpr bool BYW = decltype(byw)::value;
+            while (!f.done) {
+                histogram(1, false, by_mass, f.klo, f.khi);
+                Hit at;
+                if (!select_bin<NT, NB, BYW>(cnt[1], by_mass ? wt[1] : nullptr, f.target - (BYW ? f.weight : f.count), sm, &hit, &at))
+                    break;                 // (the row was written to while it was read)
+                const int shift = key_shift<NB>(f.khi - f.klo);
+                const u32 top = f.khi - (at.bin << shift);
+                const u32 low = top - f.klo < (1u << shift) ? f.klo : top - (1u << shift) + 1u;
+                f.khi = top;
+                f.klo = low;
+                f.count += at.count;
+                f.weight += at.weight;
+                settle<KIND, BYW>(s, f);
+            }
+            return f;
+        };
+        auto begin = [&](auto byw, u64 target, Find* f) -> bool {
+            constexpr bool BYW = decltype(byw)::value;
+            Hit at;
+            if (!select_bin<NT, NB, BYW>(cnt[0], by_mass ? wt[0] : nullptr, target, sm, &hit, &at)) return false;
+            keys_of_bin<KIND, NB>(s, at.bin, lowest, &f->klo, &f->khi);
+            f->done = 0;
+            f->ne = 0;
+            f->target = target;
+            f->count = at.count;
+            f->weight = at.weight;
+            settle<KIND, BYW>(s, *f);
+            return true;
+        };
+        Find f;
+        if (p.top_k > 0 && begin(ByCount{}, (u64)p.top_k, &f)) {
+            f = narrow(ByCount{}, f);
+            cut = Cut{f.klo, f.ne};
+            kept = (u64)p.top_k;
+            if (by_mass) mass = f.weight + (u64)f.ne * weight<KIND>(s, value_of<KIND>(f.klo));
+            have_mass = true;
+        }
+        if (by_mass) {
+            if (!have_mass) {
+                u64 part = 0;
+                for (int i = threadIdx.x; i < NB; i += NT) part += wt[0][i];
+                (void)block_scan<NT>(part, sm, &mass);
+            }
+            if (begin(ByWeight{}, mass_of(p.top_p, mass), &f)) {
+                f = narrow(ByWeight{}, f);
+                cut = Cut{f.klo, f.ne};
+                kept = f.count + f.ne;
+            }
+        }
+    }
+
+    // the chunks' numbers of kept outcomes, and their weights where the outcomes do not fit the list
+    const bool list = kept <= (u64)LIST || row.cols <= (u32)LIST;
+    for (u32 c = wave; c < nchunks; c += NT / 64) {
+        u64 w = 0;
+        u32 n;
+        if (list) chunk_sums<KIND, false>(row, s, cut, c * 64 * STEPS, STEPS, lane, &w, &n);
+        else chunk_sums<KIND, true>(row, s, cut, c * 64 * STEPS, STEPS, lane, &w, &n);
+        if (lane == 0) { chunk_w[c] = w; chunk_n[c] = n; }
+    }
+    __syncthreads();
+    u64 total, n_kept;
+    {
+        constexpr int per = (NC + NT - 1) / NT;
+        static_assert(per == 1, "a thread has a chunk");
+        const bool mine = threadIdx.x < nchunks;
+        const u32 n = mine ? chunk_n[threadIdx.x] : 0u;
+        const u64 eq = n >> 16;
+        u64 unused;
+        const u64 eq_before = block_scan<NT>(eq, sm, &unused);
+        const u64 take = eq_before >= cut.ne ? 0 : min(eq, (u64)cut.ne - eq_before);
+        const u64 num = (n & 0xffffu) + take;
+        const u64 w_cut = list ? 0 : weight<KIND>(s, value_of<KIND>(cut.key));
+        const u64 w = (mine ? chunk_w[threadIdx.x] : 0) + take * w_cut;
+        const u64 num_before = block_scan<NT>(num, sm, &n_kept);
+        const u64 w_before = block_scan<NT>(w, sm, &total);
+        if (mine) {
+            chunk_eq[threadIdx.x] = (u32)min(eq_before, (u64)kAll);
+            chunk_n[threadIdx.x] = (u32)num_before | (num ? 0x80000000u : 0u);     // (2^18 outcomes at most)
+            chunk_w[threadIdx.x] = w_before + w;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && a.kept) a.kept[r] = (int)n_kept;
+    if (list) {
+        u64* lw = wt[0];
+        u32* lk = cnt[0];
+        for (u32 c = wave; c < nchunks; c += NT / 64) {
+            const u32 packed = chunk_n[c];
+            if (!(packed >> 31)) continue;
+            u32 pos = packed & 0x7fffffffu, running = 0;
+            for (int it = 0; it < STEPS; ++it) {
+                const u32 j = c * 64 * STEPS + (u32)it * 64u + lane;
+                float v[4] = {kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f};
+                if (j < row.vecs) load4<KIND>(row, j, v);
+                const u32 keep = kept_flags<KIND>(v, cut, chunk_eq[c], lane, &running);
+                const u32 n = __popc(keep), incl = wave_scan(n, lane);
+                u32 at = pos + incl - n;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if ((keep >> i) & 1u) { lw[at] = key_of<KIND>(v[i]); lk[at] = 4u * j - row.skew + i; ++at; }
+                pos += __shfl(incl, 63, 64);
+            }
+        }
+        __syncthreads();
+        constexpr int per = LIST / NT;
+        u64 w[per], sum = 0;
+        const u32 first = threadIdx.x * per;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            w[i] = first + i < n_kept ? weight<KIND>(s, value_of<KIND>((u32)lw[first + i])) : 0;
+            sum += w[i];
+        }
+        u64 run = block_scan<NT>(sum, sm, &total);
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            run += w[i];
+            if (first + i < n_kept) lw[first + i] = run;
+        }
+        __syncthreads();
+        for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
+            const double u = a.uniforms[r * a.shots + i];
+            if (!(u >= 0.0 && u < 1.0)) { write_shot(a, r * a.shots + i, -1, 0, 1); continue; }
+            const u64 t = draw_at(u, total);
+            u32 lo = 0, len = (u32)n_kept;                 // the first with a sum above t is in lo .. lo + len - 1
+            while (len > 1) {
+                const u32 half = len >> 1;
+                if (lw[lo + half - 1] > t) len = half;
+                else { lo += half; len -= half; }
+            }
+            write_shot(a, r * a.shots + i, (long long)lk[lo], lw[lo] - (lo ? lw[lo - 1] : 0), total);
+        }
+        return;
+    }
+    for (u64 i = wave; i < (u64)a.shots; i += NT / 64) {
+        const double u = a.uniforms[r * a.shots + i];
+        long long k = -1;
+        u64 w = 0;
+        if (u >= 0.0 && u < 1.0) {
+            const u64 t = draw_at(u, total);
+            u32 c = 0;
+            for (u32 c0 = 0; c0 < nchunks; c0 += 64) {
+                const u64 above = __ballot(c0 + lane < nchunks && chunk_w[min(c0 + (u32)lane, nchunks - 1)] > t);
+                if (above) { c = c0 + (u32)__ffsll((long long)above) - 1u; break; }
+            }
+            k = find_in_chunk<KIND>(row, s, cut, c * 64 * STEPS, STEPS, chunk_eq[c], c ? chunk_w[c - 1] : 0, t, lane, &w);
+        }
+        if (lane == 0) write_shot(a, r * a.shots + i, k, w, total);
+    }
+}
+
+// ---- long rows: their parts by workgroups of their own ---------------------------------------------------------------
+// The same steps, a launch each; what a step finds out about a row goes to the next one through the workspace: the parts'
+// highest keys, histograms that all parts add to, the state of the search.  Every workgroup of a step works the state out
+// again from the one before and its histogram; the row's first one writes it down.  Steps whose cut is known already end
+// at once.
+constexpr int kLongBins = 2048, kLongThreads = 256, kLongSteps = 4, kLongChunk = 64 * kLongSteps * 4;
+constexpr int kKeySteps = 3;                       // 11 bits of a key each
+constexpr int kLevels = 1 + 2 * kKeySteps;         // distances; keys for top-k; keys for top-p
+
+struct LongState {
+    u32 ok, kmax, lowest, stage;       // stage 0: no search under way; 1: top-k; 2: top-p
+    Find f;
+    Cut cut;
+    u64 mass, kept;
+    u32 have_mass;
+};
+
+struct Long {
+    u32 parts, chunks, chunks_per_part, levels;
+    u32* pmax;             // [rows][parts]
+    u64* wt;               // [rows][kLevels][kLongBins]
+    u32* cnt;              // [rows][kLevels][kLongBins]
+    LongState* state;      // [rows][kLevels]
+    u64* chunk_w;          // [rows][chunks]
+    u32* chunk_n;          // [rows][chunks]
+};
+
+__host__ __device__ inline u64 long_chunks(int64_t cols) { return ((u64)cols + 3 + kLongChunk - 1) / kLongChunk; }
+
+// Parts of about four chunks (a wavefront each), as many as give the chip eight workgroups a CU.
+__host__ inline u32 long_parts(int64_t rows, int64_t cols) {
+    const u64 want = (long_chunks(cols) + 3) / 4, most = std::max<u64>(1, 2048 / (u64)rows);
+    return (u32)std::min(std::min(want, most), (u64)1024);
+}
+
+struct LongSizes { size_t pmax, wt, cnt, state, chunk_w, chunk_n, all; };
+__host__ inline LongSizes long_sizes(int64_t rows, int64_t cols) {
+    auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
+    LongSizes s;
+    const size_t n = (size_t)rows, chunks = (size_t)long_chunks(cols);
+    s.pmax = up(n * long_parts(rows, cols) * 4);
+    s.wt = up(n * kLevels * kLongBins * 8);
+    s.cnt = up(n * kLevels * kLongBins * 4);
+    s.state = up(n * kLevels * sizeof(LongState));
+    s.chunk_w = up(n * chunks * 8);
+    s.chunk_n = up(n * chunks * 4);
+    s.all = s.pmax + s.wt + s.cnt + s.state + s.chunk_w + s.chunk_n;
+    return s;
+}
+
+template <int KIND> __device__ __forceinline__ void part_of(const Row& row, const Long& g, u32 part, u32* j0, u32* j1) {
+    const u64 per = (u64)g.chunks_per_part * 64 * kLongSteps;
+    *j0 = (u32)min((u64)part * per, (u64)row.vecs);
+    *j1 = (u32)min((u64)(part + 1) * per, (u64)row.vecs);
+}
+
+template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_max(const SampleArgs a, const Long g) {
+    __shared__ u64 sm[kLongThreads / 64];
+    const u64 r = grid_block() / g.parts;
+    const u32 part = (u32)(grid_block() % g.parts);
+    if (r >= (u64)a.rows) return;
+    const Row row = row_of<KIND>(a, r);
+    u32 j0, j1, kmax = 0;
+    part_of<KIND>(row, g, part, &j0, &j1);
+    for (u32 j = j0 + threadIdx.x; j < j1; j += kLongThreads) {
+        float v[4];
+        load4<KIND>(row, j, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kmax = max(kmax, key_of<KIND>(v[i]));
+    }
+    kmax = block_max<kLongThreads>(kmax, sm);
+    if (threadIdx.x == 0) g.pmax[r * g.parts + part] = kmax;
+    // the row's histograms start at zero
+    const u32 bins = g.levels ? kLevels * kLongBins : 0;
+    for (u32 i = part * kLongThreads + threadIdx.x; i < bins; i += g.parts * kLongThreads) {
+        g.wt[r * (kLevels * kLongBins) + i] = 0;
+        g.cnt[r * (kLevels * kLongBins) + i] = 0;
+    }
+}
+
+__device__ __forceinline__ bool by_top_k(const SampleArgs& a, const Params& p) { return p.t > 0.f && p.top_k > 0 && (u32)p.top_k < a.cols; }
+__device__ __forceinline__ bool by_top_p(const Params& p) { return p.t > 0.f && p.top_p < 1.f; }
+
+// The histogram of the values of vectors j0 .. j1 with keys in klo .. khi, added to the row's.
+template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, u64* wt, u32* cnt, u64* gw, u32* gc) {
+    for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) { cnt[i] = 0; wt[i] = 0; }
+    __syncthreads();
+    const int shift = key_shift<kLongBins>(khi - klo);
+    for (u32 j = j0 + threadIdx.x; j < j1; j += kLongThreads) {
+        float v[4];
+        load4<KIND>(row, j, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32 k = key_of<KIND>(v[i]);
+            if (k < klo || k > khi) continue;
+            const u32 b = first ? bin_of<KIND, kLongBins>(s, v[i], k) : (khi - k) >> shift;
+            atomicAdd(&cnt[b], 1u);
+            if (weights) atomicAdd(&wt[b], weight<KIND>(s, v[i]));
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) {
+        if (cnt[i]) {
+            atomicAdd(&gc[i], cnt[i]);
+            if (weights && wt[i]) atomicAdd(&gw[i], wt[i]);
+        }
+    }
+}
+
+template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first(const SampleArgs a, const Long g) {
+    __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
+    __shared__ u32 cnt[kLongBins];
+    const u64 r = grid_block() / g.parts;
+    const u32 part = (u32)(grid_block() % g.parts);
+    if (r >= (u64)a.rows) return;
+    const Row row = row_of<KIND>(a, r);
+    const Params p = params_of(a, r);
+    u32 kmax = 0;
+    for (u32 i = threadIdx.x; i < g.parts; i += kLongThreads) kmax = max(kmax, g.pmax[r * g.parts + i]);
+    kmax = block_max<kLongThreads>(kmax, sm);
+    LongState st{};
+    st.ok = p.ok && kmax >= kLowest<KIND>;
+    st.kmax = kmax;
+    st.lowest = kLowest<KIND>;
+    st.kept = ~0ull;
+    if (st.ok) {
+        const Scale s = scale_of<KIND, kLongBins>(kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+        if (p.min_p > 0.f && p.t > 0.f)
+            st.lowest = first_key(st.lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
+        st.cut = p.t > 0.f ? Cut{st.lowest, kAll} : Cut{kmax, 1};
+        if (by_top_k(a, p) || by_top_p(p)) {
+            u32 j0, j1;
+            part_of<KIND>(row, g, part, &j0, &j1);
+            long_histogram<KIND>(row, s, j0, j1, true, by_top_p(p), st.lowest, kmax, wt, cnt, g.wt + r * (kLevels * kLongBins), g.cnt + r * (kLevels * kLongBins));
+        }
+    }
+    if (part == 0 && threadIdx.x == 0) g.state[r * kLevels] = st;
+}
+
+// The search after the histogram of level `prev`.
+template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_advance(const SampleArgs& a, const Params& p, const Scale& s, const Long& g, u64 r, int prev, u64* sm, Hit* hit, LongState* st) {
+    if (!st->stage) return;
+    Find& f = st->f;
+    const u64* wt = g.wt + (r * kLevels + prev) * kLongBins;
+    const u32* cnt = g.cnt + (r * kLevels + prev) * kLongBins;
+    if (!f.done) {
+        Hit at;
+        const bool found = st->stage == 1 ? select_bin<NT, kLongBins, false>(cnt, by_top_p(p) ? wt : nullptr, f.target - f.count, sm, hit, &at)
+                                          : select_bin<NT, kLongBins, true>(cnt, wt, f.target - f.weight, sm, hit, &at);
+        if (!found) { st->stage = 0; return; }             // (the row was written to while it was read)
+        const int shift = key_shift<kLongBins>(f.khi - f.klo);
+        const u32 top = f.khi - (at.bin << shift);
+        f.klo = top - f.klo < (1u << shift) ? f.klo : top - (1u << shift) + 1u;
+        f.khi = top;
+        f.count += at.count;
+        f.weight += at.weight;
+        if (st->stage == 1) settle<KIND, false>(s, f);
+        else settle<KIND, true>(s, f);
+    }
+    if (!f.done) return;
+    st->cut = Cut{f.klo, f.ne};
+    st->kept = f.count + f.ne;
+    if (st->stage == 1 && by_top_p(p)) {
+        st->mass = f.weight + (u64)f.ne * weight<KIND>(s, value_of<KIND>(f.klo));
+        st->have_mass = 1;
+    }
+    st->stage = 0;
+}
+
+template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs& a, const Params& p, const Scale& s, const Long& g, u64 r, u32 stage, u64* sm, Hit* hit, LongState* st) {
+    const u64* wt = g.wt + r * kLevels * kLongBins;
+    const u32* cnt = g.cnt + r * kLevels * kLongBins;
+    Hit at;
+    u64 target;
+    if (stage == 1) {
+        target = (u64)p.top_k;
+        if (!select_bin<kLongThreads, kLongBins, false>(cnt, by_top_p(p) ? wt : nullptr, target, sm, hit, &at)) return;
+    } else {
+        u64 mass = st->mass;
+        if (!st->have_mass) {
+            u64 part = 0;
+            for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) part += wt[i];
+            (void)block_scan<kLongThreads>(part, sm, &mass);
+        }
+        target = mass_of(p.top_p, mass);
+        if (!select_bin<kLongThreads, kLongBins, true>(cnt, wt, target, sm, hit, &at)) return;
+    }
+    Find f;
+    keys_of_bin<KIND, kLongBins>(s, at.bin, st->lowest, &f.klo, &f.khi);
+    f.done = 0;
+    f.ne = 0;
+    f.target = target;
+    f.count = at.count;
+    f.weight = at.weight;
+    if (stage == 1) settle<KIND, false>(s, f);
+    else settle<KIND, true>(s, f);
+    st->f = f;
+    st->stage = stage;
+    if (f.done) long_advance<KIND>(a, p, s, g, r, 0, sm, hit, st);
+}
+
+// Level `level` after level `prev`: the first level of top-k is 1, that of top-p 1 + kKeySteps.
+template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(const SampleArgs a, const Long g, int level, int prev) {
+    __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
+    __shared__ u32 cnt[kLongBins];
+    __shared__ Hit hit;
+    const u64 r = grid_block() / g.parts;
+    const u32 part = (u32)(grid_block() % g.parts);
+    if (r >= (u64)a.rows) return;
+    const Row row = row_of<KIND>(a, r);
+    const Params p = params_of(a, r);
+    LongState st = g.state[r * kLevels + prev];
+    if (st.ok) {
+        const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+        long_advance<KIND>(a, p, s, g, r, prev, sm, &hit, &st);
+        if (level == 1 && by_top_k(a, p)) long_begin<KIND>(a, p, s, g, r, 1, sm, &hit, &st);
+        if (level == 1 + kKeySteps && by_top_p(p)) long_begin<KIND>(a, p, s, g, r, 2, sm, &hit, &st);
+        if (st.stage) {
+            u32 j0, j1;
+            part_of<KIND>(row, g, part, &j0, &j1);
+            const size_t at = (r * kLevels + level) * kLongBins;
+            long_histogram<KIND>(row, s, j0, j1, false, by_top_p(p), st.f.klo, st.f.khi, wt, cnt, g.wt + at, g.cnt + at);
+        }
+    }
+    if (part == 0 && threadIdx.x == 0) g.state[r * kLevels + level] = st;
+}
+
+// The chunks' sums of what is kept.
+template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(const SampleArgs a, const Long g, int prev) {
+    __shared__ u64 sm[kLongThreads / 64];
+    __shared__ Hit hit;
+    const u64 r = grid_block() / g.parts;
+    const u32 part = (u32)(grid_block() % g.parts);
+    if (r >= (u64)a.rows) return;
+    const Row row = row_of<KIND>(a, r);
+    const Params p = params_of(a, r);
+    LongState st = g.state[r * kLevels + prev];
+    if (!st.ok) return;
+    const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    long_advance<KIND>(a, p, s, g, r, prev, sm, &hit, &st);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u32 c1 = min((part + 1) * g.chunks_per_part, g.chunks);
+    for (u32 c = part * g.chunks_per_part + wave; c < c1; c += kLongThreads / 64) {
+        u64 w;
+        u32 n;
+        chunk_sums<KIND, true>(row, s, st.cut, c * 64 * kLongSteps, kLongSteps, lane, &w, &n);
+        if (lane == 0) {
+            g.chunk_w[r * g.chunks + c] = w;
+            g.chunk_n[r * g.chunks + c] = n;
+        }
+    }
+}
+
+template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const Cut& cut, const u64* cw, const u32* ce, u32 chunks, u64 at, int lane) {
+    const double u = a.uniforms[at];
+    const u64 total = cw[chunks - 1];
+    long long k = -1;
+    u64 w = 0;
+    if (u >= 0.0 && u < 1.0) {
+        const u64 t = draw_at(u, total);
+        u32 lo = 0, len = chunks;                  // the first chunk with a sum above t is in lo .. lo + len - 1
+        while (len > 1) {
+            const u32 stride = (len + 63) >> 6;
+            const u32 probe = min((lane + 1) * stride, len) - 1;
+            const u64 above = __ballot(cw[lo + probe] > t);
+            const u32 f = above ? (u32)__ffsll((long long)above) - 1u : 63u;
+            const u32 off = min(f * stride, len - 1);
+            lo += off;
+            len = min(stride, len - off);
+        }
+        k = find_in_chunk<KIND>(row, s, cut, lo * 64 * kLongSteps, kLongSteps, ce[lo], lo ? cw[lo - 1] : 0, t, lane, &w);
+    }
+    if (lane == 0) write_shot(a, at, k, w, total);
+}
+
+// One workgroup a row: running sums over its chunks, and (draw) its shots.
+template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const SampleArgs a, const Long g, int prev, int draw) {
+    __shared__ u64 sm[16];
+    __shared__ Hit hit;
+    const u64 r = grid_block();
+    if (r >= (u64)a.rows) return;
+    const Row row = row_of<KIND>(a, r);
+    const Params p = params_of(a, r);
+    LongState st = g.state[r * kLevels + prev];
+    if (!st.ok) {
+        if (draw) write_none<1024>(a, r, 0, a.shots);
+        if (threadIdx.x == 0 && a.kept) a.kept[r] = 0;
+        if (threadIdx.x == 0) g.state[r * kLevels + kLevels - 1] = st;
+        return;
+    }
+    const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    long_advance<KIND, 1024>(a, p, s, g, r, prev, sm, &hit, &st);
+    u64* cw = g.chunk_w + r * g.chunks;
+    u32* cn = g.chunk_n + r * g.chunks;
+    const u32 per = (g.chunks + 1023) / 1024;
+    const u32 c0 = min(threadIdx.x * per, g.chunks), c1 = min(c0 + per, g.chunks);
+    u64 eq = 0, eq_all, n_kept, total;
+    for (u32 c = c0; c < c1; ++c) eq += cn[c] >> 16;
+    const u64 eq_before = block_scan<1024>(eq, sm, &eq_all);
+    const u64 w_cut = weight<KIND>(s, value_of<KIND>(st.cut.key));
+    u64 run = eq_before, num = 0, w = 0;
+    for (u32 c = c0; c < c1; ++c) {
+        const u32 n = cn[c];
+        const u64 take = run >= st.cut.ne ? 0 : min((u64)(n >> 16), (u64)st.cut.ne - run);
+        num += (n & 0xffffu) + take;
+        w += cw[c] + take * w_cut;
+        run += n >> 16;
+    }
+    (void)block_scan<1024>(num, sm, &n_kept);
+    u64 sum = block_scan<1024>(w, sm, &total);
+    run = eq_before;
+    for (u32 c = c0; c < c1; ++c) {
+        const u32 n = cn[c];
+        const u64 take = run >= st.cut.ne ? 0 : min((u64)(n >> 16), (u64)st.cut.ne - run);
+        sum += cw[c] + take * w_cut;
+        cw[c] = sum;
+        cn[c] = (u32)run;
+        run += n >> 16;
+    }
+    if (threadIdx.x == 0) {
+        if (a.kept) a.kept[r] = (int)n_kept;
+        g.state[r * kLevels + kLevels - 1] = st;
+    }
+    if (!draw) return;
+    __threadfence_block();
+    __syncthreads();
+    for (u64 i = threadIdx.x >> 6; i < (u64)a.shots; i += 16)
+        long_shot<KIND>(a, row, s, st.cut, cw, cn, g.chunks, r * a.shots + i, threadIdx.x & 63);
+}
+
+template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const SampleArgs a, const Long g) {
+    const u64 at = grid_block() * 4 + (threadIdx.x >> 6);
+    if (at >= (u64)a.rows * a.shots) return;
+    const u64 r = at / a.shots;
+    const LongState st = g.state[r * kLevels + kLevels - 1];
+    const int lane = threadIdx.x & 63;
+    if (!st.ok) {
+        if (lane == 0) write_shot(a, at, -1, 0, 1);
+        return;
+    }
+    const Row row = row_of<KIND>(a, r);
+    const Params p = params_of(a, r);
+    const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    long_shot<KIND>(a, row, s, st.cut, g.chunk_w + r * g.chunks, g.chunk_n + r * g.chunks, g.chunks, at, lane);
+}
+
+}  // namespace
+
+// Rows of more outcomes than one workgroup takes, or so few that most of the chip would idle.
+static bool takes_parts(int64_t rows, int64_t cols) {
+    return cols > (int64_t)Shape<1024>::most;
+}
+
+size_t sample_scratch_bytes(int64_t rows, int64_t cols) {
+    return rows > 0 && takes_parts(rows, cols) ? long_sizes(rows, cols).all : 0;
+}
+
+template <int KIND> static hipError_t launch_long(const SampleArgs& a, char* scratch, hipStream_t st) {
+    const LongSizes z = long_sizes(a.rows, a.cols);
+    Long g;
+    g.chunks = (u32)long_chunks(a.cols);
+    g.parts = long_parts(a.rows, a.cols);
+    g.chunks_per_part = (g.chunks + g.parts - 1) / g.parts;
+    g.levels = a.top_k || a.top_p;
+    g.wt = (u64*)scratch; scratch += z.wt;
+    g.chunk_w = (u64*)scratch; scratch += z.chunk_w;
+    g.state = (LongState*)scratch; scratch += z.state;
+    g.pmax = (u32*)scratch; scratch += z.pmax;
+    g.cnt = (u32*)scratch; scratch += z.cnt;
+    g.chunk_n = (u32*)scratch;
+    const dim3 grid = grid_of((u64)a.rows * g.parts), block(kLongThreads);
+    hipLaunchKernelGGL(k_long_max<KIND>, grid, block, 0, st, a, g);
+    hipLaunchKernelGGL(k_long_first<KIND>, grid, block, 0, st, a, g);
+    int prev = 0;
+    for (int stage = 0; stage < 2; ++stage) {
+        if (!(stage == 0 ? (const void*)a.top_k : (const void*)a.top_p)) continue;
+        for (int i = 1; i <= kKeySteps; ++i) {
+            const int level = stage * kKeySteps + i;
+            hipLaunchKernelGGL(k_long_keys<KIND>, grid, block, 0, st, a, g, level, prev);
+            prev = level;
+        }
+    }
+    hipLaunchKernelGGL(k_long_sums<KIND>, grid, block, 0, st, a, g, prev);
+    const int here = a.shots <= 16;
+    hipLaunchKernelGGL(k_long_scan<KIND>, grid_of((u64)a.rows), dim3(1024), 0, st, a, g, prev, here);
+    if (!here)
+        hipLaunchKernelGGL(k_long_draw<KIND>, grid_of(((u64)a.rows * a.shots + 3) / 4), dim3(256), 0, st, a, g);
+    return hipGetLastError();
+}
+
+template <int KIND> static hipError_t launch_kind(const SampleArgs& a, void* scratch, hipStream_t st) {
+    if (takes_parts(a.rows, a.cols)) return launch_long<KIND>(a, (char*)scratch, st);
+    const dim3 grid = grid_of((u64)a.rows);
+    if (a.cols <= Shape<64>::most) hipLaunchKernelGGL((k_sample_row<KIND, 64>), grid, dim3(64), 0, st, a);
+    else if (a.cols <= Shape<256>::most) hipLaunchKernelGGL((k_sample_row<KIND, 256>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_sample_row<KIND, 1024>), grid, dim3(1024), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_sample_scores(int kind, const SampleArgs& a, void* scratch, hipStream_t st) {
+    switch (kind) {
+        case kScoreF32: return launch_kind<kScoreF32>(a, scratch, st);
+        case kScoreF16: return launch_kind<kScoreF16>(a, scratch, st);
+        case kScoreBF16: return launch_kind<kScoreBF16>(a, scratch, st);
+        case kScoreProbs: return launch_kind<kScoreProbs>(a, scratch, st);
+        case kScoreState: return launch_kind<kScoreState>(a, scratch, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace qsv
