@@ -311,6 +311,56 @@ qsv_status qsv_loss_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_dev,
                          const float* params_dev, const float* feats_dev, const qsv_loss* loss,
                          float* loss_dev, float* grad_dev, float* mean_loss_dev, float* mean_grad_dev);
 
+/* A teacher known by its top logits: n_top entries for every row (or sample).  q_j = exp(t_j / T - norm), norm the
+ * logarithm of the sum of exp(t_j / T) over the row's entries, or top_lse: the teacher's own logarithm of that sum over all
+ * its outcomes, at the same T; Q = sum of q.  Entries with an index outside 0..cols-1 (padding) or a logit of -inf count
+ * for nothing, and a row without any other has loss 0 and gradient 0; entries with the same index add up.  With one entry
+ * a row (and its logit anything finite) the loss is the cross entropy of labels. */
+typedef struct {
+    int32_t n_top;               /* 1..1024 */
+    int32_t reserved;            /* must be 0 */
+    const int32_t* top_idx_dev;  /* [rows][n_top] */
+    const float* top_logits_dev; /* [rows][n_top] */
+    const float* top_lse_dev;    /* [rows] or NULL */
+    double temperature;          /* T: finite, > 0 */
+} qsv_teacher;
+
+/* Loss of rows of scores z of a student against a teacher's top logits, and its gradient:
+ *   p = softmax(z / T),   loss = sum_j q_j (ln q_j - ln p_{i_j}),
+ *   d loss / d z_k = g / T (Q p_k - sum over the entries j with i_j = k of q_j),   g = grad_loss (1 if NULL).
+ * (No factor T^2 is put in: it can go into grad_loss.)  Scores of -inf are masked: p = 0; an entry with q > 0 there makes
+ * the loss +inf.  A NaN or +inf among a row's scores makes its loss and gradient NaN.
+ * stats: [rows][2], the row's highest score m and the sum of exp((z - m) / T); written when have_stats = 0, and read instead
+ * of being worked out when have_stats = 1, which is the backward pass by itself (loss_dev must be NULL then).
+ * The gradient has the type of the scores, rounded once, and may be written over them (the same address and row stride);
+ * otherwise the two must not overlap.  Any of loss_dev, stats_dev and grad_dev may be NULL. */
+typedef struct {
+    int32_t kind;                /* QSV_S_F32, QSV_S_F16 or QSV_S_BF16 */
+    int32_t have_stats;
+    const void* scores_dev;      /* row r starts at element r * row_stride; aligned to its element */
+    int64_t rows;                /* 0..2^24; 0 is a no-op */
+    int64_t cols;                /* 1..2^30 */
+    int64_t row_stride;          /* >= cols (any value for one row), in elements */
+    float* loss_dev;             /* [rows] or NULL */
+    float* stats_dev;            /* [rows][2] or NULL */
+    const float* grad_loss_dev;  /* [rows] or NULL */
+    void* grad_dev;              /* [rows] rows of cols, of the scores' type, or NULL */
+    int64_t grad_stride;         /* >= cols (any value for one row), in elements */
+} qsv_distill_req;
+
+/* Workspace size in bytes that qsv_distill needs for such rows, that of the plans included; 0 on bad arguments. */
+size_t qsv_distill_workspace_bytes(int64_t rows, int64_t cols);
+qsv_status qsv_distill(qsv_ctx* ctx, const qsv_distill_req* req, const qsv_teacher* teacher);
+
+/* Per-sample loss [batch] and gradient [batch][P] of a circuit's own outcome distribution against a teacher's top logits
+ * (outcomes 0..2^n-1; teacher arrays of batch rows), and optionally their batch means, in reverse mode as qsv_loss_grad:
+ *   p_k = |a_k|^2 of the encoded sample's final state,   loss_b = sum_j q_j (ln q_j - ln p_{i_j}).
+ * The teacher's temperature softens q alone.  An entry with q > 0 at an outcome of amplitude 0 makes the loss +inf and adds
+ * nothing to the gradient.  Arguments as qsv_param_shift_grad; teacher is a host struct read during the call. */
+qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_dev, int64_t dim,
+                            const float* params_dev, const float* feats_dev, const qsv_teacher* teacher,
+                            float* loss_dev, float* grad_dev, float* mean_loss_dev, float* mean_grad_dev);
+
 /* Optimiser steps on the device, asynchronous on the context's stream; arithmetic in double, storage
  * float.  qsv_sgd_step: params -= lr * grad.  qsv_adam_step (Kingma and Ba, Algorithm 1): m, v are
  * the caller's moment buffers [count] (zero before the first step), t >= 1 the step count.

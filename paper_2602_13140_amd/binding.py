@@ -49,6 +49,18 @@ class qsv_sample_req(ctypes.Structure):
                 ("logp_dev", ctypes.c_void_p), ("kept_dev", ctypes.c_void_p)]
 
 
+class qsv_teacher(ctypes.Structure):
+    _fields_ = [("n_top", ctypes.c_int32), ("reserved", ctypes.c_int32), ("top_idx_dev", ctypes.c_void_p),
+                ("top_logits_dev", ctypes.c_void_p), ("top_lse_dev", ctypes.c_void_p), ("temperature", ctypes.c_double)]
+
+
+class qsv_distill_req(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("have_stats", ctypes.c_int32), ("scores_dev", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("loss_dev", ctypes.c_void_p), ("stats_dev", ctypes.c_void_p), ("grad_loss_dev", ctypes.c_void_p),
+                ("grad_dev", ctypes.c_void_p), ("grad_stride", ctypes.c_int64)]
+
+
 class QsvError(RuntimeError):
     def __init__(self, status, message):
         super().__init__("qsv status %d: %s" % (status, message))
@@ -109,6 +121,13 @@ def load():
     L.qsv_reset_fidelity.argtypes = [vp, ctypes.POINTER(qsv_circuit), vp, vp, ctypes.c_uint64, vp, i64, vp]
     L.qsv_shot_expz.restype = i32
     L.qsv_shot_expz.argtypes = [vp, vp, i64, vp]
+    L.qsv_distill_workspace_bytes.restype = ctypes.c_size_t
+    L.qsv_distill_workspace_bytes.argtypes = [i64, i64]
+    L.qsv_distill.restype = i32
+    L.qsv_distill.argtypes = [vp, ctypes.POINTER(qsv_distill_req), ctypes.POINTER(qsv_teacher)]
+    L.qsv_distill_grad.restype = i32
+    L.qsv_distill_grad.argtypes = [vp, ctypes.POINTER(qsv_circuit), vp, i64, vp, vp, ctypes.POINTER(qsv_teacher),
+                                   vp, vp, vp, vp]
     L.qsv_sample_workspace_bytes.restype = ctypes.c_size_t
     L.qsv_sample_workspace_bytes.argtypes = [i64, i64]
     L.qsv_sample.restype = i32
@@ -157,6 +176,10 @@ def qsv_sample_workspace_bytes(rows, cols):
     return int(load().qsv_sample_workspace_bytes(rows, cols))
 
 
+def qsv_distill_workspace_bytes(rows, cols):
+    return int(load().qsv_distill_workspace_bytes(rows, cols))
+
+
 def qsv_plan_describe(circ, n, batch=1, inverse=0, tile_log2=0):
     L = load()
     need = L.qsv_plan_describe(ctypes.byref(circ), n, batch, inverse, tile_log2, None, 0)
@@ -186,6 +209,12 @@ def _flat(t, dtype, *shape):
         return None
     assert t.is_cuda and str(t.dtype) == "torch." + dtype and tuple(t.shape) == shape and t.is_contiguous(), (dtype, shape)
     return t.data_ptr()
+
+
+def _teacher(rows, top_idx, top_logits, temperature, top_lse):
+    top = top_idx.shape[1]
+    return qsv_teacher(top, 0, _flat(top_idx, "int32", rows, top), _flat(top_logits, "float32", rows, top),
+                       _flat(top_lse, "float32", rows), float(temperature))
 
 
 class Context:
@@ -266,6 +295,26 @@ class Context:
         self._check(self.L.qsv_loss_grad(self.h, ctypes.byref(circ), _ptr(x), x.shape[1], _ptr(params),
                                          _ptr(feats), ctypes.byref(spec), _ptr(loss), _ptr(grad),
                                          _ptr(mean_loss), _ptr(mean_grad)))
+
+    def qsv_distill(self, kind, scores, top_idx, top_logits, temperature=1.0, top_lse=None, loss=None, stats=None,
+                    have_stats=0, grad_loss=None, grad=None):
+        s = _rows(scores, kind)
+        r = qsv_distill_req()
+        r.kind, r.have_stats, r.scores_dev, r.row_stride = kind, have_stats, s.data_ptr(), s.stride(0)
+        r.rows, r.cols = s.shape
+        r.loss_dev, r.stats_dev = _flat(loss, "float32", r.rows), _flat(stats, "float32", r.rows, 2)
+        r.grad_loss_dev = _flat(grad_loss, "float32", r.rows)
+        if grad is not None:
+            assert _rows(grad, kind).shape == s.shape
+            r.grad_dev, r.grad_stride = grad.data_ptr(), grad.stride(0)
+        t = _teacher(r.rows, top_idx, top_logits, temperature, top_lse)
+        self._check(self.L.qsv_distill(self.h, ctypes.byref(r), ctypes.byref(t)))
+
+    def qsv_distill_grad(self, circ, x, params, feats, top_idx, top_logits, loss, grad, mean_loss=None, mean_grad=None,
+                         temperature=1.0, top_lse=None):
+        t = _teacher(self.batch, top_idx, top_logits, temperature, top_lse)
+        self._check(self.L.qsv_distill_grad(self.h, ctypes.byref(circ), _ptr(x), x.shape[1], _ptr(params), _ptr(feats),
+                                            ctypes.byref(t), _ptr(loss), _ptr(grad), _ptr(mean_loss), _ptr(mean_grad)))
 
     def qsv_reset_fidelity(self, circ, params, feats, mask, x, out):
         self._check(self.L.qsv_reset_fidelity(self.h, ctypes.byref(circ), _ptr(params), _ptr(feats), mask,

@@ -9,8 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqsv.so")
-SOURCES = ["qsv_api.cpp", "qsv_plan.cpp", "qsv_kernels.hip", "qsv_sample.hip"]
-HEADERS = ["qsv_plan.h", "qsv_lower.h", "qsv_kernels.h", "qsv_scores.h", "qsv_requests.h", "gen_gate_asm.py", os.path.join(ROOT, "include", "qsv.h")]
+SOURCES = ["qsv_api.cpp", "qsv_plan.cpp", "qsv_kernels.hip", "qsv_sample.hip", "qsv_distill.hip"]
+HEADERS = ["qsv_plan.h", "qsv_lower.h", "qsv_kernels.h", "qsv_scores.h", "qsv_requests.h", "qsv_wave.h", "gen_gate_asm.py", os.path.join(ROOT, "include", "qsv.h")]
 
 
 def hipcc():

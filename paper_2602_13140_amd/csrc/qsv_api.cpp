@@ -1446,8 +1446,25 @@ struct Fork {
     }
 };
 
-// What reverse mode differentiates: kind 0 <Z_q>; 1 the loss 1 - P0(mask); 2 the mean squared error of <Z_q> against targets.
-struct Objective { int kind, q; uint64_t mask; const float* targets; };
+static TeacherArgs to_dev(const qsv_teacher& t) {
+    return TeacherArgs{t.top_idx_dev, t.top_logits_dev, t.top_lse_dev, t.n_top, 1.0 / t.temperature};
+}
+
+// What reverse mode differentiates: kind 0 <Z_q>; 1 the loss 1 - P0(mask); 2 the mean squared error of <Z_q> against targets;
+// 3 the loss against a teacher's top logits.
+struct Objective {
+    int kind, q;
+    uint64_t mask;
+    const float* targets;
+    TeacherArgs teacher{};
+    TeacherArgs teacher_of(int64_t sample) const {      // from this sample on
+        TeacherArgs t = teacher;
+        t.idx += sample * t.top;
+        t.logits += sample * t.top;
+        if (t.lse) t.lse += sample;
+        return t;
+    }
+};
 
 // The losses of rows 0 .. rows - 1 of A (samples sample0 + row) into f[sample][2P]; kind 2 also the coefficients of lambda.
 // res, rowdep: see launch_expz_finish; of row 0's sample on.
@@ -1455,6 +1472,12 @@ static qsv_status losses(qsv_ctx* ctx, const Objective& ob, const float2* A, int
                          double* zpart, double* zall, double* coef, double* f, const Residues* res = nullptr,
                          int rowdep = 0) {
     const int n = ctx->n;
+    if (ob.kind == 3) {
+        QSV_HIP(ctx, launch_distill_state(A, n, ob.teacher_of(sample0), rows, f + sample0 * (2 * P + 1) + 2 * P, 2 * P + 1,
+                                          nullptr, 0, ctx->stream),
+                "distillation loss");
+        return QSV_OK;
+    }
     if (ob.kind == 1) {
         QSV_HIP(ctx, launch_trash_loss(A, n, ob.mask, rows, sample0, P, zpart, f, ctx->stream, res, rowdep), "trash loss");
         return QSV_OK;
@@ -1495,7 +1518,7 @@ static qsv_status fused_sweep(qsv_ctx* ctx, const qsv_circuit& c, const Objectiv
     const size_t state_bytes = (size_t)8 << n;
     const size_t sums_bytes = pair_sums_bytes(n, per), zbytes = (size_t)chunk_blocks(n) * 13 * 8;
     auto sample_bytes = [&](size_t passes) {
-        return (passes + 1) * state_bytes + sums_bytes + zbytes + 2 * (size_t)n * 8;
+        return (passes + 1 + (ob.kind == 3)) * state_bytes + sums_bytes + zbytes + 2 * (size_t)n * 8;
     };
     // a table: the unitaries and at most as many groups' scalars, and one entry that is only prefetched
     const size_t table_bytes = 2 * mats_table_bytes(c, n, B), corr_bytes = mat_scale_bytes(to_dev(c, n), B);
@@ -1532,7 +1555,7 @@ static qsv_status fused_sweep(qsv_ctx* ctx, const qsv_circuit& c, const Objectiv
     double* residues = (double*)ar.take(corr_bytes);
     struct Scratch { float2* psi; float* sums; double *zpart, *zall, *coef; } scr[2];
     for (int i = 0; i < sets; ++i) {
-        scr[i].psi = (float2*)ar.take((passes + 1) * (size_t)chunk * state_bytes);
+        scr[i].psi = (float2*)ar.take((passes + 1 + (ob.kind == 3)) * (size_t)chunk * state_bytes);
         scr[i].sums = (float*)ar.take((size_t)chunk * sums_bytes);
         scr[i].zpart = (double*)ar.take((size_t)chunk * zbytes);
         scr[i].zall = (double*)ar.take((size_t)chunk * n * 8);
@@ -1590,7 +1613,12 @@ static qsv_status fused_sweep(qsv_ctx* ctx, const qsv_circuit& c, const Objectiv
         qsv_status s = losses(ctx, ob, state(passes), rows, b0, P, sc.zpart, sc.zall, sc.coef, f, &through, c.reupload);
         if (s != QSV_OK) return s;
         // backwards: lambda changes between the encoded states' buffer and the last states', whose pass comes first
-        const float2* lam = nullptr;
+        const float2* lam = nullptr;       // the first pass forms it from psi, or finds it in a state of its own
+        if (ob.kind == 3) {
+            QSV_HIP(ctx, launch_distill_state(state(passes), n, ob.teacher_of(b0), rows, nullptr, 0, state(passes + 1), 0, ctx->stream),
+                    "lambda of the distillation loss");
+            lam = state(passes + 1);
+        }
         for (size_t k = 0; k < passes; ++k) {
             const Pass& ps = bp->plan.passes[k];
             const DirectPass& low = bp->low_ops.passes[k];
@@ -1637,7 +1665,7 @@ static qsv_status fused_sweep(qsv_ctx* ctx, const qsv_circuit& c, const Objectiv
 static qsv_status adjoint_impl(qsv_ctx* ctx, const qsv_circuit* c, const float* x_dev, int64_t dim,
                                const float* params_dev, const float* feats_dev, int kind, int32_t obs_qubit,
                                uint64_t mask, const float* targets_dev, float* loss_dev, float* grad_dev,
-                               float* mean_loss_dev, float* mean_grad_dev) {
+                               float* mean_loss_dev, float* mean_grad_dev, const qsv_teacher* teacher = nullptr) {
     if (!ctx) return QSV_ERR_INVALID_ARG;
     std::string why;
     if (!check_circuit(c, ctx->n, &why)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
@@ -1649,6 +1677,8 @@ static qsv_status adjoint_impl(qsv_ctx* ctx, const qsv_circuit* c, const float* 
     if (kind == 1 && (mask == 0 || (mask >> n) != 0))
         return fail(ctx, QSV_ERR_INVALID_ARG, "mask must name at least one qubit and none beyond n_qubits");
     if (kind == 2 && !targets_dev) return fail(ctx, QSV_ERR_INVALID_ARG, "targets_dev is NULL");
+    if (kind == 3)
+        if (const char* bad = check_teacher(teacher)) return fail(ctx, QSV_ERR_INVALID_ARG, bad);
     const int64_t P = qsv_num_params(c, n);
     if (P > 0 && !params_dev) return fail(ctx, QSV_ERR_INVALID_ARG, "params_dev is NULL");
     if (c->reupload && !feats_dev) return fail(ctx, QSV_ERR_INVALID_ARG, "reupload = 1 needs feats_dev");
@@ -1681,7 +1711,8 @@ static qsv_status adjoint_impl(qsv_ctx* ctx, const qsv_circuit* c, const float* 
     const size_t tables = mats_bytes(*c, n, B);
     const bool keep = ctx->opt_grad_layered && P > 0 &&
                       ar.remaining() >= align_up(ckpt_bytes) + state_bytes + small_bytes + 2 * tables + 2 * kAlign;
-    const Objective ob{kind, obs_qubit, mask, targets_dev};
+    Objective ob{kind, obs_qubit, mask, targets_dev};
+    if (kind == 3) ob.teacher = to_dev(*teacher);
     auto fused = [&](bool* done) -> qsv_status {
         Arena fs = ar;       // what is taken here is given back if it does not fit
         qsv_status s = fused_sweep(ctx, *c, ob, x_dev, dim, params_dev, feats_dev, npart, nblk, inv, f, fs, done);
@@ -1699,7 +1730,7 @@ static qsv_status adjoint_impl(qsv_ctx* ctx, const qsv_circuit* c, const float* 
     }
     // Small states: the whole sweep in one launch, where the scratch has room for its sums.  It keeps psi too where there
     // is room: the gradient is then no further from 64 bits than layer by layer (psi taken back 1.2 to 1.6 times).
-    if (ctx->opt_small_apply != 0 && n <= kSmallMaxQubits && P > 0 && ctx->opt_tile == 0 && !ctx->opt_naive &&
+    if (kind != 3 && ctx->opt_small_apply != 0 && n <= kSmallMaxQubits && P > 0 && ctx->opt_tile == 0 && !ctx->opt_naive &&
         ctx->opt_grad_layered && ctx->opt_grad_chunk == 0 && (int64_t)L * n <= kSmallMats) {
         Arena sm = ar;       // what is taken here is given back if it does not fit
         float* mats = (float*)sm.take(mats_table_bytes(*c, n, B));
@@ -1801,8 +1832,12 @@ static qsv_status adjoint_impl(qsv_ctx* ctx, const qsv_circuit* c, const float* 
         if (st != QSV_OK) return st;
         if (P == 0) return QSV_OK;
         // backward: lambda = O psi (and psi beside it unless its states were kept), taken back layer by layer
-        QSV_HIP(ctx, launch_adj_init(A, n, kind, obs_qubit, mask, sc.coef, bc, sc.S, keep ? 0 : 1, ctx->stream),
-                "adjoint init");
+        if (kind == 3)
+            QSV_HIP(ctx, launch_distill_state(A, n, ob.teacher_of(b0), bc, nullptr, 0, sc.S, keep ? 0 : 1, ctx->stream),
+                    "adjoint init");
+        else
+            QSV_HIP(ctx, launch_adj_init(A, n, kind, obs_qubit, mask, sc.coef, bc, sc.S, keep ? 0 : 1, ctx->stream),
+                    "adjoint init");
         RowMap rm2 = rm1;
         if (!keep) {
             rm2.per = 2;
@@ -1871,6 +1906,44 @@ qsv_status qsv_loss_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_dev,
         return fail(ctx, QSV_ERR_INVALID_ARG, "unknown loss kind");
     return adjoint_impl(ctx, c, x_dev, dim, params_dev, feats_dev, loss->kind == QSV_LOSS_TRASH ? 1 : 2, 0,
                         loss->mask, loss->targets_dev, loss_dev, grad_dev, mean_loss_dev, mean_grad_dev);
+}
+
+// The workspace of qsv_distill behind the plans' region.
+size_t qsv_distill_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || rows > kMostRows || cols < 1 || cols > kMostCols) return 0;
+    return kOpsRegion + align_up(distill_scratch_bytes(rows, cols));
+}
+
+qsv_status qsv_distill(qsv_ctx* ctx, const qsv_distill_req* req, const qsv_teacher* teacher) {
+    if (!ctx) return QSV_ERR_INVALID_ARG;
+    if (const char* why = check_distill(req, teacher)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    if (req->rows == 0 || !(req->loss_dev || req->grad_dev || (req->stats_dev && !req->have_stats))) return QSV_OK;
+    qsv_status st = bind_device(ctx);
+    if (st != QSV_OK) return st;
+    DistillArgs a{};
+    a.scores = req->scores_dev;
+    a.rows = req->rows;
+    a.stride = req->rows > 1 ? req->row_stride : req->cols;
+    a.cols = (uint32_t)req->cols;
+    a.teacher = to_dev(*teacher);
+    a.loss = req->loss_dev;
+    a.stats = req->stats_dev;
+    a.have_stats = req->have_stats;
+    a.grad_loss = req->grad_loss_dev;
+    a.grad = req->grad_dev;
+    a.grad_stride = req->rows > 1 ? req->grad_stride : req->cols;
+    Arena ar(ctx);
+    void* scratch = ar.take(distill_scratch_bytes(req->rows, req->cols));
+    if (!scratch) return ws_fail(ctx, ar, "qsv_distill");
+    QSV_HIP(ctx, launch_distill(req->kind, a, scratch, ctx->stream), "distill");
+    return QSV_OK;
+}
+
+qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_dev, int64_t dim, const float* params_dev,
+                            const float* feats_dev, const qsv_teacher* teacher, float* loss_dev, float* grad_dev,
+                            float* mean_loss_dev, float* mean_grad_dev) {
+    return adjoint_impl(ctx, c, x_dev, dim, params_dev, feats_dev, 3, 0, 0, nullptr, loss_dev, grad_dev, mean_loss_dev,
+                        mean_grad_dev, teacher);
 }
 
 qsv_status qsv_sgd_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev, int64_t count, double lr) {

@@ -1,0 +1,510 @@
+// Loss of rows of scores against a teacher known by its top logits, and its gradient.
+//
+//   q_j = exp(t_j / T - norm) over the teacher's entries, Q = sum q;  p = softmax(z / T)
+//   L = sum_j q_j (ln q_j - ln p_{i_j}) = sum_j q_j (t_j / T - norm) - sum_j q_j (z_{i_j} - m) / T + Q ln s
+//   dL/dz_k = (Q e_k / s - sum_{j: i_j = k} q_j) / T,  e_k = exp((z_k - m) / T), m = max z, s = sum e
+//
+// Bound by memory: a row is read once and its gradient written once.  A workgroup keeps its row in registers between the
+// maximum, the sum and the gradient (16 vectors of 16 bytes a thread: up to 131072 values of 16 bits, 65536 of 32); longer
+// rows are read again for the gradient.  The gradient is written as if no entry of the teacher were there, and the few
+// places of the entries are written once more after a barrier.
+//
+// Exponentials and the values they are taken of are in 32 bits, sums over a thread's values too; sums over threads, the
+// teacher's weights and the loss, a small difference of large numbers, in 64.
+#include "qsv_scores.h"
+#include "qsv_wave.h"
+
+#include <hip/hip_fp16.h>
+
+namespace qsv {
+namespace {
+
+typedef unsigned long long u64;
+typedef unsigned u32;
+constexpr float kInf = __builtin_inff();
+
+template <int KIND> constexpr int kPer = KIND == kScoreF32 ? 4 : 8;      // values of a vector
+template <int KIND> constexpr int kSize = KIND == kScoreF32 ? 4 : 2;
+template <int KIND> constexpr u32 kNone = KIND == kScoreF32 ? 0xff800000u : KIND == kScoreBF16 ? 0xff80ff80u : 0xfc00fc00u;   // -inf
+
+// Rows start anywhere an element may: vectors of 16 bytes at the element's alignment, which the memory pipeline takes.
+typedef u32 vec __attribute__((ext_vector_type(4)));
+typedef u32 vec_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef u32 vec_at4 __attribute__((ext_vector_type(4), aligned(4)));
+
+template <int KIND> __device__ __forceinline__ float value_at(const char* row, u32 k) {
+    if (KIND == kScoreF32) return ((const float*)row)[k];
+    if (KIND == kScoreF16) return __half2float(((const __half*)row)[k]);
+    return __uint_as_float((u32)((const unsigned short*)row)[k] << 16);
+}
+
+template <int KIND> __device__ __forceinline__ void store_one(char* row, u32 k, float v) {
+    if (KIND == kScoreF32) ((float*)row)[k] = v;
+    else if (KIND == kScoreF16) ((__half*)row)[k] = __float2half_rn(v);
+    else ((__bf16*)row)[k] = (__bf16)v;
+}
+
+// Vector j of a row; -inf behind the row's end.
+template <int KIND> __device__ __forceinline__ vec load_vec(const char* row, u32 cols, u32 j) {
+    constexpr int W = kPer<KIND>;
+    vec x = {kNone<KIND>, kNone<KIND>, kNone<KIND>, kNone<KIND>};
+    const u64 k0 = (u64)j * W;
+    if (k0 + W <= cols) {
+        if (KIND == kScoreF32) x = *(const vec_at4*)(row + k0 * 4);
+        else x = *(const vec_at2*)(row + k0 * 2);
+    } else if (k0 < cols) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (k0 + i < cols) {
+                if (KIND == kScoreF32) x[i] = ((const u32*)row)[k0 + i];
+                else x[i >> 1] = (i & 1) ? (x[i >> 1] & 0xffffu) | ((u32)((const unsigned short*)row)[k0 + i] << 16)
+                                         : (x[i >> 1] & 0xffff0000u) | ((const unsigned short*)row)[k0 + i];
+            }
+    }
+    return x;
+}
+
+template <int KIND> __device__ __forceinline__ float part(const vec& x, int i) {
+    if (KIND == kScoreF32) return __uint_as_float(x[i]);
+    const u32 two = x[i >> 1];
+    if (KIND == kScoreBF16) return __uint_as_float((i & 1) ? two & 0xffff0000u : two << 16);
+    return __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
+}
+
+template <int KIND> __device__ __forceinline__ void store_vec(char* row, u32 cols, u32 j, const float (&g)[kPer<KIND>]) {
+    constexpr int W = kPer<KIND>;
+    const u64 k0 = (u64)j * W;
+    if (k0 + W <= cols) {
+        vec x;
+        if (KIND == kScoreF32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(g[i]);
+            *(vec_at4*)(row + k0 * 4) = x;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (KIND == kScoreBF16) {
+                    typedef __bf16 two __attribute__((ext_vector_type(2)));
+                    const two b = {(__bf16)g[(2 * i) % W], (__bf16)g[(2 * i + 1) % W]};
+                    x[i] = __builtin_bit_cast(u32, b);
+                } else {
+                    x[i] = (u32)__half_as_ushort(__float2half_rn(g[(2 * i) % W])) | (u32)__half_as_ushort(__float2half_rn(g[(2 * i + 1) % W])) << 16;
+                }
+            }
+            *(vec_at2*)(row + k0 * 2) = x;
+        }
+    } else if (k0 < cols) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (k0 + i < cols) store_one<KIND>(row, (u32)(k0 + i), g[i]);
+    }
+}
+
+// ---- workgroups ------------------------------------------------------------------------------------------------------
+template <int NT> __device__ __forceinline__ float block_max(float v, double* sm) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    __syncthreads();
+    if (lane == 0) sm[wave] = v;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) v = fmaxf(v, (float)sm[i]);
+    return v;
+}
+
+template <int NT, int N> __device__ __forceinline__ void block_sums(double (&v)[N], double* sm) {     // sm: 16 N entries
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
+    __syncthreads();
+    if (lane == 0)
+#pragma unroll
+        for (int k = 0; k < N; ++k) sm[k * 16 + wave] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        v[k] = 0.0;
+        for (int i = 0; i < NT / 64; ++i) v[k] += sm[k * 16 + i];
+    }
+}
+
+// A row's teacher: idx, q and z of its entries in LDS, and their sums.
+struct Taught { double q, qx; };      // sum q, sum q (t / T - norm)
+struct TeacherLds { int* idx; float *q, *z; };
+
+__device__ __forceinline__ TeacherLds teacher_lds(char* lds, int top) {
+    TeacherLds t;
+    t.idx = (int*)lds;
+    t.q = (float*)lds + top;
+    t.z = (float*)lds + 2 * top;
+    return t;
+}
+
+// LISTED: `row` holds the scores at the entries, in their order.
+template <int KIND, int NT, bool LISTED = false> __device__ __forceinline__ Taught teach(const TeacherArgs& a, u64 r, const char* row, u32 cols, const TeacherLds& l, double* sm) {
+    const int* idx = a.idx + r * a.top;
+    const float* logits = a.logits + r * a.top;
+    float high = -kInf;
+    for (int j = threadIdx.x; j < a.top; j += NT) {
+        const int i = idx[j];
+        const bool real = i >= 0 && (u32)i < cols;
+        const float t = logits[j];
+        l.idx[j] = real ? i : -1;
+        l.z[j] = real ? value_at<KIND>(row, LISTED ? (u32)j : (u32)i) : 0.f;
+        l.q[j] = t;
+        if (real) high = fmaxf(high, t);
+    }
+    double norm;
+    if (a.lse) {
+        norm = (double)a.lse[r];
+    } else {
+        high = block_max<NT>(high, sm);
+        const double top = high > -kInf ? (double)high * a.inv_t : 0.0;
+        double s[1] = {0.0};
+        for (int j = threadIdx.x; j < a.top; j += NT)
+            if (l.idx[j] >= 0) s[0] += exp((double)l.q[j] * a.inv_t - top);
+        block_sums<NT, 1>(s, sm);
+        norm = top + log(s[0]);              // no entry: -inf, and every q below 0
+    }
+    double v[2] = {0.0, 0.0};
+    for (int j = threadIdx.x; j < a.top; j += NT) {
+        const double x = (double)l.q[j] * a.inv_t - norm;
+        const double q = l.idx[j] >= 0 && l.q[j] != -kInf ? exp(x) : 0.0;
+        if (q != 0.0) {
+            v[0] += q;
+            v[1] += q * x;
+        }
+        l.q[j] = (float)q;
+    }
+    block_sums<NT, 2>(v, sm);
+    return Taught{v[0], v[1]};
+}
+
+// The thread's part of sum q (z - m) / T: differences first, scores may be large.
+template <int NT> __device__ __forceinline__ double below_top(const TeacherLds& l, int top, float m, double inv_t) {
+    double v = 0.0;
+    for (int j = threadIdx.x; j < top; j += NT)
+        if (l.q[j] != 0.f) v += l.z[j] == -kInf ? -(double)kInf : (double)l.q[j] * (((double)l.z[j] - (double)m) * inv_t);
+    return v;
+}
+
+// A row's loss from its statistics.  below: the sum over all threads.
+__device__ __forceinline__ float loss_of(const Taught& t, double below, double s) {
+    if (t.q == 0.0) return 0.f;
+    if (below == -(double)kInf && s == s) return kInf;         // an entry that the student excludes
+    return (float)(t.qx - below + t.q * log(s));
+}
+
+struct Gradient { float m, c, scale, of_q; };      // scale: of e; of_q: of q
+
+// e_k times scale is the gradient where the teacher has no entry.
+__device__ __forceinline__ Gradient gradient_of(const Taught& t, float m, double s, double inv_t, float grad_loss) {
+    Gradient g;
+    g.m = m > -kInf ? m : 0.f;
+    g.c = (float)(1.4426950408889634074 * inv_t);
+    const double by = t.q != 0.0 ? (double)grad_loss * inv_t : 0.0;
+    g.scale = s > 0.0 || s != s ? (float)(by * t.q / s) : 0.f;
+    g.of_q = (float)by;
+    return g;
+}
+
+__device__ __forceinline__ float e_of(const Gradient& g, float z) { return __builtin_amdgcn_exp2f((z - g.m) * g.c); }
+
+// The places of the teacher's entries between k0 and k1, once each, whichever entries name them.
+template <int KIND, int NT> __device__ __forceinline__ void write_entries(const TeacherLds& l, int top, const Gradient& g, char* grad, u32 k0, u32 k1) {
+    for (int j = threadIdx.x; j < top; j += NT) {
+        const int k = l.idx[j];
+        if (k < 0 || (u32)k < k0 || (u32)k >= k1) continue;
+        double q = 0.0;
+        bool first = true;
+        for (int i = 0; i < top; ++i)
+            if (l.idx[i] == k) {
+                if (i < j) { first = false; break; }
+                q += (double)l.q[i];
+            }
+        if (first) store_one<KIND>(grad, (u32)k, (float)((double)(e_of(g, l.z[j]) * g.scale) - q * (double)g.of_q));
+    }
+}
+
+// ---- one workgroup a row ---------------------------------------------------------------------------------------------
+template <int KIND, int NT, bool KEPT>
+__global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
+    constexpr int W = kPer<KIND>, NV = 16;
+    extern __shared__ char lds[];
+    __shared__ double sm[48];
+    const u64 r = grid_block();
+    if (r >= (u64)a.rows) return;
+    const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
+    const TeacherLds l = teacher_lds(lds, a.teacher.top);
+    const u32 vecs = (u32)(((u64)a.cols + W - 1) / W);
+    const float c = (float)(1.4426950408889634074 * a.teacher.inv_t);
+    vec x[KEPT ? NV : 1];
+    float m = -kInf, sum = 0.f;
+    if (KEPT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] = load_vec<KIND>(row, a.cols, (u32)i * NT + threadIdx.x);
+    }
+    const Taught t = teach<KIND, NT>(a.teacher, r, row, a.cols, l, sm);
+    if (KEPT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < W; ++k) m = fmaxf(m, part<KIND>(x[i], k));
+        m = block_max<NT>(m, sm);
+        const float base = m > -kInf ? m : 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float four = 0.f;
+#pragma unroll
+            for (int k = 0; k < W; ++k) four += __builtin_amdgcn_exp2f((part<KIND>(x[i], k) - base) * c);
+            sum += four;
+        }
+    } else {
+        // the thread's own maximum so far, and the sum relative to it
+        for (u32 j = threadIdx.x; j < vecs; j += NT) {
+            const vec y = load_vec<KIND>(row, a.cols, j);
+            float high = m;
+#pragma unroll
+            for (int k = 0; k < W; ++k) high = fmaxf(high, part<KIND>(y, k));
+            const float base = high > -kInf ? high : 0.f;
+            sum *= high > m ? __builtin_amdgcn_exp2f((m - high) * c) : 1.f;
+            m = high;
+            float four = 0.f;
+#pragma unroll
+            for (int k = 0; k < W; ++k) four += __builtin_amdgcn_exp2f((part<KIND>(y, k) - base) * c);
+            sum += four;
+        }
+        const float own = m;
+        m = block_max<NT>(m, sm);
+        if (own < m) sum *= __builtin_amdgcn_exp2f((own - m) * c);
+    }
+    double s[2] = {(double)sum, a.loss ? below_top<NT>(l, a.teacher.top, m, a.teacher.inv_t) : 0.0};
+    block_sums<NT, 2>(s, sm);
+    if (threadIdx.x == 0) {
+        if (a.loss) a.loss[r] = loss_of(t, s[1], s[0]);
+        if (a.stats) { a.stats[2 * r] = m; a.stats[2 * r + 1] = (float)s[0]; }
+    }
+    if (!a.grad) return;
+    char* grad = (char*)a.grad + r * (u64)a.grad_stride * kSize<KIND>;
+    const Gradient g = gradient_of(t, m, s[0], a.teacher.inv_t, a.grad_loss ? a.grad_loss[r] : 1.f);
+    const bool zero = t.q == 0.0;
+    auto write = [&](u32 j, const vec& y) {
+        float o[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) o[k] = zero ? 0.f : e_of(g, part<KIND>(y, k)) * g.scale;
+        store_vec<KIND>(grad, a.cols, j, o);
+    };
+    if (KEPT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) write((u32)i * NT + threadIdx.x, x[i]);
+    } else {
+        for (u32 j = threadIdx.x; j < vecs; j += NT) write(j, load_vec<KIND>(row, a.cols, j));
+    }
+    if (zero) return;
+    __syncthreads();       // the entries' places are written a second time
+    write_entries<KIND, NT>(l, a.teacher.top, g, grad, 0, a.cols);
+}
+
+// ---- few rows, or a gradient from kept statistics: parts of rows by workgroups of their own -------------------------
+constexpr int kPartThreads = 256, kPartVecs = 8;       // a part: 8 vectors a thread
+
+struct Parts {
+    u32 parts;
+    float* part;          // [rows][parts][2]: maximum, sum relative to it
+    float* z;             // [rows][top]: the scores at the teacher's entries
+};
+
+template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_stats(const DistillArgs a, const Parts p) {
+    constexpr int W = kPer<KIND>;
+    __shared__ double sm[16];
+    const u64 r = grid_block() / p.parts;
+    const u32 at = (u32)(grid_block() % p.parts);
+    if (r >= (u64)a.rows) return;
+    const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
+    const u32 j0 = at * (kPartThreads * kPartVecs) + threadIdx.x;
+    const float c = (float)(1.4426950408889634074 * a.teacher.inv_t);
+    vec x[kPartVecs];
+#pragma unroll
+    for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, a.cols, j0 + (u32)i * kPartThreads);
+    if (at == 0) {
+        // (the gradient may be written over the scores)
+        for (int j = threadIdx.x; j < a.teacher.top; j += kPartThreads) {
+            const int i = a.teacher.idx[r * a.teacher.top + j];
+            p.z[r * a.teacher.top + j] = i >= 0 && (u32)i < a.cols ? value_at<KIND>(row, (u32)i) : 0.f;
+        }
+    }
+    float m = -kInf, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPartVecs; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) m = fmaxf(m, part<KIND>(x[i], k));
+    m = block_max<kPartThreads>(m, sm);
+    const float base = m > -kInf ? m : 0.f;
+#pragma unroll
+    for (int i = 0; i < kPartVecs; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) sum += __builtin_amdgcn_exp2f((part<KIND>(x[i], k) - base) * c);
+    double s[1] = {(double)sum};
+    block_sums<kPartThreads, 1>(s, sm);
+    if (threadIdx.x == 0) {
+        p.part[(r * p.parts + at) * 2] = m;
+        p.part[(r * p.parts + at) * 2 + 1] = (float)s[0];
+    }
+}
+
+template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_apply(const DistillArgs a, const Parts p, u32 blocks) {
+    constexpr int W = kPer<KIND>;
+    extern __shared__ char lds[];
+    __shared__ double sm[48];
+    const u64 r = grid_block() / blocks;
+    const u32 at = (u32)(grid_block() % blocks);
+    if (r >= (u64)a.rows) return;
+    const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
+    const TeacherLds l = teacher_lds(lds, a.teacher.top);
+    const u32 j0 = at * (kPartThreads * kPartVecs) + threadIdx.x;
+    vec x[kPartVecs];
+    if (a.grad) {
+#pragma unroll
+        for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, a.cols, j0 + (u32)i * kPartThreads);
+    }
+    // (the scores at the entries: kept ones where the gradient of another part may be written over them)
+    const Taught t = p.z ? teach<kScoreF32, kPartThreads, true>(a.teacher, r, (const char*)(p.z + r * a.teacher.top), a.cols, l, sm)
+                         : teach<KIND, kPartThreads>(a.teacher, r, row, a.cols, l, sm);
+    float m = -kInf;
+    double s[2] = {0.0, 0.0};
+    if (a.have_stats) {
+        m = a.stats[2 * r];
+        s[0] = (double)a.stats[2 * r + 1];
+    } else {
+        const float* q = p.part + r * p.parts * 2;
+        for (u32 i = threadIdx.x; i < p.parts; i += kPartThreads) m = fmaxf(m, q[2 * i]);
+        m = block_max<kPartThreads>(m, sm);
+        for (u32 i = threadIdx.x; i < p.parts; i += kPartThreads)
+            if (q[2 * i + 1] != 0.f) s[0] += (double)q[2 * i + 1] * exp(((double)q[2 * i] - (double)m) * a.teacher.inv_t);
+        if (a.loss) s[1] = below_top<kPartThreads>(l, a.teacher.top, m, a.teacher.inv_t);
+        block_sums<kPartThreads, 2>(s, sm);
+    }
+    if (at == 0 && threadIdx.x == 0) {
+        if (a.loss) a.loss[r] = loss_of(t, s[1], s[0]);
+        if (a.stats && !a.have_stats) { a.stats[2 * r] = m; a.stats[2 * r + 1] = (float)s[0]; }
+    }
+    if (!a.grad) return;
+    char* grad = (char*)a.grad + r * (u64)a.grad_stride * kSize<KIND>;
+    const Gradient g = gradient_of(t, m, s[0], a.teacher.inv_t, a.grad_loss ? a.grad_loss[r] : 1.f);
+    const bool zero = t.q == 0.0;
+#pragma unroll
+    for (int i = 0; i < kPartVecs; ++i) {
+        float o[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) o[k] = zero ? 0.f : e_of(g, part<KIND>(x[i], k)) * g.scale;
+        store_vec<KIND>(grad, a.cols, j0 + (u32)i * kPartThreads, o);
+    }
+    if (zero) return;
+    __syncthreads();
+    const u64 k0 = (u64)at * (kPartThreads * kPartVecs * W);
+    write_entries<KIND, kPartThreads>(l, a.teacher.top, g, grad, (u32)k0, (u32)min(k0 + kPartThreads * kPartVecs * W, (u64)a.cols));
+}
+
+// ---- a circuit's own outcomes ----------------------------------------------------------------------------------------
+// The loss of rows of amplitudes a against the teacher, with p_k = |a_k|^2, and lambda_k = dL/dp_k a_k = -q_k a_k / p_k at
+// the entries, which reverse mode takes back.  (The derivative of the rows' norm is left out: no gate changes it.)  A row's
+// entries are few: a workgroup each, bound by the latency of gathering them.
+// lambda: NULL, or rows of 2^n that are zero, `per` rows apart, the first one `first` rows on.
+__global__ __launch_bounds__(256) void k_distill_state(const float2* A, int n, TeacherArgs te, u64 rows, double* f, u64 f_stride, float2* lambda, int per, int first) {
+    extern __shared__ char lds[];
+    __shared__ double sm[48];
+    const u64 r = grid_block();
+    if (r >= rows) return;
+    const float2* a = A + (r << n);
+    const u32 cols = 1u << n;
+    const TeacherLds l = teacher_lds(lds, te.top);
+    const Taught t = teach<kScoreF32, 256, true>(te, r, (const char*)(te.logits + r * te.top), cols, l, sm);
+    double loss[1] = {0.0};
+    for (int j = threadIdx.x; j < te.top; j += 256) {
+        const int k = l.idx[j];
+        if (k < 0 || l.q[j] == 0.f) continue;
+        const float2 z = a[k];
+        const double pk = (double)z.x * z.x + (double)z.y * z.y;
+        loss[0] -= (double)l.q[j] * log(pk);
+        if (!lambda) continue;
+        double q = 0.0;
+        bool once = true;
+        for (int i = 0; i < te.top; ++i)
+            if (l.idx[i] == k) {
+                if (i < j && l.q[i] != 0.f) { once = false; break; }
+                q += (double)l.q[i];
+            }
+        if (once) {
+            const double by = pk > 0.0 ? -q / pk : 0.0;
+            lambda[((r * (u64)per + (u64)first) << n) + (u64)k] = make_float2((float)(by * z.x), (float)(by * z.y));
+        }
+    }
+    block_sums<256, 1>(loss, sm);
+    if (threadIdx.x == 0 && f) f[r * f_stride] = t.q == 0.0 ? 0.0 : t.qx + loss[0];
+}
+
+// lambda's rows at zero, and (paired) psi beside them: rows 2r, 2r + 1.
+__global__ __launch_bounds__(256) void k_distill_zero(const float2* A, int n, u64 total, float2* S, int paired) {
+    const u64 e = grid_block() * 256 + threadIdx.x;
+    if (e >= total) return;
+    if (!paired) { S[e] = make_float2(0.f, 0.f); return; }
+    const u64 r = e >> n, k = e & ((1ull << n) - 1);
+    S[((2 * r) << n) | k] = A[e];
+    S[((2 * r + 1) << n) | k] = make_float2(0.f, 0.f);
+}
+
+}  // namespace
+
+static u64 part_values(int kind) { return (u64)kPartThreads * kPartVecs * (kind == kScoreF32 ? 4 : 8); }
+static u64 parts_of(int kind, int64_t cols) { return ((u64)cols + part_values(kind) - 1) / part_values(kind); }
+
+// Rows that would leave most of the chip idle, and are long enough to be split.
+static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 128 && parts_of(kind, cols) > 2; }
+
+size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
+    if (rows < 1 || !takes_parts(kScoreF32, rows, cols)) return 0;
+    return (size_t)rows * parts_of(kScoreF32, cols) * 8 + (size_t)rows * 1024 * 4;
+}
+
+template <int KIND> static hipError_t launch_kind(const DistillArgs& a, void* scratch, hipStream_t st) {
+    const size_t lds = (size_t)a.teacher.top * 12;
+    if (a.have_stats || takes_parts(KIND, a.rows, a.cols)) {
+        Parts p{};
+        p.parts = (u32)parts_of(KIND, a.cols);
+        const u32 blocks = a.grad ? p.parts : 1;
+        if (!a.have_stats) {
+            p.part = (float*)scratch;
+            p.z = p.part + (u64)a.rows * p.parts * 2;
+            hipLaunchKernelGGL(k_distill_stats<KIND>, grid_of((u64)a.rows * p.parts), dim3(kPartThreads), 0, st, a, p);
+        }
+        hipLaunchKernelGGL(k_distill_apply<KIND>, grid_of((u64)a.rows * blocks), dim3(kPartThreads), lds, st, a, p, blocks);
+        return hipGetLastError();
+    }
+    const u64 vecs = ((u64)a.cols + kPer<KIND> - 1) / kPer<KIND>;
+    const dim3 grid = grid_of((u64)a.rows);
+    if (vecs <= 64 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 64, true>), grid, dim3(64), lds, st, a);
+    else if (vecs <= 256 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 256, true>), grid, dim3(256), lds, st, a);
+    else if (vecs <= 512 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 512, true>), grid, dim3(512), lds, st, a);
+    else if (vecs <= 1024 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 1024, true>), grid, dim3(1024), lds, st, a);
+    else hipLaunchKernelGGL((k_distill_row<KIND, 1024, false>), grid, dim3(1024), lds, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_distill(int kind, const DistillArgs& a, void* scratch, hipStream_t st) {
+    switch (kind) {
+        case kScoreF32: return launch_kind<kScoreF32>(a, scratch, st);
+        case kScoreF16: return launch_kind<kScoreF16>(a, scratch, st);
+        case kScoreBF16: return launch_kind<kScoreBF16>(a, scratch, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_distill_state(const float2* A, int n, const TeacherArgs& te, int64_t rows, double* f, int64_t f_stride, float2* S, int paired, hipStream_t st) {
+    if (S) hipLaunchKernelGGL(k_distill_zero, grid_of((((u64)rows << n) + 255) / 256), dim3(256), 0, st, A, n, (u64)rows << n, S, paired);
+    hipLaunchKernelGGL(k_distill_state, grid_of((u64)rows), dim3(256), (size_t)te.top * 12, st, A, n, te, (u64)rows, f, (u64)f_stride, S,
+                       paired ? 2 : 1, paired ? 1 : 0);
+    return hipGetLastError();
+}
+
+}  // namespace qsv

@@ -9,10 +9,9 @@
 // Weights are whole numbers, rint(e 2^S) with e in 64 bits: their sums are the same in any order, so a call's results do
 // not depend on how its work was split or in which order atomics arrived.
 #include "qsv_scores.h"
+#include "qsv_wave.h"
 
 #include <hip/hip_fp16.h>
-
-#include <algorithm>
 
 namespace qsv {
 namespace {
@@ -186,27 +185,7 @@ template <int KIND, int NB> __device__ __forceinline__ u32 bin_of(const Scale& s
     return min((s.kmax - key) >> shift, (u32)(NB - 1));
 }
 
-// Workgroups are numbered over two grid dimensions (one holds less than 2^32 threads); the last ones may have no work.
-constexpr u64 kGridX = 1 << 20;
-__device__ __forceinline__ u64 grid_block() { return (u64)blockIdx.y * kGridX + blockIdx.x; }
-__host__ inline dim3 grid_of(u64 blocks) { return dim3((unsigned)std::min(blocks, kGridX), (unsigned)((blocks + kGridX - 1) / kGridX)); }
-
 // ---- wavefronts and workgroups ---------------------------------------------------------------------------------------
-template <class T> __device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
-template <class T> __device__ __forceinline__ T wave_scan(T v, int lane) {      // inclusive
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const T up = __shfl_up(v, o, 64);
-        if (lane >= o) v += up;
-    }
-    return v;
-}
-
 // Sums over the workgroup before each thread's own, and the whole sum.  sm: NT / 64 entries that nothing else uses.
 template <int NT> __device__ __forceinline__ u64 block_scan(u64 v, u64* sm, u64* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -31,4 +31,34 @@ struct SampleArgs {
 size_t sample_scratch_bytes(int64_t rows, int64_t cols);
 hipError_t launch_sample_scores(int kind, const SampleArgs& a, void* scratch, hipStream_t st);
 
+// A teacher's top logits of a row, and what they make of it.
+struct TeacherArgs {
+    const int* idx;              // [rows][top]
+    const float* logits;         // [rows][top]
+    const float* lse;            // [rows], or NULL: normalised over the entries given
+    int top;
+    double inv_t;                // 1 / T
+};
+
+struct DistillArgs {
+    const void* scores;
+    int64_t rows, stride;
+    uint32_t cols;
+    TeacherArgs teacher;
+    float* loss;                 // [rows] or NULL
+    float* stats;                // [rows][2] or NULL
+    int have_stats;              // stats are an input
+    const float* grad_loss;      // [rows] or NULL: 1
+    void* grad;                  // of the scores' type, or NULL
+    int64_t grad_stride;
+};
+
+size_t distill_scratch_bytes(int64_t rows, int64_t cols);
+hipError_t launch_distill(int kind, const DistillArgs& a, void* scratch, hipStream_t st);
+
+// Rows of 2^n amplitudes against a teacher (its arrays start at the first of them): the loss of row r to f[r * f_stride]
+// (f may be NULL), and, where S is not NULL, lambda to S: row r, or (paired) psi to row 2r and lambda to row 2r + 1.
+hipError_t launch_distill_state(const float2* A, int n, const TeacherArgs& te, int64_t rows, double* f, int64_t f_stride,
+                                float2* S, int paired, hipStream_t st);
+
 }  // namespace qsv

@@ -1,0 +1,516 @@
+"""qsv_distill and qsv_distill_grad against their formulas in 64 bits.
+
+Errors that the kernels may make, for scores whose highest lies d / T above the lowest that counts:
+  e_k   the difference, its scale and the product are rounded (3 steps of 2^-24 of an exponent of at most D = min(d / T,
+        104) in units of e: beyond, e_k is below 2^-149) and the exponential itself is good to 2 units of 2^-24
+        -> relative DELTA_E = (3 D + 2) 2^-24
+  s     a thread adds at most N = 16 * 8 values (longer rows: cols / 1024), each partial sum rounded once
+        -> relative DELTA_S = DELTA_E + N 2^-24
+  loss  Q ln s is off by Q DELTA_S, q by 2^-24 of itself (its logarithms by as much); rounded once to float32
+  gradient  g / T (Q e / s - q): the first product by DELTA_E + DELTA_S + 4 2^-24, the second by 2 2^-24, and one rounding to the
+        type: half a step, or half its smallest number"""
+import ctypes
+import math
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2602_13140_amd import binding as qb
+from paper_2602_13140_amd import workloads as wl
+from tests import gpu_util as gu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+INF, NAN = math.inf, math.nan
+U = 2.0 ** -24
+RX, RY, RZ = 1, 2, 3
+NONE, RING, LADDER = 0, 1, 2
+
+
+# ---- the formulas ----------------------------------------------------------------------------------------------------
+def teacher_q(idx, logits, lse, t, cols):
+    """q of every entry and (t_j / T - norm), one row."""
+    real = (idx >= 0) & (idx < cols) & (logits > -INF)
+    x = logits.astype(np.float64) / t
+    if lse is None:
+        norm = np.logaddexp.reduce(x[real]) if real.any() else 0.0
+    else:
+        norm = float(lse)
+    with np.errstate(over="ignore"):
+        return np.where(real, np.exp(x - norm), 0.0), x - norm
+
+
+def reference(z, idx, logits, t=1.0, lse=None, grad_loss=None, stats=None):
+    """loss [rows], gradient [rows][cols], what bounds their errors, and m and s of float64 scores z."""
+    rows, cols = z.shape
+    loss, grad, tol_l, tol_g, ms = np.zeros(rows), np.zeros((rows, cols)), np.zeros(rows), np.zeros((rows, cols)), np.zeros((rows, 2))
+    for r in range(rows):
+        q, lnq = teacher_q(idx[r], logits[r], None if lse is None else lse[r], t, cols)
+        g = 1.0 if grad_loss is None else float(grad_loss[r])
+        with np.errstate(all="ignore"):
+            m = np.nanmax(z[r]) if stats is None else float(stats[r, 0])
+            e = np.exp((z[r] - (m if m > -INF else 0.0)) / t)
+            s = e.sum() if stats is None else float(stats[r, 1])
+        ms[r] = m, s
+        if q.sum() == 0:
+            continue
+        there = z[r][np.isfinite(z[r])]
+        D = min((m - there.min()) / t if there.size else 0.0, 104.0)
+        n = max(16 * 8, cols / 1024)
+        de, ds = (3 * D + 2) * U, ((3 * D + 2) + n) * U
+        at = q > 0
+        with np.errstate(all="ignore"):
+            lnp = (z[r][idx[r][at]] - m) / t - np.log(s)
+            lnp[z[r][idx[r][at]] == -INF] = -INF
+            loss[r] = (q[at] * (lnq[at] - lnp)).sum()
+            p = q.sum() * e / s if s != 0 else np.zeros(cols)
+            qs = np.zeros(cols)
+            np.add.at(qs, idx[r][at], q[at])
+            grad[r] = g / t * (p - qs)
+            tol_l[r] = q.sum() * ds + (q[at] * (np.abs(lnq[at]) + np.abs(lnp) + 2)).sum() * U + U * abs(loss[r])
+            tol_g[r] = abs(g) / t * (p * (de + ds + 4 * U) + qs * 2 * U)
+    return loss, grad, tol_l, tol_g, ms
+
+
+def test_formulas_against_differences():
+    g = np.random.default_rng(0)
+    z, idx = g.standard_normal((3, 8)) * 2, np.array([[0, 3, 3], [7, -1, 8], [1, 2, 5]])
+    logits = g.standard_normal((3, 3)).astype(np.float32)
+    for lse in (None, np.array([2.0, 1.5, 2.5])):
+        for t in (1.0, 1.7):
+            _, grad, _, _, _ = reference(z, idx, logits, t, lse, grad_loss=np.array([1.0, 2.0, -0.5]))
+            for k in range(8):
+                h = 1e-5
+                zp, zm = z.copy(), z.copy()
+                zp[:, k] += h
+                zm[:, k] -= h
+                d = (reference(zp, idx, logits, t, lse)[0] - reference(zm, idx, logits, t, lse)[0]) / (2 * h)
+                assert np.abs(d * [1.0, 2.0, -0.5] - grad[:, k]).max() < 1e-9
+
+
+# ---- refusals, without a device --------------------------------------------------------------------------------------
+@pytest.fixture(scope="module")
+def checks(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    lib = str(tmp_path_factory.mktemp("checks") / "checks.so")
+    subprocess.check_call(["g++", "-std=c++17", "-shared", "-fPIC", "-Wall", "-Werror", "-fsanitize=undefined", "-static-libubsan",
+                           "-fno-sanitize-recover=all", "-I", os.path.join(ROOT, "include"),
+                           "-I", os.path.join(ROOT, "paper_2602_13140_amd", "csrc"),
+                           os.path.join(ROOT, "tests", "check_requests.cpp"), "-o", lib])
+    L = ctypes.CDLL(lib)
+    L.request_distill.restype = ctypes.c_char_p
+    L.request_distill.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
+    return L
+
+
+def req(**more):
+    r = qb.qsv_distill_req()
+    r.kind, r.scores_dev, r.rows, r.cols, r.row_stride = qb.QSV_S_BF16, 0x10000, 3, 10, 12
+    r.loss_dev, r.grad_dev, r.grad_stride = 0x2000, 0x20000, 10
+    for k, v in more.items():
+        setattr(r, k, v)
+    return r
+
+
+def teacher(**more):
+    t = qb.qsv_teacher(4, 0, 0x4000, 0x5000, None, 1.0)
+    for k, v in more.items():
+        setattr(t, k, v)
+    return t
+
+
+def test_refusals(checks):
+    def say(r, t):
+        return checks.request_distill(ctypes.byref(r) if r else None, ctypes.byref(t) if t else None)
+    assert say(req(), teacher()) is None
+    assert b"req" in say(None, teacher()) and b"teacher" in say(req(), None)
+    for kind in (0, qb.QSV_S_PROBS, qb.QSV_S_STATE, 9):
+        assert b"kind" in say(req(kind=kind), teacher())
+    assert b"rows" in say(req(rows=-1), teacher()) and b"cols" in say(req(cols=0), teacher())
+    assert b"row_stride" in say(req(row_stride=9), teacher())
+    assert b"scores_dev" in say(req(scores_dev=None), teacher())
+    assert b"aligned" in say(req(scores_dev=0x10001), teacher()) and b"aligned" in say(req(grad_dev=0x20001), teacher())
+    assert b"grad_stride" in say(req(grad_stride=9), teacher())
+    assert b"have_stats" in say(req(have_stats=2), teacher())
+    assert b"have_stats" in say(req(have_stats=1), teacher())                               # neither stats
+    assert b"have_stats" in say(req(have_stats=1, stats_dev=0x3000), teacher())             # with a loss
+    assert say(req(have_stats=1, stats_dev=0x3000, loss_dev=None), teacher()) is None
+    assert b"overlap" in say(req(grad_dev=0x10002), teacher())
+    assert b"overlap" in say(req(grad_dev=0x10000), teacher())                              # another stride
+    assert say(req(grad_dev=0x10000, grad_stride=12), teacher()) is None
+    assert say(req(grad_dev=0x10000 + 2 * 12 * 2 + 10 * 2), teacher()) is None              # right behind
+    assert b"overlap" in say(req(grad_dev=0x10000 + 2 * 12 * 2 + 10 * 2 - 2), teacher())
+    for top in (0, 1025, -3):
+        assert b"n_top" in say(req(), teacher(n_top=top))
+    assert b"reserved" in say(req(), teacher(reserved=1))
+    assert b"top_idx" in say(req(), teacher(top_idx_dev=None)) and b"top_logits" in say(req(), teacher(top_logits_dev=None))
+    for t in (0.0, -1.0, NAN, INF):
+        assert b"temperature" in say(req(), teacher(temperature=t))
+    assert say(req(rows=0, scores_dev=None), None) is None
+    assert qb.load().qsv_distill(None, ctypes.byref(req()), ctypes.byref(teacher())) == qb.QSV_ERR_INVALID_ARG
+    assert qb.load().qsv_distill_grad(None, None, None, 1, None, None, ctypes.byref(teacher()), None, None, None, None) == qb.QSV_ERR_INVALID_ARG
+
+
+def test_layouts():
+    assert ctypes.sizeof(qb.qsv_teacher) == 40 and ctypes.sizeof(qb.qsv_distill_req) == 80
+    assert qb.qsv_distill_workspace_bytes(-1, 5) == 0 == qb.qsv_distill_workspace_bytes(5, 0)
+    assert 0 < qb.qsv_distill_workspace_bytes(4096, 131072) and 0 < qb.qsv_distill_workspace_bytes(1, 1 << 30)
+
+
+# ---- on the GPU ------------------------------------------------------------------------------------------------------
+KIND = {"f32": qb.QSV_S_F32, "f16": qb.QSV_S_F16, "bf16": qb.QSV_S_BF16}
+
+
+def tt(src):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[src]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = qb.Context(1, 1)
+    yield c
+    c.close()
+
+
+def on_gpu(ctx, src, z, idx, logits, t=1.0, lse=None, grad_loss=None, stats=None, loss=True, grad=True, over=False, pad=0):
+    """z: a GPU tensor; the rest numpy.  (loss, gradient, stats) as numpy."""
+    import torch
+    rows, cols = z.shape
+    dev = lambda a, d: None if a is None else torch.as_tensor(np.ascontiguousarray(a)).to(d).cuda()  # noqa: E731
+    lo = torch.full((rows,), 77.0, device="cuda") if loss and stats is None else None
+    whole = torch.full((rows, cols + pad), 55.0, dtype=tt(src), device="cuda") if grad and not over else None
+    gr = z if over else whole[:, :cols] if grad else None
+    st = torch.full((rows, 2), 77.0, device="cuda") if stats is None else dev(stats, torch.float32)
+    ctx.qsv_distill(KIND[src], z, dev(idx, torch.int32), dev(logits, torch.float32), t, top_lse=dev(lse, torch.float32), loss=lo,
+                    stats=st, have_stats=int(stats is not None), grad_loss=dev(grad_loss, torch.float32), grad=gr)
+    torch.cuda.synchronize()
+    if whole is not None and pad:
+        assert bool((whole[:, cols:] == 55.0).all())
+    return (lo.cpu().numpy() if lo is not None else None, gr.double().cpu().numpy() if grad else None, st.cpu().numpy())
+
+
+def compare(src, got, ref):
+    import torch
+    loss, grad, tol_l, tol_g, ms = ref
+    f = torch.finfo(tt(src))
+    if got[0] is not None:
+        assert np.array_equal(np.isnan(got[0]), np.isnan(loss))
+        with np.errstate(invalid="ignore"):
+            assert np.all((np.abs(got[0] - loss) <= tol_l) | (got[0] == loss) | np.isnan(loss)), (got[0], loss, tol_l)
+    if got[1] is not None:
+        assert np.array_equal(np.isnan(got[1]), np.isnan(grad))
+        half = np.maximum(f.eps / 2 * np.abs(grad), f.smallest_normal * f.eps / 2)
+        with np.errstate(invalid="ignore"):
+            ok = np.abs(got[1] - grad) <= (half + tol_g) * (1 + f.eps) + 2.0 ** -126
+        assert np.all(ok | np.isnan(grad)), np.nanmax(np.abs(got[1] - grad) / (half + tol_g + 1e-300))
+
+
+def draw(src, rows, cols, top, seed, sigma=3.0, pad=0):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    z = (torch.randn((rows, cols + pad), generator=g) * sigma).to(tt(src)).cuda()[:, :cols]
+    r = np.random.default_rng(seed)
+    idx = np.stack([r.permutation(cols)[:top] if top <= cols else r.integers(0, cols, top) for _ in range(rows)])
+    return z, idx, (r.standard_normal((rows, top)) * 2).astype(np.float32)
+
+
+def f64(z):
+    return z.double().cpu().numpy()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols,top", [(1, 1), (2, 2), (7, 3), (64, 5), (255, 255), (1000, 1), (1025, 70), (4099, 8), (8193, 300), (16385, 33),
+                                      (33001, 64), (70001, 20), (140003, 1024)])
+def test_sizes(ctx, src, cols, top):
+    rows = 3
+    for n, (t, with_lse, pad) in enumerate([(1.0, False, 0), (2.0, True, 3), (0.7, False, 1)]):
+        z, idx, logits = draw(src, rows, cols, top, cols + n, pad=pad)
+        lse = np.full(rows, 6.0 / t, dtype=np.float32) if with_lse else None
+        gl = np.array([1.0, -0.5, 3.0], dtype=np.float32)
+        ref = reference(f64(z), idx, logits, t, lse, gl)
+        got = on_gpu(ctx, src, z, idx, logits, t, lse, gl, pad=pad)
+        compare(src, got, ref)
+        assert np.array_equal(got[2][:, 0], ref[4][:, 0].astype(np.float32))
+        # the two passes apart, the second from what the first one kept
+        back = on_gpu(ctx, src, z, idx, logits, t, lse, gl, stats=got[2])
+        compare(src, back, reference(f64(z), idx, logits, t, lse, gl, stats=got[2]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(130, 1000), (300, 8200), (129, 33000), (128, 70000), (127, 40000), (1030, 40)])
+def test_many_rows(ctx, src, rows, cols):
+    z, idx, logits = draw(src, rows, cols, 9, rows)
+    idx[1::3, 5:] = -1
+    idx[2::7] = cols
+    ref = reference(f64(z), idx, logits)
+    compare(src, on_gpu(ctx, src, z, idx, logits), ref)
+    got = on_gpu(ctx, src, z, idx, logits, grad=False)
+    compare(src, got, ref)
+    assert np.abs(got[2][:, 1] / ref[4][:, 1] - 1).max() < 1e-4
+    assert on_gpu(ctx, src, z, idx, logits, loss=False)[0] is None
+    compare(src, on_gpu(ctx, src, z.clone(), idx, logits, over=True), ref)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(12, 500), (12, 40000), (200, 9000)])
+def test_masks_and_odd_teachers(ctx, src, rows, cols):
+    """Rows that a mask leaves empty or nearly so, the type's lowest value, NaN and infinities, teachers without entries or with the
+    same one twice."""
+    import torch
+    z, idx, logits = draw(src, rows, cols, 6, 5)
+    low = torch.finfo(tt(src)).min
+    z = z.clone()
+    z[0] = -INF
+    z[1, 1:] = -INF
+    z[2, ::2] = -INF
+    z[3, ::2] = low
+    z[4] = low
+    z[5, 3] = NAN
+    z[6, 4] = INF
+    idx[0] = [0, 1, 2, 3, 4, 5]
+    idx[1] = [0, 0, 0, 0, 0, -1]
+    idx[2] = [1, 3, 5, 2, 7, 9]              # one of them masked
+    idx[3] = [1, 1, 3, 3, cols - 1, 1]
+    idx[7] = -5
+    idx[8] = [2, 2, 2, 2, 2, 2]
+    logits[9] = -INF
+    logits[10, 2:] = -INF
+    idx[11] = [2 ** 31 - 1, cols, -2 ** 31, 4, 4, 5]
+    ref = reference(f64(z), idx, logits)
+    assert np.isinf(ref[0][[0, 2]]).all() and np.isnan(ref[0][[5, 6]]).all() and (ref[0][[7, 9]] == 0).all()
+    got = on_gpu(ctx, src, z, idx, logits)
+    compare(src, got, ref)
+    compare(src, on_gpu(ctx, src, z.clone(), idx, logits, over=True), ref)
+    # a row that is not trained on stays at zero whatever its scores are
+    z[7, 1] = NAN
+    got = on_gpu(ctx, src, z, idx, logits)
+    assert got[0][7] == 0 and not got[1][7].any()
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences_of_the_loss(ctx):
+    """Central differences of the kernel's own losses: truncation h^2 |f'''| / 6 <= 2^-14 / 6, two losses of up to 8 rounded (2^-21)
+    and good to 1e-6 over 2 h = 2^-6."""
+    import torch
+    z, idx, logits = draw("f32", 2, 11, 4, 3, sigma=1.0)
+    grad = on_gpu(ctx, "f32", z, idx, logits)[1]
+    h = 2.0 ** -7
+    for k in range(11):
+        d = torch.zeros_like(z)
+        d[:, k] = h
+        up, down = (on_gpu(ctx, "f32", z + s * d, idx, logits, grad=False)[0].astype(np.float64) for s in (1, -1))
+        assert np.abs((up - down) / (2 * h) - grad[:, k]).max() <= 2.0 ** -14 / 6 + (2 * 2.0 ** -22 + 2e-6) * 2 ** 6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+def test_a_row_does_not_depend_on_its_alignment(ctx, src):
+    import torch
+    g = torch.Generator().manual_seed(5)
+    flat = (torch.randn(300000, generator=g) * 3).to(tt(src)).cuda()
+    for rows, cols in ((2, 5), (3, 1001), (2, 60001), (200, 900)):
+        for off in (0, 1, 3):
+            z = torch.as_strided(flat, (rows, cols), (cols + 7, 1), off)
+            idx, logits = np.tile([0, cols - 1, 2], (rows, 1)), np.ones((rows, 3), dtype=np.float32)
+            compare(src, on_gpu(ctx, src, z, idx, logits, pad=off), reference(f64(z), idx, logits))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(4, 60000), (200, 3001)])
+def test_replays_of_a_captured_step(rows, cols):
+    import torch
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = qb.Context(1, 1)
+        z, idx, logits = draw("bf16", rows, cols, 5, 1)
+        z = z.contiguous()
+        ti, tl = torch.as_tensor(idx).int().cuda(), torch.as_tensor(logits).cuda()
+        loss, grad = torch.zeros(rows, device="cuda"), torch.zeros_like(z)
+        call = lambda: c.qsv_distill(qb.QSV_S_BF16, z, ti, tl, loss=loss, grad=grad)  # noqa: E731
+        call()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call()
+        for i in range(4):
+            z.copy_(torch.randn((rows, cols), generator=torch.Generator().manual_seed(i)) * (i + 1))
+            loss.fill_(-7)
+            grad.fill_(-7)
+            graph.replay()
+            stream.synchronize()
+            a = loss.cpu().numpy(), f64(grad), None
+            compare("bf16", a, reference(f64(z), idx, logits))
+            grad.fill_(-7)
+            call()
+            stream.synchronize()
+            assert np.array_equal(f64(grad), a[1])
+        c.close()
+
+
+@pytest.mark.gpu
+def test_refused_calls_leave_their_outputs(ctx):
+    import torch
+    whole, idx, logits = draw("f32", 3, 21, 2, 1)
+    z, idx = whole[:, :20], idx % 20
+    loss, ti, tl = torch.full((3,), -7.0, device="cuda"), torch.as_tensor(idx).int().cuda(), torch.as_tensor(logits).cuda()
+    for more in (dict(temperature=0.0), dict(have_stats=1), dict(grad=whole[:, 1:])):
+        with pytest.raises(qb.QsvError):
+            ctx.qsv_distill(qb.QSV_S_F32, z, ti, tl, loss=loss, **more)
+    torch.cuda.synchronize()
+    assert bool((loss == -7).all())
+
+
+# ---- a circuit's own outcomes ----------------------------------------------------------------------------------------
+def circuit_reference(oracle, spec, n, x, params, feats, idx, logits, t, lse):
+    """Loss and gradient by the chain rule over the probabilities, whose derivatives are their shifts: dp/dangle =
+    (p(angle + pi/2) - p(angle - pi/2)) / 2, times the feature for a re-uploading weight."""
+    oc = oracle.make_circuit(spec.n_layers, list(spec.rot), spec.entangler, spec.reupload)
+
+    def probs(b, pr):
+        s, _ = oracle.amp_encode(x[b:b + 1], n)
+        oracle.apply_layers(s, oc, pr, None if feats is None else feats[b:b + 1])
+        return (np.abs(s) ** 2).reshape(-1)
+    B, P = x.shape[0], len(params)
+    loss, grad, tol = np.zeros(B), np.zeros((B, P)), np.zeros(B)
+    slots = spec.slots()
+    for b in range(B):
+        p = probs(b, params)
+        q, lnq = teacher_q(idx[b], logits[b], None if lse is None else lse[b], t, 1 << n)
+        at = q > 0
+        k = idx[b][at]
+        loss[b] = (q[at] * (lnq[at] - np.log(p[k]))).sum()
+        tol[b] = 2 * (q[at] * 3e-7 * (0.5 / p[k] + 1 / np.sqrt(p[k]))).sum() + 1e-6
+        for i in range(P):
+            weight = spec.reupload and (i // n) % slots == 0
+            f = float(feats[b, i % n]) if weight else 1.0
+            d = []
+            for sign in (1, -1):
+                pr = params.astype(np.float64).copy()
+                pr[i] += sign * math.pi / 2 / f
+                d.append(probs(b, pr))
+            grad[b, i] = -(q[at] / p[k] * f * (d[0][k] - d[1][k]) / 2).sum()
+    return loss, grad, tol
+
+
+def case(n, B, L, rot, ent, reup, seed, top):
+    spec = wl.CircuitSpec(L, tuple(rot), ent, reup)
+    g = np.random.default_rng(seed)
+    params = wl.draw_params(spec, n, seed)
+    x = g.standard_normal((B, 1 << n)).astype(np.float32)
+    feats = (g.standard_normal((B, n)) + np.sign(g.standard_normal((B, n)))).astype(np.float32) if reup else None
+    return spec, g, params, x, feats, (g.standard_normal((B, top))).astype(np.float32)
+
+
+CIRCUITS = [(1, 2, 2, (RY, RZ), NONE, 0), (2, 3, 1, (RX,), RING, 0), (4, 3, 2, (RY, RZ), RING, 1), (6, 2, 2, (RX, RY, RZ), LADDER, 0),
+            (10, 2, 2, (RY, RZ), RING, 0), (11, 2, 1, (RY, RZ), LADDER, 1), (13, 2, 2, (RY,), RING, 0)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,B,L,rot,ent,reup", CIRCUITS)
+@pytest.mark.parametrize("mode", ["default", "naive", "chunk1", "whole"])
+def test_circuit(oracle, n, B, L, rot, ent, reup, mode):
+    import torch
+    top = min(5, 1 << n)
+    spec, g, params, x, feats, logits = case(n, B, L, rot, ent, reup, 50 + n, top)
+    oc = oracle.make_circuit(L, list(rot), ent, reup)
+    s, _ = oracle.amp_encode(x, n)
+    oracle.apply_layers(s, oc, params, feats)
+    p = np.abs(s) ** 2
+    likely = np.argsort(-p, axis=1)[:, :max(top, (1 << n) // 4)]          # outcomes of a quarter of the state, none of them rare
+    idx = np.stack([g.permutation(likely[b])[:top] for b in range(B)])
+    if top >= 4:
+        idx[0, 1] = idx[0, 0]
+        idx[1, 2] = -1
+    lse = np.full(B, 2.5, dtype=np.float32) if n % 2 else None
+    ref = circuit_reference(oracle, spec, n, x, params, feats, idx, logits, 1.3, lse)
+    c = gu.make_ctx(n, B, naive=int(mode == "naive"))
+    if mode == "chunk1":
+        c.qsv_set_option("grad_chunk_rows", 1)
+    if mode == "whole":
+        c.qsv_set_option("grad_layered", 0)
+    c.state.fill_(3.0)
+    P = len(params)
+    loss, grad = torch.zeros(B, device="cuda"), torch.zeros((B, P), device="cuda")
+    ml, mg = torch.zeros(1, device="cuda"), torch.zeros(P, device="cuda")
+    c.qsv_distill_grad(qb.circuit_from_spec(spec), gu.dev(x), gu.dev(params), gu.dev(feats) if reup else None,
+                       gu.dev(idx.astype(np.int32)), gu.dev(logits), loss, grad, ml, mg, temperature=1.3,
+                       top_lse=None if lse is None else gu.dev(lse))
+    torch.cuda.synchronize()
+    gl, gg = loss.cpu().numpy(), grad.cpu().numpy()
+    assert np.all(np.abs(gl - ref[0]) <= ref[2] + 1e-5)
+    assert np.all(np.abs(gg - ref[1]).max(axis=1) <= ref[2] + 1e-5)
+    assert np.linalg.norm(gg - ref[1]) <= 1e-3 * np.linalg.norm(ref[1])
+    assert abs(ml.item() - gl.mean()) <= 1e-5 * max(1, abs(gl.mean())) and np.abs(mg.cpu().numpy() - gg.mean(0)).max() <= 1e-5 * max(1, np.abs(gg).max())
+    assert bool((c.state == 3.0).all())
+    c.close()
+
+
+@pytest.mark.gpu
+def test_circuit_special_rows():
+    """A teacher without entries, an outcome of amplitude 0, no layers; refusals that need a context."""
+    import torch
+    c = qb.Context(3, 3)
+    circ = qb.make_circuit(1, [RZ], NONE)                 # phases only: the outcomes stay as encoded
+    x = torch.zeros((3, 8), device="cuda")
+    x[:, 0] = 1.0
+    x[:, 1] = 1.0
+    pr = torch.full((3,), 0.3, device="cuda")
+    idx = torch.tensor([[0, 1], [-1, 9], [0, 5]], dtype=torch.int32, device="cuda")
+    logits = torch.zeros((3, 2), device="cuda")
+    loss, grad = torch.full((3,), 7.0, device="cuda"), torch.full((3, 3), 7.0, device="cuda")
+    c.qsv_distill_grad(circ, x, pr, None, idx, logits, loss, grad)
+    torch.cuda.synchronize()
+    assert abs(loss[0].item()) < 1e-6 and loss[1].item() == 0 and loss[2].item() == INF
+    assert bool(torch.isfinite(grad).all()) and grad.abs().max().item() < 1e-6
+    none = qb.make_circuit(0, [RZ], NONE)
+    loss.fill_(7.0)
+    c.qsv_distill_grad(none, x, None, None, idx, logits, loss, None)
+    torch.cuda.synchronize()
+    assert abs(loss[0].item()) < 1e-6 and loss[1].item() == 0 and loss[2].item() == INF
+    with pytest.raises(qb.QsvError, match="temperature"):
+        c.qsv_distill_grad(circ, x, pr, None, idx, logits, loss, grad, temperature=0.0)
+    with pytest.raises(qb.QsvError, match="teacher"):
+        c._check(c.L.qsv_distill_grad(c.h, ctypes.byref(circ), x.data_ptr(), 8, pr.data_ptr(), None, None, loss.data_ptr(), grad.data_ptr(), None, None))
+    c.close()
+
+
+@pytest.mark.gpu
+def test_training_towards_a_teacher_and_answers(oracle):
+    """Steps of a circuit towards a teacher's likeliest outcomes, then answers drawn from what it learnt: every step's gradient and
+    the drawn outcomes against the references."""
+    import torch
+    from tests.test_sample import reference as sampled, values_of
+    n, B, top = 5, 2, 4
+    spec, g, params, x, _, logits = case(n, B, 2, (RY, RZ), RING, 0, 8, top)
+    idx = np.stack([g.permutation(1 << n)[:top] for _ in range(B)])
+    c, circ, P = qb.Context(n, B), qb.circuit_from_spec(spec), len(params)
+    xd, pd = gu.dev(x), gu.dev(params)
+    loss, grad, ml, mg = (torch.zeros(s, device="cuda") for s in ((B,), (B, P), (1,), (P,)))
+    m, v = torch.zeros(P, device="cuda"), torch.zeros(P, device="cuda")
+    for step in (1, 2, 3):
+        now = pd.cpu().numpy()
+        c.qsv_distill_grad(circ, xd, pd, None, gu.dev(idx.astype(np.int32)), gu.dev(logits), loss, grad, ml, mg)
+        c.qsv_adam_step(pd, mg, m, v, step, 0.05)
+        torch.cuda.synchronize()
+        ref = circuit_reference(oracle, spec, n, x, now, None, idx, logits, 1.0, None)
+        assert np.all(np.abs(grad.cpu().numpy() - ref[1]).max(axis=1) <= ref[2] + 1e-5)
+        assert np.all(np.abs(loss.cpu().numpy() - ref[0]) <= ref[2] + 1e-5)
+    c.qsv_amp_encode(xd)
+    c.qsv_apply_layers(circ, pd, None, 0)
+    u = g.random((B, 12))
+    f = dict(top_p=[0.9, 0.6], temperature=[0.7, 1.0], min_p=[0.0, 0.02])
+    out, kept = torch.zeros((B, 12), dtype=torch.int64, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    c.qsv_sample(qb.QSV_S_STATE, out, gu.dev(u), kept=kept, **{k: torch.tensor(a, device="cuda") for k, a in f.items()})
+    p = torch.zeros((B, 1 << n), device="cuda")
+    c.qsv_measure(qb.QSV_M_PROBS, p)
+    torch.cuda.synchronize()
+    ref = sampled(values_of("probs", p), False, u, f)
+    assert np.array_equal(out.cpu().numpy(), ref[0]) and np.array_equal(kept.cpu().numpy(), ref[2])
+    c.close()
