@@ -44,24 +44,20 @@ template <int KIND> __device__ __forceinline__ void store_one(char* row, u32 k, 
     else ((__bf16*)row)[k] = (__bf16)v;
 }
 
-// Vector j of a row; -inf behind the row's end.
-template <int KIND> __device__ __forceinline__ vec load_vec(const char* row, u32 cols, u32 j) {
-    constexpr int W = kPer<KIND>;
+// Vector j of a row's whole vectors; -inf behind them.  (Offsets of 32 bits to a uniform address: a row has 4 GiB at most.)
+template <int KIND> __device__ __forceinline__ vec load_vec(const char* row, u32 whole, u32 j) {
     vec x = {kNone<KIND>, kNone<KIND>, kNone<KIND>, kNone<KIND>};
-    const u64 k0 = (u64)j * W;
-    if (k0 + W <= cols) {
-        if (KIND == kScoreF32) x = *(const vec_at4*)(row + k0 * 4);
-        else x = *(const vec_at2*)(row + k0 * 2);
-    } else if (k0 < cols) {
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            if (k0 + i < cols) {
-                if (KIND == kScoreF32) x[i] = ((const u32*)row)[k0 + i];
-                else x[i >> 1] = (i & 1) ? (x[i >> 1] & 0xffffu) | ((u32)((const unsigned short*)row)[k0 + i] << 16)
-                                         : (x[i >> 1] & 0xffff0000u) | ((const unsigned short*)row)[k0 + i];
-            }
+    if (j < whole) {
+        if (KIND == kScoreF32) x = *(const vec_at4*)(row + j * 16u);
+        else x = *(const vec_at2*)(row + j * 16u);
     }
     return x;
+}
+
+// The values behind a row's whole vectors, one a lane; -inf in the others.
+template <int KIND> __device__ __forceinline__ float load_rest(const char* row, u32 cols, u32 lane) {
+    const u32 k = cols / kPer<KIND> * kPer<KIND> + lane;
+    return lane < kPer<KIND> && k < cols ? value_at<KIND>(row, k) : -kInf;
 }
 
 template <int KIND> __device__ __forceinline__ float part(const vec& x, int i) {
@@ -71,62 +67,78 @@ template <int KIND> __device__ __forceinline__ float part(const vec& x, int i) {
     return __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
 }
 
-template <int KIND> __device__ __forceinline__ void store_vec(char* row, u32 cols, u32 j, const float (&g)[kPer<KIND>]) {
+template <int KIND> __device__ __forceinline__ void store_vec(char* row, u32 whole, u32 j, const float (&g)[kPer<KIND>]) {
     constexpr int W = kPer<KIND>;
-    const u64 k0 = (u64)j * W;
-    if (k0 + W <= cols) {
-        vec x;
-        if (KIND == kScoreF32) {
+    if (j >= whole) return;
+    vec x;
+    if (KIND == kScoreF32) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(g[i]);
-            *(vec_at4*)(row + k0 * 4) = x;
-        } else {
+        for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(g[i]);
+        *(vec_at4*)(row + j * 16u) = x;
+    } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (KIND == kScoreBF16) {
-                    typedef __bf16 two __attribute__((ext_vector_type(2)));
-                    const two b = {(__bf16)g[(2 * i) % W], (__bf16)g[(2 * i + 1) % W]};
-                    x[i] = __builtin_bit_cast(u32, b);
-                } else {
-                    x[i] = (u32)__half_as_ushort(__float2half_rn(g[(2 * i) % W])) | (u32)__half_as_ushort(__float2half_rn(g[(2 * i + 1) % W])) << 16;
-                }
+        for (int i = 0; i < 4; ++i) {
+            if (KIND == kScoreBF16) {
+                typedef __bf16 two __attribute__((ext_vector_type(2)));
+                const two b = {(__bf16)g[(2 * i) % W], (__bf16)g[(2 * i + 1) % W]};
+                x[i] = __builtin_bit_cast(u32, b);
+            } else {
+                x[i] = (u32)__half_as_ushort(__float2half_rn(g[(2 * i) % W])) | (u32)__half_as_ushort(__float2half_rn(g[(2 * i + 1) % W])) << 16;
             }
-            *(vec_at2*)(row + k0 * 2) = x;
         }
-    } else if (k0 < cols) {
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            if (k0 + i < cols) store_one<KIND>(row, (u32)(k0 + i), g[i]);
+        *(vec_at2*)(row + j * 16u) = x;
     }
+}
+
+template <int KIND> __device__ __forceinline__ void store_rest(char* row, u32 cols, u32 lane, float g) {
+    const u32 k = cols / kPer<KIND> * kPer<KIND> + lane;
+    if (lane < kPer<KIND> && k < cols) store_one<KIND>(row, k, g);
+}
+
+// The compiler keeps nothing that it worked out of the vectors: unpacked values of one phase, kept for the next, would take
+// twice the registers of the vectors themselves.
+template <int N> __device__ __forceinline__ void forget(vec (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
 }
 
 // ---- workgroups ------------------------------------------------------------------------------------------------------
+// A wavefront's result a lane, then over the lanes: a loop over the wavefronts' results would hold all of them in registers.
 template <int NT> __device__ __forceinline__ float block_max(float v, double* sm) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int NW = NT / 64;
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    if (NW == 1) return uniform(v);
     __syncthreads();
-    if (lane == 0) sm[wave] = v;
+    if (lane == 0) sm[threadIdx.x >> 6] = v;
     __syncthreads();
+    v = (float)sm[lane & (NW - 1)];
 #pragma unroll
-    for (int i = 0; i < NT / 64; ++i) v = fmaxf(v, (float)sm[i]);
-    return v;
+    for (int o = NW / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return uniform(v);
 }
 
 template <int NT, int N> __device__ __forceinline__ void block_sums(double (&v)[N], double* sm) {     // sm: 16 N entries
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int NW = NT / 64;
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
-    __syncthreads();
-    if (lane == 0)
+    if (NW > 1) {
+        __syncthreads();
+        if (lane == 0)
 #pragma unroll
-        for (int k = 0; k < N; ++k) sm[k * 16 + wave] = v[k];
-    __syncthreads();
+            for (int k = 0; k < N; ++k) sm[k * 16 + (threadIdx.x >> 6)] = v[k];
+        __syncthreads();
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        v[k] = 0.0;
-        for (int i = 0; i < NT / 64; ++i) v[k] += sm[k * 16 + i];
+        for (int k = 0; k < N; ++k) {
+            v[k] = sm[k * 16 + (lane & (NW - 1))];
+#pragma unroll
+            for (int o = NW / 2; o > 0; o >>= 1) v[k] += __shfl_xor(v[k], o, 64);
+        }
     }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = uniform(v[k]);
 }
 
 // A row's teacher: idx, q and z of its entries in LDS, and their sums.
@@ -237,14 +249,15 @@ __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
     if (r >= (u64)a.rows) return;
     const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
     const TeacherLds l = teacher_lds(lds, a.teacher.top);
-    const u32 vecs = (u32)(((u64)a.cols + W - 1) / W);
+    const u32 whole = a.cols / W;
     const float c = (float)(1.4426950408889634074 * a.teacher.inv_t);
     vec x[KEPT ? NV : 1];
-    float m = -kInf, sum = 0.f;
     if (KEPT) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) x[i] = load_vec<KIND>(row, a.cols, (u32)i * NT + threadIdx.x);
+        for (int i = 0; i < NV; ++i) x[i] = load_vec<KIND>(row, whole, (u32)i * NT + threadIdx.x);
     }
+    const float rest = load_rest<KIND>(row, a.cols, threadIdx.x);
+    float m = rest, sum;
     const Taught t = teach<KIND, NT>(a.teacher, r, row, a.cols, l, sm);
     if (KEPT) {
 #pragma unroll
@@ -252,29 +265,33 @@ __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
 #pragma unroll
             for (int k = 0; k < W; ++k) m = fmaxf(m, part<KIND>(x[i], k));
         m = block_max<NT>(m, sm);
+        forget(x);
         const float base = m > -kInf ? m : 0.f;
+        sum = __builtin_amdgcn_exp2f((rest - base) * c);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float four = 0.f;
+            float some = 0.f;
 #pragma unroll
-            for (int k = 0; k < W; ++k) four += __builtin_amdgcn_exp2f((part<KIND>(x[i], k) - base) * c);
-            sum += four;
+            for (int k = 0; k < W; ++k) some += __builtin_amdgcn_exp2f((part<KIND>(x[i], k) - base) * c);
+            sum += some;
         }
     } else {
         // the thread's own maximum so far, and the sum relative to it
-        for (u32 j = threadIdx.x; j < vecs; j += NT) {
-            const vec y = load_vec<KIND>(row, a.cols, j);
+        sum = m > -kInf ? 1.f : 0.f;
+        for (u32 j = threadIdx.x; j < whole; j += NT) {
+            const vec y = load_vec<KIND>(row, whole, j);
             float high = m;
 #pragma unroll
             for (int k = 0; k < W; ++k) high = fmaxf(high, part<KIND>(y, k));
             const float base = high > -kInf ? high : 0.f;
             sum *= high > m ? __builtin_amdgcn_exp2f((m - high) * c) : 1.f;
             m = high;
-            float four = 0.f;
+            float some = 0.f;
 #pragma unroll
-            for (int k = 0; k < W; ++k) four += __builtin_amdgcn_exp2f((part<KIND>(y, k) - base) * c);
-            sum += four;
+            for (int k = 0; k < W; ++k) some += __builtin_amdgcn_exp2f((part<KIND>(y, k) - base) * c);
+            sum += some;
         }
+        if (rest != rest) sum = rest;
         const float own = m;
         m = block_max<NT>(m, sm);
         if (own < m) sum *= __builtin_amdgcn_exp2f((own - m) * c);
@@ -293,14 +310,16 @@ __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
         float o[W];
 #pragma unroll
         for (int k = 0; k < W; ++k) o[k] = zero ? 0.f : e_of(g, part<KIND>(y, k)) * g.scale;
-        store_vec<KIND>(grad, a.cols, j, o);
+        store_vec<KIND>(grad, whole, j, o);
     };
     if (KEPT) {
+        forget(x);
 #pragma unroll
         for (int i = 0; i < NV; ++i) write((u32)i * NT + threadIdx.x, x[i]);
     } else {
-        for (u32 j = threadIdx.x; j < vecs; j += NT) write(j, load_vec<KIND>(row, a.cols, j));
+        for (u32 j = threadIdx.x; j < whole; j += NT) write(j, load_vec<KIND>(row, whole, j));
     }
+    store_rest<KIND>(grad, a.cols, threadIdx.x, zero ? 0.f : e_of(g, rest) * g.scale);
     if (zero) return;
     __syncthreads();       // the entries' places are written a second time
     write_entries<KIND, NT>(l, a.teacher.top, g, grad, 0, a.cols);
@@ -324,9 +343,11 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_st
     const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
     const u32 j0 = at * (kPartThreads * kPartVecs) + threadIdx.x;
     const float c = (float)(1.4426950408889634074 * a.teacher.inv_t);
+    const u32 whole = a.cols / W;
     vec x[kPartVecs];
 #pragma unroll
-    for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, a.cols, j0 + (u32)i * kPartThreads);
+    for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
+    const float rest = at + 1 == p.parts ? load_rest<KIND>(row, a.cols, threadIdx.x) : -kInf;
     if (at == 0) {
         // (the gradient may be written over the scores)
         for (int j = threadIdx.x; j < a.teacher.top; j += kPartThreads) {
@@ -334,13 +355,15 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_st
             p.z[r * a.teacher.top + j] = i >= 0 && (u32)i < a.cols ? value_at<KIND>(row, (u32)i) : 0.f;
         }
     }
-    float m = -kInf, sum = 0.f;
+    float m = rest;
 #pragma unroll
     for (int i = 0; i < kPartVecs; ++i)
 #pragma unroll
         for (int k = 0; k < W; ++k) m = fmaxf(m, part<KIND>(x[i], k));
     m = block_max<kPartThreads>(m, sm);
+    forget(x);
     const float base = m > -kInf ? m : 0.f;
+    float sum = __builtin_amdgcn_exp2f((rest - base) * c);
 #pragma unroll
     for (int i = 0; i < kPartVecs; ++i)
 #pragma unroll
@@ -363,10 +386,13 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_ap
     const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
     const TeacherLds l = teacher_lds(lds, a.teacher.top);
     const u32 j0 = at * (kPartThreads * kPartVecs) + threadIdx.x;
+    const u32 whole = a.cols / W;
     vec x[kPartVecs];
+    float rest = -kInf;
     if (a.grad) {
 #pragma unroll
-        for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, a.cols, j0 + (u32)i * kPartThreads);
+        for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
+        if (at + 1 == blocks) rest = load_rest<KIND>(row, a.cols, threadIdx.x);
     }
     // (the scores at the entries: kept ones where the gradient of another part may be written over them)
     const Taught t = p.z ? teach<kScoreF32, kPartThreads, true>(a.teacher, r, (const char*)(p.z + r * a.teacher.top), a.cols, l, sm)
@@ -398,8 +424,9 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_ap
         float o[W];
 #pragma unroll
         for (int k = 0; k < W; ++k) o[k] = zero ? 0.f : e_of(g, part<KIND>(x[i], k)) * g.scale;
-        store_vec<KIND>(grad, a.cols, j0 + (u32)i * kPartThreads, o);
+        store_vec<KIND>(grad, whole, j0 + (u32)i * kPartThreads, o);
     }
+    if (at + 1 == blocks) store_rest<KIND>(grad, a.cols, threadIdx.x, zero ? 0.f : e_of(g, rest) * g.scale);
     if (zero) return;
     __syncthreads();
     const u64 k0 = (u64)at * (kPartThreads * kPartVecs * W);

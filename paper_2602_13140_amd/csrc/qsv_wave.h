@@ -29,4 +29,12 @@ template <class T> __device__ __forceinline__ T wave_scan(T v, int lane) {      
     return v;
 }
 
+// The same value in all lanes, as one that the compiler knows to be: in scalar registers.
+__device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+__device__ __forceinline__ unsigned long long uniform(unsigned long long v) {
+    return ((unsigned long long)uniform((unsigned)(v >> 32)) << 32) | uniform((unsigned)v);
+}
+__device__ __forceinline__ double uniform(double v) { return __longlong_as_double((long long)uniform((unsigned long long)__double_as_longlong(v))); }
+
 }  // namespace qsv
