@@ -1,7 +1,7 @@
 // Outcomes drawn from rows of scores, probabilities or amplitudes after temperature, min-p, top-k and top-p.
 //
 // All filters cut one order: value descending, ties by the lowest index first.  So what is left of a row is known by a
-// cut (key, ne): everything above the key and the first ne, by index, of what equals it.  Keys are the values' bits made
+// cut (key, idx): everything above the key, and what equals it up to that index.  Keys are the values' bits made
 // to order as whole numbers, 16 of them for 16-bit scores.  A cut is found without sorting: a histogram over the distance
 // from the row's highest value (counts, and for top-p weights), then histograms over the keys of the one bin the cut falls
 // into, 11 bits at a time, until the bin is one key.
@@ -20,7 +20,7 @@ typedef unsigned long long u64;
 typedef unsigned u32;
 
 constexpr float kInf = __builtin_inff();
-constexpr u32 kAll = 0xffffffffu;      // a cut that keeps every outcome that equals its key
+constexpr u32 kAll = 0xffffffffu;      // of a cut: every outcome that equals its key
 
 template <int KIND> constexpr bool kLogs = KIND <= kScoreBF16;          // scores; else probabilities
 template <int KIND> constexpr bool kKeys16 = KIND == kScoreF16 || KIND == kScoreBF16;
@@ -112,6 +112,11 @@ template <int KIND> __device__ __forceinline__ void load4(const Row& w, u32 j, f
         for (int i = 0; i < 4; ++i) v[i] = clean<KIND>(v[i]);
         return;
     }
+    if (j >= w.vecs) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = kLogs<KIND> ? -kInf : 0.f;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const long long k = first + i;
@@ -145,8 +150,11 @@ __device__ __forceinline__ double exp2_neg(double x) {
 // How a row's values become weights.
 struct Scale {
     float m;           // the highest value
-    double md, c;      // scores: log2(e) / T; probabilities: 1 / T
+    double md;
+    double mq, rm;     // for quotients: m and 1 / m, or 1 and 0 where m is infinite
+    double c;          // scores: log2(e) / T; probabilities: 1 / T
     double one;        // 2^S
+    int bits;          // S
     float per_bin;     // scores: bins for a distance of 1 below m
     bool t_one;
     u32 kmax;
@@ -157,6 +165,9 @@ template <int KIND, int NB> __device__ __forceinline__ Scale scale_of(u32 kmax, 
     s.kmax = kmax;
     s.m = value_of<KIND>(kmax);
     s.md = (double)s.m;
+    s.mq = s.m < kInf ? s.md : 1.0;
+    s.rm = s.m < kInf ? 1.0 / s.md : 0.0;
+    s.bits = bits;
     s.c = (kLogs<KIND> ? 1.4426950408889634074 : 1.0) / (double)t;
     s.one = __builtin_ldexp(1.0, bits);
     s.t_one = t == 1.f;
@@ -171,10 +182,33 @@ template <int KIND> __device__ __forceinline__ double weight64(const Scale& s, f
     return s.t_one ? q : exp2_neg(log2(q) * s.c);
 }
 
-template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, float v) {
-    // adding 2^52 rounds to a whole number, which the low bits then hold
-    const double x = fma(weight64<KIND>(s, v), s.one, 4503599627370496.0);
-    return (u64)__double_as_longlong(x) & 0xfffffffffffffull;
+// 2^(i / 256): a kernel's copy in LDS, filled by its threads before their next barrier.
+constexpr int kPowers = 256;
+template <int NT> __device__ __forceinline__ void fill_powers(double* powers) {
+    for (int i = threadIdx.x; i < kPowers; i += NT) powers[i] = 2.0 * exp2_neg((double)i / kPowers - 1.0);
+}
+
+// rint(e 2^S), the whole number that adding 2^52 leaves in the low bits.  2^x as a power of 2^(1/256) from the table times
+// a series of four terms (|r| <= 2^-9: the next term is below 2^-54): half the arithmetic of exp2_neg.
+__device__ __forceinline__ u64 whole(double x) { return (u64)__double_as_longlong(x) & 0xfffffffffffffull; }
+template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, const double* powers, float v) {
+    if (!kLogs<KIND> && s.t_one) {
+        const double q = (double)v * s.rm;
+        const double e = fma(fma(-q, s.mq, (double)v), s.rm, q);      // v / m
+        return whole(fma(v == s.m ? 1.0 : e, s.one, 4503599627370496.0));
+    }
+    double x = kLogs<KIND> ? ((double)v - s.md) * (s.c * kPowers) : log2((double)v / s.md) * (s.c * kPowers);
+    x = fmax(x, -200.0 * kPowers);
+    if (v == s.m) x = 0.0;                                            // (also where both are infinite)
+    const double y = x + 6755399441055744.0;                          // 1.5 2^52: the nearest whole number in the low bits
+    const int n = (int)__double_as_longlong(y);
+    const double r = x - (y - 6755399441055744.0);
+    constexpr double l = 0.69314718055994530942 / kPowers;
+    double p = fma(l * l * l * l / 24.0, r, l * l * l / 6.0);
+    p = fma(p, r, l * l / 2.0);
+    p = fma(p, r, l);
+    p = fma(p, r, 1.0);
+    return whole(fma(__builtin_ldexp(powers[n & (kPowers - 1)], (n >> 8) + s.bits), p, 4503599627370496.0));
 }
 
 // Bin of the first histogram: not decreasing in the distance from the highest value.  Scores: linear in it over the S + 2
@@ -188,32 +222,34 @@ template <int KIND, int NB> __device__ __forceinline__ u32 bin_of(const Scale& s
 // ---- wavefronts and workgroups ---------------------------------------------------------------------------------------
 // Sums over the workgroup before each thread's own, and the whole sum.  sm: NT / 64 entries that nothing else uses.
 template <int NT> __device__ __forceinline__ u64 block_scan(u64 v, u64* sm, u64* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const u64 incl = wave_scan(v, lane);
+    constexpr int NW = NT / 64;
+    const u32 lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const u64 incl = wave_scan(v);
+    if (NW == 1) {
+        *total = last_lane(incl);
+        return incl - v;
+    }
     __syncthreads();
     if (lane == 63) sm[wave] = incl;
     __syncthreads();
-    u64 before = 0, all = 0;
-#pragma unroll
-    for (int i = 0; i < NT / 64; ++i) {
-        const u64 x = sm[i];
-        if (i < wave) before += x;
-        all += x;
-    }
-    *total = all;
-    return before + incl - v;
+    const u64 waves = wave_scan(lane < NW ? sm[lane & (NW - 1)] : 0ull);
+    *total = last_lane(waves);
+    return (wave ? lane_of(waves, wave - 1) : 0) + incl - v;
 }
 
 template <int NT> __device__ __forceinline__ u32 block_max(u32 v, u64* sm) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int NW = NT / 64;
+    const u32 lane = threadIdx.x & 63;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = max(v, (u32)__shfl_xor((int)v, o, 64));
+    if (NW == 1) return uniform(v);
     __syncthreads();
-    if (lane == 0) sm[wave] = v;
+    if (lane == 0) sm[threadIdx.x >> 6] = v;
     __syncthreads();
+    v = (u32)sm[lane & (NW - 1)];
 #pragma unroll
-    for (int i = 0; i < NT / 64; ++i) v = max(v, (u32)sm[i]);
-    return v;
+    for (int o = NW / 2; o > 0; o >>= 1) v = max(v, (u32)__shfl_xor((int)v, o, 64));
+    return uniform(v);
 }
 
 // The lowest key of lo .. hi for which `is` holds; it holds for hi and, with a key, for all above.  64 probes at a time.
@@ -233,7 +269,7 @@ template <class F> __device__ __forceinline__ u32 first_key(u32 lo, u32 hi, F is
 }
 
 // ---- the search for a cut --------------------------------------------------------------------------------------------
-struct Cut { u32 key, ne; };
+struct Cut { u32 key, idx; };     // kept: keys above, and of what equals the key the indices up to idx
 
 struct Find {
     u32 klo, khi;        // the keys the cut is among
@@ -243,48 +279,49 @@ struct Find {
     u64 count, weight;   // of what lies above khi
 };
 
-// The bin in which the running sum (of counts, or of weights) over cnt / wt reaches target, and what lies before it.  false: it
-// never does.  Ends with a barrier.
-struct Hit { u32 bin; u64 count, weight; };
-struct ByCount { static constexpr bool value = false; };
-struct ByWeight { static constexpr bool value = true; };
-template <int NT, int NB, bool BYW> __device__ __forceinline__ bool select_bin(const u32* cnt, const u64* wt, u64 target, u64* sm, Hit* hit, Hit* at) {
-    constexpr int per = NB / NT > 0 ? NB / NT : 1;
-    const int b0 = threadIdx.x * per;
-    u64 c = 0, w = 0;
-    if (b0 < NB) {
-#pragma unroll
-        for (int i = 0; i < per; ++i) { c += cnt[b0 + i]; if (wt) w += wt[b0 + i]; }
-    }
-    u64 ct, wtot = 0, cb = block_scan<NT>(c, sm, &ct), wb = 0;
-    if (wt) wb = block_scan<NT>(w, sm, &wtot);
-    const u64 before = BYW ? wb : cb, mine = BYW ? w : c;
-    if (before < target && before + mine >= target) {
-        u32 b = b0;
-        u64 run = before;
-        for (int i = 0; i < per; ++i) {
-            const u64 x = BYW ? wt[b0 + i] : (u64)cnt[b0 + i];
-            if (run + x >= target) { b = b0 + i; break; }
-            run += x;
-            cb += cnt[b0 + i];
-            if (wt) wb += wt[b0 + i];
-        }
-        hit->bin = b;
-        hit->count = cb;
-        hit->weight = wb;
-    }
-    __syncthreads();
-    *at = *hit;
-    __syncthreads();
-    return (BYW ? wtot : ct) >= target;
-}
-
 // ceil(P W / 2^31), the weights that top-p keeps of W; at least 1, which the first outcome alone exceeds.
 __device__ __forceinline__ u64 mass_of(float top_p, u64 w) {
     const u64 part = (u64)__builtin_rint((double)top_p * 2147483648.0);
     const u64 low = part * (w & 0x7fffffffull);
     const u64 h = part * (w >> 31) + (low >> 31) + ((low & 0x7fffffffull) != 0);
     return h > 0 ? h : 1;
+}
+
+// The bin in which the running sum (of counts, or of weights) over cnt / wt reaches target, and what lies before it.  false: it
+// never does.  total: target holds top_p's bits, which the whole weight turns into the target.  Ends with a barrier.
+struct Hit { u32 bin; u64 count, weight, own; };        // own: outcomes in the bin
+struct ByCount { static constexpr bool value = false; };
+struct ByWeight { static constexpr bool value = true; };
+template <int NT, int NB, bool BYW> __device__ __forceinline__ bool select_bin(const u32* cnt, const u64* wt, u64 target, u64* sm, Hit* hit, Hit* at, u64* total = nullptr) {
+    constexpr int per = NB / NT > 0 ? NB / NT : 1;
+    const int b0 = threadIdx.x * per;
+    u64 c = 0, w = 0;
+    if (b0 < NB) {
+#pragma unroll
+        for (int i = 0; i < per; ++i) { if (cnt) c += cnt[b0 + i]; if (wt) w += wt[b0 + i]; }
+    }
+    u64 ct = 0, wtot = 0, cb = 0, wb = 0;
+    if (cnt) cb = block_scan<NT>(c, sm, &ct);
+    if (wt) wb = block_scan<NT>(w, sm, &wtot);
+    if (total) { *total = wtot; target = mass_of(__uint_as_float((u32)target), wtot); }
+    const u64 before = BYW ? wb : cb, mine = BYW ? w : c;
+    if (before < target && before + mine >= target) {
+        u32 b = b0;
+        u64 run = before, own = 0;
+        for (int i = 0; i < per; ++i) {
+            const u64 x = BYW ? wt[b0 + i] : (u64)cnt[b0 + i];
+            own = cnt ? cnt[b0 + i] : 0;
+            if (run + x >= target) { b = b0 + i; break; }
+            run += x;
+            if (cnt) cb += cnt[b0 + i];
+            if (wt) wb += wt[b0 + i];
+        }
+        *hit = Hit{b, cb, wb, own};
+    }
+    __syncthreads();
+    *at = *hit;
+    __syncthreads();
+    return (BYW ? wtot : ct) >= target;
 }
 
 // The keys of bin b of the first histogram, from `lowest` on.
@@ -302,11 +339,11 @@ template <int NB> __device__ __forceinline__ int key_shift(u32 range) {
 }
 
 // What is known of the cut once its bin is: the next keys to look at, or the cut itself.
-template <int KIND, bool BYW> __device__ __forceinline__ void settle(const Scale& s, Find& f) {
+template <int KIND, bool BYW> __device__ __forceinline__ void settle(const Scale& s, const double* powers, Find& f) {
     if (f.klo < f.khi) return;
     f.done = 1;
     if (BYW) {
-        const u64 w = weight<KIND>(s, value_of<KIND>(f.klo));
+        const u64 w = weight<KIND>(s, powers, value_of<KIND>(f.klo));
         f.ne = (u32)((f.target - f.weight + w - 1) / (w ? w : 1));
     } else {
         f.ne = (u32)(f.target - f.count);
@@ -345,268 +382,460 @@ template <int NT> __device__ __forceinline__ void write_none(const SampleArgs& a
 }
 
 // ---- a row's chunks --------------------------------------------------------------------------------------------------
-// What a wavefront's vectors of one step hold of the outcomes that are kept: four flags a lane; running: equals so far.
-template <int KIND> __device__ __forceinline__ u32 kept_flags(const float (&v)[4], const Cut& cut, u64 eq_before, int lane, u32* running) {
-    u32 gt = 0, eq = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const u32 k = key_of<KIND>(v[i]);
-        gt |= (u32)(k > cut.key) << i;
-        eq |= (u32)(k == cut.key) << i;
-    }
-    if (cut.ne == kAll) return gt | eq;
-    if (__ballot(eq != 0) == 0) return gt;
-    const u32 n = __popc(eq), incl = wave_scan(n, lane);
-    u64 rank = eq_before + *running + incl - n;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if ((eq >> i) & 1u) { if (rank < cut.ne) gt |= 1u << i; ++rank; }
-    *running += __shfl(incl, 63, 64);
-    return gt;
+template <int KIND> __device__ __forceinline__ bool keeps(const Cut& cut, u32 key, u32 idx) {
+    return key > cut.key || (key == cut.key && idx <= cut.idx);
 }
 
-// One chunk's sums: weights above the cut (WEIGHTS), and numbers above and at it (packed, 16 bits each).
-template <int KIND, bool WEIGHTS> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const Cut& cut, u32 j0, int steps, int lane, u64* w, u32* n) {
+// One chunk's numbers and (WEIGHTS) weights of what is kept.
+template <int KIND, int STEPS, bool WEIGHTS> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const double* powers, const Cut& cut, u32 j0, u32 lane, u64* w, u32* n) {
+    float v[STEPS][4];
+#pragma unroll
+    for (int it = 0; it < STEPS; ++it) load4<KIND>(row, j0 + it * 64u + lane, v[it]);
     u64 sum = 0;
     u32 num = 0;
-    for (int it = 0; it < steps; ++it) {
-        const u32 j = j0 + (u32)it * 64u + lane;
-        if (j >= row.vecs) break;
-        float v[4];
-        load4<KIND>(row, j, v);
+#pragma unroll
+    for (int it = 0; it < STEPS; ++it)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const u32 k = key_of<KIND>(v[i]);
-            num += (k > cut.key) + ((u32)(k == cut.key) << 16);
-            if (WEIGHTS && k > cut.key) sum += weight<KIND>(s, v[i]);
+            const bool keep = keeps<KIND>(cut, key_of<KIND>(v[it][i]), 4 * (j0 + it * 64u + lane) - row.skew + i);
+            num += keep;
+            if (WEIGHTS && keep) sum += weight<KIND>(s, powers, v[it][i]);
         }
-    }
     *n = wave_sum(num);
-    if (WEIGHTS) *w = wave_sum(sum);
+    *w = WEIGHTS ? wave_sum(sum) : 0;
+}
+
+// The index of the ne-th value of a chunk, `before` of them in earlier ones, that equals key; the whole wavefront asks.
+template <int KIND, int STEPS> __device__ __forceinline__ u32 nth_equal(const Row& row, u32 key, u32 ne, u32 j0, u32 lane) {
+    u32 run = 0, found = kAll;
+    for (int it = 0; it < STEPS; ++it) {
+        float v[4];
+        const u32 j = j0 + it * 64u + lane;
+        load4<KIND>(row, j, v);
+        u32 n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += key_of<KIND>(v[i]) == key;
+        const u32 incl = wave_scan(n);
+        u32 rank = run + incl - n, mine = kAll;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (key_of<KIND>(v[i]) == key && ++rank == ne) mine = 4 * j - row.skew + i;
+        const u64 who = __ballot(mine != kAll);
+        if (who) { found = lane_of(mine, (u32)__ffsll((long long)who) - 1u); break; }
+        run += last_lane(incl);
+    }
+    return found;
 }
 
 // The outcome of a chunk at which the running sum of kept weights, `base` before the chunk, exceeds t.  Whole wavefront.
-template <int KIND> __device__ __forceinline__ long long find_in_chunk(const Row& row, const Scale& s, const Cut& cut, u32 j0, int steps, u64 eq_before, u64 base, u64 t, int lane, u64* w_at) {
-    u32 running = 0;
-    for (int it = 0; it < steps; ++it) {
-        const u32 j = j0 + (u32)it * 64u + lane;
-        float v[4] = {kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f};
-        if (j < row.vecs) load4<KIND>(row, j, v);
-        const u32 keep = kept_flags<KIND>(v, cut, eq_before, lane, &running);
+template <int KIND, int STEPS> __device__ __forceinline__ long long find_in_chunk(const Row& row, const Scale& s, const double* powers, const Cut& cut, u32 j0, u64 base, u64 t, u32 lane, u64* w_at) {
+    for (int it = 0; it < STEPS; ++it) {
+        const u32 j = j0 + it * 64u + lane;
+        float v[4];
+        load4<KIND>(row, j, v);
         u64 w[4], four = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { w[i] = (keep >> i) & 1u ? weight<KIND>(s, v[i]) : 0; four += w[i]; }
-        const u64 incl = wave_scan(four, lane);
+        for (int i = 0; i < 4; ++i) {
+            w[i] = 0;
+            if (keeps<KIND>(cut, key_of<KIND>(v[i]), 4 * j - row.skew + i)) w[i] = weight<KIND>(s, powers, v[i]);
+            four += w[i];
+        }
+        const u64 incl = wave_scan(four);
         const u64 hit = __ballot(base + incl > t);
         if (hit) {
-            const int who = __ffsll((long long)hit) - 1;
+            const u32 who = (u32)__ffsll((long long)hit) - 1u;
             u64 run = base + incl - four, wk = 0;
-            long long k = 4ll * j - row.skew;
-            int at = -1;
+            u32 at = 4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { run += w[i]; if (at < 0 && run > t) { at = i; wk = w[i]; } }
-            k += at;
-            *w_at = __shfl(wk, who, 64);
-            return __shfl(k, who, 64);
+            for (u32 i = 0; i < 4; ++i) { run += w[i]; if (at == 4 && run > t) { at = i; wk = w[i]; } }
+            *w_at = lane_of(wk, who);
+            return (long long)lane_of(4 * j - row.skew + at, who);
         }
-        base += __shfl(incl, 63, 64);
+        base += last_lane(incl);
     }
     *w_at = 0;
     return -1;
 }
 
+// ---- sorting in LDS --------------------------------------------------------------------------------------------------
+// Ascending, n <= 2^k entries; those behind the n-th up to the next power of two are set to the highest number.
+template <int NT> __device__ __forceinline__ void sort_lds(u64* a, u32 n) {
+    u32 size = 2;
+    while (size < n) size <<= 1;
+    for (u32 i = n + threadIdx.x; i < size; i += NT) a[i] = ~0ull;
+    __syncthreads();
+    const bool one = size <= 128;                 // a wavefront's work: no barriers
+    if (!one || threadIdx.x < 64) {
+        for (u32 k = 2; k <= size; k <<= 1)
+            for (u32 j = k >> 1; j > 0; j >>= 1) {
+                for (u32 i = threadIdx.x; i < size / 2; i += NT) {
+                    const u32 lo = 2 * i - (i & (j - 1)), hi = lo + j;
+                    const u64 x = a[lo], y = a[hi];
+                    if ((x > y) == ((lo & k) == 0)) { a[lo] = y; a[hi] = x; }
+                }
+                if (one) __threadfence_block();
+                else __syncthreads();
+            }
+    }
+    __syncthreads();
+}
+
 // ---- one workgroup a row ---------------------------------------------------------------------------------------------
 template <int NT> struct Shape;
-// bins of a histogram, chunks, vectors of a lane in a chunk, outcomes of the list
-template <> struct Shape<64> { static constexpr int bins = 256, chunks = 4, steps = 1, list = 512; static constexpr u32 most = 512; };
-template <> struct Shape<256> { static constexpr int bins = 1024, chunks = 36, steps = 1, list = 2048; static constexpr u32 most = 8192; };
-template <> struct Shape<1024> { static constexpr int bins = 2048, chunks = 264, steps = 4, list = 2048; static constexpr u32 most = 262144; };
+// bins of a histogram (and entries of a list to be sorted), chunks, vectors of a lane in a chunk
+template <> struct Shape<64> { static constexpr int bins = 256, chunks = 4, steps = 1; static constexpr u32 most = 512; };
+template <> struct Shape<256> { static constexpr int bins = 1024, chunks = 36, steps = 1; static constexpr u32 most = 8192; };
+template <> struct Shape<1024> { static constexpr int bins = 2048, chunks = 264, steps = 4; static constexpr u32 most = 262144; };
 
 template <int KIND, int NT>
 __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
-    constexpr int NB = Shape<NT>::bins, NC = Shape<NT>::chunks, STEPS = Shape<NT>::steps, LIST = Shape<NT>::list;
-    __shared__ u64 wt[2][NB];
-    __shared__ u32 cnt[2][NB];
+    constexpr int NB = Shape<NT>::bins, NC = Shape<NT>::chunks, STEPS = Shape<NT>::steps, LIST = 2 * NB;
+    constexpr int UN = NT == 1024 ? 4 : 2;  // vectors of a thread on their way at once
+    __shared__ u64 wt[2 * NB];              // two histograms' weights, or: weights and entries of a list to be sorted, or: a list
+    __shared__ u32 cnt[2 * NB];
+    __shared__ double powers[kPowers];
     __shared__ u64 sm[16];
     __shared__ Hit hit;
-    __shared__ u64 chunk_w[NC];             // kept weights up to the chunk's end
-    __shared__ u32 chunk_n[NC], chunk_eq[NC];
-    static_assert(sizeof(u64) * LIST <= sizeof wt && sizeof(u32) * LIST <= sizeof cnt, "the list takes the histograms' place");
+    __shared__ u32 list_n, found;
+    __shared__ u64 chunk_w[NC];             // kept weights of chunks, later of those up to each
+    __shared__ u32 chunk_n[NC];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u32 lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const u64 r = grid_block();
     if (r >= (u64)a.rows) return;
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
     const u32 nchunks = (row.vecs + 64 * STEPS - 1) / (64 * STEPS);
 
-    u32 kmax = 0;
-    for (u32 j = threadIdx.x; j < row.vecs; j += NT) {
-        float v[4];
-        load4<KIND>(row, j, v);
+    auto each = [&](auto f) {               // f(key, value, index) for every value of the row, masked ones too
+        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
+            float v[UN][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) kmax = max(kmax, key_of<KIND>(v[i]));
-    }
+            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
+#pragma unroll
+            for (int u = 0; u < UN; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f(key_of<KIND>(v[u][i]), v[u][i], 4 * (j + u * NT) - row.skew + i);
+        }
+    };
+    u32 kmax = 0;
+    each([&](u32 k, float, u32) { kmax = max(kmax, k); });
+    fill_powers<NT>(powers);
+    if (threadIdx.x == 0) list_n = 0;
     kmax = block_max<NT>(kmax, sm);
+    __syncthreads();
     if (!p.ok || kmax < kLowest<KIND>) {
         write_none<NT>(a, r, 0, a.shots);
         if (threadIdx.x == 0 && a.kept) a.kept[r] = 0;
         return;
     }
-    const bool greedy = p.t == 0.f;
-    const Scale s = scale_of<KIND, NB>(kmax, greedy ? 1.f : p.t, a.bits);
+    if (p.t == 0.f) {
+        u32 first = 0;                      // the complement of the lowest index
+        each([&](u32 k, float, u32 idx) { if (k == kmax) first = max(first, ~idx); });
+        first = ~block_max<NT>(first, sm);
+        for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
+            const double u = a.uniforms[r * a.shots + i];
+            write_shot(a, r * a.shots + i, u >= 0.0 && u < 1.0 ? (long long)first : -1, 1, 1);
+        }
+        if (threadIdx.x == 0 && a.kept) a.kept[r] = 1;
+        return;
+    }
+    const Scale s = scale_of<KIND, NB>(kmax, p.t, a.bits);
     u32 lowest = kLowest<KIND>;
-    if (p.min_p > 0.f && !greedy)
+    if (p.min_p > 0.f)
         lowest = first_key(lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
+    u64* const lw = wt;                     // of a list to be sorted: weights, and entries
+    u64* const le = wt + NB;
 
-    // a histogram of the values with keys in klo .. khi: the first one over distances, later ones over keys
-    auto histogram = [&](int h, bool first, bool weights, u32 klo, u32 khi) {
-        for (int i = threadIdx.x; i < NB; i += NT) { cnt[h][i] = 0; wt[h][i] = 0; }
+    // a histogram (counts, weights) of the values with keys in klo .. khi: the first one over distances, later ones over keys
+    auto histogram = [&](int h, bool first, bool counts, bool weights, u32 klo, u32 khi) {
+        for (int i = threadIdx.x; i < NB; i += NT) { cnt[h * NB + i] = 0; wt[h * NB + i] = 0; }
         __syncthreads();
         const int shift = key_shift<NB>(khi - klo);
-        for (u32 j = threadIdx.x; j < row.vecs; j += NT) {
-            float v[4];
-            load4<KIND>(row, j, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const u32 k = key_of<KIND>(v[i]);
-                if (k < klo || k > khi) continue;
-                const u32 b = first ? bin_of<KIND, NB>(s, v[i], k) : (khi - k) >> shift;
-                atomicAdd(&cnt[h][b], 1u);
-                if (weights) atomicAdd(&wt[h][b], weight<KIND>(s, v[i]));
-            }
-        }
+        each([&](u32 k, float v, u32) {
+            if (k < klo || k > khi) return;
+            const u32 b = h * NB + (first ? bin_of<KIND, NB>(s, v, k) : (khi - k) >> shift);
+            if (counts) atomicAdd(&cnt[b], 1u);
+            if (weights) atomicAdd(&wt[b], weight<KIND>(s, powers, v));
+        });
         __syncthreads();
     };
+    // the list in order, its entries' weights; the sum of the weights before each thread's entries
+    constexpr int per = NB / NT;
+    auto ordered = [&](u32 n, u64 (&w)[per]) -> u64 {
+        sort_lds<NT>(le, n);
+        u64 sum = 0;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const u32 at = threadIdx.x * per + i;
+            w[i] = at < n ? weight<KIND>(s, powers, value_of<KIND>(~(u32)(le[at] >> 32))) : 0;
+            sum += w[i];
+        }
+        u64 all;
+        return block_scan<NT>(sum, sm, &all);
+    };
+    // how many of the first n entries it takes for `before` and their weights to reach target (all of them at most)
+    auto reach = [&](const u64 (&w)[per], u64 sum, u32 n, u64 before, u64 target) -> u32 {
+        if (threadIdx.x == 0) found = n;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const u32 at = threadIdx.x * per + i;
+            if (at < n && before + sum < target && before + sum + w[i] >= target) found = at + 1;
+            sum += w[i];
+        }
+        __syncthreads();
+        return uniform(found);
+    };
 
+    bool by_k = p.top_k > 0 && (u32)p.top_k < row.cols, by_p = p.top_p < 1.f, summed = false, slow = false;
     Cut cut{lowest, kAll};
-    u64 kept = ~0ull;                      // not known yet
-    if (greedy) {
-        cut = Cut{kmax, 1};
-        kept = 1;
-    } else if ((p.top_k > 0 && (u32)p.top_k < row.cols) || p.top_p < 1.f) {
-        const bool by_mass = p.top_p < 1.f;
-        histogram(0, true, by_mass, lowest, kmax);
-        u64 mass = 0;
-        bool have_mass = false;
-        auto narrow = [&](auto byw, Find f) -> Find {
-            constexpr bool BYW = decltype(byw)::value;
-            while (!f.done) {
-                histogram(1, false, by_mass, f.klo, f.khi);
-                Hit at;
-                if (!select_bin<NT, NB, BYW>(cnt[1], by_mass ? wt[1] : nullptr, f.target - (BYW ? f.weight : f.count), sm, &hit, &at))
-                    break;                 // (the row was written to while it was read)
-                const int shift = key_shift<NB>(f.khi - f.klo);
-                const u32 top = f.khi - (at.bin << shift);
-                const u32 low = top - f.klo < (1u << shift) ? f.klo : top - (1u << shift) + 1u;
-                f.khi = top;
-                f.klo = low;
-                f.count += at.count;
-                f.weight += at.weight;
-                settle<KIND, BYW>(s, f);
+    Hit at;
+    if (by_k) {
+        histogram(0, true, true, false, lowest, kmax);
+        by_k = select_bin<NT, NB, false>(cnt, nullptr, (u64)p.top_k, sm, &hit, &at);
+        slow = by_k && (by_p || at.own > NB);
+    }
+    if (by_k && at.count + at.own <= NB) {
+        // few outcomes down to the bin: in order they give the cut, and by index the draw
+        each([&](u32 k, float v, u32 idx) {
+            if (k >= lowest && bin_of<KIND, NB>(s, v, k) <= at.bin) {
+                const u32 slot = atomicAdd(&list_n, 1u);
+                if (slot < NB) le[slot] = (u64)~k << 32 | idx;
             }
-            return f;
-        };
-        auto begin = [&](auto byw, u64 target, Find* f) -> bool {
+        });
+        __syncthreads();
+        u64 w[per];
+        u32 n = min(list_n, (u32)NB);      // (more only if the row was written to meanwhile)
+        const u64 before = ordered(n, w);
+        n = min(n, (u32)p.top_k);
+        if (by_p) {
+            u64 mass = 0;
+#pragma unroll
+            for (int i = 0; i < per; ++i) if (threadIdx.x * per + i < n) mass += w[i];
+            u64 all;
+            (void)block_scan<NT>(mass, sm, &all);
+            n = reach(w, before, n, 0, mass_of(p.top_p, all));
+        }
+        u64 e[per];
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const u32 k = threadIdx.x * per + i;
+            lw[k] = w[i];
+            e[i] = k < n ? (le[k] & 0xffffffffull) << 32 | k : 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < per; ++i) if (threadIdx.x * per + i < n) le[threadIdx.x * per + i] = e[i];
+        __syncthreads();
+        sort_lds<NT>(le, n);
+        u64 sum = 0, total;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const u32 k = threadIdx.x * per + i;
+            w[i] = k < n ? lw[(u32)le[k]] : 0;
+            sum += w[i];
+        }
+        u64 run = block_scan<NT>(sum, sm, &total);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < per; ++i) { run += w[i]; lw[threadIdx.x * per + i] = run; }
+        __syncthreads();
+        if (threadIdx.x == 0 && a.kept) a.kept[r] = (int)n;
+        for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
+            const double u = a.uniforms[r * a.shots + i];
+            if (!(u >= 0.0 && u < 1.0)) { write_shot(a, r * a.shots + i, -1, 0, 1); continue; }
+            const u64 t = draw_at(u, total);
+            u32 lo = 0, len = n;                           // the first with a sum above t is in lo .. lo + len - 1
+            while (len > 1) {
+                const u32 half = len >> 1;
+                if (lw[lo + half - 1] > t) len = half;
+                else { lo += half; len -= half; }
+            }
+            write_shot(a, r * a.shots + i, (long long)(le[lo] >> 32), lw[lo] - (lo ? lw[lo - 1] : 0), total);
+        }
+        return;
+    }
+    u64 mass = 0;
+    if (!by_k && by_p) {
+        histogram(0, true, false, true, lowest, kmax);
+        (void)select_bin<NT, NB, true>(nullptr, wt, (u64)__float_as_uint(p.top_p), sm, &hit, &at, &mass);
+    }
+    if ((by_k || by_p) && !slow) {
+        // what lies above the bin is kept, what lies in it decides: the chunks' sums of the ones, a list of the others
+        for (u32 c = wave; c < nchunks; c += NT / 64) {
+            float v[STEPS][4];
+#pragma unroll
+            for (int it = 0; it < STEPS; ++it) load4<KIND>(row, c * 64 * STEPS + it * 64u + lane, v[it]);
+            u64 sum = 0;
+            u32 num = 0;
+#pragma unroll
+            for (int it = 0; it < STEPS; ++it)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const u32 k = key_of<KIND>(v[it][i]);
+                    const u32 b = k >= lowest ? bin_of<KIND, NB>(s, v[it][i], k) : kAll;
+                    if (b < at.bin) { ++num; sum += weight<KIND>(s, powers, v[it][i]); }
+                    if (b == at.bin) {
+                        const u32 slot = atomicAdd(&list_n, 1u);
+                        if (slot < NB) le[slot] = (u64)~k << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
+                    }
+                }
+            num = wave_sum(num);
+            sum = wave_sum(sum);
+            if (lane == 0) { chunk_n[c] = num; chunk_w[c] = sum; }
+        }
+        __syncthreads();
+        u32 n = list_n;
+        if (n <= NB) {
+            u64 w[per];
+            const u64 before = ordered(n, w);
+            n = by_k ? min(n, (u32)((u64)p.top_k - at.count)) : reach(w, before, n, at.weight, mass_of(p.top_p, mass));
+            const u64 last = le[n > 0 ? n - 1 : 0];
+            cut = Cut{~(u32)(last >> 32), (u32)last};
+#pragma unroll
+            for (int i = 0; i < per; ++i) {
+                const u32 k = threadIdx.x * per + i;
+                if (k >= n) continue;
+                const u32 c = ((u32)le[k] + row.skew) / (256 * STEPS);
+                atomicAdd(&chunk_n[c], 1u);
+                atomicAdd(&chunk_w[c], w[i]);
+            }
+            summed = true;
+        } else {
+            slow = true;                   // a bin of (nearly) equal values
+        }
+        __syncthreads();
+    }
+    if (slow) {
+        // bins of keys, narrower each time, down to the cut's own
+        histogram(0, true, true, by_p, lowest, kmax);
+        bool have_mass = false;
+        auto narrow = [&](auto byw, u64 target, Find* f) -> bool {
             constexpr bool BYW = decltype(byw)::value;
-            Hit at;
-            if (!select_bin<NT, NB, BYW>(cnt[0], by_mass ? wt[0] : nullptr, target, sm, &hit, &at)) return false;
-            keys_of_bin<KIND, NB>(s, at.bin, lowest, &f->klo, &f->khi);
+            Hit in;
+            if (!select_bin<NT, NB, BYW>(cnt, by_p ? wt : nullptr, target, sm, &hit, &in)) return false;
+            keys_of_bin<KIND, NB>(s, in.bin, lowest, &f->klo, &f->khi);
             f->done = 0;
             f->ne = 0;
             f->target = target;
-            f->count = at.count;
-            f->weight = at.weight;
-            settle<KIND, BYW>(s, *f);
+            f->count = in.count;
+            f->weight = in.weight;
+            settle<KIND, BYW>(s, powers, *f);
+            while (!f->done) {
+                histogram(1, false, true, by_p, f->klo, f->khi);
+                if (!select_bin<NT, NB, BYW>(cnt + NB, by_p ? wt + NB : nullptr, f->target - (BYW ? f->weight : f->count), sm, &hit, &in))
+                    return false;          // (the row was written to while it was read)
+                const int shift = key_shift<NB>(f->khi - f->klo);
+                const u32 top = f->khi - (in.bin << shift);
+                f->klo = top - f->klo < (1u << shift) ? f->klo : top - (1u << shift) + 1u;
+                f->khi = top;
+                f->count += in.count;
+                f->weight += in.weight;
+                settle<KIND, BYW>(s, powers, *f);
+            }
             return true;
         };
         Find f;
-        if (p.top_k > 0 && begin(ByCount{}, (u64)p.top_k, &f)) {
-            f = narrow(ByCount{}, f);
-            cut = Cut{f.klo, f.ne};
-            kept = (u64)p.top_k;
-            if (by_mass) mass = f.weight + (u64)f.ne * weight<KIND>(s, value_of<KIND>(f.klo));
+        u32 ne = kAll;
+        if (by_k && narrow(ByCount{}, (u64)p.top_k, &f)) {
+            cut.key = f.klo;
+            ne = f.ne;
+            if (by_p) mass = f.weight + (u64)f.ne * weight<KIND>(s, powers, value_of<KIND>(f.klo));
             have_mass = true;
         }
-        if (by_mass) {
+        if (by_p) {
             if (!have_mass) {
-                u64 part = 0;
-                for (int i = threadIdx.x; i < NB; i += NT) part += wt[0][i];
-                (void)block_scan<NT>(part, sm, &mass);
+                u64 sum = 0;
+                for (int i = threadIdx.x; i < NB; i += NT) sum += wt[i];
+                (void)block_scan<NT>(sum, sm, &mass);
             }
-            if (begin(ByWeight{}, mass_of(p.top_p, mass), &f)) {
-                f = narrow(ByWeight{}, f);
-                cut = Cut{f.klo, f.ne};
-                kept = f.count + f.ne;
+            if (narrow(ByWeight{}, mass_of(p.top_p, mass), &f)) {
+                cut.key = f.klo;
+                ne = f.ne;
             }
         }
+        // the index of the last that stays of what equals the key
+        for (u32 c = wave; c < nchunks; c += NT / 64) {
+            u32 n = 0;
+            for (int it = 0; it < STEPS; ++it) {
+                float v[4];
+                load4<KIND>(row, c * 64 * STEPS + it * 64u + lane, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n += key_of<KIND>(v[i]) == cut.key;
+            }
+            n = wave_sum(n);
+            if (lane == 0) chunk_n[c] = n;
+        }
+        if (threadIdx.x == 0) found = kAll;
+        __syncthreads();
+        static_assert(NC <= NT || NT == 64, "a thread has a chunk");
+        const u32 mine = threadIdx.x < nchunks ? chunk_n[threadIdx.x] : 0;
+        u64 all;
+        const u64 before = block_scan<NT>((u64)mine, sm, &all);
+        if (before < ne && before + mine >= ne) { found = threadIdx.x; list_n = (u32)(ne - before); }
+        __syncthreads();
+        if (found != kAll) cut.idx = nth_equal<KIND, STEPS>(row, cut.key, list_n, found * 64 * STEPS, lane);
+        __syncthreads();
     }
-
-    // the chunks' numbers of kept outcomes, and their weights where the outcomes do not fit the list
-    const bool list = kept <= (u64)LIST || row.cols <= (u32)LIST;
-    for (u32 c = wave; c < nchunks; c += NT / 64) {
-        u64 w = 0;
-        u32 n;
-        if (list) chunk_sums<KIND, false>(row, s, cut, c * 64 * STEPS, STEPS, lane, &w, &n);
-        else chunk_sums<KIND, true>(row, s, cut, c * 64 * STEPS, STEPS, lane, &w, &n);
-        if (lane == 0) { chunk_w[c] = w; chunk_n[c] = n; }
+    if (!summed) {
+        for (u32 c = wave; c < nchunks; c += NT / 64) {
+            u64 w;
+            u32 n;
+            chunk_sums<KIND, STEPS, true>(row, s, powers, cut, c * 64 * STEPS, lane, &w, &n);
+            if (lane == 0) { chunk_w[c] = w; chunk_n[c] = n; }
+        }
+        __syncthreads();
     }
-    __syncthreads();
     u64 total, n_kept;
     {
-        constexpr int per = (NC + NT - 1) / NT;
-        static_assert(per == 1, "a thread has a chunk");
         const bool mine = threadIdx.x < nchunks;
         const u32 n = mine ? chunk_n[threadIdx.x] : 0u;
-        const u64 eq = n >> 16;
-        u64 unused;
-        const u64 eq_before = block_scan<NT>(eq, sm, &unused);
-        const u64 take = eq_before >= cut.ne ? 0 : min(eq, (u64)cut.ne - eq_before);
-        const u64 num = (n & 0xffffu) + take;
-        const u64 w_cut = list ? 0 : weight<KIND>(s, value_of<KIND>(cut.key));
-        const u64 w = (mine ? chunk_w[threadIdx.x] : 0) + take * w_cut;
-        const u64 num_before = block_scan<NT>(num, sm, &n_kept);
+        const u64 w = mine ? chunk_w[threadIdx.x] : 0u;
+        const u64 n_before = block_scan<NT>((u64)n, sm, &n_kept);
         const u64 w_before = block_scan<NT>(w, sm, &total);
         if (mine) {
-            chunk_eq[threadIdx.x] = (u32)min(eq_before, (u64)kAll);
-            chunk_n[threadIdx.x] = (u32)num_before | (num ? 0x80000000u : 0u);     // (2^18 outcomes at most)
+            chunk_n[threadIdx.x] = (u32)n_before | (n ? 0x80000000u : 0u);     // (2^18 outcomes at most)
             chunk_w[threadIdx.x] = w_before + w;
         }
     }
     __syncthreads();
     if (threadIdx.x == 0 && a.kept) a.kept[r] = (int)n_kept;
-    if (list) {
-        u64* lw = wt[0];
-        u32* lk = cnt[0];
+    if (n_kept <= LIST && a.shots > NT / 64) {
+        // several shots a wavefront: what is left as a list by index, a thread for every shot
+        u64* lw = wt;
+        u32* lk = cnt;
         for (u32 c = wave; c < nchunks; c += NT / 64) {
             const u32 packed = chunk_n[c];
             if (!(packed >> 31)) continue;
-            u32 pos = packed & 0x7fffffffu, running = 0;
+            u32 pos = packed & 0x7fffffffu;
             for (int it = 0; it < STEPS; ++it) {
-                const u32 j = c * 64 * STEPS + (u32)it * 64u + lane;
-                float v[4] = {kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f, kLogs<KIND> ? -kInf : 0.f};
-                if (j < row.vecs) load4<KIND>(row, j, v);
-                const u32 keep = kept_flags<KIND>(v, cut, chunk_eq[c], lane, &running);
-                const u32 n = __popc(keep), incl = wave_scan(n, lane);
-                u32 at = pos + incl - n;
+                const u32 j = c * 64 * STEPS + it * 64u + lane;
+                float v[4];
+                load4<KIND>(row, j, v);
+                u32 keep = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) keep |= (u32)keeps<KIND>(cut, key_of<KIND>(v[i]), 4 * j - row.skew + i) << i;
+                const u32 n = __popc(keep), incl = wave_scan(n);
+                u32 to = pos + incl - n;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if ((keep >> i) & 1u) { lw[at] = key_of<KIND>(v[i]); lk[at] = 4u * j - row.skew + i; ++at; }
-                pos += __shfl(incl, 63, 64);
+                    if ((keep >> i) & 1u) { lw[to] = key_of<KIND>(v[i]); lk[to] = 4u * j - row.skew + i; ++to; }
+                pos += last_lane(incl);
             }
         }
         __syncthreads();
-        constexpr int per = LIST / NT;
-        u64 w[per], sum = 0;
-        const u32 first = threadIdx.x * per;
+        constexpr int own = LIST / NT;
+        u64 w[own], sum = 0;
+        const u32 first = threadIdx.x * own;
 #pragma unroll
-        for (int i = 0; i < per; ++i) {
-            w[i] = first + i < n_kept ? weight<KIND>(s, value_of<KIND>((u32)lw[first + i])) : 0;
+        for (int i = 0; i < own; ++i) {
+            w[i] = first + i < n_kept ? weight<KIND>(s, powers, value_of<KIND>((u32)lw[first + i])) : 0;
             sum += w[i];
         }
         u64 run = block_scan<NT>(sum, sm, &total);
 #pragma unroll
-        for (int i = 0; i < per; ++i) {
+        for (int i = 0; i < own; ++i) {
             run += w[i];
             if (first + i < n_kept) lw[first + i] = run;
         }
@@ -615,7 +844,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             const double u = a.uniforms[r * a.shots + i];
             if (!(u >= 0.0 && u < 1.0)) { write_shot(a, r * a.shots + i, -1, 0, 1); continue; }
             const u64 t = draw_at(u, total);
-            u32 lo = 0, len = (u32)n_kept;                 // the first with a sum above t is in lo .. lo + len - 1
+            u32 lo = 0, len = (u32)n_kept;
             while (len > 1) {
                 const u32 half = len >> 1;
                 if (lw[lo + half - 1] > t) len = half;
@@ -633,10 +862,10 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             const u64 t = draw_at(u, total);
             u32 c = 0;
             for (u32 c0 = 0; c0 < nchunks; c0 += 64) {
-                const u64 above = __ballot(c0 + lane < nchunks && chunk_w[min(c0 + (u32)lane, nchunks - 1)] > t);
+                const u64 above = __ballot(c0 + lane < nchunks && chunk_w[min(c0 + lane, nchunks - 1)] > t);
                 if (above) { c = c0 + (u32)__ffsll((long long)above) - 1u; break; }
             }
-            k = find_in_chunk<KIND>(row, s, cut, c * 64 * STEPS, STEPS, chunk_eq[c], c ? chunk_w[c - 1] : 0, t, lane, &w);
+            k = find_in_chunk<KIND, STEPS>(row, s, powers, cut, c * 64 * STEPS, c ? chunk_w[c - 1] : 0, t, lane, &w);
         }
         if (lane == 0) write_shot(a, r * a.shots + i, k, w, total);
     }
@@ -655,8 +884,9 @@ struct LongState {
     u32 ok, kmax, lowest, stage;       // stage 0: no search under way; 1: top-k; 2: top-p
     Find f;
     Cut cut;
-    u64 mass, kept;
+    u32 ne;              // how many of what equals the cut's key stay
     u32 have_mass;
+    u64 mass;
 };
 
 struct Long {
@@ -706,11 +936,14 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_max(c
     const Row row = row_of<KIND>(a, r);
     u32 j0, j1, kmax = 0;
     part_of<KIND>(row, g, part, &j0, &j1);
-    for (u32 j = j0 + threadIdx.x; j < j1; j += kLongThreads) {
-        float v[4];
-        load4<KIND>(row, j, v);
+    for (u32 j = j0 + threadIdx.x; j < j1; j += 4 * kLongThreads) {
+        float v[4][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) kmax = max(kmax, key_of<KIND>(v[i]));
+        for (int u = 0; u < 4; ++u) load4<KIND>(row, min(j + u * kLongThreads, j1 - 1), v[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) kmax = max(kmax, key_of<KIND>(v[u][i]));
     }
     kmax = block_max<kLongThreads>(kmax, sm);
     if (threadIdx.x == 0) g.pmax[r * g.parts + part] = kmax;
@@ -726,21 +959,27 @@ __device__ __forceinline__ bool by_top_k(const SampleArgs& a, const Params& p) {
 __device__ __forceinline__ bool by_top_p(const Params& p) { return p.t > 0.f && p.top_p < 1.f; }
 
 // The histogram of the values of vectors j0 .. j1 with keys in klo .. khi, added to the row's.
-template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, u64* wt, u32* cnt, u64* gw, u32* gc) {
+template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, const double* powers, u64* wt, u32* cnt, u64* gw, u32* gc) {
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) { cnt[i] = 0; wt[i] = 0; }
     __syncthreads();
     const int shift = key_shift<kLongBins>(khi - klo);
-    for (u32 j = j0 + threadIdx.x; j < j1; j += kLongThreads) {
-        float v[4];
-        load4<KIND>(row, j, v);
+    for (u32 j = j0 + threadIdx.x; j < j1; j += 4 * kLongThreads) {
+        float v[4][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32 k = key_of<KIND>(v[i]);
-            if (k < klo || k > khi) continue;
-            const u32 b = first ? bin_of<KIND, kLongBins>(s, v[i], k) : (khi - k) >> shift;
-            atomicAdd(&cnt[b], 1u);
-            if (weights) atomicAdd(&wt[b], weight<KIND>(s, v[i]));
+        for (int u = 0; u < 4; ++u) {
+            if (j + u * kLongThreads < j1) load4<KIND>(row, j + u * kLongThreads, v[u]);
+            else for (int i = 0; i < 4; ++i) v[u][i] = kLogs<KIND> ? -kInf : 0.f;
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32 k = key_of<KIND>(v[u][i]);
+                if (k < klo || k > khi) continue;
+                const u32 b = first ? bin_of<KIND, kLongBins>(s, v[u][i], k) : (khi - k) >> shift;
+                atomicAdd(&cnt[b], 1u);
+                if (weights) atomicAdd(&wt[b], weight<KIND>(s, powers, v[u][i]));
+            }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) {
@@ -754,6 +993,9 @@ template <int KIND> __device__ __forceinline__ void long_histogram(const Row& ro
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first(const SampleArgs a, const Long g) {
     __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
     __shared__ u32 cnt[kLongBins];
+    __shared__ double powers[kPowers];
+    fill_powers<kLongThreads>(powers);
+    __syncthreads();
     const u64 r = grid_block() / g.parts;
     const u32 part = (u32)(grid_block() % g.parts);
     if (r >= (u64)a.rows) return;
@@ -766,23 +1008,23 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first
     st.ok = p.ok && kmax >= kLowest<KIND>;
     st.kmax = kmax;
     st.lowest = kLowest<KIND>;
-    st.kept = ~0ull;
     if (st.ok) {
         const Scale s = scale_of<KIND, kLongBins>(kmax, p.t > 0.f ? p.t : 1.f, a.bits);
         if (p.min_p > 0.f && p.t > 0.f)
             st.lowest = first_key(st.lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
-        st.cut = p.t > 0.f ? Cut{st.lowest, kAll} : Cut{kmax, 1};
+        st.cut = Cut{p.t > 0.f ? st.lowest : kmax, kAll};
+        st.ne = p.t > 0.f ? kAll : 1;
         if (by_top_k(a, p) || by_top_p(p)) {
             u32 j0, j1;
             part_of<KIND>(row, g, part, &j0, &j1);
-            long_histogram<KIND>(row, s, j0, j1, true, by_top_p(p), st.lowest, kmax, wt, cnt, g.wt + r * (kLevels * kLongBins), g.cnt + r * (kLevels * kLongBins));
+            long_histogram<KIND>(row, s, j0, j1, true, by_top_p(p), st.lowest, kmax, powers, wt, cnt, g.wt + r * (kLevels * kLongBins), g.cnt + r * (kLevels * kLongBins));
         }
     }
     if (part == 0 && threadIdx.x == 0) g.state[r * kLevels] = st;
 }
 
 // The search after the histogram of level `prev`.
-template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_advance(const SampleArgs& a, const Params& p, const Scale& s, const Long& g, u64 r, int prev, u64* sm, Hit* hit, LongState* st) {
+template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_advance(const SampleArgs& a, const Params& p, const Scale& s, const double* powers, const Long& g, u64 r, int prev, u64* sm, Hit* hit, LongState* st) {
     if (!st->stage) return;
     Find& f = st->f;
     const u64* wt = g.wt + (r * kLevels + prev) * kLongBins;
@@ -798,20 +1040,20 @@ template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_
         f.khi = top;
         f.count += at.count;
         f.weight += at.weight;
-        if (st->stage == 1) settle<KIND, false>(s, f);
-        else settle<KIND, true>(s, f);
+        if (st->stage == 1) settle<KIND, false>(s, powers, f);
+        else settle<KIND, true>(s, powers, f);
     }
     if (!f.done) return;
-    st->cut = Cut{f.klo, f.ne};
-    st->kept = f.count + f.ne;
+    st->cut = Cut{f.klo, kAll};
+    st->ne = f.ne;
     if (st->stage == 1 && by_top_p(p)) {
-        st->mass = f.weight + (u64)f.ne * weight<KIND>(s, value_of<KIND>(f.klo));
+        st->mass = f.weight + (u64)f.ne * weight<KIND>(s, powers, value_of<KIND>(f.klo));
         st->have_mass = 1;
     }
     st->stage = 0;
 }
 
-template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs& a, const Params& p, const Scale& s, const Long& g, u64 r, u32 stage, u64* sm, Hit* hit, LongState* st) {
+template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs& a, const Params& p, const Scale& s, const double* powers, const Long& g, u64 r, u32 stage, u64* sm, Hit* hit, LongState* st) {
     const u64* wt = g.wt + r * kLevels * kLongBins;
     const u32* cnt = g.cnt + r * kLevels * kLongBins;
     Hit at;
@@ -836,17 +1078,20 @@ template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs&
     f.target = target;
     f.count = at.count;
     f.weight = at.weight;
-    if (stage == 1) settle<KIND, false>(s, f);
-    else settle<KIND, true>(s, f);
+    if (stage == 1) settle<KIND, false>(s, powers, f);
+    else settle<KIND, true>(s, powers, f);
     st->f = f;
     st->stage = stage;
-    if (f.done) long_advance<KIND>(a, p, s, g, r, 0, sm, hit, st);
+    if (f.done) long_advance<KIND>(a, p, s, powers, g, r, 0, sm, hit, st);
 }
 
 // Level `level` after level `prev`: the first level of top-k is 1, that of top-p 1 + kKeySteps.
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(const SampleArgs a, const Long g, int level, int prev) {
     __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
     __shared__ u32 cnt[kLongBins];
+    __shared__ double powers[kPowers];
+    fill_powers<kLongThreads>(powers);
+    __syncthreads();
     __shared__ Hit hit;
     const u64 r = grid_block() / g.parts;
     const u32 part = (u32)(grid_block() % g.parts);
@@ -856,23 +1101,26 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(
     LongState st = g.state[r * kLevels + prev];
     if (st.ok) {
         const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-        long_advance<KIND>(a, p, s, g, r, prev, sm, &hit, &st);
-        if (level == 1 && by_top_k(a, p)) long_begin<KIND>(a, p, s, g, r, 1, sm, &hit, &st);
-        if (level == 1 + kKeySteps && by_top_p(p)) long_begin<KIND>(a, p, s, g, r, 2, sm, &hit, &st);
+        long_advance<KIND>(a, p, s, powers, g, r, prev, sm, &hit, &st);
+        if (level == 1 && by_top_k(a, p)) long_begin<KIND>(a, p, s, powers, g, r, 1, sm, &hit, &st);
+        if (level == 1 + kKeySteps && by_top_p(p)) long_begin<KIND>(a, p, s, powers, g, r, 2, sm, &hit, &st);
         if (st.stage) {
             u32 j0, j1;
             part_of<KIND>(row, g, part, &j0, &j1);
             const size_t at = (r * kLevels + level) * kLongBins;
-            long_histogram<KIND>(row, s, j0, j1, false, by_top_p(p), st.f.klo, st.f.khi, wt, cnt, g.wt + at, g.cnt + at);
+            long_histogram<KIND>(row, s, j0, j1, false, by_top_p(p), st.f.klo, st.f.khi, powers, wt, cnt, g.wt + at, g.cnt + at);
         }
     }
     if (part == 0 && threadIdx.x == 0) g.state[r * kLevels + level] = st;
 }
 
-// The chunks' sums of what is kept.
+// The chunks' weights and numbers above the cut's key, and how many equal it.
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(const SampleArgs a, const Long g, int prev) {
     __shared__ u64 sm[kLongThreads / 64];
     __shared__ Hit hit;
+    __shared__ double powers[kPowers];
+    fill_powers<kLongThreads>(powers);
+    __syncthreads();
     const u64 r = grid_block() / g.parts;
     const u32 part = (u32)(grid_block() % g.parts);
     if (r >= (u64)a.rows) return;
@@ -881,13 +1129,25 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     LongState st = g.state[r * kLevels + prev];
     if (!st.ok) return;
     const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-    long_advance<KIND>(a, p, s, g, r, prev, sm, &hit, &st);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    long_advance<KIND>(a, p, s, powers, g, r, prev, sm, &hit, &st);
+    const u32 lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const u32 c1 = min((part + 1) * g.chunks_per_part, g.chunks);
     for (u32 c = part * g.chunks_per_part + wave; c < c1; c += kLongThreads / 64) {
-        u64 w;
-        u32 n;
-        chunk_sums<KIND, true>(row, s, st.cut, c * 64 * kLongSteps, kLongSteps, lane, &w, &n);
+        float v[kLongSteps][4];
+#pragma unroll
+        for (int it = 0; it < kLongSteps; ++it) load4<KIND>(row, c * 64 * kLongSteps + it * 64u + lane, v[it]);
+        u64 w = 0;
+        u32 n = 0;
+#pragma unroll
+        for (int it = 0; it < kLongSteps; ++it)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32 k = key_of<KIND>(v[it][i]);
+                n += (k > st.cut.key) + ((u32)(k == st.cut.key) << 16);
+                if (k > st.cut.key) w += weight<KIND>(s, powers, v[it][i]);
+            }
+        n = wave_sum(n);
+        w = wave_sum(w);
         if (lane == 0) {
             g.chunk_w[r * g.chunks + c] = w;
             g.chunk_n[r * g.chunks + c] = n;
@@ -895,7 +1155,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     }
 }
 
-template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const Cut& cut, const u64* cw, const u32* ce, u32 chunks, u64 at, int lane) {
+template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const double* powers, const Cut& cut, const u64* cw, u32 chunks, u64 at, u32 lane) {
     const double u = a.uniforms[at];
     const u64 total = cw[chunks - 1];
     long long k = -1;
@@ -912,20 +1172,27 @@ template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& 
             lo += off;
             len = min(stride, len - off);
         }
-        k = find_in_chunk<KIND>(row, s, cut, lo * 64 * kLongSteps, kLongSteps, ce[lo], lo ? cw[lo - 1] : 0, t, lane, &w);
+        k = find_in_chunk<KIND, kLongSteps>(row, s, powers, cut, lo * 64 * kLongSteps, lo ? cw[lo - 1] : 0, t, lane, &w);
     }
     if (lane == 0) write_shot(a, at, k, w, total);
 }
 
-// One workgroup a row: running sums over its chunks, and (draw) its shots.
+// One workgroup a row: running sums over its chunks, the last index that stays of what equals the cut's key, and (draw) its
+// shots.
 template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const SampleArgs a, const Long g, int prev, int draw) {
     __shared__ u64 sm[16];
     __shared__ Hit hit;
+    __shared__ double powers[kPowers];
+    __shared__ u32 found, rank;
+    fill_powers<1024>(powers);
+    if (threadIdx.x == 0) found = kAll;
+    __syncthreads();
     const u64 r = grid_block();
     if (r >= (u64)a.rows) return;
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
     LongState st = g.state[r * kLevels + prev];
+    __syncthreads();                               // (the state that is written may be the one that was read)
     if (!st.ok) {
         if (draw) write_none<1024>(a, r, 0, a.shots);
         if (threadIdx.x == 0 && a.kept) a.kept[r] = 0;
@@ -933,19 +1200,20 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
         return;
     }
     const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-    long_advance<KIND, 1024>(a, p, s, g, r, prev, sm, &hit, &st);
+    long_advance<KIND, 1024>(a, p, s, powers, g, r, prev, sm, &hit, &st);
     u64* cw = g.chunk_w + r * g.chunks;
-    u32* cn = g.chunk_n + r * g.chunks;
+    const u32* cn = g.chunk_n + r * g.chunks;
     const u32 per = (g.chunks + 1023) / 1024;
     const u32 c0 = min(threadIdx.x * per, g.chunks), c1 = min(c0 + per, g.chunks);
     u64 eq = 0, eq_all, n_kept, total;
     for (u32 c = c0; c < c1; ++c) eq += cn[c] >> 16;
     const u64 eq_before = block_scan<1024>(eq, sm, &eq_all);
-    const u64 w_cut = weight<KIND>(s, value_of<KIND>(st.cut.key));
+    const u64 w_cut = weight<KIND>(s, powers, value_of<KIND>(st.cut.key));
     u64 run = eq_before, num = 0, w = 0;
     for (u32 c = c0; c < c1; ++c) {
         const u32 n = cn[c];
-        const u64 take = run >= st.cut.ne ? 0 : min((u64)(n >> 16), (u64)st.cut.ne - run);
+        const u64 take = run >= st.ne ? 0 : min((u64)(n >> 16), (u64)st.ne - run);
+        if (run < st.ne && run + (n >> 16) >= st.ne) { found = c; rank = (u32)(st.ne - run); }
         num += (n & 0xffffu) + take;
         w += cw[c] + take * w_cut;
         run += n >> 16;
@@ -955,12 +1223,13 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     run = eq_before;
     for (u32 c = c0; c < c1; ++c) {
         const u32 n = cn[c];
-        const u64 take = run >= st.cut.ne ? 0 : min((u64)(n >> 16), (u64)st.cut.ne - run);
+        const u64 take = run >= st.ne ? 0 : min((u64)(n >> 16), (u64)st.ne - run);
         sum += cw[c] + take * w_cut;
         cw[c] = sum;
-        cn[c] = (u32)run;
         run += n >> 16;
     }
+    const u32 lane = threadIdx.x & 63;
+    if (found != kAll) st.cut.idx = nth_equal<KIND, kLongSteps>(row, st.cut.key, rank, found * 64 * kLongSteps, lane);
     if (threadIdx.x == 0) {
         if (a.kept) a.kept[r] = (int)n_kept;
         g.state[r * kLevels + kLevels - 1] = st;
@@ -969,15 +1238,18 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     __threadfence_block();
     __syncthreads();
     for (u64 i = threadIdx.x >> 6; i < (u64)a.shots; i += 16)
-        long_shot<KIND>(a, row, s, st.cut, cw, cn, g.chunks, r * a.shots + i, threadIdx.x & 63);
+        long_shot<KIND>(a, row, s, powers, st.cut, cw, g.chunks, r * a.shots + i, lane);
 }
 
 template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const SampleArgs a, const Long g) {
+    __shared__ double powers[kPowers];
+    fill_powers<256>(powers);
+    __syncthreads();
     const u64 at = grid_block() * 4 + (threadIdx.x >> 6);
     if (at >= (u64)a.rows * a.shots) return;
     const u64 r = at / a.shots;
     const LongState st = g.state[r * kLevels + kLevels - 1];
-    const int lane = threadIdx.x & 63;
+    const u32 lane = threadIdx.x & 63;
     if (!st.ok) {
         if (lane == 0) write_shot(a, at, -1, 0, 1);
         return;
@@ -985,7 +1257,7 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
     const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-    long_shot<KIND>(a, row, s, st.cut, g.chunk_w + r * g.chunks, g.chunk_n + r * g.chunks, g.chunks, at, lane);
+    long_shot<KIND>(a, row, s, powers, st.cut, g.chunk_w + r * g.chunks, g.chunks, at, lane);
 }
 
 }  // namespace
