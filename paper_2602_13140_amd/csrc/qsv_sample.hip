@@ -27,13 +27,12 @@ template <int KIND> constexpr bool kKeys16 = KIND == kScoreF16 || KIND == kScore
 // the lowest key an outcome can have; masked ones have lower ones
 template <int KIND> constexpr u32 kLowest = KIND == kScoreF32 ? 0x00800000u : KIND == kScoreBF16 ? 0x0080u : KIND == kScoreF16 ? 0x0400u : 1u;
 
-// Masked values (NaN, -inf; of probabilities all that are not positive) as one value, -0 as 0.
-template <int KIND> __device__ __forceinline__ float clean(float v) {
-    if (kLogs<KIND>) return v > -kInf ? v + 0.f : -kInf;
-    return v > 0.f ? v : 0.f;
-}
+template <int KIND> constexpr float kMasked = kLogs<KIND> ? -kInf : 0.f;
 
+// Values are compared as they are: a masked one (NaN, -inf; of probabilities all that are not positive) is never as high as a
+// value that a row's filters name, and -0 equals 0.  Their keys: of masked values below the lowest, of -0 that of 0.
 template <int KIND> __device__ __forceinline__ u32 key_of(float v) {
+    v = kLogs<KIND> ? (v > -kInf ? v + 0.f : -kInf) : (v > 0.f ? v : 0.f);
     if (!kLogs<KIND>) return __float_as_uint(v);
     if (KIND == kScoreF16) {
         const u32 b = __half_as_ushort(__float2half_rn(v));
@@ -108,19 +107,17 @@ template <int KIND> __device__ __forceinline__ void load4(const Row& w, u32 j, f
             const float4 x = *(const float4*)(w.p + first * 4);
             v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = clean<KIND>(v[i]);
         return;
     }
     if (j >= w.vecs) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = kLogs<KIND> ? -kInf : 0.f;
+        for (int i = 0; i < 4; ++i) v[i] = kMasked<KIND>;
         return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const long long k = first + i;
-        v[i] = k >= 0 && k < (long long)w.cols ? clean<KIND>(one_value<KIND>(w, (u32)k)) : (kLogs<KIND> ? -kInf : 0.f);
+        v[i] = k >= 0 && k < (long long)w.cols ? one_value<KIND>(w, (u32)k) : kMasked<KIND>;
     }
 }
 
@@ -182,22 +179,51 @@ template <int KIND> __device__ __forceinline__ double weight64(const Scale& s, f
     return s.t_one ? q : exp2_neg(log2(q) * s.c);
 }
 
-// 2^(i / 256): a kernel's copy in LDS, filled by its threads before their next barrier.
 constexpr int kPowers = 256;
-template <int NT> __device__ __forceinline__ void fill_powers(double* powers) {
-    for (int i = threadIdx.x; i < kPowers; i += NT) powers[i] = 2.0 * exp2_neg((double)i / kPowers - 1.0);
+
+// log2 of a positive float in 64 bits, for probabilities at another temperature than 1: v = 2^k f, f in 1..2, its upper 8 bits
+// name a factor c near 1 / f; log2 v = k - log2 c + log2(1 + r), r = f c - 1, |r| < 2^-8: the series to r^7.  16 instructions;
+// the library's log2 takes some sixty.
+struct Logs { double c[256], log2_c[256]; };
+template <int NT> __device__ __forceinline__ void fill_logs(Logs* l) {
+    for (int i = threadIdx.x; i < 256; i += NT) {
+        const double c = (double)(float)(512.0 / (513.0 + 2 * i));     // (24 bits: f c - 1 is exact)
+        l->c[i] = c;
+        l->log2_c[i] = log2(c);
+    }
 }
+__device__ __forceinline__ double log2_of(const Logs* l, float v) {
+    const u64 b = (u64)__double_as_longlong((double)v);
+    const int k = (int)(b >> 52) - 1023, i = (int)(b >> 44) & 255;
+    const double f = __longlong_as_double((long long)((b & 0xfffffffffffffull) | 0x3ff0000000000000ull));
+    const double r = fma(f, l->c[i], -1.0);
+    double s = 1.0 / 7.0;
+    s = fma(s, -r, 1.0 / 6.0);
+    s = fma(s, -r, 1.0 / 5.0);
+    s = fma(s, -r, 1.0 / 4.0);
+    s = fma(s, -r, 1.0 / 3.0);
+    s = fma(s, -r, 1.0 / 2.0);
+    s = fma(s, -r, 1.0);
+    return ((double)k - l->log2_c[i]) + s * r * 1.4426950408889634074;
+}
+
+// What weights are looked up in: a kernel's tables in LDS.
+template <int KIND> struct Tables { double powers[256]; };
+template <> struct Tables<kScoreProbs> { double powers[256]; Logs logs; };
+template <> struct Tables<kScoreState> { double powers[256]; Logs logs; };
 
 // rint(e 2^S), the whole number that adding 2^52 leaves in the low bits.  2^x as a power of 2^(1/256) from the table times
 // a series of four terms (|r| <= 2^-9: the next term is below 2^-54): half the arithmetic of exp2_neg.
 __device__ __forceinline__ u64 whole(double x) { return (u64)__double_as_longlong(x) & 0xfffffffffffffull; }
-template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, const double* powers, float v) {
+template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, const Tables<KIND>* tables, float v) {
     if (!kLogs<KIND> && s.t_one) {
         const double q = (double)v * s.rm;
         const double e = fma(fma(-q, s.mq, (double)v), s.rm, q);      // v / m
         return whole(fma(v == s.m ? 1.0 : e, s.one, 4503599627370496.0));
     }
-    double x = kLogs<KIND> ? ((double)v - s.md) * (s.c * kPowers) : log2((double)v / s.md) * (s.c * kPowers);
+    double x;
+    if constexpr (kLogs<KIND>) x = ((double)v - s.md) * (s.c * kPowers);
+    else x = s.m < kInf ? (log2_of(&tables->logs, v) - log2_of(&tables->logs, s.m)) * (s.c * kPowers) : -1e300;
     x = fmax(x, -200.0 * kPowers);
     if (v == s.m) x = 0.0;                                            // (also where both are infinite)
     const double y = x + 6755399441055744.0;                          // 1.5 2^52: the nearest whole number in the low bits
@@ -208,15 +234,22 @@ template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, const 
     p = fma(p, r, l * l / 2.0);
     p = fma(p, r, l);
     p = fma(p, r, 1.0);
-    return whole(fma(__builtin_ldexp(powers[n & (kPowers - 1)], (n >> 8) + s.bits), p, 4503599627370496.0));
+    return whole(fma(__builtin_ldexp(tables->powers[n & (kPowers - 1)], (n >> 8) + s.bits), p, 4503599627370496.0));
+}
+
+// Filled by a kernel's threads before their next barrier: 2^(i / 256), and logarithms where a row will ask for them.
+template <int KIND, int NT> __device__ __forceinline__ void fill_tables(Tables<KIND>* tables, bool t_one) {
+    if (!kLogs<KIND> && t_one) return;
+    for (int i = threadIdx.x; i < kPowers; i += NT) tables->powers[i] = 2.0 * exp2_neg((double)i / kPowers - 1.0);
+    if constexpr (!kLogs<KIND>) fill_logs<NT>(&tables->logs);
 }
 
 // Bin of the first histogram: not decreasing in the distance from the highest value.  Scores: linear in it over the S + 2
 // factors of two in which weights are not 0; probabilities: 32 bins a factor of two.
-template <int KIND, int NB> __device__ __forceinline__ u32 bin_of(const Scale& s, float v, u32 key) {
+template <int KIND, int NB> __device__ __forceinline__ u32 bin_of(const Scale& s, float v) {
     if (kLogs<KIND>) return v == s.m ? 0u : (u32)fminf((s.m - v) * s.per_bin, (float)(NB - 1));
     constexpr int shift = NB >= 2048 ? 18 : NB >= 1024 ? 19 : 21;
-    return min((s.kmax - key) >> shift, (u32)(NB - 1));
+    return min((s.kmax - __float_as_uint(v)) >> shift, (u32)(NB - 1));
 }
 
 // ---- wavefronts and workgroups ---------------------------------------------------------------------------------------
@@ -269,7 +302,7 @@ template <class F> __device__ __forceinline__ u32 first_key(u32 lo, u32 hi, F is
 }
 
 // ---- the search for a cut --------------------------------------------------------------------------------------------
-struct Cut { u32 key, idx; };     // kept: keys above, and of what equals the key the indices up to idx
+struct Cut { float v; u32 idx; };     // kept: values above, and of what equals v the indices up to idx
 
 struct Find {
     u32 klo, khi;        // the keys the cut is among
@@ -326,7 +359,7 @@ template <int NT, int NB, bool BYW> __device__ __forceinline__ bool select_bin(c
 
 // The keys of bin b of the first histogram, from `lowest` on.
 template <int KIND, int NB> __device__ __forceinline__ void keys_of_bin(const Scale& s, u32 b, u32 lowest, u32* klo, u32* khi) {
-    auto bin = [&](u32 k) { return bin_of<KIND, NB>(s, value_of<KIND>(k), k); };
+    auto bin = [&](u32 k) { return bin_of<KIND, NB>(s, value_of<KIND>(k)); };
     *klo = first_key(lowest, s.kmax, [&](u32 k) { return bin(k) <= b; });
     // the first key of a lower bin, if there is one, ends the bin
     *khi = b == 0 ? s.kmax : first_key(*klo, s.kmax, [&](u32 k) { return bin(k) < b; }) - 1u;
@@ -339,11 +372,11 @@ template <int NB> __device__ __forceinline__ int key_shift(u32 range) {
 }
 
 // What is known of the cut once its bin is: the next keys to look at, or the cut itself.
-template <int KIND, bool BYW> __device__ __forceinline__ void settle(const Scale& s, const double* powers, Find& f) {
+template <int KIND, bool BYW> __device__ __forceinline__ void settle(const Scale& s, const Tables<KIND>* tables, Find& f) {
     if (f.klo < f.khi) return;
     f.done = 1;
     if (BYW) {
-        const u64 w = weight<KIND>(s, powers, value_of<KIND>(f.klo));
+        const u64 w = weight<KIND>(s, tables, value_of<KIND>(f.klo));
         f.ne = (u32)((f.target - f.weight + w - 1) / (w ? w : 1));
     } else {
         f.ne = (u32)(f.target - f.count);
@@ -382,12 +415,10 @@ template <int NT> __device__ __forceinline__ void write_none(const SampleArgs& a
 }
 
 // ---- a row's chunks --------------------------------------------------------------------------------------------------
-template <int KIND> __device__ __forceinline__ bool keeps(const Cut& cut, u32 key, u32 idx) {
-    return key > cut.key || (key == cut.key && idx <= cut.idx);
-}
+__device__ __forceinline__ bool keeps(const Cut& cut, float v, u32 idx) { return v > cut.v || (v == cut.v && idx <= cut.idx); }
 
 // One chunk's numbers and (WEIGHTS) weights of what is kept.
-template <int KIND, int STEPS, bool WEIGHTS> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const double* powers, const Cut& cut, u32 j0, u32 lane, u64* w, u32* n) {
+template <int KIND, int STEPS, bool WEIGHTS> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const Tables<KIND>* tables, const Cut& cut, u32 j0, u32 lane, u64* w, u32* n) {
     float v[STEPS][4];
 #pragma unroll
     for (int it = 0; it < STEPS; ++it) load4<KIND>(row, j0 + it * 64u + lane, v[it]);
@@ -397,16 +428,16 @@ template <int KIND, int STEPS, bool WEIGHTS> __device__ __forceinline__ void chu
     for (int it = 0; it < STEPS; ++it)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bool keep = keeps<KIND>(cut, key_of<KIND>(v[it][i]), 4 * (j0 + it * 64u + lane) - row.skew + i);
+            const bool keep = keeps(cut, v[it][i], 4 * (j0 + it * 64u + lane) - row.skew + i);
             num += keep;
-            if (WEIGHTS && keep) sum += weight<KIND>(s, powers, v[it][i]);
+            if (WEIGHTS && keep) sum += weight<KIND>(s, tables, v[it][i]);
         }
     *n = wave_sum(num);
     *w = WEIGHTS ? wave_sum(sum) : 0;
 }
 
-// The index of the ne-th value of a chunk, `before` of them in earlier ones, that equals key; the whole wavefront asks.
-template <int KIND, int STEPS> __device__ __forceinline__ u32 nth_equal(const Row& row, u32 key, u32 ne, u32 j0, u32 lane) {
+// The index of a chunk's ne-th value that equals `value`; the whole wavefront asks.
+template <int KIND, int STEPS> __device__ __forceinline__ u32 nth_equal(const Row& row, float value, u32 ne, u32 j0, u32 lane) {
     u32 run = 0, found = kAll;
     for (int it = 0; it < STEPS; ++it) {
         float v[4];
@@ -414,12 +445,12 @@ template <int KIND, int STEPS> __device__ __forceinline__ u32 nth_equal(const Ro
         load4<KIND>(row, j, v);
         u32 n = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) n += key_of<KIND>(v[i]) == key;
+        for (int i = 0; i < 4; ++i) n += v[i] == value;
         const u32 incl = wave_scan(n);
         u32 rank = run + incl - n, mine = kAll;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (key_of<KIND>(v[i]) == key && ++rank == ne) mine = 4 * j - row.skew + i;
+            if (v[i] == value && ++rank == ne) mine = 4 * j - row.skew + i;
         const u64 who = __ballot(mine != kAll);
         if (who) { found = lane_of(mine, (u32)__ffsll((long long)who) - 1u); break; }
         run += last_lane(incl);
@@ -428,7 +459,7 @@ template <int KIND, int STEPS> __device__ __forceinline__ u32 nth_equal(const Ro
 }
 
 // The outcome of a chunk at which the running sum of kept weights, `base` before the chunk, exceeds t.  Whole wavefront.
-template <int KIND, int STEPS> __device__ __forceinline__ long long find_in_chunk(const Row& row, const Scale& s, const double* powers, const Cut& cut, u32 j0, u64 base, u64 t, u32 lane, u64* w_at) {
+template <int KIND, int STEPS> __device__ __forceinline__ long long find_in_chunk(const Row& row, const Scale& s, const Tables<KIND>* tables, const Cut& cut, u32 j0, u64 base, u64 t, u32 lane, u64* w_at) {
     for (int it = 0; it < STEPS; ++it) {
         const u32 j = j0 + it * 64u + lane;
         float v[4];
@@ -437,7 +468,7 @@ template <int KIND, int STEPS> __device__ __forceinline__ long long find_in_chun
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             w[i] = 0;
-            if (keeps<KIND>(cut, key_of<KIND>(v[i]), 4 * j - row.skew + i)) w[i] = weight<KIND>(s, powers, v[i]);
+            if (keeps(cut, v[i], 4 * j - row.skew + i)) w[i] = weight<KIND>(s, tables, v[i]);
             four += w[i];
         }
         const u64 incl = wave_scan(four);
@@ -458,26 +489,47 @@ template <int KIND, int STEPS> __device__ __forceinline__ long long find_in_chun
 }
 
 // ---- sorting in LDS --------------------------------------------------------------------------------------------------
-// Ascending, n <= 2^k entries; those behind the n-th up to the next power of two are set to the highest number.
+// Ascending, n <= 2 NT distinct entries.  Up to 256: each one's rank is the number of entries below it (64 entries, one
+// wavefront: 0.6 us; by exchanges 4).  Else by exchanges, entries behind the n-th up to a power of two at the highest number.
 template <int NT> __device__ __forceinline__ void sort_lds(u64* a, u32 n) {
-    u32 size = 2;
+    if (n <= 256) {
+        constexpr int per = NT < 256 ? 256 / NT : 1;
+        u64 mine[per];
+        u32 rank[per];
+        const u32 pad = (n + 3) & ~3u;
+        if (threadIdx.x < pad - n) a[n + threadIdx.x] = ~0ull;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < per; ++k) {
+            rank[k] = 0;
+            mine[k] = threadIdx.x + k * NT < n ? a[threadIdx.x + k * NT] : 0;
+        }
+        if (threadIdx.x < n)
+            for (u32 i = 0; i < pad; i += 4) {
+                const u64 x = a[i], y = a[i + 1], z = a[i + 2], w = a[i + 3];
+#pragma unroll
+                for (int k = 0; k < per; ++k) rank[k] += (x < mine[k]) + (y < mine[k]) + (z < mine[k]) + (w < mine[k]);
+            }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < per; ++k)
+            if (threadIdx.x + k * NT < n) a[rank[k]] = mine[k];
+        __syncthreads();
+        return;
+    }
+    u32 size = 512;
     while (size < n) size <<= 1;
     for (u32 i = n + threadIdx.x; i < size; i += NT) a[i] = ~0ull;
     __syncthreads();
-    const bool one = size <= 128;                 // a wavefront's work: no barriers
-    if (!one || threadIdx.x < 64) {
-        for (u32 k = 2; k <= size; k <<= 1)
-            for (u32 j = k >> 1; j > 0; j >>= 1) {
-                for (u32 i = threadIdx.x; i < size / 2; i += NT) {
-                    const u32 lo = 2 * i - (i & (j - 1)), hi = lo + j;
-                    const u64 x = a[lo], y = a[hi];
-                    if ((x > y) == ((lo & k) == 0)) { a[lo] = y; a[hi] = x; }
-                }
-                if (one) __threadfence_block();
-                else __syncthreads();
+    for (u32 k = 2; k <= size; k <<= 1)
+        for (u32 j = k >> 1; j > 0; j >>= 1) {
+            for (u32 i = threadIdx.x; i < size / 2; i += NT) {
+                const u32 lo = 2 * i - (i & (j - 1)), hi = lo + j;
+                const u64 x = a[lo], y = a[hi];
+                if ((x > y) == ((lo & k) == 0)) { a[lo] = y; a[hi] = x; }
             }
-    }
-    __syncthreads();
+            __syncthreads();
+        }
 }
 
 // ---- one workgroup a row ---------------------------------------------------------------------------------------------
@@ -493,7 +545,8 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     constexpr int UN = NT == 1024 ? 4 : 2;  // vectors of a thread on their way at once
     __shared__ u64 wt[2 * NB];              // two histograms' weights, or: weights and entries of a list to be sorted, or: a list
     __shared__ u32 cnt[2 * NB];
-    __shared__ double powers[kPowers];
+    __shared__ Tables<KIND> lds_tables;
+    const Tables<KIND>* const tables = &lds_tables;
     __shared__ u64 sm[16];
     __shared__ Hit hit;
     __shared__ u32 list_n, found;
@@ -507,7 +560,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     const Params p = params_of(a, r);
     const u32 nchunks = (row.vecs + 64 * STEPS - 1) / (64 * STEPS);
 
-    auto each = [&](auto f) {               // f(key, value, index) for every value of the row, masked ones too
+    auto each = [&](auto f) {               // f(value, index) for every value of the row, masked ones too
         for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
             float v[UN][4];
 #pragma unroll
@@ -515,14 +568,14 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
 #pragma unroll
             for (int u = 0; u < UN; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f(key_of<KIND>(v[u][i]), v[u][i], 4 * (j + u * NT) - row.skew + i);
+                for (int i = 0; i < 4; ++i) f(v[u][i], 4 * (j + u * NT) - row.skew + i);
         }
     };
-    u32 kmax = 0;
-    each([&](u32 k, float, u32) { kmax = max(kmax, k); });
-    fill_powers<NT>(powers);
+    float high = kMasked<KIND>;             // of the thread's values
+    each([&](float v, u32) { high = fmaxf(high, v); });
+    fill_tables<KIND, NT>(&lds_tables, p.t == 1.f);
     if (threadIdx.x == 0) list_n = 0;
-    kmax = block_max<NT>(kmax, sm);
+    const u32 kmax = block_max<NT>(key_of<KIND>(high), sm);
     __syncthreads();
     if (!p.ok || kmax < kLowest<KIND>) {
         write_none<NT>(a, r, 0, a.shots);
@@ -531,7 +584,8 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     }
     if (p.t == 0.f) {
         u32 first = 0;                      // the complement of the lowest index
-        each([&](u32 k, float, u32 idx) { if (k == kmax) first = max(first, ~idx); });
+        const float top = value_of<KIND>(kmax);
+        each([&](float v, u32 idx) { if (v == top) first = max(first, ~idx); });
         first = ~block_max<NT>(first, sm);
         for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
             const double u = a.uniforms[r * a.shots + i];
@@ -552,11 +606,12 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         for (int i = threadIdx.x; i < NB; i += NT) { cnt[h * NB + i] = 0; wt[h * NB + i] = 0; }
         __syncthreads();
         const int shift = key_shift<NB>(khi - klo);
-        each([&](u32 k, float v, u32) {
-            if (k < klo || k > khi) return;
-            const u32 b = h * NB + (first ? bin_of<KIND, NB>(s, v, k) : (khi - k) >> shift);
+        const float from = value_of<KIND>(klo), to = value_of<KIND>(khi);
+        each([&](float v, u32) {
+            if (!(v >= from && v <= to)) return;
+            const u32 b = h * NB + (first ? bin_of<KIND, NB>(s, v) : (khi - key_of<KIND>(v)) >> shift);
             if (counts) atomicAdd(&cnt[b], 1u);
-            if (weights) atomicAdd(&wt[b], weight<KIND>(s, powers, v));
+            if (weights) atomicAdd(&wt[b], weight<KIND>(s, tables, v));
         });
         __syncthreads();
     };
@@ -568,7 +623,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
 #pragma unroll
         for (int i = 0; i < per; ++i) {
             const u32 at = threadIdx.x * per + i;
-            w[i] = at < n ? weight<KIND>(s, powers, value_of<KIND>(~(u32)(le[at] >> 32))) : 0;
+            w[i] = at < n ? weight<KIND>(s, tables, value_of<KIND>(~(u32)(le[at] >> 32))) : 0;
             sum += w[i];
         }
         u64 all;
@@ -588,23 +643,56 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         return uniform(found);
     };
 
-    bool by_k = p.top_k > 0 && (u32)p.top_k < row.cols, by_p = p.top_p < 1.f, summed = false, slow = false;
-    Cut cut{lowest, kAll};
+    const float low = value_of<KIND>(lowest);
+    bool by_k = p.top_k > 0 && (u32)p.top_k < row.cols, by_p = p.top_p < 1.f, summed = false, slow = false, listed = false;
+    Cut cut{low, kAll};
     Hit at;
-    if (by_k) {
-        histogram(0, true, true, false, lowest, kmax);
-        by_k = select_bin<NT, NB, false>(cnt, nullptr, (u64)p.top_k, sm, &hit, &at);
-        slow = by_k && (by_p || at.own > NB);
-    }
-    if (by_k && at.count + at.own <= NB) {
-        // few outcomes down to the bin: in order they give the cut, and by index the draw
-        each([&](u32 k, float v, u32 idx) {
-            if (k >= lowest && bin_of<KIND, NB>(s, v, k) <= at.bin) {
-                const u32 slot = atomicAdd(&list_n, 1u);
-                if (slot < NB) le[slot] = (u64)~k << 32 | idx;
+    // the outcomes from the distance's bin b up as a list; false: they are more than it holds
+    auto collect = [&](u32 b) -> bool {
+        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
+            float v[UN][4];
+#pragma unroll
+            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+                const float top = fmaxf(fmaxf(v[u][0], v[u][1]), fmaxf(v[u][2], v[u][3]));
+                if (!(top >= low) || bin_of<KIND, NB>(s, top) > b) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!(v[u][i] >= low) || bin_of<KIND, NB>(s, v[u][i]) > b) continue;
+                    const u32 slot = atomicAdd(&list_n, 1u);
+                    if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[u][i]) << 32 | (4 * (j + u * NT) - row.skew + i);
+                }
             }
-        });
+        }
         __syncthreads();
+        const bool fits = list_n <= NB;
+        if (!fits) {
+            __syncthreads();
+            if (threadIdx.x == 0) list_n = 0;
+            __syncthreads();
+        }
+        return fits;
+    };
+    if (by_k) {
+        // The k-th highest of the threads' own highest values has k values at or above it, and not many more: of 1024
+        // threads' values the 50 highest come from about 49 threads.
+        if (p.top_k <= NT * 5 / 8) {
+            for (int i = threadIdx.x; i < NB; i += NT) cnt[i] = 0;
+            __syncthreads();
+            if (high >= low) atomicAdd(&cnt[bin_of<KIND, NB>(s, high)], 1u);
+            __syncthreads();
+            listed = select_bin<NT, NB, false>(cnt, nullptr, (u64)p.top_k, sm, &hit, &at) && collect(at.bin);
+        }
+        if (!listed) {
+            histogram(0, true, true, false, lowest, kmax);
+            by_k = select_bin<NT, NB, false>(cnt, nullptr, (u64)p.top_k, sm, &hit, &at);
+            listed = by_k && at.count + at.own <= NB && collect(at.bin);
+            slow = by_k && (by_p || at.own > NB);
+        }
+    }
+    if (listed) {
+        // few outcomes down to the bin: in order they give the cut, and by index the draw
         u64 w[per];
         u32 n = min(list_n, (u32)NB);      // (more only if the row was written to meanwhile)
         const u64 before = ordered(n, w);
@@ -673,12 +761,11 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             for (int it = 0; it < STEPS; ++it)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const u32 k = key_of<KIND>(v[it][i]);
-                    const u32 b = k >= lowest ? bin_of<KIND, NB>(s, v[it][i], k) : kAll;
-                    if (b < at.bin) { ++num; sum += weight<KIND>(s, powers, v[it][i]); }
+                    const u32 b = v[it][i] >= low ? bin_of<KIND, NB>(s, v[it][i]) : kAll;
+                    if (b < at.bin) { ++num; sum += weight<KIND>(s, tables, v[it][i]); }
                     if (b == at.bin) {
                         const u32 slot = atomicAdd(&list_n, 1u);
-                        if (slot < NB) le[slot] = (u64)~k << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
+                        if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[it][i]) << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
                     }
                 }
             num = wave_sum(num);
@@ -692,7 +779,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             const u64 before = ordered(n, w);
             n = by_k ? min(n, (u32)((u64)p.top_k - at.count)) : reach(w, before, n, at.weight, mass_of(p.top_p, mass));
             const u64 last = le[n > 0 ? n - 1 : 0];
-            cut = Cut{~(u32)(last >> 32), (u32)last};
+            cut = Cut{value_of<KIND>(~(u32)(last >> 32)), (u32)last};
 #pragma unroll
             for (int i = 0; i < per; ++i) {
                 const u32 k = threadIdx.x * per + i;
@@ -721,7 +808,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             f->target = target;
             f->count = in.count;
             f->weight = in.weight;
-            settle<KIND, BYW>(s, powers, *f);
+            settle<KIND, BYW>(s, tables, *f);
             while (!f->done) {
                 histogram(1, false, true, by_p, f->klo, f->khi);
                 if (!select_bin<NT, NB, BYW>(cnt + NB, by_p ? wt + NB : nullptr, f->target - (BYW ? f->weight : f->count), sm, &hit, &in))
@@ -732,16 +819,16 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
                 f->khi = top;
                 f->count += in.count;
                 f->weight += in.weight;
-                settle<KIND, BYW>(s, powers, *f);
+                settle<KIND, BYW>(s, tables, *f);
             }
             return true;
         };
         Find f;
         u32 ne = kAll;
         if (by_k && narrow(ByCount{}, (u64)p.top_k, &f)) {
-            cut.key = f.klo;
+            cut.v = value_of<KIND>(f.klo);
             ne = f.ne;
-            if (by_p) mass = f.weight + (u64)f.ne * weight<KIND>(s, powers, value_of<KIND>(f.klo));
+            if (by_p) mass = f.weight + (u64)f.ne * weight<KIND>(s, tables, value_of<KIND>(f.klo));
             have_mass = true;
         }
         if (by_p) {
@@ -751,7 +838,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
                 (void)block_scan<NT>(sum, sm, &mass);
             }
             if (narrow(ByWeight{}, mass_of(p.top_p, mass), &f)) {
-                cut.key = f.klo;
+                cut.v = value_of<KIND>(f.klo);
                 ne = f.ne;
             }
         }
@@ -762,7 +849,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
                 float v[4];
                 load4<KIND>(row, c * 64 * STEPS + it * 64u + lane, v);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) n += key_of<KIND>(v[i]) == cut.key;
+                for (int i = 0; i < 4; ++i) n += v[i] == cut.v;
             }
             n = wave_sum(n);
             if (lane == 0) chunk_n[c] = n;
@@ -775,14 +862,18 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         const u64 before = block_scan<NT>((u64)mine, sm, &all);
         if (before < ne && before + mine >= ne) { found = threadIdx.x; list_n = (u32)(ne - before); }
         __syncthreads();
-        if (found != kAll) cut.idx = nth_equal<KIND, STEPS>(row, cut.key, list_n, found * 64 * STEPS, lane);
+        if (found != kAll) cut.idx = nth_equal<KIND, STEPS>(row, cut.v, list_n, found * 64 * STEPS, lane);
         __syncthreads();
     }
+    // several shots a wavefront: what is left goes into a list, if there is room
+    const bool many = a.shots > NT / 64;
     if (!summed) {
+        const bool count = many && row.cols <= (u32)LIST;
         for (u32 c = wave; c < nchunks; c += NT / 64) {
             u64 w;
             u32 n;
-            chunk_sums<KIND, STEPS, true>(row, s, powers, cut, c * 64 * STEPS, lane, &w, &n);
+            if (count) chunk_sums<KIND, STEPS, false>(row, s, tables, cut, c * 64 * STEPS, lane, &w, &n);
+            else chunk_sums<KIND, STEPS, true>(row, s, tables, cut, c * 64 * STEPS, lane, &w, &n);
             if (lane == 0) { chunk_w[c] = w; chunk_n[c] = n; }
         }
         __syncthreads();
@@ -801,8 +892,8 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     }
     __syncthreads();
     if (threadIdx.x == 0 && a.kept) a.kept[r] = (int)n_kept;
-    if (n_kept <= LIST && a.shots > NT / 64) {
-        // several shots a wavefront: what is left as a list by index, a thread for every shot
+    if (n_kept <= LIST && many) {
+        // by index, a thread for every shot
         u64* lw = wt;
         u32* lk = cnt;
         for (u32 c = wave; c < nchunks; c += NT / 64) {
@@ -815,7 +906,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
                 load4<KIND>(row, j, v);
                 u32 keep = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) keep |= (u32)keeps<KIND>(cut, key_of<KIND>(v[i]), 4 * j - row.skew + i) << i;
+                for (int i = 0; i < 4; ++i) keep |= (u32)keeps(cut, v[i], 4 * j - row.skew + i) << i;
                 const u32 n = __popc(keep), incl = wave_scan(n);
                 u32 to = pos + incl - n;
 #pragma unroll
@@ -830,7 +921,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         const u32 first = threadIdx.x * own;
 #pragma unroll
         for (int i = 0; i < own; ++i) {
-            w[i] = first + i < n_kept ? weight<KIND>(s, powers, value_of<KIND>((u32)lw[first + i])) : 0;
+            w[i] = first + i < n_kept ? weight<KIND>(s, tables, value_of<KIND>((u32)lw[first + i])) : 0;
             sum += w[i];
         }
         u64 run = block_scan<NT>(sum, sm, &total);
@@ -865,7 +956,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
                 const u64 above = __ballot(c0 + lane < nchunks && chunk_w[min(c0 + lane, nchunks - 1)] > t);
                 if (above) { c = c0 + (u32)__ffsll((long long)above) - 1u; break; }
             }
-            k = find_in_chunk<KIND, STEPS>(row, s, powers, cut, c * 64 * STEPS, c ? chunk_w[c - 1] : 0, t, lane, &w);
+            k = find_in_chunk<KIND, STEPS>(row, s, tables, cut, c * 64 * STEPS, c ? chunk_w[c - 1] : 0, t, lane, &w);
         }
         if (lane == 0) write_shot(a, r * a.shots + i, k, w, total);
     }
@@ -934,7 +1025,8 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_max(c
     const u32 part = (u32)(grid_block() % g.parts);
     if (r >= (u64)a.rows) return;
     const Row row = row_of<KIND>(a, r);
-    u32 j0, j1, kmax = 0;
+    u32 j0, j1;
+    float high = kMasked<KIND>;
     part_of<KIND>(row, g, part, &j0, &j1);
     for (u32 j = j0 + threadIdx.x; j < j1; j += 4 * kLongThreads) {
         float v[4][4];
@@ -943,9 +1035,9 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_max(c
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) kmax = max(kmax, key_of<KIND>(v[u][i]));
+            for (int i = 0; i < 4; ++i) high = fmaxf(high, v[u][i]);
     }
-    kmax = block_max<kLongThreads>(kmax, sm);
+    const u32 kmax = block_max<kLongThreads>(key_of<KIND>(high), sm);
     if (threadIdx.x == 0) g.pmax[r * g.parts + part] = kmax;
     // the row's histograms start at zero
     const u32 bins = g.levels ? kLevels * kLongBins : 0;
@@ -959,26 +1051,26 @@ __device__ __forceinline__ bool by_top_k(const SampleArgs& a, const Params& p) {
 __device__ __forceinline__ bool by_top_p(const Params& p) { return p.t > 0.f && p.top_p < 1.f; }
 
 // The histogram of the values of vectors j0 .. j1 with keys in klo .. khi, added to the row's.
-template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, const double* powers, u64* wt, u32* cnt, u64* gw, u32* gc) {
+template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, const Tables<KIND>* tables, u64* wt, u32* cnt, u64* gw, u32* gc) {
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) { cnt[i] = 0; wt[i] = 0; }
     __syncthreads();
     const int shift = key_shift<kLongBins>(khi - klo);
+    const float low = value_of<KIND>(klo), high = value_of<KIND>(khi);
     for (u32 j = j0 + threadIdx.x; j < j1; j += 4 * kLongThreads) {
         float v[4][4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             if (j + u * kLongThreads < j1) load4<KIND>(row, j + u * kLongThreads, v[u]);
-            else for (int i = 0; i < 4; ++i) v[u][i] = kLogs<KIND> ? -kInf : 0.f;
+            else for (int i = 0; i < 4; ++i) v[u][i] = kMasked<KIND>;
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const u32 k = key_of<KIND>(v[u][i]);
-                if (k < klo || k > khi) continue;
-                const u32 b = first ? bin_of<KIND, kLongBins>(s, v[u][i], k) : (khi - k) >> shift;
+                if (!(v[u][i] >= low && v[u][i] <= high)) continue;
+                const u32 b = first ? bin_of<KIND, kLongBins>(s, v[u][i]) : (khi - key_of<KIND>(v[u][i])) >> shift;
                 atomicAdd(&cnt[b], 1u);
-                if (weights) atomicAdd(&wt[b], weight<KIND>(s, powers, v[u][i]));
+                if (weights) atomicAdd(&wt[b], weight<KIND>(s, tables, v[u][i]));
             }
     }
     __syncthreads();
@@ -993,8 +1085,9 @@ template <int KIND> __device__ __forceinline__ void long_histogram(const Row& ro
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first(const SampleArgs a, const Long g) {
     __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
     __shared__ u32 cnt[kLongBins];
-    __shared__ double powers[kPowers];
-    fill_powers<kLongThreads>(powers);
+    __shared__ Tables<KIND> lds_tables;
+    const Tables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, kLongThreads>(&lds_tables, false);
     __syncthreads();
     const u64 r = grid_block() / g.parts;
     const u32 part = (u32)(grid_block() % g.parts);
@@ -1012,19 +1105,19 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first
         const Scale s = scale_of<KIND, kLongBins>(kmax, p.t > 0.f ? p.t : 1.f, a.bits);
         if (p.min_p > 0.f && p.t > 0.f)
             st.lowest = first_key(st.lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
-        st.cut = Cut{p.t > 0.f ? st.lowest : kmax, kAll};
+        st.cut = Cut{value_of<KIND>(p.t > 0.f ? st.lowest : kmax), kAll};
         st.ne = p.t > 0.f ? kAll : 1;
         if (by_top_k(a, p) || by_top_p(p)) {
             u32 j0, j1;
             part_of<KIND>(row, g, part, &j0, &j1);
-            long_histogram<KIND>(row, s, j0, j1, true, by_top_p(p), st.lowest, kmax, powers, wt, cnt, g.wt + r * (kLevels * kLongBins), g.cnt + r * (kLevels * kLongBins));
+            long_histogram<KIND>(row, s, j0, j1, true, by_top_p(p), st.lowest, kmax, tables, wt, cnt, g.wt + r * (kLevels * kLongBins), g.cnt + r * (kLevels * kLongBins));
         }
     }
     if (part == 0 && threadIdx.x == 0) g.state[r * kLevels] = st;
 }
 
 // The search after the histogram of level `prev`.
-template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_advance(const SampleArgs& a, const Params& p, const Scale& s, const double* powers, const Long& g, u64 r, int prev, u64* sm, Hit* hit, LongState* st) {
+template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_advance(const SampleArgs& a, const Params& p, const Scale& s, const Tables<KIND>* tables, const Long& g, u64 r, int prev, u64* sm, Hit* hit, LongState* st) {
     if (!st->stage) return;
     Find& f = st->f;
     const u64* wt = g.wt + (r * kLevels + prev) * kLongBins;
@@ -1040,20 +1133,20 @@ template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_
         f.khi = top;
         f.count += at.count;
         f.weight += at.weight;
-        if (st->stage == 1) settle<KIND, false>(s, powers, f);
-        else settle<KIND, true>(s, powers, f);
+        if (st->stage == 1) settle<KIND, false>(s, tables, f);
+        else settle<KIND, true>(s, tables, f);
     }
     if (!f.done) return;
-    st->cut = Cut{f.klo, kAll};
+    st->cut = Cut{value_of<KIND>(f.klo), kAll};
     st->ne = f.ne;
     if (st->stage == 1 && by_top_p(p)) {
-        st->mass = f.weight + (u64)f.ne * weight<KIND>(s, powers, value_of<KIND>(f.klo));
+        st->mass = f.weight + (u64)f.ne * weight<KIND>(s, tables, value_of<KIND>(f.klo));
         st->have_mass = 1;
     }
     st->stage = 0;
 }
 
-template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs& a, const Params& p, const Scale& s, const double* powers, const Long& g, u64 r, u32 stage, u64* sm, Hit* hit, LongState* st) {
+template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs& a, const Params& p, const Scale& s, const Tables<KIND>* tables, const Long& g, u64 r, u32 stage, u64* sm, Hit* hit, LongState* st) {
     const u64* wt = g.wt + r * kLevels * kLongBins;
     const u32* cnt = g.cnt + r * kLevels * kLongBins;
     Hit at;
@@ -1078,19 +1171,20 @@ template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs&
     f.target = target;
     f.count = at.count;
     f.weight = at.weight;
-    if (stage == 1) settle<KIND, false>(s, powers, f);
-    else settle<KIND, true>(s, powers, f);
+    if (stage == 1) settle<KIND, false>(s, tables, f);
+    else settle<KIND, true>(s, tables, f);
     st->f = f;
     st->stage = stage;
-    if (f.done) long_advance<KIND>(a, p, s, powers, g, r, 0, sm, hit, st);
+    if (f.done) long_advance<KIND>(a, p, s, tables, g, r, 0, sm, hit, st);
 }
 
 // Level `level` after level `prev`: the first level of top-k is 1, that of top-p 1 + kKeySteps.
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(const SampleArgs a, const Long g, int level, int prev) {
     __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
     __shared__ u32 cnt[kLongBins];
-    __shared__ double powers[kPowers];
-    fill_powers<kLongThreads>(powers);
+    __shared__ Tables<KIND> lds_tables;
+    const Tables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, kLongThreads>(&lds_tables, false);
     __syncthreads();
     __shared__ Hit hit;
     const u64 r = grid_block() / g.parts;
@@ -1101,14 +1195,14 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(
     LongState st = g.state[r * kLevels + prev];
     if (st.ok) {
         const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-        long_advance<KIND>(a, p, s, powers, g, r, prev, sm, &hit, &st);
-        if (level == 1 && by_top_k(a, p)) long_begin<KIND>(a, p, s, powers, g, r, 1, sm, &hit, &st);
-        if (level == 1 + kKeySteps && by_top_p(p)) long_begin<KIND>(a, p, s, powers, g, r, 2, sm, &hit, &st);
+        long_advance<KIND>(a, p, s, tables, g, r, prev, sm, &hit, &st);
+        if (level == 1 && by_top_k(a, p)) long_begin<KIND>(a, p, s, tables, g, r, 1, sm, &hit, &st);
+        if (level == 1 + kKeySteps && by_top_p(p)) long_begin<KIND>(a, p, s, tables, g, r, 2, sm, &hit, &st);
         if (st.stage) {
             u32 j0, j1;
             part_of<KIND>(row, g, part, &j0, &j1);
             const size_t at = (r * kLevels + level) * kLongBins;
-            long_histogram<KIND>(row, s, j0, j1, false, by_top_p(p), st.f.klo, st.f.khi, powers, wt, cnt, g.wt + at, g.cnt + at);
+            long_histogram<KIND>(row, s, j0, j1, false, by_top_p(p), st.f.klo, st.f.khi, tables, wt, cnt, g.wt + at, g.cnt + at);
         }
     }
     if (part == 0 && threadIdx.x == 0) g.state[r * kLevels + level] = st;
@@ -1118,8 +1212,9 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(const SampleArgs a, const Long g, int prev) {
     __shared__ u64 sm[kLongThreads / 64];
     __shared__ Hit hit;
-    __shared__ double powers[kPowers];
-    fill_powers<kLongThreads>(powers);
+    __shared__ Tables<KIND> lds_tables;
+    const Tables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, kLongThreads>(&lds_tables, false);
     __syncthreads();
     const u64 r = grid_block() / g.parts;
     const u32 part = (u32)(grid_block() % g.parts);
@@ -1129,7 +1224,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     LongState st = g.state[r * kLevels + prev];
     if (!st.ok) return;
     const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-    long_advance<KIND>(a, p, s, powers, g, r, prev, sm, &hit, &st);
+    long_advance<KIND>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     const u32 lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const u32 c1 = min((part + 1) * g.chunks_per_part, g.chunks);
     for (u32 c = part * g.chunks_per_part + wave; c < c1; c += kLongThreads / 64) {
@@ -1142,9 +1237,8 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
         for (int it = 0; it < kLongSteps; ++it)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const u32 k = key_of<KIND>(v[it][i]);
-                n += (k > st.cut.key) + ((u32)(k == st.cut.key) << 16);
-                if (k > st.cut.key) w += weight<KIND>(s, powers, v[it][i]);
+                n += (v[it][i] > st.cut.v) + ((u32)(v[it][i] == st.cut.v) << 16);
+                if (v[it][i] > st.cut.v) w += weight<KIND>(s, tables, v[it][i]);
             }
         n = wave_sum(n);
         w = wave_sum(w);
@@ -1155,7 +1249,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     }
 }
 
-template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const double* powers, const Cut& cut, const u64* cw, u32 chunks, u64 at, u32 lane) {
+template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const Tables<KIND>* tables, const Cut& cut, const u64* cw, u32 chunks, u64 at, u32 lane) {
     const double u = a.uniforms[at];
     const u64 total = cw[chunks - 1];
     long long k = -1;
@@ -1172,7 +1266,7 @@ template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& 
             lo += off;
             len = min(stride, len - off);
         }
-        k = find_in_chunk<KIND, kLongSteps>(row, s, powers, cut, lo * 64 * kLongSteps, lo ? cw[lo - 1] : 0, t, lane, &w);
+        k = find_in_chunk<KIND, kLongSteps>(row, s, tables, cut, lo * 64 * kLongSteps, lo ? cw[lo - 1] : 0, t, lane, &w);
     }
     if (lane == 0) write_shot(a, at, k, w, total);
 }
@@ -1182,9 +1276,10 @@ template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& 
 template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const SampleArgs a, const Long g, int prev, int draw) {
     __shared__ u64 sm[16];
     __shared__ Hit hit;
-    __shared__ double powers[kPowers];
+    __shared__ Tables<KIND> lds_tables;
+    const Tables<KIND>* const tables = &lds_tables;
     __shared__ u32 found, rank;
-    fill_powers<1024>(powers);
+    fill_tables<KIND, 1024>(&lds_tables, false);
     if (threadIdx.x == 0) found = kAll;
     __syncthreads();
     const u64 r = grid_block();
@@ -1200,7 +1295,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
         return;
     }
     const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-    long_advance<KIND, 1024>(a, p, s, powers, g, r, prev, sm, &hit, &st);
+    long_advance<KIND, 1024>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     u64* cw = g.chunk_w + r * g.chunks;
     const u32* cn = g.chunk_n + r * g.chunks;
     const u32 per = (g.chunks + 1023) / 1024;
@@ -1208,7 +1303,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     u64 eq = 0, eq_all, n_kept, total;
     for (u32 c = c0; c < c1; ++c) eq += cn[c] >> 16;
     const u64 eq_before = block_scan<1024>(eq, sm, &eq_all);
-    const u64 w_cut = weight<KIND>(s, powers, value_of<KIND>(st.cut.key));
+    const u64 w_cut = weight<KIND>(s, tables, st.cut.v);
     u64 run = eq_before, num = 0, w = 0;
     for (u32 c = c0; c < c1; ++c) {
         const u32 n = cn[c];
@@ -1229,7 +1324,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
         run += n >> 16;
     }
     const u32 lane = threadIdx.x & 63;
-    if (found != kAll) st.cut.idx = nth_equal<KIND, kLongSteps>(row, st.cut.key, rank, found * 64 * kLongSteps, lane);
+    if (found != kAll) st.cut.idx = nth_equal<KIND, kLongSteps>(row, st.cut.v, rank, found * 64 * kLongSteps, lane);
     if (threadIdx.x == 0) {
         if (a.kept) a.kept[r] = (int)n_kept;
         g.state[r * kLevels + kLevels - 1] = st;
@@ -1238,12 +1333,13 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     __threadfence_block();
     __syncthreads();
     for (u64 i = threadIdx.x >> 6; i < (u64)a.shots; i += 16)
-        long_shot<KIND>(a, row, s, powers, st.cut, cw, g.chunks, r * a.shots + i, lane);
+        long_shot<KIND>(a, row, s, tables, st.cut, cw, g.chunks, r * a.shots + i, lane);
 }
 
 template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const SampleArgs a, const Long g) {
-    __shared__ double powers[kPowers];
-    fill_powers<256>(powers);
+    __shared__ Tables<KIND> lds_tables;
+    const Tables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, 256>(&lds_tables, false);
     __syncthreads();
     const u64 at = grid_block() * 4 + (threadIdx.x >> 6);
     if (at >= (u64)a.rows * a.shots) return;
@@ -1257,7 +1353,7 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
     const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-    long_shot<KIND>(a, row, s, powers, st.cut, g.chunk_w + r * g.chunks, g.chunks, at, lane);
+    long_shot<KIND>(a, row, s, tables, st.cut, g.chunk_w + r * g.chunks, g.chunks, at, lane);
 }
 
 }  // namespace
