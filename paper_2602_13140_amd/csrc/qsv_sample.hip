@@ -58,67 +58,69 @@ template <int KIND> __device__ __forceinline__ float value_of(u32 k) {
 // A row is read four values a lane in aligned vectors: vector j holds the values 4 j - skew .. 4 j - skew + 3, where skew
 // values lie between the last aligned address and the row's start.  Vectors that reach over an end are read value by value.
 struct Row {
-    const char* p;
+    in_global<char>* base;     // where vector 0 would start
     u32 cols, skew, vecs;
+    u32 first, whole;          // the first whole vector, and how many there are
 };
 
 template <int KIND> __device__ __forceinline__ Row row_of(const SampleArgs& a, u64 r) {
     constexpr int size = KIND == kScoreState ? 8 : kKeys16<KIND> ? 2 : 4;
     Row w;
-    w.p = (const char*)a.scores + r * (u64)a.stride * size;
+    const char* p = (const char*)a.scores + r * (u64)a.stride * size;
     w.cols = a.cols;
-    w.skew = KIND == kScoreState ? 0u : (u32)(((uintptr_t)w.p / size) & 3u);
+    w.skew = KIND == kScoreState ? 0u : (u32)(((uintptr_t)p / size) & 3u);
+    w.base = (in_global<char>*)(p - w.skew * size);
     w.vecs = (w.cols + w.skew + 3u) >> 2;
+    w.first = w.skew ? 1u : 0u;
+    w.whole = (w.cols + w.skew) / 4u > w.first ? (w.cols + w.skew) / 4u - w.first : 0u;
     return w;
 }
 
+// Value number k behind the row's vector 0.
 template <int KIND> __device__ __forceinline__ float one_value(const Row& w, u32 k) {
-    if (KIND == kScoreState) {
-        const float2 z = ((const float2*)w.p)[k];
-        return __builtin_fmaf(z.y, z.y, z.x * z.x);     // the probability as every measurement has it
+    if constexpr (KIND == kScoreState) {
+        in_global<float>* z = (in_global<float>*)w.base + 2ull * k;
+        return __builtin_fmaf(z[1], z[1], z[0] * z[0]);     // the probability as every measurement has it
+    } else if constexpr (kKeys16<KIND>) {
+        const unsigned short b = ((in_global<unsigned short>*)w.base)[k];
+        return KIND == kScoreF16 ? __half2float(__ushort_as_half(b)) : __uint_as_float((u32)b << 16);
+    } else {
+        return ((in_global<float>*)w.base)[k];
     }
-    if (KIND == kScoreF16) return __half2float(((const __half*)w.p)[k]);
-    if (KIND == kScoreBF16) return __uint_as_float((u32)((const unsigned short*)w.p)[k] << 16);
-    return ((const float*)w.p)[k];
 }
 
 template <int KIND> __device__ __forceinline__ void load4(const Row& w, u32 j, float (&v)[4]) {
-    const long long first = 4ll * j - w.skew;
-    if (first >= 0 && first + 4 <= (long long)w.cols) {
-        if (KIND == kScoreState) {
-            const float4* q = (const float4*)(w.p + first * 8);
-            const float4 x = q[0], y = q[1];
-            v[0] = __builtin_fmaf(x.y, x.y, x.x * x.x);
-            v[1] = __builtin_fmaf(x.w, x.w, x.z * x.z);
-            v[2] = __builtin_fmaf(y.y, y.y, y.x * y.x);
-            v[3] = __builtin_fmaf(y.w, y.w, y.z * y.z);
-        } else if (kKeys16<KIND>) {
-            const uint2 x = *(const uint2*)(w.p + first * 2);
-            if (KIND == kScoreBF16) {
-                v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u);
-                v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
-            } else {
-                v[0] = __half2float(__ushort_as_half((unsigned short)x.x));
-                v[1] = __half2float(__ushort_as_half((unsigned short)(x.x >> 16)));
-                v[2] = __half2float(__ushort_as_half((unsigned short)x.y));
-                v[3] = __half2float(__ushort_as_half((unsigned short)(x.y >> 16)));
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    typedef u32 u2 __attribute__((ext_vector_type(2)));
+    if (j - w.first < w.whole) {
+        if constexpr (KIND == kScoreState) {
+            in_global<f4>* q = (in_global<f4>*)w.base + 2ull * j;
+            const f4 x = q[0], y = q[1];
+            v[0] = __builtin_fmaf(x[1], x[1], x[0] * x[0]);
+            v[1] = __builtin_fmaf(x[3], x[3], x[2] * x[2]);
+            v[2] = __builtin_fmaf(y[1], y[1], y[0] * y[0]);
+            v[3] = __builtin_fmaf(y[3], y[3], y[2] * y[2]);
+        } else if constexpr (kKeys16<KIND>) {
+            const u2 x = ((in_global<u2>*)w.base)[j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32 two = x[i >> 1];
+                if (KIND == kScoreBF16) v[i] = __uint_as_float((i & 1) ? two & 0xffff0000u : two << 16);
+                else v[i] = __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
             }
         } else {
-            const float4 x = *(const float4*)(w.p + first * 4);
-            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+            const f4 x = ((in_global<f4>*)w.base)[j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = x[i];
         }
         return;
     }
-    if (j >= w.vecs) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = kMasked<KIND>;
-        return;
-    }
+    for (int i = 0; i < 4; ++i) v[i] = kMasked<KIND>;
+    if (j >= w.vecs) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const long long k = first + i;
-        v[i] = k >= 0 && k < (long long)w.cols ? one_value<KIND>(w, (u32)k) : kMasked<KIND>;
-    }
+    for (u32 i = 0; i < 4; ++i)
+        if (4 * j + i >= w.skew && 4 * j + i - w.skew < w.cols) v[i] = one_value<KIND>(w, 4 * j + i);
 }
 
 // ---- weights ---------------------------------------------------------------------------------------------------------
@@ -196,7 +198,7 @@ __device__ __forceinline__ double log2_of(const Logs* l, float v) {
     const u64 b = (u64)__double_as_longlong((double)v);
     const int k = (int)(b >> 52) - 1023, i = (int)(b >> 44) & 255;
     const double f = __longlong_as_double((long long)((b & 0xfffffffffffffull) | 0x3ff0000000000000ull));
-    const double r = fma(f, l->c[i], -1.0);
+    const double r = fma(f, ((in_lds<double>*)l->c)[i], -1.0);
     double s = 1.0 / 7.0;
     s = fma(s, -r, 1.0 / 6.0);
     s = fma(s, -r, 1.0 / 5.0);
@@ -204,7 +206,7 @@ __device__ __forceinline__ double log2_of(const Logs* l, float v) {
     s = fma(s, -r, 1.0 / 3.0);
     s = fma(s, -r, 1.0 / 2.0);
     s = fma(s, -r, 1.0);
-    return ((double)k - l->log2_c[i]) + s * r * 1.4426950408889634074;
+    return ((double)k - ((in_lds<double>*)l->log2_c)[i]) + s * r * 1.4426950408889634074;
 }
 
 // What weights are looked up in: a kernel's tables in LDS.
@@ -234,7 +236,7 @@ template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, const 
     p = fma(p, r, l * l / 2.0);
     p = fma(p, r, l);
     p = fma(p, r, 1.0);
-    return whole(fma(__builtin_ldexp(tables->powers[n & (kPowers - 1)], (n >> 8) + s.bits), p, 4503599627370496.0));
+    return whole(fma(__builtin_ldexp(((in_lds<double>*)tables->powers)[n & (kPowers - 1)], (n >> 8) + s.bits), p, 4503599627370496.0));
 }
 
 // Filled by a kernel's threads before their next barrier: 2^(i / 256), and logarithms where a row will ask for them.
@@ -430,7 +432,10 @@ template <int KIND, int STEPS, bool WEIGHTS> __device__ __forceinline__ void chu
         for (int i = 0; i < 4; ++i) {
             const bool keep = keeps(cut, v[it][i], 4 * (j0 + it * 64u + lane) - row.skew + i);
             num += keep;
-            if (WEIGHTS && keep) sum += weight<KIND>(s, tables, v[it][i]);
+            if (WEIGHTS) {
+                const u64 x = weight<KIND>(s, tables, v[it][i]);
+                sum += keep ? x : 0;
+            }
         }
     *n = wave_sum(num);
     *w = WEIGHTS ? wave_sum(sum) : 0;
@@ -532,6 +537,25 @@ template <int NT> __device__ __forceinline__ void sort_lds(u64* a, u32 n) {
         }
 }
 
+// Four values of a lane into a histogram (counts, weights) of those in from .. to: over distances (first), or over keys down
+// from khi.  The weights of all four are worked out side by side, then what is in the range is added.
+template <int KIND, int NB> __device__ __forceinline__ void add4(const Scale& s, const Tables<KIND>* tables, const float (&v)[4], bool first, bool counts, bool weights, float from, float to, u32 khi, int shift, u64* wt, u32* cnt) {
+    u64 w[4];
+    u32 b[4];
+    if (weights) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = weight<KIND>(s, tables, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = first ? bin_of<KIND, NB>(s, v[i]) : (khi - key_of<KIND>(v[i])) >> shift;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (v[i] >= from && v[i] <= to) {
+            if (counts) atomicAdd(&cnt[b[i]], 1u);
+            if (weights) atomicAdd(&wt[b[i]], w[i]);
+        }
+}
+
 // ---- one workgroup a row ---------------------------------------------------------------------------------------------
 template <int NT> struct Shape;
 // bins of a histogram (and entries of a list to be sorted), chunks, vectors of a lane in a chunk
@@ -607,12 +631,13 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         __syncthreads();
         const int shift = key_shift<NB>(khi - klo);
         const float from = value_of<KIND>(klo), to = value_of<KIND>(khi);
-        each([&](float v, u32) {
-            if (!(v >= from && v <= to)) return;
-            const u32 b = h * NB + (first ? bin_of<KIND, NB>(s, v) : (khi - key_of<KIND>(v)) >> shift);
-            if (counts) atomicAdd(&cnt[b], 1u);
-            if (weights) atomicAdd(&wt[b], weight<KIND>(s, tables, v));
-        });
+        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
+            float v[UN][4];
+#pragma unroll
+            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
+#pragma unroll
+            for (int u = 0; u < UN; ++u) add4<KIND, NB>(s, tables, v[u], first, counts, weights, from, to, khi, shift, wt + h * NB, cnt + h * NB);
+        }
         __syncthreads();
     };
     // the list in order, its entries' weights; the sum of the weights before each thread's entries
@@ -758,16 +783,24 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             u64 sum = 0;
             u32 num = 0;
 #pragma unroll
-            for (int it = 0; it < STEPS; ++it)
+            for (int it = 0; it < STEPS; ++it) {
+                u32 b[4], any = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const u32 b = v[it][i] >= low ? bin_of<KIND, NB>(s, v[it][i]) : kAll;
-                    if (b < at.bin) { ++num; sum += weight<KIND>(s, tables, v[it][i]); }
-                    if (b == at.bin) {
-                        const u32 slot = atomicAdd(&list_n, 1u);
-                        if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[it][i]) << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
-                    }
+                    b[i] = v[it][i] >= low ? bin_of<KIND, NB>(s, v[it][i]) : kAll;
+                    num += b[i] < at.bin;
+                    any |= b[i] < at.bin;
+                    if (b[i] != at.bin) continue;
+                    const u32 slot = atomicAdd(&list_n, 1u);
+                    if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[it][i]) << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
                 }
+                if (__ballot(any != 0) == 0) continue;
+                u64 w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = weight<KIND>(s, tables, v[it][i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum += b[i] < at.bin ? w[i] : 0;
+            }
             num = wave_sum(num);
             sum = wave_sum(sum);
             if (lane == 0) { chunk_n[c] = num; chunk_w[c] = sum; }
@@ -1064,14 +1097,7 @@ template <int KIND> __device__ __forceinline__ void long_histogram(const Row& ro
             else for (int i = 0; i < 4; ++i) v[u][i] = kMasked<KIND>;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!(v[u][i] >= low && v[u][i] <= high)) continue;
-                const u32 b = first ? bin_of<KIND, kLongBins>(s, v[u][i]) : (khi - key_of<KIND>(v[u][i])) >> shift;
-                atomicAdd(&cnt[b], 1u);
-                if (weights) atomicAdd(&wt[b], weight<KIND>(s, tables, v[u][i]));
-            }
+        for (int u = 0; u < 4; ++u) add4<KIND, kLongBins>(s, tables, v[u], first, true, weights, low, high, khi, shift, wt, cnt);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) {
@@ -1238,7 +1264,8 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 n += (v[it][i] > st.cut.v) + ((u32)(v[it][i] == st.cut.v) << 16);
-                if (v[it][i] > st.cut.v) w += weight<KIND>(s, tables, v[it][i]);
+                const u64 x = weight<KIND>(s, tables, v[it][i]);
+                w += v[it][i] > st.cut.v ? x : 0;
             }
         n = wave_sum(n);
         w = wave_sum(w);

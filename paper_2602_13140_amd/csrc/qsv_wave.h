@@ -44,6 +44,10 @@ __device__ __forceinline__ unsigned long long uniform(unsigned long long v) {
 }
 __device__ __forceinline__ double uniform(double v) { return __longlong_as_double((long long)uniform((unsigned long long)__double_as_longlong(v))); }
 
+// Pointers whose memory is known: through a struct or a lambda the compiler loses it, and a flat access waits for both kinds.
+template <class T> using in_global = const __attribute__((address_space(1))) T;
+template <class T> using in_lds = const __attribute__((address_space(3))) T;
+
 template <class T> __device__ __forceinline__ T last_lane(T v);
 template <> __device__ __forceinline__ unsigned last_lane(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)v, 63); }
 template <> __device__ __forceinline__ unsigned long long last_lane(unsigned long long v) {
