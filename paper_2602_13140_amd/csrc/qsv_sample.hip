@@ -151,37 +151,28 @@ struct Scale {
     float m;           // the highest value
     double md;
     double mq, rm;     // for quotients: m and 1 / m, or 1 and 0 where m is infinite
-    double c;          // scores: log2(e) / T; probabilities: 1 / T
+    double log_m;      // probabilities: log2 m
+    double c0, c;      // scores: log2(e) / T; probabilities: 1 / T; and that NP times
     double one;        // 2^S
-    int bits;          // S
     float per_bin;     // scores: bins for a distance of 1 below m
+    float low_w;       // the lowest value whose weight may differ from 0
     bool t_one;
     u32 kmax;
 };
 
-template <int KIND, int NB> __device__ __forceinline__ Scale scale_of(u32 kmax, float t, int bits) {
-    Scale s;
-    s.kmax = kmax;
-    s.m = value_of<KIND>(kmax);
-    s.md = (double)s.m;
-    s.mq = s.m < kInf ? s.md : 1.0;
-    s.rm = s.m < kInf ? 1.0 / s.md : 0.0;
-    s.bits = bits;
-    s.c = (kLogs<KIND> ? 1.4426950408889634074 : 1.0) / (double)t;
-    s.one = __builtin_ldexp(1.0, bits);
-    s.t_one = t == 1.f;
-    s.per_bin = (float)(s.c * (double)NB / (double)(bits + 2));
-    return s;
+// The lowest float that is not below x.
+__device__ __forceinline__ float float_from(double x) {
+    const float f = (float)x;
+    if ((double)f >= x) return f;
+    return f < 0.f ? __uint_as_float(__float_as_uint(f) - 1u) : __uint_as_float(__float_as_uint(f) + 1u);
 }
 
 template <int KIND> __device__ __forceinline__ double weight64(const Scale& s, float v) {
     if (v == s.m) return 1.0;
-    if (kLogs<KIND>) return exp2_neg(((double)v - s.md) * s.c);
+    if (kLogs<KIND>) return exp2_neg(((double)v - s.md) * s.c0);
     const double q = (double)v / s.md;
-    return s.t_one ? q : exp2_neg(log2(q) * s.c);
+    return s.t_one ? q : exp2_neg(log2(q) * s.c0);
 }
-
-constexpr int kPowers = 256;
 
 // log2 of a positive float in 64 bits, for probabilities at another temperature than 1: v = 2^k f, f in 1..2, its upper 8 bits
 // name a factor c near 1 / f; log2 v = k - log2 c + log2(1 + r), r = f c - 1, |r| < 2^-8: the series to r^7.  16 instructions;
@@ -210,39 +201,74 @@ __device__ __forceinline__ double log2_of(const Logs* l, float v) {
 }
 
 // What weights are looked up in: a kernel's tables in LDS.
-template <int KIND> struct Tables { double powers[256]; };
-template <> struct Tables<kScoreProbs> { double powers[256]; Logs logs; };
-template <> struct Tables<kScoreState> { double powers[256]; Logs logs; };
+// 2^S 2^(i / NP): 1024 of them save a term of the series, 256 are filled sooner.
+template <int KIND, int NP> struct Tables { double powers[NP]; };
+template <int NP> struct Tables<kScoreProbs, NP> { double powers[NP]; Logs logs; };
+template <int NP> struct Tables<kScoreState, NP> { double powers[NP]; Logs logs; };
+template <int NT> constexpr int kPowers = NT > 64 ? 1024 : 256;
 
-// rint(e 2^S), the whole number that adding 2^52 leaves in the low bits.  2^x as a power of 2^(1/256) from the table times
-// a series of four terms (|r| <= 2^-9: the next term is below 2^-54): half the arithmetic of exp2_neg.
+template <int KIND, int NB, int NP> __device__ __forceinline__ Scale scale_of(const Tables<KIND, NP>* tables, u32 kmax, float t, int bits) {
+    Scale s;
+    s.kmax = kmax;
+    s.m = value_of<KIND>(kmax);
+    s.md = (double)s.m;
+    s.mq = s.m < kInf ? s.md : 1.0;
+    s.rm = s.m < kInf ? 1.0 / s.md : 0.0;
+    s.c0 = (kLogs<KIND> ? 1.4426950408889634074 : 1.0) / (double)t;
+    s.c = s.c0 * NP;
+    s.log_m = 0.0;
+    if constexpr (!kLogs<KIND>) s.log_m = log2_of(&tables->logs, s.m);
+    s.one = __builtin_ldexp(1.0, bits);
+    s.t_one = t == 1.f;
+    s.per_bin = (float)s.c0 * ((float)NB / (float)(bits + 2));
+    // weights end below 2^-(S + 2)
+    if (!(s.m < kInf)) s.low_w = s.m;
+    else if (kLogs<KIND>) s.low_w = float_from(s.md - (double)(bits + 2) * (0.69314718055994530942 * (double)t));
+    else s.low_w = float_from(s.md * exp2_neg(-(double)(bits + 2) * (double)t));
+    return s;
+}
+
+// rint(e 2^S), the whole number that adding 2^52 leaves in the low bits.  2^x as a power from the table, its exponent raised by
+// whole steps, times a series of three terms (NP = 256: four; the next is below 2^-50): half the arithmetic of exp2_neg.
+// For values from s.low_w on; lower ones weigh nothing.  steps: NP times the distance from m, in factors of two.
 __device__ __forceinline__ u64 whole(double x) { return (u64)__double_as_longlong(x) & 0xfffffffffffffull; }
-template <int KIND> __device__ __forceinline__ u64 weight(const Scale& s, const Tables<KIND>* tables, float v) {
+template <int KIND, int NP> __device__ __forceinline__ u64 weight_of(const Scale& s, const Tables<KIND, NP>* tables, float v, u32* steps) {
     if (!kLogs<KIND> && s.t_one) {
         const double q = (double)v * s.rm;
         const double e = fma(fma(-q, s.mq, (double)v), s.rm, q);      // v / m
+        *steps = ((s.kmax - __float_as_uint(v)) >> 18) * (NP / 32);
         return whole(fma(v == s.m ? 1.0 : e, s.one, 4503599627370496.0));
     }
     double x;
-    if constexpr (kLogs<KIND>) x = ((double)v - s.md) * (s.c * kPowers);
-    else x = s.m < kInf ? (log2_of(&tables->logs, v) - log2_of(&tables->logs, s.m)) * (s.c * kPowers) : -1e300;
-    x = fmax(x, -200.0 * kPowers);
-    if (v == s.m) x = 0.0;                                            // (also where both are infinite)
+    if constexpr (kLogs<KIND>) x = ((double)v - s.md) * s.c;
+    else x = (log2_of(&tables->logs, v) - s.log_m) * s.c;
+    if (!(s.m < kInf)) x = 0.0;                                       // (only the infinite ones have a weight)
     const double y = x + 6755399441055744.0;                          // 1.5 2^52: the nearest whole number in the low bits
-    const int n = (int)__double_as_longlong(y);
+    const u32 n = (u32)__double_as_longlong(y);
+    *steps = 0u - n;
     const double r = x - (y - 6755399441055744.0);
-    constexpr double l = 0.69314718055994530942 / kPowers;
-    double p = fma(l * l * l * l / 24.0, r, l * l * l / 6.0);
+    constexpr double l = 0.69314718055994530942 / NP;
+    double p = NP > 256 ? l * l * l / 6.0 : fma(l * l * l * l / 24.0, r, l * l * l / 6.0);
     p = fma(p, r, l * l / 2.0);
     p = fma(p, r, l);
     p = fma(p, r, 1.0);
-    return whole(fma(__builtin_ldexp(((in_lds<double>*)tables->powers)[n & (kPowers - 1)], (n >> 8) + s.bits), p, 4503599627370496.0));
+    constexpr int bits = NP > 256 ? 10 : 8;
+    const u64 t = (u64)__double_as_longlong(((in_lds<double>*)tables->powers)[n & (NP - 1)]);
+    const u32 high = (u32)(t >> 32) + ((n & ~(u32)(NP - 1)) << (20 - bits));
+    return whole(fma(__longlong_as_double((long long)((u64)high << 32 | (u32)t)), p, 4503599627370496.0));
+}
+
+template <int KIND, int NP> __device__ __forceinline__ u64 weight(const Scale& s, const Tables<KIND, NP>* tables, float v) {
+    u32 steps;
+    const u64 w = weight_of<KIND, NP>(s, tables, v, &steps);
+    return v >= s.low_w ? w : 0;
 }
 
 // Filled by a kernel's threads before their next barrier: 2^(i / 256), and logarithms where a row will ask for them.
-template <int KIND, int NT> __device__ __forceinline__ void fill_tables(Tables<KIND>* tables, bool t_one) {
+template <int KIND, int NT, int NP> __device__ __forceinline__ void fill_tables(Tables<KIND, NP>* tables, int bits, bool t_one) {
     if (!kLogs<KIND> && t_one) return;
-    for (int i = threadIdx.x; i < kPowers; i += NT) tables->powers[i] = 2.0 * exp2_neg((double)i / kPowers - 1.0);
+    const double two = __builtin_ldexp(2.0, bits);
+    for (int i = threadIdx.x; i < NP; i += NT) tables->powers[i] = two * exp2_neg((double)i / NP - 1.0);
     if constexpr (!kLogs<KIND>) fill_logs<NT>(&tables->logs);
 }
 
@@ -374,11 +400,11 @@ template <int NB> __device__ __forceinline__ int key_shift(u32 range) {
 }
 
 // What is known of the cut once its bin is: the next keys to look at, or the cut itself.
-template <int KIND, bool BYW> __device__ __forceinline__ void settle(const Scale& s, const Tables<KIND>* tables, Find& f) {
+template <int KIND, bool BYW, int NP> __device__ __forceinline__ void settle(const Scale& s, const Tables<KIND, NP>* tables, Find& f) {
     if (f.klo < f.khi) return;
     f.done = 1;
     if (BYW) {
-        const u64 w = weight<KIND>(s, tables, value_of<KIND>(f.klo));
+        const u64 w = weight(s, tables, value_of<KIND>(f.klo));
         f.ne = (u32)((f.target - f.weight + w - 1) / (w ? w : 1));
     } else {
         f.ne = (u32)(f.target - f.count);
@@ -420,7 +446,7 @@ template <int NT> __device__ __forceinline__ void write_none(const SampleArgs& a
 __device__ __forceinline__ bool keeps(const Cut& cut, float v, u32 idx) { return v > cut.v || (v == cut.v && idx <= cut.idx); }
 
 // One chunk's numbers and (WEIGHTS) weights of what is kept.
-template <int KIND, int STEPS, bool WEIGHTS> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const Tables<KIND>* tables, const Cut& cut, u32 j0, u32 lane, u64* w, u32* n) {
+template <int KIND, int STEPS, bool WEIGHTS, int NP> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const Tables<KIND, NP>* tables, const Cut& cut, u32 j0, u32 lane, u64* w, u32* n) {
     float v[STEPS][4];
 #pragma unroll
     for (int it = 0; it < STEPS; ++it) load4<KIND>(row, j0 + it * 64u + lane, v[it]);
@@ -433,7 +459,7 @@ template <int KIND, int STEPS, bool WEIGHTS> __device__ __forceinline__ void chu
             const bool keep = keeps(cut, v[it][i], 4 * (j0 + it * 64u + lane) - row.skew + i);
             num += keep;
             if (WEIGHTS) {
-                const u64 x = weight<KIND>(s, tables, v[it][i]);
+                const u64 x = weight(s, tables, v[it][i]);
                 sum += keep ? x : 0;
             }
         }
@@ -464,7 +490,7 @@ template <int KIND, int STEPS> __device__ __forceinline__ u32 nth_equal(const Ro
 }
 
 // The outcome of a chunk at which the running sum of kept weights, `base` before the chunk, exceeds t.  Whole wavefront.
-template <int KIND, int STEPS> __device__ __forceinline__ long long find_in_chunk(const Row& row, const Scale& s, const Tables<KIND>* tables, const Cut& cut, u32 j0, u64 base, u64 t, u32 lane, u64* w_at) {
+template <int KIND, int STEPS, int NP> __device__ __forceinline__ long long find_in_chunk(const Row& row, const Scale& s, const Tables<KIND, NP>* tables, const Cut& cut, u32 j0, u64 base, u64 t, u32 lane, u64* w_at) {
     for (int it = 0; it < STEPS; ++it) {
         const u32 j = j0 + it * 64u + lane;
         float v[4];
@@ -473,7 +499,7 @@ template <int KIND, int STEPS> __device__ __forceinline__ long long find_in_chun
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             w[i] = 0;
-            if (keeps(cut, v[i], 4 * j - row.skew + i)) w[i] = weight<KIND>(s, tables, v[i]);
+            if (keeps(cut, v[i], 4 * j - row.skew + i)) w[i] = weight(s, tables, v[i]);
             four += w[i];
         }
         const u64 incl = wave_scan(four);
@@ -539,12 +565,12 @@ template <int NT> __device__ __forceinline__ void sort_lds(u64* a, u32 n) {
 
 // Four values of a lane into a histogram (counts, weights) of those in from .. to: over distances (first), or over keys down
 // from khi.  The weights of all four are worked out side by side, then what is in the range is added.
-template <int KIND, int NB> __device__ __forceinline__ void add4(const Scale& s, const Tables<KIND>* tables, const float (&v)[4], bool first, bool counts, bool weights, float from, float to, u32 khi, int shift, u64* wt, u32* cnt) {
+template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const Scale& s, const Tables<KIND, NP>* tables, const float (&v)[4], bool first, bool counts, bool weights, float from, float to, u32 khi, int shift, u64* wt, u32* cnt) {
     u64 w[4];
     u32 b[4];
     if (weights) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = weight<KIND>(s, tables, v[i]);
+        for (int i = 0; i < 4; ++i) w[i] = weight(s, tables, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) b[i] = first ? bin_of<KIND, NB>(s, v[i]) : (khi - key_of<KIND>(v[i])) >> shift;
@@ -569,8 +595,9 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     constexpr int UN = NT == 1024 ? 4 : 2;  // vectors of a thread on their way at once
     __shared__ u64 wt[2 * NB];              // two histograms' weights, or: weights and entries of a list to be sorted, or: a list
     __shared__ u32 cnt[2 * NB];
-    __shared__ Tables<KIND> lds_tables;
-    const Tables<KIND>* const tables = &lds_tables;
+    constexpr int NP = kPowers<NT>;
+    __shared__ Tables<KIND, NP> lds_tables;
+    const Tables<KIND, NP>* const tables = &lds_tables;
     __shared__ u64 sm[16];
     __shared__ Hit hit;
     __shared__ u32 list_n, found;
@@ -597,7 +624,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     };
     float high = kMasked<KIND>;             // of the thread's values
     each([&](float v, u32) { high = fmaxf(high, v); });
-    fill_tables<KIND, NT>(&lds_tables, p.t == 1.f);
+    fill_tables<KIND, NT>(&lds_tables, a.bits, p.t == 1.f);
     if (threadIdx.x == 0) list_n = 0;
     const u32 kmax = block_max<NT>(key_of<KIND>(high), sm);
     __syncthreads();
@@ -618,7 +645,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         if (threadIdx.x == 0 && a.kept) a.kept[r] = 1;
         return;
     }
-    const Scale s = scale_of<KIND, NB>(kmax, p.t, a.bits);
+    const Scale s = scale_of<KIND, NB, NP>(tables, kmax, p.t, a.bits);
     u32 lowest = kLowest<KIND>;
     if (p.min_p > 0.f)
         lowest = first_key(lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
@@ -648,7 +675,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
 #pragma unroll
         for (int i = 0; i < per; ++i) {
             const u32 at = threadIdx.x * per + i;
-            w[i] = at < n ? weight<KIND>(s, tables, value_of<KIND>(~(u32)(le[at] >> 32))) : 0;
+            w[i] = at < n ? weight(s, tables, value_of<KIND>(~(u32)(le[at] >> 32))) : 0;
             sum += w[i];
         }
         u64 all;
@@ -770,12 +797,44 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         return;
     }
     u64 mass = 0;
-    if (!by_k && by_p) {
-        histogram(0, true, false, true, lowest, kmax);
+    u32 klo = 0, khi = 0;                   // the keys of the bin that the cut falls into
+    if (by_k && !slow) {
+        keys_of_bin<KIND, NB>(s, at.bin, lowest, &klo, &khi);
+    } else if (!by_k && by_p) {
+        // a histogram of weights over the steps that they were worked out from, 32 to a factor of two
+        static_assert(NB >= 256, "53 factors of two, or 5 steps each");
+        constexpr int shift = (NP > 256 ? 10 : 8) - (NB >= 2048 ? 5 : NB >= 1024 ? 4 : 2);
+        const float from = fmaxf(low, s.low_w);
+        for (int i = threadIdx.x; i < NB; i += NT) wt[i] = 0;
+        __syncthreads();
+        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
+            float v[UN][4];
+#pragma unroll
+            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+                u64 w[4];
+                u32 n[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = weight_of(s, tables, v[u][i], &n[i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v[u][i] >= from) atomicAdd(&wt[min(n[i] >> shift, (u32)(NB - 1))], w[i]);
+            }
+        }
+        __syncthreads();
         (void)select_bin<NT, NB, true>(nullptr, wt, (u64)__float_as_uint(p.top_p), sm, &hit, &at, &mass);
+        auto bin = [&](u32 k) -> u32 {
+            u32 n;
+            (void)weight_of(s, tables, value_of<KIND>(k), &n);
+            return min(n >> shift, (u32)(NB - 1));
+        };
+        klo = first_key(key_of<KIND>(from), kmax, [&](u32 k) { return bin(k) <= at.bin; });
+        khi = at.bin == 0 ? kmax : first_key(klo, kmax, [&](u32 k) { return bin(k) < at.bin; }) - 1u;
     }
     if ((by_k || by_p) && !slow) {
         // what lies above the bin is kept, what lies in it decides: the chunks' sums of the ones, a list of the others
+        const float from = value_of<KIND>(klo), to = value_of<KIND>(khi);
         for (u32 c = wave; c < nchunks; c += NT / 64) {
             float v[STEPS][4];
 #pragma unroll
@@ -784,22 +843,24 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             u32 num = 0;
 #pragma unroll
             for (int it = 0; it < STEPS; ++it) {
-                u32 b[4], any = 0;
+                const float top = fmaxf(fmaxf(v[it][0], v[it][1]), fmaxf(v[it][2], v[it][3]));
+                if (__ballot(top >= from) == 0) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v[it][i] >= from && v[it][i] <= to) {
+                        const u32 slot = atomicAdd(&list_n, 1u);
+                        if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[it][i]) << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
+                    }
+                if (__ballot(top > to) == 0) continue;
+                u64 w[4];
+                u32 unused;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = weight_of(s, tables, v[it][i], &unused);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    b[i] = v[it][i] >= low ? bin_of<KIND, NB>(s, v[it][i]) : kAll;
-                    num += b[i] < at.bin;
-                    any |= b[i] < at.bin;
-                    if (b[i] != at.bin) continue;
-                    const u32 slot = atomicAdd(&list_n, 1u);
-                    if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[it][i]) << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
+                    num += v[it][i] > to;
+                    sum += v[it][i] > to && v[it][i] >= s.low_w ? w[i] : 0;
                 }
-                if (__ballot(any != 0) == 0) continue;
-                u64 w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = weight<KIND>(s, tables, v[it][i]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum += b[i] < at.bin ? w[i] : 0;
             }
             num = wave_sum(num);
             sum = wave_sum(sum);
@@ -861,7 +922,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         if (by_k && narrow(ByCount{}, (u64)p.top_k, &f)) {
             cut.v = value_of<KIND>(f.klo);
             ne = f.ne;
-            if (by_p) mass = f.weight + (u64)f.ne * weight<KIND>(s, tables, value_of<KIND>(f.klo));
+            if (by_p) mass = f.weight + (u64)f.ne * weight(s, tables, value_of<KIND>(f.klo));
             have_mass = true;
         }
         if (by_p) {
@@ -954,7 +1015,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         const u32 first = threadIdx.x * own;
 #pragma unroll
         for (int i = 0; i < own; ++i) {
-            w[i] = first + i < n_kept ? weight<KIND>(s, tables, value_of<KIND>((u32)lw[first + i])) : 0;
+            w[i] = first + i < n_kept ? weight(s, tables, value_of<KIND>((u32)lw[first + i])) : 0;
             sum += w[i];
         }
         u64 run = block_scan<NT>(sum, sm, &total);
@@ -1001,6 +1062,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
 // again from the one before and its histogram; the row's first one writes it down.  Steps whose cut is known already end
 // at once.
 constexpr int kLongBins = 2048, kLongThreads = 256, kLongSteps = 4, kLongChunk = 64 * kLongSteps * 4;
+template <int KIND> using LongTables = Tables<KIND, kPowers<kLongThreads>>;
 constexpr int kKeySteps = 3;                       // 11 bits of a key each
 constexpr int kLevels = 1 + 2 * kKeySteps;         // distances; keys for top-k; keys for top-p
 
@@ -1084,7 +1146,7 @@ __device__ __forceinline__ bool by_top_k(const SampleArgs& a, const Params& p) {
 __device__ __forceinline__ bool by_top_p(const Params& p) { return p.t > 0.f && p.top_p < 1.f; }
 
 // The histogram of the values of vectors j0 .. j1 with keys in klo .. khi, added to the row's.
-template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, const Tables<KIND>* tables, u64* wt, u32* cnt, u64* gw, u32* gc) {
+template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, const LongTables<KIND>* tables, u64* wt, u32* cnt, u64* gw, u32* gc) {
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) { cnt[i] = 0; wt[i] = 0; }
     __syncthreads();
     const int shift = key_shift<kLongBins>(khi - klo);
@@ -1111,9 +1173,9 @@ template <int KIND> __device__ __forceinline__ void long_histogram(const Row& ro
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first(const SampleArgs a, const Long g) {
     __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
     __shared__ u32 cnt[kLongBins];
-    __shared__ Tables<KIND> lds_tables;
-    const Tables<KIND>* const tables = &lds_tables;
-    fill_tables<KIND, kLongThreads>(&lds_tables, false);
+    __shared__ LongTables<KIND> lds_tables;
+    const LongTables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, kLongThreads>(&lds_tables, a.bits, false);
     __syncthreads();
     const u64 r = grid_block() / g.parts;
     const u32 part = (u32)(grid_block() % g.parts);
@@ -1128,7 +1190,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first
     st.kmax = kmax;
     st.lowest = kLowest<KIND>;
     if (st.ok) {
-        const Scale s = scale_of<KIND, kLongBins>(kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+        const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, kmax, p.t > 0.f ? p.t : 1.f, a.bits);
         if (p.min_p > 0.f && p.t > 0.f)
             st.lowest = first_key(st.lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
         st.cut = Cut{value_of<KIND>(p.t > 0.f ? st.lowest : kmax), kAll};
@@ -1143,7 +1205,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first
 }
 
 // The search after the histogram of level `prev`.
-template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_advance(const SampleArgs& a, const Params& p, const Scale& s, const Tables<KIND>* tables, const Long& g, u64 r, int prev, u64* sm, Hit* hit, LongState* st) {
+template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_advance(const SampleArgs& a, const Params& p, const Scale& s, const LongTables<KIND>* tables, const Long& g, u64 r, int prev, u64* sm, Hit* hit, LongState* st) {
     if (!st->stage) return;
     Find& f = st->f;
     const u64* wt = g.wt + (r * kLevels + prev) * kLongBins;
@@ -1166,13 +1228,13 @@ template <int KIND, int NT = kLongThreads> __device__ __forceinline__ void long_
     st->cut = Cut{value_of<KIND>(f.klo), kAll};
     st->ne = f.ne;
     if (st->stage == 1 && by_top_p(p)) {
-        st->mass = f.weight + (u64)f.ne * weight<KIND>(s, tables, value_of<KIND>(f.klo));
+        st->mass = f.weight + (u64)f.ne * weight(s, tables, value_of<KIND>(f.klo));
         st->have_mass = 1;
     }
     st->stage = 0;
 }
 
-template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs& a, const Params& p, const Scale& s, const Tables<KIND>* tables, const Long& g, u64 r, u32 stage, u64* sm, Hit* hit, LongState* st) {
+template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs& a, const Params& p, const Scale& s, const LongTables<KIND>* tables, const Long& g, u64 r, u32 stage, u64* sm, Hit* hit, LongState* st) {
     const u64* wt = g.wt + r * kLevels * kLongBins;
     const u32* cnt = g.cnt + r * kLevels * kLongBins;
     Hit at;
@@ -1208,9 +1270,9 @@ template <int KIND> __device__ __forceinline__ void long_begin(const SampleArgs&
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(const SampleArgs a, const Long g, int level, int prev) {
     __shared__ u64 sm[kLongThreads / 64], wt[kLongBins];
     __shared__ u32 cnt[kLongBins];
-    __shared__ Tables<KIND> lds_tables;
-    const Tables<KIND>* const tables = &lds_tables;
-    fill_tables<KIND, kLongThreads>(&lds_tables, false);
+    __shared__ LongTables<KIND> lds_tables;
+    const LongTables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, kLongThreads>(&lds_tables, a.bits, false);
     __syncthreads();
     __shared__ Hit hit;
     const u64 r = grid_block() / g.parts;
@@ -1220,7 +1282,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(
     const Params p = params_of(a, r);
     LongState st = g.state[r * kLevels + prev];
     if (st.ok) {
-        const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+        const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
         long_advance<KIND>(a, p, s, tables, g, r, prev, sm, &hit, &st);
         if (level == 1 && by_top_k(a, p)) long_begin<KIND>(a, p, s, tables, g, r, 1, sm, &hit, &st);
         if (level == 1 + kKeySteps && by_top_p(p)) long_begin<KIND>(a, p, s, tables, g, r, 2, sm, &hit, &st);
@@ -1238,9 +1300,9 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(
 template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(const SampleArgs a, const Long g, int prev) {
     __shared__ u64 sm[kLongThreads / 64];
     __shared__ Hit hit;
-    __shared__ Tables<KIND> lds_tables;
-    const Tables<KIND>* const tables = &lds_tables;
-    fill_tables<KIND, kLongThreads>(&lds_tables, false);
+    __shared__ LongTables<KIND> lds_tables;
+    const LongTables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, kLongThreads>(&lds_tables, a.bits, false);
     __syncthreads();
     const u64 r = grid_block() / g.parts;
     const u32 part = (u32)(grid_block() % g.parts);
@@ -1249,7 +1311,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     const Params p = params_of(a, r);
     LongState st = g.state[r * kLevels + prev];
     if (!st.ok) return;
-    const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_advance<KIND>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     const u32 lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const u32 c1 = min((part + 1) * g.chunks_per_part, g.chunks);
@@ -1264,7 +1326,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 n += (v[it][i] > st.cut.v) + ((u32)(v[it][i] == st.cut.v) << 16);
-                const u64 x = weight<KIND>(s, tables, v[it][i]);
+                const u64 x = weight(s, tables, v[it][i]);
                 w += v[it][i] > st.cut.v ? x : 0;
             }
         n = wave_sum(n);
@@ -1276,7 +1338,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     }
 }
 
-template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const Tables<KIND>* tables, const Cut& cut, const u64* cw, u32 chunks, u64 at, u32 lane) {
+template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const LongTables<KIND>* tables, const Cut& cut, const u64* cw, u32 chunks, u64 at, u32 lane) {
     const double u = a.uniforms[at];
     const u64 total = cw[chunks - 1];
     long long k = -1;
@@ -1303,10 +1365,10 @@ template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& 
 template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const SampleArgs a, const Long g, int prev, int draw) {
     __shared__ u64 sm[16];
     __shared__ Hit hit;
-    __shared__ Tables<KIND> lds_tables;
-    const Tables<KIND>* const tables = &lds_tables;
+    __shared__ LongTables<KIND> lds_tables;
+    const LongTables<KIND>* const tables = &lds_tables;
     __shared__ u32 found, rank;
-    fill_tables<KIND, 1024>(&lds_tables, false);
+    fill_tables<KIND, 1024>(&lds_tables, a.bits, false);
     if (threadIdx.x == 0) found = kAll;
     __syncthreads();
     const u64 r = grid_block();
@@ -1321,7 +1383,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
         if (threadIdx.x == 0) g.state[r * kLevels + kLevels - 1] = st;
         return;
     }
-    const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_advance<KIND, 1024>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     u64* cw = g.chunk_w + r * g.chunks;
     const u32* cn = g.chunk_n + r * g.chunks;
@@ -1330,7 +1392,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     u64 eq = 0, eq_all, n_kept, total;
     for (u32 c = c0; c < c1; ++c) eq += cn[c] >> 16;
     const u64 eq_before = block_scan<1024>(eq, sm, &eq_all);
-    const u64 w_cut = weight<KIND>(s, tables, st.cut.v);
+    const u64 w_cut = weight(s, tables, st.cut.v);
     u64 run = eq_before, num = 0, w = 0;
     for (u32 c = c0; c < c1; ++c) {
         const u32 n = cn[c];
@@ -1364,9 +1426,9 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
 }
 
 template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const SampleArgs a, const Long g) {
-    __shared__ Tables<KIND> lds_tables;
-    const Tables<KIND>* const tables = &lds_tables;
-    fill_tables<KIND, 256>(&lds_tables, false);
+    __shared__ LongTables<KIND> lds_tables;
+    const LongTables<KIND>* const tables = &lds_tables;
+    fill_tables<KIND, 256>(&lds_tables, a.bits, false);
     __syncthreads();
     const u64 at = grid_block() * 4 + (threadIdx.x >> 6);
     if (at >= (u64)a.rows * a.shots) return;
@@ -1379,7 +1441,7 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
     }
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
-    const Scale s = scale_of<KIND, kLongBins>(st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_shot<KIND>(a, row, s, tables, st.cut, g.chunk_w + r * g.chunks, g.chunks, at, lane);
 }
 
