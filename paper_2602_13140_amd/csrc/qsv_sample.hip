@@ -89,38 +89,77 @@ template <int KIND> __device__ __forceinline__ float one_value(const Row& w, u32
     }
 }
 
-template <int KIND> __device__ __forceinline__ void load4(const Row& w, u32 j, float (&v)[4]) {
+// Vector j, which lies in the row whole.
+template <int KIND> __device__ __forceinline__ void load_whole(const Row& w, u32 j, float (&v)[4]) {
     typedef float f4 __attribute__((ext_vector_type(4)));
     typedef u32 u2 __attribute__((ext_vector_type(2)));
-    if (j - w.first < w.whole) {
-        if constexpr (KIND == kScoreState) {
-            in_global<f4>* q = (in_global<f4>*)w.base + 2ull * j;
-            const f4 x = q[0], y = q[1];
-            v[0] = __builtin_fmaf(x[1], x[1], x[0] * x[0]);
-            v[1] = __builtin_fmaf(x[3], x[3], x[2] * x[2]);
-            v[2] = __builtin_fmaf(y[1], y[1], y[0] * y[0]);
-            v[3] = __builtin_fmaf(y[3], y[3], y[2] * y[2]);
-        } else if constexpr (kKeys16<KIND>) {
-            const u2 x = ((in_global<u2>*)w.base)[j];
+    if constexpr (KIND == kScoreState) {
+        in_global<f4>* q = (in_global<f4>*)w.base + 2ull * j;
+        const f4 x = q[0], y = q[1];
+        v[0] = __builtin_fmaf(x[1], x[1], x[0] * x[0]);
+        v[1] = __builtin_fmaf(x[3], x[3], x[2] * x[2]);
+        v[2] = __builtin_fmaf(y[1], y[1], y[0] * y[0]);
+        v[3] = __builtin_fmaf(y[3], y[3], y[2] * y[2]);
+    } else if constexpr (kKeys16<KIND>) {
+        const u2 x = ((in_global<u2>*)w.base)[j];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const u32 two = x[i >> 1];
-                if (KIND == kScoreBF16) v[i] = __uint_as_float((i & 1) ? two & 0xffff0000u : two << 16);
-                else v[i] = __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
-            }
-        } else {
-            const f4 x = ((in_global<f4>*)w.base)[j];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = x[i];
+        for (int i = 0; i < 4; ++i) {
+            const u32 two = x[i >> 1];
+            if (KIND == kScoreBF16) v[i] = __uint_as_float((i & 1) ? two & 0xffff0000u : two << 16);
+            else v[i] = __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
         }
-        return;
+    } else {
+        const f4 x = ((in_global<f4>*)w.base)[j];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = x[i];
     }
+}
+
+// Any vector: masked values where it reaches over the row's ends.
+template <int KIND> __device__ __forceinline__ void load4(const Row& w, u32 j, float (&v)[4]) {
+    if (j - w.first < w.whole) return load_whole<KIND>(w, j, v);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = kMasked<KIND>;
     if (j >= w.vecs) return;
 #pragma unroll
     for (u32 i = 0; i < 4; ++i)
         if (4 * j + i >= w.skew && 4 * j + i - w.skew < w.cols) v[i] = one_value<KIND>(w, 4 * j + i);
+}
+
+// f(values, j) for every vector from j0 to j1 (or the row's end), a thread each, UN of a thread on their way at once.
+template <int KIND, int NT, int UN, class F> __device__ __forceinline__ void walk(const Row& w, u32 j0, u32 j1, F f) {
+    if (j0 == 0 && w.first) {
+        if (threadIdx.x == 0) {
+            float v[4];
+            load4<KIND>(w, 0, v);
+            f(v, 0u);
+        }
+        j0 = 1;
+    }
+    const u32 end = min(j1, w.first + w.whole);
+    for (; j0 + NT * UN <= end; j0 += NT * UN) {
+        float v[UN][4];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) load_whole<KIND>(w, j0 + u * NT + threadIdx.x, v[u]);
+#pragma unroll
+        for (int u = 0; u < UN; ++u) f(v[u], j0 + u * NT + threadIdx.x);
+    }
+    for (u32 j = j0 + threadIdx.x; j < min(j1, w.vecs); j += NT) {
+        float v[4];
+        load4<KIND>(w, j, v);
+        f(v, j);
+    }
+}
+
+// The vectors j0 + lane, j0 + 64 + lane, ... of a wavefront's chunk.
+template <int KIND, int STEPS> __device__ __forceinline__ void load_chunk(const Row& w, u32 j0, u32 lane, float (&v)[STEPS][4]) {
+    if (j0 >= w.first && j0 + 64 * STEPS <= w.first + w.whole) {
+#pragma unroll
+        for (int it = 0; it < STEPS; ++it) load_whole<KIND>(w, j0 + it * 64u + lane, v[it]);
+    } else {
+#pragma unroll
+        for (int it = 0; it < STEPS; ++it) load4<KIND>(w, j0 + it * 64u + lane, v[it]);
+    }
 }
 
 // ---- weights ---------------------------------------------------------------------------------------------------------
@@ -149,6 +188,7 @@ __device__ __forceinline__ double exp2_neg(double x) {
 // How a row's values become weights.
 struct Scale {
     float m;           // the highest value
+    float top;         // m, or the highest finite float
     double md;
     double mq, rm;     // for quotients: m and 1 / m, or 1 and 0 where m is infinite
     double log_m;      // probabilities: log2 m
@@ -169,6 +209,7 @@ __device__ __forceinline__ float float_from(double x) {
 
 template <int KIND> __device__ __forceinline__ double weight64(const Scale& s, float v) {
     if (v == s.m) return 1.0;
+    if (!(s.m < kInf)) return 0.0;
     if (kLogs<KIND>) return exp2_neg(((double)v - s.md) * s.c0);
     const double q = (double)v / s.md;
     return s.t_one ? q : exp2_neg(log2(q) * s.c0);
@@ -201,23 +242,24 @@ __device__ __forceinline__ double log2_of(const Logs* l, float v) {
 }
 
 // What weights are looked up in: a kernel's tables in LDS.
-// 2^S 2^(i / NP): 1024 of them save a term of the series, 256 are filled sooner.
+// 2^(S - 63) 2^(i / NP): 1024 of them save a term of the series, 256 are filled sooner.
 template <int KIND, int NP> struct Tables { double powers[NP]; };
 template <int NP> struct Tables<kScoreProbs, NP> { double powers[NP]; Logs logs; };
 template <int NP> struct Tables<kScoreState, NP> { double powers[NP]; Logs logs; };
-template <int NT> constexpr int kPowers = NT > 64 ? 1024 : 256;
+template <int NT> constexpr int kPowers = NT > 256 ? 1024 : 256;
 
 template <int KIND, int NB, int NP> __device__ __forceinline__ Scale scale_of(const Tables<KIND, NP>* tables, u32 kmax, float t, int bits) {
     Scale s;
     s.kmax = kmax;
     s.m = value_of<KIND>(kmax);
-    s.md = (double)s.m;
+    s.top = fminf(s.m, 3.402823466e38f);
+    s.md = (double)s.top;
     s.mq = s.m < kInf ? s.md : 1.0;
     s.rm = s.m < kInf ? 1.0 / s.md : 0.0;
     s.c0 = (kLogs<KIND> ? 1.4426950408889634074 : 1.0) / (double)t;
     s.c = s.c0 * NP;
     s.log_m = 0.0;
-    if constexpr (!kLogs<KIND>) s.log_m = log2_of(&tables->logs, s.m);
+    if constexpr (!kLogs<KIND>) s.log_m = log2_of(&tables->logs, s.top);
     s.one = __builtin_ldexp(1.0, bits);
     s.t_one = t == 1.f;
     s.per_bin = (float)s.c0 * ((float)NB / (float)(bits + 2));
@@ -230,31 +272,39 @@ template <int KIND, int NB, int NP> __device__ __forceinline__ Scale scale_of(co
 
 // rint(e 2^S), the whole number that adding 2^52 leaves in the low bits.  2^x as a power from the table, its exponent raised by
 // whole steps, times a series of three terms (NP = 256: four; the next is below 2^-50): half the arithmetic of exp2_neg.
-// For values from s.low_w on; lower ones weigh nothing.  steps: NP times the distance from m, in factors of two.
+// For values from s.low_w on; lower ones weigh nothing.  step: NP times the distance from m, in factors of two, below 63 NP.
+// (Of its instructions those that the compiler would spend moves or a 64-bit addition on are named.)
+template <int NP> constexpr u32 kTopStep = 63 * NP;
+__device__ __forceinline__ double fma3(double a, double b, double c) {
+    double d;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
 __device__ __forceinline__ u64 whole(double x) { return (u64)__double_as_longlong(x) & 0xfffffffffffffull; }
-template <int KIND, int NP> __device__ __forceinline__ u64 weight_of(const Scale& s, const Tables<KIND, NP>* tables, float v, u32* steps) {
+template <int KIND, int NP> __device__ __forceinline__ u64 weight_of(const Scale& s, const Tables<KIND, NP>* tables, float v, u32* step) {
     if (!kLogs<KIND> && s.t_one) {
         const double q = (double)v * s.rm;
         const double e = fma(fma(-q, s.mq, (double)v), s.rm, q);      // v / m
-        *steps = ((s.kmax - __float_as_uint(v)) >> 18) * (NP / 32);
+        *step = kTopStep<NP> - ((s.kmax - __float_as_uint(v)) >> 18) * (NP / 32);
         return whole(fma(v == s.m ? 1.0 : e, s.one, 4503599627370496.0));
     }
     double x;
-    if constexpr (kLogs<KIND>) x = ((double)v - s.md) * s.c;
-    else x = (log2_of(&tables->logs, v) - s.log_m) * s.c;
-    if (!(s.m < kInf)) x = 0.0;                                       // (only the infinite ones have a weight)
-    const double y = x + 6755399441055744.0;                          // 1.5 2^52: the nearest whole number in the low bits
+    if constexpr (kLogs<KIND>) x = ((double)fminf(v, s.top) - s.md) * s.c;
+    else x = (log2_of(&tables->logs, fminf(v, s.top)) - s.log_m) * s.c;
+    constexpr double magic = 6755399441055744.0 + kTopStep<NP>;       // 1.5 2^52: the nearest whole number in the low bits
+    const double y = x + magic;
     const u32 n = (u32)__double_as_longlong(y);
-    *steps = 0u - n;
-    const double r = x - (y - 6755399441055744.0);
+    *step = n;
+    const double r = x - (y - magic);
     constexpr double l = 0.69314718055994530942 / NP;
-    double p = NP > 256 ? l * l * l / 6.0 : fma(l * l * l * l / 24.0, r, l * l * l / 6.0);
-    p = fma(p, r, l * l / 2.0);
-    p = fma(p, r, l);
+    double p = NP > 256 ? l * l * l / 6.0 : fma3(l * l * l * l / 24.0, r, l * l * l / 6.0);
+    p = fma3(p, r, l * l / 2.0);
+    p = fma3(p, r, l);
     p = fma(p, r, 1.0);
     constexpr int bits = NP > 256 ? 10 : 8;
     const u64 t = (u64)__double_as_longlong(((in_lds<double>*)tables->powers)[n & (NP - 1)]);
-    const u32 high = (u32)(t >> 32) + ((n & ~(u32)(NP - 1)) << (20 - bits));
+    u32 high;
+    asm("v_lshl_add_u32 %0, %1, %2, %3" : "=v"(high) : "v"(n & ~(u32)(NP - 1)), "n"(20 - bits), "v"((u32)(t >> 32)));
     return whole(fma(__longlong_as_double((long long)((u64)high << 32 | (u32)t)), p, 4503599627370496.0));
 }
 
@@ -267,7 +317,7 @@ template <int KIND, int NP> __device__ __forceinline__ u64 weight(const Scale& s
 // Filled by a kernel's threads before their next barrier: 2^(i / 256), and logarithms where a row will ask for them.
 template <int KIND, int NT, int NP> __device__ __forceinline__ void fill_tables(Tables<KIND, NP>* tables, int bits, bool t_one) {
     if (!kLogs<KIND> && t_one) return;
-    const double two = __builtin_ldexp(2.0, bits);
+    const double two = __builtin_ldexp(2.0, bits - 63);        // (steps start at 63 factors of two)
     for (int i = threadIdx.x; i < NP; i += NT) tables->powers[i] = two * exp2_neg((double)i / NP - 1.0);
     if constexpr (!kLogs<KIND>) fill_logs<NT>(&tables->logs);
 }
@@ -353,9 +403,11 @@ __device__ __forceinline__ u64 mass_of(float top_p, u64 w) {
 struct Hit { u32 bin; u64 count, weight, own; };        // own: outcomes in the bin
 struct ByCount { static constexpr bool value = false; };
 struct ByWeight { static constexpr bool value = true; };
-template <int NT, int NB, bool BYW> __device__ __forceinline__ bool select_bin(const u32* cnt, const u64* wt, u64 target, u64* sm, Hit* hit, Hit* at, u64* total = nullptr) {
+// MIRROR: weights in bins that rise with the value; the bin's number counts from the last one.
+template <int NT, int NB, bool BYW, bool MIRROR = false> __device__ __forceinline__ bool select_bin(const u32* cnt, const u64* weights, u64 target, u64* sm, Hit* hit, Hit* at, u64* total = nullptr) {
     constexpr int per = NB / NT > 0 ? NB / NT : 1;
     const int b0 = threadIdx.x * per;
+    struct { const u64* p; __device__ u64 operator[](int b) const { return p[MIRROR ? NB - 1 - b : b]; } __device__ operator bool() const { return p; } } const wt{weights};
     u64 c = 0, w = 0;
     if (b0 < NB) {
 #pragma unroll
@@ -448,8 +500,7 @@ __device__ __forceinline__ bool keeps(const Cut& cut, float v, u32 idx) { return
 // One chunk's numbers and (WEIGHTS) weights of what is kept.
 template <int KIND, int STEPS, bool WEIGHTS, int NP> __device__ __forceinline__ void chunk_sums(const Row& row, const Scale& s, const Tables<KIND, NP>* tables, const Cut& cut, u32 j0, u32 lane, u64* w, u32* n) {
     float v[STEPS][4];
-#pragma unroll
-    for (int it = 0; it < STEPS; ++it) load4<KIND>(row, j0 + it * 64u + lane, v[it]);
+    load_chunk<KIND, STEPS>(row, j0, lane, v);
     u64 sum = 0;
     u32 num = 0;
 #pragma unroll
@@ -563,6 +614,11 @@ template <int NT> __device__ __forceinline__ void sort_lds(u64* a, u32 n) {
         }
 }
 
+// What was worked out for all four is there before any of it is used: the compiler would move each one's work behind its test.
+__device__ __forceinline__ void side_by_side(u64 (&w)[4]) {
+    asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+}
+
 // Four values of a lane into a histogram (counts, weights) of those in from .. to: over distances (first), or over keys down
 // from khi.  The weights of all four are worked out side by side, then what is in the range is added.
 template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const Scale& s, const Tables<KIND, NP>* tables, const float (&v)[4], bool first, bool counts, bool weights, float from, float to, u32 khi, int shift, u64* wt, u32* cnt) {
@@ -571,14 +627,15 @@ template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const S
     if (weights) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = weight(s, tables, v[i]);
+        side_by_side(w);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) b[i] = first ? bin_of<KIND, NB>(s, v[i]) : (khi - key_of<KIND>(v[i])) >> shift;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (v[i] >= from && v[i] <= to) {
-            if (counts) atomicAdd(&cnt[b[i]], 1u);
-            if (weights) atomicAdd(&wt[b[i]], w[i]);
+            if (counts) lds_add(cnt + b[i], 1u);
+            if (weights) lds_add(wt + b[i], w[i]);
         }
 }
 
@@ -593,8 +650,10 @@ template <int KIND, int NT>
 __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     constexpr int NB = Shape<NT>::bins, NC = Shape<NT>::chunks, STEPS = Shape<NT>::steps, LIST = 2 * NB;
     constexpr int UN = NT == 1024 ? 4 : 2;  // vectors of a thread on their way at once
-    __shared__ u64 wt[2 * NB];              // two histograms' weights, or: weights and entries of a list to be sorted, or: a list
-    __shared__ u32 cnt[2 * NB];
+    // two histograms; or: a list to be sorted, its entries and their weights, or values on their way; or: a list to be searched
+    __shared__ struct { u64 wt[2 * NB]; u32 cnt[2 * NB]; } lds;
+    u64* const wt = lds.wt;
+    u32* const cnt = lds.cnt;
     constexpr int NP = kPowers<NT>;
     __shared__ Tables<KIND, NP> lds_tables;
     const Tables<KIND, NP>* const tables = &lds_tables;
@@ -611,19 +670,8 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     const Params p = params_of(a, r);
     const u32 nchunks = (row.vecs + 64 * STEPS - 1) / (64 * STEPS);
 
-    auto each = [&](auto f) {               // f(value, index) for every value of the row, masked ones too
-        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
-            float v[UN][4];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
-#pragma unroll
-            for (int u = 0; u < UN; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f(v[u][i], 4 * (j + u * NT) - row.skew + i);
-        }
-    };
     float high = kMasked<KIND>;             // of the thread's values
-    each([&](float v, u32) { high = fmaxf(high, v); });
+    walk<KIND, NT, UN>(row, 0, row.vecs, [&high](const float (&v)[4], u32) { high = fmaxf(fmaxf(high, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])); });
     fill_tables<KIND, NT>(&lds_tables, a.bits, p.t == 1.f);
     if (threadIdx.x == 0) list_n = 0;
     const u32 kmax = block_max<NT>(key_of<KIND>(high), sm);
@@ -636,7 +684,10 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     if (p.t == 0.f) {
         u32 first = 0;                      // the complement of the lowest index
         const float top = value_of<KIND>(kmax);
-        each([&](float v, u32 idx) { if (v == top) first = max(first, ~idx); });
+        walk<KIND, NT, UN>(row, 0, row.vecs, [&first, top, skew = row.skew](const float (&v)[4], u32 j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (v[i] == top) first = max(first, ~(4 * j - skew + i));
+        });
         first = ~block_max<NT>(first, sm);
         for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
             const double u = a.uniforms[r * a.shots + i];
@@ -649,8 +700,8 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     u32 lowest = kLowest<KIND>;
     if (p.min_p > 0.f)
         lowest = first_key(lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
-    u64* const lw = wt;                     // of a list to be sorted: weights, and entries
-    u64* const le = wt + NB;
+    u64* const le = wt;                     // of a list to be sorted: entries, and weights
+    u64* const lw = wt + NB;
 
     // a histogram (counts, weights) of the values with keys in klo .. khi: the first one over distances, later ones over keys
     auto histogram = [&](int h, bool first, bool counts, bool weights, u32 klo, u32 khi) {
@@ -658,13 +709,9 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         __syncthreads();
         const int shift = key_shift<NB>(khi - klo);
         const float from = value_of<KIND>(klo), to = value_of<KIND>(khi);
-        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
-            float v[UN][4];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
-#pragma unroll
-            for (int u = 0; u < UN; ++u) add4<KIND, NB>(s, tables, v[u], first, counts, weights, from, to, khi, shift, wt + h * NB, cnt + h * NB);
-        }
+        walk<KIND, NT, UN>(row, 0, row.vecs, [=](const float (&v)[4], u32) {
+            add4<KIND, NB>(s, tables, v, first, counts, weights, from, to, khi, shift, wt + h * NB, cnt + h * NB);
+        });
         __syncthreads();
     };
     // the list in order, its entries' weights; the sum of the weights before each thread's entries
@@ -701,22 +748,17 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     Hit at;
     // the outcomes from the distance's bin b up as a list; false: they are more than it holds
     auto collect = [&](u32 b) -> bool {
-        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
-            float v[UN][4];
+        u32* const slots = &list_n;
+        walk<KIND, NT, UN>(row, 0, row.vecs, [s, low, b, slots, le, skew = row.skew](const float (&v)[4], u32 j) {
+            const float top = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+            if (!(top >= low) || bin_of<KIND, NB>(s, top) > b) return;
 #pragma unroll
-            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
-#pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                const float top = fmaxf(fmaxf(v[u][0], v[u][1]), fmaxf(v[u][2], v[u][3]));
-                if (!(top >= low) || bin_of<KIND, NB>(s, top) > b) continue;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!(v[u][i] >= low) || bin_of<KIND, NB>(s, v[u][i]) > b) continue;
-                    const u32 slot = atomicAdd(&list_n, 1u);
-                    if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[u][i]) << 32 | (4 * (j + u * NT) - row.skew + i);
-                }
+            for (int i = 0; i < 4; ++i) {
+                if (!(v[i] >= low) || bin_of<KIND, NB>(s, v[i]) > b) continue;
+                const u32 slot = lds_add(slots, 1u);
+                if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[i]) << 32 | (4 * j - skew + i);
             }
-        }
+        });
         __syncthreads();
         const bool fits = list_n <= NB;
         if (!fits) {
@@ -732,7 +774,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         if (p.top_k <= NT * 5 / 8) {
             for (int i = threadIdx.x; i < NB; i += NT) cnt[i] = 0;
             __syncthreads();
-            if (high >= low) atomicAdd(&cnt[bin_of<KIND, NB>(s, high)], 1u);
+            if (high >= low) lds_add(cnt + bin_of<KIND, NB>(s, high), 1u);
             __syncthreads();
             listed = select_bin<NT, NB, false>(cnt, nullptr, (u64)p.top_k, sm, &hit, &at) && collect(at.bin);
         }
@@ -801,70 +843,75 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     if (by_k && !slow) {
         keys_of_bin<KIND, NB>(s, at.bin, lowest, &klo, &khi);
     } else if (!by_k && by_p) {
-        // a histogram of weights over the steps that they were worked out from, 32 to a factor of two
-        static_assert(NB >= 256, "53 factors of two, or 5 steps each");
+        // a histogram of weights over the steps that they were worked out from, 32 to a factor of two (of small ones 16, 4)
         constexpr int shift = (NP > 256 ? 10 : 8) - (NB >= 2048 ? 5 : NB >= 1024 ? 4 : 2);
+        static_assert((kTopStep<NP> >> shift) < NB, "");
         const float from = fmaxf(low, s.low_w);
         for (int i = threadIdx.x; i < NB; i += NT) wt[i] = 0;
         __syncthreads();
-        for (u32 j = threadIdx.x; j < row.vecs; j += NT * UN) {
-            float v[UN][4];
+        walk<KIND, NT, UN>(row, 0, row.vecs, [s, tables, from, wt](const float (&v)[4], u32) {
+            u64 w[4];
+            u32 n[4];
 #pragma unroll
-            for (int u = 0; u < UN; ++u) load4<KIND>(row, j + u * NT, v[u]);
+            for (int i = 0; i < 4; ++i) w[i] = weight_of(s, tables, v[i], &n[i]);
+            side_by_side(w);
 #pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                u64 w[4];
-                u32 n[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = weight_of(s, tables, v[u][i], &n[i]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (v[u][i] >= from) atomicAdd(&wt[min(n[i] >> shift, (u32)(NB - 1))], w[i]);
-            }
-        }
+            for (int i = 0; i < 4; ++i)
+                if (v[i] >= from) lds_add(wt + (n[i] >> shift), w[i]);
+        });
         __syncthreads();
-        (void)select_bin<NT, NB, true>(nullptr, wt, (u64)__float_as_uint(p.top_p), sm, &hit, &at, &mass);
+        (void)select_bin<NT, NB, true, true>(nullptr, wt, (u64)__float_as_uint(p.top_p), sm, &hit, &at, &mass);
+        const u32 b = NB - 1 - at.bin;
         auto bin = [&](u32 k) -> u32 {
             u32 n;
             (void)weight_of(s, tables, value_of<KIND>(k), &n);
-            return min(n >> shift, (u32)(NB - 1));
+            return n >> shift;
         };
-        klo = first_key(key_of<KIND>(from), kmax, [&](u32 k) { return bin(k) <= at.bin; });
-        khi = at.bin == 0 ? kmax : first_key(klo, kmax, [&](u32 k) { return bin(k) < at.bin; }) - 1u;
+        const u32 lowest_w = key_of<KIND>(from);
+        klo = first_key(lowest_w, kmax, [&](u32 k) { return bin(k) >= b; });
+        khi = bin(kmax) == b ? kmax : first_key(klo, kmax, [&](u32 k) { return bin(k) > b; }) - 1u;
     }
     if ((by_k || by_p) && !slow) {
         // what lies above the bin is kept, what lies in it decides: the chunks' sums of the ones, a list of the others
         const float from = value_of<KIND>(klo), to = value_of<KIND>(khi);
+        // a wavefront's kept values are gathered in the lower histogram's place: their weights take fewer rounds then
+        constexpr u32 room = 4 * NB / (NT / 64);
+        static_assert(room >= 512, "a step's values fit behind another's");
+        float* const kept_v = (float*)lw + wave * room;
         for (u32 c = wave; c < nchunks; c += NT / 64) {
             float v[STEPS][4];
-#pragma unroll
-            for (int it = 0; it < STEPS; ++it) load4<KIND>(row, c * 64 * STEPS + it * 64u + lane, v[it]);
+            load_chunk<KIND, STEPS>(row, c * 64 * STEPS, lane, v);
+            u32 num = 0, kept = 0;
             u64 sum = 0;
-            u32 num = 0;
 #pragma unroll
             for (int it = 0; it < STEPS; ++it) {
                 const float top = fmaxf(fmaxf(v[it][0], v[it][1]), fmaxf(v[it][2], v[it][3]));
                 if (__ballot(top >= from) == 0) continue;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i) {
+                    const u64 above = __ballot(v[it][i] > to);
+                    if (v[it][i] > to) kept_v[num + __popcll(above & ((1ull << lane) - 1))] = v[it][i];
+                    num += (u32)__popcll(above);
                     if (v[it][i] >= from && v[it][i] <= to) {
-                        const u32 slot = atomicAdd(&list_n, 1u);
+                        const u32 slot = lds_add(&list_n, 1u);
                         if (slot < NB) le[slot] = (u64)~key_of<KIND>(v[it][i]) << 32 | (4 * (c * 64 * STEPS + it * 64u + lane) - row.skew + i);
                     }
-                if (__ballot(top > to) == 0) continue;
-                u64 w[4];
-                u32 unused;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = weight_of(s, tables, v[it][i], &unused);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    num += v[it][i] > to;
-                    sum += v[it][i] > to && v[it][i] >= s.low_w ? w[i] : 0;
                 }
+                if (it + 1 < STEPS && num <= room - 256) continue;
+                __threadfence_block();
+                for (u32 k = lane; k < num; k += 64) sum += weight(s, tables, kept_v[k]);
+                __threadfence_block();
+                kept += num;
+                num = 0;
             }
-            num = wave_sum(num);
+            if (num > 0) {                  // (the last steps had nothing to add)
+                __threadfence_block();
+                for (u32 k = lane; k < num; k += 64) sum += weight(s, tables, kept_v[k]);
+                __threadfence_block();
+                kept += num;
+            }
             sum = wave_sum(sum);
-            if (lane == 0) { chunk_n[c] = num; chunk_w[c] = sum; }
+            if (lane == 0) { chunk_n[c] = kept; chunk_w[c] = sum; }
         }
         __syncthreads();
         u32 n = list_n;
@@ -879,8 +926,8 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
                 const u32 k = threadIdx.x * per + i;
                 if (k >= n) continue;
                 const u32 c = ((u32)le[k] + row.skew) / (256 * STEPS);
-                atomicAdd(&chunk_n[c], 1u);
-                atomicAdd(&chunk_w[c], w[i]);
+                lds_add(chunk_n + c, 1u);
+                lds_add(chunk_w + c, w[i]);
             }
             summed = true;
         } else {
@@ -1062,7 +1109,7 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
 // again from the one before and its histogram; the row's first one writes it down.  Steps whose cut is known already end
 // at once.
 constexpr int kLongBins = 2048, kLongThreads = 256, kLongSteps = 4, kLongChunk = 64 * kLongSteps * 4;
-template <int KIND> using LongTables = Tables<KIND, kPowers<kLongThreads>>;
+template <int KIND> using LongTables = Tables<KIND, 1024>;
 constexpr int kKeySteps = 3;                       // 11 bits of a key each
 constexpr int kLevels = 1 + 2 * kKeySteps;         // distances; keys for top-k; keys for top-p
 
@@ -1123,15 +1170,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_max(c
     u32 j0, j1;
     float high = kMasked<KIND>;
     part_of<KIND>(row, g, part, &j0, &j1);
-    for (u32 j = j0 + threadIdx.x; j < j1; j += 4 * kLongThreads) {
-        float v[4][4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) load4<KIND>(row, min(j + u * kLongThreads, j1 - 1), v[u]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) high = fmaxf(high, v[u][i]);
-    }
+    walk<KIND, kLongThreads, 4>(row, j0, j1, [&high](const float (&v)[4], u32) { high = fmaxf(fmaxf(high, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])); });
     const u32 kmax = block_max<kLongThreads>(key_of<KIND>(high), sm);
     if (threadIdx.x == 0) g.pmax[r * g.parts + part] = kmax;
     // the row's histograms start at zero
@@ -1151,16 +1190,9 @@ template <int KIND> __device__ __forceinline__ void long_histogram(const Row& ro
     __syncthreads();
     const int shift = key_shift<kLongBins>(khi - klo);
     const float low = value_of<KIND>(klo), high = value_of<KIND>(khi);
-    for (u32 j = j0 + threadIdx.x; j < j1; j += 4 * kLongThreads) {
-        float v[4][4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (j + u * kLongThreads < j1) load4<KIND>(row, j + u * kLongThreads, v[u]);
-            else for (int i = 0; i < 4; ++i) v[u][i] = kMasked<KIND>;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) add4<KIND, kLongBins>(s, tables, v[u], first, true, weights, low, high, khi, shift, wt, cnt);
-    }
+    walk<KIND, kLongThreads, 4>(row, j0, j1, [=](const float (&v)[4], u32) {
+        add4<KIND, kLongBins>(s, tables, v, first, true, weights, low, high, khi, shift, wt, cnt);
+    });
     __syncthreads();
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) {
         if (cnt[i]) {
@@ -1190,7 +1222,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first
     st.kmax = kmax;
     st.lowest = kLowest<KIND>;
     if (st.ok) {
-        const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+        const Scale s = scale_of<KIND, kLongBins, 1024>(tables, kmax, p.t > 0.f ? p.t : 1.f, a.bits);
         if (p.min_p > 0.f && p.t > 0.f)
             st.lowest = first_key(st.lowest, kmax, [&](u32 k) { return weight64<KIND>(s, value_of<KIND>(k)) >= (double)p.min_p; });
         st.cut = Cut{value_of<KIND>(p.t > 0.f ? st.lowest : kmax), kAll};
@@ -1282,7 +1314,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(
     const Params p = params_of(a, r);
     LongState st = g.state[r * kLevels + prev];
     if (st.ok) {
-        const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+        const Scale s = scale_of<KIND, kLongBins, 1024>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
         long_advance<KIND>(a, p, s, tables, g, r, prev, sm, &hit, &st);
         if (level == 1 && by_top_k(a, p)) long_begin<KIND>(a, p, s, tables, g, r, 1, sm, &hit, &st);
         if (level == 1 + kKeySteps && by_top_p(p)) long_begin<KIND>(a, p, s, tables, g, r, 2, sm, &hit, &st);
@@ -1311,14 +1343,13 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     const Params p = params_of(a, r);
     LongState st = g.state[r * kLevels + prev];
     if (!st.ok) return;
-    const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    const Scale s = scale_of<KIND, kLongBins, 1024>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_advance<KIND>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     const u32 lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const u32 c1 = min((part + 1) * g.chunks_per_part, g.chunks);
     for (u32 c = part * g.chunks_per_part + wave; c < c1; c += kLongThreads / 64) {
         float v[kLongSteps][4];
-#pragma unroll
-        for (int it = 0; it < kLongSteps; ++it) load4<KIND>(row, c * 64 * kLongSteps + it * 64u + lane, v[it]);
+        load_chunk<KIND, kLongSteps>(row, c * 64 * kLongSteps, lane, v);
         u64 w = 0;
         u32 n = 0;
 #pragma unroll
@@ -1383,7 +1414,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
         if (threadIdx.x == 0) g.state[r * kLevels + kLevels - 1] = st;
         return;
     }
-    const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    const Scale s = scale_of<KIND, kLongBins, 1024>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_advance<KIND, 1024>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     u64* cw = g.chunk_w + r * g.chunks;
     const u32* cn = g.chunk_n + r * g.chunks;
@@ -1441,7 +1472,7 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
     }
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
-    const Scale s = scale_of<KIND, kLongBins, kPowers<kLongThreads>>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
+    const Scale s = scale_of<KIND, kLongBins, 1024>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_shot<KIND>(a, row, s, tables, st.cut, g.chunk_w + r * g.chunks, g.chunks, at, lane);
 }
 

@@ -48,6 +48,10 @@ __device__ __forceinline__ double uniform(double v) { return __longlong_as_doubl
 template <class T> using in_global = const __attribute__((address_space(1))) T;
 template <class T> using in_lds = const __attribute__((address_space(3))) T;
 
+template <class T> __device__ __forceinline__ T lds_add(T* p, T v) {
+    return __hip_atomic_fetch_add((__attribute__((address_space(3))) T*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
 template <class T> __device__ __forceinline__ T last_lane(T v);
 template <> __device__ __forceinline__ unsigned last_lane(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)v, 63); }
 template <> __device__ __forceinline__ unsigned long long last_lane(unsigned long long v) {
