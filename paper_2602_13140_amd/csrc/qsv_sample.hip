@@ -647,7 +647,7 @@ template <> struct Shape<256> { static constexpr int bins = 1024, chunks = 36, s
 template <> struct Shape<1024> { static constexpr int bins = 2048, chunks = 264, steps = 4; static constexpr u32 most = 262144; };
 
 template <int KIND, int NT>
-__global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_sample_row(const SampleArgs a) {
     constexpr int NB = Shape<NT>::bins, NC = Shape<NT>::chunks, STEPS = Shape<NT>::steps, LIST = 2 * NB;
     constexpr int UN = NT == 1024 ? 4 : 2;  // vectors of a thread on their way at once
     // two histograms; or: a list to be sorted, its entries and their weights, or values on their way; or: a list to be searched
@@ -703,17 +703,6 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
     u64* const le = wt;                     // of a list to be sorted: entries, and weights
     u64* const lw = wt + NB;
 
-    // a histogram (counts, weights) of the values with keys in klo .. khi: the first one over distances, later ones over keys
-    auto histogram = [&](int h, bool first, bool counts, bool weights, u32 klo, u32 khi) {
-        for (int i = threadIdx.x; i < NB; i += NT) { cnt[h * NB + i] = 0; wt[h * NB + i] = 0; }
-        __syncthreads();
-        const int shift = key_shift<NB>(khi - klo);
-        const float from = value_of<KIND>(klo), to = value_of<KIND>(khi);
-        walk<KIND, NT, UN>(row, 0, row.vecs, [=](const float (&v)[4], u32) {
-            add4<KIND, NB>(s, tables, v, first, counts, weights, from, to, khi, shift, wt + h * NB, cnt + h * NB);
-        });
-        __syncthreads();
-    };
     // the list in order, its entries' weights; the sum of the weights before each thread's entries
     constexpr int per = NB / NT;
     auto ordered = [&](u32 n, u64 (&w)[per]) -> u64 {
@@ -779,7 +768,14 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
             listed = select_bin<NT, NB, false>(cnt, nullptr, (u64)p.top_k, sm, &hit, &at) && collect(at.bin);
         }
         if (!listed) {
-            histogram(0, true, true, false, lowest, kmax);
+            for (int i = threadIdx.x; i < NB; i += NT) cnt[i] = 0;
+            __syncthreads();
+            walk<KIND, NT, UN>(row, 0, row.vecs, [s, low, cnt](const float (&v)[4], u32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v[i] >= low) lds_add(cnt + bin_of<KIND, NB>(s, v[i]), 1u);
+            });
+            __syncthreads();
             by_k = select_bin<NT, NB, false>(cnt, nullptr, (u64)p.top_k, sm, &hit, &at);
             listed = by_k && at.count + at.own <= NB && collect(at.bin);
             slow = by_k && (by_p || at.own > NB);
@@ -936,51 +932,59 @@ __global__ __launch_bounds__(NT) void k_sample_row(const SampleArgs a) {
         __syncthreads();
     }
     if (slow) {
-        // bins of keys, narrower each time, down to the cut's own
-        histogram(0, true, true, by_p, lowest, kmax);
-        bool have_mass = false;
-        auto narrow = [&](auto byw, u64 target, Find* f) -> bool {
-            constexpr bool BYW = decltype(byw)::value;
-            Hit in;
-            if (!select_bin<NT, NB, BYW>(cnt, by_p ? wt : nullptr, target, sm, &hit, &in)) return false;
-            keys_of_bin<KIND, NB>(s, in.bin, lowest, &f->klo, &f->khi);
-            f->done = 0;
-            f->ne = 0;
-            f->target = target;
-            f->count = in.count;
-            f->weight = in.weight;
-            settle<KIND, BYW>(s, tables, *f);
-            while (!f->done) {
-                histogram(1, false, true, by_p, f->klo, f->khi);
-                if (!select_bin<NT, NB, BYW>(cnt + NB, by_p ? wt + NB : nullptr, f->target - (BYW ? f->weight : f->count), sm, &hit, &in))
-                    return false;          // (the row was written to while it was read)
-                const int shift = key_shift<NB>(f->khi - f->klo);
-                const u32 top = f->khi - (in.bin << shift);
-                f->klo = top - f->klo < (1u << shift) ? f->klo : top - (1u << shift) + 1u;
-                f->khi = top;
-                f->count += in.count;
-                f->weight += in.weight;
-                settle<KIND, BYW>(s, tables, *f);
-            }
-            return true;
-        };
-        Find f;
+        // bins of keys, narrower each time, down to the cut's own: for top-k by counts, then for top-p by weights
         u32 ne = kAll;
-        if (by_k && narrow(ByCount{}, (u64)p.top_k, &f)) {
+        bool have_mass = false;
+        auto count = [=](u32 h, bool first, u32 lo, u32 hi) {
+            for (int i = threadIdx.x; i < NB; i += NT) { cnt[h + i] = 0; wt[h + i] = 0; }
+            __syncthreads();
+            const int shift = key_shift<NB>(hi - lo);
+            const float from = value_of<KIND>(lo), to = value_of<KIND>(hi);
+            walk<KIND, NT, 1>(row, 0, row.vecs, [=](const float (&v)[4], u32) {
+                add4<KIND, NB>(s, tables, v, first, true, by_p, from, to, hi, shift, wt + h, cnt + h);
+            });
+            __syncthreads();
+        };
+        count(0, true, lowest, kmax);
+        for (int stage = by_k ? 0 : 1; stage < (by_p ? 2 : 1); ++stage) {
+            u64 target = (u64)p.top_k;
+            if (stage == 1) {
+                if (!have_mass) {
+                    u64 sum = 0;
+                    for (int i = threadIdx.x; i < NB; i += NT) sum += wt[i];
+                    (void)block_scan<NT>(sum, sm, &mass);
+                }
+                target = mass_of(p.top_p, mass);
+            }
+            Find f{};
+            f.target = target;
+            for (u32 h = 0;; h = NB) {
+                Hit in;
+                const u64* const w = by_p ? wt + h : nullptr;
+                if (!(stage == 0 ? select_bin<NT, NB, false>(cnt + h, w, target - f.count, sm, &hit, &in)
+                                 : select_bin<NT, NB, true>(cnt + h, w, target - f.weight, sm, &hit, &in)))
+                    break;                 // (the row was written to while it was read)
+                if (h == 0) {
+                    keys_of_bin<KIND, NB>(s, in.bin, lowest, &f.klo, &f.khi);
+                } else {
+                    const int shift = key_shift<NB>(f.khi - f.klo);
+                    const u32 top = f.khi - (in.bin << shift);
+                    f.klo = top - f.klo < (1u << shift) ? f.klo : top - (1u << shift) + 1u;
+                    f.khi = top;
+                }
+                f.count += in.count;
+                f.weight += in.weight;
+                if (stage == 0) settle<KIND, false>(s, tables, f);
+                else settle<KIND, true>(s, tables, f);
+                if (f.done) break;
+                count(NB, false, f.klo, f.khi);
+            }
+            if (!f.done) continue;
             cut.v = value_of<KIND>(f.klo);
             ne = f.ne;
-            if (by_p) mass = f.weight + (u64)f.ne * weight(s, tables, value_of<KIND>(f.klo));
-            have_mass = true;
-        }
-        if (by_p) {
-            if (!have_mass) {
-                u64 sum = 0;
-                for (int i = threadIdx.x; i < NB; i += NT) sum += wt[i];
-                (void)block_scan<NT>(sum, sm, &mass);
-            }
-            if (narrow(ByWeight{}, mass_of(p.top_p, mass), &f)) {
-                cut.v = value_of<KIND>(f.klo);
-                ne = f.ne;
+            if (stage == 0 && by_p) {
+                mass = f.weight + (u64)f.ne * weight(s, tables, cut.v);
+                have_mass = true;
             }
         }
         // the index of the last that stays of what equals the key
