@@ -620,11 +620,12 @@ __device__ __forceinline__ void side_by_side(u64 (&w)[4]) {
 }
 
 // Four values of a lane into a histogram (counts, weights) of those in from .. to: over distances (first), or over keys down
-// from khi.  The weights of all four are worked out side by side, then what is in the range is added.
+// from khi.  The weights of all four are worked out side by side, then what is in the range is added; over keys few are, and
+// only theirs are worked out.
 template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const Scale& s, const Tables<KIND, NP>* tables, const float (&v)[4], bool first, bool counts, bool weights, float from, float to, u32 khi, int shift, u64* wt, u32* cnt) {
-    u64 w[4];
+    u64 w[4] = {0, 0, 0, 0};
     u32 b[4];
-    if (weights) {
+    if (weights && first) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = weight(s, tables, v[i]);
         side_by_side(w);
@@ -635,7 +636,7 @@ template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const S
     for (int i = 0; i < 4; ++i)
         if (v[i] >= from && v[i] <= to) {
             if (counts) lds_add(cnt + b[i], 1u);
-            if (weights) lds_add(wt + b[i], w[i]);
+            if (weights) lds_add(wt + b[i], first ? w[i] : weight(s, tables, v[i]));
         }
 }
 
@@ -670,6 +671,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
     const Params p = params_of(a, r);
     const u32 nchunks = (row.vecs + 64 * STEPS - 1) / (64 * STEPS);
 
+    // the first shots' uniforms are on their way while the row is read: a thread's, and a wavefront's
+    const double* const uniforms = a.uniforms + r * a.shots;
+    const double u_thread = threadIdx.x < (u64)a.shots ? uniforms[threadIdx.x] : 0.0;
+    const double u_wave = wave < (u64)a.shots ? uniforms[wave] : 0.0;
     float high = kMasked<KIND>;             // of the thread's values
     walk<KIND, NT, UN>(row, 0, row.vecs, [&high](const float (&v)[4], u32) { high = fmaxf(fmaxf(high, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])); });
     fill_tables<KIND, NT>(&lds_tables, a.bits, p.t == 1.f);
@@ -690,7 +695,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
         });
         first = ~block_max<NT>(first, sm);
         for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
-            const double u = a.uniforms[r * a.shots + i];
+            const double u = i < NT ? u_thread : uniforms[i];
             write_shot(a, r * a.shots + i, u >= 0.0 && u < 1.0 ? (long long)first : -1, 1, 1);
         }
         if (threadIdx.x == 0 && a.kept) a.kept[r] = 1;
@@ -783,45 +788,79 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
     }
     if (listed) {
         // few outcomes down to the bin: in order they give the cut, and by index the draw
-        u64 w[per];
         u32 n = min(list_n, (u32)NB);      // (more only if the row was written to meanwhile)
-        const u64 before = ordered(n, w);
-        n = min(n, (u32)p.top_k);
-        if (by_p) {
-            u64 mass = 0;
+        u64 total;
+        if (n <= 64) {
+            // a wavefront's registers hold them: ranks by reading every lane, no barriers (32768 scores, 22 left: 0.7 us less of a call)
+            if (wave == 0) {
+                u64 e = lane < n ? le[lane] : ~0ull;
+                u32 rank = 0;
+                for (u32 i = 0; i < n; ++i) rank += lane_of(e, i) < e;
+                if (lane < n) le[rank] = e;
+                __threadfence_block();
+                e = lane < n ? le[lane] : ~0ull;
+                n = min(n, (u32)p.top_k);
+                u64 w = lane < n ? weight(s, tables, value_of<KIND>(~(u32)(e >> 32))) : 0;
+                if (by_p) {
+                    const u64 incl = wave_scan(w);
+                    const u64 border = mass_of(p.top_p, last_lane(incl));
+                    n = (u32)__popcll(__ballot(lane < n && (lane == 0 || incl - w < border)));
+                }
+                const u32 idx = (u32)e;
+                rank = 0;
+                for (u32 i = 0; i < n; ++i) rank += lane_of(idx, i) < idx;
+                if (lane < n) {
+                    le[rank] = (u64)idx << 32;
+                    lw[rank] = w;
+                }
+                __threadfence_block();
+                w = wave_scan(lane < n ? lw[lane] : 0ull);
+                if (lane < n) lw[lane] = w;
+                if (lane == 0) found = n;
+            }
+            __syncthreads();
+            n = uniform(found);
+            total = lw[n - 1];
+        } else {
+            u64 w[per];
+            const u64 before = ordered(n, w);
+            n = min(n, (u32)p.top_k);
+            if (by_p) {
+                u64 mass = 0;
 #pragma unroll
-            for (int i = 0; i < per; ++i) if (threadIdx.x * per + i < n) mass += w[i];
-            u64 all;
-            (void)block_scan<NT>(mass, sm, &all);
-            n = reach(w, before, n, 0, mass_of(p.top_p, all));
+                for (int i = 0; i < per; ++i) if (threadIdx.x * per + i < n) mass += w[i];
+                u64 all;
+                (void)block_scan<NT>(mass, sm, &all);
+                n = reach(w, before, n, 0, mass_of(p.top_p, all));
+            }
+            u64 e[per];
+#pragma unroll
+            for (int i = 0; i < per; ++i) {
+                const u32 k = threadIdx.x * per + i;
+                lw[k] = w[i];
+                e[i] = k < n ? (le[k] & 0xffffffffull) << 32 | k : 0;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < per; ++i) if (threadIdx.x * per + i < n) le[threadIdx.x * per + i] = e[i];
+            __syncthreads();
+            sort_lds<NT>(le, n);
+            u64 sum = 0;
+#pragma unroll
+            for (int i = 0; i < per; ++i) {
+                const u32 k = threadIdx.x * per + i;
+                w[i] = k < n ? lw[(u32)le[k]] : 0;
+                sum += w[i];
+            }
+            u64 run = block_scan<NT>(sum, sm, &total);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < per; ++i) { run += w[i]; lw[threadIdx.x * per + i] = run; }
+            __syncthreads();
         }
-        u64 e[per];
-#pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const u32 k = threadIdx.x * per + i;
-            lw[k] = w[i];
-            e[i] = k < n ? (le[k] & 0xffffffffull) << 32 | k : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < per; ++i) if (threadIdx.x * per + i < n) le[threadIdx.x * per + i] = e[i];
-        __syncthreads();
-        sort_lds<NT>(le, n);
-        u64 sum = 0, total;
-#pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const u32 k = threadIdx.x * per + i;
-            w[i] = k < n ? lw[(u32)le[k]] : 0;
-            sum += w[i];
-        }
-        u64 run = block_scan<NT>(sum, sm, &total);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < per; ++i) { run += w[i]; lw[threadIdx.x * per + i] = run; }
-        __syncthreads();
         if (threadIdx.x == 0 && a.kept) a.kept[r] = (int)n;
         for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
-            const double u = a.uniforms[r * a.shots + i];
+            const double u = i < NT ? u_thread : uniforms[i];
             if (!(u >= 0.0 && u < 1.0)) { write_shot(a, r * a.shots + i, -1, 0, 1); continue; }
             const u64 t = draw_at(u, total);
             u32 lo = 0, len = n;                           // the first with a sum above t is in lo .. lo + len - 1
@@ -1077,7 +1116,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
         }
         __syncthreads();
         for (u64 i = threadIdx.x; i < (u64)a.shots; i += NT) {
-            const double u = a.uniforms[r * a.shots + i];
+            const double u = i < NT ? u_thread : uniforms[i];
             if (!(u >= 0.0 && u < 1.0)) { write_shot(a, r * a.shots + i, -1, 0, 1); continue; }
             const u64 t = draw_at(u, total);
             u32 lo = 0, len = (u32)n_kept;
@@ -1091,7 +1130,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
         return;
     }
     for (u64 i = wave; i < (u64)a.shots; i += NT / 64) {
-        const double u = a.uniforms[r * a.shots + i];
+        const double u = i < NT / 64 ? u_wave : uniforms[i];
         long long k = -1;
         u64 w = 0;
         if (u >= 0.0 && u < 1.0) {
@@ -1112,7 +1151,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
 // highest keys, histograms that all parts add to, the state of the search.  Every workgroup of a step works the state out
 // again from the one before and its histogram; the row's first one writes it down.  Steps whose cut is known already end
 // at once.
-constexpr int kLongBins = 2048, kLongThreads = 256, kLongSteps = 4, kLongChunk = 64 * kLongSteps * 4;
+constexpr int kLongBins = 2048, kLongThreads = 1024, kLongSteps = 4, kLongChunk = 64 * kLongSteps * 4;
 template <int KIND> using LongTables = Tables<KIND, 1024>;
 constexpr int kKeySteps = 3;                       // 11 bits of a key each
 constexpr int kLevels = 1 + 2 * kKeySteps;         // distances; keys for top-k; keys for top-p
@@ -1132,19 +1171,22 @@ struct Long {
     u64* wt;               // [rows][kLevels][kLongBins]
     u32* cnt;              // [rows][kLevels][kLongBins]
     LongState* state;      // [rows][kLevels]
-    u64* chunk_w;          // [rows][chunks]
-    u32* chunk_n;          // [rows][chunks]
+    u64* chunk_w;          // [rows][chunks]: weights above the cut's value
+    u32* chunk_n;          // [rows][chunks]: numbers above it (low half) and of those that equal it
+    u64* part_w;           // [rows][parts]: weights above the cut's value; then kept ones up to the part's end
+    u64* part_n;           // [rows][parts]: numbers, halves of 32 bits; then equals before the part
 };
 
 __host__ __device__ inline u64 long_chunks(int64_t cols) { return ((u64)cols + 3 + kLongChunk - 1) / kLongChunk; }
 
-// Parts of about four chunks (a wavefront each), as many as give the chip eight workgroups a CU.
+// Parts of a chunk for each wavefront or more, and a workgroup or two a CU: every part adds its histogram to the row's, a
+// few hundred bins at the same addresses (24 qubits: 1024 parts of 256 threads 47 us, 256 of 1024 threads 37).
 __host__ inline u32 long_parts(int64_t rows, int64_t cols) {
-    const u64 want = (long_chunks(cols) + 3) / 4, most = std::max<u64>(1, 2048 / (u64)rows);
-    return (u32)std::min(std::min(want, most), (u64)1024);
+    const u64 want = (long_chunks(cols) + kLongThreads / 64 - 1) / (kLongThreads / 64), most = std::max<u64>(1, 512 / (u64)rows);
+    return (u32)std::min(std::min(want, most), (u64)256);
 }
 
-struct LongSizes { size_t pmax, wt, cnt, state, chunk_w, chunk_n, all; };
+struct LongSizes { size_t pmax, wt, cnt, state, chunk_w, chunk_n, part, all; };
 __host__ inline LongSizes long_sizes(int64_t rows, int64_t cols) {
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
     LongSizes s;
@@ -1155,7 +1197,8 @@ __host__ inline LongSizes long_sizes(int64_t rows, int64_t cols) {
     s.state = up(n * kLevels * sizeof(LongState));
     s.chunk_w = up(n * chunks * 8);
     s.chunk_n = up(n * chunks * 4);
-    s.all = s.pmax + s.wt + s.cnt + s.state + s.chunk_w + s.chunk_n;
+    s.part = up(n * long_parts(rows, cols) * 8);
+    s.all = s.pmax + s.wt + s.cnt + s.state + s.chunk_w + s.chunk_n + 2 * s.part;
     return s;
 }
 
@@ -1189,20 +1232,18 @@ __device__ __forceinline__ bool by_top_k(const SampleArgs& a, const Params& p) {
 __device__ __forceinline__ bool by_top_p(const Params& p) { return p.t > 0.f && p.top_p < 1.f; }
 
 // The histogram of the values of vectors j0 .. j1 with keys in klo .. khi, added to the row's.
-template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool weights, u32 klo, u32 khi, const LongTables<KIND>* tables, u64* wt, u32* cnt, u64* gw, u32* gc) {
+template <int KIND> __device__ __forceinline__ void long_histogram(const Row& row, const Scale& s, u32 j0, u32 j1, bool first, bool counts, bool weights, u32 klo, u32 khi, const LongTables<KIND>* tables, u64* wt, u32* cnt, u64* gw, u32* gc) {
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) { cnt[i] = 0; wt[i] = 0; }
     __syncthreads();
     const int shift = key_shift<kLongBins>(khi - klo);
     const float low = value_of<KIND>(klo), high = value_of<KIND>(khi);
     walk<KIND, kLongThreads, 4>(row, j0, j1, [=](const float (&v)[4], u32) {
-        add4<KIND, kLongBins>(s, tables, v, first, true, weights, low, high, khi, shift, wt, cnt);
+        add4<KIND, kLongBins>(s, tables, v, first, counts, weights, low, high, khi, shift, wt, cnt);
     });
     __syncthreads();
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) {
-        if (cnt[i]) {
-            atomicAdd(&gc[i], cnt[i]);
-            if (weights && wt[i]) atomicAdd(&gw[i], wt[i]);
-        }
+        if (counts && cnt[i]) atomicAdd(&gc[i], cnt[i]);
+        if (weights && wt[i]) atomicAdd(&gw[i], wt[i]);
     }
 }
 
@@ -1234,7 +1275,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_first
         if (by_top_k(a, p) || by_top_p(p)) {
             u32 j0, j1;
             part_of<KIND>(row, g, part, &j0, &j1);
-            long_histogram<KIND>(row, s, j0, j1, true, by_top_p(p), st.lowest, kmax, tables, wt, cnt, g.wt + r * (kLevels * kLongBins), g.cnt + r * (kLevels * kLongBins));
+            long_histogram<KIND>(row, s, j0, j1, true, by_top_k(a, p), by_top_p(p), st.lowest, kmax, tables, wt, cnt, g.wt + r * (kLevels * kLongBins), g.cnt + r * (kLevels * kLongBins));
         }
     }
     if (part == 0 && threadIdx.x == 0) g.state[r * kLevels] = st;
@@ -1326,7 +1367,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_keys(
             u32 j0, j1;
             part_of<KIND>(row, g, part, &j0, &j1);
             const size_t at = (r * kLevels + level) * kLongBins;
-            long_histogram<KIND>(row, s, j0, j1, false, by_top_p(p), st.f.klo, st.f.khi, tables, wt, cnt, g.wt + at, g.cnt + at);
+            long_histogram<KIND>(row, s, j0, j1, false, st.stage == 1, by_top_p(p), st.f.klo, st.f.khi, tables, wt, cnt, g.wt + at, g.cnt + at);
         }
     }
     if (part == 0 && threadIdx.x == 0) g.state[r * kLevels + level] = st;
@@ -1351,6 +1392,7 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
     long_advance<KIND>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     const u32 lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const u32 c1 = min((part + 1) * g.chunks_per_part, g.chunks);
+    u64 part_w = 0, part_n = 0;
     for (u32 c = part * g.chunks_per_part + wave; c < c1; c += kLongThreads / 64) {
         float v[kLongSteps][4];
         load_chunk<KIND, kLongSteps>(row, c * 64 * kLongSteps, lane, v);
@@ -1366,36 +1408,65 @@ template <int KIND> __global__ __launch_bounds__(kLongThreads) void k_long_sums(
             }
         n = wave_sum(n);
         w = wave_sum(w);
+        part_w += w;
+        part_n += (u64)(n >> 16) << 32 | (n & 0xffffu);
         if (lane == 0) {
             g.chunk_w[r * g.chunks + c] = w;
             g.chunk_n[r * g.chunks + c] = n;
         }
     }
+    u64 sum_w, sum_n;
+    (void)block_scan<kLongThreads>(lane == 0 ? part_w : 0, sm, &sum_w);
+    (void)block_scan<kLongThreads>(lane == 0 ? part_n : 0, sm, &sum_n);
+    if (threadIdx.x == 0) {
+        g.part_w[r * g.parts + part] = sum_w;
+        g.part_n[r * g.parts + part] = sum_n;
+    }
 }
 
-template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const LongTables<KIND>* tables, const Cut& cut, const u64* cw, u32 chunks, u64 at, u32 lane) {
+// A wavefront's search of the row's shot number `at`: its part by the parts' sums, its chunk by those of the part's.
+template <int KIND> __device__ __forceinline__ void long_shot(const SampleArgs& a, const Row& row, const Scale& s, const LongTables<KIND>* tables, const LongState& st, const Long& g, u64 r, u64 w_cut, u64 at, u32 lane) {
+    const u64* pw = g.part_w + r * g.parts;
     const double u = a.uniforms[at];
-    const u64 total = cw[chunks - 1];
+    const u64 total = pw[g.parts - 1];
     long long k = -1;
     u64 w = 0;
     if (u >= 0.0 && u < 1.0) {
         const u64 t = draw_at(u, total);
-        u32 lo = 0, len = chunks;                  // the first chunk with a sum above t is in lo .. lo + len - 1
+        u32 lo = 0, len = g.parts;                 // the first part with a sum above t is in lo .. lo + len - 1
         while (len > 1) {
             const u32 stride = (len + 63) >> 6;
             const u32 probe = min((lane + 1) * stride, len) - 1;
-            const u64 above = __ballot(cw[lo + probe] > t);
+            const u64 above = __ballot(pw[lo + probe] > t);
             const u32 f = above ? (u32)__ffsll((long long)above) - 1u : 63u;
             const u32 off = min(f * stride, len - 1);
             lo += off;
             len = min(stride, len - off);
         }
-        k = find_in_chunk<KIND, kLongSteps>(row, s, tables, cut, lo * 64 * kLongSteps, lo ? cw[lo - 1] : 0, t, lane, &w);
+        u64 base = lo ? pw[lo - 1] : 0, eq = g.part_n[r * g.parts + lo];
+        const u32 c1 = min((lo + 1) * g.chunks_per_part, g.chunks);
+        for (u32 c0 = lo * g.chunks_per_part; c0 < c1; c0 += 64) {
+            const u32 c = c0 + lane;
+            const u32 n = c < c1 ? g.chunk_n[r * g.chunks + c] >> 16 : 0;
+            const u64 before = eq + wave_scan((u64)n) - n;
+            const u64 take = before >= st.ne ? 0 : min((u64)n, (u64)st.ne - before);
+            const u64 own = (c < c1 ? g.chunk_w[r * g.chunks + c] : 0) + take * w_cut;
+            const u64 incl = wave_scan(own);
+            const u64 above = __ballot(base + incl > t);
+            if (above) {
+                const u32 f = (u32)__ffsll((long long)above) - 1u;
+                base += lane_of(incl - own, f);
+                k = find_in_chunk<KIND, kLongSteps>(row, s, tables, st.cut, (c0 + f) * 64 * kLongSteps, base, t, lane, &w);
+                break;
+            }
+            base += last_lane(incl);
+            eq = last_lane(before + n);
+        }
     }
     if (lane == 0) write_shot(a, at, k, w, total);
 }
 
-// One workgroup a row: running sums over its chunks, the last index that stays of what equals the cut's key, and (draw) its
+// One workgroup a row: running sums over its parts, the last index that stays of what equals the cut's value, and (draw) its
 // shots.
 template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const SampleArgs a, const Long g, int prev, int draw) {
     __shared__ u64 sm[16];
@@ -1420,33 +1491,34 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     }
     const Scale s = scale_of<KIND, kLongBins, 1024>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_advance<KIND, 1024>(a, p, s, tables, g, r, prev, sm, &hit, &st);
-    u64* cw = g.chunk_w + r * g.chunks;
-    const u32* cn = g.chunk_n + r * g.chunks;
-    const u32 per = (g.chunks + 1023) / 1024;
-    const u32 c0 = min(threadIdx.x * per, g.chunks), c1 = min(c0 + per, g.chunks);
-    u64 eq = 0, eq_all, n_kept, total;
-    for (u32 c = c0; c < c1; ++c) eq += cn[c] >> 16;
-    const u64 eq_before = block_scan<1024>(eq, sm, &eq_all);
     const u64 w_cut = weight(s, tables, st.cut.v);
-    u64 run = eq_before, num = 0, w = 0;
-    for (u32 c = c0; c < c1; ++c) {
-        const u32 n = cn[c];
-        const u64 take = run >= st.ne ? 0 : min((u64)(n >> 16), (u64)st.ne - run);
-        if (run < st.ne && run + (n >> 16) >= st.ne) { found = c; rank = (u32)(st.ne - run); }
-        num += (n & 0xffffu) + take;
-        w += cw[c] + take * w_cut;
-        run += n >> 16;
+    const bool mine = threadIdx.x < g.parts;       // (1024 parts at most)
+    const u64 n = mine ? g.part_n[r * g.parts + threadIdx.x] : 0;
+    const u64 eq = n >> 32;
+    u64 eq_all, n_kept, total;
+    const u64 eq_before = block_scan<1024>(eq, sm, &eq_all);
+    const u64 take = eq_before >= st.ne ? 0 : min(eq, (u64)st.ne - eq_before);
+    (void)block_scan<1024>((n & 0xffffffffull) + take, sm, &n_kept);
+    const u64 own = (mine ? g.part_w[r * g.parts + threadIdx.x] : 0) + take * w_cut;
+    const u64 w_before = block_scan<1024>(own, sm, &total);
+    if (mine) {
+        g.part_w[r * g.parts + threadIdx.x] = w_before + own;
+        g.part_n[r * g.parts + threadIdx.x] = eq_before;
     }
-    (void)block_scan<1024>(num, sm, &n_kept);
-    u64 sum = block_scan<1024>(w, sm, &total);
-    run = eq_before;
-    for (u32 c = c0; c < c1; ++c) {
-        const u32 n = cn[c];
-        const u64 take = run >= st.ne ? 0 : min((u64)(n >> 16), (u64)st.ne - run);
-        sum += cw[c] + take * w_cut;
-        cw[c] = sum;
-        run += n >> 16;
+    // the ne-th of the equals: the thread that has its part looks through the part's chunks
+    if (eq_before < st.ne && eq_before + eq >= st.ne) {
+        u32 left = (u32)(st.ne - eq_before);
+        u32 c = threadIdx.x * g.chunks_per_part;
+        const u32 c1 = min(c + g.chunks_per_part, g.chunks);
+        for (; c + 1 < c1; ++c) {
+            const u32 k = g.chunk_n[r * g.chunks + c] >> 16;
+            if (k >= left) break;
+            left -= k;
+        }
+        found = c;
+        rank = left;
     }
+    __syncthreads();
     const u32 lane = threadIdx.x & 63;
     if (found != kAll) st.cut.idx = nth_equal<KIND, kLongSteps>(row, st.cut.v, rank, found * 64 * kLongSteps, lane);
     if (threadIdx.x == 0) {
@@ -1457,7 +1529,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     __threadfence_block();
     __syncthreads();
     for (u64 i = threadIdx.x >> 6; i < (u64)a.shots; i += 16)
-        long_shot<KIND>(a, row, s, tables, st.cut, cw, g.chunks, r * a.shots + i, lane);
+        long_shot<KIND>(a, row, s, tables, st, g, r, w_cut, r * a.shots + i, lane);
 }
 
 template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const SampleArgs a, const Long g) {
@@ -1477,7 +1549,7 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
     const Scale s = scale_of<KIND, kLongBins, 1024>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
-    long_shot<KIND>(a, row, s, tables, st.cut, g.chunk_w + r * g.chunks, g.chunks, at, lane);
+    long_shot<KIND>(a, row, s, tables, st, g, r, weight(s, tables, st.cut.v), at, lane);
 }
 
 }  // namespace
@@ -1500,6 +1572,8 @@ template <int KIND> static hipError_t launch_long(const SampleArgs& a, char* scr
     g.levels = a.top_k || a.top_p;
     g.wt = (u64*)scratch; scratch += z.wt;
     g.chunk_w = (u64*)scratch; scratch += z.chunk_w;
+    g.part_w = (u64*)scratch; scratch += z.part;
+    g.part_n = (u64*)scratch; scratch += z.part;
     g.state = (LongState*)scratch; scratch += z.state;
     g.pmax = (u32*)scratch; scratch += z.pmax;
     g.cnt = (u32*)scratch; scratch += z.cnt;
