@@ -194,12 +194,20 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-_TYPE_OF = {QSV_S_F32: "torch.float32", QSV_S_F16: "torch.float16", QSV_S_BF16: "torch.bfloat16", QSV_S_PROBS: "torch.float32"}
+_TYPE_OF = {QSV_S_F32: "float32", QSV_S_F16: "float16", QSV_S_BF16: "bfloat16", QSV_S_PROBS: "float32"}
+_dtypes = {}
+
+
+def _dtype(name):
+    if not _dtypes:
+        import torch
+        _dtypes.update((n, getattr(torch, n)) for n in ("float16", "bfloat16", "float32", "float64", "int32", "int64"))
+    return _dtypes[name]
 
 
 def _rows(t, kind):
     """Rows of scores: [rows][cols] of the kind's type, values of a row next to each other, any row stride."""
-    assert t.is_cuda and t.dim() == 2 and str(t.dtype) == _TYPE_OF[kind] and (t.shape[1] == 1 or t.stride(1) == 1)
+    assert t.is_cuda and t.dim() == 2 and t.dtype is _dtype(_TYPE_OF[kind]) and (t.shape[1] == 1 or t.stride(1) == 1)
     return t
 
 
@@ -207,7 +215,7 @@ def _flat(t, dtype, *shape):
     """The address of a contiguous tensor of this type and shape; None stays None."""
     if t is None:
         return None
-    assert t.is_cuda and str(t.dtype) == "torch." + dtype and tuple(t.shape) == shape and t.is_contiguous(), (dtype, shape)
+    assert t.dtype is _dtype(dtype) and t.shape == shape and t.is_cuda and t.is_contiguous(), (dtype, shape)
     return t.data_ptr()
 
 

@@ -146,18 +146,22 @@ struct Taught { double q, qx; };      // sum q, sum q (t / T - norm)
 struct TeacherLds { int* idx; float *q, *z; };
 
 __device__ __forceinline__ TeacherLds teacher_lds(char* lds, int top) {
+    const int room = (top + 3) & ~3;
     TeacherLds t;
     t.idx = (int*)lds;
-    t.q = (float*)lds + top;
-    t.z = (float*)lds + 2 * top;
+    t.q = (float*)lds + room;
+    t.z = (float*)lds + 2 * room;
     return t;
 }
+
+inline size_t teacher_bytes(int top) { return (size_t)((top + 3) & ~3) * 12; }
 
 // LISTED: `row` holds the scores at the entries, in their order.
 template <int KIND, int NT, bool LISTED = false> __device__ __forceinline__ Taught teach(const TeacherArgs& a, u64 r, const char* row, u32 cols, const TeacherLds& l, double* sm) {
     const int* idx = a.idx + r * a.top;
     const float* logits = a.logits + r * a.top;
     float high = -kInf;
+    if (threadIdx.x < ((a.top + 3) & ~3) - a.top) l.idx[a.top + threadIdx.x] = -1;
     for (int j = threadIdx.x; j < a.top; j += NT) {
         const int i = idx[j];
         const bool real = i >= 0 && (u32)i < cols;
@@ -223,18 +227,26 @@ __device__ __forceinline__ Gradient gradient_of(const Taught& t, float m, double
 
 __device__ __forceinline__ float e_of(const Gradient& g, float z) { return __builtin_amdgcn_exp2f((z - g.m) * g.c); }
 
-// The places of the teacher's entries between k0 and k1, once each, whichever entries name them.
+// The places of the teacher's entries between k0 and k1, once each, whichever entries name them.  The others are looked
+// through four at a time: an entry twice is rare, and the search bound by the latency of LDS.
 template <int KIND, int NT> __device__ __forceinline__ void write_entries(const TeacherLds& l, int top, const Gradient& g, char* grad, u32 k0, u32 k1) {
+    typedef int four __attribute__((ext_vector_type(4)));
     for (int j = threadIdx.x; j < top; j += NT) {
         const int k = l.idx[j];
         if (k < 0 || (u32)k < k0 || (u32)k >= k1) continue;
-        double q = 0.0;
+        double q = (double)l.q[j];
         bool first = true;
-        for (int i = 0; i < top; ++i)
-            if (l.idx[i] == k) {
-                if (i < j) { first = false; break; }
-                q += (double)l.q[i];
-            }
+#pragma unroll 4
+        for (int i = 0; i < top; i += 4) {
+            const four x = *(const four*)(l.idx + i);
+            if (x[0] != k && x[1] != k && x[2] != k && x[3] != k) continue;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (x[u] == k && i + u != j) {
+                    if (i + u < j) first = false;
+                    q += (double)l.q[i + u];
+                }
+        }
         if (first) store_one<KIND>(grad, (u32)k, (float)((double)(e_of(g, l.z[j]) * g.scale) - q * (double)g.of_q));
     }
 }
@@ -330,17 +342,34 @@ constexpr int kPartThreads = 256, kPartVecs = 8;       // a part: 8 vectors a th
 
 struct Parts {
     u32 parts;
+    double* taught;       // [rows][2]: sum q, sum q (t / T - norm)
     float* part;          // [rows][parts][2]: maximum, sum relative to it
-    float* z;             // [rows][top]: the scores at the teacher's entries
+    float *q, *z;         // [rows][top]: of the teacher's entries, and the scores there
 };
 
+// A row's parts, and one workgroup more for its teacher (its scores are read here: the gradient may be written over them).
 template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_stats(const DistillArgs a, const Parts p) {
     constexpr int W = kPer<KIND>;
-    __shared__ double sm[16];
-    const u64 r = grid_block() / p.parts;
-    const u32 at = (u32)(grid_block() % p.parts);
+    extern __shared__ char lds[];
+    __shared__ double sm[48];
+    const u64 r = grid_block() / (p.parts + 1);
+    const u32 at = (u32)(grid_block() % (p.parts + 1));
     if (r >= (u64)a.rows) return;
     const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
+    if (at == p.parts) {
+        const int top = a.teacher.top;
+        const TeacherLds l = teacher_lds(lds, top);
+        const Taught t = teach<KIND, kPartThreads>(a.teacher, r, row, a.cols, l, sm);
+        for (int j = threadIdx.x; j < top; j += kPartThreads) {
+            p.q[r * top + j] = l.q[j];
+            p.z[r * top + j] = l.z[j];
+        }
+        if (threadIdx.x == 0) {
+            p.taught[2 * r] = t.q;
+            p.taught[2 * r + 1] = t.qx;
+        }
+        return;
+    }
     const u32 j0 = at * (kPartThreads * kPartVecs) + threadIdx.x;
     const float c = (float)(1.4426950408889634074 * a.teacher.inv_t);
     const u32 whole = a.cols / W;
@@ -348,13 +377,6 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_st
 #pragma unroll
     for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
     const float rest = at + 1 == p.parts ? load_rest<KIND>(row, a.cols, threadIdx.x) : -kInf;
-    if (at == 0) {
-        // (the gradient may be written over the scores)
-        for (int j = threadIdx.x; j < a.teacher.top; j += kPartThreads) {
-            const int i = a.teacher.idx[r * a.teacher.top + j];
-            p.z[r * a.teacher.top + j] = i >= 0 && (u32)i < a.cols ? value_at<KIND>(row, (u32)i) : 0.f;
-        }
-    }
     float m = rest;
 #pragma unroll
     for (int i = 0; i < kPartVecs; ++i)
@@ -394,22 +416,40 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_ap
         for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
         if (at + 1 == blocks) rest = load_rest<KIND>(row, a.cols, threadIdx.x);
     }
-    // (the scores at the entries: kept ones where the gradient of another part may be written over them)
-    const Taught t = p.z ? teach<kScoreF32, kPartThreads, true>(a.teacher, r, (const char*)(p.z + r * a.teacher.top), a.cols, l, sm)
-                         : teach<KIND, kPartThreads>(a.teacher, r, row, a.cols, l, sm);
+    const int top = a.teacher.top;
+    Taught t;
     float m = -kInf;
     double s[2] = {0.0, 0.0};
     if (a.have_stats) {
+        t = teach<KIND, kPartThreads>(a.teacher, r, row, a.cols, l, sm);
         m = a.stats[2 * r];
         s[0] = (double)a.stats[2 * r + 1];
     } else {
-        const float* q = p.part + r * p.parts * 2;
-        for (u32 i = threadIdx.x; i < p.parts; i += kPartThreads) m = fmaxf(m, q[2 * i]);
-        m = block_max<kPartThreads>(m, sm);
-        for (u32 i = threadIdx.x; i < p.parts; i += kPartThreads)
-            if (q[2 * i + 1] != 0.f) s[0] += (double)q[2 * i + 1] * exp(((double)q[2 * i] - (double)m) * a.teacher.inv_t);
-        if (a.loss) s[1] = below_top<kPartThreads>(l, a.teacher.top, m, a.teacher.inv_t);
-        block_sums<kPartThreads, 2>(s, sm);
+        const float* part = p.part + r * p.parts * 2;
+        t = Taught{p.taught[2 * r], p.taught[2 * r + 1]};
+        // the parts' sums, each wavefront for itself: there are few
+        const u32 lane = threadIdx.x & 63;
+        for (u32 i = lane; i < p.parts; i += 64) m = fmaxf(m, part[2 * i]);
+        if (threadIdx.x < ((top + 3) & ~3) - top) l.idx[top + threadIdx.x] = -1;
+        for (int j = threadIdx.x; j < top; j += kPartThreads) {
+            const int i = a.teacher.idx[r * top + j];
+            l.idx[j] = i >= 0 && (u32)i < a.cols ? i : -1;
+            l.q[j] = p.q[r * top + j];
+            l.z[j] = p.z[r * top + j];
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        m = uniform(m);
+        for (u32 i = lane; i < p.parts; i += 64)
+            if (part[2 * i + 1] != 0.f) s[0] += (double)part[2 * i + 1] * exp(((double)part[2 * i] - (double)m) * a.teacher.inv_t);
+        s[0] = uniform(wave_sum(s[0]));
+        __syncthreads();
+        if (a.loss && at == 0) {
+            s[1] = below_top<kPartThreads>(l, top, m, a.teacher.inv_t);
+            double v[1] = {s[1]};
+            block_sums<kPartThreads, 1>(v, sm);
+            s[1] = v[0];
+        }
     }
     if (at == 0 && threadIdx.x == 0) {
         if (a.loss) a.loss[r] = loss_of(t, s[1], s[0]);
@@ -491,19 +531,21 @@ static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 12
 
 size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || !takes_parts(kScoreF32, rows, cols)) return 0;
-    return (size_t)rows * parts_of(kScoreF32, cols) * 8 + (size_t)rows * 1024 * 4;
+    return (size_t)rows * (16 + parts_of(kScoreF32, cols) * 8 + 2 * 1024 * 4);
 }
 
 template <int KIND> static hipError_t launch_kind(const DistillArgs& a, void* scratch, hipStream_t st) {
-    const size_t lds = (size_t)a.teacher.top * 12;
+    const size_t lds = teacher_bytes(a.teacher.top);
     if (a.have_stats || takes_parts(KIND, a.rows, a.cols)) {
         Parts p{};
         p.parts = (u32)parts_of(KIND, a.cols);
         const u32 blocks = a.grad ? p.parts : 1;
         if (!a.have_stats) {
-            p.part = (float*)scratch;
-            p.z = p.part + (u64)a.rows * p.parts * 2;
-            hipLaunchKernelGGL(k_distill_stats<KIND>, grid_of((u64)a.rows * p.parts), dim3(kPartThreads), 0, st, a, p);
+            p.taught = (double*)scratch;
+            p.part = (float*)(p.taught + 2 * (u64)a.rows);
+            p.q = p.part + (u64)a.rows * p.parts * 2;
+            p.z = p.q + (u64)a.rows * a.teacher.top;
+            hipLaunchKernelGGL(k_distill_stats<KIND>, grid_of((u64)a.rows * (p.parts + 1)), dim3(kPartThreads), lds, st, a, p);
         }
         hipLaunchKernelGGL(k_distill_apply<KIND>, grid_of((u64)a.rows * blocks), dim3(kPartThreads), lds, st, a, p, blocks);
         return hipGetLastError();
@@ -529,7 +571,7 @@ hipError_t launch_distill(int kind, const DistillArgs& a, void* scratch, hipStre
 
 hipError_t launch_distill_state(const float2* A, int n, const TeacherArgs& te, int64_t rows, double* f, int64_t f_stride, float2* S, int paired, hipStream_t st) {
     if (S) hipLaunchKernelGGL(k_distill_zero, grid_of((((u64)rows << n) + 255) / 256), dim3(256), 0, st, A, n, (u64)rows << n, S, paired);
-    hipLaunchKernelGGL(k_distill_state, grid_of((u64)rows), dim3(256), (size_t)te.top * 12, st, A, n, te, (u64)rows, f, (u64)f_stride, S,
+    hipLaunchKernelGGL(k_distill_state, grid_of((u64)rows), dim3(256), teacher_bytes(te.top), st, A, n, te, (u64)rows, f, (u64)f_stride, S,
                        paired ? 2 : 1, paired ? 1 : 0);
     return hipGetLastError();
 }
