@@ -346,7 +346,9 @@ __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
 }
 
 // ---- few rows, or a gradient from kept statistics: parts of rows by workgroups of their own -------------------------
-constexpr int kPartThreads = 256, kPartVecs = 8;       // a part: 8 vectors a thread
+// A part: PV vectors a thread.  Few rows take 2, which spreads them over four times the CUs; a gradient from kept statistics 8,
+// since every part works its row's teacher out again.
+constexpr int kPartThreads = 256;
 
 struct Parts {
     u32 parts;
@@ -356,7 +358,7 @@ struct Parts {
 };
 
 // A row's parts, and one workgroup more for its teacher (its scores are read here: the gradient may be written over them).
-template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_stats(const DistillArgs a, const Parts p) {
+template <int KIND, int PV> __global__ __launch_bounds__(kPartThreads) void k_distill_stats(const DistillArgs a, const Parts p) {
     constexpr int W = kPer<KIND>;
     extern __shared__ char lds[];
     __shared__ double sm[48];
@@ -378,16 +380,16 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_st
         }
         return;
     }
-    const u32 j0 = at * (kPartThreads * kPartVecs) + threadIdx.x;
+    const u32 j0 = at * (kPartThreads * PV) + threadIdx.x;
     const float c = (float)(1.4426950408889634074 * a.teacher.inv_t);
     const u32 whole = a.cols / W;
-    vec x[kPartVecs];
+    vec x[PV];
 #pragma unroll
-    for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
+    for (int i = 0; i < PV; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
     const float rest = at + 1 == p.parts ? load_rest<KIND>(row, a.cols, threadIdx.x) : -kInf;
     float m = rest;
 #pragma unroll
-    for (int i = 0; i < kPartVecs; ++i)
+    for (int i = 0; i < PV; ++i)
 #pragma unroll
         for (int k = 0; k < W; ++k) m = fmaxf(m, part<KIND>(x[i], k));
     m = block_max<kPartThreads>(m, sm);
@@ -395,7 +397,7 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_st
     const float base = m > -kInf ? m : 0.f;
     float sum = __builtin_amdgcn_exp2f((rest - base) * c);
 #pragma unroll
-    for (int i = 0; i < kPartVecs; ++i)
+    for (int i = 0; i < PV; ++i)
 #pragma unroll
         for (int k = 0; k < W; ++k) sum += __builtin_amdgcn_exp2f((part<KIND>(x[i], k) - base) * c);
     double s[1] = {(double)sum};
@@ -406,7 +408,7 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_st
     }
 }
 
-template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_apply(const DistillArgs a, const Parts p, u32 blocks) {
+template <int KIND, int PV> __global__ __launch_bounds__(kPartThreads) void k_distill_apply(const DistillArgs a, const Parts p, u32 blocks) {
     constexpr int W = kPer<KIND>;
     extern __shared__ char lds[];
     __shared__ double sm[48];
@@ -415,13 +417,13 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_ap
     if (r >= (u64)a.rows) return;
     const char* row = (const char*)a.scores + r * (u64)a.stride * kSize<KIND>;
     const TeacherLds l = teacher_lds(lds, a.teacher.top);
-    const u32 j0 = at * (kPartThreads * kPartVecs) + threadIdx.x;
+    const u32 j0 = at * (kPartThreads * PV) + threadIdx.x;
     const u32 whole = a.cols / W;
-    vec x[kPartVecs];
+    vec x[PV];
     float rest = -kInf;
     if (a.grad) {
 #pragma unroll
-        for (int i = 0; i < kPartVecs; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
+        for (int i = 0; i < PV; ++i) x[i] = load_vec<KIND>(row, whole, j0 + (u32)i * kPartThreads);
         if (at + 1 == blocks) rest = load_rest<KIND>(row, a.cols, threadIdx.x);
     }
     const int top = a.teacher.top;
@@ -468,7 +470,7 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_ap
     const Gradient g = gradient_of(t, m, s[0], a.teacher.inv_t, a.grad_loss ? a.grad_loss[r] : 1.f);
     const bool zero = t.q == 0.0;
 #pragma unroll
-    for (int i = 0; i < kPartVecs; ++i) {
+    for (int i = 0; i < PV; ++i) {
         float o[W];
 #pragma unroll
         for (int k = 0; k < W; ++k) o[k] = zero ? 0.f : e_of(g, part<KIND>(x[i], k)) * g.scale;
@@ -477,8 +479,8 @@ template <int KIND> __global__ __launch_bounds__(kPartThreads) void k_distill_ap
     if (at + 1 == blocks) store_rest<KIND>(grad, a.cols, threadIdx.x, zero ? 0.f : e_of(g, rest) * g.scale);
     if (zero) return;
     __syncthreads();
-    const u64 k0 = (u64)at * (kPartThreads * kPartVecs * W);
-    write_entries<KIND, kPartThreads>(l, a.teacher.top, g, grad, (u32)k0, (u32)min(k0 + kPartThreads * kPartVecs * W, (u64)a.cols));
+    const u64 k0 = (u64)at * (kPartThreads * PV * W);
+    write_entries<KIND, kPartThreads>(l, a.teacher.top, g, grad, (u32)k0, (u32)min(k0 + kPartThreads * PV * W, (u64)a.cols));
 }
 
 // ---- a circuit's own outcomes ----------------------------------------------------------------------------------------
@@ -531,31 +533,37 @@ __global__ __launch_bounds__(256) void k_distill_zero(const float2* A, int n, u6
 
 }  // namespace
 
-static u64 part_values(int kind) { return (u64)kPartThreads * kPartVecs * (kind == kScoreF32 ? 4 : 8); }
-static u64 parts_of(int kind, int64_t cols) { return ((u64)cols + part_values(kind) - 1) / part_values(kind); }
+static u64 parts_of(int kind, int64_t cols, int vecs) {
+    const u64 values = (u64)kPartThreads * vecs * (kind == kScoreF32 ? 4 : 8);
+    return ((u64)cols + values - 1) / values;
+}
+constexpr int kFewVecs = 2, kBackVecs = 8;
 
 // Rows that would leave most of the chip idle, and are long enough to be split.
-static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 128 && parts_of(kind, cols) > 2; }
+static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 128 && parts_of(kind, cols, kBackVecs) > 2; }
 
 size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || !takes_parts(kScoreF32, rows, cols)) return 0;
-    return (size_t)rows * (16 + parts_of(kScoreF32, cols) * 8 + 2 * 1024 * 4);
+    return (size_t)rows * (16 + parts_of(kScoreF32, cols, kFewVecs) * 8 + 2 * 1024 * 4);
 }
 
 template <int KIND> static hipError_t launch_kind(const DistillArgs& a, void* scratch, hipStream_t st) {
     const size_t lds = teacher_bytes(a.teacher.top);
     if (a.have_stats || takes_parts(KIND, a.rows, a.cols)) {
         Parts p{};
-        p.parts = (u32)parts_of(KIND, a.cols);
-        const u32 blocks = a.grad ? p.parts : 1;
-        if (!a.have_stats) {
-            p.taught = (double*)scratch;
-            p.part = (float*)(p.taught + 2 * (u64)a.rows);
-            p.q = p.part + (u64)a.rows * p.parts * 2;
-            p.z = p.q + (u64)a.rows * a.teacher.top;
-            hipLaunchKernelGGL(k_distill_stats<KIND>, grid_of((u64)a.rows * (p.parts + 1)), dim3(kPartThreads), lds, st, a, p);
+        if (a.have_stats) {
+            p.parts = a.grad ? (u32)parts_of(KIND, a.cols, kBackVecs) : 1;
+            hipLaunchKernelGGL((k_distill_apply<KIND, kBackVecs>), grid_of((u64)a.rows * p.parts), dim3(kPartThreads), lds, st, a, p, p.parts);
+            return hipGetLastError();
         }
-        hipLaunchKernelGGL(k_distill_apply<KIND>, grid_of((u64)a.rows * blocks), dim3(kPartThreads), lds, st, a, p, blocks);
+        p.parts = (u32)parts_of(KIND, a.cols, kFewVecs);
+        const u32 blocks = a.grad ? p.parts : 1;
+        p.taught = (double*)scratch;
+        p.part = (float*)(p.taught + 2 * (u64)a.rows);
+        p.q = p.part + (u64)a.rows * p.parts * 2;
+        p.z = p.q + (u64)a.rows * a.teacher.top;
+        hipLaunchKernelGGL((k_distill_stats<KIND, kFewVecs>), grid_of((u64)a.rows * (p.parts + 1)), dim3(kPartThreads), lds, st, a, p);
+        hipLaunchKernelGGL((k_distill_apply<KIND, kFewVecs>), grid_of((u64)a.rows * blocks), dim3(kPartThreads), lds, st, a, p, blocks);
         return hipGetLastError();
     }
     const u64 vecs = ((u64)a.cols + kPer<KIND> - 1) / kPer<KIND>;
