@@ -645,10 +645,19 @@ template <int NT> struct Shape;
 // bins of a histogram (and entries of a list to be sorted), chunks, vectors of a lane in a chunk
 template <> struct Shape<64> { static constexpr int bins = 256, chunks = 4, steps = 1; static constexpr u32 most = 512; };
 template <> struct Shape<256> { static constexpr int bins = 1024, chunks = 36, steps = 1; static constexpr u32 most = 8192; };
+template <> struct Shape<512> { static constexpr int bins = 2048, chunks = 264, steps = 4; static constexpr u32 most = 262144; };
 template <> struct Shape<1024> { static constexpr int bins = 2048, chunks = 264, steps = 4; static constexpr u32 most = 262144; };
 
+// A row whose shots a later launch draws, all over the chip: what is kept of it (ok = 0: they are drawn already), and its kept
+// weights up to the end of every chunk.
+struct RowDraw { u32 ok, kmax; Cut cut; };
+struct Later {
+    RowDraw* rows;         // [rows], or NULL: nothing is left for later
+    u64* chunk_w;          // [rows][Shape<1024>::chunks]
+};
+
 template <int KIND, int NT>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_sample_row(const SampleArgs a) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_sample_row(const SampleArgs a, const Later later) {
     constexpr int NB = Shape<NT>::bins, NC = Shape<NT>::chunks, STEPS = Shape<NT>::steps, LIST = 2 * NB;
     constexpr int UN = NT == 1024 ? 4 : 2;  // vectors of a thread on their way at once
     // two histograms; or: a list to be sorted, its entries and their weights, or values on their way; or: a list to be searched
@@ -670,6 +679,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
     const Row row = row_of<KIND>(a, r);
     const Params p = params_of(a, r);
     const u32 nchunks = (row.vecs + 64 * STEPS - 1) / (64 * STEPS);
+    if (later.rows && threadIdx.x == 0) later.rows[r] = RowDraw{0, 0, {0.f, 0}};
 
     // the first shots' uniforms are on their way while the row is read: a thread's, and a wavefront's
     const double* const uniforms = a.uniforms + r * a.shots;
@@ -1129,6 +1139,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
         }
         return;
     }
+    if (later.rows) {
+        if (threadIdx.x < nchunks) later.chunk_w[r * NC + threadIdx.x] = chunk_w[threadIdx.x];
+        if (threadIdx.x == 0) later.rows[r] = RowDraw{1, kmax, cut};
+        return;
+    }
     for (u64 i = wave; i < (u64)a.shots; i += NT / 64) {
         const double u = i < NT / 64 ? u_wave : uniforms[i];
         long long k = -1;
@@ -1144,6 +1159,40 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
         }
         if (lane == 0) write_shot(a, r * a.shots + i, k, w, total);
     }
+}
+
+// The shots that were left for later, a wavefront each.
+template <int KIND> __global__ __launch_bounds__(256) void k_row_draw(const SampleArgs a, const Later later) {
+    constexpr int NC = Shape<1024>::chunks, STEPS = Shape<1024>::steps, NP = kPowers<1024>;
+    __shared__ Tables<KIND, NP> lds_tables;
+    const Tables<KIND, NP>* const tables = &lds_tables;
+    fill_tables<KIND, 256>(&lds_tables, a.bits, false);
+    __syncthreads();
+    const u64 at = grid_block() * 4 + (threadIdx.x >> 6);
+    if (at >= (u64)a.rows * a.shots) return;
+    const u64 r = at / a.shots;
+    const RowDraw d = later.rows[r];
+    if (!d.ok) return;
+    const u32 lane = threadIdx.x & 63;
+    const Row row = row_of<KIND>(a, r);
+    const Params p = params_of(a, r);
+    const Scale s = scale_of<KIND, Shape<1024>::bins, NP>(tables, d.kmax, p.t, a.bits);
+    const u32 nchunks = (row.vecs + 64 * STEPS - 1) / (64 * STEPS);
+    const u64* cw = later.chunk_w + r * NC;
+    const u64 total = cw[nchunks - 1];
+    const double u = a.uniforms[at];
+    long long k = -1;
+    u64 w = 0;
+    if (u >= 0.0 && u < 1.0) {
+        const u64 t = draw_at(u, total);
+        u32 c = 0;
+        for (u32 c0 = 0; c0 < nchunks; c0 += 64) {
+            const u64 above = __ballot(c0 + lane < nchunks && cw[min(c0 + lane, nchunks - 1)] > t);
+            if (above) { c = c0 + (u32)__ffsll((long long)above) - 1u; break; }
+        }
+        k = find_in_chunk<KIND, STEPS>(row, s, tables, d.cut, c * 64 * STEPS, c ? cw[c - 1] : 0, t, lane, &w);
+    }
+    if (lane == 0) write_shot(a, at, k, w, total);
 }
 
 // ---- long rows: their parts by workgroups of their own ---------------------------------------------------------------
@@ -1560,7 +1609,9 @@ static bool takes_parts(int64_t rows, int64_t cols) {
 }
 
 size_t sample_scratch_bytes(int64_t rows, int64_t cols) {
-    return rows > 0 && takes_parts(rows, cols) ? long_sizes(rows, cols).all : 0;
+    if (rows < 1 || cols <= (int64_t)Shape<256>::most) return 0;
+    if (takes_parts(rows, cols)) return long_sizes(rows, cols).all;
+    return (size_t)rows * (Shape<1024>::chunks * sizeof(u64) + sizeof(RowDraw));
 }
 
 template <int KIND> static hipError_t launch_long(const SampleArgs& a, char* scratch, hipStream_t st) {
@@ -1601,9 +1652,27 @@ template <int KIND> static hipError_t launch_long(const SampleArgs& a, char* scr
 template <int KIND> static hipError_t launch_kind(const SampleArgs& a, void* scratch, hipStream_t st) {
     if (takes_parts(a.rows, a.cols)) return launch_long<KIND>(a, (char*)scratch, st);
     const dim3 grid = grid_of((u64)a.rows);
-    if (a.cols <= Shape<64>::most) hipLaunchKernelGGL((k_sample_row<KIND, 64>), grid, dim3(64), 0, st, a);
-    else if (a.cols <= Shape<256>::most) hipLaunchKernelGGL((k_sample_row<KIND, 256>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_sample_row<KIND, 1024>), grid, dim3(1024), 0, st, a);
+    Later later{nullptr, nullptr};
+    if (a.cols <= Shape<64>::most) {
+        hipLaunchKernelGGL((k_sample_row<KIND, 64>), grid, dim3(64), 0, st, a, later);
+        return hipGetLastError();
+    }
+    if (a.cols <= Shape<256>::most) {
+        hipLaunchKernelGGL((k_sample_row<KIND, 256>), grid, dim3(256), 0, st, a, later);
+        return hipGetLastError();
+    }
+    // More shots of a row than two for each of its wavefronts are drawn by another launch (6 x 66088 f32, 564 shots, wide
+    // nuclei: 209 -> 56 us; for a shot or two the launch costs more).
+    if (a.shots > 32) {
+        later.chunk_w = (u64*)scratch;
+        later.rows = (RowDraw*)(later.chunk_w + (u64)a.rows * Shape<1024>::chunks);
+    }
+    // A row for every CU or fewer: all of its threads for the row.  Two workgroups of half of them, which fill each other's
+    // waits, where there are more rows (516 x 13885 f16: 48.5 -> 37 us).
+    if (a.rows <= 256) hipLaunchKernelGGL((k_sample_row<KIND, 1024>), grid, dim3(1024), 0, st, a, later);
+    else hipLaunchKernelGGL((k_sample_row<KIND, 512>), grid, dim3(512), 0, st, a, later);
+    if (later.rows)
+        hipLaunchKernelGGL(k_row_draw<KIND>, grid_of(((u64)a.rows * a.shots + 3) / 4), dim3(256), 0, st, a, later);
     return hipGetLastError();
 }
 

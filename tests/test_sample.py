@@ -337,6 +337,22 @@ def test_state(n, batch):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16", "probs"])
+@pytest.mark.parametrize("rows,cols,shots", [(3, 9000, 33), (2, 70001, 200), (300, 8193, 40), (300, 9999, 3)])
+def test_many_shots_and_many_rows(ctx, src, rows, cols, shots):
+    """Rows whose shots another launch draws, and more rows than there are CUs; all kinds of cuts side by side."""
+    import torch
+    g = torch.Generator().manual_seed(rows + cols)
+    z = torch.randn((rows, cols), generator=g) * 2
+    z[rows // 2] = -INF if src in LOGS else 0.0
+    z = (z.exp() if src == "probs" else z).to(torch_type(src)).cuda()
+    u = torch.rand((rows, shots), generator=g, dtype=torch.float64).numpy()
+    u[0, 1] = 1.5
+    for filters in ({}, spread(EACH, rows), dict(top_p=[0.97] * rows, temperature=[1.5] * rows)):
+        same(on_gpu(ctx, src, z, u, filters), reference(values_of(src, z), src in LOGS, u, filters))
+
+
+@pytest.mark.gpu
 def test_outputs_left_out_and_shots_of_none(ctx):
     import torch
     z = torch.randn((3, 400), generator=torch.Generator().manual_seed(2)).cuda()
@@ -372,7 +388,7 @@ def test_workspace_refused_before_anything_runs():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("cols", [3000, 300000])
+@pytest.mark.parametrize("cols", [3000, 20000, 300000])
 def test_replays_of_a_captured_call(cols):
     """New scores and uniforms between the replays; eager calls of the same context in between."""
     import torch
@@ -381,8 +397,8 @@ def test_replays_of_a_captured_call(cols):
     with torch.cuda.stream(stream):
         c = qb.Context(1, 1)
         z = torch.zeros((2, cols), device="cuda")
-        u = torch.zeros((2, 5), dtype=torch.float64, device="cuda")
-        out = torch.zeros((2, 5), dtype=torch.int64, device="cuda")
+        u = torch.zeros((2, 50), dtype=torch.float64, device="cuda")
+        out = torch.zeros((2, 50), dtype=torch.int64, device="cuda")
         kept = torch.zeros(2, dtype=torch.int32, device="cuda")
         f = dict(top_p=torch.full((2,), 0.9, device="cuda"), top_k=torch.full((2,), 500, dtype=torch.int32, device="cuda"))
         call = lambda: c.qsv_sample(qb.QSV_S_F32, out, u, scores=z, kept=kept, **f)  # noqa: E731
@@ -393,7 +409,7 @@ def test_replays_of_a_captured_call(cols):
             call()
         for i in range(4):
             z.copy_(torch.randn((2, cols), generator=g) * (i + 1))
-            u.copy_(torch.rand((2, 5), generator=g, dtype=torch.float64))
+            u.copy_(torch.rand((2, 50), generator=g, dtype=torch.float64))
             out.fill_(-7)
             graph.replay()
             stream.synchronize()
