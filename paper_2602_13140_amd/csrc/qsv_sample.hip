@@ -1,13 +1,23 @@
 // Outcomes drawn from rows of scores, probabilities or amplitudes after temperature, min-p, top-k and top-p.
 //
 // All filters cut one order: value descending, ties by the lowest index first.  So what is left of a row is known by a
-// cut (key, idx): everything above the key, and what equals it up to that index.  Keys are the values' bits made
-// to order as whole numbers, 16 of them for 16-bit scores.  A cut is found without sorting: a histogram over the distance
-// from the row's highest value (counts, and for top-p weights), then histograms over the keys of the one bin the cut falls
-// into, 11 bits at a time, until the bin is one key.
+// cut (value, index): everything above the value, and what equals it up to that index.  No row is sorted:
+//   top-k   Every thread knows the highest of its own values.  The k-th of those is a bound that k outcomes reach and few
+//           more; they go into a list, and the list is sorted in LDS (32768 scores, k = 50: some 55 entries).
+//   top-p   Needs the weight of the whole row: one scan adds every weight to a histogram over its distance from the
+//           highest value; what lies above the bin that the cut falls into is kept, what lies in it is sorted.
+//   else    (k large, a bin of nearly equal values, a row in parts) histograms over the bits of the values in the bin, 11
+//           at a time, until the bin is one value.
+// The draw finds the 1024 values that the running sum passes the shot in by sums over such chunks, and then the value.
 //
 // Weights are whole numbers, rint(e 2^S) with e in 64 bits: their sums are the same in any order, so a call's results do
 // not depend on how its work was split or in which order atomics arrived.
+//
+// A row of up to 262144 outcomes is one workgroup's, which reads it two or three times: bound by memory for top-k (256 x
+// 131072 f32: 58 us, 7 TB/s in each of two scans out of the memory-side cache), by vector issue for top-p (108 us; a weight
+// takes 19 instructions, and the slowest of 256 rows has half of its outcomes left).  Few rows are bound by latency (1 x
+// 32768 bf16: 11 us).  64-bit atomics, weights and the search of a cut in 64 bits cost nothing here that 32 bits would
+// save: double precision issues at the rate of single.
 #include "qsv_scores.h"
 #include "qsv_wave.h"
 
@@ -266,7 +276,7 @@ template <int KIND, int NB, int NP> __device__ __forceinline__ Scale scale_of(co
     // weights end below 2^-(S + 2)
     if (!(s.m < kInf)) s.low_w = s.m;
     else if (kLogs<KIND>) s.low_w = float_from(s.md - (double)(bits + 2) * (0.69314718055994530942 * (double)t));
-    else s.low_w = float_from(s.md * exp2_neg(-(double)(bits + 2) * (double)t));
+    else s.low_w = fmaxf(float_from(s.md * exp2(-(double)(bits + 2) * (double)t)), __uint_as_float(1u));
     return s;
 }
 
@@ -314,7 +324,7 @@ template <int KIND, int NP> __device__ __forceinline__ u64 weight(const Scale& s
     return v >= s.low_w ? w : 0;
 }
 
-// Filled by a kernel's threads before their next barrier: 2^(i / 256), and logarithms where a row will ask for them.
+// Filled by a kernel's threads before their next barrier; not at all where a row will not look anything up.
 template <int KIND, int NT, int NP> __device__ __forceinline__ void fill_tables(Tables<KIND, NP>* tables, int bits, bool t_one) {
     if (!kLogs<KIND> && t_one) return;
     const double two = __builtin_ldexp(2.0, bits - 63);        // (steps start at 63 factors of two)
@@ -401,8 +411,6 @@ __device__ __forceinline__ u64 mass_of(float top_p, u64 w) {
 // The bin in which the running sum (of counts, or of weights) over cnt / wt reaches target, and what lies before it.  false: it
 // never does.  total: target holds top_p's bits, which the whole weight turns into the target.  Ends with a barrier.
 struct Hit { u32 bin; u64 count, weight, own; };        // own: outcomes in the bin
-struct ByCount { static constexpr bool value = false; };
-struct ByWeight { static constexpr bool value = true; };
 // MIRROR: weights in bins that rise with the value; the bin's number counts from the last one.
 template <int NT, int NB, bool BYW, bool MIRROR = false> __device__ __forceinline__ bool select_bin(const u32* cnt, const u64* weights, u64 target, u64* sm, Hit* hit, Hit* at, u64* total = nullptr) {
     constexpr int per = NB / NT > 0 ? NB / NT : 1;
