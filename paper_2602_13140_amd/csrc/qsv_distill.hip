@@ -67,14 +67,16 @@ template <int KIND> __device__ __forceinline__ float part(const vec& x, int i) {
     return __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
 }
 
-template <int KIND> __device__ __forceinline__ void store_vec(char* row, u32 whole, u32 j, const float (&g)[kPer<KIND>]) {
+// PAST: past the caches.
+template <int KIND, bool PAST> __device__ __forceinline__ void store_vec(char* row, u32 whole, u32 j, const float (&g)[kPer<KIND>]) {
     constexpr int W = kPer<KIND>;
     if (j >= whole) return;
     vec x;
     if (KIND == kScoreF32) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(g[i]);
-        *(vec_at4*)(row + j * 16u) = x;
+        if (PAST) __builtin_nontemporal_store(x, (vec_at4*)(row + j * 16u));
+        else *(vec_at4*)(row + j * 16u) = x;
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -86,7 +88,8 @@ template <int KIND> __device__ __forceinline__ void store_vec(char* row, u32 who
                 x[i] = (u32)__half_as_ushort(__float2half_rn(g[(2 * i) % W])) | (u32)__half_as_ushort(__float2half_rn(g[(2 * i + 1) % W])) << 16;
             }
         }
-        *(vec_at2*)(row + j * 16u) = x;
+        if (PAST) __builtin_nontemporal_store(x, (vec_at2*)(row + j * 16u));
+        else *(vec_at2*)(row + j * 16u) = x;
     }
 }
 
@@ -252,7 +255,7 @@ template <int KIND, int NT> __device__ __forceinline__ void write_entries(const 
 }
 
 // ---- one workgroup a row ---------------------------------------------------------------------------------------------
-template <int KIND, int NT, bool KEPT>
+template <int KIND, int NT, bool KEPT, bool PAST>
 __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
     constexpr int W = kPer<KIND>, NV = 16;
     extern __shared__ char lds[];
@@ -330,7 +333,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
         float o[W];
 #pragma unroll
         for (int k = 0; k < W; ++k) o[k] = zero ? 0.f : e_of(g, part<KIND>(y, k)) * g.scale;
-        store_vec<KIND>(grad, whole, j, o);
+        store_vec<KIND, PAST>(grad, whole, j, o);
     };
     if (KEPT) {
         forget(x);
@@ -408,7 +411,7 @@ template <int KIND, int PV> __global__ __launch_bounds__(kPartThreads) void k_di
     }
 }
 
-template <int KIND, int PV> __global__ __launch_bounds__(kPartThreads) void k_distill_apply(const DistillArgs a, const Parts p, u32 blocks) {
+template <int KIND, int PV, bool PAST> __global__ __launch_bounds__(kPartThreads) void k_distill_apply(const DistillArgs a, const Parts p, u32 blocks) {
     constexpr int W = kPer<KIND>;
     extern __shared__ char lds[];
     __shared__ double sm[48];
@@ -474,7 +477,7 @@ template <int KIND, int PV> __global__ __launch_bounds__(kPartThreads) void k_di
         float o[W];
 #pragma unroll
         for (int k = 0; k < W; ++k) o[k] = zero ? 0.f : e_of(g, part<KIND>(x[i], k)) * g.scale;
-        store_vec<KIND>(grad, whole, j0 + (u32)i * kPartThreads, o);
+        store_vec<KIND, PAST>(grad, whole, j0 + (u32)i * kPartThreads, o);
     }
     if (at + 1 == blocks) store_rest<KIND>(grad, a.cols, threadIdx.x, zero ? 0.f : e_of(g, rest) * g.scale);
     if (zero) return;
@@ -547,39 +550,49 @@ size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
     return (size_t)rows * (16 + parts_of(kScoreF32, cols, kFewVecs) * 8 + 2 * 1024 * 4);
 }
 
-template <int KIND> static hipError_t launch_kind(const DistillArgs& a, void* scratch, hipStream_t st) {
+// Gradients of this size and more are written past the caches, which would not hold them for the next reader either (256 MiB:
+// 124 us through the caches, 126 past them; 512 MiB 196 / 183; 1 GiB 553 / 515).
+constexpr u64 kPastBytes = (u64)384 << 20;
+
+template <int KIND, bool PAST> static hipError_t launch_kind(const DistillArgs& a, void* scratch, hipStream_t st) {
     const size_t lds = teacher_bytes(a.teacher.top);
-    if (a.have_stats || takes_parts(KIND, a.rows, a.cols)) {
+    const dim3 block(kPartThreads);
+    if (a.have_stats) {
+        const u32 blocks = (u32)parts_of(KIND, a.cols, kBackVecs);
+        hipLaunchKernelGGL((k_distill_apply<KIND, kBackVecs, PAST>), grid_of((u64)a.rows * blocks), block, lds, st, a, Parts{}, blocks);
+        return hipGetLastError();
+    }
+    if (takes_parts(KIND, a.rows, a.cols)) {
         Parts p{};
-        if (a.have_stats) {
-            p.parts = a.grad ? (u32)parts_of(KIND, a.cols, kBackVecs) : 1;
-            hipLaunchKernelGGL((k_distill_apply<KIND, kBackVecs>), grid_of((u64)a.rows * p.parts), dim3(kPartThreads), lds, st, a, p, p.parts);
-            return hipGetLastError();
-        }
         p.parts = (u32)parts_of(KIND, a.cols, kFewVecs);
         const u32 blocks = a.grad ? p.parts : 1;
         p.taught = (double*)scratch;
         p.part = (float*)(p.taught + 2 * (u64)a.rows);
         p.q = p.part + (u64)a.rows * p.parts * 2;
         p.z = p.q + (u64)a.rows * a.teacher.top;
-        hipLaunchKernelGGL((k_distill_stats<KIND, kFewVecs>), grid_of((u64)a.rows * (p.parts + 1)), dim3(kPartThreads), lds, st, a, p);
-        hipLaunchKernelGGL((k_distill_apply<KIND, kFewVecs>), grid_of((u64)a.rows * blocks), dim3(kPartThreads), lds, st, a, p, blocks);
+        hipLaunchKernelGGL((k_distill_stats<KIND, kFewVecs>), grid_of((u64)a.rows * (p.parts + 1)), block, lds, st, a, p);
+        hipLaunchKernelGGL((k_distill_apply<KIND, kFewVecs, PAST>), grid_of((u64)a.rows * blocks), block, lds, st, a, p, blocks);
         return hipGetLastError();
     }
     const u64 vecs = ((u64)a.cols + kPer<KIND> - 1) / kPer<KIND>;
     const dim3 grid = grid_of((u64)a.rows);
     if (!a.grad && vecs > 64 * 16) {
         // A loss alone needs nothing kept: half the registers and twice the rows on a CU (513 x 50021 f16: 20.8 -> 16.4 us).
-        if (vecs <= 256 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 256, false>), grid, dim3(256), lds, st, a);
-        else hipLaunchKernelGGL((k_distill_row<KIND, 512, false>), grid, dim3(512), lds, st, a);
+        if (vecs <= 256 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 256, false, false>), grid, dim3(256), lds, st, a);
+        else hipLaunchKernelGGL((k_distill_row<KIND, 512, false, false>), grid, dim3(512), lds, st, a);
         return hipGetLastError();
     }
-    if (vecs <= 64 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 64, true>), grid, dim3(64), lds, st, a);
-    else if (vecs <= 256 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 256, true>), grid, dim3(256), lds, st, a);
-    else if (vecs <= 512 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 512, true>), grid, dim3(512), lds, st, a);
-    else if (vecs <= 1024 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 1024, true>), grid, dim3(1024), lds, st, a);
-    else hipLaunchKernelGGL((k_distill_row<KIND, 1024, false>), grid, dim3(1024), lds, st, a);
+    if (vecs <= 64 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 64, true, PAST>), grid, dim3(64), lds, st, a);
+    else if (vecs <= 256 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 256, true, PAST>), grid, dim3(256), lds, st, a);
+    else if (vecs <= 512 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 512, true, PAST>), grid, dim3(512), lds, st, a);
+    else if (vecs <= 1024 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 1024, true, PAST>), grid, dim3(1024), lds, st, a);
+    else hipLaunchKernelGGL((k_distill_row<KIND, 1024, false, PAST>), grid, dim3(1024), lds, st, a);
     return hipGetLastError();
+}
+
+template <int KIND> static hipError_t launch_kind(const DistillArgs& a, void* scratch, hipStream_t st) {
+    const bool past = a.grad && (u64)a.rows * a.cols * kSize<KIND> >= kPastBytes;
+    return past ? launch_kind<KIND, true>(a, scratch, st) : launch_kind<KIND, false>(a, scratch, st);
 }
 
 hipError_t launch_distill(int kind, const DistillArgs& a, void* scratch, hipStream_t st) {

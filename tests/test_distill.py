@@ -295,6 +295,34 @@ def test_masks_and_odd_teachers(ctx, src, rows, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src,cols", [("bf16", 4001), ("f16", 30000), ("bf16", 60001), ("bf16", 131072), ("f32", 70003)])
+def test_gradients_larger_than_the_caches(ctx, src, cols):
+    """Gradients of 384 MiB and more, which are written another way: the same bits as of two calls of half the rows, and of the
+    backward pass by itself the same as well."""
+    import torch
+    size = 4 if src == "f32" else 2
+    rows = (384 << 20) // (cols * size) // 2 * 2 + 2
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    z = (torch.randn((rows, cols), generator=g, device="cuda") * 3).to(tt(src))
+    idx = torch.randint(0, cols, (rows, 3), generator=g, device="cuda", dtype=torch.int32)
+    logits = torch.randn((rows, 3), generator=g, device="cuda")
+    whole, halves = torch.zeros_like(z), torch.zeros_like(z)
+    loss, stats = torch.zeros(rows, device="cuda"), torch.zeros((rows, 2), device="cuda")
+    ctx.qsv_distill(KIND[src], z, idx, logits, loss=loss, stats=stats, grad=whole)
+    h = rows // 2
+    for a in (0, h):
+        ctx.qsv_distill(KIND[src], z[a:a + h], idx[a:a + h], logits[a:a + h], grad=halves[a:a + h])
+    assert torch.equal(whole, halves)
+    for a in (0, h):
+        ctx.qsv_distill(KIND[src], z[a:a + h], idx[a:a + h], logits[a:a + h], stats=stats[a:a + h], have_stats=1, grad=halves[a:a + h])
+    whole.zero_()
+    ctx.qsv_distill(KIND[src], z, idx, logits, stats=stats, have_stats=1, grad=whole)
+    assert torch.equal(whole, halves)
+    at = [0, 1, rows - 1]
+    compare(src, (loss[at].cpu().numpy(), f64(whole[at]), None), reference(f64(z[at]), idx[at].cpu().numpy(), logits[at].cpu().numpy()))
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences_of_the_loss(ctx):
     """Central differences of the kernel's own losses: truncation h^2 |f'''| / 6 <= 2^-14 / 6, two losses of up to 8 rounded (2^-21)
     and good to 1e-6 over 2 h = 2^-6."""
