@@ -627,10 +627,11 @@ __device__ __forceinline__ void side_by_side(u64 (&w)[4]) {
     asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
 }
 
-// Four values of a lane into a histogram (counts, weights) of those in from .. to: over distances (first), or over keys down
-// from khi.  The weights of all four are worked out side by side, then what is in the range is added; over keys few are, and
-// only theirs are worked out.
-template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const Scale& s, const Tables<KIND, NP>* tables, const float (&v)[4], bool first, bool counts, bool weights, float from, float to, u32 khi, int shift, u64* wt, u32* cnt) {
+// Four values of a lane into a histogram (counts, weights) of those with keys in klo .. khi: over distances (first: khi is the
+// highest there is), or over keys down from khi.  The weights of all four are worked out side by side, then what is in the
+// range is added; over keys few are, and only theirs are worked out.  (Over keys it is keys that are compared: a range may end
+// between those of -0 and 0, which are equal as values.)
+template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const Scale& s, const Tables<KIND, NP>* tables, const float (&v)[4], bool first, bool counts, bool weights, float low, u32 klo, u32 khi, int shift, u64* wt, u32* cnt) {
     u64 w[4] = {0, 0, 0, 0};
     u32 b[4];
     if (weights && first) {
@@ -639,12 +640,13 @@ template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const S
         side_by_side(w);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = first ? bin_of<KIND, NB>(s, v[i]) : (khi - key_of<KIND>(v[i])) >> shift;
+    for (int i = 0; i < 4; ++i) b[i] = first ? bin_of<KIND, NB>(s, v[i]) : khi - key_of<KIND>(v[i]);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (v[i] >= from && v[i] <= to) {
-            if (counts) lds_add(cnt + b[i], 1u);
-            if (weights) lds_add(wt + b[i], first ? w[i] : weight(s, tables, v[i]));
+        if (first ? v[i] >= low : b[i] <= khi - klo) {
+            const u32 at = first ? b[i] : b[i] >> shift;
+            if (counts) lds_add(cnt + at, 1u);
+            if (weights) lds_add(wt + at, first ? w[i] : weight(s, tables, v[i]));
         }
 }
 
@@ -996,9 +998,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
             for (int i = threadIdx.x; i < NB; i += NT) { cnt[h + i] = 0; wt[h + i] = 0; }
             __syncthreads();
             const int shift = key_shift<NB>(hi - lo);
-            const float from = value_of<KIND>(lo), to = value_of<KIND>(hi);
+            const float from = value_of<KIND>(lo);
             walk<KIND, NT, 1>(row, 0, row.vecs, [=](const float (&v)[4], u32) {
-                add4<KIND, NB>(s, tables, v, first, true, by_p, from, to, hi, shift, wt + h, cnt + h);
+                add4<KIND, NB>(s, tables, v, first, true, by_p, from, lo, hi, shift, wt + h, cnt + h);
             });
             __syncthreads();
         };
@@ -1293,9 +1295,9 @@ template <int KIND> __device__ __forceinline__ void long_histogram(const Row& ro
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) { cnt[i] = 0; wt[i] = 0; }
     __syncthreads();
     const int shift = key_shift<kLongBins>(khi - klo);
-    const float low = value_of<KIND>(klo), high = value_of<KIND>(khi);
+    const float low = value_of<KIND>(klo);
     walk<KIND, kLongThreads, 4>(row, j0, j1, [=](const float (&v)[4], u32) {
-        add4<KIND, kLongBins>(s, tables, v, first, counts, weights, low, high, khi, shift, wt, cnt);
+        add4<KIND, kLongBins>(s, tables, v, first, counts, weights, low, klo, khi, shift, wt, cnt);
     });
     __syncthreads();
     for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) {

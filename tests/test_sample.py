@@ -302,6 +302,27 @@ def test_rows_of_near_equal_values(ctx, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cols", [9000, 270000])
+@pytest.mark.parametrize("src,high,low", [("f32", 0x3b1fffff, 0xfffff), ("bf16", 0x3b1f, 0xf), ("f16", 0x18ff, 0x7)])
+def test_cuts_right_below_zero(ctx, src, high, low, cols):
+    """Scores about 0 in one bin, whose keys are parted right between those of -0 and 0: the highest key is chosen for that.  The
+    cut falls among the negative ones, with many zeros (of both signs) beside it."""
+    import torch
+    g = np.random.default_rng(cols)
+    sign = 1 << (31 if src == "f32" else 15)
+    what = g.integers(0, 10, (4, cols))
+    bits = np.where(what < 2, g.integers(high // 2, high, (4, cols)), np.where(what < 6, 0, sign | g.integers(1, low + 1, (4, cols))))
+    bits = np.where(what == 5, sign, bits)
+    bits[:, 7] = high
+    word = bits.astype(np.uint32).view(np.int32) if src == "f32" else bits.astype(np.uint16).view(np.int16)
+    z = torch.from_numpy(word).view(torch_type(src)).cuda()
+    u = g.random((4, 6))
+    k = [cols * 7 // 10, cols * 6 // 10 + 3, cols * 8 // 10, cols * 9 // 10]
+    for filters in (dict(top_k=k), dict(top_p=[0.7, 0.65, 0.8, 0.95]), dict(top_k=k, top_p=[0.99, 0.95, 0.9, 0.8])):
+        same(on_gpu(ctx, src, z, u, filters), reference(values_of(src, z), True, u, filters))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src", ["f16", "f32"])
 def test_a_row_does_not_depend_on_its_alignment(ctx, src):
     import torch
