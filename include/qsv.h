@@ -322,7 +322,7 @@ typedef struct {
     const int32_t* top_idx_dev;  /* [rows][n_top] */
     const float* top_logits_dev; /* [rows][n_top] */
     const float* top_lse_dev;    /* [rows] or NULL */
-    double temperature;          /* T: finite, > 0 */
+    double temperature;          /* T: 2^-100..2^100 */
 } qsv_teacher;
 
 /* Loss of rows of scores z of a student against a teacher's top logits, and its gradient:

@@ -45,7 +45,8 @@ inline const char* check_teacher(const qsv_teacher* t) {
     if (t->reserved != 0) return "reserved must be 0";
     if (t->n_top < 1 || t->n_top > 1024) return "n_top must be in 1..1024";
     if (!t->top_idx_dev || !t->top_logits_dev) return "top_idx_dev or top_logits_dev is NULL";
-    if (!(t->temperature > 0.0) || !(t->temperature < __builtin_inf())) return "temperature must be finite and > 0";
+    // further out the scores' factor 1 / T would leave the range of 32 bits, and 0 times infinity make rows NaN
+    if (!(t->temperature >= 0x1p-100) || !(t->temperature <= 0x1p100)) return "temperature must be in 2^-100..2^100";
     return nullptr;
 }
 

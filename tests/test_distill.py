@@ -154,6 +154,13 @@ def test_refusals(checks):
     assert qb.load().qsv_distill_grad(None, None, None, 1, None, None, ctypes.byref(teacher()), None, None, None, None) == qb.QSV_ERR_INVALID_ARG
 
 
+def test_temperatures_that_32_bits_do_not_take(checks):
+    say = lambda t: checks.request_distill(ctypes.byref(req()), ctypes.byref(teacher(temperature=t)))  # noqa: E731
+    for t in (1e-310, 1e-39, 1e-31, 2.0 ** -100.5, 2.0 ** 100.5, 1e40, 1e300):
+        assert b"temperature" in say(t)
+    assert say(2.0 ** -100) is None and say(2.0 ** 100) is None
+
+
 def test_layouts():
     assert ctypes.sizeof(qb.qsv_teacher) == 40 and ctypes.sizeof(qb.qsv_distill_req) == 80
     assert qb.qsv_distill_workspace_bytes(-1, 5) == 0 == qb.qsv_distill_workspace_bytes(5, 0)
@@ -335,6 +342,27 @@ def test_gradient_against_differences_of_the_loss(ctx):
         d[:, k] = h
         up, down = (on_gpu(ctx, "f32", z + s * d, idx, logits, grad=False)[0].astype(np.float64) for s in (1, -1))
         assert np.abs((up - down) / (2 * h) - grad[:, k]).max() <= 2.0 ** -14 / 6 + (2 * 2.0 ** -22 + 2e-6) * 2 ** 6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(3, 40), (3, 40000), (200, 9000)])
+def test_lowest_and_highest_temperature(ctx, src, rows, cols):
+    """At 2^100 all that is not masked is as likely; at 2^-100 the highest is certain, and the others are too far for any loss
+    but the distance over T."""
+    z, idx, logits = draw(src, rows, cols, 1, 5)
+    z[:, 1] = -INF
+    z[:, 2] = 30.0
+    idx[:] = 2
+    loss, grad, stats = on_gpu(ctx, src, z, idx, logits, 2.0 ** 100)
+    assert np.abs(loss - math.log(cols - 1)).max() <= 1e-5 and np.abs(stats[:, 1] - (cols - 1)).max() <= 1e-5 * cols
+    assert np.all(np.isfinite(grad)) and np.abs(grad).max() <= 1e-30
+    loss, grad, stats = on_gpu(ctx, src, z, idx, logits, 2.0 ** -100)
+    assert np.all(loss == 0) and np.all(grad == 0) and np.all(stats[:, 1] == 1)
+    idx[:] = 3
+    loss, _, _ = on_gpu(ctx, src, z, idx, logits, 2.0 ** -100, grad=False)
+    far = (30.0 - f64(z)[:, 3]) * 2.0 ** 100
+    assert np.abs(loss - far).max() <= 1e-6 * far.max()
 
 
 @pytest.mark.gpu
