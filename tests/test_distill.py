@@ -538,6 +538,30 @@ def test_circuit_special_rows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n", [3, 11])
+def test_circuit_amplitudes_below_the_normal_range(n):
+    """An entry at an outcome whose amplitude's inverse 32 bits do not hold: the gradient is that of the other entries."""
+    import torch
+    c = qb.Context(n, 2)
+    circ = qb.make_circuit(1, [RY], NONE)
+    x = torch.zeros((2, 1 << n), device="cuda")
+    x[:, 0], x[:, 1], x[:, 6] = 0.8, 0.6, 1e-41
+    pr = torch.zeros(n, device="cuda")
+    logits = torch.zeros((2, 2), device="cuda")
+    lse = torch.full((2,), 0.5, device="cuda")
+    got = []
+    for second in (6, -1):
+        idx = torch.tensor([[0, second], [1, second]], dtype=torch.int32, device="cuda")
+        loss, grad = torch.full((2,), 7.0, device="cuda"), torch.full((2, n), 7.0, device="cuda")
+        c.qsv_distill_grad(circ, x, pr, None, idx, logits, loss, grad, top_lse=lse)
+        torch.cuda.synchronize()
+        assert not bool(torch.isnan(loss).any())
+        got.append(grad.cpu())
+    assert bool(torch.isfinite(got[0]).all()) and torch.equal(got[0], got[1]) and got[0].abs().max().item() > 0.1
+    c.close()
+
+
+@pytest.mark.gpu
 def test_training_towards_a_teacher_and_answers(oracle):
     """Steps of a circuit towards a teacher's likeliest outcomes, then answers drawn from what it learnt: every step's gradient and
     the drawn outcomes against the references."""
