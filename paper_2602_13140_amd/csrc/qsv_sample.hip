@@ -14,7 +14,7 @@
 // not depend on how its work was split or in which order atomics arrived.
 //
 // A row of up to 262144 outcomes is one workgroup's, which reads it two or three times: bound by memory for top-k (256 x
-// 131072 f32: 58 us, 7 TB/s in each of two scans out of the memory-side cache), by vector issue for top-p (108 us; a weight
+// 131072 f32: 58 us, 7 TB/s in each of two scans out of the memory-side cache), by vector issue for top-p (110 us; a weight
 // takes 19 instructions, and the slowest of 256 rows has half of its outcomes left).  Few rows are bound by latency (1 x
 // 32768 bf16: 11 us).  64-bit atomics, weights and the search of a cut in 64 bits cost nothing here that 32 bits would
 // save: double precision issues at the rate of single.
@@ -579,8 +579,8 @@ template <int KIND, int STEPS, int NP> __device__ __forceinline__ long long find
 }
 
 // ---- sorting in LDS --------------------------------------------------------------------------------------------------
-// Ascending, n <= 2 NT distinct entries.  Up to 256: each one's rank is the number of entries below it (64 entries, one
-// wavefront: 0.6 us; by exchanges 4).  Else by exchanges, entries behind the n-th up to a power of two at the highest number.
+// Ascending, n <= 2 NT distinct entries.  Up to 256: each one's rank is the number of entries below it (1 x 32768
+// bf16, some 55 entries: sorting and drawing 1.7 us, by exchanges 5.2).  Else by exchanges, entries behind the n-th up to a power of two at the highest number.
 template <int NT> __device__ __forceinline__ void sort_lds(u64* a, u32 n) {
     if (n <= 256) {
         constexpr int per = NT < 256 ? 256 / NT : 1;
@@ -1206,7 +1206,8 @@ template <int KIND> __global__ __launch_bounds__(256) void k_row_draw(const Samp
 }
 
 // ---- long rows: their parts by workgroups of their own ---------------------------------------------------------------
-// The same steps, a launch each; what a step finds out about a row goes to the next one through the workspace: the parts'
+// Bound by memory, a scan after the other (24 qubits, 128 MiB of state a scan: highest value 24 us, 5.6 TB/s; distances 37; keys
+// 32 and 25, the third level ends at once; sums 26; running sums 12; 4096 shots 13).  The same steps, a launch each; what a step finds out about a row goes to the next one through the workspace: the parts'
 // highest keys, histograms that all parts add to, the state of the search.  Every workgroup of a step works the state out
 // again from the one before and its histogram; the row's first one writes it down.  Steps whose cut is known already end
 // at once.
@@ -1613,14 +1614,13 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
 
 }  // namespace
 
-// Rows of more outcomes than one workgroup takes, or so few that most of the chip would idle.
-static bool takes_parts(int64_t rows, int64_t cols) {
-    return cols > (int64_t)Shape<1024>::most;
-}
+// Rows of more outcomes than one workgroup takes.  (Shorter ones are not split however few there are: a split row takes 5
+// to 11 launches, 6 us each where it has nothing to do; 24 x 50021 f16 take 31 us in one.)
+static bool takes_parts(int64_t cols) { return cols > (int64_t)Shape<1024>::most; }
 
 size_t sample_scratch_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || cols <= (int64_t)Shape<256>::most) return 0;
-    if (takes_parts(rows, cols)) return long_sizes(rows, cols).all;
+    if (takes_parts(cols)) return long_sizes(rows, cols).all;
     return (size_t)rows * (Shape<1024>::chunks * sizeof(u64) + sizeof(RowDraw));
 }
 
@@ -1660,7 +1660,7 @@ template <int KIND> static hipError_t launch_long(const SampleArgs& a, char* scr
 }
 
 template <int KIND> static hipError_t launch_kind(const SampleArgs& a, void* scratch, hipStream_t st) {
-    if (takes_parts(a.rows, a.cols)) return launch_long<KIND>(a, (char*)scratch, st);
+    if (takes_parts(a.cols)) return launch_long<KIND>(a, (char*)scratch, st);
     const dim3 grid = grid_of((u64)a.rows);
     Later later{nullptr, nullptr};
     if (a.cols <= Shape<64>::most) {
