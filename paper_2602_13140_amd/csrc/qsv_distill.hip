@@ -361,6 +361,7 @@ struct Parts {
     double* taught;       // [rows][2]: sum q, sum q (t / T - norm)
     float* part;          // [rows][parts][2]: maximum, sum relative to it
     float *q, *z;         // [rows][top]: of the teacher's entries, and the scores there
+    double* joined;       // [rows][2]: the whole row's maximum and sum, or NULL: every part joins the parts' by itself
 };
 
 // A row's parts, and one workgroup more for its teacher (its scores are read here: the gradient may be written over them).
@@ -414,6 +415,22 @@ template <int KIND, int PV> __global__ __launch_bounds__(kPartThreads) void k_di
     }
 }
 
+// The parts' maxima and sums joined, a workgroup a row.
+__global__ __launch_bounds__(1024) void k_distill_join(const DistillArgs a, const Parts p) {
+    __shared__ double sm[16];
+    const u64 r = grid_block();
+    if (r >= (u64)a.rows) return;
+    const float* part = p.part + r * p.parts * 2;
+    float m = -kInf;
+    for (u32 i = threadIdx.x; i < p.parts; i += 1024) m = fmaxf(m, part[2 * i]);
+    m = block_max<1024>(m, sm);
+    double s[1] = {0.0};
+    for (u32 i = threadIdx.x; i < p.parts; i += 1024)
+        if (part[2 * i + 1] != 0.f) s[0] += (double)part[2 * i + 1] * exp(((double)part[2 * i] - (double)m) * a.teacher.inv_t);
+    block_sums<1024, 1>(s, sm);
+    if (threadIdx.x == 0) { p.joined[2 * r] = (double)m; p.joined[2 * r + 1] = s[0]; }
+}
+
 template <int KIND, int PV, bool PAST> __global__ __launch_bounds__(kPartThreads) void k_distill_apply(const DistillArgs a, const Parts p, u32 blocks) {
     constexpr int W = kPer<KIND>;
     extern __shared__ char lds[];
@@ -443,9 +460,6 @@ template <int KIND, int PV, bool PAST> __global__ __launch_bounds__(kPartThreads
     } else {
         const float* part = p.part + r * p.parts * 2;
         t = Taught{p.taught[2 * r], p.taught[2 * r + 1]};
-        // the parts' sums, each wavefront for itself: there are few
-        const u32 lane = threadIdx.x & 63;
-        for (u32 i = lane; i < p.parts; i += 64) m = fmaxf(m, part[2 * i]);
         if (threadIdx.x < ((top + 3) & ~3) - top) l.idx[top + threadIdx.x] = -1;
         for (int j = threadIdx.x; j < top; j += kPartThreads) {
             const int i = a.teacher.idx[r * top + j];
@@ -453,12 +467,19 @@ template <int KIND, int PV, bool PAST> __global__ __launch_bounds__(kPartThreads
             l.q[j] = p.q[r * top + j];
             l.z[j] = p.z[r * top + j];
         }
+        if (p.joined) {
+            m = (float)p.joined[2 * r];
+            s[0] = p.joined[2 * r + 1];
+        } else {                           // few: each wavefront for itself
+            const u32 lane = threadIdx.x & 63;
+            for (u32 i = lane; i < p.parts; i += 64) m = fmaxf(m, part[2 * i]);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-        m = uniform(m);
-        for (u32 i = lane; i < p.parts; i += 64)
-            if (part[2 * i + 1] != 0.f) s[0] += (double)part[2 * i + 1] * exp(((double)part[2 * i] - (double)m) * a.teacher.inv_t);
-        s[0] = uniform(wave_sum(s[0]));
+            for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+            m = uniform(m);
+            for (u32 i = lane; i < p.parts; i += 64)
+                if (part[2 * i + 1] != 0.f) s[0] += (double)part[2 * i + 1] * exp(((double)part[2 * i] - (double)m) * a.teacher.inv_t);
+            s[0] = uniform(wave_sum(s[0]));
+        }
         __syncthreads();
         if (a.loss && at == 0) {
             s[1] = below_top<kPartThreads>(l, top, m, a.teacher.inv_t);
@@ -550,12 +571,33 @@ static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 12
 
 size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || !takes_parts(kScoreF32, rows, cols)) return 0;
-    return (size_t)rows * (16 + parts_of(kScoreF32, cols, kFewVecs) * 8 + 2 * 1024 * 4);
+    return (size_t)rows * (32 + parts_of(kScoreF32, cols, kFewVecs) * 8 + 2 * 1024 * 4);
 }
 
 // Gradients of this size and more are written past the caches, which would not hold them for the next reader either (256 MiB:
 // 124 us through the caches, 126 past them; 512 MiB 196 / 183; 1 GiB 553 / 515).
 constexpr u64 kPastBytes = (u64)384 << 20;
+
+// Rows of more parts than this take larger ones, and a launch that joins them.
+constexpr u64 kFewParts = 256;
+
+template <int KIND, int PV, bool PAST> static hipError_t launch_parts(const DistillArgs& a, void* scratch, hipStream_t st) {
+    const size_t lds = teacher_bytes(a.teacher.top);
+    const dim3 block(kPartThreads);
+    Parts p{};
+    p.parts = (u32)parts_of(KIND, a.cols, PV);
+    const u32 blocks = a.grad ? p.parts : 1;
+    p.taught = (double*)scratch;
+    double* const joined = p.taught + 2 * (u64)a.rows;
+    if (PV != kFewVecs) p.joined = joined;
+    p.part = (float*)(joined + 2 * (u64)a.rows);
+    p.q = p.part + (u64)a.rows * p.parts * 2;
+    p.z = p.q + (u64)a.rows * a.teacher.top;
+    hipLaunchKernelGGL((k_distill_stats<KIND, PV>), grid_of((u64)a.rows * (p.parts + 1)), block, lds, st, a, p);
+    if (p.joined) hipLaunchKernelGGL(k_distill_join, grid_of((u64)a.rows), dim3(1024), 0, st, a, p);
+    hipLaunchKernelGGL((k_distill_apply<KIND, PV, PAST>), grid_of((u64)a.rows * blocks), block, lds, st, a, p, blocks);
+    return hipGetLastError();
+}
 
 template <int KIND, bool PAST> static hipError_t launch_kind(const DistillArgs& a, void* scratch, hipStream_t st) {
     const size_t lds = teacher_bytes(a.teacher.top);
@@ -565,18 +607,9 @@ template <int KIND, bool PAST> static hipError_t launch_kind(const DistillArgs& 
         hipLaunchKernelGGL((k_distill_apply<KIND, kBackVecs, PAST>), grid_of((u64)a.rows * blocks), block, lds, st, a, Parts{}, blocks);
         return hipGetLastError();
     }
-    if (takes_parts(KIND, a.rows, a.cols)) {
-        Parts p{};
-        p.parts = (u32)parts_of(KIND, a.cols, kFewVecs);
-        const u32 blocks = a.grad ? p.parts : 1;
-        p.taught = (double*)scratch;
-        p.part = (float*)(p.taught + 2 * (u64)a.rows);
-        p.q = p.part + (u64)a.rows * p.parts * 2;
-        p.z = p.q + (u64)a.rows * a.teacher.top;
-        hipLaunchKernelGGL((k_distill_stats<KIND, kFewVecs>), grid_of((u64)a.rows * (p.parts + 1)), block, lds, st, a, p);
-        hipLaunchKernelGGL((k_distill_apply<KIND, kFewVecs, PAST>), grid_of((u64)a.rows * blocks), block, lds, st, a, p, blocks);
-        return hipGetLastError();
-    }
+    if (takes_parts(KIND, a.rows, a.cols))
+        return parts_of(KIND, a.cols, kFewVecs) <= kFewParts ? launch_parts<KIND, kFewVecs, PAST>(a, scratch, st)
+                                                             : launch_parts<KIND, kBackVecs, PAST>(a, scratch, st);
     const u64 vecs = ((u64)a.cols + kPer<KIND> - 1) / kPer<KIND>;
     const dim3 grid = grid_of((u64)a.rows);
     if (!a.grad && vecs > 64 * 16) {

@@ -1614,7 +1614,7 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
 
 }  // namespace
 
-// Rows of more outcomes than one workgroup takes.  (Shorter ones are not split however few there are: a split row takes 5
+// Rows of more outcomes than one workgroup takes.  (Shorter ones are not split however few there are: a split row takes 4
 // to 11 launches, 6 us each where it has nothing to do; 24 x 50021 f16 take 31 us in one.)
 static bool takes_parts(int64_t cols) { return cols > (int64_t)Shape<1024>::most; }
 

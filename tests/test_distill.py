@@ -346,6 +346,56 @@ def test_gradient_against_differences_of_the_loss(ctx):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 524288), (2, 524289), (1, 1048577), (2, 3000001)])
+def test_long_rows(src, rows, cols):
+    import torch
+    ctx = qb.Context(1, 1, ws_bytes=max(qb.qsv_workspace_bytes(1, 1), qb.qsv_distill_workspace_bytes(rows, cols)))
+    z, idx, logits = draw(src, rows, cols, 9, cols)
+    z[:, 5::7] = -INF
+    z[0, cols // 2:] = -INF
+    idx[:, 0] = cols - 1
+    idx[:, 1] = cols - 2
+    for r in range(rows):
+        z[r, torch.as_tensor(idx[r]).cuda()] = 0.25          # (no entry at a masked score)
+    ref = reference(f64(z), idx, logits, 0.8)
+    got = on_gpu(ctx, src, z, idx, logits, 0.8)
+    compare(src, got, ref)
+    compare(src, on_gpu(ctx, src, z, idx, logits, 0.8, grad=False), ref)
+    compare(src, on_gpu(ctx, src, z, idx, logits, 0.8, stats=got[2]), ref)
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_the_longest_row():
+    """2^30 scores, the gradient over them: few are not masked, and only there anything is written but 0."""
+    import torch
+    cols = 1 << 30
+    c = qb.Context(1, 1, ws_bytes=max(qb.qsv_workspace_bytes(1, 1), qb.qsv_distill_workspace_bytes(1, cols)))
+    z = torch.full((1, cols), -INF, device="cuda")
+    at = [0, 1, cols // 2 - 1, cols - 2, cols - 1]
+    v = np.array([0.5, -1.0, 2.0, 1.5, -0.25])
+    for k, x in zip(at, v):
+        z[0, k] = float(x)
+    idx, logits = np.array([[cols - 1, cols // 2 - 1]]), np.array([[0.0, 1.0]], dtype=np.float32)
+    loss, _, stats = on_gpu(c, "f32", z, idx, logits, grad=False)
+    p = np.exp(v - 2.0)
+    q = np.exp([0.0, 1.0]) / (1 + math.e)
+    want = (q * (np.log(q) - (v[[4, 2]] - 2.0 - math.log(p.sum())))).sum()
+    assert abs(loss[0] - want) <= 1e-6 and abs(stats[0, 1] - p.sum()) <= 1e-6
+    lo = torch.zeros(1, device="cuda")
+    c.qsv_distill(qb.QSV_S_F32, z, torch.as_tensor(idx).int().cuda(), torch.as_tensor(logits).cuda(), loss=lo, grad=z)
+    torch.cuda.synchronize()
+    g = p / p.sum()
+    g[4] -= q[0]
+    g[2] -= q[1]
+    assert abs(lo.item() - want) <= 1e-6
+    assert np.abs(np.array([z[0, k].item() for k in at]) - g).max() <= 1e-6
+    assert int(torch.count_nonzero(z).item()) == 5
+    c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows,cols", [(3, 40), (3, 40000), (200, 9000)])
 def test_lowest_and_highest_temperature(ctx, src, rows, cols):
     """At 2^100 all that is not masked is as likely; at 2^-100 the highest is certain, and the others are too far for any loss

@@ -302,6 +302,31 @@ def test_rows_of_near_equal_values(ctx, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+def test_the_longest_rows(src):
+    """Two rows of 2^30, more than 2^32 bytes to the second one's start; few scores are not masked."""
+    import torch
+    cols, stride = 1 << 30, (1 << 30) + 5
+    c = qb.Context(1, 1, ws_bytes=max(qb.qsv_workspace_bytes(1, 1), qb.qsv_sample_workspace_bytes(2, cols)))
+    flat = torch.full((2 * stride,), -np.inf, dtype=torch_type(src), device="cuda")
+    scores = flat[:2 * stride].view(2, stride)[:, :cols]
+    at = np.array([0, 3, cols // 3, cols - 2, cols - 1])
+    v = np.array([[0.5, -1.0, 2.0, 1.5, -0.25], [1.0, 1.0, -3.0, 0.75, 1.0]])
+    for r in range(2):
+        for k, x in zip(at, v[r]):
+            scores[r, int(k)] = float(x)
+    u = np.random.default_rng(3).random((2, 40))
+    for filters in ({}, dict(top_k=[3, 2]), dict(top_p=[0.9, 0.6]), dict(temperature=[0.0, 0.7])):
+        # the few among few (whose weights have more bits; no border is that near)
+        few = np.full((2, 6), -np.inf)
+        few[:, :5] = v
+        ref = reference(few, True, u, filters)
+        out = np.where(ref[0] >= 0, at[np.minimum(ref[0], 4)], -1)
+        same(on_gpu(c, src, scores, u, filters), (out, ref[1], ref[2]))
+    c.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("cols", [9000, 270000])
 @pytest.mark.parametrize("src,high,low", [("f32", 0x3b1fffff, 0xfffff), ("bf16", 0x3b1f, 0xf), ("f16", 0x18ff, 0x7)])
 def test_cuts_right_below_zero(ctx, src, high, low, cols):
