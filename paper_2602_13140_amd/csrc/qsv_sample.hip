@@ -64,6 +64,12 @@ template <int KIND> __device__ __forceinline__ float value_of(u32 k) {
     return __uint_as_float(KIND == kScoreBF16 ? (f ^ 0xffff0000u) : ~f);
 }
 
+// The lowest key of a value that is not below x.  (16 bits: x itself may lie between two, and its key then be the lower one's.)
+template <int KIND> __device__ __forceinline__ u32 key_from(float x) {
+    const u32 k = key_of<KIND>(x);
+    return kKeys16<KIND> && value_of<KIND>(k) < x ? k + 1u : k;
+}
+
 // ---- rows ------------------------------------------------------------------------------------------------------------
 // A row is read four values a lane in aligned vectors: vector j holds the values 4 j - skew .. 4 j - skew + 3, where skew
 // values lie between the last aligned address and the row's start.  Vectors that reach over an end are read value by value.
@@ -922,7 +928,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
             (void)weight_of(s, tables, value_of<KIND>(k), &n);
             return n >> shift;
         };
-        const u32 lowest_w = key_of<KIND>(from);
+        // (the steps of values below s.low_w may pass 0 and come out as high ones: 63 factors of two are few spacings of 16 bits at
+        // a low temperature)
+        const u32 lowest_w = key_from<KIND>(from);
         klo = first_key(lowest_w, kmax, [&](u32 k) { return bin(k) >= b; });
         khi = bin(kmax) == b ? kmax : first_key(klo, kmax, [&](u32 k) { return bin(k) > b; }) - 1u;
     }
@@ -974,8 +982,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
             u64 w[per];
             const u64 before = ordered(n, w);
             n = by_k ? min(n, (u32)((u64)p.top_k - at.count)) : reach(w, before, n, at.weight, mass_of(p.top_p, mass));
-            const u64 last = le[n > 0 ? n - 1 : 0];
-            cut = Cut{value_of<KIND>(~(u32)(last >> 32)), (u32)last};
+            cut = Cut{to, kAll};           // (an empty list: the row was written to while it was read)
+            if (n > 0) cut = Cut{value_of<KIND>(~(u32)(le[n - 1] >> 32)), (u32)le[n - 1]};
 #pragma unroll
             for (int i = 0; i < per; ++i) {
                 const u32 k = threadIdx.x * per + i;

@@ -348,6 +348,32 @@ def test_cuts_right_below_zero(ctx, src, high, low, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cols", [300, 1000, 8192, 9000, 60000, 270000])
+@pytest.mark.parametrize("src,m,t", [("bf16", 200.0, 0.11), ("bf16", 40.0, 0.028), ("bf16", -200.0, 0.1), ("bf16", 3e38, 1.3e35),
+                                     ("f16", 2000.0, 0.11), ("f16", 60000.0, 1.6), ("f16", -40.0, 0.002), ("f16", 4e-7, 4e-9)])
+def test_scores_whose_spacing_is_many_temperatures(ctx, src, m, t, cols):
+    """Two neighbouring scores of 16 bits lie so far apart that the next below the lowest with a weight is more than 63 factors of two
+    from the highest.  One of the highest, many one and two spacings below, and top-p without top-k: cuts in every one of them."""
+    import torch
+    g = np.random.default_rng(cols)
+    word = int(torch.tensor([m], dtype=torch_type(src)).view(torch.int16).item()) & 0xffff
+    down = lambda d: word - d if m > 0 else word + d  # noqa: E731
+    bits = np.full((6, cols), down(40) if m < 0 or word > 40 else 0)
+    bits[:, 7] = word
+    for d, many in ((1, 20), (2, 200), (3, 30), (5, 30)):
+        for r in range(6):
+            bits[r, 10 + g.permutation(cols - 10)[:min(many, cols // 8)]] = down(min(d, word - 1))
+    bits[1, 11] = bits[2, cols - 1] = word
+    z = torch.from_numpy(bits.astype(np.uint16).view(np.int16)).view(torch_type(src)).cuda()
+    for shots in (1, 40):
+        u = g.random((6, shots))
+        for top_p in ([0.999] * 6, [1 - 2.0 ** -20] * 6, [0.5, 0.9, 0.99, 0.9999, 0.99999, 0.0]):
+            for more in ({}, dict(min_p=[0.0, 1e-9, 1e-4, 0.0, 1e-30, 0.5])):
+                filters = dict(temperature=[t] * 6, top_p=top_p, **more)
+                same(on_gpu(ctx, src, z, u, filters), reference(values_of(src, z), True, u, filters))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src", ["f16", "f32"])
 def test_a_row_does_not_depend_on_its_alignment(ctx, src):
     import torch
