@@ -294,8 +294,8 @@ __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
             sum += some;
         }
     } else {
-        // the thread's own maximum so far, and the sum relative to it
-        sum = m > -kInf ? 1.f : 0.f;
+        // the thread's own maximum so far, and the sum relative to it: of one value 1, or 0 where that is -inf, or NaN (of +inf too)
+        sum = __builtin_amdgcn_exp2f((rest - (m > -kInf ? m : 0.f)) * c);
         for (u32 j = threadIdx.x; j < whole; j += 4 * NT) {
             vec y[4];
 #pragma unroll
@@ -317,7 +317,6 @@ __global__ __launch_bounds__(NT) void k_distill_row(const DistillArgs a) {
                 sum += some;
             }
         }
-        if (rest != rest) sum = rest;
         const float own = m;
         m = block_max<NT>(m, sm);
         if (own < m) sum *= __builtin_amdgcn_exp2f((own - m) * c);

@@ -302,6 +302,33 @@ def test_masks_and_odd_teachers(ctx, src, rows, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(9, 1003), (9, 4099), (9, 9003), (9, 33003), (130, 33003), (130, 132003)])
+@pytest.mark.parametrize("what", ["loss", "both"])
+def test_infinities_and_nan_wherever_they_stand(ctx, src, rows, cols, what):
+    """One +inf or NaN in a row's first value, a middle one, the last ones, which no whole vector has: loss, sum and gradient are
+    NaN, the gradient from the kept statistics as well; a row of them that has no entry stays at 0."""
+    z, idx, logits = draw(src, rows, cols, 4, 3)
+    z = z.clone()
+    for r, (k, v) in enumerate([(0, INF), (cols // 2, INF), (cols - 1, INF), (cols - 2, INF), (0, NAN), (cols // 2, NAN), (cols - 1, NAN),
+                                (cols - 3, NAN)]):
+        z[r, k] = v
+    z[8, -3:] = -INF
+    idx[:, 0] = 7
+    idx[2:4, 1:] = -1
+    ref = reference(f64(z), idx, logits)
+    assert np.isnan(ref[0][:8]).all() and np.isfinite(ref[0][8:]).all()
+    got = on_gpu(ctx, src, z, idx, logits, grad=what == "both")
+    compare(src, got, ref)
+    assert np.isnan(got[2][:8, 1]).all() and np.isfinite(got[2][8:]).all()
+    back = on_gpu(ctx, src, z, idx, logits, stats=got[2])
+    assert np.isnan(back[1][:8]).all() and np.isfinite(back[1][8:]).all()
+    idx[:8] = -1
+    got = on_gpu(ctx, src, z, idx, logits)
+    assert not got[0][:8].any() and not got[1][:8].any()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src,cols", [("bf16", 4001), ("f16", 30000), ("bf16", 60001), ("bf16", 131072), ("f32", 70003)])
 def test_gradients_larger_than_the_caches(ctx, src, cols):
     """Gradients of 384 MiB and more, which are written another way: the same bits as of two calls of half the rows, and of the
