@@ -146,18 +146,18 @@ template <int NT, int N> __device__ __forceinline__ void block_sums(double (&v)[
 
 // A row's teacher: idx, q and z of its entries in LDS, and their sums.
 struct Taught { double q, qx; };      // sum q, sum q (t / T - norm)
-struct TeacherLds { int* idx; float *q, *z; };
+struct TeacherLds { double* q; int* idx; float* z; };
 
 __device__ __forceinline__ TeacherLds teacher_lds(char* lds, int top) {
     const int room = (top + 3) & ~3;
     TeacherLds t;
-    t.idx = (int*)lds;
-    t.q = (float*)lds + room;
-    t.z = (float*)lds + 2 * room;
+    t.q = (double*)lds;
+    t.idx = (int*)(t.q + room);
+    t.z = (float*)(t.idx + room);
     return t;
 }
 
-inline size_t teacher_bytes(int top) { return (size_t)((top + 3) & ~3) * 12; }
+inline size_t teacher_bytes(int top) { return (size_t)((top + 3) & ~3) * 16; }
 
 // LISTED: `row` holds the scores at the entries, in their order.
 template <int KIND, int NT, bool LISTED = false> __device__ __forceinline__ Taught teach(const TeacherArgs& a, u64 r, const char* row, u32 cols, const TeacherLds& l, double* sm) {
@@ -171,7 +171,7 @@ template <int KIND, int NT, bool LISTED = false> __device__ __forceinline__ Taug
         const float t = logits[j];
         l.idx[j] = real ? i : -1;
         l.z[j] = real ? value_at<KIND>(row, LISTED ? (u32)j : (u32)i) : 0.f;
-        l.q[j] = t;
+        l.q[j] = (double)t;
         if (real) high = fmaxf(high, t);
     }
     double norm;
@@ -182,19 +182,19 @@ template <int KIND, int NT, bool LISTED = false> __device__ __forceinline__ Taug
         const double top = high > -kInf ? (double)high * a.inv_t : 0.0;
         double s[1] = {0.0};
         for (int j = threadIdx.x; j < a.top; j += NT)
-            if (l.idx[j] >= 0) s[0] += exp((double)l.q[j] * a.inv_t - top);
+            if (l.idx[j] >= 0) s[0] += exp(l.q[j] * a.inv_t - top);
         block_sums<NT, 1>(s, sm);
         norm = top + log(s[0]);              // no entry: -inf, and every q below 0
     }
     double v[2] = {0.0, 0.0};
     for (int j = threadIdx.x; j < a.top; j += NT) {
-        const double x = (double)l.q[j] * a.inv_t - norm;
-        const double q = l.idx[j] >= 0 && l.q[j] != -kInf ? exp(x) : 0.0;
+        const double x = l.q[j] * a.inv_t - norm;
+        const double q = l.idx[j] >= 0 && l.q[j] != -(double)kInf ? exp(x) : 0.0;
         if (q != 0.0) {
             v[0] += q;
             v[1] += q * x;
         }
-        l.q[j] = (float)q;
+        l.q[j] = q;
     }
     block_sums<NT, 2>(v, sm);
     return Taught{v[0], v[1]};
@@ -204,7 +204,7 @@ template <int KIND, int NT, bool LISTED = false> __device__ __forceinline__ Taug
 template <int NT> __device__ __forceinline__ double below_top(const TeacherLds& l, int top, float m, double inv_t) {
     double v = 0.0;
     for (int j = threadIdx.x; j < top; j += NT)
-        if (l.q[j] != 0.f) v += l.z[j] == -kInf ? -(double)kInf : (double)l.q[j] * (((double)l.z[j] - (double)m) * inv_t);
+        if (l.q[j] != 0.0) v += l.z[j] == -kInf ? -(double)kInf : l.q[j] * (((double)l.z[j] - (double)m) * inv_t);
     return v;
 }
 
@@ -237,7 +237,7 @@ template <int KIND, int NT> __device__ __forceinline__ void write_entries(const 
     for (int j = threadIdx.x; j < top; j += NT) {
         const int k = l.idx[j];
         if (k < 0 || (u32)k < k0 || (u32)k >= k1) continue;
-        double q = (double)l.q[j];
+        double q = l.q[j];
         bool first = true;
 #pragma unroll 4
         for (int i = 0; i < top; i += 4) {
@@ -247,7 +247,7 @@ template <int KIND, int NT> __device__ __forceinline__ void write_entries(const 
             for (int u = 0; u < 4; ++u)
                 if (x[u] == k && i + u != j) {
                     if (i + u < j) first = false;
-                    q += (double)l.q[i + u];
+                    q += l.q[i + u];
                 }
         }
         if (first) store_one<KIND>(grad, (u32)k, (float)((double)(e_of(g, l.z[j]) * g.scale) - q * (double)g.of_q));
@@ -359,7 +359,8 @@ struct Parts {
     u32 parts;
     double* taught;       // [rows][2]: sum q, sum q (t / T - norm)
     float* part;          // [rows][parts][2]: maximum, sum relative to it
-    float *q, *z;         // [rows][top]: of the teacher's entries, and the scores there
+    double* q;            // [rows][top]: of the teacher's entries
+    float* z;             // [rows][top]: the scores there
     double* joined;       // [rows][2]: the whole row's maximum and sum, or NULL: every part joins the parts' by itself
 };
 
@@ -526,17 +527,17 @@ __global__ __launch_bounds__(256) void k_distill_state(const float2* A, int n, T
     double loss[1] = {0.0};
     for (int j = threadIdx.x; j < te.top; j += 256) {
         const int k = l.idx[j];
-        if (k < 0 || l.q[j] == 0.f) continue;
+        if (k < 0 || l.q[j] == 0.0) continue;
         const float2 z = a[k];
         const double pk = (double)z.x * z.x + (double)z.y * z.y;
-        loss[0] -= (double)l.q[j] * log(pk);
+        loss[0] -= l.q[j] * log(pk);
         if (!lambda) continue;
         double q = 0.0;
         bool once = true;
         for (int i = 0; i < te.top; ++i)
             if (l.idx[i] == k) {
-                if (i < j && l.q[i] != 0.f) { once = false; break; }
-                q += (double)l.q[i];
+                if (i < j && l.q[i] != 0.0) { once = false; break; }
+                q += l.q[i];
             }
         if (once) {
             const double by = pk >= 0x1p-252 ? -q / pk : 0.0;      // (lambda of lower amplitudes would leave the range of 32 bits)
@@ -570,7 +571,7 @@ static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 12
 
 size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || !takes_parts(kScoreF32, rows, cols)) return 0;
-    return (size_t)rows * (32 + parts_of(kScoreF32, cols, kFewVecs) * 8 + 2 * 1024 * 4);
+    return (size_t)rows * (32 + parts_of(kScoreF32, cols, kFewVecs) * 8 + 1024 * (8 + 4));
 }
 
 // Gradients of this size and more are written past the caches, which would not hold them for the next reader either (256 MiB:
@@ -590,9 +591,9 @@ template <int KIND, int PV, bool PAST> static hipError_t launch_parts(const Dist
     p.taught = (double*)scratch;
     double* const joined = p.taught + 2 * (u64)a.rows;
     if (PV != kFewVecs) p.joined = joined;
-    p.part = (float*)(joined + 2 * (u64)a.rows);
-    p.q = p.part + (u64)a.rows * p.parts * 2;
-    p.z = p.q + (u64)a.rows * a.teacher.top;
+    p.q = joined + 2 * (u64)a.rows;
+    p.part = (float*)(p.q + (u64)a.rows * a.teacher.top);
+    p.z = p.part + (u64)a.rows * p.parts * 2;
     hipLaunchKernelGGL((k_distill_stats<KIND, PV>), grid_of((u64)a.rows * (p.parts + 1)), block, lds, st, a, p);
     if (p.joined) hipLaunchKernelGGL(k_distill_join, grid_of((u64)a.rows), dim3(1024), 0, st, a, p);
     hipLaunchKernelGGL((k_distill_apply<KIND, PV, PAST>), grid_of((u64)a.rows * blocks), block, lds, st, a, p, blocks);

@@ -329,6 +329,42 @@ def test_infinities_and_nan_wherever_they_stand(ctx, src, rows, cols, what):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(1, 1000), (3, 40000), (200, 9000), (1, 600000)])
+def test_loss_of_a_student_near_its_teacher(ctx, rows, cols):
+    """The student gives the teacher's entries nearly the teacher's own small probabilities: the terms are q (some 30 less some 30),
+    and their difference 2^-10.  What is in 64 bits keeps 2^-50 of each of the two, and the sum s = 1 + sum e is off by the errors
+    of e, 2^-16 of e at most at such distances."""
+    import torch
+    g = np.random.default_rng(cols)
+    z = torch.full((rows, cols), -INF, device="cuda")
+    z[:, 0] = 0.0
+    idx = np.stack([1 + g.permutation(cols - 1)[:5] for _ in range(rows)])
+    zt = g.uniform(-40, -25, (rows, 5)).astype(np.float32)
+    logits = (zt + np.float32(2.0 ** -10)).astype(np.float32)
+    for r in range(rows):
+        z[r, torch.as_tensor(idx[r]).cuda()] = torch.as_tensor(zt[r]).cuda()
+    lse = np.zeros(rows, dtype=np.float32)
+    got = on_gpu(ctx, "f32", z, idx, logits, lse=lse, grad=False)[0]
+    q, e = np.exp(logits.astype(np.float64)), np.exp(zt.astype(np.float64))
+    want = (q * (logits.astype(np.float64) - zt + np.log1p(e.sum(1, keepdims=True)))).sum(1)
+    tol = 2.0 ** -24 * want + (q * 160).sum(1) * 2.0 ** -50 + q.sum(1) * e.sum(1) * 2.0 ** -16
+    assert np.all(np.abs(got - want) <= tol), np.abs(got - want) / want
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(1, 1000), (3, 40000), (200, 9000)])
+def test_an_unlikely_entry_that_the_student_excludes(ctx, rows, cols):
+    """q = exp(-110) is less than float32 holds, and not 0."""
+    z, idx, logits = draw("f32", rows, cols, 3, 1)
+    z = z.clone()
+    z[:, 5] = -INF
+    idx[:] = [5, 6, 7]
+    logits[:] = [-110.0, 0.0, 1.0]
+    got = on_gpu(ctx, "f32", z, idx, logits, lse=np.full(rows, 2.0, dtype=np.float32))
+    assert np.all(got[0] == INF) and np.isfinite(got[1]).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src,cols", [("bf16", 4001), ("f16", 30000), ("bf16", 60001), ("bf16", 131072), ("f32", 70003)])
 def test_gradients_larger_than_the_caches(ctx, src, cols):
     """Gradients of 384 MiB and more, which are written another way: the same bits as of two calls of half the rows, and of the
