@@ -358,7 +358,7 @@ constexpr int kPartThreads = 256;
 struct Parts {
     u32 parts;
     double* taught;       // [rows][2]: sum q, sum q (t / T - norm)
-    float* part;          // [rows][parts][2]: maximum, sum relative to it
+    double* part;         // [rows][parts][2]: maximum, sum relative to it
     double* q;            // [rows][top]: of the teacher's entries
     float* z;             // [rows][top]: the scores there
     double* joined;       // [rows][2]: the whole row's maximum and sum, or NULL: every part joins the parts' by itself
@@ -410,8 +410,8 @@ template <int KIND, int PV> __global__ __launch_bounds__(kPartThreads) void k_di
     double s[1] = {(double)sum};
     block_sums<kPartThreads, 1>(s, sm);
     if (threadIdx.x == 0) {
-        p.part[(r * p.parts + at) * 2] = m;
-        p.part[(r * p.parts + at) * 2 + 1] = (float)s[0];
+        p.part[(r * p.parts + at) * 2] = (double)m;
+        p.part[(r * p.parts + at) * 2 + 1] = s[0];
     }
 }
 
@@ -420,13 +420,13 @@ __global__ __launch_bounds__(1024) void k_distill_join(const DistillArgs a, cons
     __shared__ double sm[16];
     const u64 r = grid_block();
     if (r >= (u64)a.rows) return;
-    const float* part = p.part + r * p.parts * 2;
+    const double* part = p.part + r * p.parts * 2;
     float m = -kInf;
-    for (u32 i = threadIdx.x; i < p.parts; i += 1024) m = fmaxf(m, part[2 * i]);
+    for (u32 i = threadIdx.x; i < p.parts; i += 1024) m = fmaxf(m, (float)part[2 * i]);
     m = block_max<1024>(m, sm);
     double s[1] = {0.0};
     for (u32 i = threadIdx.x; i < p.parts; i += 1024)
-        if (part[2 * i + 1] != 0.f) s[0] += (double)part[2 * i + 1] * exp(((double)part[2 * i] - (double)m) * a.teacher.inv_t);
+        if (part[2 * i + 1] != 0.0) s[0] += part[2 * i + 1] * exp((part[2 * i] - (double)m) * a.teacher.inv_t);
     block_sums<1024, 1>(s, sm);
     if (threadIdx.x == 0) { p.joined[2 * r] = (double)m; p.joined[2 * r + 1] = s[0]; }
 }
@@ -458,7 +458,7 @@ template <int KIND, int PV, bool PAST> __global__ __launch_bounds__(kPartThreads
         m = a.stats[2 * r];
         s[0] = (double)a.stats[2 * r + 1];
     } else {
-        const float* part = p.part + r * p.parts * 2;
+        const double* part = p.part + r * p.parts * 2;
         t = Taught{p.taught[2 * r], p.taught[2 * r + 1]};
         if (threadIdx.x < ((top + 3) & ~3) - top) l.idx[top + threadIdx.x] = -1;
         for (int j = threadIdx.x; j < top; j += kPartThreads) {
@@ -472,12 +472,12 @@ template <int KIND, int PV, bool PAST> __global__ __launch_bounds__(kPartThreads
             s[0] = p.joined[2 * r + 1];
         } else {                           // few: each wavefront for itself
             const u32 lane = threadIdx.x & 63;
-            for (u32 i = lane; i < p.parts; i += 64) m = fmaxf(m, part[2 * i]);
+            for (u32 i = lane; i < p.parts; i += 64) m = fmaxf(m, (float)part[2 * i]);
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
             m = uniform(m);
             for (u32 i = lane; i < p.parts; i += 64)
-                if (part[2 * i + 1] != 0.f) s[0] += (double)part[2 * i + 1] * exp(((double)part[2 * i] - (double)m) * a.teacher.inv_t);
+                if (part[2 * i + 1] != 0.0) s[0] += part[2 * i + 1] * exp((part[2 * i] - (double)m) * a.teacher.inv_t);
             s[0] = uniform(wave_sum(s[0]));
         }
         __syncthreads();
@@ -571,7 +571,7 @@ static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 12
 
 size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
     if (rows < 1 || !takes_parts(kScoreF32, rows, cols)) return 0;
-    return (size_t)rows * (32 + parts_of(kScoreF32, cols, kFewVecs) * 8 + 1024 * (8 + 4));
+    return (size_t)rows * (32 + parts_of(kScoreF32, cols, kFewVecs) * 16 + 1024 * (8 + 4));
 }
 
 // Gradients of this size and more are written past the caches, which would not hold them for the next reader either (256 MiB:
@@ -592,8 +592,8 @@ template <int KIND, int PV, bool PAST> static hipError_t launch_parts(const Dist
     double* const joined = p.taught + 2 * (u64)a.rows;
     if (PV != kFewVecs) p.joined = joined;
     p.q = joined + 2 * (u64)a.rows;
-    p.part = (float*)(p.q + (u64)a.rows * a.teacher.top);
-    p.z = p.part + (u64)a.rows * p.parts * 2;
+    p.part = p.q + (u64)a.rows * a.teacher.top;
+    p.z = (float*)(p.part + (u64)a.rows * p.parts * 2);
     hipLaunchKernelGGL((k_distill_stats<KIND, PV>), grid_of((u64)a.rows * (p.parts + 1)), block, lds, st, a, p);
     if (p.joined) hipLaunchKernelGGL(k_distill_join, grid_of((u64)a.rows), dim3(1024), 0, st, a, p);
     hipLaunchKernelGGL((k_distill_apply<KIND, PV, PAST>), grid_of((u64)a.rows * blocks), block, lds, st, a, p, blocks);

@@ -365,6 +365,26 @@ def test_an_unlikely_entry_that_the_student_excludes(ctx, rows, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(2, 40960), (130, 40960), (1, 614400)])
+def test_sums_of_parts(rows, cols):
+    """s = the ones, one in 2048, and the others at exp(-25) = 2^-36: 2^-25 of the ones together, which 32 bits do not hold beside
+    them.  A thread loses the 15 at most that it adds to a one of its own.  The entry's q is 1 / s but for what 64 bits lose, and the
+    loss q (ln q - ln p) what the kernel's s is off."""
+    import torch
+    ctx = qb.Context(1, 1, ws_bytes=max(qb.qsv_workspace_bytes(1, 1), qb.qsv_distill_workspace_bytes(rows, cols)))
+    z = torch.full((rows, cols), -25.0, device="cuda")
+    z[:, ::2048] = 0.0
+    ones = cols // 2048
+    s = ones * (1.0 + 2047 * math.exp(-25.0))
+    lse = np.float32(math.log(s))
+    t = np.float32(float(lse) - math.log(s))
+    want = math.exp(float(t) - float(lse)) * ((float(t) - float(lse)) + math.log(s))
+    got = on_gpu(ctx, "f32", z, np.zeros((rows, 1)), np.full((rows, 1), t), lse=np.full(rows, lse), grad=False)[0]
+    ctx.close()
+    assert np.abs(got - want).max() <= 2.0 ** -31 / s, (got[0] * s, want * s)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src,cols", [("bf16", 4001), ("f16", 30000), ("bf16", 60001), ("bf16", 131072), ("f32", 70003)])
 def test_gradients_larger_than_the_caches(ctx, src, cols):
     """Gradients of 384 MiB and more, which are written another way: the same bits as of two calls of half the rows, and of the
