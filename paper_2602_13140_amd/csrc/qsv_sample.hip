@@ -930,7 +930,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
         };
         // (the steps of values below s.low_w may pass 0 and come out as high ones: 63 factors of two are few spacings of 16 bits at
         // a low temperature)
-        const u32 lowest_w = key_from<KIND>(from);
+        const u32 lowest_w = uniform(key_from<KIND>(from));
         klo = first_key(lowest_w, kmax, [&](u32 k) { return bin(k) >= b; });
         khi = bin(kmax) == b ? kmax : first_key(klo, kmax, [&](u32 k) { return bin(k) > b; }) - 1u;
     }
@@ -982,8 +982,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
             u64 w[per];
             const u64 before = ordered(n, w);
             n = by_k ? min(n, (u32)((u64)p.top_k - at.count)) : reach(w, before, n, at.weight, mass_of(p.top_p, mass));
-            cut = Cut{to, kAll};           // (an empty list: the row was written to while it was read)
-            if (n > 0) cut = Cut{value_of<KIND>(~(u32)(le[n - 1] >> 32)), (u32)le[n - 1]};
+            // (an empty list: the row was written to while it was read)
+            const u64 last = n > 0 ? le[n - 1] : (u64)~khi << 32 | kAll;
+            cut = Cut{value_of<KIND>(~(u32)(last >> 32)), (u32)last};
 #pragma unroll
             for (int i = 0; i < per; ++i) {
                 const u32 k = threadIdx.x * per + i;
