@@ -1474,7 +1474,7 @@ static qsv_status losses(qsv_ctx* ctx, const Objective& ob, const float2* A, int
     const int n = ctx->n;
     if (ob.kind == 3) {
         QSV_HIP(ctx, launch_distill_state(A, n, ob.teacher_of(sample0), rows, f + sample0 * (2 * P + 1) + 2 * P, 2 * P + 1,
-                                          nullptr, 0, ctx->stream),
+                                          nullptr, 0, ctx->stream, res, rowdep),
                 "distillation loss");
         return QSV_OK;
     }

@@ -515,7 +515,10 @@ template <int KIND, int PV, bool PAST> __global__ __launch_bounds__(kPartThreads
 // the entries, which reverse mode takes back.  (The derivative of the rows' norm is left out: no gate changes it.)  A row's
 // entries are few: a workgroup each, bound by the latency of gathering them.
 // lambda: NULL, or rows of 2^n that are zero, `per` rows apart, the first one `first` rows on.
-__global__ __launch_bounds__(256) void k_distill_state(const float2* A, int n, TeacherArgs te, u64 rows, double* f, u64 f_stride, float2* lambda, int per, int first) {
+// res: what the rounded scalars of a table's groups have made of a row's length; as a factor m of every p_k it would make the loss
+// wrong by -Q ln m, some 3e-8 a group, and is taken out (14 qubits, 40 layers of rotations: 4.0e-7 from 64 bits with it, 1.0e-7
+// without).  In lambda, which goes as 1 / a, it meets the inverse of itself in psi.
+__global__ __launch_bounds__(256) void k_distill_state(const float2* A, int n, TeacherArgs te, u64 rows, double* f, u64 f_stride, float2* lambda, int per, int first, Residues res, int rowdep) {
     extern __shared__ char lds[];
     __shared__ double sm[48];
     const u64 r = grid_block();
@@ -545,7 +548,14 @@ __global__ __launch_bounds__(256) void k_distill_state(const float2* A, int n, T
         }
     }
     block_sums<256, 1>(loss, sm);
-    if (threadIdx.x == 0 && f) f[r * f_stride] = t.q == 0.0 ? 0.0 : t.qx + loss[0];
+    double m = 1.0;
+    if (f && res.count) {
+        const double* e = res.table + ((rowdep ? r * (u64)res.stride : 0) + (u64)res.first) * 2;
+        for (int k = threadIdx.x & 63; k < res.count; k += 64) m *= e[2 * k] * e[2 * k] + e[2 * k + 1] * e[2 * k + 1];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m *= __shfl_xor(m, o, 64);
+    }
+    if (threadIdx.x == 0 && f) f[r * f_stride] = t.q == 0.0 ? 0.0 : t.qx + loss[0] + t.q * log(m);
 }
 
 // lambda's rows at zero, and (paired) psi beside them: rows 2r, 2r + 1.
@@ -641,10 +651,11 @@ hipError_t launch_distill(int kind, const DistillArgs& a, void* scratch, hipStre
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_distill_state(const float2* A, int n, const TeacherArgs& te, int64_t rows, double* f, int64_t f_stride, float2* S, int paired, hipStream_t st) {
+hipError_t launch_distill_state(const float2* A, int n, const TeacherArgs& te, int64_t rows, double* f, int64_t f_stride, float2* S, int paired, hipStream_t st,
+                                const Residues* res, int rowdep) {
     if (S) hipLaunchKernelGGL(k_distill_zero, grid_of((((u64)rows << n) + 255) / 256), dim3(256), 0, st, A, n, (u64)rows << n, S, paired);
     hipLaunchKernelGGL(k_distill_state, grid_of((u64)rows), dim3(256), teacher_bytes(te.top), st, A, n, te, (u64)rows, f, (u64)f_stride, S,
-                       paired ? 2 : 1, paired ? 1 : 0);
+                       paired ? 2 : 1, paired ? 1 : 0, res ? *res : Residues{nullptr, 0, 0, 0}, rowdep);
     return hipGetLastError();
 }
 

@@ -6,6 +6,8 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "qsv_kernels.h"
+
 namespace qsv {
 
 // What a row holds (the values of qsv_scores_kind).
@@ -58,7 +60,8 @@ hipError_t launch_distill(int kind, const DistillArgs& a, void* scratch, hipStre
 
 // Rows of 2^n amplitudes against a teacher (its arrays start at the first of them): the loss of row r to f[r * f_stride]
 // (f may be NULL), and, where S is not NULL, lambda to S: row r, or (paired) psi to row 2r and lambda to row 2r + 1.
+// res, rowdep: see launch_expz_finish.
 hipError_t launch_distill_state(const float2* A, int n, const TeacherArgs& te, int64_t rows, double* f, int64_t f_stride,
-                                float2* S, int paired, hipStream_t st);
+                                float2* S, int paired, hipStream_t st, const Residues* res = nullptr, int rowdep = 0);
 
 }  // namespace qsv

@@ -642,6 +642,45 @@ def test_circuit(oracle, n, B, L, rot, ent, reup, mode):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,B,L,opts", [(14, 4, 40, {}), (13, 12, 64, {"grad_chunk_rows": 5}), (12, 12, 64, {}), (15, 12, 64, {}),
+                                        (16, 3, 40, {"tile_log2": 10})])
+@pytest.mark.parametrize("reup", [0, 1])
+def test_circuit_losses_without_the_rounding_of_their_scalars(oracle, n, B, L, opts, reup):
+    """Rotations of 10 qubits about one axis, no entangler, no amplitude where another qubit reads 1, and a teacher that gives each of
+    the 1024 outcomes its own probability: the loss is what the state's length is off.  A rotation rounds an amplitude 1.5
+    times (three multiply-adds for two), up or down as it comes, by 5e-8 of 2^-5 at one standard deviation; so the length is off
+    by 2 * 5e-8 sqrt(10 L) 2^-5, and four times that is the tolerance.  The scalar that a group of unitaries shares makes all
+    amplitudes longer or shorter, by 3e-8 a group, of which there are dozens."""
+    torch = gu.torch_cuda()
+    spec = wl.CircuitSpec(L, () if reup else (RY,), NONE, reup)
+    circ, P = qb.circuit_from_spec(spec), spec.num_params(n)
+    g = np.random.default_rng(n)
+    still = g.permutation(n)[:n - 10]
+    live = np.flatnonzero((np.arange(1 << n) & sum(1 << int(q) for q in still)) == 0)
+    x = np.zeros((B, 1 << n), dtype=np.float32)
+    x[:, live] = g.standard_normal((B, 1024))
+    f = g.standard_normal((B, n)).astype(np.float32)
+    p = (g.random((L, n)) * 6.0).astype(np.float32)
+    p[:, still] = 0.0
+    p = p.reshape(-1)
+    s, _ = oracle.amp_encode(x, n)
+    oracle.apply_layers(s, oracle.make_circuit(L, list(spec.rot), NONE, reup), p, f if reup else None)
+    top = (np.abs(s) ** 2).reshape(B, -1)[:, live]
+    logits = np.log(top).astype(np.float32)
+    want = (np.exp(logits.astype(np.float64)) * (logits - np.log(top))).sum(1)
+    c = gu.make_ctx(n, B, ws_bytes=qb.qsv_grad_workspace_bytes(n, B, circ))
+    for k, v in opts.items():
+        c.qsv_set_option(k, v)
+    loss, grad = torch.zeros(B, device="cuda"), torch.zeros((B, P), device="cuda")
+    c.qsv_distill_grad(circ, gu.dev(x), gu.dev(p), gu.dev(f) if reup else None, gu.dev(np.tile(live, (B, 1)).astype(np.int32)), gu.dev(logits),
+                       loss, grad, top_lse=torch.zeros(B, device="cuda"))
+    torch.cuda.synchronize()
+    c.close()
+    err = loss.cpu().numpy() - want
+    assert np.abs(err).max() <= 4 * 2 * 5e-8 * math.sqrt(10 * L) * 2.0 ** -5, err
+
+
+@pytest.mark.gpu
 def test_circuit_special_rows():
     """A teacher without entries, an outcome of amplitude 0, no layers; refusals that need a context."""
     import torch
