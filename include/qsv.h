@@ -348,7 +348,8 @@ typedef struct {
     int64_t grad_stride;         /* >= cols (any value for one row), in elements */
 } qsv_distill_req;
 
-/* Workspace size in bytes that qsv_distill needs for such rows, that of the plans included; 0 on bad arguments. */
+/* Workspace size in bytes that qsv_distill needs for such rows, that of the plans included; 0 on bad arguments.  (A call with
+ * have_stats = 1 needs none beside the plans'.) */
 size_t qsv_distill_workspace_bytes(int64_t rows, int64_t cols);
 qsv_status qsv_distill(qsv_ctx* ctx, const qsv_distill_req* req, const qsv_teacher* teacher);
 

@@ -1933,7 +1933,7 @@ qsv_status qsv_distill(qsv_ctx* ctx, const qsv_distill_req* req, const qsv_teach
     a.grad = req->grad_dev;
     a.grad_stride = req->rows > 1 ? req->grad_stride : req->cols;
     Arena ar(ctx);
-    void* scratch = ar.take(distill_scratch_bytes(req->rows, req->cols));
+    void* scratch = ar.take(req->have_stats ? 0 : distill_scratch_bytes(req->rows, req->cols));
     if (!scratch) return ws_fail(ctx, ar, "qsv_distill");
     QSV_HIP(ctx, launch_distill(req->kind, a, scratch, ctx->stream), "distill");
     return QSV_OK;

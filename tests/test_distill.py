@@ -499,6 +499,34 @@ def test_lowest_and_highest_temperature(ctx, src, rows, cols):
 
 
 @pytest.mark.gpu
+def test_the_backward_pass_needs_no_workspace():
+    """Rows whose forward pass needs more than the context's workspace; the gradient from kept statistics, over the scores."""
+    import torch
+    c = qb.Context(1, 1)
+    rows, cols = 127, (1 << 28) + (1 << 25) + 3
+    assert qb.qsv_distill_workspace_bytes(rows, cols) > qb.qsv_workspace_bytes(1, 1)
+    if torch.cuda.mem_get_info()[0] < rows * cols * 2 + (8 << 30):
+        pytest.skip("the device has not enough free memory")
+    z = torch.full((rows, cols), -INF, dtype=torch.bfloat16, device="cuda")
+    z[:, 5], z[:, cols - 1] = 1.0, 2.0
+    idx = torch.tensor([[cols - 1, 5]], dtype=torch.int32, device="cuda").repeat(rows, 1)
+    logits = torch.tensor([[0.0, 1.0]], device="cuda").repeat(rows, 1)
+    stats = torch.tensor([[2.0, 1 + math.exp(-1)]], device="cuda").repeat(rows, 1)
+    loss = torch.full((rows,), -7.0, device="cuda")
+    with pytest.raises(qb.QsvError) as refused:
+        c.qsv_distill(qb.QSV_S_BF16, z, idx, logits, loss=loss)
+    assert refused.value.status == qb.QSV_ERR_WORKSPACE
+    c.qsv_distill(qb.QSV_S_BF16, z, idx, logits, stats=stats, have_stats=1, grad=z)
+    torch.cuda.synchronize()
+    p, q = 1 / (1 + math.exp(-1)), 1 / (1 + math.e)
+    for r in (0, 64, rows - 1):
+        assert int(torch.count_nonzero(z[r]).item()) == 2
+        assert abs(z[r, cols - 1].item() - (p - q)) <= 2.0 ** -8 and abs(z[r, 5].item() - (q - p)) <= 2.0 ** -8
+    assert bool((loss == -7).all())
+    c.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src", ["f32", "bf16"])
 def test_a_row_does_not_depend_on_its_alignment(ctx, src):
     import torch
