@@ -245,7 +245,8 @@ typedef struct {
     int32_t* kept_dev;            /* int32 [rows] or NULL: the number of outcomes left */
 } qsv_sample_req;
 
-/* Workspace size in bytes that qsv_sample needs for such rows, that of the plans included; 0 on bad arguments. */
+/* Workspace size in bytes that qsv_sample needs for such rows, that of the plans included; 0 on bad arguments.  (Up to 32 shots
+ * a row need none beside the plans' up to 262144 outcomes.) */
 size_t qsv_sample_workspace_bytes(int64_t rows, int64_t cols);
 qsv_status qsv_sample(qsv_ctx* ctx, const qsv_sample_req* req);
 

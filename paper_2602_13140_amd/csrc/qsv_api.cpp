@@ -1054,7 +1054,7 @@ qsv_status qsv_measure_static(qsv_ctx* ctx, const qsv_measure_req* req) {
 // The workspace of qsv_sample behind the plans' region.
 size_t qsv_sample_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || rows > kMostRows || cols < 1 || cols > kMostCols) return 0;
-    return kOpsRegion + align_up(sample_scratch_bytes(rows, cols));
+    return kOpsRegion + align_up(sample_scratch_bytes(rows, cols, kMostShots));
 }
 
 qsv_status qsv_sample(qsv_ctx* ctx, const qsv_sample_req* req) {
@@ -1080,7 +1080,7 @@ qsv_status qsv_sample(qsv_ctx* ctx, const qsv_sample_req* req) {
     a.logp = req->logp_dev;
     a.kept = req->kept_dev;
     Arena ar(ctx);
-    void* scratch = ar.take(sample_scratch_bytes(req->rows, req->cols));
+    void* scratch = ar.take(sample_scratch_bytes(req->rows, req->cols, req->shots));
     if (!scratch) return ws_fail(ctx, ar, "qsv_sample");
     QSV_HIP(ctx, launch_sample_scores(req->kind, a, scratch, ctx->stream), "sample scores");
     return QSV_OK;

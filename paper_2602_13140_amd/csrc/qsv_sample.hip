@@ -1627,9 +1627,14 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
 // to 11 launches, 6 us each where it has nothing to do; 24 x 50021 f16 take 31 us in one.)
 static bool takes_parts(int64_t cols) { return cols > (int64_t)Shape<1024>::most; }
 
-size_t sample_scratch_bytes(int64_t rows, int64_t cols) {
+// More shots of a row than two for each of its wavefronts are drawn by another launch (6 x 66088 f32, 564 shots, wide nuclei:
+// 209 -> 56 us; for a shot or two the launch costs more).
+static bool drawn_later(int64_t shots) { return shots > 32; }
+
+size_t sample_scratch_bytes(int64_t rows, int64_t cols, int64_t shots) {
     if (rows < 1 || cols <= (int64_t)Shape<256>::most) return 0;
     if (takes_parts(cols)) return long_sizes(rows, cols).all;
+    if (!drawn_later(shots)) return 0;
     return (size_t)rows * (Shape<1024>::chunks * sizeof(u64) + sizeof(RowDraw));
 }
 
@@ -1680,9 +1685,7 @@ template <int KIND> static hipError_t launch_kind(const SampleArgs& a, void* scr
         hipLaunchKernelGGL((k_sample_row<KIND, 256>), grid, dim3(256), 0, st, a, later);
         return hipGetLastError();
     }
-    // More shots of a row than two for each of its wavefronts are drawn by another launch (6 x 66088 f32, 564 shots, wide
-    // nuclei: 209 -> 56 us; for a shot or two the launch costs more).
-    if (a.shots > 32) {
+    if (drawn_later(a.shots)) {
         later.chunk_w = (u64*)scratch;
         later.rows = (RowDraw*)(later.chunk_w + (u64)a.rows * Shape<1024>::chunks);
     }

@@ -29,8 +29,8 @@ struct SampleArgs {
     int* kept;                   // [rows] or NULL
 };
 
-// Bytes of workspace that launch_sample needs for such rows (0: none).
-size_t sample_scratch_bytes(int64_t rows, int64_t cols);
+// Bytes of workspace that launch_sample_scores needs for such rows (0: none).
+size_t sample_scratch_bytes(int64_t rows, int64_t cols, int64_t shots);
 hipError_t launch_sample_scores(int kind, const SampleArgs& a, void* scratch, hipStream_t st);
 
 // A teacher's top logits of a row, and what they make of it.

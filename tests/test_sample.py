@@ -460,6 +460,31 @@ def test_workspace_refused_before_anything_runs():
 
 
 @pytest.mark.gpu
+def test_few_shots_need_no_workspace():
+    """More rows than the context's workspace has room for the weights of, which only many shots need."""
+    import torch
+    c = qb.Context(1, 1)
+    rows, cols = 140000, 8200
+    assert qb.qsv_sample_workspace_bytes(rows, cols) > qb.qsv_workspace_bytes(1, 1)
+    z = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    at = torch.randint(0, cols, (rows, 1), generator=torch.Generator().manual_seed(4)).cuda()
+    z.scatter_(1, at, torch.tensor(40.0, dtype=torch.bfloat16, device="cuda").expand(rows, 1))
+    f = dict(top_p=torch.full((rows,), 0.5, device="cuda"))
+    kept = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    for shots, fits in ((1, True), (32, True), (33, False)):
+        out = torch.full((rows, shots), -7, dtype=torch.int64, device="cuda")
+        u = torch.rand((rows, shots), dtype=torch.float64, device="cuda")
+        if fits:
+            c.qsv_sample(qb.QSV_S_BF16, out, u, scores=z, kept=kept, **f)
+            assert bool((out == at).all()) and bool((kept == 1).all())
+        else:
+            with pytest.raises(qb.QsvError) as refused:
+                c.qsv_sample(qb.QSV_S_BF16, out, u, scores=z, **f)
+            assert refused.value.status == qb.QSV_ERR_WORKSPACE and bool((out == -7).all())
+    c.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("cols", [3000, 20000, 300000])
 def test_replays_of_a_captured_call(cols):
     """New scores and uniforms between the replays; eager calls of the same context in between."""
