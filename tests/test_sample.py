@@ -374,6 +374,26 @@ def test_scores_whose_spacing_is_many_temperatures(ctx, src, m, t, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cols", [40, 300, 9000, 270000])
+def test_probabilities_over_the_whole_range_at_high_temperatures(ctx, cols):
+    """Values from the smallest number that float32 holds to the largest, 2^277 apart: at T = 8 the lowest still weigh 2^-35."""
+    import torch
+    g = np.random.default_rng(cols)
+    v = np.exp2(g.uniform(-149, 127.9, (6, cols))).astype(np.float32)
+    v[:, 0], v[:, 1], v[:, 2] = 2.0 ** -149, 3e38, 2.0 ** -120
+    v[1, 3:] = 2.0 ** -149                        # all but three at the lowest
+    v[2, 3:] = 2.0 ** -110
+    z = torch.from_numpy(v).cuda()
+    t = [8.0, 8.0, 4.0, 5.5, 16.0, 1000.0]
+    for shots in (3, 40):
+        u = g.random((6, shots))
+        for filters in (dict(temperature=t), dict(temperature=t, top_p=[0.999, 0.9, 0.9999, 0.8, 0.5, 0.97]),
+                        dict(temperature=t, top_k=[cols - 1, 5, cols // 2, 0, 7, 30], top_p=[0.9999] * 6),
+                        dict(temperature=t, min_p=[1e-11, 1e-10, 1e-18, 0.01, 1e-6, 0.9])):
+            same(on_gpu(ctx, "probs", z, u, filters), reference(values_of("probs", z), False, u, filters))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src", ["f16", "f32"])
 def test_a_row_does_not_depend_on_its_alignment(ctx, src):
     import torch
