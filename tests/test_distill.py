@@ -709,6 +709,54 @@ def test_circuit_losses_without_the_rounding_of_their_scalars(oracle, n, B, L, o
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,B,L,rot,ent,reup,opts", [
+    (13, 5, 3, (RY, RZ), RING, 0, {"tile_log2": 10}),                                          # deferred CNOTs: passes with an index map
+    (13, 5, 3, (RY, RZ), RING, 0, {"tile_log2": 10, "split_streams": 1, "grad_chunk_rows": 2}),  # three chunks on two streams
+    (12, 6, 2, (RX, RY), LADDER, 1, {"split_streams": 1}),                                     # halves on two streams, tables of their own
+    (14, 3, 4, (RY, RX), RING, 1, {"tile_log2": 11, "split_streams": 1, "grad_chunk_rows": 1}),
+    (11, 4, 2, (RY, RZ), RING, 0, {"tile_log2": 10, "defer_cnots": 0}),
+    (10, 2100, 1, (RY,), RING, 0, {}),                                                         # 10 qubits in whole passes
+])
+def test_circuit_in_whole_passes_and_layer_by_layer(oracle, n, B, L, rot, ent, reup, opts):
+    """The loss and gradient of every sample the same both ways, and against the formulas for the first sample, one in the middle
+    and the last one."""
+    torch = gu.torch_cuda()
+    spec, g, params, x, feats, logits = case(n, B, L, rot, ent, reup, 90 + n, 5)
+    oc = oracle.make_circuit(L, list(rot), ent, reup)
+    s, _ = oracle.amp_encode(x, n)
+    oracle.apply_layers(s, oc, params, feats)
+    p = np.abs(s) ** 2
+    likely = np.argsort(-p, axis=1)[:, :(1 << n) // 4]
+    idx = np.stack([g.permutation(likely[b])[:5] for b in range(B)])
+    idx[B - 1, 2] = idx[B - 1, 1]
+    idx[0, 4] = -1
+    circ, P = qb.circuit_from_spec(spec), len(params)
+    got = []
+    for o in (opts, {"naive": 1}):
+        c = gu.make_ctx(n, B, ws_bytes=qb.qsv_grad_workspace_bytes(n, B, circ))
+        for k, v in o.items():
+            c.qsv_set_option(k, v)
+        loss, grad = torch.zeros(B, device="cuda"), torch.zeros((B, P), device="cuda")
+        for _ in range(2):
+            loss.fill_(7.0), grad.fill_(7.0)
+            c.qsv_distill_grad(circ, gu.dev(x), gu.dev(params), gu.dev(feats) if reup else None, gu.dev(idx.astype(np.int32)),
+                               gu.dev(logits), loss, grad, temperature=1.3)
+            torch.cuda.synchronize()
+            got.append((loss.cpu().numpy(), grad.cpu().numpy()))
+        c.close()
+    assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
+    at = sorted({0, B // 2, B - 1})
+    ref = circuit_reference(oracle, spec, n, x[at], params, None if feats is None else feats[at], idx[at], logits[at], 1.3, None)
+    for l, gr in got:
+        assert np.all(np.abs(l[at] - ref[0]) <= ref[2] + 1e-5)
+        assert np.all(np.abs(gr[at] - ref[1]).max(axis=1) <= ref[2] + 1e-5)
+    # (each way is off by the tolerance of the formulas' test at most)
+    pk = np.take_along_axis(p.reshape(B, -1), idx.clip(0), 1)
+    tol = 2 * (2 * 3e-7 * (0.5 / pk + 1 / np.sqrt(pk)).max(1) + 1e-6 + 1e-5)
+    assert np.all(np.abs(got[0][0] - got[2][0]) <= tol) and np.all(np.abs(got[0][1] - got[2][1]).max(1) <= tol)
+
+
+@pytest.mark.gpu
 def test_circuit_special_rows():
     """A teacher without entries, an outcome of amplitude 0, no layers; refusals that need a context."""
     import torch
