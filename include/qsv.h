@@ -358,7 +358,10 @@ qsv_status qsv_distill(qsv_ctx* ctx, const qsv_distill_req* req, const qsv_teach
  * (outcomes 0..2^n-1; teacher arrays of batch rows), and optionally their batch means, in reverse mode as qsv_loss_grad:
  *   p_k = |a_k|^2 of the encoded sample's final state,   loss_b = sum_j q_j (ln q_j - ln p_{i_j}).
  * The teacher's temperature softens q alone.  An entry with q > 0 at an outcome of amplitude 0 makes the loss +inf; one at
- * an amplitude below 2^-126 adds nothing to the gradient.  Arguments as qsv_param_shift_grad; teacher is a host struct read during the call. */
+ * an amplitude below 2^-126 adds nothing to the gradient.  Arguments as qsv_param_shift_grad; teacher is a host struct read during the call.
+ * qsv_distill_grad_workspace_bytes: the workspace with which this call works as qsv_loss_grad does with
+ * qsv_grad_workspace_bytes, a state per sample more; with less it still works, layer by layer.  Returns 0 on bad arguments. */
+size_t qsv_distill_grad_workspace_bytes(int n_qubits, int batch, const qsv_circuit* c);
 qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_dev, int64_t dim,
                             const float* params_dev, const float* feats_dev, const qsv_teacher* teacher,
                             float* loss_dev, float* grad_dev, float* mean_loss_dev, float* mean_grad_dev);

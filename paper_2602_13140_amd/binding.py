@@ -125,6 +125,8 @@ def load():
     L.qsv_distill_workspace_bytes.argtypes = [i64, i64]
     L.qsv_distill.restype = i32
     L.qsv_distill.argtypes = [vp, ctypes.POINTER(qsv_distill_req), ctypes.POINTER(qsv_teacher)]
+    L.qsv_distill_grad_workspace_bytes.restype = ctypes.c_size_t
+    L.qsv_distill_grad_workspace_bytes.argtypes = [i32, i32, ctypes.POINTER(qsv_circuit)]
     L.qsv_distill_grad.restype = i32
     L.qsv_distill_grad.argtypes = [vp, ctypes.POINTER(qsv_circuit), vp, i64, vp, vp, ctypes.POINTER(qsv_teacher),
                                    vp, vp, vp, vp]
@@ -178,6 +180,10 @@ def qsv_sample_workspace_bytes(rows, cols):
 
 def qsv_distill_workspace_bytes(rows, cols):
     return int(load().qsv_distill_workspace_bytes(rows, cols))
+
+
+def qsv_distill_grad_workspace_bytes(n, batch, circ):
+    return int(load().qsv_distill_grad_workspace_bytes(n, batch, ctypes.byref(circ)))
 
 
 def qsv_plan_describe(circ, n, batch=1, inverse=0, tile_log2=0):

@@ -756,6 +756,37 @@ def test_circuit_in_whole_passes_and_layer_by_layer(oracle, n, B, L, rot, ent, r
     assert np.all(np.abs(got[0][0] - got[2][0]) <= tol) and np.all(np.abs(got[0][1] - got[2][1]).max(1) <= tol)
 
 
+def test_the_circuits_workspace():
+    c = qb.make_circuit(6, [RY, RZ], RING)
+    for n, B in ((4, 3), (22, 2)):
+        more = qb.qsv_distill_grad_workspace_bytes(n, B, c) - qb.qsv_grad_workspace_bytes(n, B, c)
+        assert B * (8 << n) <= more < B * (8 << n) + 256
+    assert qb.qsv_distill_grad_workspace_bytes(0, 1, c) == 0 == qb.qsv_distill_grad_workspace_bytes(4, 1, qb.make_circuit(1, [9], 1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,B,L,ent", [(22, 2, 6, RING), (24, 2, 3, LADDER), (22, 4, 2, RING)])
+def test_circuit_workspace_for_whole_passes(n, B, L, ent):
+    """Circuits with as many passes as qsv_grad_workspace_bytes has states for: with one more a sample the call goes the way that it
+    goes with many more, bit by bit."""
+    import torch
+    spec = wl.CircuitSpec(L, (RY, RZ), ent, 0)
+    circ, P = qb.circuit_from_spec(spec), spec.num_params(n)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x, p = torch.randn((B, 1 << n), device="cuda", generator=g), torch.rand(P, device="cuda", generator=g)
+    idx = torch.randint(0, 1 << n, (B, 7), device="cuda", generator=g, dtype=torch.int32)
+    logits = torch.randn((B, 7), device="cuda", generator=g)
+    ws, got = qb.qsv_distill_grad_workspace_bytes(n, B, circ), []
+    for size in (ws, ws + (2 << 30)):
+        c = gu.make_ctx(n, B, ws_bytes=size)
+        loss, grad = torch.full((B,), 7.0, device="cuda"), torch.full((B, P), 7.0, device="cuda")
+        c.qsv_distill_grad(circ, x, p, None, idx, logits, loss, grad)
+        torch.cuda.synchronize()
+        got.append((loss.clone(), grad.clone()))
+        c.close()
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and bool(torch.isfinite(got[0][1]).all())
+
+
 @pytest.mark.gpu
 def test_circuit_special_rows():
     """A teacher without entries, an outcome of amplitude 0, no layers; refusals that need a context."""
