@@ -211,24 +211,35 @@ def _dtype(name):
     return _dtypes[name]
 
 
-def _rows(t, kind):
+def _need(ok, what):
+    if not ok:
+        raise QsvError(QSV_ERR_INVALID_ARG, what)
+
+
+def _rows(t, kind, dev, what):
     """Rows of scores: [rows][cols] of the kind's type, values of a row next to each other, any row stride."""
-    assert t.is_cuda and t.dim() == 2 and t.dtype is _dtype(_TYPE_OF[kind]) and (t.shape[1] == 1 or t.stride(1) == 1)
+    _need(kind in _TYPE_OF, "unknown kind of scores")
+    if not (t is not None and t.get_device() == dev and t.dim() == 2 and t.dtype is _dtype(_TYPE_OF[kind])
+            and (t.shape[1] == 1 or t.stride(1) == 1)):
+        _need(False, "%s must be rows of %s on cuda:%d, the values of a row next to each other" % (what, _TYPE_OF[kind], dev))
     return t
 
 
-def _flat(t, dtype, *shape):
-    """The address of a contiguous tensor of this type and shape; None stays None."""
+def _flat(t, dtype, dev, what, *shape):
+    """The address of a contiguous tensor of this type and shape (one number: any shape of as many); None stays None."""
     if t is None:
         return None
-    assert t.dtype is _dtype(dtype) and t.shape == shape and t.is_cuda and t.is_contiguous(), (dtype, shape)
+    if not (t.dtype is _dtype(dtype) and t.get_device() == dev and t.is_contiguous() and (t.shape == shape or shape == (t.numel(),))):
+        _need(False, "%s must be a contiguous tensor of %s %s on cuda:%d" % (what, dtype, list(shape), dev))
     return t.data_ptr()
 
 
-def _teacher(rows, top_idx, top_logits, temperature, top_lse):
+def _teacher(rows, top_idx, top_logits, temperature, top_lse, dev):
+    _need(top_idx is not None and top_idx.dim() == 2, "top_idx must be [rows][n_top]")
     top = top_idx.shape[1]
-    return qsv_teacher(top, 0, _flat(top_idx, "int32", rows, top), _flat(top_logits, "float32", rows, top),
-                       _flat(top_lse, "float32", rows), float(temperature))
+    return qsv_teacher(top, 0, _flat(top_idx, "int32", dev, "top_idx", rows, top),
+                       _flat(top_logits, "float32", dev, "top_logits", rows, top),
+                       _flat(top_lse, "float32", dev, "top_lse", rows), float(temperature))
 
 
 class Context:
@@ -312,23 +323,29 @@ class Context:
 
     def qsv_distill(self, kind, scores, top_idx, top_logits, temperature=1.0, top_lse=None, loss=None, stats=None,
                     have_stats=0, grad_loss=None, grad=None):
-        s = _rows(scores, kind)
+        d = self.dev.index
+        s = _rows(scores, kind, d, "scores")
         r = qsv_distill_req()
         r.kind, r.have_stats, r.scores_dev, r.row_stride = kind, have_stats, s.data_ptr(), s.stride(0)
         r.rows, r.cols = s.shape
-        r.loss_dev, r.stats_dev = _flat(loss, "float32", r.rows), _flat(stats, "float32", r.rows, 2)
-        r.grad_loss_dev = _flat(grad_loss, "float32", r.rows)
+        r.loss_dev, r.stats_dev = _flat(loss, "float32", d, "loss", r.rows), _flat(stats, "float32", d, "stats", r.rows, 2)
+        r.grad_loss_dev = _flat(grad_loss, "float32", d, "grad_loss", r.rows)
         if grad is not None:
-            assert _rows(grad, kind).shape == s.shape
+            _need(_rows(grad, kind, d, "grad").shape == s.shape, "grad must have the shape of the scores")
             r.grad_dev, r.grad_stride = grad.data_ptr(), grad.stride(0)
-        t = _teacher(r.rows, top_idx, top_logits, temperature, top_lse)
+        t = _teacher(r.rows, top_idx, top_logits, temperature, top_lse, d)
         self._check(self.L.qsv_distill(self.h, ctypes.byref(r), ctypes.byref(t)))
 
     def qsv_distill_grad(self, circ, x, params, feats, top_idx, top_logits, loss, grad, mean_loss=None, mean_grad=None,
                          temperature=1.0, top_lse=None):
-        t = _teacher(self.batch, top_idx, top_logits, temperature, top_lse)
-        self._check(self.L.qsv_distill_grad(self.h, ctypes.byref(circ), _ptr(x), x.shape[1], _ptr(params), _ptr(feats),
-                                            ctypes.byref(t), _ptr(loss), _ptr(grad), _ptr(mean_loss), _ptr(mean_grad)))
+        d, B, P = self.dev.index, self.batch, max(0, qsv_num_params(circ, self.n))       # (a bad circuit is the library's to refuse)
+        t = _teacher(B, top_idx, top_logits, temperature, top_lse, d)
+        _need(x is not None and x.dim() == 2, "x must be [batch][dim]")
+        at = (_flat(x, "float32", d, "x", B, x.shape[1]), x.shape[1], _flat(params, "float32", d, "params", P),
+              _flat(feats, "float32", d, "feats", B * self.n) if circ.reupload else None)
+        out = (_flat(loss, "float32", d, "loss", B), _flat(grad, "float32", d, "grad", B * P),
+               _flat(mean_loss, "float32", d, "mean_loss", 1), _flat(mean_grad, "float32", d, "mean_grad", P))
+        self._check(self.L.qsv_distill_grad(self.h, ctypes.byref(circ), *at, ctypes.byref(t), *out))
 
     def qsv_reset_fidelity(self, circ, params, feats, mask, x, out):
         self._check(self.L.qsv_reset_fidelity(self.h, ctypes.byref(circ), _ptr(params), _ptr(feats), mask,
@@ -339,23 +356,24 @@ class Context:
 
     def qsv_sample(self, kind, out, uniforms, scores=None, temperature=None, top_k=None, top_p=None, min_p=None,
                    logp=None, kept=None):
-        r = qsv_sample_req()
+        r, d = qsv_sample_req(), self.dev.index
         r.kind = kind
         if kind == QSV_S_STATE:
-            assert scores is None
+            _need(scores is None, "scores must be None for the context's state")
             r.rows, r.cols = self.batch, 1 << self.n
         else:
-            s = _rows(scores, kind)
+            s = _rows(scores, kind, d, "scores")
             r.scores_dev, r.rows, r.cols, r.row_stride = s.data_ptr(), s.shape[0], s.shape[1], s.stride(0)
+        _need(uniforms is not None and uniforms.dim() == 2, "uniforms must be [rows][shots]")
         r.shots = uniforms.shape[1]
-        r.temperature_dev = _flat(temperature, "float32", r.rows)
-        r.top_k_dev = _flat(top_k, "int32", r.rows)
-        r.top_p_dev = _flat(top_p, "float32", r.rows)
-        r.min_p_dev = _flat(min_p, "float32", r.rows)
-        r.uniforms_dev = _flat(uniforms, "float64", r.rows, r.shots)
-        r.out_dev = _flat(out, "int64", r.rows, r.shots)
-        r.logp_dev = _flat(logp, "float32", r.rows, r.shots)
-        r.kept_dev = _flat(kept, "int32", r.rows)
+        r.temperature_dev = _flat(temperature, "float32", d, "temperature", r.rows)
+        r.top_k_dev = _flat(top_k, "int32", d, "top_k", r.rows)
+        r.top_p_dev = _flat(top_p, "float32", d, "top_p", r.rows)
+        r.min_p_dev = _flat(min_p, "float32", d, "min_p", r.rows)
+        r.uniforms_dev = _flat(uniforms, "float64", d, "uniforms", r.rows, r.shots)
+        r.out_dev = _flat(out, "int64", d, "out", r.rows, r.shots)
+        r.logp_dev = _flat(logp, "float32", d, "logp", r.rows, r.shots)
+        r.kept_dev = _flat(kept, "int32", d, "kept", r.rows)
         self._check(self.L.qsv_sample(self.h, ctypes.byref(r)))
 
     def qsv_pauli_expect(self, out, xmask=0, ymask=0, zmask=0):

@@ -167,6 +167,34 @@ def test_layouts():
     assert 0 < qb.qsv_distill_workspace_bytes(4096, 131072) and 0 < qb.qsv_distill_workspace_bytes(1, 1 << 30)
 
 
+def test_tensors_that_the_binding_refuses():
+    """By their type, shape, order and device (-1 is the host), as every refusal is raised."""
+    import torch
+    here = -1
+    z = torch.zeros((3, 8))
+    assert qb._rows(z, qb.QSV_S_F32, here, "scores") is z and qb._rows(z[:, :5], qb.QSV_S_F32, here, "scores") is not None
+    assert qb._rows(torch.zeros((1, 3)).t(), qb.QSV_S_F32, here, "scores") is not None
+    for bad, dev in ((None, here), (z[0], here), (z.t(), here), (z[:, ::2], here), (z.half(), here), (z, 0)):
+        with pytest.raises(qb.QsvError, match="scores") as e:
+            qb._rows(bad, qb.QSV_S_F32, dev, "scores")
+        assert e.value.status == qb.QSV_ERR_INVALID_ARG
+    with pytest.raises(qb.QsvError, match="kind"):
+        qb._rows(z, qb.QSV_S_STATE, here, "scores")
+    assert qb._flat(None, "float32", here, "loss", 3) is None
+    assert qb._flat(z, "float32", here, "stats", 3, 8) == z.data_ptr() == qb._flat(z, "float32", here, "params", 24)
+    for bad, dev, shape in ((z, here, (3, 7)), (z, here, (8, 3)), (z, here, (23,)), (z.t(), here, (8, 3)), (z.double(), here, (3, 8)), (z, 1, (3, 8))):
+        with pytest.raises(qb.QsvError, match="stats"):
+            qb._flat(bad, "float32", dev, "stats", *shape)
+    idx = torch.zeros((3, 2), dtype=torch.int32)
+    assert qb._teacher(3, idx, torch.zeros((3, 2)), 1.0, None, here).n_top == 2
+    for i, t, lse in ((None, z, None), (idx[0], z, None), (idx.long(), z[:, :2].clone(), None), (idx, z, None), (idx, z[:, :2], None),
+                      (idx, z[:, :2].clone(), z[:2, 0].clone())):
+        with pytest.raises(qb.QsvError):
+            qb._teacher(3, i, t, 1.0, lse, here)
+    with pytest.raises(qb.QsvError, match="cuda:0"):
+        qb._teacher(3, idx, torch.zeros((3, 2)), 1.0, None, 0)
+
+
 # ---- on the GPU ------------------------------------------------------------------------------------------------------
 KIND = {"f32": qb.QSV_S_F32, "f16": qb.QSV_S_F16, "bf16": qb.QSV_S_BF16}
 
@@ -582,6 +610,37 @@ def test_refused_calls_leave_their_outputs(ctx):
             ctx.qsv_distill(qb.QSV_S_F32, z, ti, tl, loss=loss, **more)
     torch.cuda.synchronize()
     assert bool((loss == -7).all())
+
+
+@pytest.mark.gpu
+def test_tensors_refused_before_anything_runs(ctx):
+    """Host tensors, another type, too few results: refused with asserts left out as well, and nothing is written."""
+    import torch
+    z, idx, logits = torch.zeros((3, 20), device="cuda"), torch.zeros((3, 2), dtype=torch.int32, device="cuda"), torch.zeros((3, 2), device="cuda")
+    loss = torch.full((3,), -7.0, device="cuda")
+    for scores, more in ((z.cpu(), {}), (z.half(), {}), (z, dict(loss=loss[:2])), (z, dict(grad=z[:, :19])), (z, dict(stats=loss)),
+                         (z, dict(grad_loss=loss.cpu())), (z, dict(top_lse=loss.double()))):
+        with pytest.raises(qb.QsvError):
+            ctx.qsv_distill(qb.QSV_S_F32, scores, idx, logits, **dict(dict(loss=loss), **more))
+    out, u = torch.full((3, 1), -7, dtype=torch.int64, device="cuda"), torch.zeros((3, 1), dtype=torch.float64, device="cuda")
+    for more in (dict(scores=z.cpu()), dict(scores=None), dict(uniforms=u.cpu()), dict(uniforms=u.float()), dict(top_k=loss), dict(out=out[:2]),
+                 dict(temperature=loss[:2]), dict(kind=qb.QSV_S_STATE)):
+        with pytest.raises(qb.QsvError):
+            ctx.qsv_sample(**dict(dict(kind=qb.QSV_S_F32, out=out, uniforms=u, scores=z), **more))
+    c = qb.Context(2, 3)
+    circ = qb.make_circuit(1, [RY], NONE, 1)
+    good = dict(x=torch.ones((3, 4), device="cuda"), params=torch.zeros(4, device="cuda"), feats=torch.zeros((3, 2), device="cuda"), loss=loss,
+                grad=torch.full((3, 4), -7.0, device="cuda"))
+    for k, bad in (("x", good["x"].cpu()), ("x", good["x"].t()), ("params", good["params"][:3]), ("feats", good["feats"][:2]), ("feats", good["feats"].cpu()),
+                   ("loss", loss[:2]), ("grad", good["grad"][:, :3]), ("mean_grad", loss), ("mean_loss", loss)):
+        with pytest.raises(qb.QsvError):
+            c.qsv_distill_grad(circ, top_idx=idx, top_logits=logits, **dict(good, **{k: bad}))
+    torch.cuda.synchronize()
+    assert bool((loss == -7).all()) and bool((out == -7).all()) and bool((good["grad"] == -7).all())
+    c.qsv_distill_grad(circ, top_idx=idx, top_logits=logits, **good)
+    torch.cuda.synchronize()
+    assert bool((loss != -7).all())
+    c.close()
 
 
 # ---- a circuit's own outcomes ----------------------------------------------------------------------------------------
