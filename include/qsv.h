@@ -224,9 +224,9 @@ typedef enum {
  *                less than H, and the first one always (top_p >= 1: all).
  * The draw is QSV_M_SAMPLE's: W' the sum of w over what is left, r = floor(u 2^53), t = floor(r W' / 2^53), the smallest k
  * whose running sum in the order of the INDEX exceeds t.  e_k is taken in float64, so a result can differ from the
- * definition only where a value lies within about 2^-48 of a border; sums are of whole numbers, so a call's results do not
- * depend on how its work is split.  A row without an outcome, or with a parameter out of its range (NaN too), gives -1 for
- * every shot, logp -inf and kept 0; a uniform outside [0, 1) gives -1 and -inf for its shot. */
+ * definition only where a value lies within about 2^-48 (probabilities at T != 1: 2^-45 / T) of a border; sums are of whole
+ * numbers, so a call's results do not depend on how its work is split.  A row without an outcome, or with a parameter out of
+ * its range (NaN too), gives -1 for every shot, logp -inf and kept 0; a uniform outside [0, 1) gives -1 and -inf for its shot. */
 typedef struct {
     int32_t kind;                 /* qsv_scores_kind */
     int32_t reserved;             /* must be 0 */
@@ -329,8 +329,8 @@ typedef struct {
 /* Loss of rows of scores z of a student against a teacher's top logits, and its gradient:
  *   p = softmax(z / T),   loss = sum_j q_j (ln q_j - ln p_{i_j}),
  *   d loss / d z_k = g / T (Q p_k - sum over the entries j with i_j = k of q_j),   g = grad_loss (1 if NULL).
- * (No factor T^2 is put in: it can go into grad_loss.)  Scores of -inf are masked: p = 0; an entry with q > 0 there makes
- * the loss +inf.  A NaN or +inf among a row's scores makes its loss and gradient NaN.
+ * (No factor T^2 is put in: it can go into grad_loss.  g / T has to be in float32's range.)  Scores of -inf are masked: p = 0;
+ * an entry with q > 0 there makes the loss +inf.  A NaN or +inf among a row's scores makes its loss and gradient NaN, unless the row has no entry.
  * stats: [rows][2], the row's highest score m and the sum of exp((z - m) / T); written when have_stats = 0, and read instead
  * of being worked out when have_stats = 1, which is the backward pass by itself (loss_dev must be NULL then).
  * The gradient has the type of the scores, rounded once, and may be written over them (the same address and row stride);
@@ -358,7 +358,8 @@ qsv_status qsv_distill(qsv_ctx* ctx, const qsv_distill_req* req, const qsv_teach
  * (outcomes 0..2^n-1; teacher arrays of batch rows), and optionally their batch means, in reverse mode as qsv_loss_grad:
  *   p_k = |a_k|^2 of the encoded sample's final state,   loss_b = sum_j q_j (ln q_j - ln p_{i_j}).
  * The teacher's temperature softens q alone.  An entry with q > 0 at an outcome of amplitude 0 makes the loss +inf; one at
- * an amplitude below 2^-126 adds nothing to the gradient.  Arguments as qsv_param_shift_grad; teacher is a host struct read during the call.
+ * an amplitude below 2^-126 adds nothing to the gradient.  Arguments as qsv_param_shift_grad; teacher is a host struct read
+ * during the call.
  * qsv_distill_grad_workspace_bytes: the workspace with which this call works as qsv_loss_grad does with
  * qsv_grad_workspace_bytes, a state per sample more; with less it still works, layer by layer.  Returns 0 on bad arguments. */
 size_t qsv_distill_grad_workspace_bytes(int n_qubits, int batch, const qsv_circuit* c);

@@ -576,7 +576,9 @@ static u64 parts_of(int kind, int64_t cols, int vecs) {
 }
 constexpr int kFewVecs = 2, kBackVecs = 8;
 
-// Rows that would leave most of the chip idle, and are long enough to be split.
+// Rows that would leave half of the chip idle, and are long enough to be split.  Loss and gradient, whole / split, us: 96 x 50021
+// bf16 19.3 / 16.1, 127 19.7 / 17.9, 192 20.6 / 22.7, 512 31 / 41; 32 x 131072 f32 28.5 / 17.7, 127 39.5 / 39.7, 512 159 / 171; a loss
+// alone 96 x 262144 bf16 24 / 17, 192 24.5 / 24.4, 256 26 / 30.
 static bool takes_parts(int kind, int64_t rows, int64_t cols) { return rows < 128 && parts_of(kind, cols, kBackVecs) > 2; }
 
 size_t distill_scratch_bytes(int64_t rows, int64_t cols) {
@@ -624,11 +626,17 @@ template <int KIND, bool PAST> static hipError_t launch_kind(const DistillArgs& 
     const u64 vecs = ((u64)a.cols + kPer<KIND> - 1) / kPer<KIND>;
     const dim3 grid = grid_of((u64)a.rows);
     if (!a.grad && vecs > 64 * 16) {
-        // A loss alone needs nothing kept: half the registers and twice the rows on a CU (513 x 50021 f16: 20.8 -> 16.4 us).
+        // A loss alone needs nothing kept: half the registers and twice the rows on a CU (513 x 50021 f16: 20.8 -> 16.4 us; 2048 x
+        // 30000 bf16 30.5 -> 25.8).  Rows that one wavefront's registers hold are kept all the same (4096 x 4000 f32 17 us, streamed
+        // 21).  By 256 threads / 512: 300 x 16000 f32 8.8 / 9.4, 2048 x 30000 bf16 25.6 / 30.6.
         if (vecs <= 256 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 256, false, false>), grid, dim3(256), lds, st, a);
         else hipLaunchKernelGGL((k_distill_row<KIND, 512, false, false>), grid, dim3(512), lds, st, a);
         return hipGetLastError();
     }
+    // The fewest threads whose registers hold the row: barriers of fewer wavefronts, more rows on a CU.  The fewer / the more, us: 64 or 256
+    // threads 16 x 1000 f32, 64 entries 9.7 / 10.7, 4096 x 1000 19 / 42, 4096 x 4000 29 / 47; 256 or 512 2048 x 16000 66 / 75; 512 or 1024 2048
+    // x 32000 116 / 159.  Hundreds of entries are weighed and looked through by one wavefront then, which few rows do not cover:
+    // 300 x 4000 f32, 256 entries 40 / 18, 1024 rows 44 / 26, 4096 72 / 76.
     if (vecs <= 64 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 64, true, PAST>), grid, dim3(64), lds, st, a);
     else if (vecs <= 256 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 256, true, PAST>), grid, dim3(256), lds, st, a);
     else if (vecs <= 512 * 16) hipLaunchKernelGGL((k_distill_row<KIND, 512, true, PAST>), grid, dim3(512), lds, st, a);

@@ -14,7 +14,7 @@
 // not depend on how its work was split or in which order atomics arrived.
 //
 // A row of up to 262144 outcomes is one workgroup's, which reads it two or three times: bound by memory for top-k (256 x
-// 131072 f32: 58 us, 7 TB/s in each of two scans out of the memory-side cache), by vector issue for top-p (110 us; a weight
+// 131072 f32, k = 50: 52 us, two scans of 134 MB at 5.2 TB/s), by vector issue for top-p (105 us; a weight
 // takes 19 instructions, and the slowest of 256 rows has half of its outcomes left).  Few rows are bound by latency (1 x
 // 32768 bf16: 11 us).  64-bit atomics, weights and the search of a cut in 64 bits cost nothing here that 32 bits would
 // save: double precision issues at the rate of single.
@@ -585,8 +585,9 @@ template <int KIND, int STEPS, int NP> __device__ __forceinline__ long long find
 }
 
 // ---- sorting in LDS --------------------------------------------------------------------------------------------------
-// Ascending, n <= 2 NT distinct entries.  Up to 256: each one's rank is the number of entries below it (1 x 32768
-// bf16, some 55 entries: sorting and drawing 1.7 us, by exchanges 5.2).  Else by exchanges, entries behind the n-th up to a power of two at the highest number.
+// Ascending, n distinct entries in room for a power of two of them, 256 or more.  Up to 256: each one's rank is the number of
+// entries below it (1 x 32768 bf16, some 55 entries: sorting and drawing 1.7 us, by exchanges 5.2).  Else by exchanges, entries
+// behind the n-th up to a power of two at the highest number.
 template <int NT> __device__ __forceinline__ void sort_lds(u64* a, u32 n) {
     if (n <= 256) {
         constexpr int per = NT < 256 ? 256 / NT : 1;
@@ -658,7 +659,10 @@ template <int KIND, int NB, int NP> __device__ __forceinline__ void add4(const S
 
 // ---- one workgroup a row ---------------------------------------------------------------------------------------------
 template <int NT> struct Shape;
-// bins of a histogram (and entries of a list to be sorted), chunks, vectors of a lane in a chunk
+// Bins of a histogram (and entries of a list to be sorted), chunks, vectors of a lane in a chunk; the most outcomes of a row that
+// are given as many threads.  bf16, T, top-k and top-p of every row, in us by the fewer / the more threads: 64 or 256 threads 1 x 512
+// 9.7 / 9.5, 1024 x 512 11.4 / 12.4, 8192 x 512 28.6 / 64; 256 or 1024 (more than 256 rows: 512) 1 x 1000 9.1 / 10.0, 1 x 8000
+// 13.6 / 11.6, 512 x 8000 16.1 / 16.6, 4096 x 8000 59 / 106.  Top-p alone 1 x 8000 19.2 / 15.7, 4096 x 8000 95 / 149.
 template <> struct Shape<64> { static constexpr int bins = 256, chunks = 4, steps = 1; static constexpr u32 most = 512; };
 template <> struct Shape<256> { static constexpr int bins = 1024, chunks = 36, steps = 1; static constexpr u32 most = 8192; };
 template <> struct Shape<512> { static constexpr int bins = 2048, chunks = 264, steps = 4; static constexpr u32 most = 262144; };
@@ -675,6 +679,7 @@ struct Later {
 template <int KIND, int NT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_sample_row(const SampleArgs a, const Later later) {
     constexpr int NB = Shape<NT>::bins, NC = Shape<NT>::chunks, STEPS = Shape<NT>::steps, LIST = 2 * NB;
+    static_assert(NB >= 256 && (NB & (NB - 1)) == 0 && NB % NT == 0, "lists of up to NB entries are sorted in place, NB / NT of a thread");
     constexpr int UN = NT == 1024 ? 4 : 2;  // vectors of a thread on their way at once
     // two histograms; or: a list to be sorted, its entries and their weights, or values on their way; or: a list to be searched
     __shared__ struct { u64 wt[2 * NB]; u32 cnt[2 * NB]; } lds;
@@ -790,7 +795,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
     };
     if (by_k) {
         // The k-th highest of the threads' own highest values has k values at or above it, and not many more: of 1024
-        // threads' values the 50 highest come from about 49 threads.
+        // threads' values the 50 highest come from about 49 threads.  From k near the number of threads on the lowest of these
+        // maxima bounds little, and the scan is lost (with it / without, us: 256 x 131072 f32 k = 50 51 / 68, 640 81 / 93, 900
+        // 115 / 94; 64 x 50021 300 35 / 39, 640 49 / 47).
         if (p.top_k <= NT * 5 / 8) {
             for (int i = threadIdx.x; i < NB; i += NT) cnt[i] = 0;
             __syncthreads();
@@ -1561,7 +1568,7 @@ template <int KIND> __global__ __launch_bounds__(1024) void k_long_scan(const Sa
     const Scale s = scale_of<KIND, kLongBins, 1024>(tables, st.kmax, p.t > 0.f ? p.t : 1.f, a.bits);
     long_advance<KIND, 1024>(a, p, s, tables, g, r, prev, sm, &hit, &st);
     const u64 w_cut = weight(s, tables, st.cut.v);
-    const bool mine = threadIdx.x < g.parts;       // (1024 parts at most)
+    const bool mine = threadIdx.x < g.parts;       // (256 parts at most)
     const u64 n = mine ? g.part_n[r * g.parts + threadIdx.x] : 0;
     const u64 eq = n >> 32;
     u64 eq_all, n_kept, total;
@@ -1624,7 +1631,8 @@ template <int KIND> __global__ __launch_bounds__(256) void k_long_draw(const Sam
 }  // namespace
 
 // Rows of more outcomes than one workgroup takes.  (Shorter ones are not split however few there are: a split row takes 4
-// to 11 launches, 6 us each where it has nothing to do; 24 x 50021 f16 take 31 us in one.)
+// launches, 3 more for each of top-k and top-p, and one for many shots, 6 us each where it has nothing to do; 24 x 50021 f16
+// take 31 us in one.)
 static bool takes_parts(int64_t cols) { return cols > (int64_t)Shape<1024>::most; }
 
 // More shots of a row than two for each of its wavefronts are drawn by another launch (6 x 66088 f32, 564 shots, wide nuclei:
@@ -1690,7 +1698,8 @@ template <int KIND> static hipError_t launch_kind(const SampleArgs& a, void* scr
         later.rows = (RowDraw*)(later.chunk_w + (u64)a.rows * Shape<1024>::chunks);
     }
     // A row for every CU or fewer: all of its threads for the row.  Two workgroups of half of them, which fill each other's
-    // waits, where there are more rows (516 x 13885 f16: 48.5 -> 37 us).
+    // waits, where there are more rows (top-p, one / two: 256 x 13885 f16 25.1 / 25.7 us, 300 41.6 / 29.0, 512 46.2 / 31.6; 256 x
+    // 131072 f32 105 / 127, 300 164 / 161, 512 195 / 185).
     if (a.rows <= 256) hipLaunchKernelGGL((k_sample_row<KIND, 1024>), grid, dim3(1024), 0, st, a, later);
     else hipLaunchKernelGGL((k_sample_row<KIND, 512>), grid, dim3(512), 0, st, a, later);
     if (later.rows)
