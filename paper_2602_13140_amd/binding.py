@@ -226,11 +226,20 @@ def _rows(t, kind, dev, what):
 
 
 def _flat(t, dtype, dev, what, *shape):
-    """The address of a contiguous tensor of this type and shape (one number: any shape of as many); None stays None."""
+    """The address of a contiguous tensor of this type and shape; None stays None."""
     if t is None:
         return None
-    if not (t.dtype is _dtype(dtype) and t.get_device() == dev and t.is_contiguous() and (t.shape == shape or shape == (t.numel(),))):
+    if not (t.dtype is _dtype(dtype) and t.get_device() == dev and t.is_contiguous() and t.shape == shape):
         _need(False, "%s must be a contiguous tensor of %s %s on cuda:%d" % (what, dtype, list(shape), dev))
+    return t.data_ptr()
+
+
+def _room(t, dtype, dev, what, count):
+    """The address of a contiguous tensor of this type, of `count` values or more; None stays None."""
+    if t is None:
+        return None
+    if not (t.dtype is _dtype(dtype) and t.get_device() == dev and t.is_contiguous() and t.numel() >= count):
+        _need(False, "%s must be a contiguous tensor of %d values of %s on cuda:%d" % (what, count, dtype, dev))
     return t.data_ptr()
 
 
@@ -341,10 +350,10 @@ class Context:
         d, B, P = self.dev.index, self.batch, max(0, qsv_num_params(circ, self.n))       # (a bad circuit is the library's to refuse)
         t = _teacher(B, top_idx, top_logits, temperature, top_lse, d)
         _need(x is not None and x.dim() == 2, "x must be [batch][dim]")
-        at = (_flat(x, "float32", d, "x", B, x.shape[1]), x.shape[1], _flat(params, "float32", d, "params", P),
-              _flat(feats, "float32", d, "feats", B * self.n) if circ.reupload else None)
-        out = (_flat(loss, "float32", d, "loss", B), _flat(grad, "float32", d, "grad", B * P),
-               _flat(mean_loss, "float32", d, "mean_loss", 1), _flat(mean_grad, "float32", d, "mean_grad", P))
+        at = (_room(x, "float32", d, "x", B * x.shape[1]), x.shape[1], _room(params, "float32", d, "params", P),
+              _room(feats, "float32", d, "feats", B * self.n) if circ.reupload else None)
+        out = (_room(loss, "float32", d, "loss", B), _room(grad, "float32", d, "grad", B * P),
+               _room(mean_loss, "float32", d, "mean_loss", 1), _room(mean_grad, "float32", d, "mean_grad", P))
         self._check(self.L.qsv_distill_grad(self.h, ctypes.byref(circ), *at, ctypes.byref(t), *out))
 
     def qsv_reset_fidelity(self, circ, params, feats, mask, x, out):

@@ -181,7 +181,11 @@ def test_tensors_that_the_binding_refuses():
     with pytest.raises(qb.QsvError, match="kind"):
         qb._rows(z, qb.QSV_S_STATE, here, "scores")
     assert qb._flat(None, "float32", here, "loss", 3) is None
-    assert qb._flat(z, "float32", here, "stats", 3, 8) == z.data_ptr() == qb._flat(z, "float32", here, "params", 24)
+    assert qb._flat(z, "float32", here, "stats", 3, 8) == z.data_ptr() == qb._room(z, "float32", here, "params", 24)
+    assert qb._room(z, "float32", here, "params", 20) == z.data_ptr() and qb._room(None, "float32", here, "params", 20) is None
+    for bad, dev, count in ((z, here, 25), (z.t(), here, 24), (z.double(), here, 24), (z, 0, 24)):
+        with pytest.raises(qb.QsvError, match="params"):
+            qb._room(bad, "float32", dev, "params", count)
     for bad, dev, shape in ((z, here, (3, 7)), (z, here, (8, 3)), (z, here, (23,)), (z.t(), here, (8, 3)), (z.double(), here, (3, 8)), (z, 1, (3, 8))):
         with pytest.raises(qb.QsvError, match="stats"):
             qb._flat(bad, "float32", dev, "stats", *shape)
@@ -632,7 +636,7 @@ def test_tensors_refused_before_anything_runs(ctx):
     good = dict(x=torch.ones((3, 4), device="cuda"), params=torch.zeros(4, device="cuda"), feats=torch.zeros((3, 2), device="cuda"), loss=loss,
                 grad=torch.full((3, 4), -7.0, device="cuda"))
     for k, bad in (("x", good["x"].cpu()), ("x", good["x"].t()), ("params", good["params"][:3]), ("feats", good["feats"][:2]), ("feats", good["feats"].cpu()),
-                   ("loss", loss[:2]), ("grad", good["grad"][:, :3]), ("mean_grad", loss), ("mean_loss", loss)):
+                   ("loss", loss[:2]), ("grad", good["grad"][:, :3]), ("grad", good["grad"][:2]), ("mean_grad", loss), ("mean_loss", loss[:0])):
         with pytest.raises(qb.QsvError):
             c.qsv_distill_grad(circ, top_idx=idx, top_logits=logits, **dict(good, **{k: bad}))
     torch.cuda.synchronize()
