@@ -79,6 +79,7 @@ def load():
         raise FileNotFoundError(
             "%s not found: build it with `python -m paper_2602_13140_amd.build` "
             "(there is no fallback path)" % LIB_PATH)
+    import torch  # noqa: F401  (first: the library then takes the HIP runtime that torch brings; with one of its own it finds no device)
     L = ctypes.CDLL(LIB_PATH)
     vp, i32, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
     L.qsv_num_params.restype = i64

@@ -3,6 +3,8 @@ and argument errors are reported before anything touches a device."""
 import ctypes
 import os
 import re
+import subprocess
+import sys
 
 from paper_2602_13140_amd import binding as qb
 
@@ -54,3 +56,10 @@ def test_workspace_size_grows_with_the_state():
     extra = qb.qsv_grad_workspace_bytes(16, 256, c) - qb.qsv_workspace_bytes(16, 256)
     assert 256 * 11 * (8 << 16) <= extra <= 256 * 11 * (8 << 16) + 4096
     assert qb.qsv_grad_workspace_bytes(16, 256, qb.make_circuit(1, [9], 1)) == 0
+
+
+def test_one_hip_runtime_whatever_is_asked_first():
+    """Sizes asked of the library before torch is imported: both end on one HIP runtime (with two of them a context finds no device)."""
+    code = ("from paper_2602_13140_amd import binding as qb; qb.qsv_workspace_bytes(1, 1); import torch; "
+            "print(len({l.split()[-1] for l in open('/proc/self/maps') if 'libamdhip64' in l}))")
+    assert subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, check=True).stdout.split()[-1] == "1"
