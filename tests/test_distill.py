@@ -904,6 +904,78 @@ def test_circuit_amplitudes_below_the_normal_range(n):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,B,ent,opts", [(5, 3, RING, {}), (10, 1100, RING, {}), (13, 6, RING, {"tile_log2": 10}), (12, 4, LADDER, {"split_streams": 1})])
+def test_replays_of_a_captured_circuit_step(n, B, ent, opts):
+    """Loss, gradient and an optimiser's step in a graph: layer by layer, in whole passes, with index maps, on two streams.  New inputs,
+    parameters and teachers between the replays, each against the same call made eagerly, bit by bit."""
+    import torch
+    spec = wl.CircuitSpec(2, (RY, RZ), ent, 0)
+    circ, P = qb.circuit_from_spec(spec), spec.num_params(n)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = gu.make_ctx(n, B, ws_bytes=qb.qsv_distill_grad_workspace_bytes(n, B, circ))
+        for k, v in opts.items():
+            c.qsv_set_option(k, v)
+        x, p = torch.ones((B, 1 << n), device="cuda"), torch.zeros(P, device="cuda")
+        idx, logits = torch.zeros((B, 4), dtype=torch.int32, device="cuda"), torch.zeros((B, 4), device="cuda")
+        loss, grad, ml, mg = (torch.zeros(s, device="cuda") for s in ((B,), (B, P), (1,), (P,)))
+
+        def call():
+            c.qsv_distill_grad(circ, x, p, None, idx, logits, loss, grad, ml, mg)
+            c.qsv_sgd_step(p, mg, 0.05)
+        call()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call()
+        g = torch.Generator(device="cuda").manual_seed(n)
+        for i in range(4):
+            x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+            start = torch.rand(P, device="cuda", generator=g) * 3
+            idx.copy_(torch.randint(-1, 1 << n, idx.shape, device="cuda", generator=g))
+            logits.copy_(torch.randn(logits.shape, device="cuda", generator=g))
+            got = []
+            for go in (graph.replay, call):
+                p.copy_(start)
+                for t in (loss, grad, ml, mg):
+                    t.fill_(-7.0)
+                go()
+                stream.synchronize()
+                got.append([t.clone() for t in (loss, grad, ml, mg, p)])
+            assert all(torch.equal(a, b) for a, b in zip(*got)) and bool(torch.isfinite(got[0][0]).all()) and not torch.equal(got[0][4], start)
+        c.close()
+
+
+@pytest.mark.gpu
+def test_contexts_side_by_side():
+    """Two contexts, a stream each, whose calls run at once: rows in parts, long rows, many shots; the results are those of calls alone."""
+    import torch
+    from tests.test_sample import reference as sampled, same, values_of
+    g = torch.Generator().manual_seed(2)
+    u = torch.rand((3, 40), generator=g, dtype=torch.float64)
+    sides = []
+    for i in range(2):
+        st = torch.cuda.Stream()
+        with torch.cuda.stream(st):
+            z, idx, logits = draw("f32", 3, 300001 + i, 6, i)
+            z = z.contiguous()
+            sides.append(dict(st=st, c=qb.Context(1, 1), z=z, idx=idx, logits=logits, ti=torch.as_tensor(idx).int().cuda(), tl=torch.as_tensor(logits).cuda(),
+                              loss=torch.zeros(3, device="cuda"), grad=torch.zeros_like(z), u=u.cuda(), out=torch.zeros((3, 40), dtype=torch.int64, device="cuda"),
+                              kept=torch.zeros(3, dtype=torch.int32, device="cuda"), p=torch.full((3,), 0.9, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s in sides:
+            with torch.cuda.stream(s["st"]):
+                s["c"].qsv_distill(qb.QSV_S_F32, s["z"], s["ti"], s["tl"], loss=s["loss"], grad=s["grad"])
+                s["c"].qsv_sample(qb.QSV_S_F32, s["out"], s["u"], scores=s["z"], kept=s["kept"], top_p=s["p"])
+    torch.cuda.synchronize()
+    for s in sides:
+        compare("f32", (s["loss"].cpu().numpy(), f64(s["grad"]), None), reference(f64(s["z"]), s["idx"], s["logits"]))
+        same((s["out"].cpu().numpy(), None, s["kept"].cpu().numpy()), sampled(values_of("f32", s["z"]), True, u.numpy(), dict(top_p=[0.9] * 3)))
+        s["c"].close()
+
+
+@pytest.mark.gpu
 def test_training_towards_a_teacher_and_answers(oracle):
     """Steps of a circuit towards a teacher's likeliest outcomes, then answers drawn from what it learnt: every step's gradient and
     the drawn outcomes against the references."""
