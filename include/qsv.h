@@ -367,6 +367,71 @@ qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_d
                             const float* params_dev, const float* feats_dev, const qsv_teacher* teacher,
                             float* loss_dev, float* grad_dev, float* mean_loss_dev, float* mean_grad_dev);
 
+/* Penalties for repeated outcomes, biases and masks on rows of scores, before a draw (qsv_sample) or a loss (qsv_distill):
+ *   v = z
+ *   s_k:  v = v > 0 ? v / R : v R           s_k: outcome k is among the row's earlier outcomes that count
+ *   v -= F c_k + A [c_k > 0]                c_k: how often it is among those from prompt_len on
+ *   v += b_k + sum over the entries j with i_j = k of e_j
+ *   masked: v = -inf, whatever v is.
+ * Earlier outcomes: the first prior_len entries of the row's prior, of which the first prompt_len (a prompt) count for R alone;
+ * entries outside 0..cols-1 (padding) count for nothing.  Biases may be -inf; what has been named by an entry's index outside
+ * 0..cols-1 counts for nothing; entries with the same index add up in their order.  Bit k % 32 of word k / 32 of a mask allows outcome
+ * k (bits behind cols are not looked at); a mask may leave a row without any.  A score of -inf stays -inf, NaN stays NaN.
+ * Results are rounded once to the scores' type (beyond its range: to infinity); a place with a history or an entry is worked out
+ * in float64 and rounded to float32 first, the others, a score plus a shared bias, in float32.
+ * A row with a parameter out of its range (R not positive and finite, F or A not finite, not 0 <= prompt_len <= prior_len <= n_prior,
+ * a mask outside -1..n_masks-1) becomes NaN, which qsv_sample takes as a row without outcomes.
+ * out may be the scores themselves (the same address and row stride): then only the places that change are written, and, without a
+ * shared bias, read; otherwise the two must not overlap.  The other arrays must not overlap out. */
+typedef struct {
+    int32_t kind;                 /* QSV_S_F32, QSV_S_F16 or QSV_S_BF16 */
+    int32_t n_entries;            /* 0..1023: a row's own biases */
+    const void* scores_dev;       /* row r starts at element r * row_stride; aligned to its element */
+    int64_t rows;                 /* 0..2^24; 0 is a no-op */
+    int64_t cols;                 /* 1..2^30 */
+    int64_t row_stride;           /* >= cols (any value for one row), in elements */
+    void* out_dev;                /* of the scores' type */
+    int64_t out_stride;           /* >= cols (any value for one row) */
+    const int32_t* prior_dev;     /* row r starts at element r * prior_stride; may be NULL where n_prior = 0 */
+    int64_t n_prior;              /* 0..2^20 */
+    int64_t prior_stride;         /* >= n_prior (any value for one row) */
+    const int32_t* prior_len_dev; /* [rows] or NULL (n_prior) */
+    const int32_t* prompt_len_dev; /* [rows] or NULL (0) */
+    const float* repetition_dev;  /* R: [rows] or NULL (1) */
+    const float* frequency_dev;   /* F: [rows] or NULL (0) */
+    const float* presence_dev;    /* A: [rows] or NULL (0) */
+    const float* bias_dev;        /* b: [cols], the same for all rows, or NULL (0) */
+    const int32_t* entry_idx_dev; /* i: [rows][n_entries] */
+    const float* entry_bias_dev;  /* e: [rows][n_entries] */
+    const uint32_t* masks_dev;    /* mask i starts at word i * mask_stride; NULL: all outcomes are allowed */
+    int64_t n_masks;              /* 1..2^24 where masks_dev is given */
+    int64_t mask_stride;          /* >= ceil(cols / 32) (any value for one mask) */
+    const int32_t* mask_of_dev;   /* [rows]: the row's mask, -1: none; NULL: mask r for row r (n_masks = rows) or one for all (n_masks = 1) */
+} qsv_adjust_req;
+
+qsv_status qsv_adjust(qsv_ctx* ctx, const qsv_adjust_req* req);
+
+/* The backward pass of qsv_adjust, G the gradient by its result and a_k 1 where the mask allows outcome k, 0 elsewhere:
+ *   d / d z_k = a_k G_k f,  f = s_k ? (z_k > 0 ? 1 / R : R) : 1,
+ *   d / d b_k = sum over the rows of a_k G_k,   d / d e_j = a_k G_k at k = i_j (0 for an index outside 0..cols-1).
+ * A masked place gives 0 whatever G is there.  req is the forward call's: out_dev, out_stride, bias_dev and entry_bias_dev are not
+ * looked at, and scores_dev may be NULL where it has no repetition_dev or no history, or where grad_dev is NULL.  G and grad have
+ * the scores' type, rounded once.  grad may be G itself (the same address and row stride; then only the places that change are
+ * written, and unless grad_bias_dev is asked for, read), and must not overlap the scores.  Sums over rows are in float32 over 256 of them
+ * at most and in float64 over those.  A row with a parameter out of its range gives NaN, in d / d b too.  Any of the results may be
+ * NULL.  Workspace: for grad_bias_dev alone, qsv_adjust_grad_workspace_bytes (that of the plans included; 0 on bad arguments). */
+typedef struct {
+    const void* grad_out_dev;     /* G: row r starts at element r * grad_out_stride */
+    int64_t grad_out_stride;      /* >= cols (any value for one row) */
+    void* grad_dev;               /* or NULL */
+    int64_t grad_stride;          /* >= cols (any value for one row) */
+    float* grad_bias_dev;         /* [cols] or NULL */
+    float* grad_entry_dev;        /* [rows][n_entries] or NULL */
+} qsv_adjust_grad_req;
+
+size_t qsv_adjust_grad_workspace_bytes(int64_t rows, int64_t cols);
+qsv_status qsv_adjust_grad(qsv_ctx* ctx, const qsv_adjust_req* req, const qsv_adjust_grad_req* grad);
+
 /* Optimiser steps on the device, asynchronous on the context's stream; arithmetic in double, storage
  * float.  qsv_sgd_step: params -= lr * grad.  qsv_adam_step (Kingma and Ba, Algorithm 1): m, v are
  * the caller's moment buffers [count] (zero before the first step), t >= 1 the step count.
@@ -374,6 +439,42 @@ qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_d
 qsv_status qsv_sgd_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev, int64_t count, double lr);
 qsv_status qsv_adam_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev, float* m_dev, float* v_dev,
                          int64_t count, int64_t t, double lr, double beta1, double beta2, double eps);
+
+/* The norm of the gradients of many tensors together, and the gradients scaled to a highest norm:
+ *   N = sqrt(sum over all values of g^2),  f = N > max_norm ? max_norm / N : 1,  out = f g.
+ * Squares, their sum and the products are in float64; norm_dev (float32 [1] or NULL) receives N, and every value is rounded once to
+ * its tensor's type.  outs NULL: in place (nothing is written where f = 1); otherwise n tensors of the gradients' kinds and shapes.
+ * max_norm = +inf: f = 1, so that with outs NULL the norm alone is worked out.  As arithmetic has it, a NaN among the gradients makes
+ * N and, with a finite max_norm, all values NaN; an infinite one makes N infinite, finite values 0 and infinite ones NaN.
+ * Results do not depend on anything but the list.  An out must be its own gradient (the same address and row stride) or overlap no
+ * gradient, and outs must not overlap each other; columns of one buffer (the same row stride, other columns) do not overlap.
+ * The lists are host arrays, read during the call.  No workspace beyond what qsv_workspace_bytes asks for. */
+typedef struct {
+    int32_t kind;        /* QSV_S_F32, QSV_S_F16 or QSV_S_BF16 */
+    int32_t reserved;    /* must be 0 */
+    void* data_dev;      /* row r starts at element r * row_stride; aligned to its element; may be NULL where it has no values */
+    int64_t rows, cols;  /* >= 0, rows * cols <= 2^38 */
+    int64_t row_stride;  /* >= cols (any value for one row), in elements, <= 2^38 */
+} qsv_tensor;
+
+qsv_status qsv_clip_grads(qsv_ctx* ctx, const qsv_tensor* grads, const qsv_tensor* outs, int64_t n /* 0..4096 */, double max_norm /* >= 0 */,
+                          float* norm_dev);
+
+/* qsv_adam_step over many tensors at once, of the gradients times f of qsv_clip_grads (which are read, not written): the values
+ * are those of qsv_adam_step on f g.  norm_dev receives N.  Where N is not finite nothing but norm_dev is written: the step is left out.
+ * max_norm = +inf: f = 1.  param, m and v of the tensors must not overlap each other or any gradient. */
+typedef struct {
+    int32_t kind;          /* of the gradient: QSV_S_F32, QSV_S_F16 or QSV_S_BF16 */
+    int32_t reserved;      /* must be 0 */
+    float* param_dev;      /* [count] */
+    const void* grad_dev;  /* [count] */
+    float* m_dev;          /* [count] */
+    float* v_dev;          /* [count] */
+    int64_t count;         /* 0..2^38 */
+} qsv_adam_tensor;
+
+qsv_status qsv_adam_clipped(qsv_ctx* ctx, const qsv_adam_tensor* tensors, int64_t n /* 0..4096 */, int64_t t, double lr, double beta1,
+                            double beta2, double eps, double max_norm, float* norm_dev);
 
 /* Host-only introspection of the pass plan the library would run for a circuit (no GPU needed):
  * writes a text description (one line per pass, one token per operation) into buf and returns the

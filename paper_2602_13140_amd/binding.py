@@ -61,6 +61,33 @@ class qsv_distill_req(ctypes.Structure):
                 ("grad_dev", ctypes.c_void_p), ("grad_stride", ctypes.c_int64)]
 
 
+class qsv_adjust_req(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("n_entries", ctypes.c_int32), ("scores_dev", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("out_dev", ctypes.c_void_p), ("out_stride", ctypes.c_int64),
+                ("prior_dev", ctypes.c_void_p), ("n_prior", ctypes.c_int64), ("prior_stride", ctypes.c_int64),
+                ("prior_len_dev", ctypes.c_void_p), ("prompt_len_dev", ctypes.c_void_p),
+                ("repetition_dev", ctypes.c_void_p), ("frequency_dev", ctypes.c_void_p), ("presence_dev", ctypes.c_void_p),
+                ("bias_dev", ctypes.c_void_p), ("entry_idx_dev", ctypes.c_void_p), ("entry_bias_dev", ctypes.c_void_p),
+                ("masks_dev", ctypes.c_void_p), ("n_masks", ctypes.c_int64), ("mask_stride", ctypes.c_int64),
+                ("mask_of_dev", ctypes.c_void_p)]
+
+
+class qsv_adjust_grad_req(ctypes.Structure):
+    _fields_ = [("grad_out_dev", ctypes.c_void_p), ("grad_out_stride", ctypes.c_int64), ("grad_dev", ctypes.c_void_p),
+                ("grad_stride", ctypes.c_int64), ("grad_bias_dev", ctypes.c_void_p), ("grad_entry_dev", ctypes.c_void_p)]
+
+
+class qsv_tensor(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("reserved", ctypes.c_int32), ("data_dev", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class qsv_adam_tensor(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("reserved", ctypes.c_int32), ("param_dev", ctypes.c_void_p),
+                ("grad_dev", ctypes.c_void_p), ("m_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("count", ctypes.c_int64)]
+
+
 class QsvError(RuntimeError):
     def __init__(self, status, message):
         super().__init__("qsv status %d: %s" % (status, message))
@@ -135,6 +162,17 @@ def load():
     L.qsv_sample_workspace_bytes.argtypes = [i64, i64]
     L.qsv_sample.restype = i32
     L.qsv_sample.argtypes = [vp, ctypes.POINTER(qsv_sample_req)]
+    L.qsv_adjust.restype = i32
+    L.qsv_adjust.argtypes = [vp, ctypes.POINTER(qsv_adjust_req)]
+    L.qsv_adjust_grad_workspace_bytes.restype = ctypes.c_size_t
+    L.qsv_adjust_grad_workspace_bytes.argtypes = [i64, i64]
+    L.qsv_adjust_grad.restype = i32
+    L.qsv_adjust_grad.argtypes = [vp, ctypes.POINTER(qsv_adjust_req), ctypes.POINTER(qsv_adjust_grad_req)]
+    L.qsv_clip_grads.restype = i32
+    L.qsv_clip_grads.argtypes = [vp, vp, vp, i64, ctypes.c_double, vp]
+    L.qsv_adam_clipped.restype = i32
+    L.qsv_adam_clipped.argtypes = [vp, vp, i64, i64, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                   ctypes.c_double, vp]
     L.qsv_pauli_expect.restype = i32
     L.qsv_pauli_expect.argtypes = [vp, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint64, vp]
     L.qsv_plan_describe.restype = i64
@@ -185,6 +223,10 @@ def qsv_distill_workspace_bytes(rows, cols):
 
 def qsv_distill_grad_workspace_bytes(n, batch, circ):
     return int(load().qsv_distill_grad_workspace_bytes(n, batch, ctypes.byref(circ)))
+
+
+def qsv_adjust_grad_workspace_bytes(rows, cols):
+    return int(load().qsv_adjust_grad_workspace_bytes(rows, cols))
 
 
 def qsv_plan_describe(circ, n, batch=1, inverse=0, tile_log2=0):
@@ -250,6 +292,80 @@ def _teacher(rows, top_idx, top_logits, temperature, top_lse, dev):
     return qsv_teacher(top, 0, _flat(top_idx, "int32", dev, "top_idx", rows, top),
                        _flat(top_logits, "float32", dev, "top_logits", rows, top),
                        _flat(top_lse, "float32", dev, "top_lse", rows), float(temperature))
+
+
+def _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of):
+    """The part of a request that qsv_adjust and its backward pass share; tensors of whole numbers may have rows further apart."""
+    def table(t, what, rows_at):
+        if not (t.get_device() == d and t.dim() == 2 and t.dtype is _dtype("int32") and (t.shape[1] < 2 or t.stride(1) == 1)
+                and rows_at in (None, t.shape[0])):
+            _need(False, "%s must be rows of int32 on cuda:%d, the values of a row next to each other" % (what, d))
+        return t
+    if prior is not None:
+        table(prior, "prior", rows)
+        r.prior_dev, r.n_prior, r.prior_stride = prior.data_ptr(), prior.shape[1], prior.stride(0)
+    r.prior_len_dev, r.prompt_len_dev = _flat(prior_len, "int32", d, "prior_len", rows), _flat(prompt_len, "int32", d, "prompt_len", rows)
+    r.repetition_dev, r.frequency_dev = _flat(repetition, "float32", d, "repetition", rows), _flat(frequency, "float32", d, "frequency", rows)
+    r.presence_dev = _flat(presence, "float32", d, "presence", rows)
+    if entry_idx is not None:
+        _need(entry_idx.dim() == 2, "entry_idx must be [rows][n_entries]")
+        r.n_entries = entry_idx.shape[1]
+        r.entry_idx_dev = _flat(entry_idx, "int32", d, "entry_idx", rows, r.n_entries)
+    if masks is not None:
+        table(masks, "masks", None)
+        _need(masks.shape[1] >= (r.cols + 31) // 32, "masks must have a bit for each outcome")
+        r.masks_dev, r.n_masks, r.mask_stride = masks.data_ptr(), masks.shape[0], masks.stride(0)
+        r.mask_of_dev = _flat(mask_of, "int32", d, "mask_of", rows)
+    else:
+        _need(mask_of is None, "mask_of without masks")
+
+
+def _kind_of(t):
+    for kind in (QSV_S_F32, QSV_S_F16, QSV_S_BF16):
+        if t.dtype is _dtype(_TYPE_OF[kind]):
+            return kind
+    _need(False, "tensors must be float32, float16 or bfloat16")
+
+
+class TensorList:
+    """Tensors as qsv_clip_grads takes them, laid out once: contiguous ones of any shape, or rows (of two dimensions) further apart.
+    Holds the tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.at = (qsv_tensor * max(1, len(self.tensors)))()
+        for e, t in zip(self.at, self.tensors):
+            flat = t.is_contiguous()
+            _need(flat or (t.dim() == 2 and (t.shape[1] < 2 or t.stride(1) == 1) and (t.shape[0] < 2 or t.stride(0) >= t.shape[1])),
+                  "tensors must be contiguous, or rows whose values lie next to each other")
+            e.kind, e.data_dev = _kind_of(t), t.data_ptr() or None
+            e.rows, e.cols = t.shape if t.dim() == 2 else (1, t.numel())
+            e.row_stride = e.cols if flat else t.stride(0)
+        self.devices = {t.get_device() for t in self.tensors}
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+class AdamList:
+    """Parameters, gradients and moments as qsv_adam_clipped takes them, laid out once.  Holds the tensors."""
+
+    def __init__(self, params, grads, m, v):
+        self.tensors = [list(x) for x in (params, grads, m, v)]
+        n = len(self.tensors[0])
+        _need(all(len(x) == n for x in self.tensors), "params, grads, m and v must be as many")
+        self.at = (qsv_adam_tensor * max(1, n))()
+        for e, p, g, a, b in zip(self.at, *self.tensors):
+            for t in (p, a, b):
+                _need(t.dtype is _dtype("float32"), "params, m and v must be float32")
+            for t in (p, g, a, b):
+                _need(t.is_contiguous() and t.shape == p.shape, "params, grads, m and v must be contiguous, of one shape")
+            e.kind, e.count = _kind_of(g), p.numel()
+            e.param_dev, e.grad_dev, e.m_dev, e.v_dev = (t.data_ptr() or None for t in (p, g, a, b))
+        self.devices = {t.get_device() for x in self.tensors for t in x}
+
+    def __len__(self):
+        return len(self.tensors[0])
 
 
 class Context:
@@ -385,6 +501,60 @@ class Context:
         r.logp_dev = _flat(logp, "float32", d, "logp", r.rows, r.shots)
         r.kept_dev = _flat(kept, "int32", d, "kept", r.rows)
         self._check(self.L.qsv_sample(self.h, ctypes.byref(r)))
+
+    def qsv_adjust(self, kind, scores, out=None, prior=None, prior_len=None, prompt_len=None, repetition=None, frequency=None,
+                   presence=None, bias=None, entry_idx=None, entry_bias=None, masks=None, mask_of=None):
+        """out None: over the scores."""
+        r, d = qsv_adjust_req(), self.dev.index
+        s = _rows(scores, kind, d, "scores")
+        o = s if out is None else _rows(out, kind, d, "out")
+        _need(o.shape == s.shape, "out must have the shape of the scores")
+        r.kind, r.scores_dev, r.row_stride, r.out_dev, r.out_stride = kind, s.data_ptr(), s.stride(0), o.data_ptr(), o.stride(0)
+        r.rows, r.cols = s.shape
+        _adjustment(r, d, r.rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
+        r.bias_dev = _flat(bias, "float32", d, "bias", r.cols)
+        _need((entry_idx is None) == (entry_bias is None), "entry_idx and entry_bias go together")
+        r.entry_bias_dev = _flat(entry_bias, "float32", d, "entry_bias", r.rows, r.n_entries)
+        self._check(self.L.qsv_adjust(self.h, ctypes.byref(r)))
+
+    def qsv_adjust_grad(self, kind, grad_out, grad=None, scores=None, grad_bias=None, grad_entry=None, prior=None, prior_len=None,
+                        prompt_len=None, repetition=None, frequency=None, presence=None, entry_idx=None, masks=None, mask_of=None):
+        """grad may be grad_out; None: the gradients of the biases alone."""
+        r, b, d = qsv_adjust_req(), qsv_adjust_grad_req(), self.dev.index
+        g = _rows(grad_out, kind, d, "grad_out")
+        r.kind = kind
+        r.rows, r.cols = g.shape
+        for t, what in ((scores, "scores"), (grad, "grad")):
+            _need(t is None or _rows(t, kind, d, what).shape == g.shape, "%s must have the shape of grad_out" % what)
+        if scores is not None:
+            r.scores_dev, r.row_stride = scores.data_ptr(), scores.stride(0)
+        b.grad_out_dev, b.grad_out_stride = g.data_ptr(), g.stride(0)
+        if grad is not None:
+            b.grad_dev, b.grad_stride = grad.data_ptr(), grad.stride(0)
+        _adjustment(r, d, r.rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
+        b.grad_bias_dev = _flat(grad_bias, "float32", d, "grad_bias", r.cols)
+        b.grad_entry_dev = _flat(grad_entry, "float32", d, "grad_entry", r.rows, r.n_entries)
+        self._check(self.L.qsv_adjust_grad(self.h, ctypes.byref(r), ctypes.byref(b)))
+
+    def _list(self, tensors, cls):
+        got = tensors if isinstance(tensors, cls) else cls(tensors)
+        _need(got.devices <= {self.dev.index}, "tensors must be on cuda:%d" % self.dev.index)
+        return got
+
+    def qsv_clip_grads(self, grads, max_norm, norm=None, out=None):
+        """grads, out: tensors, or a TensorList of them; out None: over the gradients."""
+        g = self._list(grads, TensorList)
+        o = None if out is None else self._list(out, TensorList)
+        _need(o is None or len(o) == len(g), "out must be as many as grads")
+        at = _flat(norm, "float32", self.dev.index, "norm", 1)
+        self._check(self.L.qsv_clip_grads(self.h, g.at, None if o is None else o.at, len(g), max_norm, at))
+
+    def qsv_adam_clipped(self, tensors, t, lr, max_norm, beta1=0.9, beta2=0.999, eps=1e-8, norm=None):
+        """tensors: an AdamList."""
+        _need(isinstance(tensors, AdamList), "tensors must be an AdamList")
+        a = self._list(tensors, AdamList)
+        at = _flat(norm, "float32", self.dev.index, "norm", 1)
+        self._check(self.L.qsv_adam_clipped(self.h, a.at, len(a), t, lr, beta1, beta2, eps, max_norm, at))
 
     def qsv_pauli_expect(self, out, xmask=0, ymask=0, zmask=0):
         self._check(self.L.qsv_pauli_expect(self.h, xmask, ymask, zmask, _ptr(out)))

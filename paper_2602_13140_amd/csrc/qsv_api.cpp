@@ -19,6 +19,7 @@
 #include "qsv_scores.h"
 #include "qsv_lower.h"
 #include "qsv_plan.h"
+#include "qsv_tensors.h"
 
 using namespace qsv;
 
@@ -1950,6 +1951,105 @@ qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_d
                             float* mean_loss_dev, float* mean_grad_dev) {
     return adjoint_impl(ctx, c, x_dev, dim, params_dev, feats_dev, 3, 0, 0, nullptr, loss_dev, grad_dev, mean_loss_dev,
                         mean_grad_dev, teacher);
+}
+
+namespace {
+
+AdjustArgs to_dev(const qsv_adjust_req& q) {
+    const bool more = q.rows > 1;
+    AdjustArgs a{};
+    a.scores = q.scores_dev;
+    a.rows = q.rows;
+    a.cols = (uint32_t)q.cols;
+    a.stride = more ? q.row_stride : 0;
+    a.n_prior = (int)q.n_prior;
+    a.prior = q.prior_dev;
+    a.prior_stride = more ? q.prior_stride : 0;
+    a.prior_len = q.prior_len_dev;
+    a.prompt_len = q.prompt_len_dev;
+    a.repetition = q.repetition_dev;
+    a.frequency = q.frequency_dev;
+    a.presence = q.presence_dev;
+    a.n_entries = q.n_entries;
+    a.entry_idx = q.entry_idx_dev;
+    a.masks = q.masks_dev;
+    a.n_masks = q.n_masks;
+    a.mask_stride = q.n_masks > 1 ? q.mask_stride : 0;
+    a.mask_of = q.mask_of_dev;
+    a.mask_each = q.n_masks > 1;
+    return a;
+}
+
+}  // namespace
+
+qsv_status qsv_adjust(qsv_ctx* ctx, const qsv_adjust_req* req) {
+    if (!ctx) return QSV_ERR_INVALID_ARG;
+    if (const char* why = check_adjust(req)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    if (req->rows == 0) return QSV_OK;
+    qsv_status st = bind_device(ctx);
+    if (st != QSV_OK) return st;
+    AdjustArgs a = to_dev(*req);
+    a.out = req->out_dev;
+    a.out_stride = req->rows > 1 ? req->out_stride : 0;
+    a.bias = req->bias_dev;
+    a.entry_bias = req->entry_bias_dev;
+    QSV_HIP(ctx, launch_adjust(req->kind, a, ctx->stream), "adjust");
+    return QSV_OK;
+}
+
+// The workspace of qsv_adjust_grad behind the plans' region.
+size_t qsv_adjust_grad_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || rows > kMostRows || cols < 1 || cols > kMostCols) return 0;
+    return kOpsRegion + align_up(adjust_grad_scratch_bytes(rows, cols));
+}
+
+qsv_status qsv_adjust_grad(qsv_ctx* ctx, const qsv_adjust_req* req, const qsv_adjust_grad_req* grad) {
+    if (!ctx) return QSV_ERR_INVALID_ARG;
+    if (const char* why = check_adjust_grad(req, grad)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    if (!(grad->grad_dev || grad->grad_bias_dev || grad->grad_entry_dev)) return QSV_OK;
+    if (req->rows == 0 && !grad->grad_bias_dev) return QSV_OK;
+    qsv_status st = bind_device(ctx);
+    if (st != QSV_OK) return st;
+    AdjustArgs a = to_dev(*req);
+    a.grad_out = grad->grad_out_dev;
+    a.grad_out_stride = req->rows > 1 ? grad->grad_out_stride : 0;
+    a.grad = grad->grad_dev;
+    a.grad_stride = req->rows > 1 ? grad->grad_stride : 0;
+    a.grad_bias = grad->grad_bias_dev;
+    a.grad_entry = grad->grad_entry_dev;
+    Arena ar(ctx);
+    void* scratch = ar.take(grad->grad_bias_dev ? adjust_grad_scratch_bytes(req->rows, req->cols) : 0);
+    if (!scratch) return ws_fail(ctx, ar, "qsv_adjust_grad");
+    QSV_HIP(ctx, launch_adjust_grad(req->kind, a, scratch, ctx->stream), "adjust grad");
+    return QSV_OK;
+}
+
+qsv_status qsv_clip_grads(qsv_ctx* ctx, const qsv_tensor* grads, const qsv_tensor* outs, int64_t n, double max_norm, float* norm_dev) {
+    if (!ctx) return QSV_ERR_INVALID_ARG;
+    if (const char* why = check_clip(grads, outs, n, max_norm)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    qsv_status st = bind_device(ctx);
+    if (st != QSV_OK) return st;
+    Arena ar(ctx);
+    void* scratch = ar.take(norm_scratch_bytes());
+    if (!scratch) return ws_fail(ctx, ar, "qsv_clip_grads");
+    QSV_HIP(ctx, launch_clip(grads, outs, n, max_norm, norm_dev, scratch, ctx->stream), "clip grads");
+    return QSV_OK;
+}
+
+qsv_status qsv_adam_clipped(qsv_ctx* ctx, const qsv_adam_tensor* tensors, int64_t n, int64_t t, double lr, double beta1, double beta2,
+                            double eps, double max_norm, float* norm_dev) {
+    if (!ctx) return QSV_ERR_INVALID_ARG;
+    if (t < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0))
+        return fail(ctx, QSV_ERR_INVALID_ARG, "qsv_adam_clipped: t must be >= 1, beta1 and beta2 in [0, 1), eps positive");
+    if (const char* why = check_adam_list(tensors, n, max_norm)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    qsv_status st = bind_device(ctx);
+    if (st != QSV_OK) return st;
+    Arena ar(ctx);
+    void* scratch = ar.take(norm_scratch_bytes());
+    if (!scratch) return ws_fail(ctx, ar, "qsv_adam_clipped");
+    const AdamRates by{lr, beta1, beta2, eps, 1.0 - pow(beta1, (double)t), 1.0 - pow(beta2, (double)t)};
+    QSV_HIP(ctx, launch_adam_clipped(tensors, n, max_norm, by, norm_dev, scratch, ctx->stream), "adam clipped");
+    return QSV_OK;
 }
 
 qsv_status qsv_sgd_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev, int64_t count, double lr) {

@@ -11,10 +11,9 @@
 //
 // Exponentials and the values they are taken of are in 32 bits, sums over a thread's values too; sums over threads, the
 // teacher's weights and the loss, a small difference of large numbers, in 64.
+#include "qsv_rows.h"
 #include "qsv_scores.h"
 #include "qsv_wave.h"
-
-#include <hip/hip_fp16.h>
 
 namespace qsv {
 namespace {
@@ -23,34 +22,12 @@ typedef unsigned long long u64;
 typedef unsigned u32;
 constexpr float kInf = __builtin_inff();
 
-template <int KIND> constexpr int kPer = KIND == kScoreF32 ? 4 : 8;      // values of a vector
-template <int KIND> constexpr int kSize = KIND == kScoreF32 ? 4 : 2;
 template <int KIND> constexpr u32 kNone = KIND == kScoreF32 ? 0xff800000u : KIND == kScoreBF16 ? 0xff80ff80u : 0xfc00fc00u;   // -inf
-
-// Rows start anywhere an element may: vectors of 16 bytes at the element's alignment, which the memory pipeline takes.
-typedef u32 vec __attribute__((ext_vector_type(4)));
-typedef u32 vec_at2 __attribute__((ext_vector_type(4), aligned(2)));
-typedef u32 vec_at4 __attribute__((ext_vector_type(4), aligned(4)));
-
-template <int KIND> __device__ __forceinline__ float value_at(const char* row, u32 k) {
-    if (KIND == kScoreF32) return ((const float*)row)[k];
-    if (KIND == kScoreF16) return __half2float(((const __half*)row)[k]);
-    return __uint_as_float((u32)((const unsigned short*)row)[k] << 16);
-}
-
-template <int KIND> __device__ __forceinline__ void store_one(char* row, u32 k, float v) {
-    if (KIND == kScoreF32) ((float*)row)[k] = v;
-    else if (KIND == kScoreF16) ((__half*)row)[k] = __float2half_rn(v);
-    else ((__bf16*)row)[k] = (__bf16)v;
-}
 
 // Vector j of a row's whole vectors; -inf behind them.  (Offsets of 32 bits to a uniform address: a row has 4 GiB at most.)
 template <int KIND> __device__ __forceinline__ vec load_vec(const char* row, u32 whole, u32 j) {
     vec x = {kNone<KIND>, kNone<KIND>, kNone<KIND>, kNone<KIND>};
-    if (j < whole) {
-        if (KIND == kScoreF32) x = *(const vec_at4*)(row + j * 16u);
-        else x = *(const vec_at2*)(row + j * 16u);
-    }
+    if (j < whole) x = vec_at<KIND>(row + j * 16u);
     return x;
 }
 
@@ -60,37 +37,9 @@ template <int KIND> __device__ __forceinline__ float load_rest(const char* row, 
     return lane < kPer<KIND> && k < cols ? value_at<KIND>(row, k) : -kInf;
 }
 
-template <int KIND> __device__ __forceinline__ float part(const vec& x, int i) {
-    if (KIND == kScoreF32) return __uint_as_float(x[i]);
-    const u32 two = x[i >> 1];
-    if (KIND == kScoreBF16) return __uint_as_float((i & 1) ? two & 0xffff0000u : two << 16);
-    return __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
-}
-
 // PAST: past the caches.
 template <int KIND, bool PAST> __device__ __forceinline__ void store_vec(char* row, u32 whole, u32 j, const float (&g)[kPer<KIND>]) {
-    constexpr int W = kPer<KIND>;
-    if (j >= whole) return;
-    vec x;
-    if (KIND == kScoreF32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(g[i]);
-        if (PAST) __builtin_nontemporal_store(x, (vec_at4*)(row + j * 16u));
-        else *(vec_at4*)(row + j * 16u) = x;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (KIND == kScoreBF16) {
-                typedef __bf16 two __attribute__((ext_vector_type(2)));
-                const two b = {(__bf16)g[(2 * i) % W], (__bf16)g[(2 * i + 1) % W]};
-                x[i] = __builtin_bit_cast(u32, b);
-            } else {
-                x[i] = (u32)__half_as_ushort(__float2half_rn(g[(2 * i) % W])) | (u32)__half_as_ushort(__float2half_rn(g[(2 * i + 1) % W])) << 16;
-            }
-        }
-        if (PAST) __builtin_nontemporal_store(x, (vec_at2*)(row + j * 16u));
-        else *(vec_at2*)(row + j * 16u) = x;
-    }
+    if (j < whole) put_vec<KIND, PAST>(row + j * 16u, packed<KIND>(g));
 }
 
 template <int KIND> __device__ __forceinline__ void store_rest(char* row, u32 cols, u32 lane, float g) {

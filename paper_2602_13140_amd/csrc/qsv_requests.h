@@ -1,6 +1,9 @@
-// Checks of the requests on rows of scores: host only, no device is asked.
+// Checks of the requests on rows of scores and on lists of tensors: host only, no device is asked.
 #pragma once
+#include <algorithm>
 #include <cstdint>
+#include <memory>
+#include <new>
 
 #include "qsv.h"
 
@@ -73,6 +76,178 @@ inline const char* check_distill(const qsv_distill_req* q, const qsv_teacher* t)
             return "grad_dev must be the scores themselves or not overlap them";
     }
     return nullptr;
+}
+
+// Rows that results go to, beside rows that are read: what is wrong with them, or NULL.  same: they may be those rows.
+inline const char* check_apart(int kind, int64_t rows, int64_t cols, const void* from, int64_t from_stride, const void* to, int64_t to_stride, bool same) {
+    const uint64_t s = (uintptr_t)from, g = (uintptr_t)to;
+    if (!from || s >= g + span_bytes(kind, rows, cols, to_stride) || g >= s + span_bytes(kind, rows, cols, from_stride)) return nullptr;
+    if (same && s == g && (rows == 1 || from_stride == to_stride)) return nullptr;
+    return same ? "the result must be the rows themselves or not overlap them" : "the gradient must not overlap the scores";
+}
+
+inline const char* check_out(int kind, int64_t rows, int64_t cols, const void* out, int64_t stride) {
+    if (!out) return "the result's address is NULL";
+    if ((uintptr_t)out % score_bytes(kind)) return "results must be aligned to their element";
+    if (rows > 1 && (stride < cols || stride > kMostStride)) return "the stride of results must be in cols..2^36";
+    return nullptr;
+}
+
+constexpr int64_t kMostPrior = (int64_t)1 << 20, kMostEntries = 1023, kMostMasks = (int64_t)1 << 24;
+
+// What a request of qsv_adjust says about history, entries and masks, with at least one row.
+inline const char* check_adjust_lists(const qsv_adjust_req* q, bool back) {
+    if (q->n_prior < 0 || q->n_prior > kMostPrior) return "n_prior must be in 0..2^20";
+    if (q->n_prior > 0) {
+        if (!q->prior_dev) return "prior_dev is NULL";
+        if (q->rows > 1 && (q->prior_stride < q->n_prior || q->prior_stride > kMostStride)) return "prior_stride must be in n_prior..2^36";
+    }
+    if (q->n_entries < 0 || q->n_entries > kMostEntries) return "n_entries must be in 0..1023";
+    if (q->n_entries > 0 && (!q->entry_idx_dev || (!back && !q->entry_bias_dev))) return "entry_idx_dev or entry_bias_dev is NULL";
+    if (q->masks_dev) {
+        if (q->n_masks < 1 || q->n_masks > kMostMasks) return "n_masks must be in 1..2^24";
+        if (q->n_masks > 1 && (q->mask_stride < (q->cols + 31) / 32 || q->mask_stride > kMostStride)) return "mask_stride must be in ceil(cols / 32)..2^36";
+        if (!q->mask_of_dev && q->n_masks != 1 && q->n_masks != q->rows) return "without mask_of_dev there must be one mask, or one for each row";
+    }
+    return nullptr;
+}
+
+inline bool score_kind(int kind) { return kind == QSV_S_F32 || kind == QSV_S_F16 || kind == QSV_S_BF16; }
+
+// What is wrong with a request of qsv_adjust, or NULL.
+inline const char* check_adjust(const qsv_adjust_req* q) {
+    if (!q) return "req is NULL";
+    if (!score_kind(q->kind)) return "kind must be one of the three types of scores";
+    if (const char* why = check_rows(q->kind, q->scores_dev, q->rows, q->cols, q->row_stride)) return why;
+    if (q->rows == 0) return nullptr;
+    if (const char* why = check_out(q->kind, q->rows, q->cols, q->out_dev, q->out_stride)) return why;
+    if (const char* why = check_apart(q->kind, q->rows, q->cols, q->scores_dev, q->row_stride, q->out_dev, q->out_stride, true)) return why;
+    return check_adjust_lists(q, false);
+}
+
+// What is wrong with a request of qsv_adjust_grad, or NULL.
+inline const char* check_adjust_grad(const qsv_adjust_req* q, const qsv_adjust_grad_req* g) {
+    if (!q || !g) return "req or grad is NULL";
+    if (!score_kind(q->kind)) return "kind must be one of the three types of scores";
+    const bool scores = g->grad_dev && q->repetition_dev && q->n_prior > 0;      // they are read
+    if (const char* why = check_rows(q->kind, scores ? q->scores_dev : g->grad_out_dev, q->rows, q->cols, scores ? q->row_stride : g->grad_out_stride)) return why;
+    if (q->rows == 0) return nullptr;
+    if (const char* why = check_adjust_lists(q, true)) return why;
+    if (!g->grad_out_dev) return "grad_out_dev is NULL";
+    if ((uintptr_t)g->grad_out_dev % score_bytes(q->kind)) return "grad_out_dev must be aligned to its element";
+    if (q->rows > 1 && (g->grad_out_stride < q->cols || g->grad_out_stride > kMostStride)) return "grad_out_stride must be in cols..2^36";
+    if (g->grad_entry_dev && q->n_entries == 0) return "grad_entry_dev without entries";
+    if (!g->grad_dev) return nullptr;
+    if (const char* why = check_out(q->kind, q->rows, q->cols, g->grad_dev, g->grad_stride)) return why;
+    if (const char* why = check_apart(q->kind, q->rows, q->cols, g->grad_out_dev, g->grad_out_stride, g->grad_dev, g->grad_stride, true)) return why;
+    return scores ? check_apart(q->kind, q->rows, q->cols, q->scores_dev, q->row_stride, g->grad_dev, g->grad_stride, false) : nullptr;
+}
+
+// ---- lists of tensors ------------------------------------------------------------------------------------------------
+constexpr int64_t kMostTensors = 4096, kMostValues = (int64_t)1 << 38;
+
+struct Span {                 // bytes; rows of `width` at `stride`
+    uint64_t from, to, width, stride;
+    int64_t own;              // the tensor it is of
+    bool written;
+};
+
+// Columns of one buffer: rows at the same stride that never meet.
+inline bool columns_apart(const Span& a, const Span& b) {      // a.from <= b.from
+    if (a.stride != b.stride || a.stride == 0) return false;
+    const uint64_t behind = (b.from - a.from) % a.stride;
+    return behind >= a.width && behind + b.width <= a.stride;
+}
+
+// Whether something that is written meets something else (a tensor's own gradient, the same rows, is let through).
+inline bool spans_meet(Span* s, int64_t n) {
+    std::sort(s, s + n, [](const Span& a, const Span& b) { return a.from < b.from; });
+    int64_t open = 0;            // those before i that may reach over it are kept at the front
+    for (int64_t i = 0; i < n; ++i) {
+        const Span now = s[i];
+        int64_t left = 0;
+        for (int64_t j = 0; j < open; ++j) {
+            if (s[j].to <= now.from) continue;
+            s[left++] = s[j];
+            const Span& b = s[left - 1];
+            if (!b.written && !now.written) continue;
+            if (b.own == now.own && b.written != now.written && b.from == now.from && b.to == now.to && b.stride == now.stride) continue;
+            if (!columns_apart(b, now)) return true;
+        }
+        s[left++] = now;
+        open = left;
+    }
+    return false;
+}
+
+inline Span span_of(const qsv_tensor& t, int64_t own, bool written) {
+    const uint64_t size = (uint64_t)score_bytes(t.kind), from = (uintptr_t)t.data_dev;
+    const uint64_t stride = t.rows > 1 ? (uint64_t)t.row_stride : 0;
+    return Span{from, from + ((uint64_t)(t.rows - 1) * stride + (uint64_t)t.cols) * size, (uint64_t)t.cols * size, stride * size, own, written};
+}
+
+inline const char* check_tensor(const qsv_tensor& t) {
+    if (t.reserved != 0) return "reserved must be 0";
+    if (!score_kind(t.kind)) return "kind must be one of the three types of scores";
+    if (t.rows < 0 || t.cols < 0 || t.rows > kMostValues || t.cols > kMostValues || (t.cols > 0 && t.rows > kMostValues / t.cols))
+        return "a tensor has rows and cols >= 0, and 2^38 values at most";
+    if (t.rows == 0 || t.cols == 0) return nullptr;
+    if (!t.data_dev) return "data_dev is NULL";
+    if ((uintptr_t)t.data_dev % score_bytes(t.kind)) return "data_dev must be aligned to its element";
+    if (t.rows > 1 && (t.row_stride < t.cols || t.row_stride > kMostValues)) return "row_stride must be in cols..2^38";
+    return nullptr;
+}
+
+// What is wrong with a request of qsv_clip_grads, or NULL.
+inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, int64_t n, double max_norm) {
+    if (n < 0 || n > kMostTensors) return "a list has 0..4096 tensors";
+    if (n > 0 && !grads) return "grads is NULL";
+    if (!(max_norm >= 0.0)) return "max_norm must be >= 0";
+    for (int64_t i = 0; i < n; ++i) {
+        if (const char* why = check_tensor(grads[i])) return why;
+        if (!outs) continue;
+        if (const char* why = check_tensor(outs[i])) return why;
+        if (outs[i].kind != grads[i].kind || outs[i].rows != grads[i].rows || outs[i].cols != grads[i].cols)
+            return "outs must have the kinds and shapes of the gradients";
+    }
+    if (!outs && max_norm > 1.7976931348623157e308) return nullptr;      // nothing is written
+    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)(outs ? 2 * n : n) + 1]);
+    if (!spans) return "out of host memory";
+    int64_t m = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (grads[i].rows == 0 || grads[i].cols == 0) continue;
+        spans[m++] = span_of(grads[i], i, !outs);
+        if (outs) spans[m++] = span_of(outs[i], i, true);
+    }
+    return spans_meet(spans.get(), m) ? "a tensor that is written overlaps another one" : nullptr;
+}
+
+// What is wrong with a request of qsv_adam_clipped, or NULL.
+inline const char* check_adam_list(const qsv_adam_tensor* tensors, int64_t n, double max_norm) {
+    if (n < 0 || n > kMostTensors) return "a list has 0..4096 tensors";
+    if (n > 0 && !tensors) return "tensors is NULL";
+    if (!(max_norm >= 0.0)) return "max_norm must be >= 0";
+    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)(4 * n) + 1]);
+    if (!spans) return "out of host memory";
+    int64_t m = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        const qsv_adam_tensor& t = tensors[i];
+        if (t.reserved != 0) return "reserved must be 0";
+        if (!score_kind(t.kind)) return "kind must be one of the three types of scores";
+        if (t.count < 0 || t.count > kMostValues) return "count must be in 0..2^38";
+        if (t.count == 0) continue;
+        if (!t.param_dev || !t.grad_dev || !t.m_dev || !t.v_dev) return "param_dev, grad_dev, m_dev or v_dev is NULL";
+        if (((uintptr_t)t.param_dev | (uintptr_t)t.m_dev | (uintptr_t)t.v_dev) % 4 || (uintptr_t)t.grad_dev % score_bytes(t.kind))
+            return "tensors must be aligned to their element";
+        const void* at[4] = {t.param_dev, t.m_dev, t.v_dev, t.grad_dev};
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t from = (uintptr_t)at[k], bytes = (uint64_t)t.count * (k < 3 ? 4 : score_bytes(t.kind));
+            spans[m++] = Span{from, from + bytes, bytes, 0, i, k < 3};
+        }
+    }
+    // (own: a parameter that is its own gradient is refused as well)
+    for (int64_t k = 0; k < m; ++k) spans[k].own = k;
+    return spans_meet(spans.get(), m) ? "a tensor that is written overlaps another one" : nullptr;
 }
 
 }  // namespace qsv

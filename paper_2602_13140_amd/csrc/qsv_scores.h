@@ -1,5 +1,5 @@
 // Launch interface of the kernels on rows of scores, probabilities or amplitudes (gfx950 only): sampling after filters,
-// distillation from a teacher's top logits.
+// distillation from a teacher's top logits, penalties, biases and masks.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -63,5 +63,39 @@ hipError_t launch_distill(int kind, const DistillArgs& a, void* scratch, hipStre
 // res, rowdep: see launch_expz_finish.
 hipError_t launch_distill_state(const float2* A, int n, const TeacherArgs& te, int64_t rows, double* f, int64_t f_stride,
                                 float2* S, int paired, hipStream_t st, const Residues* res = nullptr, int rowdep = 0);
+
+// Rows of scores after penalties, biases and masks; the backward pass has the gradients behind them.
+struct AdjustArgs {
+    const void* scores;          // row r starts r * stride elements further
+    void* out;
+    int64_t rows, stride, out_stride;
+    uint32_t cols;
+    int n_prior;                 // earlier outcomes of a row: at most so many
+    const int* prior;            // row r starts r * prior_stride further
+    int64_t prior_stride;
+    const int* prior_len;        // [rows] or NULL: n_prior
+    const int* prompt_len;       // [rows] or NULL: 0
+    const float* repetition;     // [rows], or NULL: off, as the next two
+    const float* frequency;
+    const float* presence;
+    const float* bias;           // [cols] or NULL
+    int n_entries;               // a row's own biases
+    const int* entry_idx;        // [rows][n_entries]
+    const float* entry_bias;     // [rows][n_entries], or NULL in the backward pass
+    const unsigned* masks;       // [n_masks] rows of mask_stride words, or NULL
+    int64_t n_masks, mask_stride;
+    const int* mask_of;          // [rows] or NULL
+    int mask_each;               // mask_of NULL: row r takes mask r, or (0) all take the one
+    const void* grad_out;
+    void* grad;                  // or NULL
+    int64_t grad_out_stride, grad_stride;
+    float* grad_bias;            // [cols] or NULL
+    float* grad_entry;           // [rows][n_entries] or NULL
+};
+
+hipError_t launch_adjust(int kind, const AdjustArgs& a, hipStream_t st);
+// Bytes of workspace for grad_bias.
+size_t adjust_grad_scratch_bytes(int64_t rows, int64_t cols);
+hipError_t launch_adjust_grad(int kind, const AdjustArgs& a, void* scratch, hipStream_t st);
 
 }  // namespace qsv
