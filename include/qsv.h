@@ -417,8 +417,8 @@ qsv_status qsv_adjust(qsv_ctx* ctx, const qsv_adjust_req* req);
  * A masked place gives 0 whatever G is there.  req is the forward call's: out_dev, out_stride, bias_dev and entry_bias_dev are not
  * looked at, and scores_dev may be NULL where it has no repetition_dev or no history, or where grad_dev is NULL.  G and grad have
  * the scores' type, rounded once.  grad may be G itself (the same address and row stride; then only the places that change are
- * written, and unless grad_bias_dev is asked for, read), and must not overlap the scores.  Sums over rows are in float32 over 256 of them
- * at most and in float64 over those.  A row with a parameter out of its range gives NaN, in d / d b too.  Any of the results may be
+ * written, and unless grad_bias_dev is asked for, read), and must not overlap the scores.  Sums over rows are in float64, in an order
+ * that the sizes alone decide.  A row with a parameter out of its range gives NaN, in d / d b too.  Any of the results may be
  * NULL.  Workspace: for grad_bias_dev alone, qsv_adjust_grad_workspace_bytes (that of the plans included; 0 on bad arguments). */
 typedef struct {
     const void* grad_out_dev;     /* G: row r starts at element r * grad_out_stride */
