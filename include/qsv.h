@@ -448,12 +448,12 @@ qsv_status qsv_adam_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev,
  * N and, with a finite max_norm, all values NaN; an infinite one makes N infinite, finite values 0 and infinite ones NaN.
  * Results do not depend on anything but the list.  An out must be its own gradient (the same address and row stride) or overlap no
  * gradient, and outs must not overlap each other; columns of one buffer (the same row stride, other columns) do not overlap.
- * The lists are host arrays, read during the call.  No workspace beyond what qsv_workspace_bytes asks for. */
+ * The lists are host arrays of 2^38 values at most, read during the call.  No workspace beyond what qsv_workspace_bytes asks for. */
 typedef struct {
     int32_t kind;        /* QSV_S_F32, QSV_S_F16 or QSV_S_BF16 */
     int32_t reserved;    /* must be 0 */
     void* data_dev;      /* row r starts at element r * row_stride; aligned to its element; may be NULL where it has no values */
-    int64_t rows, cols;  /* >= 0, rows * cols <= 2^38 */
+    int64_t rows, cols;  /* >= 0 */
     int64_t row_stride;  /* >= cols (any value for one row), in elements, <= 2^38 */
 } qsv_tensor;
 

@@ -203,8 +203,10 @@ inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, i
     if (n < 0 || n > kMostTensors) return "a list has 0..4096 tensors";
     if (n > 0 && !grads) return "grads is NULL";
     if (!(max_norm >= 0.0)) return "max_norm must be >= 0";
+    int64_t values = 0;
     for (int64_t i = 0; i < n; ++i) {
         if (const char* why = check_tensor(grads[i])) return why;
+        if ((values += grads[i].rows * grads[i].cols) > kMostValues) return "a list has 2^38 values at most";
         if (!outs) continue;
         if (const char* why = check_tensor(outs[i])) return why;
         if (outs[i].kind != grads[i].kind || outs[i].rows != grads[i].rows || outs[i].cols != grads[i].cols)
@@ -229,12 +231,13 @@ inline const char* check_adam_list(const qsv_adam_tensor* tensors, int64_t n, do
     if (!(max_norm >= 0.0)) return "max_norm must be >= 0";
     std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)(4 * n) + 1]);
     if (!spans) return "out of host memory";
-    int64_t m = 0;
+    int64_t m = 0, values = 0;
     for (int64_t i = 0; i < n; ++i) {
         const qsv_adam_tensor& t = tensors[i];
         if (t.reserved != 0) return "reserved must be 0";
         if (!score_kind(t.kind)) return "kind must be one of the three types of scores";
         if (t.count < 0 || t.count > kMostValues) return "count must be in 0..2^38";
+        if ((values += t.count) > kMostValues) return "a list has 2^38 values at most";
         if (t.count == 0) continue;
         if (!t.param_dev || !t.grad_dev || !t.m_dev || !t.v_dev) return "param_dev, grad_dev, m_dev or v_dev is NULL";
         if (((uintptr_t)t.param_dev | (uintptr_t)t.m_dev | (uintptr_t)t.v_dev) % 4 || (uintptr_t)t.grad_dev % score_bytes(t.kind))

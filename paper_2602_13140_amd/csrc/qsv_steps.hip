@@ -4,10 +4,10 @@
 //   m = b1 m + (1 - b1) f g,  v = b2 v + (1 - b2) (f g)^2,  p -= lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 //
 // Bound by memory: every gradient is read for the norm and once more for what is made of it.  Tensors are cut into pieces of
-// kPiece values (whole rows where they are shorter), numbered through a list of up to kList tensors that comes with the launch's
-// arguments; a workgroup takes every so many-th piece and leaves one sum.  The next launch's workgroups each add all of these
-// in the same order, so results depend on nothing but the list.  Squares and their sums are in 64 bits, where no float32 value
-// overflows or vanishes.
+// 256 to 4096 values (whole rows where they are shorter), numbered through a list that comes with the launch's arguments; a
+// wavefront takes every so many-th piece, and a workgroup leaves one sum.  The next launch's workgroups each add all of these in
+// the same order, so results depend on nothing but the list, and take the pieces from the last to the first, which the first
+// launch has read last.  Squares and their sums are in 64 bits, where no float32 value overflows or vanishes.
 #include "qsv_rows.h"
 #include "qsv_tensors.h"
 #include "qsv_wave.h"
@@ -20,75 +20,108 @@ namespace {
 typedef unsigned long long u64;
 typedef unsigned u32;
 
-constexpr int kList = 60;             // tensors of a launch: 64 bytes each, within 4 KiB of arguments; no more than lanes
 constexpr int kThreads = 256;
-constexpr u32 kPiece = 8192;
 constexpr u32 kSums = 2048;           // sums of all launches together; rounded up for each of them
-constexpr int kMostLists = (kMostTensors + kList - 1) / kList;
+constexpr int kKindBit = 56;
 
+// Lists within 4 KiB of arguments: tensors of any rows; rows without a gap, which are one; Adam's.
 struct Seg {
     const char* src;
     char* dst;                        // where the scaled gradient goes
     u64 rows, cols;
     u64 src_stride, dst_stride;       // bytes
-    u32 first;                        // its first piece's number
     u32 row_pieces;                   // pieces of a row; 0: rows_piece rows are a piece
     u32 rows_piece;
     u32 kind;
 };
-struct Segs {
-    u32 n, pieces;
-    Seg seg[kList];
+constexpr int kSegs = 58, kFlats = 140, kAdams = 90;
+struct SegList {
+    static constexpr int kRoom = kSegs;
+    u32 n, pieces, piece;
+    u32 first[kSegs];                 // a tensor's first piece's number
+    Seg seg[kSegs];
+};
+struct FlatList {
+    static constexpr int kRoom = kFlats;
+    u32 n, pieces, piece;
+    u32 first[kFlats];
+    u64 count[kFlats];                // | kind << kKindBit
+    const char* src[kFlats];
+    char* dst[kFlats];
+};
+struct AdamList {
+    static constexpr int kRoom = kAdams;
+    u32 n, pieces, piece;
+    u32 first[kAdams];
+    u64 count[kAdams];
+    float* p[kAdams];
+    const char* g[kAdams];
+    float* m[kAdams];
+    float* v[kAdams];
+};
+static_assert(sizeof(SegList) <= 4032 && sizeof(FlatList) <= 4032 && sizeof(AdamList) <= 4032, "a launch's arguments");
+constexpr int kMostLists = kMostTensors / kSegs + 2 + kMostTensors / kAdams + 2;
+
+// The place in the list of a piece's tensor: a lane asks for some of them.
+template <class L> struct Places {
+    static constexpr int N = (L::kRoom + 63) / 64;
+    u32 first[N];
+    __device__ __forceinline__ explicit Places(const L& list) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const u32 at = i * 64 + (threadIdx.x & 63);
+            first[i] = at < list.n ? list.first[at] : ~0u;
+        }
+    }
+    __device__ __forceinline__ u32 of(u32 piece) const {
+        u32 n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += (u32)__popcll(__ballot(first[i] <= piece));
+        return uniform(n - 1);
+    }
 };
 
-struct AdamSeg {
-    float* p;
-    const char* g;
-    float* m;
-    float* v;
-    u64 count;
-    u32 first, kind;
-};
-struct AdamSegs {
-    u32 n, pieces;
-    AdamSeg seg[kList];
-};
-
-// The place in the list of a piece's tensor: a lane asks for each of them.
-template <class L> __device__ __forceinline__ u32 firsts(const L& list) {
-    const u32 lane = threadIdx.x & 63;
-    return lane < list.n ? list.seg[lane].first : ~0u;
-}
-__device__ __forceinline__ u32 place_of(u32 piece, u32 first) { return (u32)__popcll(__ballot(first <= piece)) - 1; }
-
-__device__ __forceinline__ double block_sum(double v, double* sm) {
+// A sum over the workgroup, the same in all threads.
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double sm[16];
     v = wave_sum(v);
+    __syncthreads();
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) v += sm[w];
+    for (u32 w = 0; w < blockDim.x / 64; ++w) v += sm[w];
     return v;
 }
 
-// Every value of a piece: whole vectors (with the place their results go to), and single values.
-template <int KIND, class F> __device__ __forceinline__ void visit(const Seg& s, u32 q, F&& f) {
+// n values next to each other, by a wavefront: whole vectors (with the place their results go to), and single values.
+template <int KIND, class F> __device__ __forceinline__ void visit(const char* src, char* dst, u32 n, F&& f) {
+    constexpr u32 W = kPer<KIND>, N = 4;
+    const u32 lane = threadIdx.x & 63, whole = n / W;
+    u32 j = lane;
+    for (; j - lane + N * 64 <= whole; j += N * 64) {
+        vec x[N];
+#pragma unroll
+        for (u32 i = 0; i < N; ++i) x[i] = vec_at<KIND>(src + (j + i * 64) * 16);
+#pragma unroll
+        for (u32 i = 0; i < N; ++i) f.whole(x[i], dst + (j + i * 64) * 16);
+    }
+    for (; j < whole; j += 64) f.whole(vec_at<KIND>(src + j * 16), dst + j * 16);
+    const u32 k = whole * W + lane;
+    if (k < n) f.one(value_at<KIND>(src, k), dst, k);
+}
+
+template <int KIND, class F> __device__ __forceinline__ void visit(const Seg& s, u32 q, u32 piece, F&& f) {
     constexpr u32 W = kPer<KIND>, S = kSize<KIND>;
     if (s.row_pieces) {
-        const u64 row = q / s.row_pieces, c0 = (u64)(q % s.row_pieces) * kPiece;
-        const u32 n = (u32)min((u64)kPiece, s.cols - c0), whole = n / W;
-        const char* src = s.src + row * s.src_stride + c0 * S;
-        char* dst = s.dst + row * s.dst_stride + c0 * S;
-        for (u32 j = threadIdx.x; j < whole; j += kThreads) f.whole(vec_at<KIND>(src + j * 16), dst + j * 16);
-        const u32 k = whole * W + threadIdx.x;
-        if (k < n) f.one(value_at<KIND>(src, k), dst, k);
+        const u64 row = q / s.row_pieces, c0 = (u64)(q % s.row_pieces) * piece;
+        visit<KIND>(s.src + row * s.src_stride + c0 * S, s.dst + row * s.dst_stride + c0 * S, (u32)min((u64)piece, s.cols - c0), f);
         return;
     }
     const u64 row = (u64)q * s.rows_piece;
-    const u32 cols = (u32)s.cols, units = (cols + W - 1) / W, n = (u32)min((u64)s.rows_piece, s.rows - row) * units;
-    const u32 dr = kThreads / units, du = kThreads % units;
-    u32 r = threadIdx.x / units, u = threadIdx.x % units;
-    for (u32 i = threadIdx.x; i < n; i += kThreads) {
+    const u32 lane = threadIdx.x & 63, cols = (u32)s.cols, units = (cols + W - 1) / W, n = (u32)min((u64)s.rows_piece, s.rows - row) * units;
+    const u32 dr = 64 / units, du = 64 % units;
+    u32 r = lane / units, u = lane % units;
+    for (u32 i = lane; i < n; i += 64) {
         const char* src = s.src + (row + r) * s.src_stride;
         char* dst = s.dst + (row + r) * s.dst_stride;
         if (u * W + W <= cols) f.whole(vec_at<KIND>(src + u * 16), dst + u * 16);
@@ -100,49 +133,62 @@ template <int KIND, class F> __device__ __forceinline__ void visit(const Seg& s,
     }
 }
 
-template <int KIND> struct Squares {
+// F<KIND> made by `make` sees every value of a piece.
+template <class M> __device__ __forceinline__ void visit(const SegList& l, u32 at, u32 piece, M&& make) {
+    const Seg& s = l.seg[at];
+    const u32 q = piece - l.first[at];
+    if (s.kind == kScoreF32) visit<kScoreF32>(s, q, l.piece, make.template of<kScoreF32>());
+    else if (s.kind == kScoreF16) visit<kScoreF16>(s, q, l.piece, make.template of<kScoreF16>());
+    else visit<kScoreBF16>(s, q, l.piece, make.template of<kScoreBF16>());
+}
+template <class M> __device__ __forceinline__ void visit(const FlatList& l, u32 at, u32 piece, M&& make) {
+    const u64 c0 = (u64)(piece - l.first[at]) * l.piece, count = l.count[at];
+    const u32 kind = (u32)(count >> kKindBit), n = (u32)min((u64)l.piece, (count & ((1ull << kKindBit) - 1)) - c0);
+    const u64 off = c0 * (kind == kScoreF32 ? 4 : 2);
+    if (kind == kScoreF32) visit<kScoreF32>(l.src[at] + off, l.dst[at] + off, n, make.template of<kScoreF32>());
+    else if (kind == kScoreF16) visit<kScoreF16>(l.src[at] + off, l.dst[at] + off, n, make.template of<kScoreF16>());
+    else visit<kScoreBF16>(l.src[at] + off, l.dst[at] + off, n, make.template of<kScoreBF16>());
+}
+
+struct Squares {
     double sum = 0.0;
-    __device__ __forceinline__ void whole(const vec& x, char*) {
+    template <int KIND> struct Of {
+        double& sum;
+        __device__ __forceinline__ void whole(const vec& x, char*) {
 #pragma unroll
-        for (int i = 0; i < kPer<KIND>; ++i) one(part<KIND>(x, i), nullptr, 0);
-    }
-    __device__ __forceinline__ void one(float x, char*, u32) { sum = fma((double)x, (double)x, sum); }
+            for (int i = 0; i < kPer<KIND>; ++i) one(part<KIND>(x, i), nullptr, 0);
+        }
+        __device__ __forceinline__ void one(float x, char*, u32) { sum = fma((double)x, (double)x, sum); }
+    };
+    template <int KIND> __device__ __forceinline__ Of<KIND> of() { return Of<KIND>{sum}; }
 };
 
-__global__ __launch_bounds__(kThreads) void k_squares(const Segs list, double* sums) {
-    __shared__ double sm[kThreads / 64];
-    const u32 first = firsts(list);
-    double sum = 0.0;
-    for (u32 piece = blockIdx.x; piece < list.pieces; piece += gridDim.x) {
-        const Seg& s = list.seg[uniform(place_of(piece, first))];
-        if (s.kind == kScoreF32) {
-            Squares<kScoreF32> f;
-            visit<kScoreF32>(s, piece - s.first, f);
-            sum += f.sum;
-        } else if (s.kind == kScoreF16) {
-            Squares<kScoreF16> f;
-            visit<kScoreF16>(s, piece - s.first, f);
-            sum += f.sum;
-        } else {
-            Squares<kScoreBF16> f;
-            visit<kScoreBF16>(s, piece - s.first, f);
-            sum += f.sum;
-        }
-    }
-    sum = block_sum(sum, sm);
+// The workgroup's sum of squares; (pieces that it takes: its wavefronts' numbers, and so on by all wavefronts').
+template <class L> __device__ __forceinline__ double squares(const L& list, const Places<L>& places) {
+    const u32 waves = blockDim.x / 64;
+    Squares f;
+    for (u32 piece = uniform(blockIdx.x * waves + threadIdx.x / 64); piece < list.pieces; piece += gridDim.x * waves) visit(list, places.of(piece), piece, f);
+    return block_sum(f.sum);
+}
+
+template <class L> __global__ __launch_bounds__(kThreads) void k_squares(const L list, double* sums) {
+    const double sum = squares(list, Places<L>(list));
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
 
-// The norm from all sums, the same in every workgroup, and the factor.  (A NaN makes the factor NaN, an infinite norm makes it 0.)
+// The norm, and the factor.  (A NaN makes the factor NaN, an infinite norm makes it 0.)
 struct Norm { double norm, factor; };
-__device__ __forceinline__ Norm norm_of(const double* sums, u32 n, double most) {
-    __shared__ double sm[kThreads / 64];
-    double v = 0.0;
-    for (u32 i = threadIdx.x; i < n; i += kThreads) v += sums[i];
+__device__ __forceinline__ Norm norm_of(double sum, double most) {
     Norm r;
-    r.norm = sqrt(block_sum(v, sm));
+    r.norm = sqrt(sum);
     r.factor = r.norm <= most || most == __builtin_inf() ? 1.0 : most / r.norm;
     return r;
+}
+// ... from all sums, the same in every workgroup.
+__device__ __forceinline__ Norm norm_of(const double* sums, u32 n, double most) {
+    double v = 0.0;
+    for (u32 i = threadIdx.x; i < n; i += kThreads) v += sums[i];
+    return norm_of(block_sum(v), most);
 }
 
 __global__ __launch_bounds__(kThreads) void k_norm(const double* sums, u32 n, float* norm) {
@@ -150,29 +196,47 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double* sums, u32 n, fl
     if (threadIdx.x == 0) *norm = (float)r.norm;
 }
 
-template <int KIND> struct Scaled {
+// PAST: results go past the caches.
+template <bool PAST> struct Scaled {
     double factor;
-    __device__ __forceinline__ float of(float x) const { return (float)((double)x * factor); }
-    __device__ __forceinline__ void whole(const vec& x, char* to) {
-        float v[kPer<KIND>];
+    template <int KIND> struct Of {
+        double factor;
+        __device__ __forceinline__ float of(float x) const { return (float)((double)x * factor); }
+        __device__ __forceinline__ void whole(const vec& x, char* to) {
+            float v[kPer<KIND>];
 #pragma unroll
-        for (int i = 0; i < kPer<KIND>; ++i) v[i] = of(part<KIND>(x, i));
-        put_vec<KIND, false>(to, packed<KIND>(v));
-    }
-    __device__ __forceinline__ void one(float x, char* dst, u32 k) { store_one<KIND>(dst, k, of(x)); }
+            for (int i = 0; i < kPer<KIND>; ++i) v[i] = of(part<KIND>(x, i));
+            put_vec<KIND, PAST>(to, packed<KIND>(v));
+        }
+        __device__ __forceinline__ void one(float x, char* dst, u32 k) { store_one<KIND>(dst, k, of(x)); }
+    };
+    template <int KIND> __device__ __forceinline__ Of<KIND> of() { return Of<KIND>{factor}; }
 };
 
-__global__ __launch_bounds__(kThreads) void k_scale(const Segs list, const double* sums, u32 n_sums, double most, int over, float* norm) {
+template <bool PAST, class L> __device__ __forceinline__ void scale(const L& list, const Places<L>& places, double factor) {
+    const u32 waves = blockDim.x / 64;
+    Scaled<PAST> f{factor};
+    for (u32 piece = uniform(blockIdx.x * waves + threadIdx.x / 64); piece < list.pieces; piece += gridDim.x * waves) {
+        const u32 back = list.pieces - 1 - piece;
+        visit(list, places.of(back), back, f);
+    }
+}
+
+template <class L, bool PAST> __global__ __launch_bounds__(kThreads) void k_scale(const L list, const double* sums, u32 n_sums, double most, int over, float* norm) {
+    const Places<L> places(list);
     const Norm r = norm_of(sums, n_sums, most);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r.norm;
     if (over && r.factor == 1.0) return;
-    const u32 first = firsts(list);
-    for (u32 piece = blockIdx.x; piece < list.pieces; piece += gridDim.x) {
-        const Seg& s = list.seg[uniform(place_of(piece, first))];
-        if (s.kind == kScoreF32) visit<kScoreF32>(s, piece - s.first, Scaled<kScoreF32>{r.factor});
-        else if (s.kind == kScoreF16) visit<kScoreF16>(s, piece - s.first, Scaled<kScoreF16>{r.factor});
-        else visit<kScoreBF16>(s, piece - s.first, Scaled<kScoreBF16>{r.factor});
-    }
+    scale<PAST>(list, places, r.factor);
+}
+
+// All of it by one workgroup.
+template <class L> __global__ __launch_bounds__(1024) void k_clip_few(const L list, double most, int over, float* norm) {
+    const Places<L> places(list);
+    const Norm r = norm_of(squares(list, places), most);
+    if (norm && threadIdx.x == 0) *norm = (float)r.norm;
+    if (over && r.factor == 1.0) return;
+    scale<false>(list, places, r.factor);
 }
 
 // As qsv_adam_step, of the scaled gradient, its fused products included: their order shows in float32 where 0.9 m + 0.1 g lies in the
@@ -190,98 +254,215 @@ struct Adam {
     }
 };
 
-template <int KIND> __device__ __forceinline__ void adam_piece(const AdamSeg& s, u32 q, const Adam& step) {
-    const u64 c0 = (u64)q * kPiece;
-    const u32 n = (u32)min((u64)kPiece, s.count - c0);
-    for (u32 k = threadIdx.x; k < n; k += kThreads) {
-        float p = s.p[c0 + k], m = s.m[c0 + k], v = s.v[c0 + k];
-        step(p, value_at<KIND>(s.g + c0 * kSize<KIND>, k), m, v);
-        s.p[c0 + k] = p;
-        s.m[c0 + k] = m;
-        s.v[c0 + k] = v;
+// Four gradients from k on.
+template <int KIND> __device__ __forceinline__ void gradients_at(const char* g, u32 k, float (&x)[4]) {
+    if (KIND == kScoreF32) {
+        const vec q = *(const vec_at4*)(g + (u64)k * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(q[i]);
+    } else {
+        typedef u32 two_at2 __attribute__((ext_vector_type(2), aligned(2)));
+        const two_at2 q = *(const two_at2*)(g + (u64)k * 2);
+        const vec y = {q[0], q[1], 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = part<KIND>(y, i);
     }
 }
 
+// PAST: of what nobody reads again before the caches have seen other things.
+template <bool PAST> __device__ __forceinline__ void four_at(const float* p, float (&x)[4]) {
+    const vec q = PAST ? __builtin_nontemporal_load((const vec_at4*)p) : *(const vec_at4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(q[i]);
+}
+template <bool PAST> __device__ __forceinline__ void put_four(float* p, const float (&x)[4]) { put_vec<kScoreF32, PAST>((char*)p, packed<kScoreF32>(x)); }
+
+template <int KIND, bool PAST> __device__ __forceinline__ void adam_values(float* p, const char* g, float* m, float* v, u32 n, const Adam& step) {
+    const u32 lane = threadIdx.x & 63, whole = n / 4 * 4;
+    for (u32 k = lane * 4; k < whole; k += 256) {
+        float x[4], a[4], b[4], c[4];
+        gradients_at<KIND>(g, k, x);
+        four_at<PAST>(p + k, a);
+        four_at<PAST>(m + k, b);
+        four_at<PAST>(v + k, c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) step(a[i], x[i], b[i], c[i]);
+        put_four<PAST>(p + k, a);
+        put_four<PAST>(m + k, b);
+        put_four<PAST>(v + k, c);
+    }
+    const u32 k = whole + lane;
+    if (k < n) {
+        float a = p[k], b = m[k], c = v[k];
+        step(a, value_at<KIND>(g, k), b, c);
+        p[k] = a;
+        m[k] = b;
+        v[k] = c;
+    }
+}
+
+template <bool PAST> __device__ __forceinline__ void adam(const AdamList& l, const Places<AdamList>& places, const Adam& step) {
+    const u32 waves = blockDim.x / 64;
+    for (u32 i = uniform(blockIdx.x * waves + threadIdx.x / 64); i < l.pieces; i += gridDim.x * waves) {
+        const u32 piece = l.pieces - 1 - i, at = places.of(piece);
+        const u64 c0 = (u64)(piece - l.first[at]) * l.piece, count = l.count[at];
+        const u32 kind = (u32)(count >> kKindBit), n = (u32)min((u64)l.piece, (count & ((1ull << kKindBit) - 1)) - c0);
+        const char* g = l.g[at] + c0 * (kind == kScoreF32 ? 4 : 2);
+        if (kind == kScoreF32) adam_values<kScoreF32, PAST>(l.p[at] + c0, g, l.m[at] + c0, l.v[at] + c0, n, step);
+        else if (kind == kScoreF16) adam_values<kScoreF16, PAST>(l.p[at] + c0, g, l.m[at] + c0, l.v[at] + c0, n, step);
+        else adam_values<kScoreBF16, PAST>(l.p[at] + c0, g, l.m[at] + c0, l.v[at] + c0, n, step);
+    }
+}
+
+// The gradients of Adam's list as one whose squares are summed.
+template <class M> __device__ __forceinline__ void visit(const AdamList& l, u32 at, u32 piece, M&& make) {
+    const u64 c0 = (u64)(piece - l.first[at]) * l.piece, count = l.count[at];
+    const u32 kind = (u32)(count >> kKindBit), n = (u32)min((u64)l.piece, (count & ((1ull << kKindBit) - 1)) - c0);
+    const char* g = l.g[at] + c0 * (kind == kScoreF32 ? 4 : 2);
+    if (kind == kScoreF32) visit<kScoreF32>(g, nullptr, n, make.template of<kScoreF32>());
+    else if (kind == kScoreF16) visit<kScoreF16>(g, nullptr, n, make.template of<kScoreF16>());
+    else visit<kScoreBF16>(g, nullptr, n, make.template of<kScoreBF16>());
+}
+
 // A norm that is no number or infinite: everything is left as it is.
-__global__ __launch_bounds__(kThreads) void k_adam_list(const AdamSegs list, const double* sums, u32 n_sums, double most, const AdamRates by, float* norm) {
+template <bool PAST> __global__ __launch_bounds__(kThreads) void k_adam_list(const AdamList list, const double* sums, u32 n_sums, double most, const AdamRates by, float* norm) {
+    const Places<AdamList> places(list);
     const Norm r = norm_of(sums, n_sums, most);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r.norm;
     if (!(r.norm < __builtin_inf())) return;
-    const Adam step{by, r.factor};
-    const u32 first = firsts(list);
-    for (u32 piece = blockIdx.x; piece < list.pieces; piece += gridDim.x) {
-        const AdamSeg& s = list.seg[uniform(place_of(piece, first))];
-        if (s.kind == kScoreF32) adam_piece<kScoreF32>(s, piece - s.first, step);
-        else if (s.kind == kScoreF16) adam_piece<kScoreF16>(s, piece - s.first, step);
-        else adam_piece<kScoreBF16>(s, piece - s.first, step);
-    }
+    adam<PAST>(list, places, Adam{by, r.factor});
+}
+
+__global__ __launch_bounds__(1024) void k_adam_few(const AdamList list, double most, const AdamRates by, float* norm) {
+    const Places<AdamList> places(list);
+    const Norm r = norm_of(squares(list, places), most);
+    if (norm && threadIdx.x == 0) *norm = (float)r.norm;
+    if (!(r.norm < __builtin_inf())) return;
+    adam<false>(list, places, Adam{by, r.factor});
 }
 
 // ---- lists -----------------------------------------------------------------------------------------------------------
 u64 size_of(int kind) { return kind == kScoreF32 ? 4 : 2; }
+u64 packed_count(u64 count, int kind) { return count | (u64)kind << kKindBit; }
 
-// Adds a tensor of rows x cols values; rows without a gap are one.
-void add(Segs& l, int kind, const void* src, void* dst, u64 rows, u64 cols, u64 src_stride, u64 dst_stride) {
-    if (rows > 1 && src_stride == cols && dst_stride == cols) { cols *= rows; rows = 1; }
-    Seg& s = l.seg[l.n++];
-    s.src = (const char*)src;
-    s.dst = (char*)dst;
-    s.rows = rows;
-    s.cols = cols;
-    s.src_stride = src_stride * size_of(kind);
-    s.dst_stride = dst_stride * size_of(kind);
-    s.first = l.pieces;
-    s.kind = (u32)kind;
-    if (rows == 1 || cols > kPiece / 2) {
-        s.row_pieces = (u32)((cols + kPiece - 1) / kPiece);
-        s.rows_piece = 1;
-        l.pieces += (u32)rows * s.row_pieces;
-    } else {
-        s.row_pieces = 0;
-        s.rows_piece = (u32)(kPiece / cols);
-        l.pieces += (u32)((rows + s.rows_piece - 1) / s.rows_piece);
+// Few values in all are cut finer: more wavefronts share them, and a step's 64-bit arithmetic most of all.  Us: clipping by 1024 / 2048 /
+// 4096 values 2 x 500000 f32 8.6 / 9.0 / 10.5, 2 x 2000000 14.1 / 13.0 / 13.2, the padded
+// rows of 160 million bf16 values - / 176 / 167; Adam by 256 / 512 / 1024 2 x 8000
+// 8.7 / 8.9 / 10.1, 2 x 256000 9.8 / 10.1 / 11.7, by 1024 / 2048 / 4096 2 x 500000 13.2 / 16.6 / 24.0, 2 x 1000000 17.4 / 17.9 / 24.8,
+// 2 x 32000000 333 / 333 / 353.
+u32 clip_piece(u64 values) { return values < 1ull << 21 ? 1024 : values < 1ull << 26 ? 2048 : 4096; }
+u32 step_piece(u64 values) { return values < 3ull << 18 ? 256 : values < 1ull << 21 ? 1024 : 2048; }
+
+// Up to so many pieces are one workgroup's, in one launch.  One launch / two, us: clipping 16000 f32 5.7 / 8.7, 32000 7.0 / 8.7, 4 x 8000 bf16
+// 8.9 / 8.8, 64000 f32 10.8 / 8.7; Adam 2 x 2000 5.9 / 8.8, 2 x 4000 9.1 / 8.8, 2 x 8000 15.4 / 8.7.
+constexpr u32 kFewPieces = 24;
+
+// From so many bytes of results on they go past the caches, which the gradients' second reading has for itself then.  With / without,
+// us: clipping 2 x 4000000 f32 19.6 / 19.3, 2 x 16000000 67 / 80, 2 x 64000000 266 / 292; Adam 2 x 2000000 28.8 / 26.5, 2 x 8000000 95 /
+// 103, 2 x 64000000 746 / 821.  (Clipped gradients of less are read by the step that follows out of the cache.)
+constexpr u64 kPastClip = 128ull << 20, kPastStep = 64ull << 20;
+
+struct Clip {
+    const qsv_tensor *src, *dst;
+    int64_t n;
+    u32 piece;
+    bool all_segs;                    // one list has room for all of them
+    u64 values(int64_t i) const { return (u64)src[i].rows * (u64)src[i].cols; }
+    bool flat(int64_t i) const {
+        const qsv_tensor &a = src[i], &b = dst[i];
+        return a.rows == 1 || (a.row_stride == a.cols && b.row_stride == b.cols);
+    }
+    // Whether tensor i goes to lists of this kind, and there.
+    bool takes(const SegList&, int64_t i) const { return values(i) && (all_segs || !flat(i)); }
+    bool takes(const FlatList&, int64_t i) const { return values(i) && !all_segs && flat(i); }
+    void put(SegList& l, int64_t i) const {
+        const qsv_tensor &a = src[i], &b = dst[i];
+        const bool one = flat(i);
+        Seg& s = l.seg[l.n];
+        s.src = (const char*)a.data_dev;
+        s.dst = (char*)b.data_dev;
+        s.rows = one ? 1 : (u64)a.rows;
+        s.cols = one ? values(i) : (u64)a.cols;
+        s.src_stride = (u64)a.row_stride * size_of(a.kind);
+        s.dst_stride = (u64)b.row_stride * size_of(a.kind);
+        s.kind = (u32)a.kind;
+        const bool parts = s.rows == 1 || s.cols > piece / 2;
+        s.row_pieces = parts ? (u32)((s.cols + piece - 1) / piece) : 0;
+        s.rows_piece = parts ? 1 : (u32)(piece / s.cols);
+        l.pieces += parts ? (u32)s.rows * s.row_pieces : (u32)((s.rows + s.rows_piece - 1) / s.rows_piece);
+    }
+    void put(FlatList& l, int64_t i) const {
+        l.src[l.n] = (const char*)src[i].data_dev;
+        l.dst[l.n] = (char*)dst[i].data_dev;
+        l.count[l.n] = packed_count(values(i), src[i].kind);
+        l.pieces += (u32)((values(i) + piece - 1) / piece);
+    }
+};
+
+struct Step {
+    const qsv_adam_tensor* t;
+    int64_t n;
+    u32 piece;
+    bool takes(const FlatList&, int64_t i) const { return t[i].count > 0; }
+    bool takes(const AdamList&, int64_t i) const { return t[i].count > 0; }
+    void put(FlatList& l, int64_t i) const {
+        l.src[l.n] = (const char*)t[i].grad_dev;
+        l.dst[l.n] = nullptr;
+        l.count[l.n] = packed_count((u64)t[i].count, t[i].kind);
+        l.pieces += (u32)(((u64)t[i].count + piece - 1) / piece);
+    }
+    void put(AdamList& l, int64_t i) const {
+        l.p[l.n] = t[i].param_dev;
+        l.g[l.n] = (const char*)t[i].grad_dev;
+        l.m[l.n] = t[i].m_dev;
+        l.v[l.n] = t[i].v_dev;
+        l.count[l.n] = packed_count((u64)t[i].count, t[i].kind);
+        l.pieces += (u32)(((u64)t[i].count + piece - 1) / piece);
+    }
+};
+
+// The tensors from i on, to the end or as many as a list has room for.
+template <class L, class S> void next_list(const S& s, int64_t* i, L& l) {
+    l.n = l.pieces = 0;
+    l.piece = s.piece;
+    for (; *i < s.n && l.n < (u32)L::kRoom; ++*i) {
+        if (!s.takes(l, *i)) continue;
+        l.first[l.n] = l.pieces;
+        s.put(l, *i);
+        ++l.n;
     }
 }
 
-bool empty(const qsv_tensor& t) { return t.rows < 1 || t.cols < 1; }
-
-// Tensors from `at` on, up to a launch's room.
-void next_list(const qsv_tensor* src, const qsv_tensor* dst, int64_t n, int64_t* at, Segs& l) {
-    l.n = l.pieces = 0;
-    for (; *at < n && l.n < (u32)kList; ++*at) {
-        const qsv_tensor &a = src[*at], &b = (dst ? dst : src)[*at];
-        if (!empty(a)) add(l, a.kind, a.data_dev, b.data_dev, (u64)a.rows, (u64)a.cols, (u64)a.row_stride, (u64)b.row_stride);
-    }
-}
-void next_list(const qsv_adam_tensor* t, int64_t n, int64_t* at, Segs& l) {
-    l.n = l.pieces = 0;
-    for (; *at < n && l.n < (u32)kList; ++*at)
-        if (t[*at].count > 0) add(l, t[*at].kind, t[*at].grad_dev, nullptr, 1, (u64)t[*at].count, 0, 0);
-}
-void next_list(const qsv_adam_tensor* t, int64_t n, int64_t* at, AdamSegs& l) {
-    l.n = l.pieces = 0;
-    for (; *at < n && l.n < (u32)kList; ++*at) {
-        if (t[*at].count < 1) continue;
-        l.seg[l.n++] = AdamSeg{t[*at].param_dev, (const char*)t[*at].grad_dev, t[*at].m_dev, t[*at].v_dev, (u64)t[*at].count, l.pieces, (u32)t[*at].kind};
-        l.pieces += (u32)(((u64)t[*at].count + kPiece - 1) / kPiece);
-    }
-}
-
-// One launch of the sums a list; the number of sums left.  NEXT fills the list from a place on.
-template <class NEXT> u32 launch_squares(int64_t n, NEXT&& next, double* sums, hipStream_t st) {
-    Segs l;
-    u64 all = 0;
-    u32 lists = 0, done = 0;
-    for (int64_t at = 0; at < n;) { next(&at, l); all += l.pieces; lists += l.pieces ? 1 : 0; }
-    for (int64_t at = 0; at < n;) {
-        next(&at, l);
+// One launch of the sums a list; `all` pieces share kSums of them.
+template <class L, class S> void launch_squares(const S& s, u64 all, double* sums, u32* done, hipStream_t st) {
+    L l;
+    for (int64_t i = 0; i < s.n;) {
+        next_list(s, &i, l);
         if (!l.pieces) continue;
-        const u64 share = lists == 1 ? kSums : 1 + (u64)l.pieces * kSums / all;
-        const u32 grid = (u32)std::min((u64)l.pieces, share);
-        hipLaunchKernelGGL(k_squares, dim3(grid), dim3(kThreads), 0, st, l, sums + done);
-        done += grid;
+        const u64 blocks = (l.pieces + kThreads / 64 - 1) / (kThreads / 64);
+        const u32 grid = (u32)std::min(blocks, 1 + (u64)l.pieces * (kSums - 1) / all);
+        hipLaunchKernelGGL(k_squares<L>, dim3(grid), dim3(kThreads), 0, st, l, sums + *done);
+        *done += grid;
     }
-    return done;
+}
+
+u32 grid_for(u32 pieces) { return std::min((pieces + kThreads / 64 - 1) / (kThreads / 64), kSums); }
+
+template <class L, bool PAST> void launch_scale(const Clip& s, const double* sums, u32 done, double max_norm, int over, float** norm, hipStream_t st) {
+    L l;
+    for (int64_t i = 0; i < s.n;) {
+        next_list(s, &i, l);
+        if (!l.pieces) continue;
+        hipLaunchKernelGGL((k_scale<L, PAST>), dim3(grid_for(l.pieces)), dim3(kThreads), 0, st, l, sums, done, max_norm, over, *norm);
+        *norm = nullptr;
+    }
+}
+
+template <class L, class S> u64 all_pieces(const S& s) {
+    L l;
+    u64 all = 0;
+    for (int64_t i = 0; i < s.n;) { next_list(s, &i, l); all += l.pieces; }
+    return all;
 }
 
 }  // namespace
@@ -290,31 +471,61 @@ size_t norm_scratch_bytes() { return (kSums + kMostLists) * sizeof(double); }
 
 hipError_t launch_clip(const qsv_tensor* grads, const qsv_tensor* outs, int64_t n, double max_norm, float* norm, void* scratch, hipStream_t st) {
     double* sums = (double*)scratch;
-    const u32 done = launch_squares(n, [&](int64_t* at, Segs& l) { next_list(grads, outs, n, at, l); }, sums, st);
-    if (max_norm == HUGE_VAL && !outs) {
+    Clip s{grads, outs ? outs : grads, n, 0, n <= kSegs};
+    u64 values = 0, bytes = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        values += s.values(i);
+        bytes += s.values(i) * size_of(grads[i].kind);
+    }
+    s.piece = clip_piece(values);
+    const int over = outs ? 0 : 1;
+    if (s.all_segs) {
+        SegList l;
+        int64_t i = 0;
+        next_list(s, &i, l);
+        if (l.pieces <= kFewPieces) {
+            hipLaunchKernelGGL(k_clip_few<SegList>, dim3(1), dim3(1024), 0, st, l, max_norm, over, norm);
+            return hipGetLastError();
+        }
+    }
+    const u64 all = all_pieces<SegList>(s) + all_pieces<FlatList>(s);
+    u32 done = 0;
+    launch_squares<SegList>(s, all, sums, &done, st);
+    launch_squares<FlatList>(s, all, sums, &done, st);
+    if (!done || (over && max_norm == HUGE_VAL)) {
         if (norm) hipLaunchKernelGGL(k_norm, dim3(1), dim3(kThreads), 0, st, sums, done, norm);
         return hipGetLastError();
     }
-    if (!done && norm) hipLaunchKernelGGL(k_norm, dim3(1), dim3(kThreads), 0, st, sums, done, norm);
-    Segs l;
-    for (int64_t at = 0; at < n;) {
-        next_list(grads, outs, n, &at, l);
-        if (!l.pieces) continue;
-        hipLaunchKernelGGL(k_scale, dim3(std::min(l.pieces, kSums)), dim3(kThreads), 0, st, l, sums, done, max_norm, outs ? 0 : 1, norm);
-        norm = nullptr;
+    if (bytes >= kPastClip) {
+        launch_scale<FlatList, true>(s, sums, done, max_norm, over, &norm, st);
+        launch_scale<SegList, true>(s, sums, done, max_norm, over, &norm, st);
+    } else {
+        launch_scale<FlatList, false>(s, sums, done, max_norm, over, &norm, st);
+        launch_scale<SegList, false>(s, sums, done, max_norm, over, &norm, st);
     }
     return hipGetLastError();
 }
 
 hipError_t launch_adam_clipped(const qsv_adam_tensor* t, int64_t n, double max_norm, const AdamRates& by, float* norm, void* scratch, hipStream_t st) {
     double* sums = (double*)scratch;
-    const u32 done = launch_squares(n, [&](int64_t* at, Segs& l) { next_list(t, n, at, l); }, sums, st);
-    if (!done && norm) hipLaunchKernelGGL(k_norm, dim3(1), dim3(kThreads), 0, st, sums, done, norm);
-    AdamSegs l;
-    for (int64_t at = 0; at < n;) {
-        next_list(t, n, &at, l);
+    Step s{t, n, 0};
+    u64 values = 0;
+    for (int64_t i = 0; i < n; ++i) values += (u64)t[i].count;
+    s.piece = step_piece(values);
+    AdamList l;
+    int64_t i = 0;
+    next_list(s, &i, l);
+    if (i == n && l.pieces <= kFewPieces) {
+        hipLaunchKernelGGL(k_adam_few, dim3(1), dim3(1024), 0, st, l, max_norm, by, norm);
+        return hipGetLastError();
+    }
+    u32 done = 0;
+    launch_squares<FlatList>(s, all_pieces<FlatList>(s), sums, &done, st);
+    for (i = 0; i < n;) {
+        next_list(s, &i, l);
         if (!l.pieces) continue;
-        hipLaunchKernelGGL(k_adam_list, dim3(std::min(l.pieces, kSums)), dim3(kThreads), 0, st, l, sums, done, max_norm, by, norm);
+        if (12 * values >= kPastStep) hipLaunchKernelGGL(k_adam_list<true>, dim3(grid_for(l.pieces)), dim3(kThreads), 0, st, l, sums, done, max_norm, by, norm);
+        else hipLaunchKernelGGL(k_adam_list<false>, dim3(grid_for(l.pieces)), dim3(kThreads), 0, st, l, sums, done, max_norm, by, norm);
         norm = nullptr;
     }
     return hipGetLastError();

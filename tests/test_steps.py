@@ -65,6 +65,9 @@ def test_refusals_of_clipping(checks):
     t[0].reserved = 1
     assert b"reserved" in say(t)
     assert say(tensors((None, 0, 5, 0), (None, 5, 0, 0))) is None
+    half = 1 << 37
+    assert say(tensors((0x1000, 1, half, 0), (0x1000 + 4 * half, 1, half, 0))) is None
+    assert b"2^38" in say(tensors((0x1000, 1, half, 0), (0x1000 + 4 * half, 1, half, 0), (0x1000 + 8 * half, 1, 1, 0)))
     twice = tensors(one, one)
     assert b"overlap" in say(twice) and say(twice, norm=INF) is None                     # scaled twice, or read only
     assert b"overlap" in say(tensors(one, (0x1000 + 396, 1, 8, 0))) and say(tensors(one, (0x1000 + 400, 1, 8, 0))) is None
@@ -95,6 +98,8 @@ def test_refusals_of_adam(checks):
     one = (0x1000, 0x2000, 0x3000, 0x4000, 100)
     assert say(lists(one)) is None and say(None, 0) is None and b"NULL" in say(None, 1) and b"4096" in say(lists(one), 4097)
     assert b"max_norm" in say(lists(one), m=-0.5) and say(lists(one), m=INF) is None
+    far = [1 << 44, 2 << 44, 3 << 44, 4 << 44]
+    assert say(lists((*far, 1 << 38))) is None and b"2^38" in say(lists((*far, 1 << 38), (*[5 * x for x in far], 1)))
     assert say(lists((None, None, None, None, 0))) is None and b"count" in say(lists(one[:4] + (-1,)))
     for i in range(4):
         assert b"NULL" in say(lists(one[:i] + (None,) + one[i + 1:])) and b"aligned" in say(lists(one[:i] + (one[i] + 2,) + one[i + 1:]))
