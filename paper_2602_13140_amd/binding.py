@@ -294,30 +294,56 @@ def _teacher(rows, top_idx, top_logits, temperature, top_lse, dev):
                        _flat(top_lse, "float32", dev, "top_lse", rows), float(temperature))
 
 
+def _grid(t, dtype, dev, what):
+    """(address, rows, columns, row stride) of rows whose values lie next to each other."""
+    shape, stride = t.shape, t.stride()
+    if not (t.dtype is dtype and t.get_device() == dev and len(shape) == 2 and (stride[1] == 1 or shape[1] < 2)):
+        _need(False, "%s must be rows of %s on cuda:%d, the values of a row next to each other" % (what, str(dtype)[6:], dev))
+    return t.data_ptr(), shape[0], shape[1], stride[0]
+
+
+def _each(t, dtype, dev, shape, what):
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _need(False, "%s must be a contiguous tensor of %s %s on cuda:%d" % (what, str(dtype)[6:], list(shape), dev))
+
+
+def _scores(t, kind, dev, what):
+    _need(kind in _SCORES, "unknown kind of scores")
+    _need(t is not None, what + " must be given")
+    return _grid(t, _dtype(_TYPE_OF[kind]), dev, what)
+
+
+_SCORES = (QSV_S_F32, QSV_S_F16, QSV_S_BF16)
+
+
 def _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of):
-    """The part of a request that qsv_adjust and its backward pass share; tensors of whole numbers may have rows further apart."""
-    def table(t, what, rows_at):
-        if not (t.get_device() == d and t.dim() == 2 and t.dtype is _dtype("int32") and (t.shape[1] < 2 or t.stride(1) == 1)
-                and rows_at in (None, t.shape[0])):
-            _need(False, "%s must be rows of int32 on cuda:%d, the values of a row next to each other" % (what, d))
-        return t
+    """The part of a request that qsv_adjust and its backward pass share; rows of whole numbers may lie further apart."""
+    i32, f32, each = _dtype("int32"), _dtype("float32"), (rows,)
     if prior is not None:
-        table(prior, "prior", rows)
-        r.prior_dev, r.n_prior, r.prior_stride = prior.data_ptr(), prior.shape[1], prior.stride(0)
-    r.prior_len_dev, r.prompt_len_dev = _flat(prior_len, "int32", d, "prior_len", rows), _flat(prompt_len, "int32", d, "prompt_len", rows)
-    r.repetition_dev, r.frequency_dev = _flat(repetition, "float32", d, "repetition", rows), _flat(frequency, "float32", d, "frequency", rows)
-    r.presence_dev = _flat(presence, "float32", d, "presence", rows)
+        r.prior_dev, n, r.n_prior, r.prior_stride = _grid(prior, i32, d, "prior")
+        _need(n == rows, "prior must have the scores' rows")
     if entry_idx is not None:
         _need(entry_idx.dim() == 2, "entry_idx must be [rows][n_entries]")
         r.n_entries = entry_idx.shape[1]
         r.entry_idx_dev = _flat(entry_idx, "int32", d, "entry_idx", rows, r.n_entries)
     if masks is not None:
-        table(masks, "masks", None)
-        _need(masks.shape[1] >= (r.cols + 31) // 32, "masks must have a bit for each outcome")
-        r.masks_dev, r.n_masks, r.mask_stride = masks.data_ptr(), masks.shape[0], masks.stride(0)
-        r.mask_of_dev = _flat(mask_of, "int32", d, "mask_of", rows)
+        r.masks_dev, r.n_masks, words, r.mask_stride = _grid(masks, i32, d, "masks")
+        _need(words >= (r.cols + 31) // 32, "masks must have a bit for each outcome")
     else:
         _need(mask_of is None, "mask_of without masks")
+    if prior_len is not None:
+        r.prior_len_dev = _each(prior_len, i32, d, each, "prior_len")
+    if prompt_len is not None:
+        r.prompt_len_dev = _each(prompt_len, i32, d, each, "prompt_len")
+    if repetition is not None:
+        r.repetition_dev = _each(repetition, f32, d, each, "repetition")
+    if frequency is not None:
+        r.frequency_dev = _each(frequency, f32, d, each, "frequency")
+    if presence is not None:
+        r.presence_dev = _each(presence, f32, d, each, "presence")
+    if mask_of is not None:
+        r.mask_of_dev = _each(mask_of, i32, d, each, "mask_of")
 
 
 def _kind_of(t):
@@ -506,34 +532,38 @@ class Context:
                    presence=None, bias=None, entry_idx=None, entry_bias=None, masks=None, mask_of=None):
         """out None: over the scores."""
         r, d = qsv_adjust_req(), self.dev.index
-        s = _rows(scores, kind, d, "scores")
-        o = s if out is None else _rows(out, kind, d, "out")
-        _need(o.shape == s.shape, "out must have the shape of the scores")
-        r.kind, r.scores_dev, r.row_stride, r.out_dev, r.out_stride = kind, s.data_ptr(), s.stride(0), o.data_ptr(), o.stride(0)
-        r.rows, r.cols = s.shape
-        _adjustment(r, d, r.rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
-        r.bias_dev = _flat(bias, "float32", d, "bias", r.cols)
-        _need((entry_idx is None) == (entry_bias is None), "entry_idx and entry_bias go together")
-        r.entry_bias_dev = _flat(entry_bias, "float32", d, "entry_bias", r.rows, r.n_entries)
+        r.kind = kind
+        r.scores_dev, rows, cols, r.row_stride = at = _scores(scores, kind, d, "scores")
+        r.rows, r.cols = rows, cols
+        r.out_dev, n, m, r.out_stride = at if out is None else _scores(out, kind, d, "out")
+        _need(n == rows and m == cols, "out must have the shape of the scores")
+        _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
+        if bias is not None:
+            r.bias_dev = _flat(bias, "float32", d, "bias", cols)
+        if entry_idx is not None or entry_bias is not None:
+            _need(entry_idx is not None and entry_bias is not None, "entry_idx and entry_bias go together")
+            r.entry_bias_dev = _flat(entry_bias, "float32", d, "entry_bias", rows, r.n_entries)
         self._check(self.L.qsv_adjust(self.h, ctypes.byref(r)))
 
     def qsv_adjust_grad(self, kind, grad_out, grad=None, scores=None, grad_bias=None, grad_entry=None, prior=None, prior_len=None,
                         prompt_len=None, repetition=None, frequency=None, presence=None, entry_idx=None, masks=None, mask_of=None):
         """grad may be grad_out; None: the gradients of the biases alone."""
         r, b, d = qsv_adjust_req(), qsv_adjust_grad_req(), self.dev.index
-        g = _rows(grad_out, kind, d, "grad_out")
         r.kind = kind
-        r.rows, r.cols = g.shape
-        for t, what in ((scores, "scores"), (grad, "grad")):
-            _need(t is None or _rows(t, kind, d, what).shape == g.shape, "%s must have the shape of grad_out" % what)
+        b.grad_out_dev, rows, cols, b.grad_out_stride = _scores(grad_out, kind, d, "grad_out")
+        r.rows, r.cols = rows, cols
+        n, m = rows, cols
         if scores is not None:
-            r.scores_dev, r.row_stride = scores.data_ptr(), scores.stride(0)
-        b.grad_out_dev, b.grad_out_stride = g.data_ptr(), g.stride(0)
+            r.scores_dev, n, m, r.row_stride = _scores(scores, kind, d, "scores")
+        _need(n == rows and m == cols, "scores must have the shape of grad_out")
         if grad is not None:
-            b.grad_dev, b.grad_stride = grad.data_ptr(), grad.stride(0)
-        _adjustment(r, d, r.rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
-        b.grad_bias_dev = _flat(grad_bias, "float32", d, "grad_bias", r.cols)
-        b.grad_entry_dev = _flat(grad_entry, "float32", d, "grad_entry", r.rows, r.n_entries)
+            b.grad_dev, n, m, b.grad_stride = _scores(grad, kind, d, "grad")
+        _need(n == rows and m == cols, "grad must have the shape of grad_out")
+        _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
+        if grad_bias is not None:
+            b.grad_bias_dev = _flat(grad_bias, "float32", d, "grad_bias", cols)
+        if grad_entry is not None:
+            b.grad_entry_dev = _flat(grad_entry, "float32", d, "grad_entry", rows, r.n_entries)
         self._check(self.L.qsv_adjust_grad(self.h, ctypes.byref(r), ctypes.byref(b)))
 
     def _list(self, tensors, cls):

@@ -26,31 +26,32 @@ constexpr int kEntryBit = 21, kEntryMost = 1023;
 
 // What row r is adjusted by.
 struct Row {
-    double by, inverse, each, once;     // R, 1 / R, F, A
+    float by, each, once;      // R, F, A
     int len, prompt;
-    const u32* mask;                    // NULL: all are allowed
-    bool good;                          // its parameters are in their ranges
+    const u32* mask;           // NULL: all are allowed
+    bool good;                 // its parameters are in their ranges
 };
 
+// (Absent parameters are read from here: loads without branches between them wait for memory once.)
+__device__ const float kOff[2] = {0.f, 1.f};
+__device__ const int kNone = 0;
+
 __device__ __forceinline__ Row row_of(const AdjustArgs& a, u64 r) {
+    const float by = *(a.repetition ? a.repetition + r : kOff + 1), each = *(a.frequency ? a.frequency + r : kOff), once = *(a.presence ? a.presence + r : kOff);
+    const int len = *(a.prior_len ? a.prior_len + r : &kNone), prompt = *(a.prompt_len ? a.prompt_len + r : &kNone);
+    const int at = *(a.mask_of ? a.mask_of + r : &kNone);
     Row f;
-    const float by = a.repetition ? a.repetition[r] : 1.f, each = a.frequency ? a.frequency[r] : 0.f, once = a.presence ? a.presence[r] : 0.f;
-    f.len = a.n_prior;
-    f.prompt = 0;
-    if (a.n_prior) {
-        if (a.prior_len) f.len = a.prior_len[r];
-        if (a.prompt_len) f.prompt = a.prompt_len[r];
-    }
+    f.by = by;
+    f.each = each;
+    f.once = once;
+    f.len = a.n_prior && a.prior_len ? len : a.n_prior;
+    f.prompt = a.n_prior ? prompt : 0;
     f.good = by > 0.f && by < kInf && fabsf(each) < kInf && fabsf(once) < kInf && f.prompt >= 0 && f.prompt <= f.len && f.len <= a.n_prior;
-    f.by = (double)by;
-    f.inverse = 1.0 / f.by;
-    f.each = (double)each;
-    f.once = (double)once;
     f.mask = nullptr;
     if (a.masks) {
-        const int64_t at = a.mask_of ? (int64_t)a.mask_of[r] : a.mask_each ? (int64_t)r : 0;
-        if (at < -1 || at >= a.n_masks) f.good = false;
-        else if (at >= 0) f.mask = a.masks + (u64)at * (u64)a.mask_stride;
+        const int64_t mask = a.mask_of ? (int64_t)at : a.mask_each ? (int64_t)r : 0;
+        if (mask < -1 || mask >= a.n_masks) f.good = false;
+        else if (mask >= 0) f.mask = a.masks + (u64)mask * (u64)a.mask_stride;
     }
     return f;
 }
@@ -77,18 +78,21 @@ __device__ __forceinline__ Part part_of(char* lds, int n_entries, u32 width) {
     p.entries = (u32*)(p.bias + room);
     return p;
 }
+// Columns that the table has room for: of rows shorter than a part no more than theirs.
+__host__ __device__ inline u32 part_room(u32 width, u32 cols) { return width < cols ? width : (cols + 127) & ~127u; }
 inline size_t part_bytes(int n_entries, u32 width) { return (size_t)entry_room(n_entries) * 16 + (size_t)width * 4 + width / 8 + 16; }
 
 __device__ __forceinline__ void mark(const Part& p, u32 k) { atomicOr(&p.bits[k / 32], 1u << (k & 31)); }
 
-// 16 of the row's earlier outcomes a thread: four at a time from place i on, -1 behind the last.
+// 4 N of the row's earlier outcomes a thread: four at a time from place i0 on, -1 behind the last of len.
 typedef int four __attribute__((ext_vector_type(4)));
 typedef int four_at4 __attribute__((ext_vector_type(4), aligned(4)));
-template <int NT> __device__ __forceinline__ void prior_load(const int* prior, int len, int i0, four (&t)[4]) {
+template <int NT, int N> __device__ __forceinline__ void prior_load(const int* prior, int len, int i0, four (&t)[N]) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < N; ++u) {
         const int i = i0 + (u * NT + (int)threadIdx.x) * 4;
         t[u] = four{-1, -1, -1, -1};
+        if (i0 + u * NT * 4 >= len) continue;
         if (i + 4 <= len) {
             t[u] = *(const four_at4*)(prior + i);
         } else {
@@ -98,21 +102,33 @@ template <int NT> __device__ __forceinline__ void prior_load(const int* prior, i
         }
     }
 }
-template <int NT> __device__ __forceinline__ void prior_count(const Row& f, const Part& p, u32 c0, u32 n, int i0, const four (&t)[4]) {
+// Those behind a row's own last one become -1.
+template <int NT, int N> __device__ __forceinline__ void prior_cut(int len, four (&t)[N]) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < N; ++u) {
+        const int left = len - (u * NT + (int)threadIdx.x) * 4;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const u32 k = (u32)t[u][w] - c0;
-            if (k >= n) continue;
-            if (i0 + (u * NT + (int)threadIdx.x) * 4 + w < f.prompt) atomicOr(&p.word[k], kPrompt);
-            else atomicAdd(&p.word[k], 1u);
-            mark(p, k);
-        }
+        for (int w = 0; w < 4; ++w)
+            if (w >= left) t[u][w] = -1;
+    }
 }
 
-// The part's entries in their order, gathered by the first wavefront.
-__device__ __forceinline__ void gather_entries(const AdjustArgs& a, u64 r, const Part& p, u32 c0, u32 n) {
+// Counts an outcome at column k of the part.
+__device__ __forceinline__ void prior_add(const Part& p, u32 k, bool prompt) {
+    if (prompt) atomicOr(&p.word[k], kPrompt);
+    else atomicAdd(&p.word[k], 1u);
+    mark(p, k);
+}
+// ... and is true for the first that names the column.
+__device__ __forceinline__ bool prior_count(const Part& p, u32 k, bool prompt) {
+    const u32 was = prompt ? atomicOr(&p.word[k], kPrompt) : atomicAdd(&p.word[k], 1u);
+    if (was) return false;
+    mark(p, k);
+    return true;
+}
+
+// The part's entries in their order, gathered by the first wavefront.  ZERO: their columns' words start at 0.
+template <bool ZERO> __device__ __forceinline__ void gather_entries(const AdjustArgs& a, u64 r, const Part& p, u32 c0, u32 n) {
     const u32 lane = threadIdx.x;
     const int* idx = a.entry_idx + r * (u64)a.n_entries;
     const float* bias = a.entry_bias + r * (u64)a.n_entries;
@@ -130,7 +146,11 @@ __device__ __forceinline__ void gather_entries(const AdjustArgs& a, u64 r, const
         for (int u = 0; u < 4; ++u) {
             const u64 in = __ballot(k[u] < n);
             const u32 at = m + __popcll(in & ((1ull << lane) - 1));
-            if (k[u] < n) { p.column[at] = (int)k[u]; p.bias[at] = b[u]; }
+            if (k[u] < n) {
+                p.column[at] = (int)k[u];
+                p.bias[at] = b[u];
+                if (ZERO) p.word[k[u]] = 0;
+            }
             m += (u32)__popcll(in);
         }
     }
@@ -138,8 +158,8 @@ __device__ __forceinline__ void gather_entries(const AdjustArgs& a, u64 r, const
     if (lane == 0) *p.entries = m;
 }
 
-// A column's entries by the thread of the first of them.
-template <int NT> __device__ __forceinline__ void add_entries(const Part& p) {
+// A column's entries by the thread of the first of them; put(column, the place of that one).
+template <int NT, class F> __device__ __forceinline__ void add_entries(const Part& p, F&& put) {
     const u32 m = *p.entries;
     for (u32 j = threadIdx.x; j < m; j += NT) {
         const int k = p.column[j];
@@ -158,38 +178,19 @@ template <int NT> __device__ __forceinline__ void add_entries(const Part& p) {
         }
         if (!first) continue;
         p.sum[j] = sum;
-        atomicOr(&p.word[k], (j + 1) << kEntryBit);
-        mark(p, (u32)k);
+        put((u32)k, j);
     }
-}
-
-// The table of the part's n columns.  between: what is to be under way meanwhile.
-template <int NT, bool ENTRIES, class F> __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row& f, const Part& p, u32 c0, u32 n, u32 width, F&& between) {
-    const int* prior = a.prior + r * (u64)a.prior_stride;
-    four t[4];
-    prior_load<NT>(prior, f.len, 0, t);
-    between();
-    for (u32 i = threadIdx.x; i < (width + width / 32) / 4; i += NT) ((four*)p.word)[i] = four{0, 0, 0, 0};    // bits lie behind the words
-    if (ENTRIES && a.n_entries && threadIdx.x < 64) gather_entries(a, r, p, c0, n);
-    __syncthreads();
-    prior_count<NT>(f, p, c0, n, 0, t);
-    for (int i0 = 16 * NT; i0 < f.len; i0 += 16 * NT) {
-        prior_load<NT>(prior, f.len, i0, t);
-        prior_count<NT>(f, p, c0, n, i0, t);
-    }
-    if (ENTRIES && a.n_entries) add_entries<NT>(p);
-    __syncthreads();
 }
 
 __device__ __forceinline__ bool seen(u32 word) { return (word & (kPrompt | kCount)) != 0; }
 
-// A place whose column has a word.
-__device__ __forceinline__ float adjusted(const Row& f, const Part& p, u32 word, float z, float bias) {
+// A place whose column has a word.  inverse: 1 / R.
+__device__ __forceinline__ float adjusted(const Row& f, double inverse, const Part& p, u32 word, float z, float bias) {
     double v = (double)z;
     if (seen(word)) {
-        v *= v > 0.0 ? f.inverse : f.by;
+        v *= v > 0.0 ? inverse : (double)f.by;
         const u32 c = word & kCount;
-        if (c) v -= f.each * (double)c + f.once;
+        if (c) v -= (double)f.each * (double)c + (double)f.once;
     }
     v += (double)bias;
     const u32 e = (word >> kEntryBit) & kEntryMost;
@@ -198,8 +199,105 @@ __device__ __forceinline__ float adjusted(const Row& f, const Part& p, u32 word,
 }
 
 // ... and its gradient.
-__device__ __forceinline__ float taken_back(const Row& f, u32 word, float z, float g) {
-    return seen(word) ? (float)((double)g * (z > 0.f ? f.inverse : f.by)) : g;
+__device__ __forceinline__ float taken_back(const Row& f, double inverse, u32 word, float z, float g) {
+    return seen(word) ? (float)((double)g * (z > 0.f ? inverse : (double)f.by)) : g;
+}
+
+// The table of the part's n columns, a word turned into its place's result in 32 bits at once.  Histories that the threads keep (t, 8 NT)
+// fetch the values at their columns first, and the first that counts at a column works it out; only words of theirs start at 0.  Longer ones
+// have the bitmap looked through.  result(word, column, its value, 1 / R).
+constexpr int kKept = 2;
+template <int KIND, int NT, bool ENTRIES, class G>
+__device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row& f, const Part& p, const char* in, u32 c0, u32 n, four (&t)[kKept], G&& result) {
+    const bool kept = a.n_prior <= 4 * kKept * NT, entries = ENTRIES && a.n_entries;
+    float z[kKept][4];
+    for (u32 i = threadIdx.x; i < (n + 31) / 32; i += NT) p.bits[i] = 0;
+    if (kept) {
+        prior_cut<NT>(f.len, t);
+#pragma unroll
+        for (int u = 0; u < kKept; ++u) {
+            if (u * 4 * NT >= f.len) break;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                if ((u32)t[u][w] - c0 < n) {
+                    z[u][w] = value_at<KIND>(in, (u32)t[u][w]);
+                    p.word[(u32)t[u][w] - c0] = 0;
+                }
+        }
+    } else {
+        for (u32 i = threadIdx.x; i < (n + 3) / 4; i += NT) ((four*)p.word)[i] = four{0, 0, 0, 0};
+    }
+    if (entries && threadIdx.x < 64) gather_entries<true>(a, r, p, c0, n);
+    __syncthreads();
+    u32 mine = 0, mine_entries = 0;
+    if (kept) {
+#pragma unroll
+        for (int u = 0; u < kKept; ++u) {
+            if (u * 4 * NT >= f.len) break;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const u32 k = (u32)t[u][w] - c0;
+                if (k < n && prior_count(p, k, (u * NT + (int)threadIdx.x) * 4 + w < f.prompt)) mine |= 1u << (u * 4 + w);
+            }
+        }
+    } else {
+        const int* prior = a.prior + r * (u64)a.prior_stride;
+        for (int i0 = 0; i0 < f.len; i0 += 16 * NT) {
+            four q[4];
+            prior_load<NT>(prior, f.len, i0, q);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const u32 k = (u32)q[u][w] - c0;
+                    if (k < n) prior_add(p, k, i0 + (u * NT + (int)threadIdx.x) * 4 + w < f.prompt);
+                }
+        }
+    }
+    if (entries)
+        add_entries<NT>(p, [&](u32 k, u32 j) {
+            if (atomicOr(&p.word[k], (j + 1) << kEntryBit)) return;
+            mark(p, k);
+            mine_entries |= 1u << (j / NT);
+        });
+    __syncthreads();
+    if (kept) {
+        if (mine | mine_entries) {
+            const double inverse = 1.0 / (double)f.by;
+#pragma unroll
+            for (int u = 0; u < kKept; ++u) {
+                if (!(mine >> (u * 4) & 15)) continue;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    if (mine >> (u * 4 + w) & 1) {
+                        u32* to = p.word + ((u32)t[u][w] - c0);
+                        *to = __float_as_uint(result(*to, (u32)t[u][w], z[u][w], inverse));
+                    }
+            }
+            for (u32 left = mine_entries; left; left &= left - 1) {
+                const u32 k = (u32)p.column[__builtin_ctz(left) * NT + threadIdx.x];
+                p.word[k] = __float_as_uint(result(p.word[k], c0 + k, value_at<KIND>(in, c0 + k), inverse));
+            }
+        }
+    } else {
+        const double inverse = 1.0 / (double)f.by;
+        for (u32 k0 = threadIdx.x; k0 < n; k0 += 4 * NT) {          // four values under way
+            float x[4];
+            u32 there = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const u32 k = k0 + u * NT;
+                if (k < n && (p.bits[k / 32] >> (k & 31) & 1)) {
+                    there |= 1u << u;
+                    x[u] = value_at<KIND>(in, c0 + k);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (there >> u & 1) p.word[k0 + u * NT] = __float_as_uint(result(p.word[k0 + u * NT], c0 + k0 + u * NT, x[u], inverse));
+        }
+    }
+    __syncthreads();
 }
 
 __device__ __forceinline__ u32 allowed_at(const u32* mask, u32 k) { return mask ? mask[k >> 5] >> (k & 31) : ~0u; }
@@ -228,37 +326,39 @@ template <int KIND> __device__ __forceinline__ u32 vector_bits(const u32* bits, 
 template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_bounds__(NT) void k_adjust(const AdjustArgs a, const u32 parts) {
     constexpr u32 W = kPer<KIND>, width = NT * NV * W;
     extern __shared__ __align__(16) char lds[];
-    const u64 r = grid_block() / parts;
-    const u32 c0 = (u32)(grid_block() % parts) * width;
+    const u32 block = (u32)grid_block(), r32 = block / parts, c0 = (block - r32 * parts) * width;
+    const u64 r = r32;
     if (r >= (u64)a.rows) return;
-    const Row f = row_of(a, r);
     const u32 n = min(width, a.cols - c0), whole = n / W;
     const char* scores = (const char*)a.scores + (a.scores ? r * (u64)a.stride * kSize<KIND> : 0);
     const char* in = BACK ? (const char*)a.grad_out + r * (u64)a.grad_out_stride * kSize<KIND> : scores;
     char* out = BACK ? (char*)a.grad + r * (u64)a.grad_stride * kSize<KIND> : (char*)a.out + r * (u64)a.out_stride * kSize<KIND>;
-    const Part p = part_of(lds, BACK ? 0 : a.n_entries, width);
+    const Part p = part_of(lds, BACK ? 0 : a.n_entries, part_room(width, a.cols));
     const float none = BACK ? 0.f : -kInf;
+    four t[kKept];
+    if (TABLE && a.n_prior <= 4 * kKept * NT) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
+    vec x[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const u32 j = v * NT + threadIdx.x;
+        if (j < whole) x[v] = vec_at<KIND>(in + (u64)(c0 + j * W) * kSize<KIND>);
+    }
+    const Row f = row_of(a, r);
     if (BACK && a.grad_entry) entry_gradients<KIND, NT>(a, r, f, in, c0, c0 + n);
     if (!f.good) {
         for (u32 k = c0 + threadIdx.x; k < c0 + n; k += NT) store_one<KIND>(out, k, __builtin_nanf(""));
         return;
     }
-    vec x[NV];
     u32 allowed[NV];
-    auto load = [&]() {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const u32 j = v * NT + threadIdx.x, k = c0 + j * W;
-            if (j < whole) x[v] = vec_at<KIND>(in + (u64)k * kSize<KIND>);
-            allowed[v] = f.mask && j < whole ? vector_bits<KIND>(f.mask, k) : kBits<KIND>;
-        }
-    };
-    if (TABLE) fill_part<NT, !BACK>(a, r, f, p, c0, n, width, load);
-    else load();
-    auto place = [&](u32 k, float z) {              // a column that has a word
-        const u32 word = p.word[k - c0];
-        return BACK ? taken_back(f, word, value_at<KIND>(scores, k), z) : adjusted(f, p, word, z, a.bias ? a.bias[k] : 0.f);
-    };
+    for (int v = 0; v < NV; ++v) {
+        const u32 j = v * NT + threadIdx.x;
+        allowed[v] = f.mask && j < whole ? vector_bits<KIND>(f.mask, c0 + j * W) : kBits<KIND>;
+    }
+    if (TABLE)
+        fill_part<KIND, NT, !BACK>(a, r, f, p, in, c0, n, t, [&](u32 word, u32 k, float z, double inverse) {
+            return BACK ? taken_back(f, inverse, word, value_at<KIND>(scores, k), z) : adjusted(f, inverse, p, word, z, a.bias ? a.bias[k] : 0.f);
+        });
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const u32 j = v * NT + threadIdx.x, k = c0 + j * W;
@@ -278,11 +378,6 @@ template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_b
         if (TABLE) {
             const u32 hit = vector_bits<KIND>(p.bits, k - c0);
             if (hit) {
-                // the results take the words' places, from where every column is fetched: registers know no index
-                for (u32 left = hit; left; left &= left - 1) {
-                    const u32 i = __builtin_ctz(left);
-                    p.word[k - c0 + i] = __float_as_uint(place(k + i, value_at<KIND>(in, k + i)));
-                }
                 u32 got[W];
 #pragma unroll
                 for (u32 i = 0; i < W; i += 4) {
@@ -304,47 +399,17 @@ template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_b
     if (k < c0 + n) {
         const float z = value_at<KIND>(in, k);
         float y = !BACK && a.bias ? z + a.bias[k] : z;
-        if (TABLE && p.word[k - c0]) y = place(k, z);
+        if (TABLE && (p.bits[(k - c0) / 32] >> (k & 31) & 1)) y = __uint_as_float(p.word[k - c0]);
         store_one<KIND>(out, k, allowed_at(f.mask, k) & 1 ? y : none);
     }
 }
 
-// The same over the scores (BACK: over the gradient): only the places that change.  fill: the masked ones too.
-template <int KIND, bool BACK, int NT> __global__ __launch_bounds__(NT) void k_adjust_over(const AdjustArgs a, const u32 parts, const u32 width, const int table, const int fill) {
-    extern __shared__ __align__(16) char lds[];
-    const u64 r = grid_block() / parts;
-    const u32 c0 = (u32)(grid_block() % parts) * width;
-    if (r >= (u64)a.rows) return;
-    const Row f = row_of(a, r);
-    const u32 c1 = c0 + min(width, a.cols - c0);
-    const char* scores = (const char*)a.scores + (a.scores ? r * (u64)a.stride * kSize<KIND> : 0);
-    char* out = BACK ? (char*)a.grad + (a.grad ? r * (u64)a.grad_stride * kSize<KIND> : 0) : (char*)a.out + r * (u64)a.out_stride * kSize<KIND>;
-    const Part p = part_of(lds, BACK ? 0 : a.n_entries, width);
-    const float none = BACK ? 0.f : -kInf;
-    if (BACK && a.grad_entry) {
-        entry_gradients<KIND, NT>(a, r, f, (const char*)a.grad_out + r * (u64)a.grad_out_stride * kSize<KIND>, c0, c1);
-        __syncthreads();       // read before the places are written
-    }
-    if (BACK && !a.grad) return;
-    if (!f.good) {
-        if (fill)
-            for (u32 k = c0 + threadIdx.x; k < c1; k += NT) store_one<KIND>(out, k, __builtin_nanf(""));
-        return;
-    }
-    if (table) {
-        fill_part<NT, !BACK>(a, r, f, p, c0, c1 - c0, width, [] {});
-        for (u32 k = c0 + threadIdx.x; k < c1; k += NT) {
-            const u32 word = p.word[k - c0];
-            if (!word || !(allowed_at(f.mask, k) & 1)) continue;
-            const float x = value_at<KIND>(out, k);
-            store_one<KIND>(out, k, BACK ? taken_back(f, word, value_at<KIND>(scores, k), x) : adjusted(f, p, word, x, 0.f));
-        }
-    }
-    if (!f.mask || !fill) return;
-    // 64 words of the mask a wavefront: a store for 64 columns, by those lanes whose column is masked
+// ---- over the scores (BACK: over the gradient): only the places that change ------------------------------------------
+// A row's masked places: 64 words of the mask a wavefront, a store for 64 columns by those lanes whose column is masked.
+template <int KIND, int NT> __device__ __forceinline__ void fill_masked(const u32* mask, char* out, u32 c0, u32 c1, float none) {
     const u32 lane = threadIdx.x & 63;
     for (u32 k0 = c0 + (threadIdx.x >> 6) * 2048; k0 < c1; k0 += NT * 32) {
-        const u32 at = k0 / 32 + lane, word = at * 32 < c1 ? f.mask[at] : ~0u;
+        const u32 at = k0 / 32 + lane, word = at * 32 < c1 ? mask[at] : ~0u;
 #pragma unroll 4
         for (u32 i = 0; i < 32; ++i) {
             const u64 on = (u64)lane_of(word, 2 * i + 1) << 32 | lane_of(word, 2 * i);
@@ -354,18 +419,167 @@ template <int KIND, bool BACK, int NT> __global__ __launch_bounds__(NT) void k_a
     }
 }
 
+template <int KIND> __device__ __forceinline__ void fill_nan(char* out, u32 c0, u32 c1) {
+    for (u32 k = c0 + threadIdx.x; k < c1; k += blockDim.x) store_one<KIND>(out, k, __builtin_nanf(""));
+}
+
+// A row's earlier outcomes by their columns where they are few: a table of twice as many places and more, found by a product's upper
+// bits and the next free place.
+struct Hash {
+    u32 *key, *word;      // by place; key: the column, ~0: free
+    u32 shift;            // 32 - log2 of the places
+    __device__ __forceinline__ u32 place(u32 k) const {
+        const u32 last = (1u << (32 - shift)) - 1;
+        for (u32 at = k * 2654435769u >> shift;; at = (at + 1) & last) {       // 2^32 over the golden ratio; there is a free place
+            const u32 was = atomicCAS(&key[at], ~0u, k);
+            if (was == ~0u || was == k) return at;
+        }
+    }
+};
+constexpr int kHashMost = 4096;          // earlier outcomes and entries: 16 of them a thread are kept
+inline int hash_bits(int n) {
+    int bits = 8;
+    while (1 << bits < 2 * n) ++bits;
+    return bits;
+}
+inline size_t hash_bytes(int n_entries, int bits) { return (size_t)entry_room(n_entries) * 16 + ((size_t)8 << bits) + 16; }
+
+// A workgroup a row for its history and entries (`table`), and `parts` of `width` columns each for its masked places.  bits: log2 of the
+// table's places, 0: nothing but the entries' gradients.  nan: rows with parameters out of range are written.
+template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_over(const AdjustArgs a, const u32 parts, const u32 width, const int table, const int bits, const int nan) {
+    extern __shared__ __align__(16) char lds[];
+    const u32 block = (u32)grid_block(), r32 = block / (parts + table), at = block - r32 * (parts + table);
+    const u64 r = r32;
+    if (r >= (u64)a.rows) return;
+    const Row f = row_of(a, r);
+    char* out = BACK ? (char*)a.grad + (a.grad ? r * (u64)a.grad_stride * kSize<KIND> : 0) : (char*)a.out + r * (u64)a.out_stride * kSize<KIND>;
+    if (at < parts) {
+        const u32 c0 = at * width, c1 = c0 + min(width, a.cols - c0);
+        if (!f.good) fill_nan<KIND>(out, c0, c1);
+        else if (f.mask) fill_masked<KIND, 256>(f.mask, out, c0, c1, BACK ? 0.f : -kInf);
+        return;
+    }
+    const char* scores = (const char*)a.scores + (a.scores ? r * (u64)a.stride * kSize<KIND> : 0);
+    if (BACK && a.grad_entry) {
+        entry_gradients<KIND, 256>(a, r, f, (const char*)a.grad_out + r * (u64)a.grad_out_stride * kSize<KIND>, 0, a.cols);
+        __syncthreads();       // read before the places are written
+    }
+    if (BACK && !a.grad) return;
+    if (!f.good) {
+        if (nan && !parts) fill_nan<KIND>(out, 0, a.cols);
+        return;
+    }
+    if (!bits || (BACK && f.by == 1.f)) return;
+    four t[4];
+    prior_load<256>(a.prior + r * (u64)a.prior_stride, f.len, 0, t);
+    const double inverse = 1.0 / (double)f.by;
+    const int room = entry_room(BACK ? 0 : a.n_entries);
+    Hash h;
+    Part p;                    // of the entries alone
+    p.sum = (double*)lds;
+    h.key = (u32*)(p.sum + room);
+    h.word = h.key + (1u << bits);
+    h.shift = 32 - bits;
+    p.column = (int*)(h.word + (1u << bits));
+    p.bias = (float*)(p.column + room);
+    p.entries = (u32*)(p.bias + room);
+    for (u32 i = threadIdx.x; i < (1u << bits) / 4; i += 256) {
+        ((four*)h.key)[i] = four{-1, -1, -1, -1};
+        ((four*)h.word)[i] = four{0, 0, 0, 0};
+    }
+    const bool entries = !BACK && a.n_entries;
+    if (entries && threadIdx.x < 64) gather_entries<false>(a, r, p, 0, a.cols);
+    __syncthreads();
+    u32 place[4][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (u * 1024 >= f.len) continue;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            place[u][w] = ~0u;
+            if ((u32)t[u][w] >= a.cols) continue;
+            const u32 e = h.place((u32)t[u][w]);
+            if (u * 1024 + (int)threadIdx.x * 4 + w < f.prompt) atomicOr(&h.word[e], kPrompt);
+            else atomicAdd(&h.word[e], 1u);
+            place[u][w] = e;
+        }
+    }
+    if (entries) add_entries<256>(p, [&](u32 k, u32 j) { atomicOr(&h.word[h.place(k)], (j + 1) << kEntryBit); });
+    __syncthreads();
+    // whoever takes a column's word first writes its place
+    auto change = [&](u32 word, u32 k, float x) {
+        store_one<KIND>(out, k, BACK ? taken_back(f, inverse, word, value_at<KIND>(scores, k), x) : adjusted(f, inverse, p, word, x, 0.f));
+    };
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (u * 1024 >= f.len) continue;
+        u32 word[4];
+        float x[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            word[w] = place[u][w] != ~0u ? atomicExch(&h.word[place[u][w]], 0u) : 0;
+            if (word[w] && !(allowed_at(f.mask, (u32)t[u][w]) & 1)) word[w] = 0;
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (word[w]) x[w] = value_at<KIND>(out, (u32)t[u][w]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (word[w]) change(word[w], (u32)t[u][w], x[w]);
+    }
+    if (entries) {
+        for (u32 j = threadIdx.x; j < *p.entries; j += 256) {
+            const u32 k = (u32)p.column[j], word = atomicExch(&h.word[h.place(k)], 0u);
+            if (word && (allowed_at(f.mask, k) & 1)) change(word, k, value_at<KIND>(out, k));
+        }
+    }
+}
+
+// The same for long histories, by parts of a row with a table of their columns each.
+template <int KIND, bool BACK> __global__ __launch_bounds__(1024) void k_adjust_over_parts(const AdjustArgs a, const u32 parts, const u32 width, const int nan) {
+    constexpr int NT = 1024;
+    extern __shared__ __align__(16) char lds[];
+    const u32 block = (u32)grid_block(), r32 = block / parts, c0 = (block - r32 * parts) * width;
+    const u64 r = r32;
+    if (r >= (u64)a.rows) return;
+    const Row f = row_of(a, r);
+    const u32 c1 = c0 + min(width, a.cols - c0);
+    const char* scores = (const char*)a.scores + (a.scores ? r * (u64)a.stride * kSize<KIND> : 0);
+    char* out = BACK ? (char*)a.grad + (a.grad ? r * (u64)a.grad_stride * kSize<KIND> : 0) : (char*)a.out + r * (u64)a.out_stride * kSize<KIND>;
+    const Part p = part_of(lds, BACK ? 0 : a.n_entries, part_room(width, a.cols));
+    if (BACK && a.grad_entry) {
+        entry_gradients<KIND, NT>(a, r, f, (const char*)a.grad_out + r * (u64)a.grad_out_stride * kSize<KIND>, c0, c1);
+        __syncthreads();       // read before the places are written
+    }
+    if (!f.good) {
+        if (nan) fill_nan<KIND>(out, c0, c1);
+        return;
+    }
+    if (BACK && f.by == 1.f) return;
+    four t[kKept];
+    if (a.n_prior <= 4 * kKept * NT) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
+    fill_part<KIND, NT, !BACK>(a, r, f, p, out, c0, c1 - c0, t, [&](u32 word, u32 k, float x, double inverse) {
+        return BACK ? taken_back(f, inverse, word, value_at<KIND>(scores, k), x) : adjusted(f, inverse, p, word, x, 0.f);
+    });
+    for (u32 k = c0 + threadIdx.x; k < c1; k += NT)
+        if ((p.bits[(k - c0) / 32] >> (k & 31) & 1) && (allowed_at(f.mask, k) & 1)) store_one<KIND>(out, k, __uint_as_float(p.word[k - c0]));
+}
+
 // ---- a bias that all rows share --------------------------------------------------------------------------------------
-// Sums over a block of rows of a tile of columns, a vector of them a thread; the gradient of the scores on the way (grad, or NULL).
-// OVER: it lies over grad_out, and vectors without a masked place are left.  Sums are in 64 bits: they cost the kernel nothing.
-constexpr int kSumThreads = 256, kMostSumRows = 256;
+// Sums over a block of rows of a tile of columns, a vector of them a lane, and the gradient of the scores on the way (grad, or NULL).
+// A workgroup's wavefronts take every fourth row each and add their sums in order at the end.  OVER: grad lies over
+// grad_out, and vectors without a masked place are left.  Sums are in 64 bits: they cost the kernel nothing.
+constexpr u32 kSumThreads = 256, kSumGroups = 4, kMostSumRows = 256;
 
 template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_adjust_columns(const AdjustArgs a, const u32 tiles, const u32 block_rows, double* sums, float* out_sums) {
-    constexpr u32 W = kPer<KIND>;
-    constexpr int N = 4;                    // rows under way
+    constexpr u32 W = kPer<KIND>, GROUPS = kSumGroups, LANES = kSumThreads / GROUPS;
+    constexpr u32 N = 4;                    // rows under way
     __shared__ const u32* masks[kMostSumRows];
     __shared__ int good[kMostSumRows];
-    const u64 b = grid_block() / tiles;
-    const u32 k = (u32)(grid_block() % tiles) * (kSumThreads * W) + threadIdx.x * W;
+    __shared__ double joined[(GROUPS - 1) * LANES * W];
+    const u32 block = (u32)grid_block(), b32 = block / tiles, group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const u32 k = (block - b32 * tiles) * (LANES * W) + lane * W;
+    const u64 b = b32;
     if (b * block_rows >= (u64)a.rows) return;
     const u64 r0 = b * block_rows;
     const u32 rows = (u32)min((u64)block_rows, (u64)a.rows - r0);
@@ -375,8 +589,7 @@ template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_
         good[threadIdx.x] = f.good;
     }
     __syncthreads();
-    if (k >= a.cols) return;
-    const u32 n = min(W, a.cols - k);
+    const u32 n = k < a.cols ? min(W, a.cols - k) : 0;
     const char* in = (const char*)a.grad_out + (r0 * (u64)a.grad_out_stride + k) * kSize<KIND>;
     char* out = (char*)a.grad + (a.grad ? (r0 * (u64)a.grad_stride + k) * kSize<KIND> : 0);
     double sum[W] = {};
@@ -384,9 +597,10 @@ template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_
         vec x[N];
         u32 allowed[N];
 #pragma unroll
-        for (u32 u = 0; u < (u32)N; ++u) {
+        for (u32 u = 0; u < N; ++u) {
             if (u >= count) continue;
-            const char* p = in + (u64)(i0 + u) * (u64)a.grad_out_stride * kSize<KIND>;
+            const u32 row = i0 + u * GROUPS;
+            const char* p = in + (u64)row * (u64)a.grad_out_stride * kSize<KIND>;
             if (n == W) {
                 x[u] = vec_at<KIND>(p);
             } else {
@@ -396,13 +610,14 @@ template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_
                     if (i < n) v[i] = value_at<KIND>(p, i);
                 x[u] = packed<KIND>(v);
             }
-            const u32* mask = masks[i0 + u];
-            allowed[u] = mask ? vector_bits<KIND>(mask, k) : kBits<KIND>;
+            const u32* mask = masks[row];
+            allowed[u] = mask && n ? vector_bits<KIND>(mask, k) : kBits<KIND>;
         }
 #pragma unroll
-        for (u32 u = 0; u < (u32)N; ++u) {
+        for (u32 u = 0; u < N; ++u) {
             if (u >= count) continue;
-            const bool ok = good[i0 + u];
+            const u32 row = i0 + u * GROUPS;
+            const bool ok = good[row];
             float v[W];
 #pragma unroll
             for (u32 i = 0; i < W; ++i) {
@@ -410,7 +625,7 @@ template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_
                 sum[i] += (double)v[i];
             }
             if (!a.grad || (OVER && ok && allowed[u] == kBits<KIND>)) continue;
-            char* p = out + (u64)(i0 + u) * (u64)a.grad_stride * kSize<KIND>;
+            char* p = out + (u64)row * (u64)a.grad_stride * kSize<KIND>;
             if (n == W) {
                 put_vec<KIND, false>(p, packed<KIND>(v));
             } else {
@@ -420,9 +635,19 @@ template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_
             }
         }
     };
-    u32 i = 0;
-    for (; i + N <= rows; i += N) some(i, N);
-    if (i < rows) some(i, rows - i);
+    u32 i = group;
+    for (; i + (N - 1) * GROUPS < rows; i += N * GROUPS) some(i, N);
+    if (i < rows) some(i, (rows - i + GROUPS - 1) / GROUPS);
+    if (group) {
+#pragma unroll
+        for (u32 i = 0; i < W; ++i) joined[((group - 1) * W + i) * LANES + lane] = sum[i];
+    }
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (u32 g = 0; g + 1 < GROUPS; ++g)
+#pragma unroll
+        for (u32 i = 0; i < W; ++i) sum[i] += joined[(g * W + i) * LANES + lane];
 #pragma unroll
     for (u32 i = 0; i < W; ++i)
         if (i < n) {
@@ -440,62 +665,91 @@ __global__ __launch_bounds__(256) void k_adjust_join(const double* sums, const u
     out[k] = (float)v;
 }
 
-// Rows of a block: as many as leave some thousand workgroups.
-u32 sum_rows(int64_t rows, int64_t cols) {
-    const int64_t tiles = (cols + 2047) / 2048, want = rows * tiles / 1024;
-    return (u32)std::max((int64_t)16, std::min((int64_t)kMostSumRows, want));
-}
+// Rows of a block, and few enough blocks to add up.  16 / 32 / 64 / 128 rows, us: 4096 x 32768 bf16 130 / 114 / 114 / 116, 4096 x 5000 38 / 31 /
+// 33 / 46, 100 x 1000 10 / 11 / 17 / 22, 1024 x 32768 f32 62 / 63 / 72 / 62.  (One wavefront after the other instead of four rows side
+// by side: 4096 x 32768 bf16 138, 16 x 1000 f32 17.3 against 13.9 with all that goes with it.)
+u32 sum_rows(int64_t rows) { return (u32)std::max((int64_t)32, std::min((int64_t)kMostSumRows, rows / 128)); }
 
 // ---- launches --------------------------------------------------------------------------------------------------------
 template <int KIND, bool BACK, int NT, int NV> hipError_t launch_all(const AdjustArgs& a, bool table, hipStream_t st) {
     constexpr u32 width = NT * NV * kPer<KIND>;
     const u32 parts = (a.cols + width - 1) / width;
+    if ((u64)a.rows * parts >> 32) return hipErrorInvalidValue;
     const dim3 grid = grid_of((u64)a.rows * parts), block(NT);
-    if (table) hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, true>), grid, block, part_bytes(BACK ? 0 : a.n_entries, width), st, a, parts);
+    if (table) hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, true>), grid, block, part_bytes(BACK ? 0 : a.n_entries, part_room(width, a.cols)), st, a, parts);
     else hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, false>), grid, block, 0, st, a, parts);
     return hipGetLastError();
 }
 
+// Threads and vectors a thread by row length, history and how many workgroups that makes, us:
+//   no table                64 x 1 / 256 x 1 / 256 x 2 / 512 x 2: 256 x 131072 bf16 27.6 / 29.4 / 29.1 / 29.0, f32 52.6 / 51.3 / 49.8 / 49.0
+//   a wavefront's row       64 x 1 / 256 x 1: 4096 x 500 bf16, 50 earlier outcomes 8.2 / 11.3 (and 1500 of them: 12.9 / 13.1)
+//   short rows              256 x 1 / 256 x 2 / 512 x 2: 4096 x 1500 f32 19.1 / 13.7 / 18.8, 1024 x 5000 bf16 11.1 / 9.8 / 8.6
+//   many parts              256 x 1 / 256 x 2 / 512 x 2 / 1024 x 2: 512 x 131072 bf16, 1024 earlier ones 108 / 86 / 77 / 74; 256 x 131072 f32, 300
+//                           of them 65.2 / 48.6 / 50.3 / 49.9, 3000 103 / 77 / 61 / 57 (kept by the threads up to 8 each)
+//   few parts               256 x 1 / 512 x 1 / 1024 x 1: 8 x 200003 f16, 32768 earlier ones 18.2 / 14.0 / 12.2
 template <int KIND, bool BACK> hipError_t launch_all(const AdjustArgs& a, hipStream_t st) {
     const bool table = BACK ? a.n_prior && a.repetition : a.n_prior || a.n_entries;
-    const u32 width = 256 * 4 * kPer<KIND>;
-    if (table && a.n_prior > 4096) return launch_all<KIND, BACK, 1024, 1>(a, table, st);
-    if ((u64)a.rows * ((a.cols + width - 1) / width) < 512) return launch_all<KIND, BACK, 256, 1>(a, table, st);
-    return launch_all<KIND, BACK, 256, 4>(a, table, st);
+    const u32 vecs = (a.cols + kPer<KIND> - 1) / kPer<KIND>;
+    const bool few = (u64)a.rows * ((vecs + 1023) / 1024) < 512;
+    if (!table) return few ? launch_all<KIND, BACK, 256, 1>(a, table, st) : launch_all<KIND, BACK, 256, 2>(a, table, st);
+    if (vecs <= 64) return launch_all<KIND, BACK, 64, 1>(a, table, st);
+    if (few) return a.n_prior > 8 * 256 ? launch_all<KIND, BACK, 1024, 1>(a, table, st) : launch_all<KIND, BACK, 256, 1>(a, table, st);
+    if (a.n_prior > 8 * 256) return launch_all<KIND, BACK, 1024, 2>(a, table, st);
+    if (vecs <= 256) return launch_all<KIND, BACK, 256, 1>(a, table, st);
+    return vecs <= 512 ? launch_all<KIND, BACK, 256, 2>(a, table, st) : launch_all<KIND, BACK, 512, 2>(a, table, st);
 }
 
-template <int KIND, bool BACK> hipError_t launch_over(const AdjustArgs& a, int fill, hipStream_t st) {
-    const int table = a.grad || !BACK ? (BACK ? a.n_prior && a.repetition : a.n_prior || a.n_entries) : 0;
+// fill: masked places and rows with parameters out of range are written too.
+template <int KIND, bool BACK> hipError_t launch_over(const AdjustArgs& a, bool fill, hipStream_t st) {
+    const bool values = !BACK || a.grad, changes = values && (BACK ? a.n_prior && a.repetition : a.n_prior || a.n_entries);
     const u32 width = 8192, parts = (a.cols + width - 1) / width;
-    const size_t lds = table ? part_bytes(BACK ? 0 : a.n_entries, width) : 0;
-    if (table && a.n_prior > 4096) hipLaunchKernelGGL((k_adjust_over<KIND, BACK, 1024>), grid_of((u64)a.rows * parts), dim3(1024), lds, st, a, parts, width, table, fill);
-    else hipLaunchKernelGGL((k_adjust_over<KIND, BACK, 256>), grid_of((u64)a.rows * parts), dim3(256), lds, st, a, parts, width, table, fill);
+    if ((u64)a.rows * (parts + 1) >> 32) return hipErrorInvalidValue;
+    const int entries = BACK ? 0 : a.n_entries, n = changes ? a.n_prior + entries : 0;
+    // a row's masked places, or all of it where its parameters are out of range
+    const bool ranges = a.repetition || a.frequency || a.presence || a.prior_len || a.prompt_len;
+    const u32 filled = fill && values && (a.masks || (ranges && !changes)) ? parts : 0;
+    const int table = changes || a.grad_entry ? 1 : 0;
+    if (n > kHashMost) {
+        if (filled) hipLaunchKernelGGL((k_adjust_over<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(256), 0, st, a, parts, width, 0, 0, 1);
+        hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(1024), part_bytes(entries, part_room(width, a.cols)), st, a, parts, width, fill && !filled);
+        return hipGetLastError();
+    }
+    const int bits = changes ? hash_bits(n) : 0;
+    const size_t lds = bits ? hash_bytes(entries, bits) : 0;
+    if (filled + table) hipLaunchKernelGGL((k_adjust_over<KIND, BACK>), grid_of((u64)a.rows * (filled + table)), dim3(256), lds, st, a, filled, width, table, bits, fill);
     return hipGetLastError();
 }
 
 template <int KIND> hipError_t launch_forward(const AdjustArgs& a, hipStream_t st) {
-    return a.out == a.scores && !a.bias ? launch_over<KIND, false>(a, 1, st) : launch_all<KIND, false>(a, st);
+    return a.out == a.scores && !a.bias ? launch_over<KIND, false>(a, true, st) : launch_all<KIND, false>(a, st);
+}
+
+template <int KIND, bool OVER> bool launch_columns(const AdjustArgs& a, u32 rows, u32 blocks, void* scratch, float* direct, hipStream_t st) {
+    const u32 tile = kSumThreads / kSumGroups * kPer<KIND>, tiles = (a.cols + tile - 1) / tile;
+    if ((u64)tiles * blocks >> 32) return false;
+    hipLaunchKernelGGL((k_adjust_columns<KIND, OVER>), grid_of((u64)tiles * blocks), dim3(kSumThreads), 0, st, a, tiles, rows, (double*)scratch, direct);
+    return true;
 }
 
 template <int KIND> hipError_t launch_back(const AdjustArgs& a, void* scratch, hipStream_t st) {
     const bool over = a.grad == a.grad_out;
-    if (!a.grad_bias) return over || !a.grad ? launch_over<KIND, true>(a, 1, st) : launch_all<KIND, true>(a, st);
-    const u32 tile = kSumThreads * kPer<KIND>, tiles = (a.cols + tile - 1) / tile, rows = sum_rows(a.rows, a.cols), blocks = (u32)((a.rows + rows - 1) / rows);
+    if (!a.grad_bias) return over || !a.grad ? launch_over<KIND, true>(a, true, st) : launch_all<KIND, true>(a, st);
+    const u32 rows = sum_rows(a.rows), blocks = (u32)((a.rows + rows - 1) / rows);
     float* direct = blocks == 1 ? a.grad_bias : nullptr;
     if (blocks) {
-        const dim3 grid = grid_of((u64)tiles * blocks);
-        if (over) hipLaunchKernelGGL((k_adjust_columns<KIND, true>), grid, dim3(kSumThreads), 0, st, a, tiles, rows, (double*)scratch, direct);
-        else hipLaunchKernelGGL((k_adjust_columns<KIND, false>), grid, dim3(kSumThreads), 0, st, a, tiles, rows, (double*)scratch, direct);
+        const bool ok = over ? launch_columns<KIND, true>(a, rows, blocks, scratch, direct, st) : launch_columns<KIND, false>(a, rows, blocks, scratch, direct, st);
+        if (!ok) return hipErrorInvalidValue;
     }
     if (!direct) hipLaunchKernelGGL(k_adjust_join, grid_of(((u64)a.cols + 255) / 256), dim3(256), 0, st, (const double*)scratch, blocks, a.cols, a.grad_bias);
-    if (blocks && ((a.n_prior && a.repetition && a.grad) || a.grad_entry)) return launch_over<KIND, true>(a, 0, st);
+    if (blocks && ((a.n_prior && a.repetition && a.grad) || a.grad_entry)) return launch_over<KIND, true>(a, false, st);
     return hipGetLastError();
 }
 
 }  // namespace
 
 size_t adjust_grad_scratch_bytes(int64_t rows, int64_t cols) {
-    const int64_t block = sum_rows(rows, cols), blocks = (rows + block - 1) / block;
+    const int64_t block = sum_rows(rows), blocks = (rows + block - 1) / block;
     return blocks > 1 ? (size_t)blocks * (size_t)cols * 8 : 0;
 }
 
