@@ -33,13 +33,13 @@ struct Row {
 };
 
 // (Absent parameters are read from here: loads without branches between them wait for memory once.)
-__device__ const float kOff[2] = {0.f, 1.f};
+__device__ const float kOff[4] = {0.f, 1.f, 0.f, 0.f};
 __device__ const int kNone = 0;
+template <class T> __device__ __forceinline__ T row_value(const T* p, u64 r, const T* off) { return *(p ? (in_global<T>*)p + r : (in_global<T>*)off); }
 
 __device__ __forceinline__ Row row_of(const AdjustArgs& a, u64 r) {
-    const float by = *(a.repetition ? a.repetition + r : kOff + 1), each = *(a.frequency ? a.frequency + r : kOff), once = *(a.presence ? a.presence + r : kOff);
-    const int len = *(a.prior_len ? a.prior_len + r : &kNone), prompt = *(a.prompt_len ? a.prompt_len + r : &kNone);
-    const int at = *(a.mask_of ? a.mask_of + r : &kNone);
+    const float by = row_value(a.repetition, r, kOff + 1), each = row_value(a.frequency, r, kOff), once = row_value(a.presence, r, kOff);
+    const int len = row_value(a.prior_len, r, &kNone), prompt = row_value(a.prompt_len, r, &kNone), at = row_value(a.mask_of, r, &kNone);
     Row f;
     f.by = by;
     f.each = each;
@@ -182,6 +182,15 @@ template <int NT, class F> __device__ __forceinline__ void add_entries(const Par
     }
 }
 
+// A value as it lies in memory: turned into a float where it is used, so that nothing waits for it before.
+template <int KIND> __device__ __forceinline__ u32 raw_at(const char* row, u32 k) { return KIND == kScoreF32 ? ((const u32*)row)[k] : ((const unsigned short*)row)[k]; }
+template <int KIND> __device__ __forceinline__ float from_raw(u32 v) {
+    asm volatile("" : "+v"(v));       // here, and not where the load is
+    if (KIND == kScoreF32) return __uint_as_float(v);
+    if (KIND == kScoreF16) return __half2float(__ushort_as_half((unsigned short)v));
+    return __uint_as_float(v << 16);
+}
+
 __device__ __forceinline__ bool seen(u32 word) { return (word & (kPrompt | kCount)) != 0; }
 
 // A place whose column has a word.  inverse: 1 / R.
@@ -210,7 +219,7 @@ constexpr int kKept = 2;
 template <int KIND, int NT, bool ENTRIES, class G>
 __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row& f, const Part& p, const char* in, u32 c0, u32 n, four (&t)[kKept], G&& result) {
     const bool kept = a.n_prior <= 4 * kKept * NT, entries = ENTRIES && a.n_entries;
-    float z[kKept][4];
+    u32 z[kKept][4];
     for (u32 i = threadIdx.x; i < (n + 31) / 32; i += NT) p.bits[i] = 0;
     if (kept) {
         prior_cut<NT>(f.len, t);
@@ -220,7 +229,7 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
 #pragma unroll
             for (int w = 0; w < 4; ++w)
                 if ((u32)t[u][w] - c0 < n) {
-                    z[u][w] = value_at<KIND>(in, (u32)t[u][w]);
+                    z[u][w] = raw_at<KIND>(in, (u32)t[u][w]);
                     p.word[(u32)t[u][w] - c0] = 0;
                 }
         }
@@ -271,7 +280,7 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
                 for (int w = 0; w < 4; ++w)
                     if (mine >> (u * 4 + w) & 1) {
                         u32* to = p.word + ((u32)t[u][w] - c0);
-                        *to = __float_as_uint(result(*to, (u32)t[u][w], z[u][w], inverse));
+                        *to = __float_as_uint(result(*to, (u32)t[u][w], from_raw<KIND>(z[u][w]), inverse));
                     }
             }
             for (u32 left = mine_entries; left; left &= left - 1) {
@@ -282,19 +291,18 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
     } else {
         const double inverse = 1.0 / (double)f.by;
         for (u32 k0 = threadIdx.x; k0 < n; k0 += 4 * NT) {          // four values under way
-            float x[4];
-            u32 there = 0;
+            u32 x[4], there = 0;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const u32 k = k0 + u * NT;
                 if (k < n && (p.bits[k / 32] >> (k & 31) & 1)) {
                     there |= 1u << u;
-                    x[u] = value_at<KIND>(in, c0 + k);
+                    x[u] = raw_at<KIND>(in, c0 + k);
                 }
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (there >> u & 1) p.word[k0 + u * NT] = __float_as_uint(result(p.word[k0 + u * NT], c0 + k0 + u * NT, x[u], inverse));
+                if (there >> u & 1) p.word[k0 + u * NT] = __float_as_uint(result(p.word[k0 + u * NT], c0 + k0 + u * NT, from_raw<KIND>(x[u]), inverse));
         }
     }
     __syncthreads();
@@ -321,9 +329,28 @@ template <int KIND> __device__ __forceinline__ u32 vector_bits(const u32* bits, 
     return (((const unsigned char*)bits)[k / 8] >> (k & 7)) & kBits<KIND>;
 }
 
+template <int KIND> constexpr u32 kMasked = KIND == kScoreF32 ? 0xff800000u : KIND == kScoreBF16 ? 0xff80ff80u : 0xfc00fc00u;   // -inf
+
+// The values of x where their bit is set, those of y elsewhere, as they lie in memory.
+template <int KIND> __device__ __forceinline__ vec chosen(u32 bits, const vec& x, const vec& y) {
+    auto all = [&](int i) { return (u32)((int)(bits << (31 - i)) >> 31); };
+    vec r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u32 m = KIND == kScoreF32 ? all(i) : (all(2 * i) & 0xffffu) | (all(2 * i + 1) & 0xffff0000u);
+        r[i] = (x[i] & m) | (y[i] & ~m);
+    }
+    return r;
+}
+
+template <int KIND> __device__ __forceinline__ vec global_vec(const in_global<char>* p) {
+    if (KIND == kScoreF32) return *(const in_global<vec_at4>*)p;
+    return *(const in_global<vec_at2>*)p;
+}
+
 // Columns c0 .. c0 + NT NV W - 1 of row r, all of them written.  BACK: the gradient.  A thread's vectors of the row are under way
 // while the table is filled.
-template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_bounds__(NT) void k_adjust(const AdjustArgs a, const u32 parts) {
+template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_bounds__(NT, 8) void k_adjust(const AdjustArgs a, const u32 parts) {
     constexpr u32 W = kPer<KIND>, width = NT * NV * W;
     extern __shared__ __align__(16) char lds[];
     const u32 block = (u32)grid_block(), r32 = block / parts, c0 = (block - r32 * parts) * width;
@@ -338,10 +365,15 @@ template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_b
     four t[kKept];
     if (TABLE && a.n_prior <= 4 * kKept * NT) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
     vec x[NV];
+    // Threads without a vector take the row's last one, and a row without any something else: loads without branches between them, whose
+    // number is known, so that waiting for the ones before them is not waiting for them.
+    const bool tiny = a.cols < W;
+    const in_global<char>* in0 = tiny ? (const in_global<char>*)kOff : (const in_global<char>*)in;
+    u32 at[NV];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const u32 j = v * NT + threadIdx.x;
-        if (j < whole) x[v] = vec_at<KIND>(in + (u64)(c0 + j * W) * kSize<KIND>);
+    for (u32 v = 0; v < NV; ++v) {
+        at[v] = tiny ? 0 : min(c0 + (v * NT + threadIdx.x) * W, a.cols - W);
+        x[v] = global_vec<KIND>(in0 + at[v] * (u32)kSize<KIND>);
     }
     const Row f = row_of(a, r);
     if (BACK && a.grad_entry) entry_gradients<KIND, NT>(a, r, f, in, c0, c0 + n);
@@ -349,51 +381,46 @@ template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_b
         for (u32 k = c0 + threadIdx.x; k < c0 + n; k += NT) store_one<KIND>(out, k, __builtin_nanf(""));
         return;
     }
-    u32 allowed[NV];
+    unsigned char allowed[NV];       // of the vectors' bytes; (without a mask, something)
+    const in_global<unsigned char>* mask0 = f.mask ? (const in_global<unsigned char>*)f.mask : (const in_global<unsigned char>*)in0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const u32 j = v * NT + threadIdx.x;
-        allowed[v] = f.mask && j < whole ? vector_bits<KIND>(f.mask, c0 + j * W) : kBits<KIND>;
-    }
+    for (u32 v = 0; v < NV; ++v) allowed[v] = mask0[at[v] / 8];
     if (TABLE)
         fill_part<KIND, NT, !BACK>(a, r, f, p, in, c0, n, t, [&](u32 word, u32 k, float z, double inverse) {
             return BACK ? taken_back(f, inverse, word, value_at<KIND>(scores, k), z) : adjusted(f, inverse, p, word, z, a.bias ? a.bias[k] : 0.f);
         });
+    char* out0 = out + (u64)c0 * kSize<KIND>;
+    const char* bias0 = (const char*)a.bias + (u64)c0 * 4;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const u32 j = v * NT + threadIdx.x, k = c0 + j * W;
+    for (u32 v = 0; v < NV; ++v) {
+        const u32 j = v * NT + threadIdx.x;
         if (j >= whole) continue;
-        float y[W];
-        float b[W] = {};
+        vec y = x[v];
         if (!BACK && a.bias) {
+            float z[W];
 #pragma unroll
             for (u32 i = 0; i < W; i += 4) {
-                const vec q = *(const vec_at4*)(a.bias + k + i);
+                const vec q = *(const vec_at4*)(bias0 + (j * W + i) * 4u);
 #pragma unroll
-                for (u32 u = 0; u < 4; ++u) b[i + u] = __uint_as_float(q[u]);
+                for (u32 u = 0; u < 4; ++u) z[i + u] = part<KIND>(x[v], i + u) + __uint_as_float(q[u]);
             }
+            y = packed<KIND>(z);
         }
-#pragma unroll
-        for (u32 i = 0; i < W; ++i) y[i] = !BACK && a.bias ? part<KIND>(x[v], i) + b[i] : part<KIND>(x[v], i);
         if (TABLE) {
-            const u32 hit = vector_bits<KIND>(p.bits, k - c0);
+            const u32 hit = vector_bits<KIND>(p.bits, j * W);
             if (hit) {
-                u32 got[W];
+                float got[W];
 #pragma unroll
                 for (u32 i = 0; i < W; i += 4) {
-                    const four q = *(const four*)(p.word + (k - c0) + i);
+                    const four q = *(const four*)(p.word + j * W + i);
 #pragma unroll
-                    for (u32 u = 0; u < 4; ++u) got[i + u] = (u32)q[u];
+                    for (u32 u = 0; u < 4; ++u) got[i + u] = __uint_as_float((u32)q[u]);
                 }
-#pragma unroll
-                for (u32 i = 0; i < W; ++i)
-                    if (hit >> i & 1) y[i] = __uint_as_float(got[i]);
+                y = chosen<KIND>(hit, packed<KIND>(got), y);
             }
         }
-#pragma unroll
-        for (u32 i = 0; i < W; ++i)
-            if (!(allowed[v] >> i & 1)) y[i] = none;
-        put_vec<KIND, false>(out + (u64)k * kSize<KIND>, packed<KIND>(y));
+        if (f.mask) y = chosen<KIND>((u32)allowed[v] >> (j * W & 7), y, BACK ? vec{0, 0, 0, 0} : vec{kMasked<KIND>, kMasked<KIND>, kMasked<KIND>, kMasked<KIND>});
+        put_vec<KIND, false>(out0 + j * 16u, y);
     }
     const u32 k = c0 + whole * W + threadIdx.x;
     if (k < c0 + n) {
@@ -513,8 +540,7 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         if (u * 1024 >= f.len) continue;
-        u32 word[4];
-        float x[4];
+        u32 word[4], x[4];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             word[w] = place[u][w] != ~0u ? atomicExch(&h.word[place[u][w]], 0u) : 0;
@@ -522,10 +548,10 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
         }
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-            if (word[w]) x[w] = value_at<KIND>(out, (u32)t[u][w]);
+            if (word[w]) x[w] = raw_at<KIND>(out, (u32)t[u][w]);
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-            if (word[w]) change(word[w], (u32)t[u][w], x[w]);
+            if (word[w]) change(word[w], (u32)t[u][w], from_raw<KIND>(x[w]));
     }
     if (entries) {
         for (u32 j = threadIdx.x; j < *p.entries; j += 256) {
