@@ -478,9 +478,12 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
     const u32 block = (u32)grid_block(), r32 = block / (parts + table), at = block - r32 * (parts + table);
     const u64 r = r32;
     if (r >= (u64)a.rows) return;
+    const bool fills = at < parts;
+    four t[4];
+    if (!fills && bits) prior_load<256>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);      // with the row's parameters under way
     const Row f = row_of(a, r);
     char* out = BACK ? (char*)a.grad + (a.grad ? r * (u64)a.grad_stride * kSize<KIND> : 0) : (char*)a.out + r * (u64)a.out_stride * kSize<KIND>;
-    if (at < parts) {
+    if (fills) {
         const u32 c0 = at * width, c1 = c0 + min(width, a.cols - c0);
         if (!f.good) fill_nan<KIND>(out, c0, c1);
         else if (f.mask) fill_masked<KIND, 256>(f.mask, out, c0, c1, BACK ? 0.f : -kInf);
@@ -497,8 +500,7 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
         return;
     }
     if (!bits || (BACK && f.by == 1.f)) return;
-    four t[4];
-    prior_load<256>(a.prior + r * (u64)a.prior_stride, f.len, 0, t);
+    prior_cut<256>(f.len, t);
     const double inverse = 1.0 / (double)f.by;
     const int room = entry_room(BACK ? 0 : a.n_entries);
     Hash h;
@@ -534,29 +536,29 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
     if (entries) add_entries<256>(p, [&](u32 k, u32 j) { atomicOr(&h.word[h.place(k)], (j + 1) << kEntryBit); });
     __syncthreads();
     // whoever takes a column's word first writes its place
-    auto change = [&](u32 word, u32 k, float x) {
-        store_one<KIND>(out, k, BACK ? taken_back(f, inverse, word, value_at<KIND>(scores, k), x) : adjusted(f, inverse, p, word, x, 0.f));
+    auto change = [&](u32 word, u32 k, float x, float z) {
+        store_one<KIND>(out, k, BACK ? taken_back(f, inverse, word, z, x) : adjusted(f, inverse, p, word, x, 0.f));
     };
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         if (u * 1024 >= f.len) continue;
-        u32 word[4], x[4];
+        u32 word[4], x[4], z[4], mask[4];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             word[w] = place[u][w] != ~0u ? atomicExch(&h.word[place[u][w]], 0u) : 0;
-            if (word[w] && !(allowed_at(f.mask, (u32)t[u][w]) & 1)) word[w] = 0;
+            if (!word[w]) continue;
+            x[w] = raw_at<KIND>(out, (u32)t[u][w]);
+            if (BACK) z[w] = raw_at<KIND>(scores, (u32)t[u][w]);
+            mask[w] = f.mask ? f.mask[(u32)t[u][w] >> 5] : ~0u;
         }
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-            if (word[w]) x[w] = raw_at<KIND>(out, (u32)t[u][w]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            if (word[w]) change(word[w], (u32)t[u][w], from_raw<KIND>(x[w]));
+            if (word[w] && (mask[w] >> ((u32)t[u][w] & 31) & 1)) change(word[w], (u32)t[u][w], from_raw<KIND>(x[w]), BACK ? from_raw<KIND>(z[w]) : 0.f);
     }
     if (entries) {
         for (u32 j = threadIdx.x; j < *p.entries; j += 256) {
             const u32 k = (u32)p.column[j], word = atomicExch(&h.word[h.place(k)], 0u);
-            if (word && (allowed_at(f.mask, k) & 1)) change(word, k, value_at<KIND>(out, k));
+            if (word && (allowed_at(f.mask, k) & 1)) change(word, k, value_at<KIND>(out, k), 0.f);
         }
     }
 }
@@ -682,13 +684,18 @@ template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_
         }
 }
 
+// 64 columns a workgroup, every fourth block a wavefront.
 __global__ __launch_bounds__(256) void k_adjust_join(const double* sums, const u32 blocks, const u32 cols, float* out) {
-    const u64 k = grid_block() * 256 + threadIdx.x;
-    if (k >= cols) return;
+    __shared__ double part[256];
+    const u64 k = grid_block() * 64 + (threadIdx.x & 63);
     double v = 0.0;
+    if (k < cols) {
 #pragma unroll 8
-    for (u32 b = 0; b < blocks; ++b) v += sums[(u64)b * cols + k];
-    out[k] = (float)v;
+        for (u32 b = threadIdx.x >> 6; b < blocks; b += 4) v += sums[(u64)b * cols + k];
+    }
+    part[threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.x < 64 && k < cols) out[k] = (float)(((part[threadIdx.x] + part[threadIdx.x + 64]) + part[threadIdx.x + 128]) + part[threadIdx.x + 192]);
 }
 
 // Rows of a block, and few enough blocks to add up.  16 / 32 / 64 / 128 rows, us: 4096 x 32768 bf16 130 / 114 / 114 / 116, 4096 x 5000 38 / 31 /
@@ -767,7 +774,7 @@ template <int KIND> hipError_t launch_back(const AdjustArgs& a, void* scratch, h
         const bool ok = over ? launch_columns<KIND, true>(a, rows, blocks, scratch, direct, st) : launch_columns<KIND, false>(a, rows, blocks, scratch, direct, st);
         if (!ok) return hipErrorInvalidValue;
     }
-    if (!direct) hipLaunchKernelGGL(k_adjust_join, grid_of(((u64)a.cols + 255) / 256), dim3(256), 0, st, (const double*)scratch, blocks, a.cols, a.grad_bias);
+    if (!direct) hipLaunchKernelGGL(k_adjust_join, grid_of(((u64)a.cols + 63) / 64), dim3(256), 0, st, (const double*)scratch, blocks, a.cols, a.grad_bias);
     if (blocks && ((a.n_prior && a.repetition && a.grad) || a.grad_entry)) return launch_over<KIND, true>(a, false, st);
     return hipGetLastError();
 }
