@@ -308,13 +308,10 @@ def _each(t, dtype, dev, shape, what):
     _need(False, "%s must be a contiguous tensor of %s %s on cuda:%d" % (what, str(dtype)[6:], list(shape), dev))
 
 
-def _scores(t, kind, dev, what):
-    _need(kind in _SCORES, "unknown kind of scores")
-    _need(t is not None, what + " must be given")
-    return _grid(t, _dtype(_TYPE_OF[kind]), dev, what)
-
-
-_SCORES = (QSV_S_F32, QSV_S_F16, QSV_S_BF16)
+def _score_type(kind):
+    if kind not in (QSV_S_F32, QSV_S_F16, QSV_S_BF16):
+        _need(False, "kind must be one of the three types of scores")
+    return _dtype(_TYPE_OF[kind])
 
 
 def _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of):
@@ -322,16 +319,19 @@ def _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency,
     i32, f32, each = _dtype("int32"), _dtype("float32"), (rows,)
     if prior is not None:
         r.prior_dev, n, r.n_prior, r.prior_stride = _grid(prior, i32, d, "prior")
-        _need(n == rows, "prior must have the scores' rows")
+        if n != rows:
+            _need(False, "prior must have the scores' rows")
     if entry_idx is not None:
-        _need(entry_idx.dim() == 2, "entry_idx must be [rows][n_entries]")
-        r.n_entries = entry_idx.shape[1]
-        r.entry_idx_dev = _flat(entry_idx, "int32", d, "entry_idx", rows, r.n_entries)
+        if entry_idx.dim() != 2:
+            _need(False, "entry_idx must be [rows][n_entries]")
+        r.n_entries = n = entry_idx.shape[1]
+        r.entry_idx_dev = _each(entry_idx, i32, d, (rows, n), "entry_idx")
     if masks is not None:
         r.masks_dev, r.n_masks, words, r.mask_stride = _grid(masks, i32, d, "masks")
-        _need(words >= (r.cols + 31) // 32, "masks must have a bit for each outcome")
-    else:
-        _need(mask_of is None, "mask_of without masks")
+        if words < (r.cols + 31) // 32:
+            _need(False, "masks must have a bit for each outcome")
+    elif mask_of is not None:
+        _need(False, "mask_of without masks")
     if prior_len is not None:
         r.prior_len_dev = _each(prior_len, i32, d, each, "prior_len")
     if prompt_len is not None:
@@ -531,39 +531,46 @@ class Context:
     def qsv_adjust(self, kind, scores, out=None, prior=None, prior_len=None, prompt_len=None, repetition=None, frequency=None,
                    presence=None, bias=None, entry_idx=None, entry_bias=None, masks=None, mask_of=None):
         """out None: over the scores."""
-        r, d = qsv_adjust_req(), self.dev.index
+        r, d, dtype = qsv_adjust_req(), self.dev.index, _score_type(kind)
         r.kind = kind
-        r.scores_dev, rows, cols, r.row_stride = at = _scores(scores, kind, d, "scores")
-        r.rows, r.cols = rows, cols
-        r.out_dev, n, m, r.out_stride = at if out is None else _scores(out, kind, d, "out")
-        _need(n == rows and m == cols, "out must have the shape of the scores")
+        _need(scores is not None, "scores must be given")
+        at, rows, cols, stride = _grid(scores, dtype, d, "scores")
+        r.scores_dev, r.rows, r.cols, r.row_stride = at, rows, cols, stride
+        if out is not None:
+            at, n, m, stride = _grid(out, dtype, d, "out")
+            if n != rows or m != cols:
+                _need(False, "out must have the shape of the scores")
+        r.out_dev, r.out_stride = at, stride
         _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
         if bias is not None:
-            r.bias_dev = _flat(bias, "float32", d, "bias", cols)
-        if entry_idx is not None or entry_bias is not None:
-            _need(entry_idx is not None and entry_bias is not None, "entry_idx and entry_bias go together")
-            r.entry_bias_dev = _flat(entry_bias, "float32", d, "entry_bias", rows, r.n_entries)
+            r.bias_dev = _each(bias, _dtype("float32"), d, (cols,), "bias")
+        if entry_bias is not None and entry_idx is not None:
+            r.entry_bias_dev = _each(entry_bias, _dtype("float32"), d, (rows, r.n_entries), "entry_bias")
+        elif entry_bias is not None or entry_idx is not None:
+            _need(False, "entry_idx and entry_bias go together")
         self._check(self.L.qsv_adjust(self.h, ctypes.byref(r)))
 
     def qsv_adjust_grad(self, kind, grad_out, grad=None, scores=None, grad_bias=None, grad_entry=None, prior=None, prior_len=None,
                         prompt_len=None, repetition=None, frequency=None, presence=None, entry_idx=None, masks=None, mask_of=None):
         """grad may be grad_out; None: the gradients of the biases alone."""
-        r, b, d = qsv_adjust_req(), qsv_adjust_grad_req(), self.dev.index
+        r, b, d, dtype = qsv_adjust_req(), qsv_adjust_grad_req(), self.dev.index, _score_type(kind)
         r.kind = kind
-        b.grad_out_dev, rows, cols, b.grad_out_stride = _scores(grad_out, kind, d, "grad_out")
+        _need(grad_out is not None, "grad_out must be given")
+        b.grad_out_dev, rows, cols, b.grad_out_stride = _grid(grad_out, dtype, d, "grad_out")
         r.rows, r.cols = rows, cols
-        n, m = rows, cols
         if scores is not None:
-            r.scores_dev, n, m, r.row_stride = _scores(scores, kind, d, "scores")
-        _need(n == rows and m == cols, "scores must have the shape of grad_out")
+            r.scores_dev, n, m, r.row_stride = _grid(scores, dtype, d, "scores")
+            if n != rows or m != cols:
+                _need(False, "scores must have the shape of grad_out")
         if grad is not None:
-            b.grad_dev, n, m, b.grad_stride = _scores(grad, kind, d, "grad")
-        _need(n == rows and m == cols, "grad must have the shape of grad_out")
+            b.grad_dev, n, m, b.grad_stride = _grid(grad, dtype, d, "grad")
+            if n != rows or m != cols:
+                _need(False, "grad must have the shape of grad_out")
         _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency, presence, entry_idx, masks, mask_of)
         if grad_bias is not None:
-            b.grad_bias_dev = _flat(grad_bias, "float32", d, "grad_bias", cols)
+            b.grad_bias_dev = _each(grad_bias, _dtype("float32"), d, (cols,), "grad_bias")
         if grad_entry is not None:
-            b.grad_entry_dev = _flat(grad_entry, "float32", d, "grad_entry", rows, r.n_entries)
+            b.grad_entry_dev = _each(grad_entry, _dtype("float32"), d, (rows, r.n_entries), "grad_entry")
         self._check(self.L.qsv_adjust_grad(self.h, ctypes.byref(r), ctypes.byref(b)))
 
     def _list(self, tensors, cls):

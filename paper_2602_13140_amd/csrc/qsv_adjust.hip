@@ -450,6 +450,27 @@ template <int KIND> __device__ __forceinline__ void fill_nan(char* out, u32 c0, 
     for (u32 k = c0 + threadIdx.x; k < c1; k += blockDim.x) store_one<KIND>(out, k, __builtin_nanf(""));
 }
 
+// Sums of blocks of rows (see k_adjust_columns) added up, 64 columns a workgroup, every fourth block a wavefront.
+struct Join {
+    const double* sums;      // [blocks][cols]
+    u32 blocks, cols;
+    float* out;
+};
+__device__ __forceinline__ void join(const Join& j, u64 at) {
+    __shared__ double part[256];
+    const u64 k = at * 64 + (threadIdx.x & 63);
+    double v = 0.0;
+    if (k < j.cols) {
+#pragma unroll 8
+        for (u32 b = threadIdx.x >> 6; b < j.blocks; b += 4) v += j.sums[(u64)b * j.cols + k];
+    }
+    part[threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.x < 64 && k < j.cols) j.out[k] = (float)(((part[threadIdx.x] + part[threadIdx.x + 64]) + part[threadIdx.x + 128]) + part[threadIdx.x + 192]);
+}
+__global__ __launch_bounds__(256) void k_adjust_join(const Join j) { join(j, grid_block()); }
+inline u32 join_groups(const Join& j) { return j.out ? (j.cols + 63) / 64 : 0; }
+
 // A row's earlier outcomes by their columns where they are few: a table of twice as many places and more, found by a product's upper
 // bits and the next free place.
 struct Hash {
@@ -472,12 +493,16 @@ inline int hash_bits(int n) {
 inline size_t hash_bytes(int n_entries, int bits) { return (size_t)entry_room(n_entries) * 16 + ((size_t)8 << bits) + 16; }
 
 // A workgroup a row for its history and entries (`table`), and `parts` of `width` columns each for its masked places.  bits: log2 of the
-// table's places, 0: nothing but the entries' gradients.  nan: rows with parameters out of range are written.
-template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_over(const AdjustArgs a, const u32 parts, const u32 width, const int table, const int bits, const int nan) {
+// table's places, 0: nothing but the entries' gradients.  nan: rows with parameters out of range are written.  Workgroups behind the
+// rows' add up sums of a shared bias, which are in nobody's way (513 x 50021 f16: a launch less, 49 -> 44 us).
+template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_over(const AdjustArgs a, const u32 parts, const u32 width, const int table, const int bits, const int nan, const Join sums) {
     extern __shared__ __align__(16) char lds[];
     const u32 block = (u32)grid_block(), r32 = block / (parts + table), at = block - r32 * (parts + table);
     const u64 r = r32;
-    if (r >= (u64)a.rows) return;
+    if (r >= (u64)a.rows) {
+        if (sums.out) join(sums, block - (u32)a.rows * (parts + table));
+        return;
+    }
     const bool fills = at < parts;
     four t[4];
     if (!fills && bits) prior_load<256>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);      // with the row's parameters under way
@@ -684,32 +709,25 @@ template <int KIND, bool OVER> __global__ __launch_bounds__(kSumThreads) void k_
         }
 }
 
-// 64 columns a workgroup, every fourth block a wavefront.
-__global__ __launch_bounds__(256) void k_adjust_join(const double* sums, const u32 blocks, const u32 cols, float* out) {
-    __shared__ double part[256];
-    const u64 k = grid_block() * 64 + (threadIdx.x & 63);
-    double v = 0.0;
-    if (k < cols) {
-#pragma unroll 8
-        for (u32 b = threadIdx.x >> 6; b < blocks; b += 4) v += sums[(u64)b * cols + k];
-    }
-    part[threadIdx.x] = v;
-    __syncthreads();
-    if (threadIdx.x < 64 && k < cols) out[k] = (float)(((part[threadIdx.x] + part[threadIdx.x + 64]) + part[threadIdx.x + 128]) + part[threadIdx.x + 192]);
-}
-
 // Rows of a block, and few enough blocks to add up.  16 / 32 / 64 / 128 rows, us: 4096 x 32768 bf16 130 / 114 / 114 / 116, 4096 x 5000 38 / 31 /
 // 33 / 46, 100 x 1000 10 / 11 / 17 / 22, 1024 x 32768 f32 62 / 63 / 72 / 62.  (One wavefront after the other instead of four rows side
 // by side: 4096 x 32768 bf16 138, 16 x 1000 f32 17.3 against 13.9 with all that goes with it.)
 u32 sum_rows(int64_t rows) { return (u32)std::max((int64_t)32, std::min((int64_t)kMostSumRows, rows / 128)); }
 
 // ---- launches --------------------------------------------------------------------------------------------------------
+// A kernel is asked for before it takes more than 64 KiB of LDS.
+hipError_t room_for(const void* kernel, size_t lds) {
+    return lds > 65536 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) : hipSuccess;
+}
+
 template <int KIND, bool BACK, int NT, int NV> hipError_t launch_all(const AdjustArgs& a, bool table, hipStream_t st) {
     constexpr u32 width = NT * NV * kPer<KIND>;
     const u32 parts = (a.cols + width - 1) / width;
     if ((u64)a.rows * parts >> 32) return hipErrorInvalidValue;
     const dim3 grid = grid_of((u64)a.rows * parts), block(NT);
-    if (table) hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, true>), grid, block, part_bytes(BACK ? 0 : a.n_entries, part_room(width, a.cols)), st, a, parts);
+    const size_t lds = part_bytes(BACK ? 0 : a.n_entries, part_room(width, a.cols));
+    if (const hipError_t e = room_for((const void*)&k_adjust<KIND, BACK, NT, NV, true>, table ? lds : 0)) return e;
+    if (table) hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, true>), grid, block, lds, st, a, parts);
     else hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, false>), grid, block, 0, st, a, parts);
     return hipGetLastError();
 }
@@ -734,23 +752,24 @@ template <int KIND, bool BACK> hipError_t launch_all(const AdjustArgs& a, hipStr
 }
 
 // fill: masked places and rows with parameters out of range are written too.
-template <int KIND, bool BACK> hipError_t launch_over(const AdjustArgs& a, bool fill, hipStream_t st) {
+template <int KIND, bool BACK> hipError_t launch_over(const AdjustArgs& a, bool fill, hipStream_t st, const Join& sums = Join{nullptr, 0, 0, nullptr}) {
     const bool values = !BACK || a.grad, changes = values && (BACK ? a.n_prior && a.repetition : a.n_prior || a.n_entries);
     const u32 width = 8192, parts = (a.cols + width - 1) / width;
-    if ((u64)a.rows * (parts + 1) >> 32) return hipErrorInvalidValue;
+    if (((u64)a.rows * (parts + 1) + join_groups(sums)) >> 32) return hipErrorInvalidValue;
     const int entries = BACK ? 0 : a.n_entries, n = changes ? a.n_prior + entries : 0;
     // a row's masked places, or all of it where its parameters are out of range
     const bool ranges = a.repetition || a.frequency || a.presence || a.prior_len || a.prompt_len;
     const u32 filled = fill && values && (a.masks || (ranges && !changes)) ? parts : 0;
-    const int table = changes || a.grad_entry ? 1 : 0;
-    if (n > kHashMost) {
-        if (filled) hipLaunchKernelGGL((k_adjust_over<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(256), 0, st, a, parts, width, 0, 0, 1);
-        hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(1024), part_bytes(entries, part_room(width, a.cols)), st, a, parts, width, fill && !filled);
-        return hipGetLastError();
-    }
-    const int bits = changes ? hash_bits(n) : 0;
+    const bool by_parts = n > kHashMost;
+    const int table = !by_parts && (changes || a.grad_entry) ? 1 : 0, bits = table && changes ? hash_bits(n) : 0;
     const size_t lds = bits ? hash_bytes(entries, bits) : 0;
-    if (filled + table) hipLaunchKernelGGL((k_adjust_over<KIND, BACK>), grid_of((u64)a.rows * (filled + table)), dim3(256), lds, st, a, filled, width, table, bits, fill);
+    if (const hipError_t e = room_for((const void*)&k_adjust_over<KIND, BACK>, lds)) return e;
+    if (filled + table)
+        hipLaunchKernelGGL((k_adjust_over<KIND, BACK>), grid_of((u64)a.rows * (filled + table) + join_groups(sums)), dim3(256), lds, st, a, filled, width, table, bits, fill, sums);
+    else if (sums.out)
+        hipLaunchKernelGGL(k_adjust_join, grid_of(join_groups(sums)), dim3(256), 0, st, sums);
+    if (by_parts)
+        hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(1024), part_bytes(entries, part_room(width, a.cols)), st, a, parts, width, fill && !filled);
     return hipGetLastError();
 }
 
@@ -774,8 +793,9 @@ template <int KIND> hipError_t launch_back(const AdjustArgs& a, void* scratch, h
         const bool ok = over ? launch_columns<KIND, true>(a, rows, blocks, scratch, direct, st) : launch_columns<KIND, false>(a, rows, blocks, scratch, direct, st);
         if (!ok) return hipErrorInvalidValue;
     }
-    if (!direct) hipLaunchKernelGGL(k_adjust_join, grid_of(((u64)a.cols + 63) / 64), dim3(256), 0, st, (const double*)scratch, blocks, a.cols, a.grad_bias);
-    if (blocks && ((a.n_prior && a.repetition && a.grad) || a.grad_entry)) return launch_over<KIND, true>(a, false, st);
+    const Join sums{(const double*)scratch, blocks, a.cols, direct ? nullptr : a.grad_bias};
+    if (blocks && ((a.n_prior && a.repetition && a.grad) || a.grad_entry)) return launch_over<KIND, true>(a, false, st, sums);
+    if (!direct) hipLaunchKernelGGL(k_adjust_join, grid_of(join_groups(sums)), dim3(256), 0, st, sums);
     return hipGetLastError();
 }
 

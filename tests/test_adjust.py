@@ -387,6 +387,25 @@ def test_rows_and_histories(ctx, src, rows, cols, prior):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,prior,entries", [
+    (700, 200, 30, 5),          # a wavefront's row
+    (700, 1500, 2048, 0), (600, 1900, 90, 9), (600, 3600, 700, 2), (520, 9100, 1000, 1023),     # short rows and longer ones, kept histories
+    (520, 6000, 2049, 3), (257, 33000, 9000, 1000),                                             # the largest parts, kept and not
+    (3, 20000, 2048, 1023), (3, 20000, 2049, 40), (3, 20000, 8193, 1023), (5, 70000, 4000, 96), (5, 70000, 4097, 0)])
+def test_every_way_through(ctx, src, rows, cols, prior, entries):
+    z, q = draw(src, rows, cols, rows + cols), settings(rows, cols, rows, prior, entries, 3, rows % 2 == 1)
+    G = draw(src, rows, cols, rows + 2, sigma=0.2)
+    check_forward(ctx, src, z, q, over=False)
+    check_forward(ctx, src, z, dict(q, bias=None), over=True)
+    if rows % 2:
+        check_forward(ctx, src, z, q, over=True)
+    check_backward(ctx, src, z, G, q, bias=False)
+    check_backward(ctx, src, z, G, q, over=True)
+    check_backward(ctx, src, z, G, q, over=True, bias=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("cols", [50, 9000])
 def test_values_at_the_ends_of_the_type(ctx, src, cols):
     """-inf, +inf, NaN and the lowest value, masked and not, in rows of history and without; biases that exclude."""
