@@ -214,12 +214,13 @@ __device__ __forceinline__ float taken_back(const Row& f, double inverse, u32 wo
 
 // The table of the part's n columns, a word turned into its place's result in 32 bits at once.  Histories that the threads keep (t, 8 NT)
 // fetch the values at their columns first, and the first that counts at a column works it out; only words of theirs start at 0.  Longer ones
-// have the bitmap looked through.  result(word, column, its value, 1 / R).
+// have the bitmap looked through.  result(word, column, its value, (BACK) its score,
+// 1 / R).
 constexpr int kKept = 2;
-template <int KIND, int NT, bool ENTRIES, class G>
-__device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row& f, const Part& p, const char* in, u32 c0, u32 n, four (&t)[kKept], G&& result) {
-    const bool kept = a.n_prior <= 4 * kKept * NT, entries = ENTRIES && a.n_entries;
-    u32 z[kKept][4];
+template <int KIND, int NT, bool BACK, class G>
+__device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row& f, const Part& p, const char* in, const char* scores, u32 c0, u32 n, four (&t)[kKept], G&& result) {
+    const bool kept = a.n_prior <= 4 * kKept * NT, entries = !BACK && a.n_entries;
+    u32 z[kKept][4], of[kKept][4];
     for (u32 i = threadIdx.x; i < (n + 31) / 32; i += NT) p.bits[i] = 0;
     if (kept) {
         prior_cut<NT>(f.len, t);
@@ -230,6 +231,7 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
             for (int w = 0; w < 4; ++w)
                 if ((u32)t[u][w] - c0 < n) {
                     z[u][w] = raw_at<KIND>(in, (u32)t[u][w]);
+                    if (BACK) of[u][w] = raw_at<KIND>(scores, (u32)t[u][w]);
                     p.word[(u32)t[u][w] - c0] = 0;
                 }
         }
@@ -280,29 +282,30 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
                 for (int w = 0; w < 4; ++w)
                     if (mine >> (u * 4 + w) & 1) {
                         u32* to = p.word + ((u32)t[u][w] - c0);
-                        *to = __float_as_uint(result(*to, (u32)t[u][w], from_raw<KIND>(z[u][w]), inverse));
+                        *to = __float_as_uint(result(*to, (u32)t[u][w], from_raw<KIND>(z[u][w]), BACK ? from_raw<KIND>(of[u][w]) : 0.f, inverse));
                     }
             }
             for (u32 left = mine_entries; left; left &= left - 1) {
                 const u32 k = (u32)p.column[__builtin_ctz(left) * NT + threadIdx.x];
-                p.word[k] = __float_as_uint(result(p.word[k], c0 + k, value_at<KIND>(in, c0 + k), inverse));
+                p.word[k] = __float_as_uint(result(p.word[k], c0 + k, value_at<KIND>(in, c0 + k), 0.f, inverse));
             }
         }
     } else {
         const double inverse = 1.0 / (double)f.by;
         for (u32 k0 = threadIdx.x; k0 < n; k0 += 4 * NT) {          // four values under way
-            u32 x[4], there = 0;
+            u32 x[4], of[4], there = 0;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const u32 k = k0 + u * NT;
                 if (k < n && (p.bits[k / 32] >> (k & 31) & 1)) {
                     there |= 1u << u;
                     x[u] = raw_at<KIND>(in, c0 + k);
+                    if (BACK) of[u] = raw_at<KIND>(scores, c0 + k);
                 }
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (there >> u & 1) p.word[k0 + u * NT] = __float_as_uint(result(p.word[k0 + u * NT], c0 + k0 + u * NT, from_raw<KIND>(x[u]), inverse));
+                if (there >> u & 1) p.word[k0 + u * NT] = __float_as_uint(result(p.word[k0 + u * NT], c0 + k0 + u * NT, from_raw<KIND>(x[u]), BACK ? from_raw<KIND>(of[u]) : 0.f, inverse));
         }
     }
     __syncthreads();
@@ -386,8 +389,8 @@ template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_b
 #pragma unroll
     for (u32 v = 0; v < NV; ++v) allowed[v] = mask0[at[v] / 8];
     if (TABLE)
-        fill_part<KIND, NT, !BACK>(a, r, f, p, in, c0, n, t, [&](u32 word, u32 k, float z, double inverse) {
-            return BACK ? taken_back(f, inverse, word, value_at<KIND>(scores, k), z) : adjusted(f, inverse, p, word, z, a.bias ? a.bias[k] : 0.f);
+        fill_part<KIND, NT, BACK>(a, r, f, p, in, scores, c0, n, t, [&](u32 word, u32 k, float z, float of, double inverse) {
+            return BACK ? taken_back(f, inverse, word, of, z) : adjusted(f, inverse, p, word, z, a.bias ? a.bias[k] : 0.f);
         });
     char* out0 = out + (u64)c0 * kSize<KIND>;
     const char* bias0 = (const char*)a.bias + (u64)c0 * 4;
@@ -456,17 +459,20 @@ struct Join {
     u32 blocks, cols;
     float* out;
 };
-__device__ __forceinline__ void join(const Join& j, u64 at) {
+__device__ __forceinline__ void join(const Join& j, u64 at) {      // by the first 256 threads
     __shared__ double part[256];
-    const u64 k = at * 64 + (threadIdx.x & 63);
-    double v = 0.0;
-    if (k < j.cols) {
+    const u32 t = threadIdx.x;
+    const u64 k = at * 64 + (t & 63);
+    if (t < 256) {
+        double v = 0.0;
+        if (k < j.cols) {
 #pragma unroll 8
-        for (u32 b = threadIdx.x >> 6; b < j.blocks; b += 4) v += j.sums[(u64)b * j.cols + k];
+            for (u32 b = t >> 6; b < j.blocks; b += 4) v += j.sums[(u64)b * j.cols + k];
+        }
+        part[t] = v;
     }
-    part[threadIdx.x] = v;
     __syncthreads();
-    if (threadIdx.x < 64 && k < j.cols) j.out[k] = (float)(((part[threadIdx.x] + part[threadIdx.x + 64]) + part[threadIdx.x + 128]) + part[threadIdx.x + 192]);
+    if (t < 64 && k < j.cols) j.out[k] = (float)(((part[t] + part[t + 64]) + part[t + 128]) + part[t + 192]);
 }
 __global__ __launch_bounds__(256) void k_adjust_join(const Join j) { join(j, grid_block()); }
 inline u32 join_groups(const Join& j) { return j.out ? (j.cols + 63) / 64 : 0; }
@@ -484,7 +490,7 @@ struct Hash {
         }
     }
 };
-constexpr int kHashMost = 4096;          // earlier outcomes and entries: 16 of them a thread are kept
+constexpr int kHashMost = 8192;          // earlier outcomes and entries: up to 16 of them a thread are kept
 inline int hash_bits(int n) {
     int bits = 8;
     while (1 << bits < 2 * n) ++bits;
@@ -495,7 +501,7 @@ inline size_t hash_bytes(int n_entries, int bits) { return (size_t)entry_room(n_
 // A workgroup a row for its history and entries (`table`), and `parts` of `width` columns each for its masked places.  bits: log2 of the
 // table's places, 0: nothing but the entries' gradients.  nan: rows with parameters out of range are written.  Workgroups behind the
 // rows' add up sums of a shared bias, which are in nobody's way (513 x 50021 f16: a launch less, 49 -> 44 us).
-template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_over(const AdjustArgs a, const u32 parts, const u32 width, const int table, const int bits, const int nan, const Join sums) {
+template <int KIND, bool BACK, int NT> __global__ __launch_bounds__(NT) void k_adjust_over(const AdjustArgs a, const u32 parts, const u32 width, const int table, const int bits, const int nan, const Join sums) {
     extern __shared__ __align__(16) char lds[];
     const u32 block = (u32)grid_block(), r32 = block / (parts + table), at = block - r32 * (parts + table);
     const u64 r = r32;
@@ -505,18 +511,18 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
     }
     const bool fills = at < parts;
     four t[4];
-    if (!fills && bits) prior_load<256>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);      // with the row's parameters under way
+    if (!fills && bits) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);      // with the row's parameters under way
     const Row f = row_of(a, r);
     char* out = BACK ? (char*)a.grad + (a.grad ? r * (u64)a.grad_stride * kSize<KIND> : 0) : (char*)a.out + r * (u64)a.out_stride * kSize<KIND>;
     if (fills) {
         const u32 c0 = at * width, c1 = c0 + min(width, a.cols - c0);
         if (!f.good) fill_nan<KIND>(out, c0, c1);
-        else if (f.mask) fill_masked<KIND, 256>(f.mask, out, c0, c1, BACK ? 0.f : -kInf);
+        else if (f.mask) fill_masked<KIND, NT>(f.mask, out, c0, c1, BACK ? 0.f : -kInf);
         return;
     }
     const char* scores = (const char*)a.scores + (a.scores ? r * (u64)a.stride * kSize<KIND> : 0);
     if (BACK && a.grad_entry) {
-        entry_gradients<KIND, 256>(a, r, f, (const char*)a.grad_out + r * (u64)a.grad_out_stride * kSize<KIND>, 0, a.cols);
+        entry_gradients<KIND, NT>(a, r, f, (const char*)a.grad_out + r * (u64)a.grad_out_stride * kSize<KIND>, 0, a.cols);
         __syncthreads();       // read before the places are written
     }
     if (BACK && !a.grad) return;
@@ -525,7 +531,7 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
         return;
     }
     if (!bits || (BACK && f.by == 1.f)) return;
-    prior_cut<256>(f.len, t);
+    prior_cut<NT>(f.len, t);
     const double inverse = 1.0 / (double)f.by;
     const int room = entry_room(BACK ? 0 : a.n_entries);
     Hash h;
@@ -537,7 +543,7 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
     p.column = (int*)(h.word + (1u << bits));
     p.bias = (float*)(p.column + room);
     p.entries = (u32*)(p.bias + room);
-    for (u32 i = threadIdx.x; i < (1u << bits) / 4; i += 256) {
+    for (u32 i = threadIdx.x; i < (1u << bits) / 4; i += NT) {
         ((four*)h.key)[i] = four{-1, -1, -1, -1};
         ((four*)h.word)[i] = four{0, 0, 0, 0};
     }
@@ -547,18 +553,18 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
     u32 place[4][4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-        if (u * 1024 >= f.len) continue;
+        if (u * 4 * NT >= f.len) continue;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             place[u][w] = ~0u;
             if ((u32)t[u][w] >= a.cols) continue;
             const u32 e = h.place((u32)t[u][w]);
-            if (u * 1024 + (int)threadIdx.x * 4 + w < f.prompt) atomicOr(&h.word[e], kPrompt);
+            if (u * 4 * NT + (int)threadIdx.x * 4 + w < f.prompt) atomicOr(&h.word[e], kPrompt);
             else atomicAdd(&h.word[e], 1u);
             place[u][w] = e;
         }
     }
-    if (entries) add_entries<256>(p, [&](u32 k, u32 j) { atomicOr(&h.word[h.place(k)], (j + 1) << kEntryBit); });
+    if (entries) add_entries<NT>(p, [&](u32 k, u32 j) { atomicOr(&h.word[h.place(k)], (j + 1) << kEntryBit); });
     __syncthreads();
     // whoever takes a column's word first writes its place
     auto change = [&](u32 word, u32 k, float x, float z) {
@@ -566,7 +572,7 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
     };
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-        if (u * 1024 >= f.len) continue;
+        if (u * 4 * NT >= f.len) continue;
         u32 word[4], x[4], z[4], mask[4];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -581,7 +587,7 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(256) void k_adjust_o
             if (word[w] && (mask[w] >> ((u32)t[u][w] & 31) & 1)) change(word[w], (u32)t[u][w], from_raw<KIND>(x[w]), BACK ? from_raw<KIND>(z[w]) : 0.f);
     }
     if (entries) {
-        for (u32 j = threadIdx.x; j < *p.entries; j += 256) {
+        for (u32 j = threadIdx.x; j < *p.entries; j += NT) {
             const u32 k = (u32)p.column[j], word = atomicExch(&h.word[h.place(k)], 0u);
             if (word && (allowed_at(f.mask, k) & 1)) change(word, k, value_at<KIND>(out, k), 0.f);
         }
@@ -611,8 +617,8 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(1024) void k_adjust_
     if (BACK && f.by == 1.f) return;
     four t[kKept];
     if (a.n_prior <= 4 * kKept * NT) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
-    fill_part<KIND, NT, !BACK>(a, r, f, p, out, c0, c1 - c0, t, [&](u32 word, u32 k, float x, double inverse) {
-        return BACK ? taken_back(f, inverse, word, value_at<KIND>(scores, k), x) : adjusted(f, inverse, p, word, x, 0.f);
+    fill_part<KIND, NT, BACK>(a, r, f, p, out, scores, c0, c1 - c0, t, [&](u32 word, u32, float x, float of, double inverse) {
+        return BACK ? taken_back(f, inverse, word, of, x) : adjusted(f, inverse, p, word, x, 0.f);
     });
     for (u32 k = c0 + threadIdx.x; k < c1; k += NT)
         if ((p.bits[(k - c0) / 32] >> (k & 31) & 1) && (allowed_at(f.mask, k) & 1)) store_one<KIND>(out, k, __uint_as_float(p.word[k - c0]));
@@ -751,25 +757,34 @@ template <int KIND, bool BACK> hipError_t launch_all(const AdjustArgs& a, hipStr
     return vecs <= 512 ? launch_all<KIND, BACK, 256, 2>(a, table, st) : launch_all<KIND, BACK, 512, 2>(a, table, st);
 }
 
+// In place, 131072 columns: 256 / 1024 threads a row, us: 256 rows, 1000 earlier outcomes 8.9 / 9.3, 2000 13.8 / 11.8, 4000 22.5 / 17.3.  By rows / by
+// parts: 1 row, 6000 9.5 / 7.9, 8000 10.6 / 7.9; 64 rows with masks, 8000 26 / 31.  Parts of 8192 / 16384 / 32768 columns: 256 rows, 20000
+// 82 / 66 / 82, 32 rows 14.4 / 15.7 / 21.9.
 // fill: masked places and rows with parameters out of range are written too.
+template <int KIND, bool BACK, int NT> hipError_t launch_over(const AdjustArgs& a, u32 filled, int table, int bits, bool fill, hipStream_t st, const Join& sums) {
+    const size_t lds = bits ? hash_bytes(BACK ? 0 : a.n_entries, bits) : 0;
+    if (const hipError_t e = room_for((const void*)&k_adjust_over<KIND, BACK, NT>, lds)) return e;
+    hipLaunchKernelGGL((k_adjust_over<KIND, BACK, NT>), grid_of((u64)a.rows * (filled + table) + join_groups(sums)), dim3(NT), lds, st, a, filled, NT * 32, table, bits, fill, sums);
+    return hipGetLastError();
+}
+
 template <int KIND, bool BACK> hipError_t launch_over(const AdjustArgs& a, bool fill, hipStream_t st, const Join& sums = Join{nullptr, 0, 0, nullptr}) {
     const bool values = !BACK || a.grad, changes = values && (BACK ? a.n_prior && a.repetition : a.n_prior || a.n_entries);
-    const u32 width = 8192, parts = (a.cols + width - 1) / width;
-    if (((u64)a.rows * (parts + 1) + join_groups(sums)) >> 32) return hipErrorInvalidValue;
     const int entries = BACK ? 0 : a.n_entries, n = changes ? a.n_prior + entries : 0;
+    const u64 eights = (u64)a.rows * ((a.cols + 8191) / 8192);
+    const bool by_parts = n > kHashMost || (n > 4096 && eights <= 256), wide = !by_parts && n > 1024;
+    const u32 width = wide ? 32768 : by_parts && eights > 512 ? 16384 : 8192, parts = (a.cols + width - 1) / width;
+    if (((u64)a.rows * (parts + 1) + join_groups(sums)) >> 32) return hipErrorInvalidValue;
     // a row's masked places, or all of it where its parameters are out of range
     const bool ranges = a.repetition || a.frequency || a.presence || a.prior_len || a.prompt_len;
     const u32 filled = fill && values && (a.masks || (ranges && !changes)) ? parts : 0;
-    const bool by_parts = n > kHashMost;
     const int table = !by_parts && (changes || a.grad_entry) ? 1 : 0, bits = table && changes ? hash_bits(n) : 0;
-    const size_t lds = bits ? hash_bytes(entries, bits) : 0;
-    if (const hipError_t e = room_for((const void*)&k_adjust_over<KIND, BACK>, lds)) return e;
-    if (filled + table)
-        hipLaunchKernelGGL((k_adjust_over<KIND, BACK>), grid_of((u64)a.rows * (filled + table) + join_groups(sums)), dim3(256), lds, st, a, filled, width, table, bits, fill, sums);
-    else if (sums.out)
-        hipLaunchKernelGGL(k_adjust_join, grid_of(join_groups(sums)), dim3(256), 0, st, sums);
-    if (by_parts)
-        hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(1024), part_bytes(entries, part_room(width, a.cols)), st, a, parts, width, fill && !filled);
+    hipError_t e = hipSuccess;
+    if (filled + table) e = wide ? launch_over<KIND, BACK, 1024>(a, filled, table, bits, fill, st, sums) : launch_over<KIND, BACK, 256>(a, filled, table, bits, fill, st, sums);
+    else if (sums.out) hipLaunchKernelGGL(k_adjust_join, grid_of(join_groups(sums)), dim3(256), 0, st, sums);
+    if (e != hipSuccess || !by_parts) return e != hipSuccess ? e : hipGetLastError();
+    if ((e = room_for((const void*)&k_adjust_over_parts<KIND, BACK>, part_bytes(entries, part_room(width, a.cols)))) != hipSuccess) return e;
+    hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(1024), part_bytes(entries, part_room(width, a.cols)), st, a, parts, width, fill && !filled);
     return hipGetLastError();
 }
 

@@ -390,7 +390,7 @@ def test_rows_and_histories(ctx, src, rows, cols, prior):
 @pytest.mark.parametrize("rows,cols,prior,entries", [
     (700, 200, 30, 5),          # a wavefront's row
     (700, 1500, 2048, 0), (600, 1900, 90, 9), (600, 3600, 700, 2), (520, 9100, 1000, 1023),     # short rows and longer ones, kept histories
-    (520, 6000, 2049, 3), (257, 33000, 9000, 1000),                                             # the largest parts, kept and not
+    (520, 6000, 2049, 3), (257, 33000, 9000, 1000), (300, 33000, 5000, 1023),                                             # the largest parts, kept and not
     (3, 20000, 2048, 1023), (3, 20000, 2049, 40), (3, 20000, 8193, 1023), (5, 70000, 4000, 96), (5, 70000, 4097, 0)])
 def test_every_way_through(ctx, src, rows, cols, prior, entries):
     z, q = draw(src, rows, cols, rows + cols), settings(rows, cols, rows, prior, entries, 3, rows % 2 == 1)
