@@ -773,16 +773,17 @@ template <int KIND, bool BACK> hipError_t launch_over(const AdjustArgs& a, bool 
     const int entries = BACK ? 0 : a.n_entries, n = changes ? a.n_prior + entries : 0;
     const u64 eights = (u64)a.rows * ((a.cols + 8191) / 8192);
     const bool by_parts = n > kHashMost || (n > 4096 && eights <= 256), wide = !by_parts && n > 1024;
-    const u32 width = wide ? 32768 : by_parts && eights > 512 ? 16384 : 8192, parts = (a.cols + width - 1) / width;
-    if (((u64)a.rows * (parts + 1) + join_groups(sums)) >> 32) return hipErrorInvalidValue;
+    if ((2 * eights + (u64)a.rows + join_groups(sums)) >> 32) return hipErrorInvalidValue;
     // a row's masked places, or all of it where its parameters are out of range
     const bool ranges = a.repetition || a.frequency || a.presence || a.prior_len || a.prompt_len;
-    const u32 filled = fill && values && (a.masks || (ranges && !changes)) ? parts : 0;
+    const u32 fill_width = wide ? 1024 * 32 : 256 * 32;
+    const u32 filled = fill && values && (a.masks || (ranges && !changes)) ? (a.cols + fill_width - 1) / fill_width : 0;
     const int table = !by_parts && (changes || a.grad_entry) ? 1 : 0, bits = table && changes ? hash_bits(n) : 0;
     hipError_t e = hipSuccess;
     if (filled + table) e = wide ? launch_over<KIND, BACK, 1024>(a, filled, table, bits, fill, st, sums) : launch_over<KIND, BACK, 256>(a, filled, table, bits, fill, st, sums);
     else if (sums.out) hipLaunchKernelGGL(k_adjust_join, grid_of(join_groups(sums)), dim3(256), 0, st, sums);
     if (e != hipSuccess || !by_parts) return e != hipSuccess ? e : hipGetLastError();
+    const u32 width = eights > 512 ? 16384 : 8192, parts = (a.cols + width - 1) / width;
     if ((e = room_for((const void*)&k_adjust_over_parts<KIND, BACK>, part_bytes(entries, part_room(width, a.cols)))) != hipSuccess) return e;
     hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(1024), part_bytes(entries, part_room(width, a.cols)), st, a, parts, width, fill && !filled);
     return hipGetLastError();
