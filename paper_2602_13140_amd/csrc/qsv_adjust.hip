@@ -138,10 +138,12 @@ template <bool ZERO> __device__ __forceinline__ void gather_entries(const Adjust
         float b[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int j = j0 + u * 64 + (int)lane;
-            k[u] = j < a.n_entries ? (u32)idx[j] - c0 : ~0u;
-            b[u] = j < a.n_entries ? bias[j] : 0.f;
+            const int j = min(j0 + u * 64 + (int)lane, a.n_entries - 1);      // (loads without branches between them)
+            k[u] = (u32)idx[j];
+            b[u] = bias[j];
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) k[u] = j0 + u * 64 + (int)lane < a.n_entries ? k[u] - c0 : ~0u;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const u64 in = __ballot(k[u] < n);
@@ -217,12 +219,13 @@ __device__ __forceinline__ float taken_back(const Row& f, double inverse, u32 wo
 // have the bitmap looked through.  result(word, column, its value, (BACK) its score,
 // 1 / R).
 constexpr int kKept = 2;
-template <int KIND, int NT, bool BACK, class G>
+constexpr int kTableNone = 0, kTableKept = 1, kTableLong = 2;
+template <int KIND, int NT, bool BACK, bool KEPT, class G>
 __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row& f, const Part& p, const char* in, const char* scores, u32 c0, u32 n, four (&t)[kKept], G&& result) {
-    const bool kept = a.n_prior <= 4 * kKept * NT, entries = !BACK && a.n_entries;
+    const bool entries = !BACK && a.n_entries;
     u32 z[kKept][4], of[kKept][4];
     for (u32 i = threadIdx.x; i < (n + 31) / 32; i += NT) p.bits[i] = 0;
-    if (kept) {
+    if (KEPT) {
         prior_cut<NT>(f.len, t);
 #pragma unroll
         for (int u = 0; u < kKept; ++u) {
@@ -241,7 +244,7 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
     if (entries && threadIdx.x < 64) gather_entries<true>(a, r, p, c0, n);
     __syncthreads();
     u32 mine = 0, mine_entries = 0;
-    if (kept) {
+    if (KEPT) {
 #pragma unroll
         for (int u = 0; u < kKept; ++u) {
             if (u * 4 * NT >= f.len) break;
@@ -253,11 +256,12 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
         }
     } else {
         const int* prior = a.prior + r * (u64)a.prior_stride;
-        for (int i0 = 0; i0 < f.len; i0 += 16 * NT) {
-            four q[4];
+        constexpr int N = 8;
+        for (int i0 = 0; i0 < f.len; i0 += 4 * N * NT) {
+            four q[N];
             prior_load<NT>(prior, f.len, i0, q);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < N; ++u)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const u32 k = (u32)q[u][w] - c0;
@@ -272,7 +276,7 @@ __device__ __forceinline__ void fill_part(const AdjustArgs& a, u64 r, const Row&
             mine_entries |= 1u << (j / NT);
         });
     __syncthreads();
-    if (kept) {
+    if (KEPT) {
         if (mine | mine_entries) {
             const double inverse = 1.0 / (double)f.by;
 #pragma unroll
@@ -353,7 +357,7 @@ template <int KIND> __device__ __forceinline__ vec global_vec(const in_global<ch
 
 // Columns c0 .. c0 + NT NV W - 1 of row r, all of them written.  BACK: the gradient.  A thread's vectors of the row are under way
 // while the table is filled.
-template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_bounds__(NT, 8) void k_adjust(const AdjustArgs a, const u32 parts) {
+template <int KIND, bool BACK, int NT, int NV, int TABLE> __global__ __launch_bounds__(NT, 8) void k_adjust(const AdjustArgs a, const u32 parts) {
     constexpr u32 W = kPer<KIND>, width = NT * NV * W;
     extern __shared__ __align__(16) char lds[];
     const u32 block = (u32)grid_block(), r32 = block / parts, c0 = (block - r32 * parts) * width;
@@ -366,7 +370,7 @@ template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_b
     const Part p = part_of(lds, BACK ? 0 : a.n_entries, part_room(width, a.cols));
     const float none = BACK ? 0.f : -kInf;
     four t[kKept];
-    if (TABLE && a.n_prior <= 4 * kKept * NT) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
+    if (TABLE == kTableKept) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
     vec x[NV];
     // Threads without a vector take the row's last one, and a row without any something else: loads without branches between them, whose
     // number is known, so that waiting for the ones before them is not waiting for them.
@@ -389,7 +393,7 @@ template <int KIND, bool BACK, int NT, int NV, bool TABLE> __global__ __launch_b
 #pragma unroll
     for (u32 v = 0; v < NV; ++v) allowed[v] = mask0[at[v] / 8];
     if (TABLE)
-        fill_part<KIND, NT, BACK>(a, r, f, p, in, scores, c0, n, t, [&](u32 word, u32 k, float z, float of, double inverse) {
+        fill_part<KIND, NT, BACK, TABLE == kTableKept>(a, r, f, p, in, scores, c0, n, t, [&](u32 word, u32 k, float z, float of, double inverse) {
             return BACK ? taken_back(f, inverse, word, of, z) : adjusted(f, inverse, p, word, z, a.bias ? a.bias[k] : 0.f);
         });
     char* out0 = out + (u64)c0 * kSize<KIND>;
@@ -595,7 +599,7 @@ template <int KIND, bool BACK, int NT> __global__ __launch_bounds__(NT) void k_a
 }
 
 // The same for long histories, by parts of a row with a table of their columns each.
-template <int KIND, bool BACK> __global__ __launch_bounds__(1024) void k_adjust_over_parts(const AdjustArgs a, const u32 parts, const u32 width, const int nan) {
+template <int KIND, bool BACK, bool KEPT> __global__ __launch_bounds__(1024) void k_adjust_over_parts(const AdjustArgs a, const u32 parts, const u32 width, const int nan) {
     constexpr int NT = 1024;
     extern __shared__ __align__(16) char lds[];
     const u32 block = (u32)grid_block(), r32 = block / parts, c0 = (block - r32 * parts) * width;
@@ -616,8 +620,8 @@ template <int KIND, bool BACK> __global__ __launch_bounds__(1024) void k_adjust_
     }
     if (BACK && f.by == 1.f) return;
     four t[kKept];
-    if (a.n_prior <= 4 * kKept * NT) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
-    fill_part<KIND, NT, BACK>(a, r, f, p, out, scores, c0, c1 - c0, t, [&](u32 word, u32, float x, float of, double inverse) {
+    if (KEPT) prior_load<NT>(a.prior + r * (u64)a.prior_stride, a.n_prior, 0, t);
+    fill_part<KIND, NT, BACK, KEPT>(a, r, f, p, out, scores, c0, c1 - c0, t, [&](u32 word, u32, float x, float of, double inverse) {
         return BACK ? taken_back(f, inverse, word, of, x) : adjusted(f, inverse, p, word, x, 0.f);
     });
     for (u32 k = c0 + threadIdx.x; k < c1; k += NT)
@@ -726,35 +730,36 @@ hipError_t room_for(const void* kernel, size_t lds) {
     return lds > 65536 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) : hipSuccess;
 }
 
-template <int KIND, bool BACK, int NT, int NV> hipError_t launch_all(const AdjustArgs& a, bool table, hipStream_t st) {
+template <int KIND, bool BACK, int NT, int NV, int TABLE> hipError_t launch_all(const AdjustArgs& a, hipStream_t st) {
     constexpr u32 width = NT * NV * kPer<KIND>;
     const u32 parts = (a.cols + width - 1) / width;
     if ((u64)a.rows * parts >> 32) return hipErrorInvalidValue;
-    const dim3 grid = grid_of((u64)a.rows * parts), block(NT);
-    const size_t lds = part_bytes(BACK ? 0 : a.n_entries, part_room(width, a.cols));
-    if (const hipError_t e = room_for((const void*)&k_adjust<KIND, BACK, NT, NV, true>, table ? lds : 0)) return e;
-    if (table) hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, true>), grid, block, lds, st, a, parts);
-    else hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, false>), grid, block, 0, st, a, parts);
+    const size_t lds = TABLE != kTableNone ? part_bytes(BACK ? 0 : a.n_entries, part_room(width, a.cols)) : 0;
+    if (const hipError_t e = room_for((const void*)&k_adjust<KIND, BACK, NT, NV, TABLE>, lds)) return e;
+    hipLaunchKernelGGL((k_adjust<KIND, BACK, NT, NV, TABLE>), grid_of((u64)a.rows * parts), dim3(NT), lds, st, a, parts);
     return hipGetLastError();
+}
+template <int KIND, bool BACK, int NT, int NV> hipError_t launch_table(const AdjustArgs& a, hipStream_t st) {
+    return a.n_prior <= 4 * kKept * NT ? launch_all<KIND, BACK, NT, NV, kTableKept>(a, st) : launch_all<KIND, BACK, NT, NV, kTableLong>(a, st);
 }
 
 // Threads and vectors a thread by row length, history and how many workgroups that makes, us:
-//   no table                64 x 1 / 256 x 1 / 256 x 2 / 512 x 2: 256 x 131072 bf16 27.6 / 29.4 / 29.1 / 29.0, f32 52.6 / 51.3 / 49.8 / 49.0
-//   a wavefront's row       64 x 1 / 256 x 1: 4096 x 500 bf16, 50 earlier outcomes 8.2 / 11.3 (and 1500 of them: 12.9 / 13.1)
-//   short rows              256 x 1 / 256 x 2 / 512 x 2: 4096 x 1500 f32 19.1 / 13.7 / 18.8, 1024 x 5000 bf16 11.1 / 9.8 / 8.6
-//   many parts              256 x 1 / 256 x 2 / 512 x 2 / 1024 x 2: 512 x 131072 bf16, 1024 earlier ones 108 / 86 / 77 / 74; 256 x 131072 f32, 300
-//                           of them 65.2 / 48.6 / 50.3 / 49.9, 3000 103 / 77 / 61 / 57 (kept by the threads up to 8 each)
-//   few parts               256 x 1 / 512 x 1 / 1024 x 1: 8 x 200003 f16, 32768 earlier ones 18.2 / 14.0 / 12.2
+//   no table     256 x 1 / 256 x 2 / 512 x 2: 256 x 131072 bf16 26.9 / 27.1 / 27.6, f32 46.4 / 48.2 / 48.1; with a bias 29.4 / 29.1 / 29.0
+//   short rows   64 x 1 / 256 x 1 / 256 x 2: 4096 x 500 f32, 50 earlier outcomes 8.8 / 11.0 / 11.2; 256 x 1 / 256 x 2 / 512 x 2: 4096 x 1500 f32
+//                18.1 / 13.0 / 18.1, 1024 x 5000 bf16 9.8 / 8.5 / 8.3
+//   many parts   256 x 1 / 256 x 2 / 512 x 2 / 1024 x 2: 512 x 131072 bf16, 1024 earlier ones 88 / 71 / 66 / 68; 256 x 131072 f32, 300 of them 57.5 /
+//                47.9 / 47.3 / 48.1, 3000 94 / 67 / 55 / 57, bf16 60 / 52 / 33 / 33; 128 x 131072 bf16, 16000 50 / 41 / 34.9 / 35.7
+//   few parts    256 x 1 / 512 x 1 / 1024 x 1: 8 x 200003 f16, 32768 earlier ones 16.7 / 12.8 / 11.5
 template <int KIND, bool BACK> hipError_t launch_all(const AdjustArgs& a, hipStream_t st) {
     const bool table = BACK ? a.n_prior && a.repetition : a.n_prior || a.n_entries;
     const u32 vecs = (a.cols + kPer<KIND> - 1) / kPer<KIND>;
     const bool few = (u64)a.rows * ((vecs + 1023) / 1024) < 512;
-    if (!table) return few ? launch_all<KIND, BACK, 256, 1>(a, table, st) : launch_all<KIND, BACK, 256, 2>(a, table, st);
-    if (vecs <= 64) return launch_all<KIND, BACK, 64, 1>(a, table, st);
-    if (few) return a.n_prior > 8 * 256 ? launch_all<KIND, BACK, 1024, 1>(a, table, st) : launch_all<KIND, BACK, 256, 1>(a, table, st);
-    if (a.n_prior > 8 * 256) return launch_all<KIND, BACK, 1024, 2>(a, table, st);
-    if (vecs <= 256) return launch_all<KIND, BACK, 256, 1>(a, table, st);
-    return vecs <= 512 ? launch_all<KIND, BACK, 256, 2>(a, table, st) : launch_all<KIND, BACK, 512, 2>(a, table, st);
+    if (!table) return few ? launch_all<KIND, BACK, 256, 1, kTableNone>(a, st) : launch_all<KIND, BACK, 256, 2, kTableNone>(a, st);
+    if (vecs <= 128) return launch_table<KIND, BACK, 64, 1>(a, st);
+    if (few) return a.n_prior > 8 * 256 ? launch_table<KIND, BACK, 1024, 1>(a, st) : launch_table<KIND, BACK, 256, 1>(a, st);
+    if (a.n_prior > 8 * 256) return launch_table<KIND, BACK, 1024, 2>(a, st);
+    if (vecs <= 256) return launch_table<KIND, BACK, 256, 1>(a, st);
+    return vecs <= 512 ? launch_table<KIND, BACK, 256, 2>(a, st) : launch_table<KIND, BACK, 512, 2>(a, st);
 }
 
 // In place, 131072 columns: 256 / 1024 threads a row, us: 256 rows, 1000 earlier outcomes 8.9 / 9.3, 2000 13.8 / 11.8, 4000 22.5 / 17.3.  By rows / by
@@ -765,6 +770,14 @@ template <int KIND, bool BACK, int NT> hipError_t launch_over(const AdjustArgs& 
     const size_t lds = bits ? hash_bytes(BACK ? 0 : a.n_entries, bits) : 0;
     if (const hipError_t e = room_for((const void*)&k_adjust_over<KIND, BACK, NT>, lds)) return e;
     hipLaunchKernelGGL((k_adjust_over<KIND, BACK, NT>), grid_of((u64)a.rows * (filled + table) + join_groups(sums)), dim3(NT), lds, st, a, filled, NT * 32, table, bits, fill, sums);
+    return hipGetLastError();
+}
+
+template <int KIND, bool BACK, bool KEPT> hipError_t launch_over_parts(const AdjustArgs& a, u32 width, bool nan, hipStream_t st) {
+    const u32 parts = (a.cols + width - 1) / width;
+    const size_t lds = part_bytes(BACK ? 0 : a.n_entries, part_room(width, a.cols));
+    if (const hipError_t e = room_for((const void*)&k_adjust_over_parts<KIND, BACK, KEPT>, lds)) return e;
+    hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK, KEPT>), grid_of((u64)a.rows * parts), dim3(1024), lds, st, a, parts, width, nan);
     return hipGetLastError();
 }
 
@@ -783,10 +796,8 @@ template <int KIND, bool BACK> hipError_t launch_over(const AdjustArgs& a, bool 
     if (filled + table) e = wide ? launch_over<KIND, BACK, 1024>(a, filled, table, bits, fill, st, sums) : launch_over<KIND, BACK, 256>(a, filled, table, bits, fill, st, sums);
     else if (sums.out) hipLaunchKernelGGL(k_adjust_join, grid_of(join_groups(sums)), dim3(256), 0, st, sums);
     if (e != hipSuccess || !by_parts) return e != hipSuccess ? e : hipGetLastError();
-    const u32 width = eights > 512 ? 16384 : 8192, parts = (a.cols + width - 1) / width;
-    if ((e = room_for((const void*)&k_adjust_over_parts<KIND, BACK>, part_bytes(entries, part_room(width, a.cols)))) != hipSuccess) return e;
-    hipLaunchKernelGGL((k_adjust_over_parts<KIND, BACK>), grid_of((u64)a.rows * parts), dim3(1024), part_bytes(entries, part_room(width, a.cols)), st, a, parts, width, fill && !filled);
-    return hipGetLastError();
+    return a.n_prior <= 4 * kKept * 1024 ? launch_over_parts<KIND, BACK, true>(a, eights > 512 ? 16384 : 8192, fill && !filled, st)
+                                         : launch_over_parts<KIND, BACK, false>(a, eights > 512 ? 16384 : 8192, fill && !filled, st);
 }
 
 template <int KIND> hipError_t launch_forward(const AdjustArgs& a, hipStream_t st) {
