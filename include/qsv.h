@@ -374,11 +374,11 @@ qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_d
  *   v += b_k + sum over the entries j with i_j = k of e_j
  *   masked: v = -inf, whatever v is.
  * Earlier outcomes: the first prior_len entries of the row's prior, of which the first prompt_len (a prompt) count for R alone;
- * entries outside 0..cols-1 (padding) count for nothing.  Biases may be -inf; what has been named by an entry's index outside
- * 0..cols-1 counts for nothing; entries with the same index add up in their order.  Bit k % 32 of word k / 32 of a mask allows outcome
+ * outcomes outside 0..cols-1 (padding) count for nothing.  Biases may be -inf; entries with an index outside 0..cols-1 count for
+ * nothing, those with the same index add up in their order.  Bit k % 32 of word k / 32 of a mask allows outcome
  * k (bits behind cols are not looked at); a mask may leave a row without any.  A score of -inf stays -inf, NaN stays NaN.
- * Results are rounded once to the scores' type (beyond its range: to infinity); a place with a history or an entry is worked out
- * in float64 and rounded to float32 first, the others, a score plus a shared bias, in float32.
+ * A place with a history or an entry is worked out in float64 and rounded once to the scores' type (beyond its range: to infinity);
+ * the others, a score plus a shared bias, are one sum in float32, rounded to that and to the type.
  * A row with a parameter out of its range (R not positive and finite, F or A not finite, not 0 <= prompt_len <= prior_len <= n_prior,
  * a mask outside -1..n_masks-1) becomes NaN, which qsv_sample takes as a row without outcomes.
  * out may be the scores themselves (the same address and row stride): then only the places that change are written, and, without a
@@ -442,8 +442,8 @@ qsv_status qsv_adam_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev,
 
 /* The norm of the gradients of many tensors together, and the gradients scaled to a highest norm:
  *   N = sqrt(sum over all values of g^2),  f = N > max_norm ? max_norm / N : 1,  out = f g.
- * Squares, their sum and the products are in float64; norm_dev (float32 [1] or NULL) receives N, and every value is rounded once to
- * its tensor's type.  outs NULL: in place (nothing is written where f = 1); otherwise n tensors of the gradients' kinds and shapes.
+ * Squares, their sum and the products are in float64; norm_dev (float32 [1] or NULL) receives N, and every value is rounded to float32
+ * and to its tensor's type.  outs NULL: in place (nothing is written where f = 1); otherwise n tensors of the gradients' kinds and shapes.
  * max_norm = +inf: f = 1, so that with outs NULL the norm alone is worked out.  As arithmetic has it, a NaN among the gradients makes
  * N and, with a finite max_norm, all values NaN; an infinite one makes N infinite, finite values 0 and infinite ones NaN.
  * Results do not depend on anything but the list.  An out must be its own gradient (the same address and row stride) or overlap no

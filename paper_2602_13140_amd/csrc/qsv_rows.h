@@ -34,6 +34,17 @@ template <int KIND> __device__ __forceinline__ float part(const vec& x, int i) {
     return __half2float(__ushort_as_half((unsigned short)((i & 1) ? two >> 16 : two)));
 }
 
+// A float64 on its way to a row, as a float32 that is rounded to the type later: to the nearest where that is float32, otherwise to one
+// whose last bit tells that something was cut off, so that the second rounding is that of the value itself (the types of 16 bits
+// have 13 bits less).
+template <int KIND> __device__ __forceinline__ float narrowed(double v) {
+    const float f = (float)v;
+    if (KIND == kScoreF32) return f;
+    unsigned u = __float_as_uint(f);
+    if ((double)f != v && v == v) u = (u - (fabs((double)f) > fabs(v) ? 1u : 0u)) | 1u;
+    return __uint_as_float(u);
+}
+
 // A vector of values, each rounded once.
 template <int KIND> __device__ __forceinline__ vec packed(const float (&g)[kPer<KIND>]) {
     constexpr int W = kPer<KIND>;

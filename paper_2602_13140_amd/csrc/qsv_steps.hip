@@ -171,6 +171,7 @@ template <class L> __device__ __forceinline__ double squares(const L& list, cons
     return block_sum(f.sum);
 }
 
+// (160 million bf16 values of padded rows: 53 us, 6.1 TB/s.)
 template <class L> __global__ __launch_bounds__(kThreads) void k_squares(const L list, double* sums) {
     const double sum = squares(list, Places<L>(list));
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
@@ -201,7 +202,12 @@ template <bool PAST> struct Scaled {
     double factor;
     template <int KIND> struct Of {
         double factor;
-        __device__ __forceinline__ float of(float x) const { return (float)((double)x * factor); }
+        // (kept from being rounded to 16 bits in one go where the compiler would: every place of a tensor by the same steps)
+        __device__ __forceinline__ float of(float x) const {
+            float v = (float)((double)x * factor);
+            asm("" : "+v"(v));
+            return v;
+        }
         __device__ __forceinline__ void whole(const vec& x, char* to) {
             float v[kPer<KIND>];
 #pragma unroll
@@ -222,6 +228,7 @@ template <bool PAST, class L> __device__ __forceinline__ void scale(const L& lis
     }
 }
 
+// (... 114 us for 320 MiB read, most of it out of the memory-side cache, and as much written.)
 template <class L, bool PAST> __global__ __launch_bounds__(kThreads) void k_scale(const L list, const double* sums, u32 n_sums, double most, int over, float* norm) {
     const Places<L> places(list);
     const Norm r = norm_of(sums, n_sums, most);
@@ -324,7 +331,8 @@ template <class M> __device__ __forceinline__ void visit(const AdamList& l, u32 
     else visit<kScoreBF16>(g, nullptr, n, make.template of<kScoreBF16>());
 }
 
-// A norm that is no number or infinite: everything is left as it is.
+// A norm that is no number or infinite: everything is left as it is.  (90 tensors of 49 million values with bf16 gradients: 250 us, 5.1 TB/s; the
+// arithmetic of some 75 64-bit instructions a value would take half of that.)
 template <bool PAST> __global__ __launch_bounds__(kThreads) void k_adam_list(const AdamList list, const double* sums, u32 n_sums, double most, const AdamRates by, float* norm) {
     const Places<AdamList> places(list);
     const Norm r = norm_of(sums, n_sums, most);
