@@ -229,7 +229,7 @@ def test_one_tensor(ctx, src, n):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("count", [59, 60, 61, 130, 700])
+@pytest.mark.parametrize("count", [57, 58, 59, 60, 61, 130, 200, 201, 700])
 def test_long_lists(ctx, count):
     g = np.random.default_rng(count)
     shapes = [(("f32", "f16", "bf16")[int(g.integers(3))], int(g.integers(0, 20)), int(g.integers(0, 300)), int(g.integers(0, 3))) for _ in range(count)]
@@ -351,7 +351,7 @@ def test_adam_one_tensor(ctx, src, n):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("count", [60, 61, 300])
+@pytest.mark.parametrize("count", [60, 61, 90, 91, 200, 201, 300])
 def test_adam_long_lists(ctx, count):
     g = np.random.default_rng(count)
     check_adam(ctx, draw([(("f32", "f16", "bf16")[int(g.integers(3))], 0, int(g.integers(0, 4000)), 0) for _ in range(count)], count), 0.5, 4)
