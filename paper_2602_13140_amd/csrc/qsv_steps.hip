@@ -25,7 +25,7 @@ constexpr u32 kSums = 2048;           // sums of all launches together; rounded 
 constexpr int kKindBit = 56;
 
 // Lists within 4 KiB of arguments: tensors of any rows; rows without a gap, which are one, to be
-// summed up and to be scaled; Adam's.  (Fewer launches: 180 tensors' squares by one instead of two, Adam's step of them 552 -> 542 us.)
+// summed up and to be scaled; Adam's.  (Fewer launches: 192 tensors' squares by one instead of two, Adam's step of them 552 -> 542 us.)
 struct Seg {
     const char* src;
     char* dst;                        // where the scaled gradient goes
@@ -182,7 +182,7 @@ template <class L> __device__ __forceinline__ double squares(const L& list, cons
     return block_sum(f.sum);
 }
 
-// (160 million bf16 values of padded rows: 53 us, 6.1 TB/s.)
+// (160 million bf16 values of padded rows: 56 us, 5.7 TB/s.)
 template <class L> __global__ __launch_bounds__(kThreads) void k_squares(const L list, double* sums) {
     const double sum = squares(list, Places<L>(list));
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
@@ -239,7 +239,7 @@ template <bool PAST, class L> __device__ __forceinline__ void scale(const L& lis
     }
 }
 
-// (... 114 us for 320 MiB read, most of it out of the memory-side cache, and as much written.)
+// (... 109 us for 305 MiB read, most of it out of the memory-side cache, and as much written.)
 template <class L, bool PAST> __global__ __launch_bounds__(kThreads) void k_scale(const L list, const double* sums, u32 n_sums, double most, int over, float* norm) {
     const Places<L> places(list);
     const Norm r = norm_of(sums, n_sums, most);
