@@ -346,52 +346,63 @@ def _adjustment(r, d, rows, prior, prior_len, prompt_len, repetition, frequency,
         r.mask_of_dev = _each(mask_of, i32, d, each, "mask_of")
 
 
-def _kind_of(t):
-    for kind in (QSV_S_F32, QSV_S_F16, QSV_S_BF16):
-        if t.dtype is _dtype(_TYPE_OF[kind]):
-            return kind
-    _need(False, "tensors must be float32, float16 or bfloat16")
+def _kinds():
+    """The kinds of scores by their types."""
+    return {_dtype(_TYPE_OF[kind]): kind for kind in (QSV_S_F32, QSV_S_F16, QSV_S_BF16)}
 
 
 class TensorList:
     """Tensors as qsv_clip_grads takes them, laid out once: contiguous ones of any shape, or rows (of two dimensions) further apart.
-    Holds the tensors."""
+    Holds their memory as it is now: a tensor that is given other memory later (t.data = ...) needs another list."""
 
     def __init__(self, tensors):
-        self.tensors = list(tensors)
-        self.at = (qsv_tensor * max(1, len(self.tensors)))()
-        for e, t in zip(self.at, self.tensors):
-            flat = t.is_contiguous()
-            _need(flat or (t.dim() == 2 and (t.shape[1] < 2 or t.stride(1) == 1) and (t.shape[0] < 2 or t.stride(0) >= t.shape[1])),
-                  "tensors must be contiguous, or rows whose values lie next to each other")
-            e.kind, e.data_dev = _kind_of(t), t.data_ptr() or None
-            e.rows, e.cols = t.shape if t.dim() == 2 else (1, t.numel())
-            e.row_stride = e.cols if flat else t.stride(0)
-        self.devices = {t.get_device() for t in self.tensors}
+        tensors, kinds = list(tensors), _kinds()
+        self.at = (qsv_tensor * max(1, len(tensors)))()
+        for e, t in zip(self.at, tensors):
+            shape = t.shape
+            rows, cols = shape if len(shape) == 2 else (1, t.numel())
+            step = cols
+            if not t.is_contiguous():
+                if len(shape) != 2 or not ((cols < 2 or t.stride(1) == 1) and (rows < 2 or t.stride(0) >= cols)):
+                    _need(False, "tensors must be contiguous, or rows whose values lie next to each other")
+                step = t.stride(0)
+            kind = kinds.get(t.dtype)
+            if kind is None:
+                _need(False, "tensors must be float32, float16 or bfloat16")
+            e.kind, e.data_dev, e.rows, e.cols, e.row_stride = kind, t.data_ptr() or None, rows, cols, step
+        self.held = [t.untyped_storage() for t in tensors]
+        self.devices = {t.get_device() for t in tensors}
 
     def __len__(self):
-        return len(self.tensors)
+        return len(self.held)
 
 
 class AdamList:
-    """Parameters, gradients and moments as qsv_adam_clipped takes them, laid out once.  Holds the tensors."""
+    """Parameters, gradients and moments as qsv_adam_clipped takes them, laid out once.  Holds their memory as it is now, as TensorList."""
 
     def __init__(self, params, grads, m, v):
-        self.tensors = [list(x) for x in (params, grads, m, v)]
-        n = len(self.tensors[0])
-        _need(all(len(x) == n for x in self.tensors), "params, grads, m and v must be as many")
+        lists = [list(x) for x in (params, grads, m, v)]
+        self.n = n = len(lists[0])
+        _need(all(len(x) == n for x in lists), "params, grads, m and v must be as many")
+        kinds, f32 = _kinds(), _dtype("float32")
         self.at = (qsv_adam_tensor * max(1, n))()
-        for e, p, g, a, b in zip(self.at, *self.tensors):
-            for t in (p, a, b):
-                _need(t.dtype is _dtype("float32"), "params, m and v must be float32")
-            for t in (p, g, a, b):
-                _need(t.is_contiguous() and t.shape == p.shape, "params, grads, m and v must be contiguous, of one shape")
-            e.kind, e.count = _kind_of(g), p.numel()
-            e.param_dev, e.grad_dev, e.m_dev, e.v_dev = (t.data_ptr() or None for t in (p, g, a, b))
-        self.devices = {t.get_device() for x in self.tensors for t in x}
+        for e, p, g, a, b in zip(self.at, *lists):
+            if not (p.dtype is f32 and a.dtype is f32 and b.dtype is f32):
+                _need(False, "params, m and v must be float32")
+            shape = p.shape
+            if not (p.is_contiguous() and g.is_contiguous() and a.is_contiguous() and b.is_contiguous()
+                    and g.shape == shape and a.shape == shape and b.shape == shape):
+                _need(False, "params, grads, m and v must be contiguous, of one shape")
+            kind = kinds.get(g.dtype)
+            if kind is None:
+                _need(False, "tensors must be float32, float16 or bfloat16")
+            e.kind, e.count = kind, p.numel()
+            e.param_dev, e.grad_dev, e.m_dev, e.v_dev = p.data_ptr() or None, g.data_ptr() or None, a.data_ptr() or None, b.data_ptr() or None
+        self.held = [t.untyped_storage() for x in lists for t in x]
+        self.devices = {t.get_device() for x in lists for t in x}
 
     def __len__(self):
-        return len(self.tensors[0])
+        return self.n
 
 
 class Context:

@@ -132,6 +132,15 @@ def test_overlaps_against_every_byte(checks):
     assert let > 300
 
 
+def test_lists_hold_the_memory_that_they_name():
+    import torch
+    x = torch.ones(1000)
+    kept, at = (qb.TensorList([x]), qb.AdamList([x], [x], [x], [x])), x.data_ptr()
+    x.data = torch.zeros(1000)
+    assert x.data_ptr() != at and kept[0].at[0].data_dev == at and kept[1].at[0].param_dev == at
+    assert len(kept[0].held) == 1 and len(kept[1].held) == 4 and all(s.data_ptr() == at for k in kept for s in k.held)
+
+
 def test_lists_that_the_binding_refuses():
     import torch
     z = torch.zeros((4, 6))
