@@ -419,7 +419,7 @@ qsv_status qsv_adjust(qsv_ctx* ctx, const qsv_adjust_req* req);
  * the scores' type, rounded once.  grad may be G itself (the same address and row stride; then only the places that change are
  * written, and unless grad_bias_dev is asked for, read), and must not overlap the scores.  Sums over rows are in float64, in an order
  * that the sizes alone decide.  A row with a parameter out of its range gives NaN, in d / d b too.  Any of the results may be
- * NULL.  Workspace: for grad_bias_dev alone, qsv_adjust_grad_workspace_bytes (that of the plans included; 0 on bad arguments). */
+ * NULL; but for grad over G they must not overlap each other or what is read.  Workspace: for grad_bias_dev alone, qsv_adjust_grad_workspace_bytes (that of the plans included; 0 on bad arguments). */
 typedef struct {
     const void* grad_out_dev;     /* G: row r starts at element r * grad_out_stride */
     int64_t grad_out_stride;      /* >= cols (any value for one row) */
@@ -447,7 +447,8 @@ qsv_status qsv_adam_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev,
  * max_norm = +inf: f = 1, so that with outs NULL the norm alone is worked out.  As arithmetic has it, a NaN among the gradients makes
  * N and, with a finite max_norm, all values NaN; an infinite one makes N infinite, finite values 0 and infinite ones NaN.
  * Results do not depend on anything but the list.  An out must be its own gradient (the same address and row stride) or overlap no
- * gradient, and outs must not overlap each other; columns of one buffer (the same row stride, other columns) do not overlap.
+ * gradient, and outs must not overlap each other; columns of one buffer (the same row stride, other columns) do not overlap.  norm_dev
+ * must lie in none of them.
  * The lists are host arrays of 2^38 values at most, read during the call.  No workspace beyond what qsv_workspace_bytes asks for. */
 typedef struct {
     int32_t kind;        /* QSV_S_F32, QSV_S_F16 or QSV_S_BF16 */
@@ -462,7 +463,8 @@ qsv_status qsv_clip_grads(qsv_ctx* ctx, const qsv_tensor* grads, const qsv_tenso
 
 /* qsv_adam_step over many tensors at once, of the gradients times f of qsv_clip_grads (which are read, not written): the values
  * are those of qsv_adam_step on f g.  norm_dev receives N.  Where N is not finite nothing but norm_dev is written: the step is left out.
- * max_norm = +inf: f = 1.  param, m and v of the tensors must not overlap each other or any gradient. */
+ * max_norm = +inf: f = 1.  param, m and v of the tensors must not overlap each other or any gradient, and norm_dev must lie in none
+ * of these. */
 typedef struct {
     int32_t kind;          /* of the gradient: QSV_S_F32, QSV_S_F16 or QSV_S_BF16 */
     int32_t reserved;      /* must be 0 */

@@ -2026,7 +2026,7 @@ qsv_status qsv_adjust_grad(qsv_ctx* ctx, const qsv_adjust_req* req, const qsv_ad
 
 qsv_status qsv_clip_grads(qsv_ctx* ctx, const qsv_tensor* grads, const qsv_tensor* outs, int64_t n, double max_norm, float* norm_dev) {
     if (!ctx) return QSV_ERR_INVALID_ARG;
-    if (const char* why = check_clip(grads, outs, n, max_norm)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    if (const char* why = check_clip(grads, outs, n, max_norm, norm_dev)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
     qsv_status st = bind_device(ctx);
     if (st != QSV_OK) return st;
     Arena ar(ctx);
@@ -2041,7 +2041,7 @@ qsv_status qsv_adam_clipped(qsv_ctx* ctx, const qsv_adam_tensor* tensors, int64_
     if (!ctx) return QSV_ERR_INVALID_ARG;
     if (t < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0))
         return fail(ctx, QSV_ERR_INVALID_ARG, "qsv_adam_clipped: t must be >= 1, beta1 and beta2 in [0, 1), eps positive");
-    if (const char* why = check_adam_list(tensors, n, max_norm)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
+    if (const char* why = check_adam_list(tensors, n, max_norm, norm_dev)) return fail(ctx, QSV_ERR_INVALID_ARG, why);
     qsv_status st = bind_device(ctx);
     if (st != QSV_OK) return st;
     Arena ar(ctx);

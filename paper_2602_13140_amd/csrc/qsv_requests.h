@@ -186,6 +186,15 @@ inline Span span_of(const qsv_tensor& t, int64_t own, bool written) {
     return Span{from, from + ((uint64_t)(t.rows - 1) * stride + (uint64_t)t.cols) * size, (uint64_t)t.cols * size, stride * size, own, written};
 }
 
+// Whether the norm's four bytes meet the rows of a tensor.
+inline bool norm_meets(const Span& s, const float* norm) {
+    const uint64_t at = (uintptr_t)norm;
+    if (!norm || at + 4 <= s.from || at >= s.to) return false;
+    if (at < s.from || s.stride == 0) return true;
+    const uint64_t behind = (at - s.from) % s.stride;
+    return behind < s.width || behind + 4 > s.stride;
+}
+
 inline const char* check_tensor(const qsv_tensor& t) {
     if (t.reserved != 0) return "reserved must be 0";
     if (!score_kind(t.kind)) return "kind must be one of the three types of scores";
@@ -199,7 +208,7 @@ inline const char* check_tensor(const qsv_tensor& t) {
 }
 
 // What is wrong with a request of qsv_clip_grads, or NULL.
-inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, int64_t n, double max_norm) {
+inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, int64_t n, double max_norm, const float* norm = nullptr) {
     if (n < 0 || n > kMostTensors) return "a list has 0..4096 tensors";
     if (n > 0 && !grads) return "grads is NULL";
     if (!(max_norm >= 0.0)) return "max_norm must be >= 0";
@@ -207,10 +216,12 @@ inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, i
     for (int64_t i = 0; i < n; ++i) {
         if (const char* why = check_tensor(grads[i])) return why;
         if ((values += grads[i].rows * grads[i].cols) > kMostValues) return "a list has 2^38 values at most";
+        if (grads[i].rows && grads[i].cols && norm_meets(span_of(grads[i], i, false), norm)) return "norm_dev lies in a tensor";
         if (!outs) continue;
         if (const char* why = check_tensor(outs[i])) return why;
         if (outs[i].kind != grads[i].kind || outs[i].rows != grads[i].rows || outs[i].cols != grads[i].cols)
             return "outs must have the kinds and shapes of the gradients";
+        if (outs[i].rows && outs[i].cols && norm_meets(span_of(outs[i], i, true), norm)) return "norm_dev lies in a tensor";
     }
     if (!outs && max_norm > 1.7976931348623157e308) return nullptr;      // nothing is written
     std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)(outs ? 2 * n : n) + 1]);
@@ -225,7 +236,7 @@ inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, i
 }
 
 // What is wrong with a request of qsv_adam_clipped, or NULL.
-inline const char* check_adam_list(const qsv_adam_tensor* tensors, int64_t n, double max_norm) {
+inline const char* check_adam_list(const qsv_adam_tensor* tensors, int64_t n, double max_norm, const float* norm = nullptr) {
     if (n < 0 || n > kMostTensors) return "a list has 0..4096 tensors";
     if (n > 0 && !tensors) return "tensors is NULL";
     if (!(max_norm >= 0.0)) return "max_norm must be >= 0";
@@ -246,6 +257,7 @@ inline const char* check_adam_list(const qsv_adam_tensor* tensors, int64_t n, do
         for (int k = 0; k < 4; ++k) {
             const uint64_t from = (uintptr_t)at[k], bytes = (uint64_t)t.count * (k < 3 ? 4 : score_bytes(t.kind));
             spans[m++] = Span{from, from + bytes, bytes, 0, i, k < 3};
+            if (norm_meets(spans[m - 1], norm)) return "norm_dev lies in a tensor";
         }
     }
     // (own: a parameter that is its own gradient is refused as well)

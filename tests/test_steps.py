@@ -132,6 +132,26 @@ def test_overlaps_against_every_byte(checks):
     assert let > 300
 
 
+def test_norms_that_lie_in_a_tensor(checks):
+    checks.request_clip_norm.restype = checks.request_adam_norm.restype = ctypes.c_char_p
+    checks.request_clip_norm.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p]
+    checks.request_adam_norm.argtypes = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p]
+    g, o = tensors((0x1000, 3, 5, 8), (0, 0, 4, 4)), tensors((0x2000, 3, 5, 5), (0, 0, 4, 4))
+    rows = {0x1000 + 4 * (8 * r + c) for r in range(3) for c in range(5)}
+    for at in range(0xff0, 0x1070):
+        for norm in (1.0, INF):
+            said = checks.request_clip_norm(g, None, 2, norm, at)
+            assert (said is not None) == any(at < w + 4 and at + 4 > w for w in rows), hex(at)
+    assert checks.request_clip_norm(g, o, 2, 1.0, 0x1ffc) is None and checks.request_clip_norm(g, o, 2, 1.0, 0x203c) is None
+    assert b"norm" in checks.request_clip_norm(g, o, 2, 1.0, 0x2000) and b"norm" in checks.request_clip_norm(g, o, 2, 1.0, 0x2038)
+    a = (qb.qsv_adam_tensor * 1)()
+    a[0].kind, a[0].param_dev, a[0].grad_dev, a[0].m_dev, a[0].v_dev, a[0].count = qb.QSV_S_BF16, 0x1000, 0x2000, 0x3000, 0x4000, 10
+    for at in (0x1000, 0x1024, 0x2000, 0x2010, 0x3024, 0x4000):
+        assert b"norm" in checks.request_adam_norm(a, 1, 1.0, at)
+    for at in (None, 0xffc, 0x1028, 0x2014, 0x3028, 0x4028):
+        assert checks.request_adam_norm(a, 1, 1.0, at) is None
+
+
 def test_lists_hold_the_memory_that_they_name():
     import torch
     x = torch.ones(1000)
