@@ -64,12 +64,12 @@ template <int KIND> __device__ __forceinline__ vec packed(const float (&g)[kPer<
     return x;
 }
 
-template <int KIND> __device__ __forceinline__ vec vec_at(const char* p) {
-    if (KIND == kScoreF32) return *(const vec_at4*)p;
-    return *(const vec_at2*)p;
+// PAST: past the caches.
+template <int KIND, bool PAST = false> __device__ __forceinline__ vec vec_at(const char* p) {
+    if (KIND == kScoreF32) return PAST ? __builtin_nontemporal_load((const vec_at4*)p) : *(const vec_at4*)p;
+    return PAST ? (vec)__builtin_nontemporal_load((const vec_at2*)p) : (vec)*(const vec_at2*)p;
 }
 
-// PAST: past the caches.
 template <int KIND, bool PAST> __device__ __forceinline__ void put_vec(char* p, const vec& x) {
     if (KIND == kScoreF32) {
         if (PAST) __builtin_nontemporal_store(x, (vec_at4*)p);

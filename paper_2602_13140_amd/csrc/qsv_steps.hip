@@ -102,23 +102,23 @@ __device__ __forceinline__ double block_sum(double v) {
 }
 
 // n values next to each other, by a wavefront: whole vectors (with the place their results go to), and single values.
-template <int KIND, class F> __device__ __forceinline__ void visit(const char* src, char* dst, u32 n, F&& f) {
+template <int KIND, class F> __device__ __forceinline__ void visit(const char* src, char* dst, u32 n, const F& f) {
     constexpr u32 W = kPer<KIND>, N = 4;
     const u32 lane = threadIdx.x & 63, whole = n / W;
     u32 j = lane;
     for (; j - lane + N * 64 <= whole; j += N * 64) {
         vec x[N];
 #pragma unroll
-        for (u32 i = 0; i < N; ++i) x[i] = vec_at<KIND>(src + (j + i * 64) * 16);
+        for (u32 i = 0; i < N; ++i) x[i] = vec_at<KIND, F::kPast>(src + (j + i * 64) * 16);
 #pragma unroll
         for (u32 i = 0; i < N; ++i) f.whole(x[i], dst + (j + i * 64) * 16);
     }
-    for (; j < whole; j += 64) f.whole(vec_at<KIND>(src + j * 16), dst + j * 16);
+    for (; j < whole; j += 64) f.whole(vec_at<KIND, F::kPast>(src + j * 16), dst + j * 16);
     const u32 k = whole * W + lane;
     if (k < n) f.one(value_at<KIND>(src, k), dst, k);
 }
 
-template <int KIND, class F> __device__ __forceinline__ void visit(const Seg& s, u32 q, u32 piece, F&& f) {
+template <int KIND, class F> __device__ __forceinline__ void visit(const Seg& s, u32 q, u32 piece, const F& f) {
     constexpr u32 W = kPer<KIND>, S = kSize<KIND>;
     if (s.row_pieces) {
         const u64 row = q / s.row_pieces, c0 = (u64)(q % s.row_pieces) * piece;
@@ -132,7 +132,7 @@ template <int KIND, class F> __device__ __forceinline__ void visit(const Seg& s,
     for (u32 i = lane; i < n; i += 64) {
         const char* src = s.src + (row + r) * s.src_stride;
         char* dst = s.dst + (row + r) * s.dst_stride;
-        if (u * W + W <= cols) f.whole(vec_at<KIND>(src + u * 16), dst + u * 16);
+        if (u * W + W <= cols) f.whole(vec_at<KIND, F::kPast>(src + u * 16), dst + u * 16);
         else
             for (u32 k = u * W; k < cols; ++k) f.one(value_at<KIND>(src, k), dst, k);
         r += dr;
@@ -164,12 +164,13 @@ template <class M> __device__ __forceinline__ void visit(const AdamList& l, u32 
 struct Squares {
     double sum = 0.0;
     template <int KIND> struct Of {
+        static constexpr bool kPast = false;
         double& sum;
-        __device__ __forceinline__ void whole(const vec& x, char*) {
+        __device__ __forceinline__ void whole(const vec& x, char*) const {
 #pragma unroll
             for (int i = 0; i < kPer<KIND>; ++i) one(part<KIND>(x, i), nullptr, 0);
         }
-        __device__ __forceinline__ void one(float x, char*, u32) { sum = fma((double)x, (double)x, sum); }
+        __device__ __forceinline__ void one(float x, char*, u32) const { sum = fma((double)x, (double)x, sum); }
     };
     template <int KIND> __device__ __forceinline__ Of<KIND> of() { return Of<KIND>{sum}; }
 };
@@ -208,10 +209,11 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double* sums, u32 n, fl
     if (threadIdx.x == 0) *norm = (float)r.norm;
 }
 
-// PAST: results go past the caches.
+// PAST: results go past the caches, and the gradients' second reading leaves nothing there.
 template <bool PAST> struct Scaled {
     double factor;
     template <int KIND> struct Of {
+        static constexpr bool kPast = PAST;
         double factor;
         // (kept from being rounded to 16 bits in one go where the compiler would: every place of a tensor by the same steps)
         __device__ __forceinline__ float of(float x) const {
@@ -219,13 +221,13 @@ template <bool PAST> struct Scaled {
             asm("" : "+v"(v));
             return v;
         }
-        __device__ __forceinline__ void whole(const vec& x, char* to) {
+        __device__ __forceinline__ void whole(const vec& x, char* to) const {
             float v[kPer<KIND>];
 #pragma unroll
             for (int i = 0; i < kPer<KIND>; ++i) v[i] = of(part<KIND>(x, i));
             put_vec<KIND, PAST>(to, packed<KIND>(v));
         }
-        __device__ __forceinline__ void one(float x, char* dst, u32 k) { store_one<KIND>(dst, k, of(x)); }
+        __device__ __forceinline__ void one(float x, char* dst, u32 k) const { store_one<KIND>(dst, k, of(x)); }
     };
     template <int KIND> __device__ __forceinline__ Of<KIND> of() { return Of<KIND>{factor}; }
 };
@@ -273,14 +275,15 @@ struct Adam {
 };
 
 // Four gradients from k on.
-template <int KIND> __device__ __forceinline__ void gradients_at(const char* g, u32 k, float (&x)[4]) {
+template <int KIND, bool PAST> __device__ __forceinline__ void gradients_at(const char* g, u32 k, float (&x)[4]) {
     if (KIND == kScoreF32) {
-        const vec q = *(const vec_at4*)(g + (u64)k * 4);
+        const vec q = vec_at<KIND, PAST>(g + (u64)k * 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(q[i]);
     } else {
         typedef u32 two_at2 __attribute__((ext_vector_type(2), aligned(2)));
-        const two_at2 q = *(const two_at2*)(g + (u64)k * 2);
+        const two_at2* from = (const two_at2*)(g + (u64)k * 2);
+        const two_at2 q = PAST ? __builtin_nontemporal_load(from) : *from;
         const vec y = {q[0], q[1], 0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = part<KIND>(y, i);
@@ -299,7 +302,7 @@ template <int KIND, bool PAST> __device__ __forceinline__ void adam_values(float
     const u32 lane = threadIdx.x & 63, whole = n / 4 * 4;
     for (u32 k = lane * 4; k < whole; k += 256) {
         float x[4], a[4], b[4], c[4];
-        gradients_at<KIND>(g, k, x);
+        gradients_at<KIND, PAST>(g, k, x);
         four_at<PAST>(p + k, a);
         four_at<PAST>(m + k, b);
         four_at<PAST>(v + k, c);
@@ -368,7 +371,9 @@ constexpr u32 kFewPieces = 24;
 
 // From so many bytes of results on they go past the caches, which the gradients' second reading has for itself then.  With / without,
 // us: clipping 2 x 4000000 f32 19.6 / 19.3, 2 x 16000000 67 / 80, 2 x 64000000 266 / 292; Adam 2 x 2000000 28.8 / 26.5, 2 x 8000000 95 /
-// 103, 2 x 64000000 746 / 821.  (Clipped gradients of less are read by the step that follows out of the cache.)
+// 103, 2 x 64000000 746 / 821.  (Clipped gradients of less are read by the step that follows out of the cache.)  That second reading goes
+// past them as well: clipping 2 x 64000000 f32 248 / 265, over the gradients 145 / 162, 160 million bf16 values of padded rows 157 / 163, Adam
+// over 104 million parameters with bf16 gradients 534 / 546; the first reading too: 178 and 572.
 constexpr u64 kPastClip = 128ull << 20, kPastStep = 64ull << 20;
 
 struct Clip {
