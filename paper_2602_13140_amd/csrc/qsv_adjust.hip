@@ -635,8 +635,8 @@ template <int KIND, bool BACK, bool KEPT> __global__ __launch_bounds__(1024) voi
 // ---- a bias that all rows share --------------------------------------------------------------------------------------
 // Sums over a block of rows of a tile of columns, a vector of them a lane, and the gradient of the scores on the way (grad, or NULL).
 // A workgroup's wavefronts take every fourth row each and add their sums in order at the end.  OVER: grad lies over
-// grad_out, and vectors without a masked place are left.  Sums are in 64 bits: they cost the kernel nothing.  4096 x 32768 bf16: 104 us, 5.2
-// TB/s, and 7.5 for the join.  Results beside grad_out go past the caches: with it / without, us, 513 x 50021 f16 with histories 38 / 46,
+// grad_out, and vectors without a masked place are left.  Sums are in 64 bits: they cost the kernel nothing.  4096 x 32768 bf16: 105 us, 5.1
+// TB/s, and 7 for the join.  Results beside grad_out go past the caches: with it / without, us, 513 x 50021 f16 with histories 38 / 46,
 // 4096 x 32768 bf16 103 / 108 and with the gradient read once more 155 / 165, 256 x 32768 bf16 12.8 / 14.2 and 21.7 / 22.4, f32 16.1 /
 // 20.8 and 32.1 / 31.5; over grad_out there is no difference.
 constexpr u32 kSumThreads = 256, kSumGroups = 4, kMostSumRows = 256;

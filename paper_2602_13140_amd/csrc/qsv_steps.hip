@@ -241,7 +241,7 @@ template <bool PAST, class L> __device__ __forceinline__ void scale(const L& lis
     }
 }
 
-// (... 109 us for 305 MiB read, most of it out of the memory-side cache, and as much written.)
+// (... 104 us for 305 MiB read, most of it out of the memory-side cache, and as much written.)
 template <class L, bool PAST> __global__ __launch_bounds__(kThreads) void k_scale(const L list, const double* sums, u32 n_sums, double most, int over, float* norm) {
     const Places<L> places(list);
     const Norm r = norm_of(sums, n_sums, most);
