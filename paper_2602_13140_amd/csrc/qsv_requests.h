@@ -235,14 +235,44 @@ inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, i
     return spans_meet(spans.get(), m) ? "a tensor that is written overlaps another one" : nullptr;
 }
 
+// Bytes from .. to - 1; the lowest bit of `from`, an even address, says that they are written.
+struct Flat { uint64_t from, to; };
+
+// Whether something that is written meets something else.  Four lists of n: sorted where they are not (parameters and moments of a
+// program mostly are), and gone through side by side.  (48 tensors 1.7 us, by one sort of all 4.4: as long as a launch.)
+inline bool flats_meet(Flat* s, int64_t n) {
+    auto less = [](const Flat& a, const Flat& b) { return a.from < b.from; };
+    Flat *at[4], *end[4];
+    for (int k = 0; k < 4; ++k) {
+        at[k] = s + k * n;
+        end[k] = at[k] + n;
+        if (!std::is_sorted(at[k], end[k], less)) std::sort(at[k], end[k], less);
+    }
+    uint64_t any = 0, written = 0;      // where what came so far ends
+    for (int64_t i = 0; i < 4 * n; ++i) {
+        int next = -1;
+        for (int k = 0; k < 4; ++k)
+            if (at[k] < end[k] && (next < 0 || at[k]->from < at[next]->from)) next = k;
+        const Flat now = *at[next]++;
+        const uint64_t from = now.from & ~(uint64_t)1;
+        if (from < written || ((now.from & 1) && from < any)) return true;
+        any = std::max(any, now.to);
+        if (now.from & 1) written = std::max(written, now.to);
+    }
+    return false;
+}
+
 // What is wrong with a request of qsv_adam_clipped, or NULL.
 inline const char* check_adam_list(const qsv_adam_tensor* tensors, int64_t n, double max_norm, const float* norm = nullptr) {
     if (n < 0 || n > kMostTensors) return "a list has 0..4096 tensors";
     if (n > 0 && !tensors) return "tensors is NULL";
     if (!(max_norm >= 0.0)) return "max_norm must be >= 0";
-    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)(4 * n) + 1]);
-    if (!spans) return "out of host memory";
+    std::unique_ptr<Flat[]> flats(new (std::nothrow) Flat[(size_t)(4 * n) + 1]);
+    if (!flats) return "out of host memory";
     int64_t m = 0, values = 0;
+    const uint64_t place = (uintptr_t)norm;
+    for (int64_t i = 0; i < n; ++i) m += tensors[i].count > 0;
+    int64_t l = 0;
     for (int64_t i = 0; i < n; ++i) {
         const qsv_adam_tensor& t = tensors[i];
         if (t.reserved != 0) return "reserved must be 0";
@@ -255,14 +285,13 @@ inline const char* check_adam_list(const qsv_adam_tensor* tensors, int64_t n, do
             return "tensors must be aligned to their element";
         const void* at[4] = {t.param_dev, t.m_dev, t.v_dev, t.grad_dev};
         for (int k = 0; k < 4; ++k) {
-            const uint64_t from = (uintptr_t)at[k], bytes = (uint64_t)t.count * (k < 3 ? 4 : score_bytes(t.kind));
-            spans[m++] = Span{from, from + bytes, bytes, 0, i, k < 3};
-            if (norm_meets(spans[m - 1], norm)) return "norm_dev lies in a tensor";
+            const uint64_t from = (uintptr_t)at[k], to = from + (uint64_t)t.count * (k < 3 ? 4 : score_bytes(t.kind));
+            if (norm && place + 4 > from && place < to) return "norm_dev lies in a tensor";
+            flats[k * m + l] = Flat{from | (k < 3 ? 1u : 0u), to};
         }
+        ++l;
     }
-    // (own: a parameter that is its own gradient is refused as well)
-    for (int64_t k = 0; k < m; ++k) spans[k].own = k;
-    return spans_meet(spans.get(), m) ? "a tensor that is written overlaps another one" : nullptr;
+    return flats_meet(flats.get(), m) ? "a tensor that is written overlaps another one" : nullptr;
 }
 
 }  // namespace qsv

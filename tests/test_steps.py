@@ -132,6 +132,30 @@ def test_overlaps_against_every_byte(checks):
     assert let > 300
 
 
+def test_overlaps_of_adam_against_every_byte(checks):
+    """Parameters, moments and gradients at random, in any order: nothing is let through where a written byte comes twice, nothing else refused."""
+    g = np.random.default_rng(2)
+    let = 0
+    for trial in range(4000):
+        n = int(g.integers(1, 5))
+        a = (qb.qsv_adam_tensor * n)()
+        written, read = [], []
+        wide = int(g.choice([20, 200, 2000]))
+        for e in a:
+            e.kind, e.count = int(g.choice([qb.QSV_S_F32, qb.QSV_S_BF16])), int(g.integers(0, 5))
+            size = 4 if e.kind == qb.QSV_S_F32 else 2
+            for name in ("param_dev", "m_dev", "v_dev"):
+                at = 0x1000 + 4 * int(g.integers(0, wide))
+                setattr(e, name, at)
+                written += range(at, at + 4 * e.count)
+            e.grad_dev = 0x1000 + size * int(g.integers(0, wide * 4 // size))
+            read += range(e.grad_dev, e.grad_dev + size * e.count)
+        fine = len(written) == len(set(written)) and not set(written) & set(read)
+        assert (checks.request_adam(a, n, 1.0) is None) == fine, trial
+        let += fine
+    assert 400 < let < 3600
+
+
 def test_norms_that_lie_in_a_tensor(checks):
     checks.request_clip_norm.restype = checks.request_adam_norm.restype = ctypes.c_char_p
     checks.request_clip_norm.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p]
