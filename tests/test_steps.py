@@ -132,6 +132,33 @@ def test_overlaps_against_every_byte(checks):
     assert let > 300
 
 
+def test_overlaps_of_outs_against_every_byte(checks):
+    """Gradients and where they go, at random: nothing is let through where a written word comes twice but for a tensor's own; of single
+    rows nothing else is refused."""
+    g = np.random.default_rng(3)
+    let = own = 0
+    for trial in range(6000):
+        n, wide, stride = int(g.integers(1, 5)), int(g.choice([24, 60, 400])), int(g.integers(4, 9))
+        rows, outs = [], []
+        for _ in range(n):
+            k, m, s = int(g.choice([1, 1, 2, 3])), int(g.integers(1, 4)), stride if g.random() < 0.8 else int(g.integers(4, 9))
+            rows.append((0x1000 + 4 * int(g.integers(0, wide)), k, m, s))
+            outs.append(rows[-1] if g.random() < 0.3 else (0x1000 + 4 * int(g.integers(0, wide)), k, m, stride))
+        said = checks.request_clip(tensors(*rows), tensors(*outs), n, float(g.choice([1.0, INF])))
+        words = lambda t: [t[0] // 4 + r * t[3] + c for r in range(t[1]) for c in range(t[2])]  # noqa: E731
+        to = [w for t in outs for w in words(t)]
+        same = lambda a, b: a[:3] == b[:3] and (a[1] == 1 or a[3] == b[3])                      # noqa: E731
+        fine = len(to) == len(set(to)) and all(not set(words(a)) & set(words(b)) or (i == j and same(a, b))
+                                               for i, a in enumerate(rows) for j, b in enumerate(outs))
+        if said is None:
+            assert fine, trial
+            let += 1
+            own += any(same(a, b) for a, b in zip(rows, outs))
+        elif all(t[1] == 1 for t in rows):
+            assert not fine, trial
+    assert let > 500 and own > 100
+
+
 def test_overlaps_of_adam_against_every_byte(checks):
     """Parameters, moments and gradients at random, in any order: nothing is let through where a written byte comes twice, nothing else refused."""
     g = np.random.default_rng(2)
