@@ -319,6 +319,16 @@ def test_long_lists(ctx, count):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shapes", [[("f32", 3001, 9001, 3), ("bf16", 0, 20000011, 0)] + MIXED, [("f16", 0, 1200001 + i, 0) for i in range(60)] + MIXED],
+                         ids=["rows", "vectors"])
+@pytest.mark.parametrize("most", [0.5, 1e9])
+def test_results_past_the_caches(ctx, shapes, most):
+    grads = draw(shapes, 9)
+    for over in (False, True):
+        check_clip(ctx, grads, most, over)
+
+
+@pytest.mark.gpu
 def test_many_rows_of_few_columns(ctx):
     for shape in (("f32", 300000, 1, 1), ("bf16", 100000, 5, 3), ("f16", 20000, 129, 7), ("f32", 4000, 4097, 3), ("f16", 3000, 4095, 1)):
         check_clip(ctx, draw([shape], 3), 0.5, False)
@@ -428,6 +438,14 @@ def test_adam_one_tensor(ctx, src, n):
     check_adam(ctx, draw([(src, 0, n, 0)], n), 0.5, 3)
     x = draw([(src, 0, n + 3, 0)], n)[0]
     check_adam(ctx, [x[1:n + 1]], 0.25, 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("most", [0.5, INF])
+def test_adam_past_the_caches(ctx, most):
+    shapes = [("f32", 0, 2000003, 0), ("bf16", 0, 2000001, 0), ("f16", 0, 1900003, 0), ("f32", 0, 7, 0)]
+    check_adam(ctx, draw(shapes, 4), most, 3)
+    check_adam(ctx, [x[1:] for x in draw(shapes, 5)], most, 3)
 
 
 @pytest.mark.gpu
