@@ -462,7 +462,8 @@ qsv_status qsv_clip_grads(qsv_ctx* ctx, const qsv_tensor* grads, const qsv_tenso
                           float* norm_dev);
 
 /* qsv_adam_step over many tensors at once, of the gradients times f of qsv_clip_grads (which are read, not written): the values
- * are those of qsv_adam_step on f g.  norm_dev receives N.  Where N is not finite nothing but norm_dev is written: the step is left out.
+ * are those of qsv_adam_step on f g.  norm_dev receives N.  Where N, rounded to float32 as norm_dev has it, is not finite, nothing but
+ * norm_dev is written: the step is left out.
  * max_norm = +inf: f = 1.  param, m and v of the tensors must not overlap each other or any gradient, and norm_dev must lie in none
  * of these. */
 typedef struct {

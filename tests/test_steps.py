@@ -485,6 +485,25 @@ def test_adam_leaves_a_step_out(ctx, bad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n", [1000, 100000], ids=["one launch", "two launches"])
+def test_adam_leaves_a_step_out_by_the_norm_that_it_reports(ctx, n):
+    """Finite gradients of 3e38: their norm is finite in float64 and infinite in float32, which is what a program sees.  One of them alone has a
+    norm of 3e38, and the step is taken."""
+    import torch
+    grads = [torch.full((n,), 3e38, device="cuda"), torch.zeros(77, dtype=torch.bfloat16, device="cuda")]
+    p, m, v = moments(grads, 3)
+    keep = [x.clone() for x in p + m + v]
+    norm = torch.zeros((1,), device="cuda")
+    for most in (1.0, INF):
+        norm.zero_()
+        ctx.qsv_adam_clipped(qb.AdamList(p, grads, m, v), 3, 0.1, most, norm=norm)
+        assert norm.item() == INF and all(torch.equal(x, y) for x, y in zip(p + m + v, keep))
+    grads[0][1:] = 0.0
+    ctx.qsv_adam_clipped(qb.AdamList(p, grads, m, v), 3, 0.1, 1.0, norm=norm)
+    assert norm.item() == grads[0][0].item() and not any(torch.equal(x, y) for x, y in zip(p + m + v, keep))
+
+
+@pytest.mark.gpu
 def test_refused_on_the_device(ctx):
     import torch
     x = torch.zeros(10, device="cuda")
