@@ -380,7 +380,7 @@ qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_d
  * A place with a history or an entry is worked out in float64 and rounded once to the scores' type (beyond its range: to infinity);
  * the others, a score plus a shared bias, are one sum in float32, rounded to that and to the type.
  * A row with a parameter out of its range (R not positive and finite, F or A not finite, not 0 <= prompt_len <= prior_len <= n_prior,
- * a mask outside -1..n_masks-1) becomes NaN, which qsv_sample takes as a row without outcomes.
+ * with n_prior = 0 too, a mask outside -1..n_masks-1) becomes NaN, which qsv_sample takes as a row without outcomes.
  * out may be the scores themselves (the same address and row stride): then only the places that change are written, and, without a
  * shared bias, read; otherwise the two must not overlap.  The other arrays must not overlap out. */
 typedef struct {

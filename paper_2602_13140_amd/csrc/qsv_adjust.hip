@@ -45,8 +45,8 @@ __device__ __forceinline__ Row row_of(const AdjustArgs& a, u64 r) {
     f.by = by;
     f.each = each;
     f.once = once;
-    f.len = a.n_prior && a.prior_len ? len : a.n_prior;
-    f.prompt = a.n_prior ? prompt : 0;
+    f.len = a.prior_len ? len : a.n_prior;
+    f.prompt = prompt;
     f.good = by > 0.f && by < kInf && fabsf(each) < kInf && fabsf(once) < kInf && f.prompt >= 0 && f.prompt <= f.len && f.len <= a.n_prior;
     f.mask = nullptr;
     if (a.masks) {

@@ -460,6 +460,45 @@ def test_rows_with_parameters_out_of_range(ctx, src):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols", [70, 5000])
+def test_lengths_without_a_history(ctx, src, cols):
+    """n_prior = 0: rows that say anything but 0 <= prompt_len <= prior_len <= 0 are out of range, with entries, masks, a shared bias and without."""
+    import torch
+    rows = 7
+    lens, prompts = np.int32([0, 5, 0, -1, 0, 3, 0]), np.int32([0, 0, 1, 0, -1, 3, 0])
+    z, G = draw(src, rows, cols, 14), draw(src, rows, cols, 15)
+    empty = torch.zeros((rows, 0), dtype=torch.int32, device="cuda")
+    for n, (entries, masks, bias) in enumerate([(0, 0, False), (3, 0, False), (0, 2, True), (5, 2, True), (0, 0, True)]):
+        base = settings(rows, cols, n, 0, entries, masks, bias)
+        for given, bad in ((dict(prior_len=lens, prompt_len=prompts), [1, 2, 3, 4, 5]), (dict(prior_len=lens), [1, 3, 5]), (dict(prompt_len=prompts), [2, 4, 5])):
+            q = dict(base, **given)
+            want, big, word = forward(f64(z), base)
+            want[bad] = NAN
+            tol = np.nan_to_num(np.where(word, 2.0 ** -50 * big, U * np.abs(want) if bias and src != "f32" else 0.0), nan=0.0, posinf=0.0)
+            for near in (dev(q), dict(dev(q), prior=empty)):
+                out = torch.full_like(z, 55.0)
+                ctx.qsv_adjust(KIND[src], z, out, **near)
+                close(src, f64(out), want, tol)
+                over = z.clone()
+                ctx.qsv_adjust(KIND[src], over, **near)
+                close(src, f64(over), want, tol)
+                back = {k: v for k, v in near.items() if k not in ("bias", "entry_bias")}
+                wgrad, db, ab, de = backward(f64(z), f64(G), base)
+                wgrad[bad], de[bad] = NAN, NAN
+                db[:] = NAN
+                for over in (False, True):
+                    for with_bias in (False, True):
+                        grad = G.clone() if over else torch.full_like(G, 55.0)
+                        b = torch.zeros(cols, device="cuda") if with_bias else None
+                        e = torch.zeros(base["entry_idx"].shape, device="cuda") if entries else None
+                        ctx.qsv_adjust_grad(KIND[src], grad if over else G, grad=grad, grad_bias=b, grad_entry=e, **back)
+                        close(src, f64(grad), wgrad, np.zeros_like(wgrad))
+                        assert b is None or bool(b.isnan().all())
+                        assert e is None or np.array_equal(f64(e), de, equal_nan=True)
+
+
+@pytest.mark.gpu
 def test_masks_by_row_and_one_for_all(ctx):
     rows, cols = 6, 777
     z, q = draw("bf16", rows, cols, 5), settings(rows, cols, 5, masks=rows)
