@@ -447,7 +447,8 @@ qsv_status qsv_adam_step(qsv_ctx* ctx, float* params_dev, const float* grad_dev,
  * max_norm = +inf: f = 1, so that with outs NULL the norm alone is worked out.  As arithmetic has it, a NaN among the gradients makes
  * N and, with a finite max_norm, all values NaN; an infinite one makes N infinite, finite values 0 and infinite ones NaN.
  * Results do not depend on anything but the list.  An out must be its own gradient (the same address and row stride) or overlap no
- * gradient, and outs must not overlap each other; columns of one buffer (the same row stride, other columns) do not overlap.  norm_dev
+ * gradient, and outs must not overlap each other.  Columns of one buffer do not overlap: rows between each other's are told apart by where
+ * they lie in the greatest common divisor of their row strides (a single row has the other's); rows that meet there are refused.  norm_dev
  * must lie in none of them.
  * The lists are host arrays of 2^38 values at most, read during the call.  No workspace beyond what qsv_workspace_bytes asks for. */
 typedef struct {

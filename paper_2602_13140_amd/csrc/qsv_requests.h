@@ -4,6 +4,7 @@
 #include <cstdint>
 #include <memory>
 #include <new>
+#include <numeric>
 
 #include "qsv.h"
 
@@ -152,11 +153,13 @@ struct Span {                 // bytes; rows of `width` at `stride`
     bool written;
 };
 
-// Columns of one buffer: rows at the same stride that never meet.
+// Rows that lie between each other's, as columns of one buffer do: told apart by where they lie in a period that both strides are multiples
+// of.  (A single row has the other's.  Exact where no two strides of several rows differ: extents that overlap have rows of both in one period.)
 inline bool columns_apart(const Span& a, const Span& b) {      // a.from <= b.from
-    if (a.stride != b.stride || a.stride == 0) return false;
-    const uint64_t behind = (b.from - a.from) % a.stride;
-    return behind >= a.width && behind + b.width <= a.stride;
+    const uint64_t period = std::gcd(a.stride, b.stride);
+    if (period == 0) return false;
+    const uint64_t behind = (b.from - a.from) % period;
+    return behind >= a.width && behind + b.width <= period;
 }
 
 // Whether something that is written meets something else (a tensor's own gradient, the same rows, is let through).

@@ -132,6 +132,31 @@ def test_overlaps_against_every_byte(checks):
     assert let > 300
 
 
+def test_rows_between_other_rows(checks):
+    """A single row beside columns of its buffer (whatever its stride says), rows at a multiple of the others' stride: what is refused is what
+    overlaps, of lists whose rows have one stride."""
+    say = lambda *t: checks.request_clip(tensors(*t), None, len(t), 1.0)  # noqa: E731
+    columns = (0x1000, 5, 6, 16)
+    assert say(columns, (0x1000 + 24, 1, 10, 0)) is None and say(columns, (0x1000 + 24 + 64, 1, 10, 999)) is None
+    assert b"overlap" in say(columns, (0x1000 + 24, 1, 11, 0)) and b"overlap" in say(columns, (0x1000 + 20, 1, 10, 0))
+    assert say((0x1000 + 24, 1, 10, 0), columns, (0x1000 + 24 + 64, 1, 4, 3), (0x1000 + 24 + 64 + 16, 1, 6, 0)) is None
+    assert say(columns, (0x1000 + 24, 3, 10, 32)) is None and b"overlap" in say(columns, (0x1000 + 24, 3, 11, 32))      # every other row of the rest
+    assert say((0x1000, 3, 16, 32), (0x1000 + 64, 1, 16, 16)) is None and say((0x1000, 3, 16, 32), (0x1000 + 64, 2, 16, 32)) is None
+    g = np.random.default_rng(5)
+    let = refused = 0
+    for trial in range(6000):
+        n, stride, wide = int(g.integers(2, 6)), int(g.integers(3, 12)), int(g.choice([20, 60, 150]))
+        rows = []
+        for _ in range(n):
+            k, m = int(g.choice([1, 1, 2, 3, 5])), int(g.integers(1, 4))
+            rows.append((0x1000 + 4 * int(g.integers(0, wide)), k, m, stride if k > 1 else int(g.integers(0, 20))))
+        words = [a // 4 + r * s + c for a, k, m, s in rows for r in range(k) for c in range(m)]
+        fine = len(words) == len(set(words))
+        assert (say(*rows) is None) == fine, (trial, rows)
+        let, refused = let + fine, refused + (not fine)
+    assert let > 1000 and refused > 1000
+
+
 def test_overlaps_of_outs_against_every_byte(checks):
     """Gradients and where they go, at random: nothing is let through where a written word comes twice but for a tensor's own; of single
     rows nothing else is refused."""
