@@ -149,7 +149,6 @@ constexpr int64_t kMostTensors = 4096, kMostValues = (int64_t)1 << 38;
 
 struct Span {                 // bytes; rows of `width` at `stride`
     uint64_t from, to, width, stride;
-    int64_t own;              // the tensor it is of
     bool written;
 };
 
@@ -160,27 +159,6 @@ inline bool columns_apart(const Span& a, const Span& b) {      // a.from <= b.fr
     if (period == 0) return false;
     const uint64_t behind = (b.from - a.from) % period;
     return behind >= a.width && behind + b.width <= period;
-}
-
-// Whether something that is written meets something else (a tensor's own gradient, the same rows, is let through).
-inline bool spans_meet(Span* s, int64_t n) {
-    std::sort(s, s + n, [](const Span& a, const Span& b) { return a.from < b.from; });
-    int64_t open = 0;            // those before i that may reach over it are kept at the front
-    for (int64_t i = 0; i < n; ++i) {
-        const Span now = s[i];
-        int64_t left = 0;
-        for (int64_t j = 0; j < open; ++j) {
-            if (s[j].to <= now.from) continue;
-            s[left++] = s[j];
-            const Span& b = s[left - 1];
-            if (!b.written && !now.written) continue;
-            if (b.own == now.own && b.written != now.written && b.from == now.from && b.to == now.to && b.stride == now.stride) continue;
-            if (!columns_apart(b, now)) return true;
-        }
-        s[left++] = now;
-        open = left;
-    }
-    return false;
 }
 
 // Bytes from .. to - 1; the lowest bit of `from`, an even address, says that they are written.
@@ -206,11 +184,55 @@ template <int LISTS> bool flats_meet(Flat* (&at)[LISTS], Flat* (&end)[LISTS]) {
     }
 }
 
-inline Span span_of(const qsv_tensor& t, int64_t own, bool written) {
+// Whether rows whose extents overlap, sorted by their first bytes, meet where some of them are written: all against all in a common period
+// of their strides, and pair by pair where that says so.
+inline bool rows_meet(const Span* s, int64_t n, Span* open, Flat* room) {
+    uint64_t period = 0;
+    for (int64_t i = 0; i < n; ++i) period = std::gcd(period, s[i].stride);
+    Flat* at[1] = {room};
+    Flat* end[1] = {room};
+    bool fits = period > 0;
+    for (int64_t i = 0; fits && i < n; ++i) {
+        const uint64_t from = (s[i].from - s[0].from) % period, to = from + s[i].width, bit = s[i].written ? 1u : 0u;
+        fits = s[i].width <= period;
+        *end[0]++ = Flat{from | bit, std::min(to, period)};
+        if (to > period) *end[0]++ = Flat{bit, to - period};
+    }
+    if (fits && !flats_meet(at, end)) return false;
+    int64_t before = 0;          // those that may reach over the one that is looked at
+    for (int64_t i = 0; i < n; ++i) {
+        int64_t left = 0;
+        for (int64_t j = 0; j < before; ++j) {
+            if (open[j].to <= s[i].from) continue;
+            open[left++] = open[j];
+            if ((open[j].written || s[i].written) && !columns_apart(open[j], s[i])) return true;
+        }
+        open[left++] = s[i];
+        before = left;
+    }
+    return false;
+}
+
+// Whether something that is written meets something else; `open` has room for n, `room` for 2 n.  (Columns of one buffer, ms of the host, by one
+// period / pair by pair: 512 tensors 0.011 / 0.48, 4096 0.10 / 30.)
+inline bool spans_meet(Span* s, int64_t n, Span* open, Flat* room) {
+    std::sort(s, s + n, [](const Span& a, const Span& b) { return a.from < b.from; });
+    for (int64_t i = 0, j = 0; i < n; i = j) {
+        uint64_t to = s[i].to;
+        for (j = i + 1; j < n && s[j].from < to; ++j) to = std::max(to, s[j].to);
+        if (j - i > 1 && rows_meet(s + i, j - i, open, room)) return true;
+    }
+    return false;
+}
+
+inline Span span_of(const qsv_tensor& t, bool written) {
     const uint64_t size = (uint64_t)score_bytes(t.kind), from = (uintptr_t)t.data_dev;
     const uint64_t stride = t.rows > 1 ? (uint64_t)t.row_stride : 0;
-    return Span{from, from + ((uint64_t)(t.rows - 1) * stride + (uint64_t)t.cols) * size, (uint64_t)t.cols * size, stride * size, own, written};
+    return Span{from, from + ((uint64_t)(t.rows - 1) * stride + (uint64_t)t.cols) * size, (uint64_t)t.cols * size, stride * size, written};
 }
+
+// A gradient and where it goes, the same rows.
+inline bool same_rows(const Span& a, const Span& b) { return a.from == b.from && a.to == b.to && a.stride == b.stride; }
 
 // Whether the norm's four bytes meet the rows of a tensor.
 inline bool norm_meets(const Span& s, const float* norm) {
@@ -243,12 +265,12 @@ inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, i
     for (int64_t i = 0; i < n; ++i) {
         if (const char* why = check_tensor(grads[i])) return why;
         if ((values += grads[i].rows * grads[i].cols) > kMostValues) return "a list has 2^38 values at most";
-        if (grads[i].rows && grads[i].cols && norm_meets(span_of(grads[i], i, false), norm)) return "norm_dev lies in a tensor";
+        if (grads[i].rows && grads[i].cols && norm_meets(span_of(grads[i], false), norm)) return "norm_dev lies in a tensor";
         if (!outs) continue;
         if (const char* why = check_tensor(outs[i])) return why;
         if (outs[i].kind != grads[i].kind || outs[i].rows != grads[i].rows || outs[i].cols != grads[i].cols)
             return "outs must have the kinds and shapes of the gradients";
-        if (outs[i].rows && outs[i].cols && norm_meets(span_of(outs[i], i, true), norm)) return "norm_dev lies in a tensor";
+        if (outs[i].rows && outs[i].cols && norm_meets(span_of(outs[i], true), norm)) return "norm_dev lies in a tensor";
     }
     if (!outs && max_norm > 1.7976931348623157e308) return nullptr;      // nothing is written
     // from first byte to last, as most lists are apart already
@@ -257,26 +279,28 @@ inline const char* check_clip(const qsv_tensor* grads, const qsv_tensor* outs, i
     Flat *at[2] = {flats.get(), flats.get() + n}, *end[2] = {at[0], at[1]};
     for (int64_t i = 0; i < n; ++i) {
         if (grads[i].rows == 0 || grads[i].cols == 0) continue;
-        const Span g = span_of(grads[i], i, false);
+        const Span g = span_of(grads[i], false);
         if (!outs) {
             *end[0]++ = Flat{g.from | 1u, g.to};
             continue;
         }
-        const Span o = span_of(outs[i], i, true);
+        const Span o = span_of(outs[i], true);
         *end[1]++ = Flat{o.from | 1u, o.to};
-        if (o.from != g.from || o.to != g.to || o.stride != g.stride) *end[0]++ = Flat{g.from, g.to};
+        if (!same_rows(g, o)) *end[0]++ = Flat{g.from, g.to};
     }
     if (!flats_meet(at, end)) return nullptr;
     // row by row
-    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)(2 * n) + 1]);
-    if (!spans) return "out of host memory";
+    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)(4 * n) + 1]);
+    std::unique_ptr<Flat[]> room(new (std::nothrow) Flat[(size_t)(4 * n) + 1]);
+    if (!spans || !room) return "out of host memory";
     int64_t m = 0;
     for (int64_t i = 0; i < n; ++i) {
         if (grads[i].rows == 0 || grads[i].cols == 0) continue;
-        spans[m++] = span_of(grads[i], i, !outs);
-        if (outs) spans[m++] = span_of(outs[i], i, true);
+        const Span g = span_of(grads[i], !outs), o = outs ? span_of(outs[i], true) : g;
+        spans[m++] = o;
+        if (!same_rows(g, o)) spans[m++] = g;
     }
-    return spans_meet(spans.get(), m) ? "a tensor that is written overlaps another one" : nullptr;
+    return spans_meet(spans.get(), m, spans.get() + 2 * n, room.get()) ? "a tensor that is written overlaps another one" : nullptr;
 }
 
 // What is wrong with a request of qsv_adam_clipped, or NULL.

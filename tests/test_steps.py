@@ -8,6 +8,7 @@ import math
 import os
 import shutil
 import subprocess
+import time
 
 import numpy as np
 import pytest
@@ -155,6 +156,32 @@ def test_rows_between_other_rows(checks):
         assert (say(*rows) is None) == fine, (trial, rows)
         let, refused = let + fine, refused + (not fine)
     assert let > 1000 and refused > 1000
+
+
+def test_many_columns_of_one_buffer(checks):
+    """A list as long as it may be: what is apart is let through, one word too many is refused, and the time grows with the list, not with its
+    square (64 times from 512 tensors to 4096, against 11 of a sort)."""
+    def columns(n, wide=4, over=-1, base=0x1000):
+        return tensors(*[(base + 4 * wide * i, 8, wide + (i == over), wide * n) for i in range(n)])
+
+    def best(grads, outs):
+        took = INF
+        for _ in range(5):
+            start = time.perf_counter()
+            assert checks.request_clip(grads, outs, len(grads), 1.0) is None
+            took = min(took, time.perf_counter() - start)
+        return took
+    for outs in (None, 0x1000, 0x10000000):
+        few, many = (best(columns(n), outs and columns(n, base=outs)) for n in (512, 4096))
+        assert many < 24 * few, (few, many)
+    for over in (0, 17, 4094):
+        assert b"overlap" in checks.request_clip(columns(4096, over=over), None, 4096, 1.0)
+    assert checks.request_clip(columns(4096, over=4095), None, 4096, 1.0) is not None       # into the next row of the first
+    # blocks of a buffer, and a row that reaches from one into the next
+    blocks = [(0x1000 + 4 * (64 * 8 * 6 * j + 6 * i), 8, 6, 64 * 6) for j in range(8) for i in range(64)]
+    assert checks.request_clip(tensors(*blocks), None, 512, 1.0) is None
+    for i in (0, 100, 447):
+        assert b"overlap" in checks.request_clip(tensors(*[(b[0], b[1] + (k == i)) + b[2:] for k, b in enumerate(blocks)]), None, 512, 1.0)
 
 
 def test_overlaps_of_outs_against_every_byte(checks):
