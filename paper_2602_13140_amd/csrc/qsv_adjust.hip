@@ -752,6 +752,9 @@ template <int KIND, bool BACK, int NT, int NV> hipError_t launch_table(const Adj
 
 // Threads and vectors a thread by row length, history and how many workgroups that makes, us:
 //   no table     256 x 1 / 256 x 2 / 512 x 2: 256 x 131072 bf16 26.9 / 27.1 / 27.6, f32 46.4 / 48.2 / 48.1; with a bias 29.4 / 29.1 / 29.0
+//   up to 128 vectors  64 x 1 / 256 x 1 / 1024 x 1: 8 x 500 f32, 50 earlier outcomes 4.0 / 4.0 / 4.7, 300 4.9 / 3.9 / 4.7, 4000 7.8 / 5.5 / 5.4, 32768
+//                40 / 19.1 / 18.6; 4096 x 500 f32, 50 8.8 / 10.8 / 32, 300 10.7 / 10.9 / 32, 1000 19.3 / 12.4 / 32, 4000 56 / 31 / 41; 1024 x 70 f16,
+//                50 4.8 / 5.4 / 10.6, 1000 7.3 / 5.7 / 10.8, 4000 17.1 / 17.1 / 11.9
 //   short rows   64 x 1 / 256 x 1 / 256 x 2: 4096 x 500 f32, 50 earlier outcomes 8.8 / 11.0 / 11.2; 256 x 1 / 256 x 2 / 512 x 2: 4096 x 1500 f32
 //                18.1 / 13.0 / 18.1, 1024 x 5000 bf16 9.8 / 8.5 / 8.3
 //   many parts   256 x 1 / 256 x 2 / 512 x 2 / 1024 x 2: 512 x 131072 bf16, 1024 earlier ones 88 / 71 / 66 / 68; 256 x 131072 f32, 300 of them 57.5 /
@@ -762,8 +765,9 @@ template <int KIND, bool BACK> hipError_t launch_all(const AdjustArgs& a, hipStr
     const u32 vecs = (a.cols + kPer<KIND> - 1) / kPer<KIND>;
     const bool few = (u64)a.rows * ((vecs + 1023) / 1024) < 512;
     if (!table) return few ? launch_all<KIND, BACK, 256, 1, kTableNone>(a, st) : launch_all<KIND, BACK, 256, 2, kTableNone>(a, st);
-    if (vecs <= 128) return launch_table<KIND, BACK, 64, 1>(a, st);
+    if (vecs <= 128 && a.n_prior <= 4 * 64) return launch_table<KIND, BACK, 64, 1>(a, st);
     if (few) return a.n_prior > 8 * 256 ? launch_table<KIND, BACK, 1024, 1>(a, st) : launch_table<KIND, BACK, 256, 1>(a, st);
+    if (vecs <= 128) return launch_table<KIND, BACK, 256, 1>(a, st);
     if (a.n_prior > 8 * 256) return launch_table<KIND, BACK, 1024, 2>(a, st);
     if (vecs <= 256) return launch_table<KIND, BACK, 256, 1>(a, st);
     return vecs <= 512 ? launch_table<KIND, BACK, 256, 2>(a, st) : launch_table<KIND, BACK, 512, 2>(a, st);

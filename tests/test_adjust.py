@@ -406,6 +406,22 @@ def test_every_way_through(ctx, src, rows, cols, prior, entries):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src,rows,cols", [("f32", 5, 500), ("f16", 4, 70), ("bf16", 3, 1024), ("f32", 3, 3), ("bf16", 520, 33)])
+@pytest.mark.parametrize("prior", [255, 256, 257, 2047, 2048, 2049, 20000])
+def test_short_rows_with_long_histories(ctx, src, rows, cols, prior):
+    """More earlier outcomes than columns: with the threads that keep them and the passes that do not, few rows and many."""
+    if rows > 5 and prior > 2049:
+        prior = 3000
+    z, q = draw(src, rows, cols, rows + prior), settings(rows, cols, prior, prior, 6, 2, rows % 2 == 1)
+    G = draw(src, rows, cols, rows + 3, sigma=0.2)
+    check_forward(ctx, src, z, q, pad=1)
+    check_backward(ctx, src, z, G, q, bias=False)
+    if rows <= 5:
+        check_forward(ctx, src, z, dict(q, bias=None), over=True)
+        check_backward(ctx, src, z, G, q, over=True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("cols", [50, 9000])
 def test_values_at_the_ends_of_the_type(ctx, src, cols):
