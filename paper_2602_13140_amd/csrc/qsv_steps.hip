@@ -372,8 +372,10 @@ constexpr u32 kFewPieces = 24;
 // From so many bytes of results on they go past the caches, which the gradients' second reading has for itself then.  With / without,
 // us: clipping 2 x 4000000 f32 19.6 / 19.3, 2 x 16000000 67 / 80, 2 x 64000000 266 / 292; Adam 2 x 2000000 28.8 / 26.5, 2 x 8000000 95 /
 // 103, 2 x 64000000 746 / 821.  (Clipped gradients of less are read by the step that follows out of the cache.)  That second reading goes
-// past them as well: clipping 2 x 64000000 f32 248 / 265, over the gradients 145 / 162, 160 million bf16 values of padded rows 157 / 163, Adam
-// over 104 million parameters with bf16 gradients 534 / 546; the first reading too: 178 and 572.
+// past them as well: clipping 2 x 64000000 f32 252 / 268, 160 million bf16 values of padded rows 157 / 163, Adam over 104 million parameters with
+// bf16 gradients 534 / 546; the first reading too: 178 and 572.  Over the gradients (three lists in turn, each above the highest norm at every
+// call) the two together, with / without: 2 x 8000000 f32 41 / 35, 2 x 17500000 73 / 86, 2 x 32000000 125 / 149, 2 x 64000000 254 / 305; and with the
+// results read behind it 343 / 378.
 constexpr u64 kPastClip = 128ull << 20, kPastStep = 64ull << 20;
 
 struct Clip {
