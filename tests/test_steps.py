@@ -88,6 +88,33 @@ def test_refusals_of_clipping(checks):
     assert qb.load().qsv_clip_grads(None, two, None, 2, 1.0, None) == qb.QSV_ERR_INVALID_ARG
 
 
+def test_refusals_of_destinations(checks):
+    """Of outs that have their gradients' kind and shape: what is wrong with an address, a stride or a field is said, also behind a good one and
+    where nothing would be scaled."""
+    def say(grad, out, norm=1.0, reserved=0):
+        good = (0x40000, 1, 100, 0), (0x50000, 1, 100, 0)
+        outs = tensors(good[1], out)
+        outs[1].reserved = reserved
+        return checks.request_clip(tensors(good[0], grad), outs, 2, norm)
+    for norm in (0.0, 1.0, INF):
+        for kind, size in ((qb.QSV_S_F32, 4), (qb.QSV_S_F16, 2), (qb.QSV_S_BF16, 2)):
+            vector, rows = (0x1000, 1, 100, 0, kind), (0x1000, 4, 10, 12, kind)
+            assert say(vector, (0x9000, 1, 100, 0, kind), norm) is None and say(rows, (0x9000, 4, 10, 10, kind), norm) is None
+            for grad in (vector, rows):
+                shape = grad[1:4] + (kind,)
+                assert b"data_dev is NULL" in say(grad, (None,) + shape, norm)
+                for off in range(1, size):
+                    assert b"data_dev must be aligned" in say(grad, (0x9000 + off,) + shape, norm)
+                assert b"reserved must be 0" in say(grad, (0x9000,) + shape, norm, reserved=1)
+            for stride in (-1, 0, 9, (1 << 38) + 1):
+                assert b"row_stride must be in" in say(rows, (0x9000, 4, 10, stride, kind), norm)
+            for shape in ((1, 99, 0), (2, 50, 50), (100, 1, 1), (1, 101, 0)):
+                assert b"shapes" in say(vector, (0x9000,) + shape + (kind,), norm)
+            assert b"shapes" in say(vector, (0x9000, 1, 100, 0, qb.QSV_S_F16 if size == 4 else qb.QSV_S_F32), norm)
+            assert b"kind must be one" in say(vector, (0x9000, 1, 100, 0, 4), norm)
+            assert b"rows and cols" in say(vector, (0x9000, -1, 100, 0, kind), norm)
+
+
 def test_refusals_of_adam(checks):
     def lists(*rows):
         a = (qb.qsv_adam_tensor * max(1, len(rows)))()
