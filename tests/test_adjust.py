@@ -139,6 +139,67 @@ def settings(rows, cols, seed, prior=0, entries=0, masks=0, bias=False):
     return q
 
 
+def forward_all(z, q):
+    """forward, of all rows at once; its allowed places too."""
+    rows, cols = z.shape
+    get = lambda k, d: np.full(rows, d) if q.get(k) is None else q[k].astype(np.float64)  # noqa: E731
+    by, each, once = get("repetition", 1.0), get("frequency", 0.0), get("presence", 0.0)
+    good = (by > 0) & (by < INF) & (np.abs(each) < INF) & (np.abs(once) < INF)
+    s, c, e, word = np.zeros(z.shape, bool), np.zeros(z.shape), np.zeros(z.shape), np.zeros(z.shape, bool)
+    at = lambda k, on: np.flatnonzero(on) // k.shape[1] * cols + k[on]  # noqa: E731
+    if q.get("prior") is not None:
+        prior, place = q["prior"].astype(np.int64), np.arange(q["prior"].shape[1])
+        length, prompt = get("prior_len", float(len(place))), get("prompt_len", 0.0)
+        good &= (prompt >= 0) & (prompt <= length) & (length <= len(place))
+        real = (prior >= 0) & (prior < cols) & (place < length[:, None])
+        s.flat[at(prior, real)] = True
+        c += np.bincount(at(prior, real & (place >= prompt[:, None])), minlength=z.size).reshape(z.shape)
+        word |= s
+    if q.get("entry_idx") is not None:
+        idx = q["entry_idx"].astype(np.int64)
+        real = (idx >= 0) & (idx < cols)
+        e += np.bincount(at(idx, real), weights=q["entry_bias"][real].astype(np.float64), minlength=z.size).reshape(z.shape)
+        word.flat[at(idx, real)] = True
+    a = np.ones(z.shape, bool)
+    if q.get("masks") is not None:
+        bits = np.unpackbits(q["masks"].view(np.uint8), axis=1, bitorder="little")[:, :cols] == 1
+        a = bits[q["mask_of"]] | (q["mask_of"] < 0)[:, None]
+    b = np.zeros(cols) if q.get("bias") is None else q["bias"].astype(np.float64)
+    with np.errstate(divide="ignore"):
+        v = np.where(s, np.where(z > 0, z / by[:, None], z * by[:, None]), z)
+    less = each[:, None] * c + once[:, None] * (c > 0)
+    most = np.abs(each)[:, None] * c + np.abs(once)[:, None]
+    big = np.max([np.abs(v), np.abs(z), most, np.broadcast_to(np.abs(b), z.shape), np.abs(e)], axis=0)
+    v = np.where(a, v - less + b + e, -INF)
+    return np.where(good[:, None], v, NAN), big, word, s, a, good
+
+
+def backward_all(z, G, q):
+    """backward, of all rows at once and without the entries."""
+    _, _, _, s, a, good = forward_all(z, q)
+    by = (np.ones(len(z)) if q.get("repetition") is None else q["repetition"].astype(np.float64))[:, None]
+    g = np.where(good[:, None], np.where(a, G, 0.0), NAN)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        return np.where(s & a, np.where(z > 0, g / by, g * by), g), g.sum(0), np.abs(g).sum(0)
+
+
+def test_all_rows_at_once_as_one_by_one():
+    g = np.random.default_rng(4)
+    for seed, (rows, cols, prior, entries, masks, bias) in enumerate([(9, 40, 30, 6, 4, True), (5, 3, 9, 0, 2, False), (7, 70, 0, 5, 0, True), (6, 33, 12, 0, 3, False)]):
+        z, G, q = g.standard_normal((rows, cols)) * 3, g.standard_normal((rows, cols)), settings(rows, cols, seed, prior, entries, masks, bias)
+        if prior:
+            q["prompt_len"][1], q["repetition"][2] = q["prior_len"][1] + 1, -1.0
+        v, big, word = forward(z, q)
+        got = forward_all(z, q)
+        ok = got[5]
+        assert (~ok).sum() == (2 if prior else 0) and np.allclose(got[0], v, rtol=1e-14, atol=1e-14, equal_nan=True)
+        assert np.array_equal(got[2][ok], word[ok]) and np.allclose(got[1][ok], big[ok], rtol=1e-14)
+        grad, db, ab = backward_all(z, G, q)
+        want = backward(z, G, q)
+        assert np.allclose(grad, want[0], rtol=1e-14, equal_nan=True) and np.allclose(db, want[1], rtol=1e-14, atol=1e-13, equal_nan=True)
+        assert not ok.all() or np.allclose(ab, want[2], rtol=1e-14, atol=1e-13)
+
+
 def test_gradients_against_differences():
     g = np.random.default_rng(3)
     rows, cols, h = 4, 9, 1e-6
@@ -512,6 +573,94 @@ def test_lengths_without_a_history(ctx, src, cols):
                         close(src, f64(grad), wgrad, np.zeros_like(wgrad))
                         assert b is None or bool(b.isnan().all())
                         assert e is None or np.array_equal(f64(e), de, equal_nan=True)
+
+
+def check_all(ctx, src, z, G, q):
+    """Both directions, beside and in place, with and without the shared bias' gradient, without the entries' gradients."""
+    import torch
+    want, big, word, *_ = forward_all(f64(z), q)
+    near = dev(q)
+    out = torch.full_like(z, 55.0)
+    ctx.qsv_adjust(KIND[src], z, out, **near)
+    tol = np.where(word, 2.0 ** -50 * big, U * np.abs(want) if q.get("bias") is not None and src != "f32" else 0.0)
+    close(src, f64(out), want, np.nan_to_num(tol, nan=0.0, posinf=0.0))
+    want, big, word, *_ = forward_all(f64(z), dict(q, bias=None))
+    over = z.clone()
+    ctx.qsv_adjust(KIND[src], over, **{k: v for k, v in near.items() if k != "bias"})
+    close(src, f64(over), want, np.where(word & ~np.isnan(want), 2.0 ** -50 * big, 0.0))
+    back = {k: v for k, v in near.items() if k not in ("bias", "entry_bias")}
+    want, db, ab = backward_all(f64(z), f64(G), q)
+    for over in (False, True):
+        for bias in (False, True):
+            grad = G.clone() if over else torch.full_like(G, 55.0)
+            b = torch.full((z.shape[1],), 77.0, device="cuda") if bias else None
+            ctx.qsv_adjust_grad(KIND[src], grad if over else G, grad=grad, scores=z, grad_bias=b, **back)
+            close(src, f64(grad), want, np.where(np.isnan(want), 0.0, 2.0 ** -50 * np.abs(want)))
+            # sums of n values in float64, in any order: off by n 2^-53 of the absolute sum at most, and one rounding
+            if bias:
+                assert ((np.abs(f64(b) - db) <= U * np.abs(db) + len(z) * 2.0 ** -53 * 2.0 * ab + 2.0 ** -149) | (np.isnan(f64(b)) & np.isnan(db))).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,prior,entries", [(4225, 70, 12, 0), (5000, 70, 12, 3), (5000, 33, 0, 0), (40000, 70, 12, 3), (40000, 9, 300, 0), (1100003, 3, 3, 1)])
+def test_many_rows(ctx, src, rows, cols, prior, entries):
+    """Blocks of 33 to 256 rows of the shared bias' sums, the last one short; more workgroups than one dimension of a grid holds."""
+    c = ctx
+    if qb.qsv_adjust_grad_workspace_bytes(rows, cols) > ctx.ws.numel():
+        c = qb.Context(1, 1, ws_bytes=qb.qsv_adjust_grad_workspace_bytes(rows, cols))
+    z, G = draw(src, rows, cols, rows), draw(src, rows, cols, rows + 1, sigma=0.2)
+    q = settings(rows, cols, rows + cols, prior, entries, 5, True)
+    check_all(c, src, z, G, q)
+    if prior:
+        q["prompt_len"][rows // 2], q["repetition"][rows - 1] = -1, 0.0      # the sums of all columns become NaN
+        check_all(c, src, z, G, q)
+    if c is not ctx:
+        c.close()
+
+
+@pytest.mark.gpu
+def test_sums_of_columns_over_two_dimensions_of_workgroups():
+    """4096 rows of more than four million columns: whole numbers, whose sums are exact."""
+    import torch
+    rows, cols = 4096, (1 << 22) + 517            # 128 blocks of 32 rows, 8194 tiles of 512 columns
+    assert rows // 32 * -(-cols // 512) > 1 << 20
+    c = qb.Context(1, 1, ws_bytes=qb.qsv_adjust_grad_workspace_bytes(rows, cols))
+    k = torch.arange(cols, device="cuda", dtype=torch.int32)
+    G = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    want = torch.zeros(cols, dtype=torch.int64, device="cuda")
+    for r in range(rows):
+        row = (k * (2 * (r % 7) + 1) + r) % 11 - 5
+        G[r] = row
+        want += row
+    words = torch.randint(-2 ** 31, 2 ** 31, (1, (cols + 31) // 32), device="cuda", dtype=torch.int64, generator=torch.Generator("cuda").manual_seed(1)).to(torch.int32)
+    allowed = (words.view(-1, 1) >> torch.arange(32, device="cuda", dtype=torch.int32) & 1).flatten()[:cols]
+    b = torch.full((cols,), 77.0, device="cuda")
+    c.qsv_adjust_grad(KIND["bf16"], G, grad_bias=b, masks=words)
+    assert torch.equal(b, (want * allowed).float())
+    b.fill_(77.0)
+    c.qsv_adjust_grad(KIND["bf16"], G, grad=G, grad_bias=b, masks=words)
+    assert torch.equal(b, (want * allowed).float())
+    for r in (0, 31, 32, 2049, rows - 1):
+        assert torch.equal(G[r].int(), ((k * (2 * (r % 7) + 1) + r) % 11 - 5) * allowed)
+    c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(2, 300), (2, 9001)])
+def test_longest_histories(ctx, src, rows, cols):
+    """2^20 earlier outcomes, all of them one outcome or each at random: counts of 21 bits."""
+    n = 1 << 20
+    q = settings(rows, cols, 6, prior=n, entries=2, masks=2)
+    q["prior"][0], q["prior_len"][0], q["prompt_len"][0] = 7, n, 0
+    q["frequency"][:], q["presence"][:], q["repetition"][:] = np.float32(2.0 ** -12), 0.5, 1.25
+    q["mask_of"][:] = -1
+    z, G = draw(src, rows, cols, 17), draw(src, rows, cols, 18)
+    z[0, 7] = 2.0
+    check_all(ctx, src, z, G, q)
+    q["prompt_len"][0] = n
+    check_all(ctx, src, z, G, q)
 
 
 @pytest.mark.gpu
