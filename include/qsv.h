@@ -456,7 +456,7 @@ typedef struct {
     int32_t reserved;    /* must be 0 */
     void* data_dev;      /* row r starts at element r * row_stride; aligned to its element; may be NULL where it has no values */
     int64_t rows, cols;  /* >= 0 */
-    int64_t row_stride;  /* >= cols (any value for one row), in elements, <= 2^38 */
+    int64_t row_stride;  /* >= cols (any value for one row), in elements, <= 2^38; (rows - 1) * row_stride <= 2^56 */
 } qsv_tensor;
 
 qsv_status qsv_clip_grads(qsv_ctx* ctx, const qsv_tensor* grads, const qsv_tensor* outs, int64_t n /* 0..4096 */, double max_norm /* >= 0 */,

@@ -145,7 +145,7 @@ inline const char* check_adjust_grad(const qsv_adjust_req* q, const qsv_adjust_g
 }
 
 // ---- lists of tensors ------------------------------------------------------------------------------------------------
-constexpr int64_t kMostTensors = 4096, kMostValues = (int64_t)1 << 38;
+constexpr int64_t kMostTensors = 4096, kMostValues = (int64_t)1 << 38, kMostReach = (int64_t)1 << 56;
 
 struct Span {                 // bytes; rows of `width` at `stride`
     uint64_t from, to, width, stride;
@@ -253,6 +253,8 @@ inline const char* check_tensor(const qsv_tensor& t) {
     if (!t.data_dev) return "data_dev is NULL";
     if ((uintptr_t)t.data_dev & (score_bytes(t.kind) - 1)) return "data_dev must be aligned to its element";
     if (t.rows > 1 && (t.row_stride < t.cols || t.row_stride > kMostValues)) return "row_stride must be in cols..2^38";
+    int64_t last = 0;      // so that addresses and extents do not wrap around
+    if (t.rows > 1 && (__builtin_mul_overflow(t.rows - 1, t.row_stride, &last) || last > kMostReach)) return "a tensor's last row must start within 2^56 elements";
     return nullptr;
 }
 

@@ -185,6 +185,16 @@ def test_rows_between_other_rows(checks):
     assert let > 1000 and refused > 1000
 
 
+def test_rows_that_would_wrap_around(checks):
+    """Extents that 64 bits do not hold would pass as small ones, and what they cover as free."""
+    say = lambda *t: checks.request_clip(tensors(*t), None, len(t), 1.0)  # noqa: E731
+    for rows, stride in (((1 << 26) + 1, 1 << 38), ((1 << 38), 1 << 38), ((1 << 36) + 1, 1 << 26), ((1 << 18) + 2, 1 << 38)):
+        assert b"2^56" in say((0x1000, rows, 1, stride)), (rows, stride)
+        assert b"2^56" in say((0x1000, rows, 1, stride), (0x1000 + 4 * stride, 1, 1, 0))
+    assert say((0x1000, (1 << 18) + 1, 1, 1 << 38)) is None and say((0x1000, 1 << 38, 1, 1)) is None
+    assert b"overlap" in say((0x1000, (1 << 18) + 1, 1, 1 << 38), (0x1000 + (1 << 58), 1, 1, 0))
+
+
 def test_many_columns_of_one_buffer(checks):
     """A list as long as it may be: what is apart is let through, one word too many is refused, and the time grows with the list, not with its
     square (64 times from 512 tensors to 4096, against 11 of a sort)."""
