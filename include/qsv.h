@@ -367,7 +367,8 @@ qsv_status qsv_distill_grad(qsv_ctx* ctx, const qsv_circuit* c, const float* x_d
                             const float* params_dev, const float* feats_dev, const qsv_teacher* teacher,
                             float* loss_dev, float* grad_dev, float* mean_loss_dev, float* mean_grad_dev);
 
-/* Penalties for repeated outcomes, biases and masks on rows of scores, before a draw (qsv_sample) or a loss (qsv_distill):
+/* Penalties for repeated outcomes, biases and masks on rows of scores (alone: probabilities and amplitudes have a norm to keep), before a
+ * draw (qsv_sample) or a loss (qsv_distill):
  *   v = z
  *   s_k:  v = v > 0 ? v / R : v R           s_k: outcome k is among the row's earlier outcomes that count
  *   v -= F c_k + A [c_k > 0]                c_k: how often it is among those from prompt_len on
