@@ -424,6 +424,33 @@ def test_many_rows_of_few_columns(ctx):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(7, 24), (300, 1031), (40, 9001)])
+def test_tensors_of_one_buffer(ctx, src, rows, cols):
+    """Columns, single rows between them and every other row of the rest, in place and into such places of another buffer: what lies between
+    them is left as it is."""
+    import torch
+    a, b = cols // 3 - 1, cols // 2 + 1
+    parts = lambda x: [x[:, :a], x[0, a:b], x[1::2, a:b], x[2::4, a:b], x[:, b + 1:cols - 1], x[rows - 1, cols - 1:]]  # noqa: E731
+    buffer = draw([(src, rows, cols, 0)], rows)[0]
+    grads, lone = parts(buffer), torch.ones_like(buffer, dtype=torch.bool)
+    for x in parts(lone):
+        x.fill_(False)
+    n, before = norm_of(grads), f64(buffer)
+    assert 0 < int(lone.sum()) < buffer.numel()
+    norm, t = torch.zeros((1,), device="cuda"), torch.finfo(buffer.dtype)
+    for most in (n / 2.5, 2 * n):
+        f, other, over = min(1.0, most / n), torch.full_like(buffer, 55.0), buffer.clone()
+        ctx.qsv_clip_grads(parts(buffer), most, norm=norm, out=parts(other))
+        ctx.qsv_clip_grads(parts(over), most)
+        assert abs(norm.item() - n) <= n * 1.5 * U and np.array_equal(f64(buffer), before)
+        assert bool((other[lone] == 55.0).all()) and torch.equal(over[lone], buffer[lone]) and torch.equal(over[~lone], other[~lone])
+        want = (before * f)[~lone.cpu().numpy()]
+        half = np.maximum(t.eps / 2 * np.abs(want), t.smallest_normal * t.eps / 2)
+        assert (np.abs(f64(over[~lone]) - want) <= (half + U * np.abs(want)) * (1 + t.eps)).all()
+
+
+@pytest.mark.gpu
 def test_empty_lists_and_tensors(ctx):
     import torch
     norm = torch.full((1,), 9.0, device="cuda")
